@@ -132,7 +132,8 @@ enum {
     ONES_ERR_WORKSPACE = -5,  /* workspace too small for this population / job count */
     ONES_ERR_CUDA = -6,       /* a CUDA call failed; see ones_last_cuda_error */
     ONES_ERR_INFEASIBLE = -7, /* repair could not reach the capacity */
-    ONES_ERR_NOMEM = -8       /* host allocation failed */
+    ONES_ERR_NOMEM = -8,      /* host allocation failed */
+    ONES_ERR_TIMEOUT = -9     /* a kernel gave up waiting (ones_train.h) */
 };
 
 /* Bytes of device workspace needed for up to n_jobs_max jobs and a population of

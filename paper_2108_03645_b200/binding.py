@@ -26,7 +26,7 @@ MAX_ELITES = 256
 
 ERRORS = {0: "ONES_OK", -1: "ONES_ERR_NULL", -2: "ONES_ERR_BAD_JOB", -3: "ONES_ERR_BAD_PARAM",
           -4: "ONES_ERR_ALIGN", -5: "ONES_ERR_WORKSPACE", -6: "ONES_ERR_CUDA", -7: "ONES_ERR_INFEASIBLE",
-          -8: "ONES_ERR_NOMEM"}
+          -8: "ONES_ERR_NOMEM", -9: "ONES_ERR_TIMEOUT"}
 
 
 class OnesError(RuntimeError):

@@ -35,7 +35,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     nvcc = os.environ.get("NVCC", "nvcc")
     tmp = LIB + f".tmp{os.getpid()}"
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-Xcompiler", "-fPIC,-Wall,-Wextra", "-shared", "-I", INCLUDE, "-I", CSRC, "-o", tmp]
+           "-Xcompiler", "-fPIC,-Wall,-Wextra", "-shared", "--threads", "0", "-I", INCLUDE, "-I", CSRC, "-o", tmp]
     if verbose:
         cmd += ["-Xptxas", "-v"]
     cmd += sources()

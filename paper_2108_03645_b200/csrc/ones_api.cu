@@ -1113,6 +1113,7 @@ const char* ones_strerror(int code) {
         case ONES_ERR_CUDA: return "a CUDA call failed";
         case ONES_ERR_INFEASIBLE: return "repair could not reach the capacity";
         case ONES_ERR_NOMEM: return "host allocation failed";
+        case ONES_ERR_TIMEOUT: return "a kernel gave up waiting";
         default: return "unknown error code";
     }
 }

@@ -1,0 +1,344 @@
+// The matrix product of the training-step operators: C = A * B^T on 16-bit operands with 32-bit accumulators, where
+// what happens to C is a policy (`Epi`), so that a softmax statistic, a gradient of the logits or a polynomial of the
+// product leaves the kernel instead of the product itself.
+//
+// One persistent CTA per SM (CG = 1: tiles of 128 x 128) or pair of CTAs (CG = 2: tiles of 256 x 256, each CTA holds
+// 128 rows of A and 128 rows of B, and both tensor cores work on one tile). A ring of kStages boxes of 64 values
+// along K is filled by TMA (one thread), consumed by tcgen05.mma (one thread), and two accumulators in tensor memory
+// let the 8 epilogue warps work on one tile while the next one is multiplied. A thread of the epilogue owns one row.
+//
+// A operand is read as rows x K with K contiguous, or (AMN / BMN) as K x rows with the rows contiguous, straight from
+// the caller's layout: nothing is transposed beforehand. Sizes need not be multiples of anything: TMA fills what lies
+// outside a matrix with zeros, and epilogues skip rows and columns outside C.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <atomic>
+
+#include "ones_mma.cuh"
+
+namespace ones {
+
+constexpr int kTileK = 64;       // values along K per stage: one 128-byte swizzle row
+constexpr int kStages = 6;
+constexpr int kHalf = 128 * kTileK * 2;  // bytes of one operand's box(es) per stage and CTA
+constexpr int kStageBytes = 2 * kHalf;
+constexpr int kEpiWarps = 8;
+constexpr int kMatThreads = 128 + 32 * kEpiWarps;
+constexpr int kMatSmem = kStages * kStageBytes + 1024;
+
+// Set when a wait inside a kernel of this translation unit ran out of time.
+static __device__ unsigned g_wait_expired;
+
+struct MatShape {
+    int M, N, K;
+    int tiles_m, tiles_n, batch;
+    int sym;    // only tiles on and above the diagonal are computed (C is symmetric)
+    int group;  // row tiles that run through the columns together, so that both operands' tiles are met again in L2
+    uint32_t idesc;
+};
+
+struct TileAt {
+    int b, m, n;
+};
+
+__device__ __forceinline__ int tiles_per_matrix(const MatShape& g) {
+    return g.sym ? g.tiles_m * (g.tiles_m + 1) / 2 : g.tiles_m * g.tiles_n;
+}
+
+__device__ __forceinline__ TileAt tile_at(const MatShape& g, int t, int per) {
+    TileAt r;
+    r.b = t / per;
+    int p = t - r.b * per;
+    if (g.sym) {
+        int i = 0;
+        while (p >= g.tiles_m - i) {
+            p -= g.tiles_m - i;
+            ++i;
+        }
+        r.m = i;
+        r.n = i + p;
+    } else {
+        const int block = g.group * g.tiles_n, k = p / block, first = k * g.group;
+        const int rows = min(g.tiles_m - first, g.group);
+        p -= k * block;
+        r.n = p / rows;
+        r.m = first + (p - r.n * rows);
+    }
+    return r;
+}
+
+template <int CG, bool AMN, bool BMN, class Epi>
+__global__ void __launch_bounds__(kMatThreads, 1)
+    k_matmul(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MatShape g,
+             const typename Epi::Args ea) {
+    constexpr int BN = 128 * CG;          // columns of a tile
+    constexpr uint32_t kCols = 2 * BN;    // tensor-memory columns: two accumulators
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_done[2], s_free[2];
+    __shared__ uint32_t s_tmem;
+
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t full = smem_u32(s_full), empty = smem_u32(s_empty), done = smem_u32(s_done), free_ = smem_u32(s_free);
+
+    if (threadIdx.x == 0) {
+        tma_prefetch(&map_a);
+        tma_prefetch(&map_b);
+        for (int i = 0; i < kStages; ++i) {
+            bar_init(full + 8 * i, 1);
+            bar_init(empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(done + 8 * i, 1);
+            bar_init(free_ + 8 * i, kEpiWarps * CG);
+        }
+        bar_init_done();
+    }
+    if (warp == 2) tmem_alloc<CG>(smem_u32(&s_tmem), kCols);
+    mma_fence_before();
+    __syncthreads();
+    if constexpr (CG == 2) cluster_sync_all();
+    mma_fence_after();
+    const uint32_t tmem = s_tmem;
+
+    wait_for_predecessor();
+    let_successor_start();
+
+    const int per = tiles_per_matrix(g), total = per * g.batch;
+    const int first = blockIdx.x / CG, step = gridDim.x / CG;
+    const int nk = (g.K + kTileK - 1) / kTileK;
+    bool ok = true;
+
+    if (warp == 0 && lane == 0) {
+        // fill the ring
+        const uint32_t full_at = CG == 2 ? map_to_rank(full, 0) : full;  // the pair's bytes are counted on CTA 0's barrier
+        int s = 0;
+        uint32_t ph = 0;
+        for (int t = first; ok && t < total; t += step) {
+            const TileAt at = tile_at(g, t, per);
+            const int am = at.m * 128 * CG + (int)rank * 128, bn = at.n * BN + (int)rank * 128;
+            for (int k = 0; k < nk; ++k) {
+                if (!(ok = bar_wait(empty + 8 * s, ph ^ 1, &g_wait_expired))) break;
+                if (rank == 0) bar_expect(full + 8 * s, CG * kStageBytes);
+                const uint32_t a = base + s * kStageBytes, b = a + kHalf, bar = full_at + 8 * s;
+                if constexpr (AMN) {
+                    tma_load<CG>(a, &map_a, am, k * kTileK, at.b, bar);
+                    tma_load<CG>(a + kHalf / 2, &map_a, am + 64, k * kTileK, at.b, bar);
+                } else {
+                    tma_load<CG>(a, &map_a, k * kTileK, am, at.b, bar);
+                }
+                if constexpr (BMN) {
+                    tma_load<CG>(b, &map_b, bn, k * kTileK, at.b, bar);
+                    tma_load<CG>(b + kHalf / 2, &map_b, bn + 64, k * kTileK, at.b, bar);
+                } else {
+                    tma_load<CG>(b, &map_b, k * kTileK, bn, at.b, bar);
+                }
+                if (++s == kStages) s = 0, ph ^= 1;
+            }
+        }
+    } else if (warp == 1 && lane == 0 && rank == 0) {
+        // multiply
+        int s = 0, acc = 0;
+        uint32_t ph = 0, aph = 0;
+        constexpr uint64_t step_a = (AMN ? 2048 : 32) >> 4, step_b = (BMN ? 2048 : 32) >> 4;  // 16 values along K
+        for (int t = first; ok && t < total; t += step) {
+            if (!(ok = bar_wait(free_ + 8 * acc, aph ^ 1, &g_wait_expired))) break;
+            mma_fence_after();
+            for (int k = 0; k < nk; ++k) {
+                if (!(ok = bar_wait(full + 8 * s, ph, &g_wait_expired))) break;
+                mma_fence_after();
+                uint64_t a = operand_desc(base + s * kStageBytes, AMN, kHalf / 2);
+                uint64_t b = operand_desc(base + s * kStageBytes + kHalf, BMN, kHalf / 2);
+#pragma unroll
+                for (int i = 0; i < kTileK / 16; ++i) {
+                    mma_f16<CG>(tmem + acc * BN, a, b, g.idesc, (k | i) != 0);
+                    a += step_a;
+                    b += step_b;
+                }
+                mma_commit<CG>(empty + 8 * s);
+                if (++s == kStages) s = 0, ph ^= 1;
+            }
+            if (ok) mma_commit<CG>(done + 8 * acc);
+            if (++acc == 2) acc = 0, aph ^= 1;
+        }
+    } else if (warp >= 4) {
+        // hand the accumulators on
+        const int quad = warp % 4, half = (warp - 4) / 4;
+        const uint32_t free_at = CG == 2 ? map_to_rank(free_, 0) : free_;
+        int acc = 0;
+        uint32_t aph = 0;
+        for (int t = first; t < total; t += step) {
+            const TileAt at = tile_at(g, t, per);
+            ok = bar_wait(done + 8 * acc, aph, &g_wait_expired);
+            if (!__all_sync(0xFFFFFFFFu, ok)) break;
+            mma_fence_after();
+            const int row = at.m * 128 * CG + (int)rank * 128 + quad * 32 + lane;
+            const int col = at.n * BN + half * (BN / 2);
+            Epi::template tile<BN / 2>(ea, g, tmem + acc * BN + half * (BN / 2) + ((uint32_t)quad << 21), row, col, at, half);
+            mma_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if constexpr (CG == 2)
+                    bar_arrive_cluster(free_at + 8 * acc);
+                else
+                    bar_arrive(free_ + 8 * acc);
+            }
+            if (++acc == 2) acc = 0, aph ^= 1;
+        }
+        ok = ok || lane != 0;
+    }
+    // After a wait that ran out, copies and products may still be on their way: give them time before their memory goes.
+    if (!ok) {
+        const uint64_t begin = now_ns();
+        while (now_ns() - begin < 10000000ull) __nanosleep(1000);
+    }
+    __syncwarp();
+    mma_fence_before();
+    __syncthreads();
+    if constexpr (CG == 2) cluster_sync_all();
+    mma_fence_after();
+    if (warp == 2) tmem_free<CG>(tmem, kCols);
+    if constexpr (CG == 2) cluster_sync_all();  // neither CTA leaves while the other still gives its half back
+}
+
+// ---- what epilogues share ----
+
+struct Half16 {  // two 16-bit values of the run-time type, in one word
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi, bool f16) {
+        if (f16) {
+            __half2 h = __floats2half2_rn(lo, hi);
+            return *reinterpret_cast<uint32_t*>(&h);
+        }
+        __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<uint32_t*>(&h);
+    }
+};
+
+__device__ __forceinline__ uint16_t to16(float v, bool f16) {
+    if (f16) return __half_as_ushort(__float2half_rn(v));
+    return __bfloat16_as_ushort(__float2bfloat16_rn(v));
+}
+
+// 32 values of one row as 16 bits, from column `col` of a row of `n` columns. `wide`: rows start on 16-byte boundaries.
+__device__ __forceinline__ void store_row16(uint16_t* row, int col, int n, const float (&v)[32], bool f16, bool wide) {
+    if (wide && col + 32 <= n) {
+        uint4* p = reinterpret_cast<uint4*>(row + col);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            p[i] = make_uint4(Half16::pack(v[8 * i], v[8 * i + 1], f16), Half16::pack(v[8 * i + 2], v[8 * i + 3], f16),
+                              Half16::pack(v[8 * i + 4], v[8 * i + 5], f16), Half16::pack(v[8 * i + 6], v[8 * i + 7], f16));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (col + i < n) row[col + i] = to16(v[i], f16);
+    }
+}
+
+__device__ __forceinline__ void store_row32(float* row, int col, int n, const float (&v)[32], bool wide) {
+    if (wide && col + 32 <= n) {
+        float4* p = reinterpret_cast<float4*>(row + col);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (col + i < n) row[col + i] = v[i];
+    }
+}
+
+// ---- host side ----
+
+struct Operand {
+    const void* p;
+    int64_t ld;       // values between two rows as they lie in memory
+    int64_t batch_ld; // values between two matrices
+    bool mn;          // memory rows run along K, and hold the operand's rows (M or N)
+};
+
+cudaError_t make_map(CUtensorMap* out, const Operand& o, int rows, int k, int batch, bool f16);
+
+inline uint32_t instruction_desc(int cg, bool f16, bool amn, bool bmn) {
+    const uint32_t type = f16 ? 0u : 1u;
+    return (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)amn << 15) | ((uint32_t)bmn << 16) |
+           ((uint32_t)(128 * cg / 8) << 17) | ((uint32_t)(128 * cg / 16) << 24);
+}
+
+int device_sms();  // of the current device; 148 where that cannot be asked
+
+constexpr int kSms = 148;  // the launch rules below reckon with a B200's SMs, so that workspace sizes need no device
+
+// Pairs of CTAs and 256 x 256 tiles run the tensor cores faster, 128 x 128 tiles leave fewer SMs idle. A tile of the
+// pair keeps it busy for two units of time, a small tile its SM for `kSmallCost`: the smaller number of waves times cost wins.
+constexpr double kSmallCost = 1.3;
+
+inline bool use_pairs(int M, int N, int batch, bool sym) {
+    auto tiles = [&](int b) {
+        const int64_t m = (M + b - 1) / b, n = (N + b - 1) / b;
+        return (sym ? m * (m + 1) / 2 : m * n) * batch;
+    };
+    const int64_t big = (tiles(256) + kSms / 2 - 1) / (kSms / 2), small = (tiles(128) + kSms - 1) / kSms;
+    return 2.0 * big <= kSmallCost * small;
+}
+
+template <int CG, bool AMN, bool BMN, class Epi>
+cudaError_t launch_matmul_cg(const Operand& a, const Operand& b, MatShape g, bool f16, const typename Epi::Args& ea,
+                             cudaStream_t stream, bool dependent) {
+    CUtensorMap ma, mb;
+    cudaError_t err = make_map(&ma, a, g.M, g.K, g.batch, f16);
+    if (err == cudaSuccess) err = make_map(&mb, b, g.N, g.K, g.batch, f16);
+    if (err != cudaSuccess) return err;
+    g.tiles_m = (g.M + 128 * CG - 1) / (128 * CG);
+    g.tiles_n = (g.N + 128 * CG - 1) / (128 * CG);
+    g.group = 8 * (CG == 1 ? 2 : 1);
+    g.idesc = instruction_desc(CG, f16, AMN, BMN);
+    const int64_t per = g.sym ? (int64_t)g.tiles_m * (g.tiles_m + 1) / 2 : (int64_t)g.tiles_m * g.tiles_n;
+    const int64_t slots = device_sms() / CG, total = per * g.batch;
+    if (total > 0x7FFFFFFF) return cudaErrorInvalidValue;
+    auto kernel = k_matmul<CG, AMN, BMN, Epi>;
+    static std::atomic<uint64_t> ready{0};  // devices on which the kernel may use this much shared memory
+    int dev = 0;
+    err = cudaGetDevice(&dev);
+    if (err != cudaSuccess) return err;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (!(ready.load(std::memory_order_relaxed) & bit)) {
+        err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMatSmem);
+        if (err != cudaSuccess) return err;
+        ready.fetch_or(bit, std::memory_order_relaxed);
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((total < slots ? total : slots) * CG));
+    cfg.blockDim = dim3(kMatThreads);
+    cfg.dynamicSmemBytes = kMatSmem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    int n = 0;
+    if (CG == 2) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = 2;
+        attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    if (dependent) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = n;
+    return cudaLaunchKernelEx(&cfg, kernel, ma, mb, g, ea);
+}
+
+// `dependent`: the launch before this one on the stream is one of this call's, and the kernel may be set up beside its tail.
+template <bool AMN, bool BMN, class Epi>
+cudaError_t launch_matmul(const Operand& a, const Operand& b, int M, int N, int K, int batch, bool sym, bool f16,
+                          const typename Epi::Args& ea, cudaStream_t stream, bool dependent) {
+    MatShape g = {};
+    g.M = M, g.N = N, g.K = K, g.batch = batch, g.sym = sym;
+    return use_pairs(M, N, batch, sym) ? launch_matmul_cg<2, AMN, BMN, Epi>(a, b, g, f16, ea, stream, dependent)
+                                       : launch_matmul_cg<1, AMN, BMN, Epi>(a, b, g, f16, ea, stream, dependent);
+}
+
+}  // namespace ones
