@@ -17,6 +17,7 @@
 #include <atomic>
 
 #include "ones_mma.cuh"
+#include "ones_train_internal.h"
 
 namespace ones {
 
@@ -26,7 +27,8 @@ constexpr int kHalf = 128 * kTileK * 2;  // bytes of one operand's box(es) per s
 constexpr int kStageBytes = 2 * kHalf;
 constexpr int kEpiWarps = 8;
 constexpr int kMatThreads = 128 + 32 * kEpiWarps;
-constexpr int kMatSmem = kStages * kStageBytes + 1024;
+constexpr int kEpiBytes = 32 * 128;  // what a warp of the epilogue has to turn rows round: 32 rows of 128 bytes
+constexpr int kMatSmem = kStages * kStageBytes + kEpiWarps * kEpiBytes + 1024;
 
 // Set when a wait inside a kernel of this translation unit ran out of time.
 static __device__ unsigned g_wait_expired;
@@ -68,6 +70,102 @@ __device__ __forceinline__ TileAt tile_at(const MatShape& g, int t, int per) {
     }
     return r;
 }
+
+// ---- what epilogues share ----
+
+struct Half16 {  // two 16-bit values of the run-time type, in one word
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi, bool f16) {
+        if (f16) {
+            __half2 h = __floats2half2_rn(lo, hi);
+            return *reinterpret_cast<uint32_t*>(&h);
+        }
+        __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<uint32_t*>(&h);
+    }
+};
+
+// A thread has 128 bytes of one row; stored like that, a warp's store would touch 32 rows at once. They go through
+// shared memory instead, the 16-byte chunks of a row permuted by the row so that neither side meets a bank twice, and
+// leave with 8 lanes on one row.
+struct Turn {
+    uint8_t* at;  // 32 rows of 128 bytes, this warp's own
+    int lane;
+
+    __device__ __forceinline__ uint4& chunk(int row, int c) const {
+        return *reinterpret_cast<uint4*>(at + row * 128 + ((c ^ (row & 7)) << 4));
+    }
+    __device__ __forceinline__ void put16(const float (&v)[64], bool f16) const {
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+            chunk(lane, c) = make_uint4(Half16::pack(v[8 * c], v[8 * c + 1], f16), Half16::pack(v[8 * c + 2], v[8 * c + 3], f16),
+                                        Half16::pack(v[8 * c + 4], v[8 * c + 5], f16), Half16::pack(v[8 * c + 6], v[8 * c + 7], f16));
+        __syncwarp();
+    }
+    __device__ __forceinline__ void put32(const float (&v)[32]) const {
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+            chunk(lane, c) = make_uint4(__float_as_uint(v[4 * c]), __float_as_uint(v[4 * c + 1]), __float_as_uint(v[4 * c + 2]),
+                                        __float_as_uint(v[4 * c + 3]));
+        __syncwarp();
+    }
+    // One 16-bit / 32-bit value of what was put.
+    __device__ __forceinline__ uint16_t half_at(int row, int c) const {
+        return *reinterpret_cast<const uint16_t*>(at + row * 128 + (((c >> 3) ^ (row & 7)) << 4) + (c & 7) * 2);
+    }
+    __device__ __forceinline__ float word_at(int row, int c) const {
+        return *reinterpret_cast<const float*>(at + row * 128 + (((c >> 2) ^ (row & 7)) << 4) + (c & 3) * 4);
+    }
+
+    // The 64 x 16-bit (32 x 32-bit) columns from `col` of rows row0..row0+31, as far as they lie inside rows x cols, to
+    // `out` (row 0's first value). wide: rows start on 16-byte boundaries; otherwise single values, a row at a time.
+    __device__ __forceinline__ void store16(uint16_t* out, int64_t ld, int row0, int col, int rows, int cols, bool wide) const {
+        if (wide) {
+            const int c = lane & 7, left = cols - (col + 8 * c);
+            uint16_t* p = out + (int64_t)(row0 + lane / 8) * ld + col + 8 * c;
+#pragma unroll
+            for (int i = 0; i < 8; ++i, p += 4 * ld) {
+                const int r = 4 * i + lane / 8;
+                const uint4 q = chunk(r, c);
+                if (row0 + r >= rows || left <= 0) continue;
+                if (left >= 8) {
+                    *reinterpret_cast<uint4*>(p) = q;
+                } else {
+                    for (int j = 0; j < left; ++j) p[j] = half_at(r, 8 * c + j);
+                }
+            }
+        } else {
+            const int n = min(32, rows - row0);
+            for (int r = 0; r < n; ++r) {
+                uint16_t* p = out + (int64_t)(row0 + r) * ld + col;
+                if (col + lane < cols) p[lane] = half_at(r, lane);
+                if (col + 32 + lane < cols) p[32 + lane] = half_at(r, 32 + lane);
+            }
+        }
+    }
+    __device__ __forceinline__ void store32(float* out, int64_t ld, int row0, int col, int rows, int cols, bool wide) const {
+        if (wide) {
+            const int c = lane & 7, left = cols - (col + 4 * c);
+            float* p = out + (int64_t)(row0 + lane / 8) * ld + col + 4 * c;
+#pragma unroll
+            for (int i = 0; i < 8; ++i, p += 4 * ld) {
+                const int r = 4 * i + lane / 8;
+                const uint4 q = chunk(r, c);
+                if (row0 + r >= rows || left <= 0) continue;
+                if (left >= 4) {
+                    *reinterpret_cast<uint4*>(p) = q;
+                } else {
+                    for (int j = 0; j < left; ++j) p[j] = word_at(r, 4 * c + j);
+                }
+            }
+        } else {
+            const int n = min(32, rows - row0);
+            for (int r = 0; r < n; ++r)
+                if (col + lane < cols) out[(int64_t)(row0 + r) * ld + col + lane] = word_at(r, lane);
+        }
+    }
+};
 
 template <int CG, bool AMN, bool BMN, class Epi>
 __global__ void __launch_bounds__(kMatThreads, 1)
@@ -167,6 +265,7 @@ __global__ void __launch_bounds__(kMatThreads, 1)
     } else if (warp >= 4) {
         // hand the accumulators on
         const int quad = warp % 4, half = (warp - 4) / 4;
+        const Turn turn = {smem_raw + (base - smem_u32(smem_raw)) + kStages * kStageBytes + (warp - 4) * kEpiBytes, lane};
         const uint32_t free_at = CG == 2 ? map_to_rank(free_, 0) : free_;
         int acc = 0;
         uint32_t aph = 0;
@@ -177,7 +276,7 @@ __global__ void __launch_bounds__(kMatThreads, 1)
             mma_fence_after();
             const int row = at.m * 128 * CG + (int)rank * 128 + quad * 32 + lane;
             const int col = at.n * BN + half * (BN / 2);
-            Epi::template tile<BN / 2>(ea, g, tmem + acc * BN + half * (BN / 2) + ((uint32_t)quad << 21), row, col, at, half);
+            Epi::template tile<BN / 2>(ea, g, tmem + acc * BN + half * (BN / 2) + ((uint32_t)quad << 21), row, col, at, half, turn);
             mma_fence_before();
             __syncwarp();
             if (lane == 0) {
@@ -190,11 +289,7 @@ __global__ void __launch_bounds__(kMatThreads, 1)
         }
         ok = ok || lane != 0;
     }
-    // After a wait that ran out, copies and products may still be on their way: give them time before their memory goes.
-    if (!ok) {
-        const uint64_t begin = now_ns();
-        while (now_ns() - begin < 10000000ull) __nanosleep(1000);
-    }
+    if (!ok) let_copies_end();
     __syncwarp();
     mma_fence_before();
     __syncthreads();
@@ -202,51 +297,6 @@ __global__ void __launch_bounds__(kMatThreads, 1)
     mma_fence_after();
     if (warp == 2) tmem_free<CG>(tmem, kCols);
     if constexpr (CG == 2) cluster_sync_all();  // neither CTA leaves while the other still gives its half back
-}
-
-// ---- what epilogues share ----
-
-struct Half16 {  // two 16-bit values of the run-time type, in one word
-    static __device__ __forceinline__ uint32_t pack(float lo, float hi, bool f16) {
-        if (f16) {
-            __half2 h = __floats2half2_rn(lo, hi);
-            return *reinterpret_cast<uint32_t*>(&h);
-        }
-        __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-        return *reinterpret_cast<uint32_t*>(&h);
-    }
-};
-
-__device__ __forceinline__ uint16_t to16(float v, bool f16) {
-    if (f16) return __half_as_ushort(__float2half_rn(v));
-    return __bfloat16_as_ushort(__float2bfloat16_rn(v));
-}
-
-// 32 values of one row as 16 bits, from column `col` of a row of `n` columns. `wide`: rows start on 16-byte boundaries.
-__device__ __forceinline__ void store_row16(uint16_t* row, int col, int n, const float (&v)[32], bool f16, bool wide) {
-    if (wide && col + 32 <= n) {
-        uint4* p = reinterpret_cast<uint4*>(row + col);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            p[i] = make_uint4(Half16::pack(v[8 * i], v[8 * i + 1], f16), Half16::pack(v[8 * i + 2], v[8 * i + 3], f16),
-                              Half16::pack(v[8 * i + 4], v[8 * i + 5], f16), Half16::pack(v[8 * i + 6], v[8 * i + 7], f16));
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (col + i < n) row[col + i] = to16(v[i], f16);
-    }
-}
-
-__device__ __forceinline__ void store_row32(float* row, int col, int n, const float (&v)[32], bool wide) {
-    if (wide && col + 32 <= n) {
-        float4* p = reinterpret_cast<float4*>(row + col);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (col + i < n) row[col + i] = v[i];
-    }
 }
 
 // ---- host side ----
@@ -298,16 +348,9 @@ cudaError_t launch_matmul_cg(const Operand& a, const Operand& b, MatShape g, boo
     const int64_t slots = device_sms() / CG, total = per * g.batch;
     if (total > 0x7FFFFFFF) return cudaErrorInvalidValue;
     auto kernel = k_matmul<CG, AMN, BMN, Epi>;
-    static std::atomic<uint64_t> ready{0};  // devices on which the kernel may use this much shared memory
-    int dev = 0;
-    err = cudaGetDevice(&dev);
+    static std::atomic<uint64_t> ready{0};
+    err = allow_smem(kernel, kMatSmem, ready);
     if (err != cudaSuccess) return err;
-    const uint64_t bit = 1ull << (dev & 63);
-    if (!(ready.load(std::memory_order_relaxed) & bit)) {
-        err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMatSmem);
-        if (err != cudaSuccess) return err;
-        ready.fetch_or(bit, std::memory_order_relaxed);
-    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((total < slots ? total : slots) * CG));
     cfg.blockDim = dim3(kMatThreads);

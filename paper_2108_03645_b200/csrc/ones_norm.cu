@@ -3,6 +3,9 @@
 #include <cuda_fp16.h>
 #include <math.h>
 
+#include <atomic>
+#include <type_traits>
+
 #include "ones_mma.cuh"
 #include "ones_train.h"
 #include "ones_train_internal.h"
@@ -30,6 +33,77 @@ struct alignas(sizeof(T) * V) Pack {
     T v[V];
 };
 
+// Two 32-bit values that go through one instruction.
+struct Pair {
+    unsigned long long v;
+};
+__device__ __forceinline__ Pair pair(float lo, float hi) {
+    Pair r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ Pair both(float x) { return pair(x, x); }
+__device__ __forceinline__ float2 split(Pair a) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+    return r;
+}
+__device__ __forceinline__ Pair operator+(Pair a, Pair b) {
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Pair operator*(Pair a, Pair b) {
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ float total(Pair a) {
+    const float2 f = split(a);
+    return f.x + f.y;
+}
+
+// 16 bytes of a row: 4 values of 32 bits or 8 of 16 bits, as pairs.
+template <class T>
+struct Chunk {
+    static constexpr int kPairs = 8 / sizeof(T);
+    uint4 raw;
+    __device__ __forceinline__ Pair get(int i) const {
+        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+        if constexpr (sizeof(T) == 4) {
+            return pair(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+        } else if constexpr (std::is_same<T, __half>::value) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+            return pair(f.x, f.y);
+        } else {
+            return pair(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+        }
+    }
+    __device__ __forceinline__ void set(int i, Pair p) {
+        const float2 f = split(p);
+        uint32_t* w = reinterpret_cast<uint32_t*>(&raw);
+        if constexpr (sizeof(T) == 4) {
+            w[2 * i] = __float_as_uint(f.x), w[2 * i + 1] = __float_as_uint(f.y);
+        } else if constexpr (std::is_same<T, __half>::value) {
+            const __half2 h = __floats2half2_rn(f.x, f.y);
+            w[i] = *reinterpret_cast<const uint32_t*>(&h);
+        } else {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
+            w[i] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+    }
+};
+
+__device__ __forceinline__ float inv_sqrt(float x) {
+    const float r = rsqrtf(x);
+    return r * fmaf(-0.5f * x * r, r, 1.5f);  // a Newton step: to the last place or two
+}
+
 // weight or bias, whose type may be that of the rows or 32 bits; `none` where there is no such vector.
 template <class T, int V>
 __device__ __forceinline__ void load_param(const void* p, bool f32, int c, float none, float (&out)[V]) {
@@ -55,31 +129,61 @@ __device__ __forceinline__ void load_param(const void* p, bool f32, int c, float
     }
 }
 
-// Sum over the TPR threads of a row; `slot` alternates between calls that follow one another without another barrier.
+// The same for the columns of one Chunk, as pairs.
+template <class T>
+__device__ __forceinline__ void load_param_pairs(const void* p, bool f32, int c, float none, Pair (&out)[Chunk<T>::kPairs]) {
+    constexpr int V = 2 * Chunk<T>::kPairs;
+    float v[V];
+    load_param<T, V>(p, f32, c, none, v);
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) out[i] = pair(v[2 * i], v[2 * i + 1]);
+}
+
+// Sums of N values (1, 2 or 4) over the TPR threads of a row (or of several rows that go through together), for all of
+// them. Every exchange halves the values that a lane still carries, as long as there are several: 13 shuffles for four
+// values of 512 threads instead of 40. `s` alternates between calls that follow one another without another barrier.
 template <int TPR, int N>
-__device__ __forceinline__ void row_sum(float (&v)[N], float* s, int group) {
-#pragma unroll
-    for (int o = 16; o; o /= 2) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], o);
+__device__ __forceinline__ void row_sums(float (&v)[N], float* s, int group) {
+    static_assert(N == 1 || N == 2 || N == 4, "");
+    const int lane = threadIdx.x % 32;
+    float x;
+    int o = 16;
+    if constexpr (N == 4) {
+        const bool hi = lane & 16;
+        const float a = (hi ? v[2] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, hi ? v[0] : v[2], 16);
+        const float b = (hi ? v[3] : v[1]) + __shfl_xor_sync(0xFFFFFFFFu, hi ? v[1] : v[3], 16);
+        const bool hi8 = lane & 8;
+        x = (hi8 ? b : a) + __shfl_xor_sync(0xFFFFFFFFu, hi8 ? a : b, 8);
+        o = 4;
+    } else if constexpr (N == 2) {
+        const bool hi = lane & 16;
+        x = (hi ? v[1] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, hi ? v[0] : v[1], 16);
+        o = 8;
+    } else {
+        x = v[0];
     }
-    if constexpr (TPR > 32) {
+#pragma unroll
+    for (; o; o /= 2) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+    // the lanes of each 32 / N hold one of the values
+    if constexpr (TPR == 32) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = N == 1 ? x : __shfl_sync(0xFFFFFFFFu, x, i * (32 / N));
+    } else {
         constexpr int kW = TPR / 32;
-        const int w = (threadIdx.x / 32) % kW, lane = threadIdx.x % 32;
-        if (lane == 0) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) s[(group * kW + w) * N + i] = v[i];
-        }
+        const int w = (threadIdx.x / 32) % kW;
+        s += group * kW * N;
+        if (lane % (32 / N) == 0) s[w * N + lane / (32 / N)] = x;
         asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(TPR) : "memory");
+        x = s[lane % (kW * N)];
+        if constexpr (kW * N == 64) x += s[lane + 32];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            v[i] = lane < kW ? s[(group * kW + lane) * N + i] : 0.f;
+        for (o = (kW * N > 32 ? 32 : kW * N) / 2; o >= N; o /= 2) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
 #pragma unroll
-            for (int o = kW / 2; o; o /= 2) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], o);
-            v[i] = __shfl_sync(0xFFFFFFFFu, v[i], 0);
-        }
+        for (int i = 0; i < N; ++i) v[i] = N == 1 ? x : __shfl_sync(0xFFFFFFFFu, x, i);
     }
 }
+
+constexpr int kNormSms = 148;  // the ring kernels have one block per SM of a B200
 
 struct NormIn {
     const void *x, *w, *b;
@@ -89,9 +193,9 @@ struct NormIn {
     bool w32;
 };
 
-// A row is held in registers by TPR threads (NV packs of V neighbouring elements each): read once, the mean first and
-// the squares of the differences from it second, so that no cancellation spoils the variance.
-template <class T, int TPR, int NV, int V>
+// Rows that do not start on 16-byte boundaries: a row is held in registers by TPR threads, read once a value at a time,
+// the mean first and the squares of the differences from it second, so that no cancellation spoils the variance.
+template <class T, int TPR, int N>
 __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR)
     k_norm(const NormIn a, void* y_, int64_t ldy, float* mean_out, float* rstd_out) {
     constexpr int kThreads = TPR < 128 ? 128 : TPR, kRows = kThreads / TPR;
@@ -101,56 +205,141 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR)
     if (row >= a.rows) return;  // whole groups, and groups of more than a warp are alone in their block
     const T* x = static_cast<const T*>(a.x) + row * a.ldx;
     T* y = static_cast<T*>(y_) + row * ldy;
-    float v[NV][V];
+    float v[N];
     float sum[1] = {0.f};
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (t + i * TPR) * V;
-        if (c < a.cols) {
-            const Pack<T, V> p = *reinterpret_cast<const Pack<T, V>*>(x + c);
+    for (int i = 0; i < N; ++i) v[i] = t + i * TPR < a.cols ? to_f(x[t + i * TPR]) : 0.f;
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[i][j] = to_f(p.v[j]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j) v[i][j] = 0.f;
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) sum[0] += v[i][j];
-    }
-    row_sum<TPR>(sum, s[0], group);
+    for (int i = 0; i < N; ++i) sum[0] += v[i];
+    row_sums<TPR, 1>(sum, s[0], group);
     const float mean = sum[0] / a.cols;
     float sq[1] = {0.f};
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        if ((t + i * TPR) * V < a.cols) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                v[i][j] -= mean;
-                sq[0] = fmaf(v[i][j], v[i][j], sq[0]);
-            }
+    for (int i = 0; i < N; ++i) {
+        if (t + i * TPR < a.cols) {
+            v[i] -= mean;
+            sq[0] = fmaf(v[i], v[i], sq[0]);
         }
     }
-    row_sum<TPR>(sq, s[1], group);
-    const float rstd = 1.f / sqrtf(sq[0] / a.cols + a.eps);
+    row_sums<TPR, 1>(sq, s[1], group);
+    const float rstd = inv_sqrt(sq[0] / a.cols + a.eps);
     if (t == 0) {
         if (mean_out) mean_out[row] = mean;
         if (rstd_out) rstd_out[row] = rstd;
     }
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (t + i * TPR) * V;
+    for (int i = 0; i < N; ++i) {
+        const int c = t + i * TPR;
         if (c >= a.cols) break;
-        float w[V], b[V];
-        load_param<T, V>(a.w, a.w32, c, 1.f, w);
-        load_param<T, V>(a.b, a.w32, c, 0.f, b);
-        Pack<T, V> p;
-#pragma unroll
-        for (int j = 0; j < V; ++j) p.v[j] = from_f<T>(fmaf(v[i][j] * rstd, w[j], b[j]));
-        *reinterpret_cast<Pack<T, V>*>(y + c) = p;
+        float w[1], b[1];
+        load_param<T, 1>(a.w, a.w32, c, 1.f, w);
+        load_param<T, 1>(a.b, a.w32, c, 0.f, b);
+        y[c] = from_f<T>(fmaf(v[i] * rstd, w[0], b[0]));
     }
+}
+
+// ---- rows on 16-byte boundaries ----
+// One block per SM works through the rows, TPR threads on a row, each with NV chunks of 16 bytes. The rows come by bulk
+// copies into a ring of `stages` per group of TPR threads that is filled ahead: the bytes on their way depend neither on
+// registers nor on how many threads wait. What is left to bound the kernels is the issue of instructions, so a thread has
+// many values (the shuffles and the barrier of a sum cost as much for few) and does arithmetic on pairs.
+constexpr int kRingThreads = 512, kRingBytes = 196 * 1024, kMaxStages = 16;
+
+template <int TPR>
+__device__ __forceinline__ void group_sync(int group) {
+    if constexpr (TPR == 32)
+        __syncwarp();
+    else
+        asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(TPR) : "memory");
+}
+
+__device__ unsigned g_wait_expired;
+
+template <class T, int TPR, int NV>
+__global__ void __launch_bounds__(kRingThreads, 1)
+    k_norm_ring(const NormIn a, void* y_, int64_t ldy, float* mean_out, float* rstd_out, int stages) {
+    constexpr int P = Chunk<T>::kPairs, kGroups = kRingThreads / TPR;
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ __align__(8) uint64_t s_full[kGroups * kMaxStages];
+    __shared__ float s[2][2][kRingThreads / 32];
+    const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
+    const int cols16 = a.cols / (2 * P);  // chunks of a row
+    const uint32_t bytes = a.cols * sizeof(T), full = smem_u32(s_full + group * kMaxStages);
+    uint8_t* mine = ring + (size_t)group * stages * bytes;
+    const int first = blockIdx.x * kGroups + group, step = gridDim.x * kGroups;
+    auto fetch = [&](int64_t row, int st) {
+        bar_expect(full + 8 * st, bytes);
+        bulk_load(smem_u32(mine + st * bytes), static_cast<const T*>(a.x) + row * a.ldx, bytes, full + 8 * st);
+    };
+    if (t == 0) {
+        for (int i = 0; i < stages; ++i) bar_init(full + 8 * i, 1);
+        bar_init_done();
+        for (int i = 0; i < stages && first + (int64_t)i * step < a.rows; ++i) fetch(first + (int64_t)i * step, i);
+    }
+    Pair w[NV][P], b[NV][P];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = t + i * TPR;
+        if (c >= cols16) break;
+        load_param_pairs<T>(a.w, a.w32, c * 2 * P, 1.f, w[i]);
+        load_param_pairs<T>(a.b, a.w32, c * 2 * P, 0.f, b[i]);
+    }
+    group_sync<TPR>(group);
+    const float inv = 1.f / a.cols;
+    int st = 0, turn = 0;
+    uint32_t ph = 0;
+    bool bad = false;
+    for (int64_t row = first; row < a.rows; row += step, turn ^= 1) {
+        const bool ok = bar_wait(full + 8 * st, ph, &g_wait_expired);
+        bad = bad || !ok;
+        const uint4* at = reinterpret_cast<const uint4*>(mine + st * bytes);
+        Pair v[NV][P], acc = both(0.f);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (t + i * TPR < cols16) {
+                const Chunk<T> q = {at[t + i * TPR]};
+#pragma unroll
+                for (int j = 0; j < P; ++j) acc = acc + (v[i][j] = q.get(j));
+            }
+        }
+        float sum[1] = {total(acc)};
+        row_sums<TPR, 1>(sum, s[turn][0], group);
+        // everybody has read this row: its place is free
+        if (t == 0 && ok && row + (int64_t)stages * step < a.rows) fetch(row + (int64_t)stages * step, st);
+        const float mean = sum[0] * inv;
+        const Pair minus = both(-mean);
+        acc = both(0.f);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (t + i * TPR < cols16) {
+#pragma unroll
+                for (int j = 0; j < P; ++j) {
+                    v[i][j] = v[i][j] + minus;
+                    acc = fma2(v[i][j], v[i][j], acc);
+                }
+            }
+        }
+        float sq[1] = {total(acc)};
+        row_sums<TPR, 1>(sq, s[turn][1], group);
+        const float rstd = inv_sqrt(fmaf(sq[0], inv, a.eps));
+        if (t == 0) {
+            if (mean_out) mean_out[row] = mean;
+            if (rstd_out) rstd_out[row] = rstd;
+        }
+        uint4* y = reinterpret_cast<uint4*>(static_cast<T*>(y_) + row * ldy);
+        const Pair scale = both(rstd);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = t + i * TPR;
+            if (c >= cols16) break;
+            Chunk<T> q;
+#pragma unroll
+            for (int j = 0; j < P; ++j) q.set(j, fma2(v[i][j] * scale, w[i][j], b[i][j]));
+            y[c] = q.raw;
+        }
+        if (++st == stages) st = 0, ph ^= 1;
+    }
+    if (bad) let_copies_end();
 }
 
 // Rows longer than the registers of a block hold: three passes, the second and third from the caches.
@@ -163,14 +352,14 @@ __global__ void __launch_bounds__(kLongThreads) k_norm_long(const NormIn a, void
     T* y = static_cast<T*>(y_) + row * ldy;
     float sum[1] = {0.f}, sq[1] = {0.f};
     for (int c = threadIdx.x; c < a.cols; c += kLongThreads) sum[0] += to_f(x[c]);
-    row_sum<kLongThreads>(sum, s[0], 0);
+    row_sums<kLongThreads, 1>(sum, s[0], 0);
     const float mean = sum[0] / a.cols;
     for (int c = threadIdx.x; c < a.cols; c += kLongThreads) {
         const float d = to_f(x[c]) - mean;
         sq[0] = fmaf(d, d, sq[0]);
     }
-    row_sum<kLongThreads>(sq, s[1], 0);
-    const float rstd = 1.f / sqrtf(sq[0] / a.cols + a.eps);
+    row_sums<kLongThreads, 1>(sq, s[1], 0);
+    const float rstd = inv_sqrt(sq[0] / a.cols + a.eps);
     if (threadIdx.x == 0) {
         if (mean_out) mean_out[row] = mean;
         if (rstd_out) rstd_out[row] = rstd;
@@ -193,7 +382,7 @@ struct NormBack {
     bool w32;
 };
 
-constexpr int kBackParts = 2 * 148;  // blocks of the backward pass: two on every SM of a B200
+constexpr int kBackParts = 2 * 148;  // at most so many blocks, and parts of the sums over rows: two on every SM of a B200
 
 // Each thread keeps the same columns for all rows of its block, and with them the block's share of dweight and dbias
 // in registers; the next row's dy and x are on their way while a row is summed and written.
@@ -256,7 +445,7 @@ __global__ void __launch_bounds__(TPR < 512 ? 512 : TPR) k_norm_back(const NormB
             }
         }
         fetch(row + step);
-        row_sum<TPR>(sum, s[turn], group);
+        row_sums<TPR, 2>(sum, s[turn], group);
         const float c1 = sum[0] * inv, c2 = sum[1] * inv;
         T* dx = static_cast<T*>(a.dx) + row * a.lddx;
 #pragma unroll
@@ -304,6 +493,116 @@ __global__ void __launch_bounds__(TPR < 512 ? 512 : TPR) k_norm_back(const NormB
     let_successor_start();
 }
 
+// The same for rows on 16-byte boundaries, as k_norm_ring: x and dy come by bulk copies.
+template <class T, int TPR, int NV>
+__global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_ring(const NormBack a, int stages) {
+    constexpr int P = Chunk<T>::kPairs, kGroups = kRingThreads / TPR;
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ __align__(8) uint64_t s_full[kGroups * kMaxStages];
+    __shared__ float s[2][2 * kRingThreads / 32];
+    const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
+    const int cols16 = a.cols / (2 * P);
+    const uint32_t bytes = a.cols * sizeof(T), full = smem_u32(s_full + group * kMaxStages);
+    uint8_t* mine = ring + (size_t)group * stages * 2 * bytes;
+    const int first = blockIdx.x * kGroups + group, step = gridDim.x * kGroups;
+    auto fetch = [&](int64_t row, int st) {
+        const uint32_t at = smem_u32(mine + st * 2 * bytes);
+        bar_expect(full + 8 * st, 2 * bytes);
+        bulk_load(at, static_cast<const T*>(a.x) + row * a.ldx, bytes, full + 8 * st);
+        bulk_load(at + bytes, static_cast<const T*>(a.dy) + row * a.lddy, bytes, full + 8 * st);
+    };
+    if (t == 0) {
+        for (int i = 0; i < stages; ++i) bar_init(full + 8 * i, 1);
+        bar_init_done();
+        for (int i = 0; i < stages && first + (int64_t)i * step < a.rows; ++i) fetch(first + (int64_t)i * step, i);
+    }
+    Pair w[NV][P], dw[NV][P], db[NV][P];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (t + i * TPR < cols16) load_param_pairs<T>(a.w, a.w32, (t + i * TPR) * 2 * P, 1.f, w[i]);
+#pragma unroll
+        for (int j = 0; j < P; ++j) dw[i][j] = db[i][j] = both(0.f);
+    }
+    group_sync<TPR>(group);
+    const float inv = 1.f / a.cols;
+    int st = 0, turn = 0;
+    uint32_t ph = 0;
+    bool bad = false;
+    float nmean = first < a.rows ? a.mean[first] : 0.f, nrstd = first < a.rows ? a.rstd[first] : 0.f;
+    for (int64_t row = first; row < a.rows; row += step, turn ^= 1) {
+        const float mean = nmean, rstd = nrstd;
+        if (row + step < a.rows) nmean = a.mean[row + step], nrstd = a.rstd[row + step];
+        const bool ok = bar_wait(full + 8 * st, ph, &g_wait_expired);
+        bad = bad || !ok;
+        const uint4* at = reinterpret_cast<const uint4*>(mine + st * 2 * bytes);
+        const Pair scale = both(rstd), minus = both(-mean);
+        Pair acc1 = both(0.f), acc2 = both(0.f);
+        Chunk<T> x[NV], dy[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = t + i * TPR;
+            if (c >= cols16) break;
+            x[i].raw = at[c];
+            dy[i].raw = at[cols16 + c];
+#pragma unroll
+            for (int j = 0; j < P; ++j) {
+                const Pair d = dy[i].get(j), e = d * ((x[i].get(j) + minus) * scale);  // dy * xh
+                db[i][j] = db[i][j] + d;
+                dw[i][j] = dw[i][j] + e;
+                acc1 = fma2(d, w[i][j], acc1);
+                acc2 = fma2(e, w[i][j], acc2);
+            }
+        }
+        float sum[2] = {total(acc1), total(acc2)};
+        row_sums<TPR, 2>(sum, s[turn], group);
+        // everybody has read these rows: their place is free
+        if (t == 0 && ok && row + (int64_t)stages * step < a.rows) fetch(row + (int64_t)stages * step, st);
+        // dx = rstd * (dy * w - c1 - xh * c2)
+        const Pair c1 = both(-rstd * sum[0] * inv), c2 = both(-rstd * rstd * sum[1] * inv);
+        uint4* dx = reinterpret_cast<uint4*>(static_cast<T*>(a.dx) + row * a.lddx);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = t + i * TPR;
+            if (c >= cols16) break;
+            Chunk<T> q;
+#pragma unroll
+            for (int j = 0; j < P; ++j)
+                q.set(j, fma2(x[i].get(j) + minus, c2, fma2(dy[i].get(j) * w[i][j], scale, c1)));
+            dx[c] = q.raw;
+        }
+        if (++st == stages) st = 0, ph ^= 1;
+    }
+    if (bad) let_copies_end();
+    if (a.part) {
+        float* out = a.part + (int64_t)blockIdx.x * 2 * a.cols;
+        float* s_part = kGroups > 1 ? reinterpret_cast<float*>(ring) : out;  // [2][cols]; the ring has done its work
+        __syncthreads();
+        for (int k = 0; k < kGroups; ++k) {
+            if (group == k) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    if (t + i * TPR >= cols16) break;
+#pragma unroll
+                    for (int j = 0; j < P; ++j) {
+                        float2* p = reinterpret_cast<float2*>(s_part) + (t + i * TPR) * P + j;
+                        float2 u = split(dw[i][j]), v = split(db[i][j]);
+                        if (k) {
+                            const float2 pu = p[0], pv = p[a.cols / 2];
+                            u.x += pu.x, u.y += pu.y, v.x += pv.x, v.y += pv.y;
+                        }
+                        p[0] = u;
+                        p[a.cols / 2] = v;
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        if (kGroups > 1)
+            for (int c = threadIdx.x; c < 2 * a.cols; c += kRingThreads) out[c] = s_part[c];
+    }
+    let_successor_start();
+}
+
 // Rows longer than the registers hold: dx from two passes over the row, the sums over rows by columns.
 template <class T>
 __global__ void __launch_bounds__(kLongThreads) k_norm_back_long(const NormBack a) {
@@ -321,7 +620,7 @@ __global__ void __launch_bounds__(kLongThreads) k_norm_back_long(const NormBack 
         sum[0] += g;
         sum[1] = fmaf(g, (to_f(x[c]) - mean) * rstd, sum[1]);
     }
-    row_sum<kLongThreads>(sum, s, 0);
+    row_sums<kLongThreads, 2>(sum, s, 0);
     const float c1 = sum[0] / a.cols, c2 = sum[1] / a.cols;
     for (int c = threadIdx.x; c < a.cols; c += kLongThreads) {
         float w[1];
@@ -358,7 +657,7 @@ __global__ void __launch_bounds__(32 * kJoinLanes) k_norm_join(const float* part
     const int c = blockIdx.x * 32 + threadIdx.x % 32, l = threadIdx.x / 32;
     float sum = 0.f;
     if (c < 2 * cols) {
-#pragma unroll 4
+#pragma unroll 10
         for (int i = l; i < parts; i += kJoinLanes) sum += part[(int64_t)i * 2 * cols + c];
     }
     s[l][threadIdx.x % 32] = sum;
@@ -375,10 +674,30 @@ __global__ void __launch_bounds__(32 * kJoinLanes) k_norm_join(const float* part
 
 int parts_of(int32_t rows) { return rows < kBackParts ? rows : kBackParts; }
 
-template <class T, int TPR, int NV, int V>
+template <class T, int TPR, int N>
 cudaError_t norm(const NormIn& a, void* y, int64_t ldy, float* mean, float* rstd, cudaStream_t stream) {
     constexpr int kThreads = TPR < 128 ? 128 : TPR, kRows = kThreads / TPR;
-    k_norm<T, TPR, NV, V><<<(a.rows + kRows - 1) / kRows, kThreads, 0, stream>>>(a, y, ldy, mean, rstd);
+    k_norm<T, TPR, N><<<(a.rows + kRows - 1) / kRows, kThreads, 0, stream>>>(a, y, ldy, mean, rstd);
+    return cudaGetLastError();
+}
+
+// Stages of a group's ring.
+inline int ring_stages(int groups, size_t stage_bytes, size_t most) {
+    const size_t n = most / (groups * stage_bytes);
+    return n > kMaxStages ? kMaxStages : n < 1 ? 1 : (int)n;
+}
+
+template <class T, int TPR, int NV>
+cudaError_t norm_ring(const NormIn& a, void* y, int64_t ldy, float* mean, float* rstd, cudaStream_t stream) {
+    constexpr int kGroups = kRingThreads / TPR;
+    const int need = (a.rows + kGroups - 1) / kGroups, blocks = need < kNormSms ? need : kNormSms;
+    const size_t row = (size_t)a.cols * sizeof(T);
+    const int stages = ring_stages(kGroups, row, kRingBytes);
+    auto kernel = k_norm_ring<T, TPR, NV>;
+    static std::atomic<uint64_t> ready{0};
+    cudaError_t err = allow_smem(kernel, kRingBytes, ready);
+    if (err != cudaSuccess) return err;
+    kernel<<<blocks, kRingThreads, kGroups * stages * row, stream>>>(a, y, ldy, mean, rstd, stages);
     return cudaGetLastError();
 }
 
@@ -387,28 +706,48 @@ cudaError_t norm_of(const NormIn& a, void* y, int64_t ldy, float* mean, float* r
     constexpr int V = 16 / sizeof(T);
     const int n = a.cols;
     if (wide) {
-        if (n <= 32 * V) return norm<T, 32, 1, V>(a, y, ldy, mean, rstd, stream);
-        if (n <= 32 * V * 4) return norm<T, 32, 4, V>(a, y, ldy, mean, rstd, stream);
-        if (n <= 128 * V * 2) return norm<T, 128, 2, V>(a, y, ldy, mean, rstd, stream);
-        if (n <= 128 * V * 4) return norm<T, 128, 4, V>(a, y, ldy, mean, rstd, stream);
-        if (n <= 512 * V * 2) return norm<T, 512, 2, V>(a, y, ldy, mean, rstd, stream);
-        if (n <= 512 * V * 4) return norm<T, 512, 4, V>(a, y, ldy, mean, rstd, stream);
+        constexpr int N = 32 / V;  // chunks that hold 32 values
+        if (n <= 32 * 8) return norm_ring<T, 32, N / 4>(a, y, ldy, mean, rstd, stream);
+        if (n <= 32 * 16) return norm_ring<T, 32, N / 2>(a, y, ldy, mean, rstd, stream);
+        if (n <= 32 * 32) return norm_ring<T, 32, N>(a, y, ldy, mean, rstd, stream);
+        if (n <= 64 * 32) return norm_ring<T, 64, N>(a, y, ldy, mean, rstd, stream);
+        if (n <= 128 * 32) return norm_ring<T, 128, N>(a, y, ldy, mean, rstd, stream);
+        if (n <= 256 * 32) return norm_ring<T, 256, N>(a, y, ldy, mean, rstd, stream);
+        if (n <= 512 * 32) return norm_ring<T, 512, N>(a, y, ldy, mean, rstd, stream);
     } else {
-        if (n <= 32 * 32) return norm<T, 32, 32, 1>(a, y, ldy, mean, rstd, stream);
-        if (n <= 128 * 32) return norm<T, 128, 32, 1>(a, y, ldy, mean, rstd, stream);
-        if (n <= 512 * 32) return norm<T, 512, 32, 1>(a, y, ldy, mean, rstd, stream);
+        if (n <= 32 * 8) return norm<T, 32, 8>(a, y, ldy, mean, rstd, stream);
+        if (n <= 128 * 8) return norm<T, 128, 8>(a, y, ldy, mean, rstd, stream);
+        if (n <= 512 * 8) return norm<T, 512, 8>(a, y, ldy, mean, rstd, stream);
+        if (n <= 512 * 32) return norm<T, 512, 32>(a, y, ldy, mean, rstd, stream);
     }
     k_norm_long<T><<<a.rows, kLongThreads, 0, stream>>>(a, y, ldy, mean, rstd);
     return cudaGetLastError();
 }
 
-template <class T, int TPR, int NV, int V>
+template <class T, int TPR, int N>
 cudaError_t back(const NormBack& a, int* parts, cudaStream_t stream) {
     constexpr int kThreads = TPR < 512 ? 512 : TPR, kGroups = kThreads / TPR;
     const int need = (a.rows + kGroups - 1) / kGroups;
     *parts = need < kBackParts ? need : kBackParts;
     const size_t smem = kGroups > 1 && a.part ? (size_t)2 * a.cols * 4 : 0;  // at most 16 KiB: 2048 columns
-    k_norm_back<T, TPR, NV, V><<<*parts, kThreads, smem, stream>>>(a);
+    k_norm_back<T, TPR, N, 1><<<*parts, kThreads, smem, stream>>>(a);
+    return cudaGetLastError();
+}
+
+template <class T, int TPR, int NV>
+cudaError_t back_ring(const NormBack& a, int* parts, cudaStream_t stream) {
+    constexpr int kGroups = kRingThreads / TPR;
+    const int need = (a.rows + kGroups - 1) / kGroups;
+    *parts = need < kNormSms ? need : kNormSms;
+    const size_t stage = (size_t)a.cols * sizeof(T) * 2;
+    const int stages = ring_stages(kGroups, stage, kRingBytes);
+    auto kernel = k_norm_back_ring<T, TPR, NV>;
+    static std::atomic<uint64_t> ready{0};
+    cudaError_t err = allow_smem(kernel, kRingBytes, ready);
+    if (err != cudaSuccess) return err;
+    size_t smem = kGroups * stages * stage;
+    if (smem < (size_t)2 * a.cols * 4) smem = (size_t)2 * a.cols * 4;  // the ring's place also joins the groups' sums
+    kernel<<<*parts, kRingThreads, smem, stream>>>(a, stages);
     return cudaGetLastError();
 }
 
@@ -417,16 +756,18 @@ cudaError_t back_of(const NormBack& a, int* parts, bool wide, cudaStream_t strea
     constexpr int V = 16 / sizeof(T);
     const int n = a.cols;
     if (wide) {
-        if (n <= 32 * V) return back<T, 32, 1, V>(a, parts, stream);
-        if (n <= 32 * V * 2) return back<T, 32, 2, V>(a, parts, stream);
-        if (n <= 128 * V) return back<T, 128, 1, V>(a, parts, stream);
-        if (n <= 128 * V * 2) return back<T, 128, 2, V>(a, parts, stream);
-        if (n <= 512 * V) return back<T, 512, 1, V>(a, parts, stream);
-        if (n <= 512 * V * 2) return back<T, 512, 2, V>(a, parts, stream);
+        constexpr int N = 16 / V;  // chunks that hold 16 values
+        if (n <= 32 * 8) return back_ring<T, 32, N / 2>(a, parts, stream);
+        if (n <= 32 * 16) return back_ring<T, 32, N>(a, parts, stream);
+        if (n <= 64 * 16) return back_ring<T, 64, N>(a, parts, stream);
+        if (n <= 128 * 16) return back_ring<T, 128, N>(a, parts, stream);
+        if (n <= 256 * 16) return back_ring<T, 256, N>(a, parts, stream);
+        if (n <= 512 * 16) return back_ring<T, 512, N>(a, parts, stream);
     } else {
-        if (n <= 32 * 16) return back<T, 32, 16, 1>(a, parts, stream);
-        if (n <= 128 * 16) return back<T, 128, 16, 1>(a, parts, stream);
-        if (n <= 512 * 16) return back<T, 512, 16, 1>(a, parts, stream);
+        if (n <= 32 * 8) return back<T, 32, 8>(a, parts, stream);
+        if (n <= 128 * 8) return back<T, 128, 8>(a, parts, stream);
+        if (n <= 512 * 8) return back<T, 512, 8>(a, parts, stream);
+        if (n <= 512 * 16) return back<T, 512, 16>(a, parts, stream);
     }
     k_norm_back_long<T><<<a.rows, kLongThreads, 0, stream>>>(a);
     cudaError_t err = cudaGetLastError();
@@ -456,6 +797,13 @@ bool is_wide(const void* p, int64_t ld, int cols, int32_t type) {
 }
 
 }  // namespace
+
+cudaError_t norm_wait_expired(unsigned* out) {
+    cudaError_t err = cudaMemcpyFromSymbol(out, g_wait_expired, sizeof(*out));
+    const unsigned zero = 0;
+    if (err == cudaSuccess && *out) err = cudaMemcpyToSymbol(g_wait_expired, &zero, sizeof(zero));
+    return err;
+}
 
 }  // namespace ones
 

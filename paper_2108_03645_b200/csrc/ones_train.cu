@@ -49,7 +49,9 @@ cudaError_t make_map(CUtensorMap* out, const Operand& o, int rows, int k, int ba
 
 extern "C" int ones_train_status(void* cuda_stream) {
     if (cudaStreamSynchronize(reinterpret_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) return ONES_ERR_CUDA;
-    unsigned a = 0, b = 0;
-    if (ones::loss_wait_expired(&a) != cudaSuccess || ones::update_wait_expired(&b) != cudaSuccess) return ONES_ERR_CUDA;
-    return a || b ? ONES_ERR_TIMEOUT : ONES_OK;
+    unsigned a = 0, b = 0, c = 0;
+    if (ones::norm_wait_expired(&a) != cudaSuccess || ones::loss_wait_expired(&b) != cudaSuccess ||
+        ones::update_wait_expired(&c) != cudaSuccess)
+        return ONES_ERR_CUDA;
+    return a || b || c ? ONES_ERR_TIMEOUT : ONES_OK;
 }

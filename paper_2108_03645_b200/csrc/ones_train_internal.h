@@ -3,12 +3,29 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 namespace ones {
 
 inline bool aligned(const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
-cudaError_t loss_wait_expired(unsigned* out);    // reads and clears the flag of the loss kernels
-cudaError_t update_wait_expired(unsigned* out);  // and of the update's
+// Read and clear the flags that kernels set when they give up waiting.
+cudaError_t norm_wait_expired(unsigned* out);
+cudaError_t loss_wait_expired(unsigned* out);
+cudaError_t update_wait_expired(unsigned* out);
+
+// Lets the kernel use `bytes` of dynamic shared memory on the current device; `ready` holds the devices that know.
+template <class F>
+cudaError_t allow_smem(F kernel, int bytes, std::atomic<uint64_t>& ready) {
+    int dev = 0;
+    cudaError_t err = cudaGetDevice(&dev);
+    if (err != cudaSuccess) return err;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (dev < 64 && (ready.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+    err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (err == cudaSuccess && dev < 64) ready.fetch_or(bit, std::memory_order_relaxed);
+    return err;
+}
 
 // Launches a kernel that begins with griddepcontrol.wait beside the tail of the launch before it.
 template <class... P, class... A>

@@ -120,13 +120,15 @@ __global__ void __launch_bounds__(kNormThreads) k_ns_cast(Source g, const double
 }
 
 // The symmetric products' tiles lie on and above the diagonal; what they hold is stored on both sides of it.
-__device__ __forceinline__ void store_both(__half* out, int64_t ld, int s, int row, int col, bool mirror, const float (&v)[32]) {
-    if (row >= s) return;
-    store_row16(reinterpret_cast<uint16_t*>(out + (int64_t)row * ld), col, s, v, true, true);
-    if (!mirror) return;
+__device__ __forceinline__ void store_both(__half* out, int64_t ld, int s, int row, int col, bool mirror, const float (&v)[64], const Turn& turn) {
+    uint16_t* p = reinterpret_cast<uint16_t*>(out);
+    turn.put16(v, true);
+    turn.store16(p, ld, row - turn.lane, col, s, s, true);
+    if (!mirror || row >= s) return;
+    p += (int64_t)col * ld + row;
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
-        if (col + i < s) out[(int64_t)(col + i) * ld + row] = __float2half_rn(v[i]);
+    for (int i = 0; i < 64; ++i, p += ld)
+        if (col + i < s) *p = __half_as_ushort(__float2half_rn(v[i]));
 }
 
 // A = factor * X X^T
@@ -140,16 +142,15 @@ struct EpiGram {
     };
     template <int W>
     static __device__ __forceinline__ void tile(const Args& a, const MatShape&, uint32_t acc, int row, int col,
-                                                const TileAt& at, int) {
+                                                const TileAt& at, int, const Turn& turn) {
         const float f = a.first ? a.first[at.b].y : a.factor;
 #pragma unroll 1
-        for (int c = 0; c < W; c += 32) {
-            float v[32];
-            tmem_load32(acc + c, v);
-            if (col + c >= a.s) break;
+        for (int c = 0; c < W && col + c < a.s; c += 64) {
+            float v[64];
+            tmem_load(acc + c, v);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] *= f;
-            store_both(a.out + at.b * a.batch_ld, a.ld, a.s, row, col + c, at.m != at.n, v);
+            for (int i = 0; i < 64; ++i) v[i] *= f;
+            store_both(a.out + at.b * a.batch_ld, a.ld, a.s, row, col + c, at.m != at.n, v, turn);
         }
     }
 };
@@ -166,37 +167,42 @@ struct EpiPoly {
     };
     template <int W>
     static __device__ __forceinline__ void tile(const Args& a, const MatShape&, uint32_t acc, int row, int col,
-                                                const TileAt& at, int) {
+                                                const TileAt& at, int, const Turn& turn) {
 #pragma unroll 1
-        for (int c = 0; c < W; c += 32) {
-            float v[32];
-            tmem_load32(acc + c, v);
-            if (col + c >= a.s) break;
-            if (row < a.s) {
-                const __half* gram = a.gram + at.b * a.batch_ld + (int64_t)row * a.ld + col + c;
-                if (col + c + 32 <= a.s) {
+        for (int c = 0; c < W && col + c < a.s; c += 64) {
+            // A's values, 8 lanes to a row, by the same way that the result leaves
+            const __half* gram = a.gram + at.b * a.batch_ld;
+            const int k = turn.lane & 7, at_col = col + c + 8 * k;
+            uint4 q[8];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint4 q = reinterpret_cast<const uint4*>(gram)[j];
-                        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-                            v[8 * j + 2 * i] = fmaf(a.c, v[8 * j + 2 * i], a.b * h.x);
-                            v[8 * j + 2 * i + 1] = fmaf(a.c, v[8 * j + 2 * i + 1], a.b * h.y);
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (col + c + i < a.s) v[i] = fmaf(a.c, v[i], a.b * __half2float(gram[i]));
-                }
-                const int d = row - (col + c);
-#pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if (i == d) v[i] += a.a;
+            for (int i = 0; i < 8; ++i) {
+                const int r = row - turn.lane + 4 * i + turn.lane / 8;  // rows of A are padded to whole 16 bytes
+                q[i] = r < a.s && at_col < a.s ? *reinterpret_cast<const uint4*>(gram + (int64_t)r * a.ld + at_col) : make_uint4(0, 0, 0, 0);
             }
-            store_both(a.out + at.b * a.batch_ld, a.ld, a.s, row, col + c, at.m != at.n, v);
+            float v[64];
+            tmem_load(acc + c, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) turn.chunk(4 * i + turn.lane / 8, k) = q[i];
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint4 p = turn.chunk(turn.lane, j);
+                const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+                    v[8 * j + 2 * i] = fmaf(a.c, v[8 * j + 2 * i], a.b * h.x);
+                    v[8 * j + 2 * i + 1] = fmaf(a.c, v[8 * j + 2 * i + 1], a.b * h.y);
+                }
+            }
+            const unsigned d = (unsigned)(row - (col + c));
+            if (d < 64u) {
+#pragma unroll
+                for (int i = 0; i < 64; ++i)
+                    if (d == (unsigned)i) v[i] += a.a;
+            }
+            store_both(a.out + at.b * a.batch_ld, a.ld, a.s, row, col + c, at.m != at.n, v, turn);
+            __syncwarp();
         }
     }
 };
@@ -213,16 +219,16 @@ struct EpiApply {
     };
     template <int W>
     static __device__ __forceinline__ void tile(const Args& a, const MatShape&, uint32_t acc, int row, int col,
-                                                const TileAt& at, int) {
+                                                const TileAt& at, int, const Turn& turn) {
         const float f = a.first ? a.factor * a.first[at.b].x : a.factor;
 #pragma unroll 1
-        for (int c = 0; c < W; c += 32) {
-            float v[32];
-            tmem_load32(acc + c, v);
-            if (col + c >= a.n) break;
+        for (int c = 0; c < W && col + c < a.n; c += 64) {
+            float v[64];
+            tmem_load(acc + c, v);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] *= f;
-            if (row < a.m) store_row16(a.out + at.b * a.batch_ld + (int64_t)row * a.ld, col + c, a.n, v, a.f16, a.wide);
+            for (int i = 0; i < 64; ++i) v[i] *= f;
+            turn.put16(v, a.f16);
+            turn.store16(a.out + at.b * a.batch_ld, a.ld, row - turn.lane, col + c, a.m, a.n, a.wide);
         }
     }
 };

@@ -9,7 +9,6 @@ for the cross entropy rows that do not start on 16-byte boundaries, are copied f
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 
 import torch
@@ -57,28 +56,29 @@ def lib() -> C.CDLL:
     return _lib
 
 
-def _need(ok, what):
+def _need(ok, what, *args):
     if not ok:
-        raise ValueError(what)
+        raise ValueError(what.format(*args))
 
 
-def _on(t: torch.Tensor):
-    """Makes the tensor's device current for the call."""
+def _device(t: torch.Tensor, call):
+    """None when the tensor's device is current; otherwise the result of `call` made with it current."""
     if t.device.index == torch.cuda.current_device():
-        return contextlib.nullcontext()
-    return torch.cuda.device(t.device)
+        return None
+    with torch.cuda.device(t.device):
+        return call()
 
 
 def _rows(t: torch.Tensor, align: int = 0) -> tuple[torch.Tensor, int]:
-    """`t` [rows][cols] as it can be read, and the distance of its rows in values.  align: 8 for rows that have to start
-    on 16-byte boundaries (16-bit types)."""
+    """`t` [..][cols] as rows that can be read, and the distance between two of them in values.  align: 8 for rows that
+    have to start on 16-byte boundaries (16-bit types)."""
+    if t.dim() != 2:
+        t = t.reshape(-1, t.shape[-1])
     n, c = t.shape
-    ld = t.stride(0)
-    if n <= 1:
-        ld = max(c, 1)
-        if align:
-            ld = (ld + align - 1) // align * align  # there is no second row
-    if (t.stride(1) != 1 and c > 1) or ld < c:
+    ld, inner = t.stride()
+    if n <= 1:  # there is no second row
+        ld = (max(c, 1) + align - 1) // align * align if align else max(c, 1)
+    if (inner != 1 and c > 1) or ld < c:
         t = t.contiguous()
         ld = c
     if align and (ld % align or t.data_ptr() % 16):
@@ -89,16 +89,11 @@ def _rows(t: torch.Tensor, align: int = 0) -> tuple[torch.Tensor, int]:
     return t, ld
 
 
-def _ptr(t):
-    return None if t is None else t.data_ptr()
-
-
 def _space(nbytes: int, device) -> torch.Tensor:
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
-def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+_stream_of = torch._C._cuda_getCurrentRawStream  # current_stream(device).cuda_stream without the Stream object
 
 
 def _done(rc: int, where: str):
@@ -106,73 +101,82 @@ def _done(rc: int, where: str):
         raise _b.OnesError(rc, where)
 
 
-def _flat(t: torch.Tensor) -> torch.Tensor:
-    return t if t.dim() == 2 else t.reshape(-1, t.shape[-1])
-
-
 def _param(t, cols, x, name):
-    if t is None:
-        return
-    _need(t.shape == (cols,) and t.device == x.device and t.is_contiguous(), f"{name}: a contiguous vector of {cols} values on {x.device} is needed")
-    _need(t.dtype in (torch.float32, x.dtype), f"{name}: float32 or the type of x ({x.dtype}) is needed, not {t.dtype}")
+    _need(t.dim() == 1 and t.shape[0] == cols and t.device == x.device and t.is_contiguous(),
+          "{}: a contiguous vector of {} values on {} is needed", name, cols, x.device)
+    _need(t.dtype is x.dtype or t.dtype is torch.float32, "{}: float32 or the type of x ({}) is needed, not {}", name, x.dtype, t.dtype)
 
 
 def layer_norm(x: torch.Tensor, weight=None, bias=None, eps: float = 1e-5):
     """Layer norm over the last dimension (``ones_layer_norm``): (y, mean, rstd), mean and rstd in float32 with x's
     leading dimensions.  weight and bias: None, or vectors of x's type or of float32 (both of one type)."""
-    _need(x.is_cuda and x.dtype in _TYPES and x.dim() >= 1, "x: a float32, bfloat16 or float16 CUDA tensor is needed")
-    cols = x.shape[-1]
-    _param(weight, cols, x, "weight")
-    _param(bias, cols, x, "bias")
-    _need(weight is None or bias is None or weight.dtype == bias.dtype, "weight and bias need one type")
-    with _on(x):
-        p, ld = _rows(_flat(x))
-        rows = p.shape[0]
-        wt = weight if weight is not None else bias
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        stats = torch.empty((2, rows), dtype=torch.float32, device=x.device)
-        _done(lib().ones_layer_norm(p.data_ptr(), ld, _ptr(weight), _ptr(bias), rows, cols, eps, _TYPES[x.dtype],
-                                    F32 if wt is None else _TYPES[wt.dtype], y.data_ptr(), cols, stats[0].data_ptr(),
-                                    stats[1].data_ptr(), _stream()), "ones_layer_norm")
-    return y, stats[0].view(x.shape[:-1]), stats[1].view(x.shape[:-1])
+    kind = _TYPES.get(x.dtype)
+    _need(kind is not None and x.is_cuda and x.dim() >= 1, "x: a float32, bfloat16 or float16 CUDA tensor is needed")
+    shape = x.shape
+    cols = shape[-1]
+    wkind = F32
+    wp = bp = None
+    if bias is not None:
+        _param(bias, cols, x, "bias")
+        wkind, bp = _TYPES[bias.dtype], bias.data_ptr()
+    if weight is not None:
+        _param(weight, cols, x, "weight")
+        _need(bias is None or bias.dtype is weight.dtype, "weight and bias need one type")
+        wkind, wp = _TYPES[weight.dtype], weight.data_ptr()
+    if (other := _device(x, lambda: layer_norm(x, weight, bias, eps))) is not None:
+        return other
+    device = x.device
+    p, ld = _rows(x)
+    y = torch.empty(shape, dtype=x.dtype, device=device)
+    mean = torch.empty(shape[:-1], dtype=torch.float32, device=device)
+    rstd = torch.empty_like(mean)
+    _done(lib().ones_layer_norm(p.data_ptr(), ld, wp, bp, p.shape[0], cols, eps, kind, wkind, y.data_ptr(), cols, mean.data_ptr(),
+                                rstd.data_ptr(), _stream_of(device.index)), "ones_layer_norm")
+    return y, mean, rstd
 
 
 def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, weight=None, *,
                         parameters: bool = True):
     """Gradients of `layer_norm` (``ones_layer_norm_backward``): (dx, dweight, dbias), the latter two in the type of
     weight (float32 where it is None), or None both with parameters=False."""
-    _need(x.is_cuda and x.dtype in _TYPES and x.dim() >= 1, "x: a float32, bfloat16 or float16 CUDA tensor is needed")
-    _need(dy.shape == x.shape and dy.dtype == x.dtype and dy.device == x.device, "dy needs x's shape, type and device")
+    kind = _TYPES.get(x.dtype)
+    _need(kind is not None and x.is_cuda and x.dim() >= 1, "x: a float32, bfloat16 or float16 CUDA tensor is needed")
+    _need(dy.shape == x.shape and dy.dtype is x.dtype and dy.device == x.device, "dy needs x's shape, type and device")
     cols = x.shape[-1]
-    _param(weight, cols, x, "weight")
-    for s, name in ((mean, "mean"), (rstd, "rstd")):
-        _need(s.dtype == torch.float32 and s.device == x.device and s.numel() * cols == x.numel() and s.is_contiguous(),
-              f"{name}: what layer_norm returned is needed")
-    with _on(x):
-        p, ld = _rows(_flat(x))
-        q, ldq = _rows(_flat(dy))
-        rows = p.shape[0]
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        wt = torch.float32 if weight is None else weight.dtype
-        dw = db = space = None
-        nbytes = 0
-        if parameters:
-            both = torch.empty((2, cols), dtype=wt, device=x.device)
-            dw, db = both[0], both[1]
-            nbytes = int(lib().ones_layer_norm_workspace_bytes(rows, cols))
-            space = _space(nbytes, x.device)
-        _done(lib().ones_layer_norm_backward(q.data_ptr(), ldq, p.data_ptr(), ld, mean.data_ptr(), rstd.data_ptr(), _ptr(weight),
-                                             rows, cols, _TYPES[x.dtype], _TYPES[wt], dx.data_ptr(), cols, _ptr(dw), _ptr(db),
-                                             _ptr(space), nbytes, _stream()), "ones_layer_norm_backward")
+    wt, wp = torch.float32, None
+    if weight is not None:
+        _param(weight, cols, x, "weight")
+        wt, wp = weight.dtype, weight.data_ptr()
+    for s in (mean, rstd):
+        _need(s.dtype is torch.float32 and s.device == x.device and s.shape == x.shape[:-1] and s.is_contiguous(),
+              "mean, rstd: what layer_norm returned is needed")
+    if (other := _device(x, lambda: layer_norm_backward(dy, x, mean, rstd, weight, parameters=parameters))) is not None:
+        return other
+    device = x.device
+    p, ld = _rows(x)
+    q, ldq = _rows(dy)
+    rows = p.shape[0]
+    dx = torch.empty(x.shape, dtype=x.dtype, device=device)
+    dw = db = dwp = dbp = sp = None
+    nbytes = 0
+    if parameters:
+        dw = torch.empty(cols, dtype=wt, device=device)
+        db = torch.empty_like(dw)
+        nbytes = lib().ones_layer_norm_workspace_bytes(rows, cols)
+        space = _space(nbytes, device)
+        dwp, dbp, sp = dw.data_ptr(), db.data_ptr(), space.data_ptr()
+    _done(lib().ones_layer_norm_backward(q.data_ptr(), ldq, p.data_ptr(), ld, mean.data_ptr(), rstd.data_ptr(), wp, rows, cols, kind,
+                                         _TYPES[wt], dx.data_ptr(), cols, dwp, dbp, sp, nbytes, _stream_of(device.index)),
+          "ones_layer_norm_backward")
     return dx, dw, db
 
 
 def _ce_args(hidden, weight, target):
-    _need(hidden.is_cuda and hidden.dtype in (torch.bfloat16, torch.float16) and hidden.dim() >= 1,
+    _need(hidden.is_cuda and (hidden.dtype is torch.bfloat16 or hidden.dtype is torch.float16) and hidden.dim() >= 1,
           "hidden: a bfloat16 or float16 CUDA tensor is needed")
-    _need(weight.dim() == 2 and weight.dtype == hidden.dtype and weight.device == hidden.device and
+    _need(weight.dim() == 2 and weight.dtype is hidden.dtype and weight.device == hidden.device and
           weight.shape[1] == hidden.shape[-1], "weight: [vocab][cols] of hidden's type and device is needed")
-    _need(target.dtype == torch.int64 and target.device == hidden.device and target.shape == hidden.shape[:-1],
+    _need(target.dtype is torch.int64 and target.device == hidden.device and target.shape == hidden.shape[:-1],
           "target: int64 with hidden's leading dimensions is needed")
 
 
@@ -180,17 +184,21 @@ def linear_cross_entropy(hidden: torch.Tensor, weight: torch.Tensor, target: tor
     """Cross entropy of ``hidden @ weight.T`` at `target` without keeping the logits (``ones_linear_ce``): (loss, lse),
     float32 with hidden's leading dimensions.  Rows whose target is outside [0, vocab) have loss 0."""
     _ce_args(hidden, weight, target)
-    with _on(hidden):
-        h, ldh = _rows(_flat(hidden), 8)
-        w, ldw = _rows(weight, 8)
-        t = target.contiguous()
-        rows, cols, vocab = t.numel(), hidden.shape[-1], weight.shape[0]
-        out = torch.empty((2, rows), dtype=torch.float32, device=hidden.device)
-        nbytes = int(lib().ones_linear_ce_workspace_bytes(rows, vocab))
-        space = _space(nbytes, hidden.device)
-        _done(lib().ones_linear_ce(h.data_ptr(), ldh, w.data_ptr(), ldw, t.data_ptr(), rows, cols, vocab, _TYPES[hidden.dtype],
-                                   out[0].data_ptr(), out[1].data_ptr(), space.data_ptr(), nbytes, _stream()), "ones_linear_ce")
-    return out[0].view(target.shape), out[1].view(target.shape)
+    if (other := _device(hidden, lambda: linear_cross_entropy(hidden, weight, target))) is not None:
+        return other
+    device = hidden.device
+    h, ldh = _rows(hidden, 8)
+    w, ldw = _rows(weight, 8)
+    t = target.contiguous()
+    rows, vocab = h.shape[0], weight.shape[0]
+    loss = torch.empty(target.shape, dtype=torch.float32, device=device)
+    lse = torch.empty_like(loss)
+    nbytes = lib().ones_linear_ce_workspace_bytes(rows, vocab)
+    space = _space(nbytes, device)
+    _done(lib().ones_linear_ce(h.data_ptr(), ldh, w.data_ptr(), ldw, t.data_ptr(), rows, hidden.shape[-1], vocab,
+                               _TYPES[hidden.dtype], loss.data_ptr(), lse.data_ptr(), space.data_ptr(), nbytes,
+                               _stream_of(device.index)), "ones_linear_ce")
+    return loss, lse
 
 
 def linear_cross_entropy_backward(dloss: torch.Tensor, hidden: torch.Tensor, weight: torch.Tensor, target: torch.Tensor,
@@ -200,51 +208,56 @@ def linear_cross_entropy_backward(dloss: torch.Tensor, hidden: torch.Tensor, wei
     vocabulary that are taken at a time (a multiple of 256; 0: the library's choice)."""
     _ce_args(hidden, weight, target)
     wt = weight_gradient or weight.dtype
-    _need(wt in (torch.float32, weight.dtype), "weight_gradient: float32 or weight's type is needed")
-    for s, name in ((dloss, "dloss"), (lse, "lse")):
-        _need(s.dtype == torch.float32 and s.device == hidden.device and s.shape == target.shape,
-              f"{name}: float32 with target's shape is needed")
-    with _on(hidden):
-        h, ldh = _rows(_flat(hidden), 8)
-        w, ldw = _rows(weight, 8)
-        t, g, l = target.contiguous(), dloss.contiguous(), lse.contiguous()
-        rows, cols, vocab = t.numel(), hidden.shape[-1], weight.shape[0]
-        dh = torch.empty(hidden.shape, dtype=hidden.dtype, device=hidden.device)
-        dw = torch.empty(weight.shape, dtype=wt, device=hidden.device)
-        nbytes = int(lib().ones_linear_ce_backward_workspace_bytes(rows, cols, vocab, piece))
-        space = _space(nbytes, hidden.device)
-        _done(lib().ones_linear_ce_backward(g.data_ptr(), h.data_ptr(), ldh, w.data_ptr(), ldw, t.data_ptr(), l.data_ptr(),
-                                            rows, cols, vocab, _TYPES[hidden.dtype], _TYPES[wt], piece, dh.data_ptr(), cols,
-                                            dw.data_ptr(), cols, space.data_ptr(), nbytes, _stream()),
-              "ones_linear_ce_backward")
+    _need(wt is torch.float32 or wt is weight.dtype, "weight_gradient: float32 or weight's type is needed")
+    for s in (dloss, lse):
+        _need(s.dtype is torch.float32 and s.device == hidden.device and s.shape == target.shape,
+              "dloss, lse: float32 with target's shape is needed")
+    if (other := _device(hidden, lambda: linear_cross_entropy_backward(dloss, hidden, weight, target, lse,
+                                                                       weight_gradient=weight_gradient, piece=piece))) is not None:
+        return other
+    device = hidden.device
+    h, ldh = _rows(hidden, 8)
+    w, ldw = _rows(weight, 8)
+    t, g, l = target.contiguous(), dloss.contiguous(), lse.contiguous()
+    rows, cols, vocab = h.shape[0], hidden.shape[-1], weight.shape[0]
+    dh = torch.empty(hidden.shape, dtype=hidden.dtype, device=device)
+    dw = torch.empty(weight.shape, dtype=wt, device=device)
+    nbytes = lib().ones_linear_ce_backward_workspace_bytes(rows, cols, vocab, piece)
+    space = _space(nbytes, device)
+    _done(lib().ones_linear_ce_backward(g.data_ptr(), h.data_ptr(), ldh, w.data_ptr(), ldw, t.data_ptr(), l.data_ptr(), rows, cols,
+                                        vocab, _TYPES[hidden.dtype], _TYPES[wt], piece, dh.data_ptr(), cols, dw.data_ptr(), cols,
+                                        space.data_ptr(), nbytes, _stream_of(device.index)), "ones_linear_ce_backward")
     return dh, dw
 
 
 def orthogonalize(g: torch.Tensor, *, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7) -> torch.Tensor:
     """Newton-Schulz orthogonalised update (``ones_orthogonalize``) of a matrix [m][n], or of several [count][m][n], in
     bfloat16."""
-    _need(g.is_cuda and g.dtype in _TYPES and g.dim() in (2, 3), "g: a float32, bfloat16 or float16 CUDA matrix is needed, or several")
+    kind = _TYPES.get(g.dtype)
+    _need(kind is not None and g.is_cuda and g.dim() in (2, 3), "g: a float32, bfloat16 or float16 CUDA matrix is needed, or several")
     a, b, c = coefficients
-    with _on(g):
-        s = g if g.dim() == 3 else g[None]
-        count, m, n = s.shape
-        if (s.stride(2) != 1 and n > 1) or (s.stride(1) < n and m > 1) or s.stride(0) < 0:
-            s = s.contiguous()
-        out = torch.empty(g.shape, dtype=torch.bfloat16, device=g.device)
-        if out.numel() == 0:
-            return out
-        nbytes = int(lib().ones_orthogonalize_workspace_bytes(count, m, n))
-        if nbytes == 0:
-            raise _b.OnesError(-3, "ones_orthogonalize_workspace_bytes")
-        space = _space(nbytes, g.device)
-        _done(lib().ones_orthogonalize(s.data_ptr(), s.stride(1) if m > 1 else n, s.stride(0), count, m, n, _TYPES[g.dtype], steps,
-                                       a, b, c, eps, out.data_ptr(), space.data_ptr(), nbytes, _stream()), "ones_orthogonalize")
+    if (other := _device(g, lambda: orthogonalize(g, steps=steps, coefficients=coefficients, eps=eps))) is not None:
+        return other
+    device = g.device
+    s = g if g.dim() == 3 else g[None]
+    count, m, n = s.shape
+    if (s.stride(2) != 1 and n > 1) or (s.stride(1) < n and m > 1):
+        s = s.contiguous()
+    out = torch.empty(g.shape, dtype=torch.bfloat16, device=device)
+    if count * m * n == 0:
+        return out
+    nbytes = lib().ones_orthogonalize_workspace_bytes(count, m, n)
+    if nbytes == 0:
+        raise _b.OnesError(-3, "ones_orthogonalize_workspace_bytes")
+    space = _space(nbytes, device)
+    _done(lib().ones_orthogonalize(s.data_ptr(), s.stride(1) if m > 1 else n, s.stride(0), count, m, n, kind, steps, a, b, c, eps,
+                                   out.data_ptr(), space.data_ptr(), nbytes, _stream_of(device.index)), "ones_orthogonalize")
     return out
 
 
 def check() -> None:
     """Waits for the current stream and raises if a kernel gave up waiting since the last check (``ones_train_status``)."""
-    _done(lib().ones_train_status(_stream()), "ones_train_status")
+    _done(lib().ones_train_status(torch.cuda.current_stream().cuda_stream), "ones_train_status")
 
 
 class _LayerNorm(torch.autograd.Function):
