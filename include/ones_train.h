@@ -64,11 +64,12 @@ int ones_linear_ce(const void* d_hidden, int64_t ldh, const void* d_weight, int6
 /* Its gradients for the gradient d_dloss float[rows] of the loss and the lse of the forward call:
  *   dlogits[i][v] = (exp(logits[i][v] - lse[i]) - [v == target[i]]) * dloss[i]   (0 in rows that take no part),
  *   dhidden = dlogits * weight,   dweight = dlogits^T * hidden.
- * The vocabulary is taken in pieces of `piece` entries (a multiple of 256; 0: a default that keeps the piece's
+ * Rows that take no part cost next to nothing: the others are gathered first, so nothing of them, not even a NaN in
+ * hidden, reaches dweight.  The vocabulary is taken in pieces of `piece` entries (a multiple of 256; 0: a default that keeps the piece's
  * gradient near 256 MiB): the logits of a piece are computed again, and their gradient is kept in the workspace, as
  * 16 bits of `type` scaled by a power of two, until both products have used it.
  *   d_dhidden [rows][cols] of `type`; d_dweight [vocab][cols] of `wtype` (`type` or ONES_F32), any alignment of their
- *   elements (16-byte aligned rows are written faster); hidden and weight aligned as above.
+ *   elements (16-byte aligned rows are written faster), hidden too; weight aligned as above.
  *   d_workspace  at least ones_linear_ce_backward_workspace_bytes(rows, cols, vocab, piece) bytes. */
 size_t ones_linear_ce_backward_workspace_bytes(int32_t rows, int32_t cols, int32_t vocab, int32_t piece);
 int ones_linear_ce_backward(const float* d_dloss, const void* d_hidden, int64_t ldh, const void* d_weight, int64_t ldw,

@@ -74,71 +74,93 @@ struct EpiStats {
     }
 };
 
+// What the backward pass knows of a row that takes part, in the order in which such rows were gathered.
+struct RowInfo {
+    int target;   // entry of the vocabulary
+    float shift;  // -lse / ln 2
+    float g;      // dloss * scale
+    int row;      // of the caller
+};
+
 // Gradient of a piece's logits, as 16 bits: (exp(l - lse) - [target]) * dloss * scale.
 struct EpiDlogits {
     struct Args {
-        const int64_t* target;
-        const float *lse, *dloss, *scale;
+        const RowInfo* info;
         uint16_t* out;
         int64_t ld;
-        int rows, vocab, first, cols;  // the piece: `cols` entries from `first`
+        int rows, first, cols;  // the piece: `cols` entries from `first`
         bool f16;
     };
     template <int W>
     static __device__ __forceinline__ void tile(const Args& a, const MatShape& shape, uint32_t acc, int row, int col,
                                                 const TileAt&, int, const Turn& turn) {
         const float to2 = kLog2e * regain(shape.K);
-        const int64_t t64 = row < a.rows ? a.target[row] : -1;
-        const bool live = t64 >= 0 && t64 < a.vocab;
-        const int t = live ? (int)(t64 - a.first) : -1;
-        const float g = live ? a.dloss[row] * *a.scale : 0.f;
-        const float shift = live ? -a.lse[row] * kLog2e : 0.f;
+        const bool live = row < shape.M;
+        RowInfo r = {-1, 0.f, 0.f, 0};
+        if (live) r = a.info[row];
+        const int t = r.target - a.first;
+        // the product with the hidden rows runs over whole stages of rows: those after the last one are zero
+        const int rows = min(a.rows, (shape.M + kTileK - 1) / kTileK * kTileK);
 #pragma unroll 1
         for (int c = 0; c < W && col + c < a.cols; c += 64) {
             float v[64];
             tmem_load(acc + c, v);
 #pragma unroll
             for (int i = 0; i < 64; ++i) {
-                const float p = exp2_fast(fmaf(v[i], to2, shift));
-                v[i] = live ? p * g : 0.f;
+                const float p = exp2_fast(fmaf(v[i], to2, r.shift));
+                v[i] = live ? p * r.g : 0.f;
             }
             const unsigned at_i = (unsigned)(t - (col + c));
-            if (at_i < 64u) {
+            if (live && at_i < 64u) {
 #pragma unroll
                 for (int i = 0; i < 64; ++i)
-                    if (at_i == (unsigned)i) v[i] -= g;
+                    if (at_i == (unsigned)i) v[i] -= r.g;
             }
             turn.put16(v, a.f16);
-            turn.store16(a.out, a.ld, row - turn.lane, col + c, a.rows, a.cols, true);
+            turn.store16(a.out, a.ld, row - turn.lane, col + c, rows, a.cols, true);
         }
     }
 };
 
-// Sum over the pieces: the product is added to (first piece: put into) 32-bit sums; the last piece rounds them.
+__device__ __forceinline__ void store_grad4(uint16_t* out, float4 f, int left, bool f16, bool wide) {
+    const uint32_t lo = Half16::pack(f.x, f.y, f16), hi = Half16::pack(f.z, f.w, f16);
+    if (wide && left >= 4) {
+        *reinterpret_cast<uint2*>(out) = make_uint2(lo, hi);
+    } else {
+        if (left > 0) out[0] = (uint16_t)lo;
+        if (left > 1) out[1] = (uint16_t)(lo >> 16);
+        if (left > 2) out[2] = (uint16_t)hi;
+        if (left > 3) out[3] = (uint16_t)(hi >> 16);
+    }
+}
+
+// Sum over the pieces: the product is added to (first piece: put into) 32-bit sums; the last piece rounds them into the
+// caller's rows, unless the sums come in several parts (k_ce_rows joins those).
 struct EpiSum {
     struct Args {
-        float* sum;
+        float* sum;  // [parts][rows][ld_sum]
         int64_t ld_sum;
         uint16_t* out;
         int64_t ld_out;
         const float* scale;
+        const RowInfo* info;
         int rows, cols;
         bool first, last, f16, wide;
     };
     template <int W>
-    static __device__ __forceinline__ void tile(const Args& a, const MatShape&, uint32_t acc, int row, int col,
-                                                const TileAt&, int, const Turn& turn) {
+    static __device__ __forceinline__ void tile(const Args& a, const MatShape& shape, uint32_t acc, int row, int col,
+                                                const TileAt& at, int, const Turn& turn) {
         const float unscale = a.last ? 1.f / *a.scale : 1.f;  // a power of two
         const int r0 = row - turn.lane + turn.lane / 8, k = turn.lane & 7;
 #pragma unroll 1
         for (int c = 0; c < W && col + c < a.cols; c += 32) {
             const int at_col = col + c + 4 * k, left = a.cols - at_col;
-            float* sum = a.sum + (int64_t)r0 * a.ld_sum + at_col;  // has whole chunks of 32 columns
+            float* sum = a.sum + ((int64_t)at.b * a.rows + r0) * a.ld_sum + at_col;  // has whole chunks of 32 columns
             float4 old[8];
             if (!a.first) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (r0 + 4 * i < a.rows) old[i] = *reinterpret_cast<const float4*>(sum + 4 * i * a.ld_sum);
+                    if (r0 + 4 * i < shape.M) old[i] = *reinterpret_cast<const float4*>(sum + 4 * i * a.ld_sum);
             }
             float v[32];
             tmem_load(acc + c, v);
@@ -148,21 +170,13 @@ struct EpiSum {
                 const uint4 q = turn.chunk(4 * i + turn.lane / 8, k);
                 float4 f = make_float4(__uint_as_float(q.x), __uint_as_float(q.y), __uint_as_float(q.z), __uint_as_float(q.w));
                 if (!a.first) f.x += old[i].x, f.y += old[i].y, f.z += old[i].z, f.w += old[i].w;
-                if (r0 + 4 * i >= a.rows) continue;
+                if (r0 + 4 * i >= shape.M) continue;
                 if (!a.last) {
                     *reinterpret_cast<float4*>(sum + 4 * i * a.ld_sum) = f;
                     continue;
                 }
-                uint16_t* out = a.out + (int64_t)(r0 + 4 * i) * a.ld_out + at_col;
-                const uint32_t lo = Half16::pack(f.x * unscale, f.y * unscale, a.f16), hi = Half16::pack(f.z * unscale, f.w * unscale, a.f16);
-                if (a.wide && left >= 4) {
-                    *reinterpret_cast<uint2*>(out) = make_uint2(lo, hi);
-                } else {
-                    if (left > 0) out[0] = (uint16_t)lo;
-                    if (left > 1) out[1] = (uint16_t)(lo >> 16);
-                    if (left > 2) out[2] = (uint16_t)hi;
-                    if (left > 3) out[3] = (uint16_t)(hi >> 16);
-                }
+                f.x *= unscale, f.y *= unscale, f.z *= unscale, f.w *= unscale;
+                store_grad4(a.out + (int64_t)a.info[r0 + 4 * i].row * a.ld_out + at_col, f, left, a.f16, a.wide);
             }
         }
     }
@@ -178,16 +192,17 @@ struct EpiGrad {
         bool f32, f16, wide;
     };
     template <int W>
-    static __device__ __forceinline__ void tile(const Args& a, const MatShape&, uint32_t acc, int row, int col,
+    static __device__ __forceinline__ void tile(const Args& a, const MatShape& shape, uint32_t acc, int row, int col,
                                                 const TileAt&, int, const Turn& turn) {
         const float unscale = 1.f / *a.scale;
+        const bool none = shape.K == 0;  // no row takes part: nothing was multiplied
         const int row0 = row - turn.lane;
 #pragma unroll 1
         for (int c = 0; c < W && col + c < a.cols; c += 64) {
             float v[64];
             tmem_load(acc + c, v);
 #pragma unroll
-            for (int i = 0; i < 64; ++i) v[i] *= unscale;
+            for (int i = 0; i < 64; ++i) v[i] = none ? 0.f : v[i] * unscale;
             if (a.f32) {
                 float u[32];
 #pragma unroll
@@ -205,8 +220,9 @@ struct EpiGrad {
     }
 };
 
-// Joins the slots of a row. 4 rows x 128 threads a block: a warp reads whole 32-byte sectors.
-constexpr int kJoinRows = 4, kJoinThreads = 512;
+// Joins the slots of a row: R rows a block, 512 / R threads on a row's slots, 8 slots on their way at a time. With few
+// rows R = 4 (a warp reads whole 32-byte sectors) brings more threads to a row, else R = 32.
+constexpr int kJoinThreads = 512;
 
 __device__ __forceinline__ float2 join(float2 a, float2 b) {
     const float m = fmaxf(a.x, b.x);
@@ -214,22 +230,35 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
     return make_float2(m, a.y * exp2_fast(fmaf(a.x, kLog2e, shift)) + b.y * exp2_fast(fmaf(b.x, kLog2e, shift)));
 }
 
+template <int R>
 __global__ void __launch_bounds__(kJoinThreads) k_ce_join(const float2* part, int slots, const float* at_target, const int64_t* target,
                                                           int rows, int vocab, float* loss, float* lse) {
     wait_for_predecessor();
     __shared__ float2 s[kJoinThreads];
-    const int r = threadIdx.x % kJoinRows, row = blockIdx.x * kJoinRows + r;
+    const int r = threadIdx.x % R, row = blockIdx.x * R + r;
     float2 v = make_float2(-INFINITY, 0.f);
     if (row < rows) {
-        for (int i = threadIdx.x / kJoinRows; i < slots; i += kJoinThreads / kJoinRows) v = join(v, part[(int64_t)i * rows + row]);
+        constexpr int kStep = kJoinThreads / R;
+        for (int i = threadIdx.x / R; i < slots; i += 8 * kStep) {
+            float2 q[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                q[j] = i + j * kStep < slots ? part[(int64_t)(i + j * kStep) * rows + row] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+            for (int d = 4; d; d /= 2) {
+#pragma unroll
+                for (int j = 0; j < d; ++j) q[j] = join(q[j], q[j + d]);
+            }
+            v = join(v, q[0]);
+        }
     }
     s[threadIdx.x] = v;
     __syncthreads();
-    for (int n = kJoinThreads / 2; n >= kJoinRows; n /= 2) {
+    for (int n = kJoinThreads / 2; n >= R; n /= 2) {
         if ((int)threadIdx.x < n) s[threadIdx.x] = v = join(v, s[threadIdx.x + n]);
         __syncthreads();
     }
-    if ((int)threadIdx.x < kJoinRows && row < rows) {
+    if ((int)threadIdx.x < R && row < rows) {
         const float l = v.x + logf(v.y);
         const int64_t t = target[row];
         lse[row] = l;
@@ -237,27 +266,125 @@ __global__ void __launch_bounds__(kJoinThreads) k_ce_join(const float2* part, in
     }
 }
 
-// The power of two that brings the largest |dloss| of the rows that take part into [1, 2), so that the 16-bit gradients
-// of the logits neither overflow nor lose their small values, whatever the scale of the loss.
-__global__ void __launch_bounds__(1024) k_ce_scale(const float* dloss, const int64_t* target, int rows, int vocab, float* scale) {
-    __shared__ float s[32];
+struct Header {
+    int live;     // rows that take part
+    float scale;  // see below
+};
+
+// Finds the rows that take part, in order, and the power of two that brings their largest |dloss| into [1, 2), so that
+// the 16-bit gradients of the logits neither overflow nor lose their small values, whatever the scale of the loss.
+constexpr int kScan = 4;
+__global__ void __launch_bounds__(1024) k_ce_scan(const float* dloss, const int64_t* target, int rows, int vocab, RowInfo* info, Header* head) {
+    __shared__ int s_count[32];
+    __shared__ float s_top[32];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     float top = 0.f;
-    for (int i = threadIdx.x; i < rows; i += 1024) {
-        const int64_t t = target[i];
-        if (t >= 0 && t < vocab) top = fmaxf(top, fabsf(dloss[i]));
+    int base = 0;
+    for (int r0 = 0; r0 < rows; r0 += 1024 * kScan) {
+        const int first = r0 + threadIdx.x * kScan;
+        bool in[kScan];
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < kScan; ++i) {
+            const int64_t t = first + i < rows ? target[first + i] : -1;
+            in[i] = t >= 0 && t < vocab;
+            n += in[i];
+            if (in[i]) top = fmaxf(top, fabsf(dloss[first + i]));
+        }
+        int up_to = n;
+        for (int o = 1; o < 32; o *= 2) {
+            const int u = __shfl_up_sync(0xFFFFFFFFu, up_to, o);
+            if (lane >= o) up_to += u;
+        }
+        if (lane == 31) s_count[warp] = up_to;
+        __syncthreads();
+        int before = 0, all = 0;
+        for (int w = 0; w < 32; ++w) {
+            if (w < warp) before += s_count[w];
+            all += s_count[w];
+        }
+        int at = base + before + up_to - n;
+#pragma unroll
+        for (int i = 0; i < kScan; ++i)
+            if (in[i]) info[at++].row = first + i;
+        base += all;
+        __syncthreads();
     }
     for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-    if (threadIdx.x % 32 == 0) s[threadIdx.x / 32] = top;
+    if (lane == 0) s_top[warp] = top;
     __syncthreads();
     if (threadIdx.x < 32) {
-        top = s[threadIdx.x];
+        top = s_top[threadIdx.x];
         for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
         if (threadIdx.x == 0) {
             const int e = top > 0.f && top < INFINITY ? ilogbf(top) : 0;
-            *scale = exp2f((float)(e < -100 ? 100 : e > 100 ? -100 : -e));
+            head->scale = exp2f((float)(e < -100 ? 100 : e > 100 ? -100 : -e));
+            head->live = base;
         }
     }
     let_successor_start();
+}
+
+// Gathers the hidden rows that take part (and zeros up to a whole stage of rows), what the other kernels need to know of
+// them, and clears the gradients of the rows that take none. A warp takes a row at a time.
+__global__ void __launch_bounds__(256) k_ce_gather(const uint16_t* hidden, int64_t ldh, const int64_t* target, const float* dloss,
+                                                   const float* lse, int rows, int cols, int vocab, const Header* head, RowInfo* info,
+                                                   uint16_t* out, int64_t ld_out, uint16_t* dhidden, int64_t lddh, bool wide_in, bool wide_dh) {
+    wait_for_predecessor();
+    let_successor_start();
+    const int lane = threadIdx.x % 32, live = head->live;
+    const float scale = head->scale;
+    const int padded = min(rows, (live + kTileK - 1) / kTileK * kTileK);
+    for (int i = blockIdx.x * 8 + threadIdx.x / 32; i < rows; i += gridDim.x * 8) {
+        if (i < padded) {
+            uint16_t* to = out + (int64_t)i * ld_out;
+            const int row = i < live ? info[i].row : -1;
+            const uint16_t* from = hidden + (int64_t)row * ldh;
+            const int whole = wide_in || row < 0 ? cols / 8 : 0;  // ld_out is a multiple of 8
+            for (int c = lane; c < whole; c += 32)
+                reinterpret_cast<uint4*>(to)[c] = row >= 0 ? reinterpret_cast<const uint4*>(from)[c] : make_uint4(0, 0, 0, 0);
+            for (int c = whole * 8 + lane; c < cols; c += 32) to[c] = row >= 0 ? from[c] : 0;
+            __syncwarp();
+            if (lane == 0 && row >= 0) {
+                RowInfo r;
+                r.target = (int)target[row];
+                r.shift = -lse[row] * kLog2e;
+                r.g = dloss[row] * scale;
+                r.row = row;
+                info[i] = r;
+            }
+        }
+        const int64_t t = target[i];
+        if (t < 0 || t >= vocab) {
+            uint16_t* to = dhidden + (int64_t)i * lddh;
+            const int whole = wide_dh ? cols / 8 : 0;
+            for (int c = lane; c < whole; c += 32) reinterpret_cast<uint4*>(to)[c] = make_uint4(0, 0, 0, 0);
+            for (int c = whole * 8 + lane; c < cols; c += 32) to[c] = 0;
+        }
+    }
+}
+
+// Joins the parts of the sums over the vocabulary, in order, and rounds them into the caller's rows. A warp takes a row.
+__global__ void __launch_bounds__(256) k_ce_rows(const float* sum, int parts, int64_t ld_sum, int rows, int cols, const Header* head,
+                                                 const RowInfo* info, uint16_t* out, int64_t ld_out, bool f16, bool wide) {
+    wait_for_predecessor();
+    const int lane = threadIdx.x % 32;
+    const float unscale = 1.f / head->scale;
+    const int64_t part = (int64_t)rows * ld_sum;
+    for (int i = blockIdx.x * 8 + threadIdx.x / 32; i < head->live; i += gridDim.x * 8) {
+        const float* p = sum + (int64_t)i * ld_sum;
+        uint16_t* to = out + (int64_t)info[i].row * ld_out;
+        for (int c = lane * 4; c < cols; c += 128) {
+            float4 f = *reinterpret_cast<const float4*>(p + c);
+#pragma unroll 4
+            for (int k = 1; k < parts; ++k) {
+                const float4 q = *reinterpret_cast<const float4*>(p + k * part + c);
+                f.x += q.x, f.y += q.y, f.z += q.z, f.w += q.w;
+            }
+            f.x *= unscale, f.y *= unscale, f.z *= unscale, f.w *= unscale;
+            store_grad4(to + c, f, cols - c, f16, wide);
+        }
+    }
 }
 
 inline size_t up(size_t x, size_t a) { return (x + a - 1) / a * a; }
@@ -289,18 +416,29 @@ int32_t piece_of(int32_t rows, int32_t vocab, int32_t piece) {
 }
 
 struct BackwardLayout {
-    size_t scale, dlogits, sum, total;
-    int64_t ld_sum;
+    size_t head, info, hidden, dlogits, sum, total;
+    int64_t ld_sum, ld_hidden;
     int32_t piece;
+    Cut cut;  // of the product over a piece of the vocabulary
 };
 BackwardLayout backward_layout(int32_t rows, int32_t cols, int32_t vocab, int32_t piece) {
     BackwardLayout L;
     L.piece = piece_of(rows, vocab, piece);
+    L.cut = cut_of(rows, cols, vocab < L.piece ? vocab : L.piece);
     L.ld_sum = (int64_t)up(cols, 32);
-    L.scale = 0;
-    L.dlogits = 256;
-    L.sum = up(L.dlogits + (size_t)rows * L.piece * 2, 256);
-    L.total = up(L.sum + (L.piece < vocab ? (size_t)rows * L.ld_sum * 4 : 0), 256);
+    L.ld_hidden = (int64_t)up(cols, 8);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at = up(at + bytes, 256);
+        return here;
+    };
+    L.head = take(sizeof(Header));
+    L.info = take((size_t)rows * sizeof(RowInfo));
+    L.hidden = take((size_t)rows * L.ld_hidden * 2);
+    L.dlogits = take((size_t)rows * L.piece * 2);
+    L.sum = take(L.piece < vocab || L.cut.splits > 1 ? (size_t)L.cut.splits * rows * L.ld_sum * 4 : 0);
+    L.total = at;
     return L;
 }
 
@@ -346,8 +484,9 @@ int ones_linear_ce(const void* d_hidden, int64_t ldh, const void* d_weight, int6
     const Operand h = {d_hidden, ldh, 0, false}, w = {d_weight, ldw, 0, false};
     const EpiStats::Args ea = {d_target, part, at_target, rows, vocab};
     cudaError_t err = launch_matmul<false, false, EpiStats>(h, w, rows, vocab, cols, 1, false, type == ONES_F16, ea, stream, false);
+    const int r = rows > 4 * kSms ? 32 : 4;
     if (err == cudaSuccess)
-        err = launch_after(k_ce_join, dim3((rows + kJoinRows - 1) / kJoinRows), dim3(kJoinThreads), stream, part,
+        err = launch_after(r == 32 ? k_ce_join<32> : k_ce_join<4>, dim3((rows + r - 1) / r), dim3(kJoinThreads), stream, part,
                            slots_of(rows, vocab), at_target, d_target, rows, vocab, d_loss, d_lse);
     return err == cudaSuccess ? ONES_OK : ONES_ERR_CUDA;
 }
@@ -372,37 +511,48 @@ int ones_linear_ce_backward(const float* d_dloss, const void* d_hidden, int64_t 
     }
     if (!d_dloss || !d_hidden || !d_weight || !d_target || !d_lse || !d_dhidden || !d_workspace) return ONES_ERR_NULL;
     const size_t wsize = wtype == ONES_F32 ? 4 : 2;
-    if (!aligned(d_hidden, 16) || !aligned(d_weight, 16) || ldh % 8 || ldw % 8 || !aligned(d_dhidden, 2) ||
+    if (!aligned(d_hidden, 2) || !aligned(d_weight, 16) || ldw % 8 || !aligned(d_dhidden, 2) ||
         !aligned(d_dweight, wsize) || !aligned(d_workspace, 256))
         return ONES_ERR_ALIGN;
     const BackwardLayout L = backward_layout(rows, cols, vocab, piece);
     if (workspace_bytes < L.total) return ONES_ERR_WORKSPACE;
     char* ws = static_cast<char*>(d_workspace);
-    float* scale = reinterpret_cast<float*>(ws + L.scale);
+    Header* head = reinterpret_cast<Header*>(ws + L.head);
+    RowInfo* info = reinterpret_cast<RowInfo*>(ws + L.info);
+    uint16_t* hidden = reinterpret_cast<uint16_t*>(ws + L.hidden);
     uint16_t* dl = reinterpret_cast<uint16_t*>(ws + L.dlogits);
     float* sum = reinterpret_cast<float*>(ws + L.sum);
+    uint16_t* dh = static_cast<uint16_t*>(d_dhidden);
     const bool f16 = type == ONES_F16;
     const bool wide_h = aligned(d_dhidden, 16) && lddh % 8 == 0, wide_w = aligned(d_dweight, 16) && lddw % 8 == 0;
+    const bool wide_in = aligned(d_hidden, 16) && ldh % 8 == 0;
+    const unsigned row_blocks = (unsigned)((rows + 7) / 8 < 8 * kSms ? (rows + 7) / 8 : 8 * kSms);
 
-    k_ce_scale<<<1, 1024, 0, stream>>>(d_dloss, d_target, rows, vocab, scale);
+    k_ce_scan<<<1, 1024, 0, stream>>>(d_dloss, d_target, rows, vocab, info, head);
     cudaError_t err = cudaGetLastError();
+    if (err == cudaSuccess)
+        err = launch_after(k_ce_gather, dim3(row_blocks), dim3(256), stream, static_cast<const uint16_t*>(d_hidden), ldh, d_target, d_dloss,
+                           d_lse, rows, cols, vocab, static_cast<const Header*>(head), info, hidden, L.ld_hidden, dh, lddh, wide_in, wide_h);
     for (int32_t v0 = 0; err == cudaSuccess && v0 < vocab; v0 += L.piece) {
         const int32_t n = vocab - v0 < L.piece ? vocab - v0 : L.piece;
+        const bool last = v0 + n == vocab;
         const uint16_t* w0 = static_cast<const uint16_t*>(d_weight) + (int64_t)v0 * ldw;
-        const EpiDlogits::Args e1 = {d_target, d_lse, d_dloss, scale, dl, L.piece, rows, vocab, v0, n, f16};
-        err = launch_matmul<false, false, EpiDlogits>({d_hidden, ldh, 0, false}, {w0, ldw, 0, false}, rows, n, cols, 1, false,
-                                                      f16, e1, stream, true);
+        const EpiDlogits::Args e1 = {info, dl, L.piece, rows, v0, n, f16};
+        err = launch_matmul<false, false, EpiDlogits>({hidden, L.ld_hidden, 0, false}, {w0, ldw, 0, false}, rows, n, cols, 1, false,
+                                                      f16, e1, stream, true, &head->live);
         if (err != cudaSuccess) break;
-        const EpiSum::Args e2 = {sum, L.ld_sum, static_cast<uint16_t*>(d_dhidden), lddh, scale, rows, cols, v0 == 0,
-                                 v0 + n == vocab, f16, wide_h};
-        err = launch_matmul<false, true, EpiSum>({dl, L.piece, 0, false}, {w0, ldw, 0, true}, rows, cols, n, 1, false, f16, e2,
-                                                 stream, true);
+        const EpiSum::Args e2 = {sum, L.ld_sum, dh, lddh, &head->scale, info, rows, cols, v0 == 0, last && L.cut.splits == 1, f16, wide_h};
+        err = launch_matmul_cut<false, true, EpiSum>({dl, L.piece, 0, false}, {w0, ldw, 0, true}, rows, cols, n, L.cut, f16,
+                                                     e2, stream, true, &head->live);
         if (err != cudaSuccess) break;
-        const EpiGrad::Args e3 = {static_cast<char*>(d_dweight) + (int64_t)v0 * lddw * (int64_t)wsize, lddw, scale, n, cols,
+        const EpiGrad::Args e3 = {static_cast<char*>(d_dweight) + (int64_t)v0 * lddw * (int64_t)wsize, lddw, &head->scale, n, cols,
                                   wtype == ONES_F32, f16, wide_w};
-        err = launch_matmul<true, true, EpiGrad>({dl, L.piece, 0, true}, {d_hidden, ldh, 0, true}, n, cols, rows, 1, false, f16,
-                                                 e3, stream, true);
+        err = launch_matmul<true, true, EpiGrad>({dl, L.piece, 0, true}, {hidden, L.ld_hidden, 0, true}, n, cols, rows, 1, false, f16,
+                                                 e3, stream, true, nullptr, &head->live);
     }
+    if (err == cudaSuccess && L.cut.splits > 1)
+        err = launch_after(k_ce_rows, dim3(row_blocks), dim3(256), stream, static_cast<const float*>(sum), L.cut.splits, L.ld_sum, rows, cols,
+                           static_cast<const Header*>(head), static_cast<const RowInfo*>(info), dh, lddh, f16, wide_h);
     return err == cudaSuccess ? ONES_OK : ONES_ERR_CUDA;
 }
 

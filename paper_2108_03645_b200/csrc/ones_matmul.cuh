@@ -36,7 +36,9 @@ static __device__ unsigned g_wait_expired;
 struct MatShape {
     int M, N, K;
     int tiles_m, tiles_n, batch;
-    int sym;    // only tiles on and above the diagonal are computed (C is symmetric)
+    int splits;  // > 1: K is cut into so many parts, each with a C of its own in the place of a matrix of the batch
+    int sym;     // only tiles on and above the diagonal are computed (C is symmetric)
+    const int *live_m, *live_k;  // where M or K is known on the device only (at most the value above)
     int group;  // row tiles that run through the columns together, so that both operands' tiles are met again in L2
     uint32_t idesc;
 };
@@ -169,7 +171,7 @@ struct Turn {
 
 template <int CG, bool AMN, bool BMN, class Epi>
 __global__ void __launch_bounds__(kMatThreads, 1)
-    k_matmul(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MatShape g,
+    k_matmul(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MatShape shape,
              const typename Epi::Args ea) {
     constexpr int BN = 128 * CG;          // columns of a tile
     constexpr uint32_t kCols = 2 * BN;    // tensor-memory columns: two accumulators
@@ -177,7 +179,7 @@ __global__ void __launch_bounds__(kMatThreads, 1)
     __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_done[2], s_free[2];
     __shared__ uint32_t s_tmem;
 
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t full = smem_u32(s_full), empty = smem_u32(s_empty), done = smem_u32(s_done), free_ = smem_u32(s_free);
@@ -205,12 +207,15 @@ __global__ void __launch_bounds__(kMatThreads, 1)
     wait_for_predecessor();
     let_successor_start();
 
+    MatShape g = shape;
+    if (g.live_m) g.M = *g.live_m, g.tiles_m = (g.M + 128 * CG - 1) / (128 * CG);
+    if (g.live_k) g.K = *g.live_k;
     const int per = tiles_per_matrix(g), total = per * g.batch;
     const int first = blockIdx.x / CG, step = gridDim.x / CG;
-    const int nk = (g.K + kTileK - 1) / kTileK;
+    const int nk_all = (g.K + kTileK - 1) / kTileK, nk_part = (nk_all + g.splits - 1) / g.splits;
     bool ok = true;
 
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
         // fill the ring
         const uint32_t full_at = CG == 2 ? map_to_rank(full, 0) : full;  // the pair's bytes are counted on CTA 0's barrier
         int s = 0;
@@ -218,48 +223,56 @@ __global__ void __launch_bounds__(kMatThreads, 1)
         for (int t = first; ok && t < total; t += step) {
             const TileAt at = tile_at(g, t, per);
             const int am = at.m * 128 * CG + (int)rank * 128, bn = at.n * BN + (int)rank * 128;
-            for (int k = 0; k < nk; ++k) {
+            const int k0 = g.splits > 1 ? at.b * nk_part : 0, k1 = min(k0 + nk_part, nk_all), z = g.splits > 1 ? 0 : at.b;
+            if (g.splits > 1 && k0 >= k1) continue;  // nothing of K is left for this part
+            for (int k = k0; k < k1; ++k) {
                 if (!(ok = bar_wait(empty + 8 * s, ph ^ 1, &g_wait_expired))) break;
-                if (rank == 0) bar_expect(full + 8 * s, CG * kStageBytes);
                 const uint32_t a = base + s * kStageBytes, b = a + kHalf, bar = full_at + 8 * s;
-                if constexpr (AMN) {
-                    tma_load<CG>(a, &map_a, am, k * kTileK, at.b, bar);
-                    tma_load<CG>(a + kHalf / 2, &map_a, am + 64, k * kTileK, at.b, bar);
-                } else {
-                    tma_load<CG>(a, &map_a, k * kTileK, am, at.b, bar);
+                if (elect_one()) {
+                    if (rank == 0) bar_expect(full + 8 * s, CG * kStageBytes);
+                    if constexpr (AMN) {
+                        tma_load<CG>(a, &map_a, am, k * kTileK, z, bar);
+                        tma_load<CG>(a + kHalf / 2, &map_a, am + 64, k * kTileK, z, bar);
+                    } else {
+                        tma_load<CG>(a, &map_a, k * kTileK, am, z, bar);
+                    }
+                    if constexpr (BMN) {
+                        tma_load<CG>(b, &map_b, bn, k * kTileK, z, bar);
+                        tma_load<CG>(b + kHalf / 2, &map_b, bn + 64, k * kTileK, z, bar);
+                    } else {
+                        tma_load<CG>(b, &map_b, k * kTileK, bn, z, bar);
+                    }
                 }
-                if constexpr (BMN) {
-                    tma_load<CG>(b, &map_b, bn, k * kTileK, at.b, bar);
-                    tma_load<CG>(b + kHalf / 2, &map_b, bn + 64, k * kTileK, at.b, bar);
-                } else {
-                    tma_load<CG>(b, &map_b, k * kTileK, bn, at.b, bar);
-                }
+                __syncwarp();
                 if (++s == kStages) s = 0, ph ^= 1;
             }
         }
-    } else if (warp == 1 && lane == 0 && rank == 0) {
+    } else if (warp == 1 && rank == 0) {
         // multiply
         int s = 0, acc = 0;
         uint32_t ph = 0, aph = 0;
         constexpr uint64_t step_a = (AMN ? 2048 : 32) >> 4, step_b = (BMN ? 2048 : 32) >> 4;  // 16 values along K
+        const uint64_t desc_a = operand_desc(base, AMN, kHalf / 2), desc_b = operand_desc(base + kHalf, BMN, kHalf / 2);
         for (int t = first; ok && t < total; t += step) {
+            const int k0 = g.splits > 1 ? tile_at(g, t, per).b * nk_part : 0, nk = min(nk_part, nk_all - k0);
+            if (g.splits > 1 && nk <= 0) continue;
             if (!(ok = bar_wait(free_ + 8 * acc, aph ^ 1, &g_wait_expired))) break;
             mma_fence_after();
             for (int k = 0; k < nk; ++k) {
                 if (!(ok = bar_wait(full + 8 * s, ph, &g_wait_expired))) break;
                 mma_fence_after();
-                uint64_t a = operand_desc(base + s * kStageBytes, AMN, kHalf / 2);
-                uint64_t b = operand_desc(base + s * kStageBytes + kHalf, BMN, kHalf / 2);
+                const uint64_t a = desc_a + (uint64_t)(s * (kStageBytes >> 4)), b = desc_b + (uint64_t)(s * (kStageBytes >> 4));
+                if (elect_one()) {
 #pragma unroll
-                for (int i = 0; i < kTileK / 16; ++i) {
-                    mma_f16<CG>(tmem + acc * BN, a, b, g.idesc, (k | i) != 0);
-                    a += step_a;
-                    b += step_b;
+                    for (int i = 0; i < kTileK / 16; ++i)
+                        mma_f16<CG>(tmem + acc * BN, a + i * step_a, b + i * step_b, g.idesc, (k | i) != 0);
+                    mma_commit<CG>(empty + 8 * s);
                 }
-                mma_commit<CG>(empty + 8 * s);
+                __syncwarp();
                 if (++s == kStages) s = 0, ph ^= 1;
             }
-            if (ok) mma_commit<CG>(done + 8 * acc);
+            if (ok && elect_one()) mma_commit<CG>(done + 8 * acc);
+            __syncwarp();
             if (++acc == 2) acc = 0, aph ^= 1;
         }
     } else if (warp >= 4) {
@@ -271,6 +284,7 @@ __global__ void __launch_bounds__(kMatThreads, 1)
         uint32_t aph = 0;
         for (int t = first; t < total; t += step) {
             const TileAt at = tile_at(g, t, per);
+            if (g.splits > 1 && at.b * nk_part >= nk_all) continue;
             ok = bar_wait(done + 8 * acc, aph, &g_wait_expired);
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
             mma_fence_after();
@@ -287,7 +301,6 @@ __global__ void __launch_bounds__(kMatThreads, 1)
             }
             if (++acc == 2) acc = 0, aph ^= 1;
         }
-        ok = ok || lane != 0;
     }
     if (!ok) let_copies_end();
     __syncwarp();
@@ -320,9 +333,10 @@ int device_sms();  // of the current device; 148 where that cannot be asked
 
 constexpr int kSms = 148;  // the launch rules below reckon with a B200's SMs, so that workspace sizes need no device
 
-// Pairs of CTAs and 256 x 256 tiles run the tensor cores faster, 128 x 128 tiles leave fewer SMs idle. A tile of the
-// pair keeps it busy for two units of time, a small tile its SM for `kSmallCost`: the smaller number of waves times cost wins.
-constexpr double kSmallCost = 1.3;
+// Pairs of CTAs with tiles of 256 x 256 multiply at the tensor cores' rate (511 cycles per stage of K = 64, of 512);
+// tiles of 128 x 128 are held up by what an SM gets from L2 (450 cycles of 256), but leave fewer SMs idle. A tile of the
+// pair keeps it busy for two units of time, a small tile its SM for kSmallCost: the smaller number of waves times cost wins.
+constexpr double kSmallCost = 1.75;
 
 inline bool use_pairs(int M, int N, int batch, bool sym) {
     auto tiles = [&](int b) {
@@ -337,8 +351,9 @@ template <int CG, bool AMN, bool BMN, class Epi>
 cudaError_t launch_matmul_cg(const Operand& a, const Operand& b, MatShape g, bool f16, const typename Epi::Args& ea,
                              cudaStream_t stream, bool dependent) {
     CUtensorMap ma, mb;
-    cudaError_t err = make_map(&ma, a, g.M, g.K, g.batch, f16);
-    if (err == cudaSuccess) err = make_map(&mb, b, g.N, g.K, g.batch, f16);
+    const int matrices = g.splits > 1 ? 1 : g.batch;
+    cudaError_t err = make_map(&ma, a, g.M, g.K, matrices, f16);
+    if (err == cudaSuccess) err = make_map(&mb, b, g.N, g.K, matrices, f16);
     if (err != cudaSuccess) return err;
     g.tiles_m = (g.M + 128 * CG - 1) / (128 * CG);
     g.tiles_n = (g.N + 128 * CG - 1) / (128 * CG);
@@ -377,11 +392,45 @@ cudaError_t launch_matmul_cg(const Operand& a, const Operand& b, MatShape g, boo
 // `dependent`: the launch before this one on the stream is one of this call's, and the kernel may be set up beside its tail.
 template <bool AMN, bool BMN, class Epi>
 cudaError_t launch_matmul(const Operand& a, const Operand& b, int M, int N, int K, int batch, bool sym, bool f16,
-                          const typename Epi::Args& ea, cudaStream_t stream, bool dependent) {
+                          const typename Epi::Args& ea, cudaStream_t stream, bool dependent, const int* live_m = nullptr,
+                          const int* live_k = nullptr) {
     MatShape g = {};
-    g.M = M, g.N = N, g.K = K, g.batch = batch, g.sym = sym;
+    g.M = M, g.N = N, g.K = K, g.batch = batch, g.splits = 1, g.sym = sym, g.live_m = live_m, g.live_k = live_k;
     return use_pairs(M, N, batch, sym) ? launch_matmul_cg<2, AMN, BMN, Epi>(a, b, g, f16, ea, stream, dependent)
                                        : launch_matmul_cg<1, AMN, BMN, Epi>(a, b, g, f16, ea, stream, dependent);
+}
+
+// How a product with few tiles and a long K is cut: `splits` parts of K, on pairs of CTAs or single ones. The time of a
+// way is its waves times the stages of a part (and about 16 stages' time for filling the ring and storing a tile).
+struct Cut {
+    bool pairs;
+    int splits;
+};
+inline Cut cut_of(int M, int N, int K) {
+    Cut best = {true, 1};
+    double least = 0;
+    const int nk = (K + kTileK - 1) / kTileK;
+    for (int pairs = 1; pairs >= 0; --pairs) {
+        const int64_t b = pairs ? 256 : 128, tiles = ((M + b - 1) / b) * ((N + b - 1) / b), slots = pairs ? kSms / 2 : kSms;
+        for (int s = 1; s <= 16 && s <= nk; ++s) {
+            const int part = (nk + s - 1) / s;
+            if (s > 1 && (s - 1) * part >= nk) continue;  // no part is empty
+            const double waves = (double)((tiles * s + slots - 1) / slots);
+            // parts cost a pass over their sums: only where they win a tenth
+            const double cost = waves * (part * (pairs ? 2.0 : kSmallCost) + 32) * (s > 1 ? 1.1 : 1.0);
+            if (least == 0 || cost < least) least = cost, best = {pairs != 0, s};
+        }
+    }
+    return best;
+}
+
+template <bool AMN, bool BMN, class Epi>
+cudaError_t launch_matmul_cut(const Operand& a, const Operand& b, int M, int N, int K, Cut cut, bool f16,
+                              const typename Epi::Args& ea, cudaStream_t stream, bool dependent, const int* live_m) {
+    MatShape g = {};
+    g.M = M, g.N = N, g.K = K, g.batch = g.splits = cut.splits, g.live_m = live_m;
+    return cut.pairs ? launch_matmul_cg<2, AMN, BMN, Epi>(a, b, g, f16, ea, stream, dependent)
+                     : launch_matmul_cg<1, AMN, BMN, Epi>(a, b, g, f16, ea, stream, dependent);
 }
 
 }  // namespace ones

@@ -18,6 +18,16 @@ __device__ __forceinline__ uint64_t now_ns() {
     return t;
 }
 
+// One lane of the (converged) warp, always the same. TMA, tcgen05.mma and their barriers take their operands from uniform
+// registers: when a whole warp runs a loop and only the instruction itself is given to one lane, the operands are
+// computed there; a loop that one lane runs alone moves them over for every instruction (measured: 650 instead of 512
+// cycles for the four products of a stage).
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
+
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -60,7 +70,7 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
         "selp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(ok)
         : "r"(bar), "r"(parity)

@@ -216,7 +216,7 @@ def linear_cross_entropy_backward(dloss: torch.Tensor, hidden: torch.Tensor, wei
                                                                        weight_gradient=weight_gradient, piece=piece))) is not None:
         return other
     device = hidden.device
-    h, ldh = _rows(hidden, 8)
+    h, ldh = _rows(hidden)
     w, ldw = _rows(weight, 8)
     t, g, l = target.contiguous(), dloss.contiguous(), lse.contiguous()
     rows, cols, vocab = h.shape[0], hidden.shape[-1], weight.shape[0]
