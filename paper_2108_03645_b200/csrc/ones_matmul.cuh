@@ -40,7 +40,7 @@ struct MatShape {
     int sym;     // only tiles on and above the diagonal are computed (C is symmetric)
     const int *live_m, *live_k;  // where M or K is known on the device only (at most the value above)
     int group;  // row tiles that run through the columns together, so that both operands' tiles are met again in L2
-    uint32_t idesc;
+    bool f16;
 };
 
 struct TileAt {
@@ -71,6 +71,135 @@ __device__ __forceinline__ TileAt tile_at(const MatShape& g, int t, int per) {
         r.m = first + (p - r.n * rows);
     }
     return r;
+}
+
+// ---- the parts that the warps play ----
+
+// Ring of stages: where a warp stands in it.
+struct Ring {
+    uint32_t base, full, empty;  // stages; barriers
+    int s = 0;
+    uint32_t ph = 0;
+    __device__ __forceinline__ void next() {
+        if (++s == kStages) s = 0, ph ^= 1;
+    }
+};
+
+// How an operand lies in memory: with K contiguous, with its rows contiguous (mn), or symmetric with only the blocks on
+// and above the diagonal there (upper; blocks of BN): what lies below it is then taken from above, with the rows contiguous.
+enum class Lie { k, mn, upper };
+struct View {
+    const CUtensorMap *k, *mn;
+    Lie lie;
+    int tile;  // the block of rows, for Lie::upper
+    template <int BN>
+    __device__ __forceinline__ bool is_mn(int kb) const {
+        return lie == Lie::mn || (lie == Lie::upper && kb * kTileK / BN < tile);
+    }
+};
+
+template <int CG>
+__device__ __forceinline__ void fill_operand(uint32_t at, const View& v, int row, int kb, int z, uint32_t bar) {
+    if (v.is_mn<128 * CG>(kb)) {
+        tma_load<CG>(at, v.mn, row, kb * kTileK, z, bar);
+        tma_load<CG>(at + kHalf / 2, v.mn, row + 64, kb * kTileK, z, bar);
+    } else {
+        tma_load<CG>(at, v.k, kb * kTileK, row, z, bar);
+    }
+}
+
+// Fills the stages of one tile: K from stage k0 to k1, rows am of A and bn of B. Run by a whole warp; false: gave up.
+template <int CG>
+__device__ __forceinline__ bool fill_tile(Ring& r, const View& va, const View& vb, int am, int bn, int z, int k0, int k1, uint32_t rank,
+                                          uint32_t full_at) {
+    for (int k = k0; k < k1; ++k) {
+        if (!bar_wait(r.empty + 8 * r.s, r.ph ^ 1, &g_wait_expired)) return false;
+        const uint32_t a = r.base + r.s * kStageBytes, bar = full_at + 8 * r.s;
+        if (elect_one()) {
+            if (rank == 0) bar_expect(r.full + 8 * r.s, CG * kStageBytes);
+            fill_operand<CG>(a, va, am, k, z, bar);
+            fill_operand<CG>(a + kHalf, vb, bn, k, z, bar);
+        }
+        __syncwarp();
+        r.next();
+    }
+    return true;
+}
+
+__host__ __device__ inline uint32_t instruction_desc(int cg, bool f16, bool amn, bool bmn) {
+    const uint32_t type = f16 ? 0u : 1u;
+    return (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)amn << 15) | ((uint32_t)bmn << 16) |
+           ((uint32_t)(128 * cg / 8) << 17) | ((uint32_t)(128 * cg / 16) << 24);
+}
+
+// Multiplies the nk stages of one tile into the accumulator at `acc` and lets barrier `done` know when that is through.
+template <int CG>
+__device__ __forceinline__ bool multiply_tile(Ring& r, uint32_t acc, int nk, const View& va, const View& vb, bool f16, uint32_t done) {
+    const uint64_t a_k = operand_desc(r.base, false, kHalf / 2), a_mn = operand_desc(r.base, true, kHalf / 2);
+    const uint64_t to_b = kHalf >> 4;
+    for (int k = 0; k < nk; ++k) {
+        if (!bar_wait(r.full + 8 * r.s, r.ph, &g_wait_expired)) return false;
+        mma_fence_after();
+        const bool amn = va.is_mn<128 * CG>(k), bmn = vb.is_mn<128 * CG>(k);
+        const uint64_t off = (uint64_t)(r.s * (kStageBytes >> 4));
+        const uint64_t a = (amn ? a_mn : a_k) + off, b = (bmn ? a_mn : a_k) + off + to_b;
+        const uint64_t step_a = (amn ? 2048 : 32) >> 4, step_b = (bmn ? 2048 : 32) >> 4;  // 16 values along K
+        const uint32_t idesc = instruction_desc(CG, f16, amn, bmn);
+        if (elect_one()) {
+#pragma unroll
+            for (int i = 0; i < kTileK / 16; ++i) mma_f16<CG>(acc, a + i * step_a, b + i * step_b, idesc, (k | i) != 0);
+            mma_commit<CG>(r.empty + 8 * r.s);
+        }
+        __syncwarp();
+        r.next();
+    }
+    if (elect_one()) mma_commit<CG>(done);
+    __syncwarp();
+    return true;
+}
+
+// What a block (or pair) sets up before its first tile, and gives back after its last.
+struct Bench {
+    uint32_t base, full, empty, done, free_, tmem;
+};
+struct BenchShared {
+    uint64_t full[kStages], empty[kStages], done[2], free_[2];
+    uint32_t tmem;
+};
+template <int CG>
+__device__ __forceinline__ Bench set_up(BenchShared& s, uint8_t* smem_raw, int warp) {
+    Bench w;
+    w.base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    w.full = smem_u32(s.full), w.empty = smem_u32(s.empty), w.done = smem_u32(s.done), w.free_ = smem_u32(s.free_);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            bar_init(w.full + 8 * i, 1);
+            bar_init(w.empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(w.done + 8 * i, 1);
+            bar_init(w.free_ + 8 * i, kEpiWarps * CG);
+        }
+        bar_init_done();
+    }
+    if (warp == 2) tmem_alloc<CG>(smem_u32(&s.tmem), 256 * CG);  // two accumulators of 128 * CG columns
+    mma_fence_before();
+    __syncthreads();
+    if constexpr (CG == 2) cluster_sync_all();
+    mma_fence_after();
+    w.tmem = s.tmem;
+    return w;
+}
+template <int CG>
+__device__ __forceinline__ void clear_up(const Bench& w, int warp, bool ok) {
+    if (!ok) let_copies_end();
+    __syncwarp();
+    mma_fence_before();
+    __syncthreads();
+    if constexpr (CG == 2) cluster_sync_all();
+    mma_fence_after();
+    if (warp == 2) tmem_free<CG>(w.tmem, 256 * CG);
+    if constexpr (CG == 2) cluster_sync_all();  // neither CTA leaves while the other still gives its half back
 }
 
 // ---- what epilogues share ----
@@ -169,40 +298,37 @@ struct Turn {
     }
 };
 
+__device__ __forceinline__ Turn turn_of(uint8_t* smem_raw, uint32_t base, int warp, int lane) {
+    return {smem_raw + (base - smem_u32(smem_raw)) + kStages * kStageBytes + (warp - 4) * kEpiBytes, lane};
+}
+
+// The warp has read its part of an accumulator.
+template <int CG>
+__device__ __forceinline__ void free_accumulator(uint32_t bar, int lane) {
+    mma_fence_before();
+    __syncwarp();
+    if (lane == 0) {
+        if constexpr (CG == 2)
+            bar_arrive_cluster(bar);
+        else
+            bar_arrive(bar);
+    }
+}
+
 template <int CG, bool AMN, bool BMN, class Epi>
 __global__ void __launch_bounds__(kMatThreads, 1)
     k_matmul(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MatShape shape,
              const typename Epi::Args ea) {
-    constexpr int BN = 128 * CG;          // columns of a tile
-    constexpr uint32_t kCols = 2 * BN;    // tensor-memory columns: two accumulators
+    constexpr int BN = 128 * CG;  // columns of a tile
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_done[2], s_free[2];
-    __shared__ uint32_t s_tmem;
-
+    __shared__ BenchShared shared;
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
-    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t full = smem_u32(s_full), empty = smem_u32(s_empty), done = smem_u32(s_done), free_ = smem_u32(s_free);
-
     if (threadIdx.x == 0) {
         tma_prefetch(&map_a);
         tma_prefetch(&map_b);
-        for (int i = 0; i < kStages; ++i) {
-            bar_init(full + 8 * i, 1);
-            bar_init(empty + 8 * i, 1);
-        }
-        for (int i = 0; i < 2; ++i) {
-            bar_init(done + 8 * i, 1);
-            bar_init(free_ + 8 * i, kEpiWarps * CG);
-        }
-        bar_init_done();
     }
-    if (warp == 2) tmem_alloc<CG>(smem_u32(&s_tmem), kCols);
-    mma_fence_before();
-    __syncthreads();
-    if constexpr (CG == 2) cluster_sync_all();
-    mma_fence_after();
-    const uint32_t tmem = s_tmem;
+    const Bench w = set_up<CG>(shared, smem_raw, warp);
 
     wait_for_predecessor();
     let_successor_start();
@@ -213,103 +339,53 @@ __global__ void __launch_bounds__(kMatThreads, 1)
     const int per = tiles_per_matrix(g), total = per * g.batch;
     const int first = blockIdx.x / CG, step = gridDim.x / CG;
     const int nk_all = (g.K + kTileK - 1) / kTileK, nk_part = (nk_all + g.splits - 1) / g.splits;
+    const View va = {&map_a, &map_a, AMN ? Lie::mn : Lie::k, 0}, vb = {&map_b, &map_b, BMN ? Lie::mn : Lie::k, 0};
     bool ok = true;
 
     if (warp == 0) {
         // fill the ring
-        const uint32_t full_at = CG == 2 ? map_to_rank(full, 0) : full;  // the pair's bytes are counted on CTA 0's barrier
-        int s = 0;
-        uint32_t ph = 0;
+        const uint32_t full_at = CG == 2 ? map_to_rank(w.full, 0) : w.full;  // the pair's bytes are counted on CTA 0's barrier
+        Ring r = {w.base, w.full, w.empty};
         for (int t = first; ok && t < total; t += step) {
             const TileAt at = tile_at(g, t, per);
             const int am = at.m * 128 * CG + (int)rank * 128, bn = at.n * BN + (int)rank * 128;
             const int k0 = g.splits > 1 ? at.b * nk_part : 0, k1 = min(k0 + nk_part, nk_all), z = g.splits > 1 ? 0 : at.b;
-            if (g.splits > 1 && k0 >= k1) continue;  // nothing of K is left for this part
-            for (int k = k0; k < k1; ++k) {
-                if (!(ok = bar_wait(empty + 8 * s, ph ^ 1, &g_wait_expired))) break;
-                const uint32_t a = base + s * kStageBytes, b = a + kHalf, bar = full_at + 8 * s;
-                if (elect_one()) {
-                    if (rank == 0) bar_expect(full + 8 * s, CG * kStageBytes);
-                    if constexpr (AMN) {
-                        tma_load<CG>(a, &map_a, am, k * kTileK, z, bar);
-                        tma_load<CG>(a + kHalf / 2, &map_a, am + 64, k * kTileK, z, bar);
-                    } else {
-                        tma_load<CG>(a, &map_a, k * kTileK, am, z, bar);
-                    }
-                    if constexpr (BMN) {
-                        tma_load<CG>(b, &map_b, bn, k * kTileK, z, bar);
-                        tma_load<CG>(b + kHalf / 2, &map_b, bn + 64, k * kTileK, z, bar);
-                    } else {
-                        tma_load<CG>(b, &map_b, k * kTileK, bn, z, bar);
-                    }
-                }
-                __syncwarp();
-                if (++s == kStages) s = 0, ph ^= 1;
-            }
+            ok = fill_tile<CG>(r, va, vb, am, bn, z, k0, k1, rank, full_at);
         }
     } else if (warp == 1 && rank == 0) {
         // multiply
-        int s = 0, acc = 0;
-        uint32_t ph = 0, aph = 0;
-        constexpr uint64_t step_a = (AMN ? 2048 : 32) >> 4, step_b = (BMN ? 2048 : 32) >> 4;  // 16 values along K
-        const uint64_t desc_a = operand_desc(base, AMN, kHalf / 2), desc_b = operand_desc(base + kHalf, BMN, kHalf / 2);
+        Ring r = {w.base, w.full, w.empty};
+        int acc = 0;
+        uint32_t aph = 0;
         for (int t = first; ok && t < total; t += step) {
             const int k0 = g.splits > 1 ? tile_at(g, t, per).b * nk_part : 0, nk = min(nk_part, nk_all - k0);
-            if (g.splits > 1 && nk <= 0) continue;
-            if (!(ok = bar_wait(free_ + 8 * acc, aph ^ 1, &g_wait_expired))) break;
+            if (g.splits > 1 && nk <= 0) continue;  // nothing of K is left for this part
+            if (!(ok = bar_wait(w.free_ + 8 * acc, aph ^ 1, &g_wait_expired))) break;
             mma_fence_after();
-            for (int k = 0; k < nk; ++k) {
-                if (!(ok = bar_wait(full + 8 * s, ph, &g_wait_expired))) break;
-                mma_fence_after();
-                const uint64_t a = desc_a + (uint64_t)(s * (kStageBytes >> 4)), b = desc_b + (uint64_t)(s * (kStageBytes >> 4));
-                if (elect_one()) {
-#pragma unroll
-                    for (int i = 0; i < kTileK / 16; ++i)
-                        mma_f16<CG>(tmem + acc * BN, a + i * step_a, b + i * step_b, g.idesc, (k | i) != 0);
-                    mma_commit<CG>(empty + 8 * s);
-                }
-                __syncwarp();
-                if (++s == kStages) s = 0, ph ^= 1;
-            }
-            if (ok && elect_one()) mma_commit<CG>(done + 8 * acc);
-            __syncwarp();
+            ok = multiply_tile<CG>(r, w.tmem + acc * BN, nk, va, vb, g.f16, w.done + 8 * acc);
             if (++acc == 2) acc = 0, aph ^= 1;
         }
     } else if (warp >= 4) {
         // hand the accumulators on
         const int quad = warp % 4, half = (warp - 4) / 4;
-        const Turn turn = {smem_raw + (base - smem_u32(smem_raw)) + kStages * kStageBytes + (warp - 4) * kEpiBytes, lane};
-        const uint32_t free_at = CG == 2 ? map_to_rank(free_, 0) : free_;
+        const Turn turn = turn_of(smem_raw, w.base, warp, lane);
+        const uint32_t free_at = CG == 2 ? map_to_rank(w.free_, 0) : w.free_;
         int acc = 0;
         uint32_t aph = 0;
         for (int t = first; t < total; t += step) {
             const TileAt at = tile_at(g, t, per);
             if (g.splits > 1 && at.b * nk_part >= nk_all) continue;
-            ok = bar_wait(done + 8 * acc, aph, &g_wait_expired);
+            ok = bar_wait(w.done + 8 * acc, aph, &g_wait_expired);
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
             mma_fence_after();
             const int row = at.m * 128 * CG + (int)rank * 128 + quad * 32 + lane;
             const int col = at.n * BN + half * (BN / 2);
-            Epi::template tile<BN / 2>(ea, g, tmem + acc * BN + half * (BN / 2) + ((uint32_t)quad << 21), row, col, at, half, turn);
-            mma_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                if constexpr (CG == 2)
-                    bar_arrive_cluster(free_at + 8 * acc);
-                else
-                    bar_arrive(free_ + 8 * acc);
-            }
+            Epi::template tile<BN / 2>(ea, g, w.tmem + acc * BN + half * (BN / 2) + ((uint32_t)quad << 21), row, col, at, half, turn);
+            free_accumulator<CG>(free_at + 8 * acc, lane);
             if (++acc == 2) acc = 0, aph ^= 1;
         }
     }
-    if (!ok) let_copies_end();
-    __syncwarp();
-    mma_fence_before();
-    __syncthreads();
-    if constexpr (CG == 2) cluster_sync_all();
-    mma_fence_after();
-    if (warp == 2) tmem_free<CG>(tmem, kCols);
-    if constexpr (CG == 2) cluster_sync_all();  // neither CTA leaves while the other still gives its half back
+    clear_up<CG>(w, warp, ok);
 }
 
 // ---- host side ----
@@ -322,12 +398,6 @@ struct Operand {
 };
 
 cudaError_t make_map(CUtensorMap* out, const Operand& o, int rows, int k, int batch, bool f16);
-
-inline uint32_t instruction_desc(int cg, bool f16, bool amn, bool bmn) {
-    const uint32_t type = f16 ? 0u : 1u;
-    return (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)amn << 15) | ((uint32_t)bmn << 16) |
-           ((uint32_t)(128 * cg / 8) << 17) | ((uint32_t)(128 * cg / 16) << 24);
-}
 
 int device_sms();  // of the current device; 148 where that cannot be asked
 
@@ -358,7 +428,7 @@ cudaError_t launch_matmul_cg(const Operand& a, const Operand& b, MatShape g, boo
     g.tiles_m = (g.M + 128 * CG - 1) / (128 * CG);
     g.tiles_n = (g.N + 128 * CG - 1) / (128 * CG);
     g.group = 8 * (CG == 1 ? 2 : 1);
-    g.idesc = instruction_desc(CG, f16, AMN, BMN);
+    g.f16 = f16;
     const int64_t per = g.sym ? (int64_t)g.tiles_m * (g.tiles_m + 1) / 2 : (int64_t)g.tiles_m * g.tiles_n;
     const int64_t slots = device_sms() / CG, total = per * g.batch;
     if (total > 0x7FFFFFFF) return cudaErrorInvalidValue;

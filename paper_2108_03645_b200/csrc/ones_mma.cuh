@@ -61,9 +61,10 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
 __device__ __forceinline__ void bar_arrive(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-// `bar` is a shared::cluster address: the barrier may lie in another CTA of the cluster.
+// `bar` is a shared::cluster address: the barrier may lie in another CTA of the cluster. Orders no memory accesses (those
+// of tensor memory are ordered by the tcgen05 fences): a release would wait for every store on its way.
 __device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
@@ -95,6 +96,36 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, unsigned
 __device__ __forceinline__ void let_copies_end() {
     const uint64_t begin = now_ns();
     while (now_ns() - begin < 10000000ull) __nanosleep(1000);
+}
+
+// ---- between the blocks of a cooperative launch ----
+// One thread counts its block in, after a barrier of all threads whose writes the others are to see.
+__device__ __forceinline__ void arrive_all(unsigned* counter) {
+    __threadfence();
+    asm volatile("fence.proxy.async;" ::: "memory");  // the others read by TMA
+    asm volatile("red.relaxed.gpu.global.add.u32 [%0], 1;" ::"l"(counter) : "memory");
+}
+// Waits (a whole warp) until the counter has reached `target`; false when that has not come within kWaitLimitNs.
+__device__ __forceinline__ bool wait_all(const unsigned* counter, unsigned target, unsigned* expired) {
+    bool ok = true;
+    if (threadIdx.x % 32 == 0) {
+        uint64_t begin = 0;
+        for (;;) {
+            unsigned v;
+            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(counter) : "memory");
+            if ((int)(v - target) >= 0) break;
+            const uint64_t now = now_ns();
+            if (!begin) begin = now;
+            if (now - begin > kWaitLimitNs) {
+                atomicExch(expired, 1u);
+                ok = false;
+                break;
+            }
+        }
+    }
+    ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
+    asm volatile("fence.proxy.async;" ::: "memory");
+    return ok;
 }
 
 // ---- TMA ----

@@ -9,7 +9,7 @@ namespace ones {
 
 namespace {
 
-constexpr int kNormThreads = 256, kNormBlocks = 128;  // a warp takes a row at a time
+constexpr int kNormThreads = 256, kNormBlocks = 4 * kSms;  // a warp takes a row at a time
 
 __device__ __forceinline__ float load_as_float(const void* p, int64_t i, int type) {
     if (type == ONES_F32) return static_cast<const float*>(p)[i];
@@ -45,21 +45,27 @@ struct Source {
     bool wide;  // rows start on 16-byte boundaries and hold a multiple of 8 values
 };
 
-// Sum of squares of each matrix, in 64 bits (squares of small gradients leave the range of 32), one part per block.
-__global__ void __launch_bounds__(kNormThreads) k_ns_norm(Source g, double* part) {
+// Sum of squares of each matrix, in 64 bits (squares of small gradients leave the range of 32), one part per block. Also
+// clears the counter that the blocks of k_ns_steps meet at.
+__global__ void __launch_bounds__(kNormThreads) k_ns_norm(Source g, double* part, unsigned* counter) {
     __shared__ double s[kNormThreads / 32];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *counter = 0;
     double sum = 0.0;
     for (int r = blockIdx.x * (kNormThreads / 32) + warp; r < g.m; r += gridDim.x * (kNormThreads / 32)) {
         const int64_t at = blockIdx.y * g.stride + r * g.ld;
         if (g.wide) {
+#pragma unroll 4
             for (int c = lane * 8; c < g.n; c += 256) {
                 float v[8];
                 load8(g.p, at + c, g.type, v);
+                double e = 0.0;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum += (double)v[i] * v[i];
+                for (int i = 0; i < 8; ++i) e = fma((double)v[i], (double)v[i], e);
+                sum += e;
             }
         } else {
+#pragma unroll 8
             for (int c = lane; c < g.n; c += 32) {
                 const double v = load_as_float(g.p, at + c, g.type);
                 sum += v * v;
@@ -82,21 +88,23 @@ __global__ void __launch_bounds__(kNormThreads) k_ns_cast(Source g, const double
                                                           float2* factor) {
     wait_for_predecessor();
     let_successor_start();
+    __shared__ double s_sum[kNormThreads / 32];
     __shared__ float s_scale;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    if (warp == 0) {
-        double sum = 0.0;
-        for (int i = lane; i < parts; i += 32) sum += part[blockIdx.y * parts + i];
-        for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-        if (lane == 0) {
-            const double norm = sqrt(sum), rms = norm / sqrt((double)g.m * g.n);
-            int k = rms > 0.0 && rms < 1e300 ? ilogb(rms) : 0;
-            k = k < -120 ? -120 : k > 120 ? 120 : k;
-            s_scale = ldexpf(1.f, -k);
-            if (blockIdx.x == 0) {
-                const double f = ldexp(1.0, k) / (norm + eps);
-                factor[blockIdx.y] = make_float2((float)f, (float)(f * f));
-            }
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < parts; i += kNormThreads) sum += part[blockIdx.y * parts + i];
+    for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    if (lane == 0) s_sum[warp] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < kNormThreads / 32; ++i) sum += s_sum[i];
+        const double norm = sqrt(sum), rms = norm / sqrt((double)g.m * g.n);
+        int k = rms > 0.0 && rms < 1e300 ? ilogb(rms) : 0;
+        k = k < -120 ? -120 : k > 120 ? 120 : k;
+        s_scale = ldexpf(1.f, -k);
+        if (blockIdx.x == 0) {
+            const double f = ldexp(1.0, k) / (norm + eps);
+            factor[blockIdx.y] = make_float2((float)f, (float)(f * f));
         }
     }
     __syncthreads();
@@ -105,6 +113,7 @@ __global__ void __launch_bounds__(kNormThreads) k_ns_cast(Source g, const double
         const int64_t at = blockIdx.y * g.stride + r * g.ld;
         __half* out = x + ((int64_t)blockIdx.y * g.m + r) * ldx;
         if (g.wide) {
+#pragma unroll 4
             for (int c = lane * 8; c < g.n; c += 256) {
                 float v[8];
                 load8(g.p, at + c, g.type, v);
@@ -114,22 +123,14 @@ __global__ void __launch_bounds__(kNormThreads) k_ns_cast(Source g, const double
                                                                 Half16::pack(v[4], v[5], true), Half16::pack(v[6], v[7], true));
             }
         } else {
+#pragma unroll 8
             for (int c = lane; c < g.n; c += 32) out[c] = __float2half_rn(load_as_float(g.p, at + c, g.type) * scale);
         }
     }
 }
 
-// The symmetric products' tiles lie on and above the diagonal; what they hold is stored on both sides of it.
-__device__ __forceinline__ void store_both(__half* out, int64_t ld, int s, int row, int col, bool mirror, const float (&v)[64], const Turn& turn) {
-    uint16_t* p = reinterpret_cast<uint16_t*>(out);
-    turn.put16(v, true);
-    turn.store16(p, ld, row - turn.lane, col, s, s, true);
-    if (!mirror || row >= s) return;
-    p += (int64_t)col * ld + row;
-#pragma unroll
-    for (int i = 0; i < 64; ++i, p += ld)
-        if (col + i < s) *p = __half_as_ushort(__float2half_rn(v[i]));
-}
+// The symmetric products have only their blocks on and above the diagonal computed and stored. The products that read
+// them take what lies below from above, as an operand with its rows contiguous (Lie::upper).
 
 // A = factor * X X^T
 struct EpiGram {
@@ -141,16 +142,17 @@ struct EpiGram {
         const float2* first;  // the first step's f^2, or NULL
     };
     template <int W>
-    static __device__ __forceinline__ void tile(const Args& a, const MatShape&, uint32_t acc, int row, int col,
-                                                const TileAt& at, int, const Turn& turn) {
+    static __device__ __forceinline__ void tile(const Args& a, uint32_t acc, int row, int col, const TileAt& at, const Turn& turn) {
         const float f = a.first ? a.first[at.b].y : a.factor;
+        uint16_t* out = reinterpret_cast<uint16_t*>(a.out + at.b * a.batch_ld);
 #pragma unroll 1
         for (int c = 0; c < W && col + c < a.s; c += 64) {
             float v[64];
             tmem_load(acc + c, v);
 #pragma unroll
             for (int i = 0; i < 64; ++i) v[i] *= f;
-            store_both(a.out + at.b * a.batch_ld, a.ld, a.s, row, col + c, at.m != at.n, v, turn);
+            turn.put16(v, true);
+            turn.store16(out, a.ld, row - turn.lane, col + c, a.s, a.s, true);
         }
     }
 };
@@ -165,25 +167,28 @@ struct EpiPoly {
         int s;
         float a, b, c;
     };
+    // A's values of 64 columns, 8 lanes to a row, as the result leaves; asked for before they are needed.
+    static __device__ __forceinline__ void load(const Args& a, int row, int col, const TileAt& at, const Turn& turn, uint4 (&q)[8]) {
+        const int c = col + 8 * (turn.lane & 7);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = row - turn.lane + 4 * i + turn.lane / 8;  // rows of A are padded to whole 16 bytes
+            q[i] = r < a.s && c < a.s ? __ldcg(reinterpret_cast<const uint4*>(a.gram + at.b * a.batch_ld + (int64_t)r * a.ld + c))
+                                      : make_uint4(0, 0, 0, 0);
+        }
+    }
     template <int W>
-    static __device__ __forceinline__ void tile(const Args& a, const MatShape&, uint32_t acc, int row, int col,
-                                                const TileAt& at, int, const Turn& turn) {
+    static __device__ __forceinline__ void tile(const Args& a, uint32_t acc, int row, int col, const TileAt& at, const Turn& turn, uint4 (&q)[8]) {
+        uint16_t* out = reinterpret_cast<uint16_t*>(a.out + at.b * a.batch_ld);
 #pragma unroll 1
         for (int c = 0; c < W && col + c < a.s; c += 64) {
-            // A's values, 8 lanes to a row, by the same way that the result leaves
-            const __half* gram = a.gram + at.b * a.batch_ld;
-            const int k = turn.lane & 7, at_col = col + c + 8 * k;
-            uint4 q[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int r = row - turn.lane + 4 * i + turn.lane / 8;  // rows of A are padded to whole 16 bytes
-                q[i] = r < a.s && at_col < a.s ? *reinterpret_cast<const uint4*>(gram + (int64_t)r * a.ld + at_col) : make_uint4(0, 0, 0, 0);
-            }
             float v[64];
             tmem_load(acc + c, v);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) turn.chunk(4 * i + turn.lane / 8, k) = q[i];
             __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) turn.chunk(4 * i + turn.lane / 8, turn.lane & 7) = q[i];
+            __syncwarp();
+            if (c + 64 < W) load(a, row, col + c + 64, at, turn, q);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const uint4 p = turn.chunk(turn.lane, j);
@@ -201,8 +206,8 @@ struct EpiPoly {
                 for (int i = 0; i < 64; ++i)
                     if (d == (unsigned)i) v[i] += a.a;
             }
-            store_both(a.out + at.b * a.batch_ld, a.ld, a.s, row, col + c, at.m != at.n, v, turn);
-            __syncwarp();
+            turn.put16(v, true);
+            turn.store16(out, a.ld, row - turn.lane, col + c, a.s, a.s, true);
         }
     }
 };
@@ -218,8 +223,7 @@ struct EpiApply {
         bool f16, wide;
     };
     template <int W>
-    static __device__ __forceinline__ void tile(const Args& a, const MatShape&, uint32_t acc, int row, int col,
-                                                const TileAt& at, int, const Turn& turn) {
+    static __device__ __forceinline__ void tile(const Args& a, uint32_t acc, int row, int col, const TileAt& at, const Turn& turn) {
         const float f = a.first ? a.factor * a.first[at.b].x : a.factor;
 #pragma unroll 1
         for (int c = 0; c < W && col + c < a.n; c += 64) {
@@ -233,10 +237,154 @@ struct EpiApply {
     }
 };
 
+// All steps in one launch. A step is three products (Gram matrix, polynomial, application), each of which needs all of
+// the one before; as launches of their own the 15 of five steps cost 9 us each for small matrices and 14 for twelve of
+// 768 x 768, most of it in starting, ending and first touching of code. Here the blocks stay, with their barriers and
+// accumulators, and meet at a counter between products (a cooperative launch: all of them are on the GPU).
+struct StepsArgs {
+    int m, n, s, count, steps;
+    bool tall;  // more rows than columns: the Gram matrix is X^T X and X takes the polynomial from the right
+    float a, b, c, unit;  // unit: X is kept times this between the steps
+    __half *x[2], *gram, *poly;
+    uint16_t* out;
+    int64_t ldx, xs, lds, ss;
+    const float2* factor;
+    unsigned* counter;
+    bool wide;
+};
+struct StepsMaps {
+    CUtensorMap rows[2], cols[2];  // X with its rows as the operand's rows, and with its columns
+    CUtensorMap gram[2], poly[2];
+};
+
+// The operands of the products: X X^T or X^T X; A A; B X or X B.
+__device__ __forceinline__ void operands(const StepsMaps& maps, bool tall, int which, int buf, const TileAt& at, View& a, View& b) {
+    const View x = {&maps.rows[buf], &maps.cols[buf], Lie::k, 0};
+    if (which == 0) {
+        a = b = x;
+        if (tall) a.lie = b.lie = Lie::mn;
+    } else if (which == 1) {
+        a = {&maps.gram[0], &maps.gram[1], Lie::upper, at.m};
+        b = {&maps.gram[0], &maps.gram[1], Lie::upper, at.n};
+    } else if (tall) {
+        a = x;
+        b = {&maps.poly[0], &maps.poly[1], Lie::upper, at.n};
+    } else {
+        a = {&maps.poly[0], &maps.poly[1], Lie::upper, at.m};
+        b = x;
+        b.lie = Lie::mn;
+    }
+}
+
+template <int CG>
+__global__ void __launch_bounds__(kMatThreads, 1) k_ns_steps(const __grid_constant__ StepsMaps maps, const StepsArgs p) {
+    constexpr int BN = 128 * CG;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ BenchShared shared;
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+    __shared__ __align__(8) uint64_t s_round;  // tells the epilogue that the product before is complete: one poller a block
+    const uint32_t round_bar = smem_u32(&s_round);
+    if (threadIdx.x == 0) bar_init(round_bar, 1);
+    const Bench w = set_up<CG>(shared, smem_raw, warp);
+    wait_for_predecessor();
+
+    const int first = blockIdx.x / CG, step = gridDim.x / CG;
+    // the three products of a step
+    MatShape sym = {}, app = {};
+    sym.M = sym.N = p.s, sym.batch = p.count, sym.sym = 1, sym.tiles_m = sym.tiles_n = (p.s + BN - 1) / BN;
+    app.M = p.m, app.N = p.n, app.K = p.s, app.batch = p.count, app.tiles_m = (p.m + BN - 1) / BN, app.tiles_n = (p.n + BN - 1) / BN;
+    app.group = 16 / CG;
+    const int per_sym = tiles_per_matrix(sym), per_app = tiles_per_matrix(app);
+    const int long_side = p.tall ? p.m : p.n;
+    const int nk_gram = (long_side + kTileK - 1) / kTileK, nk_s = (p.s + kTileK - 1) / kTileK;
+    const int rounds = 3 * p.steps;
+    bool ok = true;
+
+    if (warp == 0) {
+        const uint32_t full_at = CG == 2 ? map_to_rank(w.full, 0) : w.full;
+        Ring r = {w.base, w.full, w.empty};
+        for (int round = 0; ok && round < rounds; ++round) {
+            const int which = round % 3, buf = round / 3 & 1;
+            if (round && !(ok = wait_all(p.counter, (unsigned)round * gridDim.x, &g_wait_expired))) break;
+            if (round && lane == 0) bar_arrive(round_bar);
+            const MatShape& g = which == 2 ? app : sym;
+            const int per = which == 2 ? per_app : per_sym, total = per * p.count, nk = which == 0 ? nk_gram : nk_s;
+            for (int t = first; ok && t < total; t += step) {
+                const TileAt at = tile_at(g, t, per);
+                View va, vb;
+                operands(maps, p.tall, which, buf, at, va, vb);
+                ok = fill_tile<CG>(r, va, vb, at.m * BN + (int)rank * 128, at.n * BN + (int)rank * 128, at.b, 0, nk, rank, full_at);
+            }
+        }
+    } else if (warp == 1 && rank == 0) {
+        Ring r = {w.base, w.full, w.empty};
+        int acc = 0;
+        uint32_t aph = 0;
+        for (int round = 0; ok && round < rounds; ++round) {
+            const int which = round % 3;
+            const MatShape& g = which == 2 ? app : sym;
+            const int per = which == 2 ? per_app : per_sym, total = per * p.count, nk = which == 0 ? nk_gram : nk_s;
+            for (int t = first; ok && t < total; t += step) {
+                View va, vb;
+                operands(maps, p.tall, which, 0, tile_at(g, t, per), va, vb);
+                if (!(ok = bar_wait(w.free_ + 8 * acc, aph ^ 1, &g_wait_expired))) break;
+                mma_fence_after();
+                ok = multiply_tile<CG>(r, w.tmem + acc * BN, nk, va, vb, true, w.done + 8 * acc);
+                if (++acc == 2) acc = 0, aph ^= 1;
+            }
+        }
+    } else if (warp >= 4) {
+        const int quad = warp % 4, half = (warp - 4) / 4;
+        const Turn turn = turn_of(smem_raw, w.base, warp, lane);
+        const uint32_t free_at = CG == 2 ? map_to_rank(w.free_, 0) : w.free_;
+        int acc = 0;
+        uint32_t aph = 0;
+        for (int round = 0; round < rounds; ++round) {  // a warp that gave up still comes to the barrier below
+            const int which = round % 3, k = round / 3, buf = k & 1;
+            if (ok && round) ok = __all_sync(0xFFFFFFFFu, bar_wait(round_bar, (round - 1) & 1, &g_wait_expired));
+            const MatShape& g = which == 2 ? app : sym;
+            const int per = which == 2 ? per_app : per_sym, total = per * p.count;
+            const float2* start = k == 0 ? p.factor : nullptr;
+            for (int t = first; ok && t < total; t += step) {
+                const TileAt at = tile_at(g, t, per);
+                const int row = at.m * BN + (int)rank * 128 + quad * 32 + lane, col = at.n * BN + half * (BN / 2);
+                const uint32_t tmem = w.tmem + acc * BN + half * (BN / 2) + ((uint32_t)quad << 21);
+                const EpiPoly::Args ep = {p.gram, p.poly, p.lds, p.ss, p.s, p.a, p.b, p.c};
+                uint4 q[8];
+                if (which == 1) EpiPoly::load(ep, row, col, at, turn, q);
+                ok = bar_wait(w.done + 8 * acc, aph, &g_wait_expired);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) break;
+                mma_fence_after();
+                if (which == 0) {
+                    const EpiGram::Args e = {p.gram, p.lds, p.ss, p.s, 1.f / (p.unit * p.unit), start};
+                    EpiGram::tile<BN / 2>(e, tmem, row, col, at, turn);
+                } else if (which == 1) {
+                    EpiPoly::tile<BN / 2>(ep, tmem, row, col, at, turn, q);
+                } else {
+                    EpiApply::Args e = {reinterpret_cast<uint16_t*>(p.x[1 - buf]), p.ldx, p.xs, p.m, p.n, start ? p.unit : 1.f, start, true, true};
+                    if (k + 1 == p.steps) {
+                        e.out = p.out, e.ld = p.n, e.batch_ld = (int64_t)p.m * p.n;
+                        e.factor = start ? 1.f : 1.f / p.unit;
+                        e.f16 = false, e.wide = p.wide;
+                    }
+                    EpiApply::tile<BN / 2>(e, tmem, row, col, at, turn);
+                }
+                free_accumulator<CG>(free_at + 8 * acc, lane);
+                if (++acc == 2) acc = 0, aph ^= 1;
+            }
+            asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpiWarps) : "memory");
+            if (warp == 4 && lane == 0) arrive_all(p.counter);
+        }
+    }
+    clear_up<CG>(w, warp, ok);
+}
+
 inline size_t up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 struct Layout {
-    size_t factor, part, x0, x1, gram, poly, total;
+    size_t counter, factor, part, x0, x1, gram, poly, total;
     int64_t ldx, lds;
     int s;
 };
@@ -251,14 +399,75 @@ Layout layout(int32_t count, int32_t m, int32_t n) {
         at = up(at + bytes, 256);
         return here;
     };
+    L.counter = take(256);
     L.factor = take((size_t)count * sizeof(float2));
-    L.part = take((size_t)count * kNormBlocks * 8);
+    L.part = take((size_t)(count > kNormBlocks ? count : kNormBlocks) * 8);
     L.x0 = take((size_t)count * m * L.ldx * 2);
     L.x1 = take((size_t)count * m * L.ldx * 2);
     L.gram = take((size_t)count * L.s * L.lds * 2);
     L.poly = take((size_t)count * L.s * L.lds * 2);
     L.total = at;
     return L;
+}
+
+int64_t tiles_of(int64_t rows, int64_t cols, int64_t b) { return ((rows + b - 1) / b) * ((cols + b - 1) / b); }
+int64_t half_tiles_of(int64_t s, int64_t b) { return ((s + b - 1) / b) * ((s + b - 1) / b + 1) / 2; }
+
+// Pairs of CTAs or single ones for all products of a step: the smaller time by the rule of use_pairs, a product's waves
+// times its stages (and about 16 for filling the ring and storing the last tile).
+bool pairs_win(int m, int n, int s, int count) {
+    double cost[2];
+    for (int cg = 1; cg <= 2; ++cg) {
+        const int64_t b = 128 * cg, slots = kSms / cg, nl = (m + n - s + kTileK - 1) / kTileK, ns = (s + kTileK - 1) / kTileK;
+        const double sym = (double)((half_tiles_of(s, b) * count + slots - 1) / slots), app = (double)((tiles_of(m, n, b) * count + slots - 1) / slots);
+        const double unit = cg == 2 ? 2.0 : kSmallCost;
+        cost[cg - 1] = sym * (nl * unit + 32) + sym * (ns * unit + 32) + app * (ns * unit + 32);
+    }
+    return cost[1] <= cost[0];
+}
+
+template <int CG>
+cudaError_t launch_steps(const StepsMaps& maps, const StepsArgs& p, cudaStream_t stream) {
+    auto kernel = k_ns_steps<CG>;
+    static std::atomic<uint64_t> ready{0};
+    cudaError_t err = allow_smem(kernel, kMatSmem, ready);
+    if (err != cudaSuccess) return err;
+    cudaLaunchConfig_t cfg = {};
+    cfg.blockDim = dim3(kMatThreads);
+    cfg.dynamicSmemBytes = kMatSmem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeCooperative;
+    attr[0].val.cooperative = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = CG;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = CG == 2 ? 2 : 1;
+    int64_t slots = device_sms();
+    if (CG == 2) {  // pairs that fit at a time: an SM without a neighbour stays out
+        static std::atomic<int> fit[64];
+        int dev = 0, n = 0;
+        err = cudaGetDevice(&dev);
+        if (err != cudaSuccess) return err;
+        n = fit[dev & 63].load(std::memory_order_relaxed);
+        if (!n) {
+            cfg.gridDim = dim3(2);
+            cfg.attrs = attr + 1;
+            cfg.numAttrs = 1;
+            err = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+            if (err != cudaSuccess) return err;
+            if (n < 1) return cudaErrorInvalidConfiguration;
+            fit[dev & 63].store(n, std::memory_order_relaxed);
+            cfg.attrs = attr;
+            cfg.numAttrs = 2;
+        }
+        slots = n;
+    }
+    const int64_t b = 128 * CG, half = half_tiles_of(p.s, b) * p.count, whole = tiles_of(p.m, p.n, b) * p.count, most = half > whole ? half : whole;
+    if (most > 0x7FFFFFFF) return cudaErrorInvalidValue;
+    cfg.gridDim = dim3((unsigned)((most < slots ? most : slots) * CG));
+    return cudaLaunchKernelEx(&cfg, kernel, maps, p);
 }
 
 bool bad_sizes(int32_t count, int32_t m, int32_t n) {
@@ -303,45 +512,38 @@ int ones_orthogonalize(const void* d_g, int64_t ldg, int64_t stride, int32_t cou
     __half* x[2] = {reinterpret_cast<__half*>(ws + L.x0), reinterpret_cast<__half*>(ws + L.x1)};
     __half* gram = reinterpret_cast<__half*>(ws + L.gram);
     __half* poly = reinterpret_cast<__half*>(ws + L.poly);
-    const int s = L.s;
-    const bool tall = m > n;  // the products run on the columns then
-    const int64_t xs = (int64_t)m * L.ldx, ss = (int64_t)s * L.lds;
-
+    unsigned* counter = reinterpret_cast<unsigned*>(ws + L.counter);
     const bool wide = n % 8 == 0 && aligned(d_g, 16) && ldg * size % 16 == 0 && stride * size % 16 == 0;
     const Source src = {d_g, ldg, count > 1 ? stride : 0, m, n, type, wide};
-    int blocks = (m + kNormThreads / 32 - 1) / (kNormThreads / 32);
-    if (blocks > kNormBlocks) blocks = kNormBlocks;
-    k_ns_norm<<<dim3(blocks, count), kNormThreads, 0, stream>>>(src, part);
+    int blocks = (m + kNormThreads / 32 - 1) / (kNormThreads / 32), most = kNormBlocks / count;
+    if (blocks > most) blocks = most > 0 ? most : 1;
+    k_ns_norm<<<dim3(blocks, count), kNormThreads, 0, stream>>>(src, part, counter);
     cudaError_t err = cudaGetLastError();
     if (err == cudaSuccess)
-        err = launch_after(k_ns_cast, dim3(blocks, count), dim3(kNormThreads), stream, src, part, blocks, eps, x[0], L.ldx, factor);
-    // Between the steps X is kept times 2^p, about the square root of the longer side, which brings its values near 1:
-    // after the last step they are about 1 / 2^p, before the first about 1 / sqrt(m n).
-    int p = 0;
-    while ((int64_t)1 << (2 * (p + 1)) <= (m > n ? m : n)) ++p;
-    const float unit = ldexpf(1.f, p), one_over = ldexpf(1.f, -p);
-    for (int k = 0; err == cudaSuccess && k < steps; ++k) {
-        const __half* in = x[k & 1];
-        const float2* first = k == 0 ? factor : nullptr;
-        const EpiGram::Args eg = {gram, L.lds, ss, s, one_over * one_over, first};
-        err = tall ? launch_matmul<true, true, EpiGram>({in, L.ldx, xs, true}, {in, L.ldx, xs, true}, s, s, m, count, true, true, eg, stream, true)
-                   : launch_matmul<false, false, EpiGram>({in, L.ldx, xs, false}, {in, L.ldx, xs, false}, s, s, n, count, true, true, eg, stream, true);
-        if (err != cudaSuccess) break;
-        const EpiPoly::Args ep = {gram, poly, L.lds, ss, s, a, b, c};
-        err = launch_matmul<false, false, EpiPoly>({gram, L.lds, ss, false}, {gram, L.lds, ss, false}, s, s, s, count, true, true, ep, stream, true);
-        if (err != cudaSuccess) break;
-        const bool last = k + 1 == steps;
-        EpiApply::Args ea = {reinterpret_cast<uint16_t*>(x[1 - (k & 1)]), L.ldx, xs, m, n, 1.f, first, true, true};
-        if (first) ea.factor = unit;
-        if (last) {
-            ea.out = static_cast<uint16_t*>(d_out), ea.ld = n, ea.batch_ld = (int64_t)m * n;
-            ea.factor = first ? 1.f : one_over;
-            ea.f16 = false;
-            ea.wide = n % 8 == 0 && aligned(d_out, 16);
-        }
-        err = tall ? launch_matmul<false, false, EpiApply>({in, L.ldx, xs, false}, {poly, L.lds, ss, false}, m, n, s, count, false, true, ea, stream, true)
-                   : launch_matmul<false, true, EpiApply>({poly, L.lds, ss, false}, {in, L.ldx, xs, true}, m, n, s, count, false, true, ea, stream, true);
+        err = launch_after(k_ns_cast, dim3(blocks, count), dim3(kNormThreads), stream, src, static_cast<const double*>(part), blocks, eps,
+                           x[0], L.ldx, factor);
+    StepsArgs p = {};
+    p.m = m, p.n = n, p.s = L.s, p.count = count, p.steps = steps, p.tall = m > n;
+    p.a = a, p.b = b, p.c = c;
+    // Between the steps X is kept times 2^q, about the square root of the longer side, which brings its values near 1:
+    // after the last step they are about 1 / 2^q, before the first about 1 / sqrt(m n).
+    int q = 0;
+    while ((int64_t)1 << (2 * (q + 1)) <= (m > n ? m : n)) ++q;
+    p.unit = ldexpf(1.f, q);
+    p.x[0] = x[0], p.x[1] = x[1], p.gram = gram, p.poly = poly, p.out = static_cast<uint16_t*>(d_out);
+    p.ldx = L.ldx, p.xs = (int64_t)m * L.ldx, p.lds = L.lds, p.ss = (int64_t)L.s * L.lds;
+    p.factor = factor, p.counter = counter;
+    p.wide = n % 8 == 0 && aligned(d_out, 16);
+    StepsMaps maps;
+    for (int i = 0; i < 2 && err == cudaSuccess; ++i) {
+        err = make_map(&maps.rows[i], {x[i], L.ldx, p.xs, false}, m, n, count, true);
+        if (err == cudaSuccess) err = make_map(&maps.cols[i], {x[i], L.ldx, p.xs, true}, n, m, count, true);
     }
+    for (int i = 0; i < 2 && err == cudaSuccess; ++i) {
+        err = make_map(&maps.gram[i], {gram, L.lds, p.ss, i == 1}, L.s, L.s, count, true);
+        if (err == cudaSuccess) err = make_map(&maps.poly[i], {poly, L.lds, p.ss, i == 1}, L.s, L.s, count, true);
+    }
+    if (err == cudaSuccess) err = pairs_win(m, n, L.s, count) ? launch_steps<2>(maps, p, stream) : launch_steps<1>(maps, p, stream);
     return err == cudaSuccess ? ONES_OK : ONES_ERR_CUDA;
 }
 
