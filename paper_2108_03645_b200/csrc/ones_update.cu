@@ -9,7 +9,7 @@ namespace ones {
 
 namespace {
 
-constexpr int kNormThreads = 256, kNormBlocks = 4 * kSms;  // a warp takes a row at a time
+constexpr int kNormThreads = 256, kNormBlocks = 8 * kSms;  // a warp takes a row at a time
 
 __device__ __forceinline__ float load_as_float(const void* p, int64_t i, int type) {
     if (type == ONES_F32) return static_cast<const float*>(p)[i];
@@ -381,6 +381,207 @@ __global__ void __launch_bounds__(kMatThreads, 1) k_ns_steps(const __grid_consta
     clear_up<CG>(w, warp, ok);
 }
 
+// A matrix whose shorter side is at most 128 and longer side at most 512 stays in one block's shared memory from its
+// first reading to its result: X lies there as blocks of 64 columns (of the longer side) x 128 rows with the 128-byte
+// swizzle, which serves both as the operand with K along the longer side (X X^T) and as the one with its rows along it
+// (B X). Nothing but the input and the result touches memory and nobody waits for another block: 128 x 256 takes 69 us in
+// k_ns_steps, most of it in the meetings of the blocks.
+constexpr int kSmallSide = 128, kSmallLong = 512, kSmallThreads = 512, kBlockBytes = 128 * 128;
+
+struct SmallArgs {
+    int steps;
+    float a, b, c, eps, unit;
+    uint16_t* out;
+    bool wide;
+};
+
+__global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, const SmallArgs p) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t s_bar;
+    __shared__ uint32_t s_tmem;
+    __shared__ double s_sum[kSmallThreads / 32];
+    __shared__ float s_scale, s_factor;
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
+    const bool tall = g.m > g.n;
+    const int blocks = ((tall ? g.m : g.n) + 63) / 64;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, bar = smem_u32(&s_bar);
+    uint8_t* x = smem_raw + (base - smem_u32(smem_raw));
+    uint8_t* gram = x + blocks * kBlockBytes;
+    uint8_t* poly = gram + 2 * kBlockBytes;
+    const uint32_t x_at = base, gram_at = base + blocks * kBlockBytes, poly_at = gram_at + 2 * kBlockBytes;
+    const uint32_t cols = blocks <= 2 ? 128 : blocks <= 4 ? 256 : 512;  // with this shared memory, what an SM's blocks take together fits
+    if (threadIdx.x == 0) {
+        bar_init(bar, 1);
+        bar_init_done();
+    }
+    if (warp == 0) tmem_alloc<1>(smem_u32(&s_tmem), cols);
+
+    // X0 as in k_ns_norm and k_ns_cast
+    const int64_t from = blockIdx.x * g.stride;
+    double sum = 0.0;
+#pragma unroll 4
+    for (int r = warp; r < g.m; r += kSmallThreads / 32) {
+        if (g.wide) {
+            for (int c = lane * 8; c < g.n; c += 256) {
+                float v[8];
+                load8(g.p, from + r * g.ld + c, g.type, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum = fma((double)v[i], (double)v[i], sum);
+            }
+        } else {
+            for (int c = lane; c < g.n; c += 32) {
+                const double v = load_as_float(g.p, from + r * g.ld + c, g.type);
+                sum = fma(v, v, sum);
+            }
+        }
+    }
+    for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    if (lane == 0) s_sum[warp] = sum;
+    for (int i = threadIdx.x; i < blocks * kBlockBytes / 16; i += kSmallThreads) reinterpret_cast<uint4*>(x)[i] = make_uint4(0, 0, 0, 0);
+    mma_fence_before();
+    __syncthreads();
+    mma_fence_after();
+    const uint32_t tmem = s_tmem;
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < kSmallThreads / 32; ++i) sum += s_sum[i];
+        const double norm = sqrt(sum), rms = norm / sqrt((double)g.m * g.n);
+        int k = rms > 0.0 && rms < 1e300 ? ilogb(rms) : 0;
+        k = k < -120 ? -120 : k > 120 ? 120 : k;
+        s_scale = ldexpf(1.f, -k);
+        s_factor = (float)(ldexp(1.0, k) / (norm + p.eps));
+    }
+    __syncthreads();
+    const float scale = s_scale, factor = s_factor;
+#pragma unroll 4
+    for (int r = warp; r < g.m; r += kSmallThreads / 32) {
+        if (tall) {  // row r of the matrix is column r of X
+            uint8_t* to = x + (r / 64) * kBlockBytes + (r % 8) * 2;
+            for (int c = lane; c < g.n; c += 32)
+                *reinterpret_cast<__half*>(to + c * 128 + (((r % 64 / 8) ^ (c & 7)) << 4)) =
+                    __float2half_rn(load_as_float(g.p, from + r * g.ld + c, g.type) * scale);
+        } else if (g.wide) {
+            for (int c = lane * 8; c < g.n; c += 256) {
+                float v[8];
+                load8(g.p, from + r * g.ld + c, g.type, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] *= scale;
+                *reinterpret_cast<uint4*>(x + (c / 64) * kBlockBytes + r * 128 + (((c % 64 / 8) ^ (r & 7)) << 4)) =
+                    make_uint4(Half16::pack(v[0], v[1], true), Half16::pack(v[2], v[3], true), Half16::pack(v[4], v[5], true),
+                               Half16::pack(v[6], v[7], true));
+            }
+        } else {
+            for (int c = lane; c < g.n; c += 32)
+                *reinterpret_cast<__half*>(x + (c / 64) * kBlockBytes + r * 128 + (((c % 64 / 8) ^ (r & 7)) << 4) + (c % 8) * 2) =
+                    __float2half_rn(load_as_float(g.p, from + r * g.ld + c, g.type) * scale);
+        }
+    }
+
+    const int quad = warp % 4, part = warp / 4, row = quad * 32 + lane;  // a thread has 32 columns of a row at a time
+    const uint32_t lanes = (uint32_t)quad << 21;
+    const uint32_t idesc128 = instruction_desc(1, true, false, false);
+    uint32_t ph = 0;
+    bool ok = true;
+    // What the threads wrote to shared memory is there for the tensor cores; one warp issues, all wait for the end.
+    auto ready = [&] {
+        asm volatile("fence.proxy.async;" ::: "memory");
+        mma_fence_before();
+        __syncthreads();
+        mma_fence_after();
+    };
+    auto wait = [&] {
+        ok = bar_wait(bar, ph, &g_wait_expired) && ok;
+        ph ^= 1;
+        mma_fence_after();
+    };
+    // D[128][128] = A A^T for `n` blocks of 64 columns
+    auto square = [&](uint32_t at, int n) {
+        if (warp == 0) {
+            const uint64_t d = operand_desc(at, false, 0);
+            if (elect_one()) {
+                for (int i = 0; i < n; ++i) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint64_t o = d + (uint64_t)(i * (kBlockBytes >> 4) + j * 2);
+                        mma_f16<1>(tmem, o, o, idesc128, (i | j) != 0);
+                    }
+                }
+                mma_commit<1>(bar);
+            }
+            __syncwarp();
+        }
+    };
+    // 32 values of a row into the 32 columns `n` of a blocked matrix
+    auto put = [&](uint8_t* to, int r, int n, const float (&e)[32], bool f16) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            *reinterpret_cast<uint4*>(to + (n / 2) * kBlockBytes + r * 128 + ((((n & 1) * 4 + c) ^ (r & 7)) << 4)) =
+                make_uint4(Half16::pack(e[8 * c], e[8 * c + 1], f16), Half16::pack(e[8 * c + 2], e[8 * c + 3], f16),
+                           Half16::pack(e[8 * c + 4], e[8 * c + 5], f16), Half16::pack(e[8 * c + 6], e[8 * c + 7], f16));
+    };
+    ready();
+    for (int k = 0; k < p.steps; ++k) {
+        const float f = k == 0 ? factor * factor : 1.f / (p.unit * p.unit);
+        square(x_at, blocks);
+        wait();
+        float v[32];
+        tmem_load(tmem + part * 32 + lanes, v);
+        // the polynomial takes both its terms from the rounded A: their errors then go against each other
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = __half2float(__float2half_rn(v[i] * f));
+        put(gram, row, part, v, true);
+        ready();
+        square(gram_at, 2);
+        wait();
+        {
+            float u[32];
+            tmem_load(tmem + part * 32 + lanes, u);
+            const unsigned d = (unsigned)(row - part * 32);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = fmaf(p.c, u[i], fmaf(p.b, v[i], d == (unsigned)i ? p.a : 0.f));
+        }
+        put(poly, row, part, v, true);
+        ready();
+        if (warp == 0) {
+            const uint64_t da = operand_desc(poly_at, false, 0);
+            if (elect_one()) {
+                for (int n0 = 0; n0 < blocks; n0 += 4) {
+                    const int n = min(4, blocks - n0);
+                    const uint64_t db = operand_desc(x_at + n0 * kBlockBytes, true, kBlockBytes);
+                    const uint32_t idesc = (1u << 4) | (1u << 16) | ((uint32_t)(64 * n / 8) << 17) | ((uint32_t)(128 / 16) << 24);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        mma_f16<1>(tmem + 64 * n0, da + (uint64_t)((j / 4) * (kBlockBytes >> 4) + (j % 4) * 2), db + (uint64_t)(j * (2048 >> 4)), idesc, j != 0);
+                }
+                mma_commit<1>(bar);
+            }
+            __syncwarp();
+        }
+        wait();
+        const bool last = k + 1 == p.steps;
+        const float fx = (k == 0 ? factor : 1.f / p.unit) * (last ? 1.f : p.unit);
+        for (int n = part; n < 2 * blocks; n += kSmallThreads / 128) {
+            tmem_load(tmem + 32 * n + lanes, v);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] *= fx;
+            put(x, row, n, v, !last);
+        }
+        ready();
+    }
+    // the result lies in the place of X, as bfloat16
+    uint16_t* out = p.out + (int64_t)blockIdx.x * g.m * g.n;
+    auto at = [&](int r, int c) { return x + (c / 64) * kBlockBytes + r * 128 + (((c % 64 / 8) ^ (r & 7)) << 4) + (c % 8) * 2; };
+    for (int r = warp; r < g.m; r += kSmallThreads / 32) {
+        if (p.wide && !tall) {
+            for (int c = lane * 8; c < g.n; c += 256) *reinterpret_cast<uint4*>(out + (int64_t)r * g.n + c) = *reinterpret_cast<const uint4*>(at(r, c));
+        } else {
+            for (int c = lane; c < g.n; c += 32) out[(int64_t)r * g.n + c] = *reinterpret_cast<const uint16_t*>(tall ? at(c, r) : at(r, c));
+        }
+    }
+    if (!ok) let_copies_end();
+    __syncthreads();
+    if (warp == 0) tmem_free<1>(tmem, cols);
+}
+
 inline size_t up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 struct Layout {
@@ -515,6 +716,21 @@ int ones_orthogonalize(const void* d_g, int64_t ldg, int64_t stride, int32_t cou
     unsigned* counter = reinterpret_cast<unsigned*>(ws + L.counter);
     const bool wide = n % 8 == 0 && aligned(d_g, 16) && ldg * size % 16 == 0 && stride * size % 16 == 0;
     const Source src = {d_g, ldg, count > 1 ? stride : 0, m, n, type, wide};
+    // Between the steps X is kept times 2^q, about the square root of the longer side, which brings its values near 1:
+    // after the last step they are about 1 / 2^q, before the first about 1 / sqrt(m n).
+    int q = 0;
+    while ((int64_t)1 << (2 * (q + 1)) <= (m > n ? m : n)) ++q;
+    const float unit = ldexpf(1.f, q);
+    const bool wide_out = n % 8 == 0 && aligned(d_out, 16);
+    if (L.s <= kSmallSide && (m > n ? m : n) <= kSmallLong) {
+        const SmallArgs sa = {steps, a, b, c, eps, unit, static_cast<uint16_t*>(d_out), wide_out};
+        const int bytes = (((m > n ? m : n) + 63) / 64 + 4) * kBlockBytes + 1024;
+        static std::atomic<uint64_t> ready{0};
+        cudaError_t err = allow_smem(k_ns_small, (kSmallLong / 64 + 4) * kBlockBytes + 1024, ready);
+        if (err != cudaSuccess) return ONES_ERR_CUDA;
+        k_ns_small<<<count, kSmallThreads, bytes, stream>>>(src, sa);
+        return cudaGetLastError() == cudaSuccess ? ONES_OK : ONES_ERR_CUDA;
+    }
     int blocks = (m + kNormThreads / 32 - 1) / (kNormThreads / 32), most = kNormBlocks / count;
     if (blocks > most) blocks = most > 0 ? most : 1;
     k_ns_norm<<<dim3(blocks, count), kNormThreads, 0, stream>>>(src, part, counter);
@@ -525,15 +741,11 @@ int ones_orthogonalize(const void* d_g, int64_t ldg, int64_t stride, int32_t cou
     StepsArgs p = {};
     p.m = m, p.n = n, p.s = L.s, p.count = count, p.steps = steps, p.tall = m > n;
     p.a = a, p.b = b, p.c = c;
-    // Between the steps X is kept times 2^q, about the square root of the longer side, which brings its values near 1:
-    // after the last step they are about 1 / 2^q, before the first about 1 / sqrt(m n).
-    int q = 0;
-    while ((int64_t)1 << (2 * (q + 1)) <= (m > n ? m : n)) ++q;
-    p.unit = ldexpf(1.f, q);
+    p.unit = unit;
     p.x[0] = x[0], p.x[1] = x[1], p.gram = gram, p.poly = poly, p.out = static_cast<uint16_t*>(d_out);
     p.ldx = L.ldx, p.xs = (int64_t)m * L.ldx, p.lds = L.lds, p.ss = (int64_t)L.s * L.lds;
     p.factor = factor, p.counter = counter;
-    p.wide = n % 8 == 0 && aligned(d_out, 16);
+    p.wide = wide_out;
     StepsMaps maps;
     for (int i = 0; i < 2 && err == cudaSuccess; ++i) {
         err = make_map(&maps.rows[i], {x[i], L.ldx, p.xs, false}, m, n, count, true);
