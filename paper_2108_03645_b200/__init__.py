@@ -3,4 +3,4 @@
 ``inputs`` (seeded synthetic workloads) imports without the CUDA extension;
 everything else needs ``libones.so`` and raises if it is missing.
 """
-__all__ = ["inputs", "binding", "build"]
+__all__ = ["inputs", "binding", "build", "online", "train", "profile_job"]

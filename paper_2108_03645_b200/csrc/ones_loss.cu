@@ -62,12 +62,16 @@ struct EpiStats {
 #pragma unroll
             for (int i = 1; i < 32; ++i) top = fmaxf(top, v[i]);
             const float next = fmaxf(m, top);
-            const float shift = next == -INFINITY ? 0.f : -next * to2;  // nothing but -inf so far: exp gives 0
-            s *= exp2_fast(fmaf(m, to2, shift));
-            float s4[4] = {0.f, 0.f, 0.f, 0.f};
+            const float minus = next == -INFINITY ? 0.f : -next;  // nothing but -inf so far: exp gives 0
+            s *= exp2_fast((m + minus) * to2);
+            // the difference first, which is exact near the maximum: a row that is certain of an entry has s = 1
+            Pair s2[2] = {both(0.f), both(0.f)};
 #pragma unroll
-            for (int i = 0; i < 32; ++i) s4[i & 3] += exp2_fast(fmaf(v[i], to2, shift));
-            s += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+            for (int i = 0; i < 32; i += 2) {
+                const float2 e = split((pair(v[i], v[i + 1]) + both(minus)) * both(to2));
+                s2[i / 2 & 1] = s2[i / 2 & 1] + pair(exp2_fast(e.x), exp2_fast(e.y));
+            }
+            s += total(s2[0] + s2[1]);
             m = next;
         }
         if (row < a.rows) a.part[(int64_t)(at.n * 2 + half) * a.rows + row] = make_float2(m * up, s);
@@ -165,10 +169,12 @@ struct EpiSum {
             float v[32];
             tmem_load(acc + c, v);
             turn.put32(v);
+            uint4 q[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[i] = turn.chunk(4 * i + turn.lane / 8, k);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const uint4 q = turn.chunk(4 * i + turn.lane / 8, k);
-                float4 f = make_float4(__uint_as_float(q.x), __uint_as_float(q.y), __uint_as_float(q.z), __uint_as_float(q.w));
+                float4 f = make_float4(__uint_as_float(q[i].x), __uint_as_float(q[i].y), __uint_as_float(q[i].z), __uint_as_float(q[i].w));
                 if (!a.first) f.x += old[i].x, f.y += old[i].y, f.z += old[i].z, f.w += old[i].w;
                 if (r0 + 4 * i >= shape.M) continue;
                 if (!a.last) {
@@ -221,13 +227,13 @@ struct EpiGrad {
 };
 
 // Joins the slots of a row: R rows a block, 512 / R threads on a row's slots, 8 slots on their way at a time. With few
-// rows R = 4 (a warp reads whole 32-byte sectors) brings more threads to a row, else R = 32.
+// rows R = 4 (a warp reads whole 32-byte sectors) brings more threads to a row, else R = 8.
 constexpr int kJoinThreads = 512;
 
 __device__ __forceinline__ float2 join(float2 a, float2 b) {
     const float m = fmaxf(a.x, b.x);
-    const float shift = m == -INFINITY ? 0.f : -m * kLog2e;
-    return make_float2(m, a.y * exp2_fast(fmaf(a.x, kLog2e, shift)) + b.y * exp2_fast(fmaf(b.x, kLog2e, shift)));
+    const float minus = m == -INFINITY ? 0.f : -m;
+    return make_float2(m, a.y * exp2_fast((a.x + minus) * kLog2e) + b.y * exp2_fast((b.x + minus) * kLog2e));
 }
 
 template <int R>
@@ -484,9 +490,9 @@ int ones_linear_ce(const void* d_hidden, int64_t ldh, const void* d_weight, int6
     const Operand h = {d_hidden, ldh, 0, false}, w = {d_weight, ldw, 0, false};
     const EpiStats::Args ea = {d_target, part, at_target, rows, vocab};
     cudaError_t err = launch_matmul<false, false, EpiStats>(h, w, rows, vocab, cols, 1, false, type == ONES_F16, ea, stream, false);
-    const int r = rows > 4 * kSms ? 32 : 4;
+    const int r = rows > 4 * kSms ? 8 : 4;
     if (err == cudaSuccess)
-        err = launch_after(r == 32 ? k_ce_join<32> : k_ce_join<4>, dim3((rows + r - 1) / r), dim3(kJoinThreads), stream, part,
+        err = launch_after(r == 8 ? k_ce_join<8> : k_ce_join<4>, dim3((rows + r - 1) / r), dim3(kJoinThreads), stream, part,
                            slots_of(rows, vocab), at_target, d_target, rows, vocab, d_loss, d_lse);
     return err == cudaSuccess ? ONES_OK : ONES_ERR_CUDA;
 }

@@ -255,23 +255,44 @@ struct Turn {
         if (wide) {
             const int c = lane & 7, left = cols - (col + 8 * c);
             uint16_t* p = out + (int64_t)(row0 + lane / 8) * ld + col + 8 * c;
+            uint4 q[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[i] = chunk(4 * i + lane / 8, c);
 #pragma unroll
             for (int i = 0; i < 8; ++i, p += 4 * ld) {
                 const int r = 4 * i + lane / 8;
-                const uint4 q = chunk(r, c);
                 if (row0 + r >= rows || left <= 0) continue;
                 if (left >= 8) {
-                    *reinterpret_cast<uint4*>(p) = q;
+                    *reinterpret_cast<uint4*>(p) = q[i];
                 } else {
                     for (int j = 0; j < left; ++j) p[j] = half_at(r, 8 * c + j);
                 }
             }
         } else {
-            const int n = min(32, rows - row0);
-            for (int r = 0; r < n; ++r) {
-                uint16_t* p = out + (int64_t)(row0 + r) * ld + col;
-                if (col + lane < cols) p[lane] = half_at(r, lane);
-                if (col + 32 + lane < cols) p[32 + lane] = half_at(r, 32 + lane);
+            // Two values at a time, from the first place in a row that lies on a 4-byte boundary; what is left over before
+            // and after the pairs goes alone.
+            // Eight rows are read before they are written, since the compiler cannot tell the two memories apart.
+            const int n = min(32, rows - row0), width = min(64, cols - col);
+            uint16_t* p = out + (int64_t)row0 * ld + col;
+#pragma unroll 1
+            for (int r = 0; r < n; r += 8) {
+                uint32_t v[8], lone[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int c = 2 * lane + ((int)(reinterpret_cast<uintptr_t>(p + j * ld) >> 1) & 1);
+                    v[j] = half_at(r + j, c) | (uint32_t)half_at(r + j, min(c + 1, 63)) << 16;
+                    lone[j] = half_at(r + j, 0);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j, p += ld) {
+                    if (r + j >= n) break;
+                    const int odd = (int)(reinterpret_cast<uintptr_t>(p) >> 1) & 1, c = 2 * lane + odd;
+                    if (c + 1 < width)
+                        *reinterpret_cast<uint32_t*>(p + c) = v[j];
+                    else if (c < width)
+                        p[c] = (uint16_t)v[j];
+                    if (odd && lane == 0) p[0] = (uint16_t)lone[j];
+                }
             }
         }
     }
@@ -279,21 +300,31 @@ struct Turn {
         if (wide) {
             const int c = lane & 7, left = cols - (col + 4 * c);
             float* p = out + (int64_t)(row0 + lane / 8) * ld + col + 4 * c;
+            uint4 q[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[i] = chunk(4 * i + lane / 8, c);
 #pragma unroll
             for (int i = 0; i < 8; ++i, p += 4 * ld) {
                 const int r = 4 * i + lane / 8;
-                const uint4 q = chunk(r, c);
                 if (row0 + r >= rows || left <= 0) continue;
                 if (left >= 4) {
-                    *reinterpret_cast<uint4*>(p) = q;
+                    *reinterpret_cast<uint4*>(p) = q[i];
                 } else {
                     for (int j = 0; j < left; ++j) p[j] = word_at(r, 4 * c + j);
                 }
             }
         } else {
             const int n = min(32, rows - row0);
-            for (int r = 0; r < n; ++r)
-                if (col + lane < cols) out[(int64_t)(row0 + r) * ld + col + lane] = word_at(r, lane);
+            float* p = out + (int64_t)row0 * ld + col + lane;
+#pragma unroll 1
+            for (int r = 0; r < n; r += 8) {
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = word_at(r + j, lane);
+#pragma unroll
+                for (int j = 0; j < 8; ++j, p += ld)
+                    if (r + j < n && col + lane < cols) *p = v[j];
+            }
         }
     }
 };

@@ -33,41 +33,6 @@ struct alignas(sizeof(T) * V) Pack {
     T v[V];
 };
 
-// Two 32-bit values that go through one instruction.
-struct Pair {
-    unsigned long long v;
-};
-__device__ __forceinline__ Pair pair(float lo, float hi) {
-    Pair r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ Pair both(float x) { return pair(x, x); }
-__device__ __forceinline__ float2 split(Pair a) {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
-    return r;
-}
-__device__ __forceinline__ Pair operator+(Pair a, Pair b) {
-    Pair r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
-__device__ __forceinline__ Pair operator*(Pair a, Pair b) {
-    Pair r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
-__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
-    Pair r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-    return r;
-}
-__device__ __forceinline__ float total(Pair a) {
-    const float2 f = split(a);
-    return f.x + f.y;
-}
-
 // 16 bytes of a row: 4 values of 32 bits or 8 of 16 bits, as pairs.
 template <class T>
 struct Chunk {

@@ -56,15 +56,8 @@ def lib() -> C.CDLL:
     return _lib
 
 
-def _need(ok, what, *args):
-    if not ok:
-        raise ValueError(what.format(*args))
-
-
 def _device(t: torch.Tensor, call):
-    """None when the tensor's device is current; otherwise the result of `call` made with it current."""
-    if t.device.index == torch.cuda.current_device():
-        return None
+    """The result of `call` made with the tensor's device current."""
     with torch.cuda.device(t.device):
         return call()
 
@@ -89,11 +82,16 @@ def _rows(t: torch.Tensor, align: int = 0) -> tuple[torch.Tensor, int]:
     return t, ld
 
 
-def _space(nbytes: int, device) -> torch.Tensor:
-    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+def _like(t: torch.Tensor) -> torch.Tensor:
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
+def _vector(n: int, dtype, device) -> torch.Tensor:
+    return torch.empty_strided((n,), (1,), dtype=dtype, device=device)
 
 
 _stream_of = torch._C._cuda_getCurrentRawStream  # current_stream(device).cuda_stream without the Stream object
+_current = torch.cuda.current_device
 
 
 def _done(rc: int, where: str):
@@ -101,37 +99,41 @@ def _done(rc: int, where: str):
         raise _b.OnesError(rc, where)
 
 
-def _param(t, cols, x, name):
-    _need(t.dim() == 1 and t.shape[0] == cols and t.device == x.device and t.is_contiguous(),
-          "{}: a contiguous vector of {} values on {} is needed", name, cols, x.device)
-    _need(t.dtype is x.dtype or t.dtype is torch.float32, "{}: float32 or the type of x ({}) is needed, not {}", name, x.dtype, t.dtype)
+def _is_param(t, cols, x) -> bool:
+    return (t.dim() == 1 and t.size(0) == cols and t.device == x.device and t.is_contiguous() and
+            (t.dtype is torch.float32 or t.dtype is x.dtype))
 
 
 def layer_norm(x: torch.Tensor, weight=None, bias=None, eps: float = 1e-5):
     """Layer norm over the last dimension (``ones_layer_norm``): (y, mean, rstd), mean and rstd in float32 with x's
     leading dimensions.  weight and bias: None, or vectors of x's type or of float32 (both of one type)."""
-    kind = _TYPES.get(x.dtype)
-    _need(kind is not None and x.is_cuda and x.dim() >= 1, "x: a float32, bfloat16 or float16 CUDA tensor is needed")
-    shape = x.shape
-    cols = shape[-1]
+    kind = _TYPES.get(x.dtype) if x.is_cuda and x.dim() else None
+    if kind is None:
+        raise ValueError("x: a float32, bfloat16 or float16 CUDA tensor is needed")
+    lead, cols, device = x.shape[:-1], x.shape[-1], x.device
     wkind = F32
     wp = bp = None
     if bias is not None:
-        _param(bias, cols, x, "bias")
+        if not _is_param(bias, cols, x):
+            raise ValueError(f"bias: a contiguous vector of {cols} values of float32 or x's type on {device} is needed")
         wkind, bp = _TYPES[bias.dtype], bias.data_ptr()
     if weight is not None:
-        _param(weight, cols, x, "weight")
-        _need(bias is None or bias.dtype is weight.dtype, "weight and bias need one type")
+        if not _is_param(weight, cols, x) or (bias is not None and bias.dtype is not weight.dtype):
+            raise ValueError(f"weight: a contiguous vector of {cols} values of float32 or x's type on {device} is needed, "
+                             "of one type with bias")
         wkind, wp = _TYPES[weight.dtype], weight.data_ptr()
-    if (other := _device(x, lambda: layer_norm(x, weight, bias, eps))) is not None:
-        return other
-    device = x.device
+    index = device.index
+    if index != _current():
+        return _device(x, lambda: layer_norm(x, weight, bias, eps))
     p, ld = _rows(x)
-    y = torch.empty(shape, dtype=x.dtype, device=device)
-    mean = torch.empty(shape[:-1], dtype=torch.float32, device=device)
+    rows = p.size(0)
+    y = _like(x)
+    mean = _vector(rows, torch.float32, device)
     rstd = torch.empty_like(mean)
-    _done(lib().ones_layer_norm(p.data_ptr(), ld, wp, bp, p.shape[0], cols, eps, kind, wkind, y.data_ptr(), cols, mean.data_ptr(),
-                                rstd.data_ptr(), _stream_of(device.index)), "ones_layer_norm")
+    _done((_lib or lib()).ones_layer_norm(p.data_ptr(), ld, wp, bp, rows, cols, eps, kind, wkind, y.data_ptr(), cols,
+                                          mean.data_ptr(), rstd.data_ptr(), _stream_of(index)), "ones_layer_norm")
+    if len(lead) != 1:
+        mean, rstd = mean.view(lead), rstd.view(lead)
     return y, mean, rstd
 
 
@@ -139,65 +141,74 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
                         parameters: bool = True):
     """Gradients of `layer_norm` (``ones_layer_norm_backward``): (dx, dweight, dbias), the latter two in the type of
     weight (float32 where it is None), or None both with parameters=False."""
-    kind = _TYPES.get(x.dtype)
-    _need(kind is not None and x.is_cuda and x.dim() >= 1, "x: a float32, bfloat16 or float16 CUDA tensor is needed")
-    _need(dy.shape == x.shape and dy.dtype is x.dtype and dy.device == x.device, "dy needs x's shape, type and device")
-    cols = x.shape[-1]
+    kind = _TYPES.get(x.dtype) if x.is_cuda and x.dim() else None
+    if kind is None:
+        raise ValueError("x: a float32, bfloat16 or float16 CUDA tensor is needed")
+    shape, device = x.shape, x.device
+    cols = shape[-1]
+    if dy.shape != shape or dy.dtype is not x.dtype or dy.device != device:
+        raise ValueError("dy needs x's shape, type and device")
     wt, wp = torch.float32, None
     if weight is not None:
-        _param(weight, cols, x, "weight")
+        if not _is_param(weight, cols, x):
+            raise ValueError(f"weight: a contiguous vector of {cols} values of float32 or x's type on {device} is needed")
         wt, wp = weight.dtype, weight.data_ptr()
     for s in (mean, rstd):
-        _need(s.dtype is torch.float32 and s.device == x.device and s.shape == x.shape[:-1] and s.is_contiguous(),
-              "mean, rstd: what layer_norm returned is needed")
-    if (other := _device(x, lambda: layer_norm_backward(dy, x, mean, rstd, weight, parameters=parameters))) is not None:
-        return other
-    device = x.device
+        if s.dtype is not torch.float32 or s.device != device or s.shape != shape[:-1] or not s.is_contiguous():
+            raise ValueError("mean, rstd: what layer_norm returned is needed")
+    index = device.index
+    if index != _current():
+        return _device(x, lambda: layer_norm_backward(dy, x, mean, rstd, weight, parameters=parameters))
+    L = _lib or lib()
     p, ld = _rows(x)
     q, ldq = _rows(dy)
-    rows = p.shape[0]
-    dx = torch.empty(x.shape, dtype=x.dtype, device=device)
+    rows = p.size(0)
+    dx = _like(x)
     dw = db = dwp = dbp = sp = None
     nbytes = 0
     if parameters:
-        dw = torch.empty(cols, dtype=wt, device=device)
+        dw = torch.empty_like(weight) if weight is not None else _vector(cols, wt, device)
         db = torch.empty_like(dw)
-        nbytes = lib().ones_layer_norm_workspace_bytes(rows, cols)
-        space = _space(nbytes, device)
+        nbytes = L.ones_layer_norm_workspace_bytes(rows, cols)
+        space = _vector(nbytes, torch.uint8, device)
         dwp, dbp, sp = dw.data_ptr(), db.data_ptr(), space.data_ptr()
-    _done(lib().ones_layer_norm_backward(q.data_ptr(), ldq, p.data_ptr(), ld, mean.data_ptr(), rstd.data_ptr(), wp, rows, cols, kind,
-                                         _TYPES[wt], dx.data_ptr(), cols, dwp, dbp, sp, nbytes, _stream_of(device.index)),
+    _done(L.ones_layer_norm_backward(q.data_ptr(), ldq, p.data_ptr(), ld, mean.data_ptr(), rstd.data_ptr(), wp, rows, cols, kind,
+                                     _TYPES[wt], dx.data_ptr(), cols, dwp, dbp, sp, nbytes, _stream_of(index)),
           "ones_layer_norm_backward")
     return dx, dw, db
 
 
 def _ce_args(hidden, weight, target):
-    _need(hidden.is_cuda and (hidden.dtype is torch.bfloat16 or hidden.dtype is torch.float16) and hidden.dim() >= 1,
-          "hidden: a bfloat16 or float16 CUDA tensor is needed")
-    _need(weight.dim() == 2 and weight.dtype is hidden.dtype and weight.device == hidden.device and
-          weight.shape[1] == hidden.shape[-1], "weight: [vocab][cols] of hidden's type and device is needed")
-    _need(target.dtype is torch.int64 and target.device == hidden.device and target.shape == hidden.shape[:-1],
-          "target: int64 with hidden's leading dimensions is needed")
+    if not hidden.is_cuda or hidden.dtype not in (torch.bfloat16, torch.float16) or not hidden.dim():
+        raise ValueError("hidden: a bfloat16 or float16 CUDA tensor is needed")
+    if (weight.dim() != 2 or weight.dtype is not hidden.dtype or weight.device != hidden.device or
+            weight.size(1) != hidden.size(-1)):
+        raise ValueError("weight: [vocab][cols] of hidden's type and device is needed")
+    if target.dtype is not torch.int64 or target.device != hidden.device or target.shape != hidden.shape[:-1]:
+        raise ValueError("target: int64 with hidden's leading dimensions is needed")
 
 
 def linear_cross_entropy(hidden: torch.Tensor, weight: torch.Tensor, target: torch.Tensor):
     """Cross entropy of ``hidden @ weight.T`` at `target` without keeping the logits (``ones_linear_ce``): (loss, lse),
     float32 with hidden's leading dimensions.  Rows whose target is outside [0, vocab) have loss 0."""
     _ce_args(hidden, weight, target)
-    if (other := _device(hidden, lambda: linear_cross_entropy(hidden, weight, target))) is not None:
-        return other
     device = hidden.device
+    index = device.index
+    if index != _current():
+        return _device(hidden, lambda: linear_cross_entropy(hidden, weight, target))
+    L = _lib or lib()
     h, ldh = _rows(hidden, 8)
     w, ldw = _rows(weight, 8)
     t = target.contiguous()
-    rows, vocab = h.shape[0], weight.shape[0]
-    loss = torch.empty(target.shape, dtype=torch.float32, device=device)
+    rows, vocab, lead = h.size(0), w.size(0), target.shape
+    loss = _vector(rows, torch.float32, device)
     lse = torch.empty_like(loss)
-    nbytes = lib().ones_linear_ce_workspace_bytes(rows, vocab)
-    space = _space(nbytes, device)
-    _done(lib().ones_linear_ce(h.data_ptr(), ldh, w.data_ptr(), ldw, t.data_ptr(), rows, hidden.shape[-1], vocab,
-                               _TYPES[hidden.dtype], loss.data_ptr(), lse.data_ptr(), space.data_ptr(), nbytes,
-                               _stream_of(device.index)), "ones_linear_ce")
+    nbytes = L.ones_linear_ce_workspace_bytes(rows, vocab)
+    space = _vector(nbytes, torch.uint8, device)
+    _done(L.ones_linear_ce(h.data_ptr(), ldh, w.data_ptr(), ldw, t.data_ptr(), rows, hidden.size(-1), vocab, _TYPES[hidden.dtype],
+                           loss.data_ptr(), lse.data_ptr(), space.data_ptr(), nbytes, _stream_of(index)), "ones_linear_ce")
+    if len(lead) != 1:
+        loss, lse = loss.view(lead), lse.view(lead)
     return loss, lse
 
 
@@ -208,37 +219,43 @@ def linear_cross_entropy_backward(dloss: torch.Tensor, hidden: torch.Tensor, wei
     vocabulary that are taken at a time (a multiple of 256; 0: the library's choice)."""
     _ce_args(hidden, weight, target)
     wt = weight_gradient or weight.dtype
-    _need(wt is torch.float32 or wt is weight.dtype, "weight_gradient: float32 or weight's type is needed")
-    for s in (dloss, lse):
-        _need(s.dtype is torch.float32 and s.device == hidden.device and s.shape == target.shape,
-              "dloss, lse: float32 with target's shape is needed")
-    if (other := _device(hidden, lambda: linear_cross_entropy_backward(dloss, hidden, weight, target, lse,
-                                                                       weight_gradient=weight_gradient, piece=piece))) is not None:
-        return other
+    if wt is not torch.float32 and wt is not weight.dtype:
+        raise ValueError("weight_gradient: float32 or weight's type is needed")
     device = hidden.device
+    for s in (dloss, lse):
+        if s.dtype is not torch.float32 or s.device != device or s.shape != target.shape:
+            raise ValueError("dloss, lse: float32 with target's shape is needed")
+    index = device.index
+    if index != _current():
+        return _device(hidden, lambda: linear_cross_entropy_backward(dloss, hidden, weight, target, lse,
+                                                                     weight_gradient=weight_gradient, piece=piece))
+    L = _lib or lib()
     h, ldh = _rows(hidden)
     w, ldw = _rows(weight, 8)
     t, g, l = target.contiguous(), dloss.contiguous(), lse.contiguous()
-    rows, cols, vocab = h.shape[0], hidden.shape[-1], weight.shape[0]
-    dh = torch.empty(hidden.shape, dtype=hidden.dtype, device=device)
+    rows, cols, vocab = h.size(0), hidden.size(-1), w.size(0)
+    dh = _like(hidden)
     dw = torch.empty(weight.shape, dtype=wt, device=device)
-    nbytes = lib().ones_linear_ce_backward_workspace_bytes(rows, cols, vocab, piece)
-    space = _space(nbytes, device)
-    _done(lib().ones_linear_ce_backward(g.data_ptr(), h.data_ptr(), ldh, w.data_ptr(), ldw, t.data_ptr(), l.data_ptr(), rows, cols,
-                                        vocab, _TYPES[hidden.dtype], _TYPES[wt], piece, dh.data_ptr(), cols, dw.data_ptr(), cols,
-                                        space.data_ptr(), nbytes, _stream_of(device.index)), "ones_linear_ce_backward")
+    nbytes = L.ones_linear_ce_backward_workspace_bytes(rows, cols, vocab, piece)
+    space = _vector(nbytes, torch.uint8, device)
+    _done(L.ones_linear_ce_backward(g.data_ptr(), h.data_ptr(), ldh, w.data_ptr(), ldw, t.data_ptr(), l.data_ptr(), rows, cols,
+                                    vocab, _TYPES[hidden.dtype], _TYPES[wt], piece, dh.data_ptr(), cols, dw.data_ptr(), cols,
+                                    space.data_ptr(), nbytes, _stream_of(index)), "ones_linear_ce_backward")
     return dh, dw
 
 
 def orthogonalize(g: torch.Tensor, *, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7) -> torch.Tensor:
     """Newton-Schulz orthogonalised update (``ones_orthogonalize``) of a matrix [m][n], or of several [count][m][n], in
     bfloat16."""
-    kind = _TYPES.get(g.dtype)
-    _need(kind is not None and g.is_cuda and g.dim() in (2, 3), "g: a float32, bfloat16 or float16 CUDA matrix is needed, or several")
+    kind = _TYPES.get(g.dtype) if g.is_cuda and g.dim() in (2, 3) else None
+    if kind is None:
+        raise ValueError("g: a float32, bfloat16 or float16 CUDA matrix is needed, or several")
     a, b, c = coefficients
-    if (other := _device(g, lambda: orthogonalize(g, steps=steps, coefficients=coefficients, eps=eps))) is not None:
-        return other
     device = g.device
+    index = device.index
+    if index != _current():
+        return _device(g, lambda: orthogonalize(g, steps=steps, coefficients=coefficients, eps=eps))
+    L = _lib or lib()
     s = g if g.dim() == 3 else g[None]
     count, m, n = s.shape
     if (s.stride(2) != 1 and n > 1) or (s.stride(1) < n and m > 1):
@@ -246,12 +263,12 @@ def orthogonalize(g: torch.Tensor, *, steps: int = 5, coefficients=(3.4445, -4.7
     out = torch.empty(g.shape, dtype=torch.bfloat16, device=device)
     if count * m * n == 0:
         return out
-    nbytes = lib().ones_orthogonalize_workspace_bytes(count, m, n)
+    nbytes = L.ones_orthogonalize_workspace_bytes(count, m, n)
     if nbytes == 0:
         raise _b.OnesError(-3, "ones_orthogonalize_workspace_bytes")
-    space = _space(nbytes, device)
-    _done(lib().ones_orthogonalize(s.data_ptr(), s.stride(1) if m > 1 else n, s.stride(0), count, m, n, kind, steps, a, b, c, eps,
-                                   out.data_ptr(), space.data_ptr(), nbytes, _stream_of(device.index)), "ones_orthogonalize")
+    space = _vector(nbytes, torch.uint8, device)
+    _done(L.ones_orthogonalize(s.data_ptr(), s.stride(1) if m > 1 else n, s.stride(0), count, m, n, kind, steps, a, b, c, eps,
+                               out.data_ptr(), space.data_ptr(), nbytes, _stream_of(index)), "ones_orthogonalize")
     return out
 
 
