@@ -132,30 +132,81 @@ __global__ void __launch_bounds__(kNormThreads) k_ns_cast(Source g, const double
 // The symmetric products have only their blocks on and above the diagonal computed and stored. The products that read
 // them take what lies below from above, as an operand with its rows contiguous (Lie::upper).
 
-// A = factor * X X^T
+// A = factor * X X^T, and its diagonal in 32 bits.
 struct EpiGram {
     struct Args {
         __half* out;
+        float* diag;  // [count][s]
         int64_t ld, batch_ld;
         int s;
         float factor;
         const float2* first;  // the first step's f^2, or NULL
+        float* part;          // where K is cut: the sums of this part [count][s][ld_part], else NULL
+        int64_t ld_part;
     };
     template <int W>
     static __device__ __forceinline__ void tile(const Args& a, uint32_t acc, int row, int col, const TileAt& at, const Turn& turn) {
+        if (a.part) {
+            float* out = a.part + (int64_t)at.b * a.s * a.ld_part;
+#pragma unroll 1
+            for (int c = 0; c < W && col + c < a.s; c += 32) {
+                float v[32];
+                tmem_load(acc + c, v);
+                turn.put32(v);
+                turn.store32(out, a.ld_part, row - turn.lane, col + c, a.s, a.s, true);
+            }
+            return;
+        }
         const float f = a.first ? a.first[at.b].y : a.factor;
         uint16_t* out = reinterpret_cast<uint16_t*>(a.out + at.b * a.batch_ld);
 #pragma unroll 1
         for (int c = 0; c < W && col + c < a.s; c += 64) {
             float v[64];
             tmem_load(acc + c, v);
+            const unsigned d = (unsigned)(row - (col + c));
+            if (d < 64u && row < a.s) {
+                float own = 0.f;
+#pragma unroll
+                for (int i = 0; i < 64; ++i) own = d == (unsigned)i ? v[i] : own;
+                a.diag[(int64_t)at.b * a.s + row] = own * f;
+            }
 #pragma unroll
             for (int i = 0; i < 64; ++i) v[i] *= f;
             turn.put16(v, true);
             turn.store16(out, a.ld, row - turn.lane, col + c, a.s, a.s, true);
         }
     }
+    // Joins the parts of a row's sums, in order, from the diagonal's block on. Run by a warp.
+    static __device__ __forceinline__ void join(const Args& a, int parts, int64_t stride, int b, int row, int block, int lane) {
+        const float f = a.first ? a.first[b].y : a.factor;
+        const float* from = a.part + ((int64_t)b * a.s + row) * a.ld_part;
+        __half* to = a.out + b * a.batch_ld + (int64_t)row * a.ld;
+        for (int c = row / block * block + 4 * lane; c < a.s; c += 128) {
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+            for (int k = 0; k < parts; ++k) {
+                const float4 q = __ldcg(reinterpret_cast<const float4*>(from + k * stride + c));
+                v.x += q.x, v.y += q.y, v.z += q.z, v.w += q.w;
+            }
+            v.x *= f, v.y *= f, v.z *= f, v.w *= f;
+            if (row >= c && row < c + 4) a.diag[(int64_t)b * a.s + row] = row == c ? v.x : row == c + 1 ? v.y : row == c + 2 ? v.z : v.w;
+            // the row is padded to whole 16 bytes; what lies behind its end is not read
+            *reinterpret_cast<uint2*>(to + c) = make_uint2(Half16::pack(v.x, v.y, true), Half16::pack(v.z, v.w, true));
+        }
+    }
 };
+
+// An entry of the diagonal of the polynomial from the entry of A in 32 bits: a product of rounded matrices has it with
+// the error of the rounded entry, which is the largest of its row and the same for the whole row of the next product.
+__device__ __forceinline__ float mend_diagonal(float p, float exact, float a, float b, float c) {
+    const float rounded = __half2float(__float2half_rn(exact));
+    return p + a + b * (exact - rounded) + c * (exact * exact - rounded * rounded);
+}
+// What a row of the next product has to be multiplied by so that the rounding of the diagonal's entry does not count.
+__device__ __forceinline__ float regain_row(float p) {
+    const float rounded = __half2float(__float2half_rn(p)), r = __fdividef(p, rounded);
+    return fabsf(r - 1.f) < 0.002f ? r : 1.f;  // not where the entry is next to nothing
+}
 
 // B = a I + b A + c A A. With a I inside B the next product needs no second operand, and B's values near the end are
 // those of a I + b A + c A^2 (about 1), not of its terms (several times that), so its rounding is finer.
@@ -163,6 +214,8 @@ struct EpiPoly {
     struct Args {
         const __half* gram;
         __half* out;
+        const float* diag;
+        float* regain;  // [count][s]
         int64_t ld, batch_ld;
         int s;
         float a, b, c;
@@ -178,7 +231,8 @@ struct EpiPoly {
         }
     }
     template <int W>
-    static __device__ __forceinline__ void tile(const Args& a, uint32_t acc, int row, int col, const TileAt& at, const Turn& turn, uint4 (&q)[8]) {
+    static __device__ __forceinline__ void tile(const Args& a, uint32_t acc, int row, int col, const TileAt& at, const Turn& turn, uint4 (&q)[8],
+                                                float exact) {
         uint16_t* out = reinterpret_cast<uint16_t*>(a.out + at.b * a.batch_ld);
 #pragma unroll 1
         for (int c = 0; c < W && col + c < a.s; c += 64) {
@@ -201,10 +255,14 @@ struct EpiPoly {
                 }
             }
             const unsigned d = (unsigned)(row - (col + c));
-            if (d < 64u) {
+            if (d < 64u && row < a.s) {
+                float own = 0.f;
 #pragma unroll
-                for (int i = 0; i < 64; ++i)
-                    if (d == (unsigned)i) v[i] += a.a;
+                for (int i = 0; i < 64; ++i) own = d == (unsigned)i ? v[i] : own;
+                own = mend_diagonal(own, exact, a.a, a.b, a.c);
+#pragma unroll
+                for (int i = 0; i < 64; ++i) v[i] = d == (unsigned)i ? own : v[i];
+                a.regain[(int64_t)at.b * a.s + row] = regain_row(own);
             }
             turn.put16(v, true);
             turn.store16(out, a.ld, row - turn.lane, col + c, a.s, a.s, true);
@@ -220,17 +278,31 @@ struct EpiApply {
         int m, n;
         float factor;
         const float2* first;  // the first step's f, or NULL
-        bool f16, wide;
+        const float* regain;  // [count][s]: of the rows, or (tall) of the columns
+        bool tall, f16, wide;
     };
     template <int W>
-    static __device__ __forceinline__ void tile(const Args& a, uint32_t acc, int row, int col, const TileAt& at, const Turn& turn) {
-        const float f = a.first ? a.factor * a.first[at.b].x : a.factor;
+    static __device__ __forceinline__ void tile(const Args& a, uint32_t acc, int row, int col, const TileAt& at, const Turn& turn, float own) {
+        const float* regain = a.regain + (int64_t)at.b * a.n;
+        const float f = (a.first ? a.factor * a.first[at.b].x : a.factor) * own;
 #pragma unroll 1
         for (int c = 0; c < W && col + c < a.n; c += 64) {
-            float v[64];
+            float v[64], r0 = 1.f, r1 = 1.f;
+            if (a.tall) {
+                const int k = col + c + 2 * turn.lane;
+                if (k < a.n) r0 = __ldcg(regain + k);
+                if (k + 1 < a.n) r1 = __ldcg(regain + k + 1);
+            }
             tmem_load(acc + c, v);
 #pragma unroll
             for (int i = 0; i < 64; ++i) v[i] *= f;
+            if (a.tall) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    v[2 * i] *= __shfl_sync(0xFFFFFFFFu, r0, i);
+                    v[2 * i + 1] *= __shfl_sync(0xFFFFFFFFu, r1, i);
+                }
+            }
             turn.put16(v, a.f16);
             turn.store16(a.out + at.b * a.batch_ld, a.ld, row - turn.lane, col + c, a.m, a.n, a.wide);
         }
@@ -243,6 +315,9 @@ struct EpiApply {
 // accumulators, and meet at a counter between products (a cooperative launch: all of them are on the GPU).
 struct StepsArgs {
     int m, n, s, count, steps;
+    int parts;  // > 1: K of the Gram matrix is cut into so many parts, joined in a round of its own
+    float *diag, *regain, *part;
+    int64_t ld_part, part_stride;
     bool tall;  // more rows than columns: the Gram matrix is X^T X and X takes the polynomial from the right
     float a, b, c, unit;  // unit: X is kept times this between the steps
     __half *x[2], *gram, *poly;
@@ -298,23 +373,41 @@ __global__ void __launch_bounds__(kMatThreads, 1) k_ns_steps(const __grid_consta
     const int per_sym = tiles_per_matrix(sym), per_app = tiles_per_matrix(app);
     const int long_side = p.tall ? p.m : p.n;
     const int nk_gram = (long_side + kTileK - 1) / kTileK, nk_s = (p.s + kTileK - 1) / kTileK;
-    const int rounds = 3 * p.steps;
+    // a step's rounds: Gram matrix, (3: its parts joined,) polynomial, application
+    const int per_step = p.parts > 1 ? 4 : 3, rounds = per_step * p.steps;
+    const int gram_part = (nk_gram + p.parts - 1) / p.parts;
+    auto which_of = [&](int round) {
+        const int i = round % per_step;
+        return per_step == 3 ? i : i == 0 ? 0 : i == 1 ? 3 : i - 1;
+    };
+    auto tiles_in = [&](int which) { return which == 0 ? per_sym * p.count * p.parts : which == 1 ? per_sym * p.count : which == 2 ? per_app * p.count : 0; };
+    // tile t of a round, the part of K that it takes and what that is
+    auto tile_of = [&](int which, int t, int& k0, int& nk, int& cut) {
+        cut = 0;
+        if (which == 0) {
+            cut = t / (per_sym * p.count);
+            t -= cut * per_sym * p.count;
+            k0 = cut * gram_part, nk = min(gram_part, nk_gram - k0);
+        } else {
+            k0 = 0, nk = nk_s;
+        }
+        return tile_at(which == 2 ? app : sym, t, which == 2 ? per_app : per_sym);
+    };
     bool ok = true;
 
     if (warp == 0) {
         const uint32_t full_at = CG == 2 ? map_to_rank(w.full, 0) : w.full;
         Ring r = {w.base, w.full, w.empty};
         for (int round = 0; ok && round < rounds; ++round) {
-            const int which = round % 3, buf = round / 3 & 1;
+            const int which = which_of(round), buf = round / per_step & 1, total = tiles_in(which);
             if (round && !(ok = wait_all(p.counter, (unsigned)round * gridDim.x, &g_wait_expired))) break;
             if (round && lane == 0) bar_arrive(round_bar);
-            const MatShape& g = which == 2 ? app : sym;
-            const int per = which == 2 ? per_app : per_sym, total = per * p.count, nk = which == 0 ? nk_gram : nk_s;
             for (int t = first; ok && t < total; t += step) {
-                const TileAt at = tile_at(g, t, per);
+                int k0, nk, cut;
+                const TileAt at = tile_of(which, t, k0, nk, cut);
                 View va, vb;
                 operands(maps, p.tall, which, buf, at, va, vb);
-                ok = fill_tile<CG>(r, va, vb, at.m * BN + (int)rank * 128, at.n * BN + (int)rank * 128, at.b, 0, nk, rank, full_at);
+                ok = fill_tile<CG>(r, va, vb, at.m * BN + (int)rank * 128, at.n * BN + (int)rank * 128, at.b, k0, k0 + nk, rank, full_at);
             }
         }
     } else if (warp == 1 && rank == 0) {
@@ -322,12 +415,11 @@ __global__ void __launch_bounds__(kMatThreads, 1) k_ns_steps(const __grid_consta
         int acc = 0;
         uint32_t aph = 0;
         for (int round = 0; ok && round < rounds; ++round) {
-            const int which = round % 3;
-            const MatShape& g = which == 2 ? app : sym;
-            const int per = which == 2 ? per_app : per_sym, total = per * p.count, nk = which == 0 ? nk_gram : nk_s;
+            const int which = which_of(round), total = tiles_in(which);
             for (int t = first; ok && t < total; t += step) {
+                int k0, nk, cut;
                 View va, vb;
-                operands(maps, p.tall, which, 0, tile_at(g, t, per), va, vb);
+                operands(maps, p.tall, which, 0, tile_of(which, t, k0, nk, cut), va, vb);
                 if (!(ok = bar_wait(w.free_ + 8 * acc, aph ^ 1, &g_wait_expired))) break;
                 mma_fence_after();
                 ok = multiply_tile<CG>(r, w.tmem + acc * BN, nk, va, vb, true, w.done + 8 * acc);
@@ -341,35 +433,42 @@ __global__ void __launch_bounds__(kMatThreads, 1) k_ns_steps(const __grid_consta
         int acc = 0;
         uint32_t aph = 0;
         for (int round = 0; round < rounds; ++round) {  // a warp that gave up still comes to the barrier below
-            const int which = round % 3, k = round / 3, buf = k & 1;
+            const int which = which_of(round), k = round / per_step, buf = k & 1, total = tiles_in(which);
             if (ok && round) ok = __all_sync(0xFFFFFFFFu, bar_wait(round_bar, (round - 1) & 1, &g_wait_expired));
-            const MatShape& g = which == 2 ? app : sym;
-            const int per = which == 2 ? per_app : per_sym, total = per * p.count;
             const float2* start = k == 0 ? p.factor : nullptr;
+            EpiGram::Args eg = {p.gram, p.diag, p.lds, p.ss, p.s, 1.f / (p.unit * p.unit), start, p.part, p.ld_part};
+            if (ok && which == 3)
+                for (int i = blockIdx.x * kEpiWarps + warp - 4; i < p.count * p.s; i += gridDim.x * kEpiWarps)
+                    EpiGram::join(eg, p.parts, p.part_stride, i / p.s, i % p.s, BN, lane);
             for (int t = first; ok && t < total; t += step) {
-                const TileAt at = tile_at(g, t, per);
+                int k0, nk, cut;
+                const TileAt at = tile_of(which, t, k0, nk, cut);
                 const int row = at.m * BN + (int)rank * 128 + quad * 32 + lane, col = at.n * BN + half * (BN / 2);
                 const uint32_t tmem = w.tmem + acc * BN + half * (BN / 2) + ((uint32_t)quad << 21);
-                const EpiPoly::Args ep = {p.gram, p.poly, p.lds, p.ss, p.s, p.a, p.b, p.c};
+                const EpiPoly::Args ep = {p.gram, p.poly, p.diag, p.regain, p.lds, p.ss, p.s, p.a, p.b, p.c};
                 uint4 q[8];
+                // what the epilogue needs of the round before, asked for while the tile is multiplied
+                float own = 1.f;
                 if (which == 1) EpiPoly::load(ep, row, col, at, turn, q);
+                if (row < p.s && (which == 1 || (which == 2 && !p.tall)))
+                    own = __ldcg((which == 1 ? p.diag : p.regain) + (int64_t)at.b * p.s + row);
                 ok = bar_wait(w.done + 8 * acc, aph, &g_wait_expired);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 mma_fence_after();
                 if (which == 0) {
-                    const EpiGram::Args e = {p.gram, p.lds, p.ss, p.s, 1.f / (p.unit * p.unit), start};
-                    EpiGram::tile<BN / 2>(e, tmem, row, col, at, turn);
+                    if (p.part) eg.part = p.part + cut * p.part_stride;
+                    EpiGram::tile<BN / 2>(eg, tmem, row, col, at, turn);
                 } else if (which == 1) {
-                    EpiPoly::tile<BN / 2>(ep, tmem, row, col, at, turn, q);
+                    EpiPoly::tile<BN / 2>(ep, tmem, row, col, at, turn, q, own);
                 } else {
-                    EpiApply::Args e = {reinterpret_cast<uint16_t*>(p.x[1 - buf]), p.ldx, p.xs, p.m, p.n, start ? p.unit : 1.f, start, true, true};
+                    EpiApply::Args e = {reinterpret_cast<uint16_t*>(p.x[1 - buf]), p.ldx, p.xs, p.m, p.n, start ? p.unit : 1.f, start, p.regain, p.tall, true, true};
                     if (k + 1 == p.steps) {
                         e.out = p.out, e.ld = p.n, e.batch_ld = (int64_t)p.m * p.n;
                         e.factor = start ? 1.f : 1.f / p.unit;
                         e.f16 = false, e.wide = p.wide;
                     }
-                    EpiApply::tile<BN / 2>(e, tmem, row, col, at, turn);
+                    EpiApply::tile<BN / 2>(e, tmem, row, col, at, turn, own);
                 }
                 free_accumulator<CG>(free_at + 8 * acc, lane);
                 if (++acc == 2) acc = 0, aph ^= 1;
@@ -400,7 +499,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, c
     __shared__ __align__(8) uint64_t s_bar;
     __shared__ uint32_t s_tmem;
     __shared__ double s_sum[kSmallThreads / 32];
-    __shared__ float s_scale, s_factor;
+    __shared__ float s_scale, s_factor, s_regain[128];
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const bool tall = g.m > g.n;
     const int blocks = ((tall ? g.m : g.n) + 63) / 64;
@@ -525,6 +624,13 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, c
         wait();
         float v[32];
         tmem_load(tmem + part * 32 + lanes, v);
+        const unsigned d = (unsigned)(row - part * 32);
+        float exact = 0.f;
+        if (d < 32u) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) exact = d == (unsigned)i ? v[i] : exact;
+            exact *= f;
+        }
         // the polynomial takes both its terms from the rounded A: their errors then go against each other
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] = __half2float(__float2half_rn(v[i] * f));
@@ -535,9 +641,17 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, c
         {
             float u[32];
             tmem_load(tmem + part * 32 + lanes, u);
-            const unsigned d = (unsigned)(row - part * 32);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = fmaf(p.c, u[i], fmaf(p.b, v[i], d == (unsigned)i ? p.a : 0.f));
+            for (int i = 0; i < 32; ++i) v[i] = fmaf(p.c, u[i], p.b * v[i]);
+            if (d < 32u) {  // all of a warp or none
+                float own = 0.f;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) own = d == (unsigned)i ? v[i] : own;
+                own = mend_diagonal(own, exact, p.a, p.b, p.c);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = d == (unsigned)i ? own : v[i];
+                s_regain[row] = regain_row(own);
+            }
         }
         put(poly, row, part, v, true);
         ready();
@@ -558,7 +672,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, c
         }
         wait();
         const bool last = k + 1 == p.steps;
-        const float fx = (k == 0 ? factor : 1.f / p.unit) * (last ? 1.f : p.unit);
+        const float fx = (k == 0 ? factor : 1.f / p.unit) * (last ? 1.f : p.unit) * s_regain[row];
         for (int n = part; n < 2 * blocks; n += kSmallThreads / 128) {
             tmem_load(tmem + 32 * n + lanes, v);
 #pragma unroll
@@ -584,16 +698,57 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, c
 
 inline size_t up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
+int64_t tiles_of(int64_t rows, int64_t cols, int64_t b) { return ((rows + b - 1) / b) * ((cols + b - 1) / b); }
+int64_t half_tiles_of(int64_t s, int64_t b) { return ((s + b - 1) / b) * ((s + b - 1) / b + 1) / 2; }
+
+bool stays_in_a_block(int m, int n) { return (m < n ? m : n) <= kSmallSide && (m < n ? n : m) <= kSmallLong; }
+
+// Pairs of CTAs or single ones, and the parts of the Gram matrix's K: the smallest time by the rule of use_pairs. In units
+// of 256 cycles, a product takes its waves times its stages (and about 32 for the meeting of the blocks, filling the ring
+// and storing the last tile); joining parts is a round of its own that reads and writes their sums.
+struct Plan {
+    bool pairs;
+    int parts;
+};
+Plan plan_of(int m, int n, int count) {
+    const int s = m < n ? m : n;
+    Plan best = {true, 1};
+    double least = 0;
+    const int nl = ((m < n ? n : m) + kTileK - 1) / kTileK, ns = (s + kTileK - 1) / kTileK;
+    for (int cg = 2; cg >= 1; --cg) {
+        const int64_t b = 128 * cg, slots = kSms / cg, half = half_tiles_of(s, b) * count, whole = tiles_of(m, n, b) * count;
+        const double unit = cg == 2 ? 2.0 : kSmallCost;
+        const double rest = (double)((half + slots - 1) / slots) * (ns * unit + 32) + (double)((whole + slots - 1) / slots) * (ns * unit + 32);
+        for (int parts = 1; parts <= 32 && parts <= nl; ++parts) {
+            const int part = (nl + parts - 1) / parts;
+            if (parts > 1 && (int64_t)(parts - 1) * part >= nl) continue;  // no part is empty
+            const double bytes = parts > 1 ? 6.0 * parts * s * s * count : 0.0;  // half of the square, written and read
+            if (bytes > 512e6) break;
+            const double join = parts > 1 ? 32 + bytes / 0.6e6 : 0.0;
+            const double cost = (double)((half * parts + slots - 1) / slots) * (part * unit + 32) + join + rest;
+            if (least == 0 || cost < least) least = cost, best = {cg == 2, parts};
+        }
+    }
+    return best;
+}
+
 struct Layout {
-    size_t counter, factor, part, x0, x1, gram, poly, total;
-    int64_t ldx, lds;
+    size_t counter, factor, sums, x0, x1, gram, poly, diag, regain, part, total;
+    int64_t ldx, lds, ld_part;
     int s;
+    Plan plan;
 };
 Layout layout(int32_t count, int32_t m, int32_t n) {
-    Layout L;
+    Layout L = {};
+    if (stays_in_a_block(m, n)) {
+        L.total = 256;  // nothing, but never a size of zero
+        return L;
+    }
     L.s = m < n ? m : n;
+    L.plan = plan_of(m, n, count);
     L.ldx = (int64_t)up(n, 8);
     L.lds = (int64_t)up(L.s, 8);
+    L.ld_part = (int64_t)up(L.s, 4);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -602,29 +757,16 @@ Layout layout(int32_t count, int32_t m, int32_t n) {
     };
     L.counter = take(256);
     L.factor = take((size_t)count * sizeof(float2));
-    L.part = take((size_t)(count > kNormBlocks ? count : kNormBlocks) * 8);
+    L.sums = take((size_t)(count > kNormBlocks ? count : kNormBlocks) * 8);
     L.x0 = take((size_t)count * m * L.ldx * 2);
     L.x1 = take((size_t)count * m * L.ldx * 2);
     L.gram = take((size_t)count * L.s * L.lds * 2);
     L.poly = take((size_t)count * L.s * L.lds * 2);
+    L.diag = take((size_t)count * L.s * 4);
+    L.regain = take((size_t)count * L.s * 4);
+    L.part = take(L.plan.parts > 1 ? (size_t)L.plan.parts * count * L.s * L.ld_part * 4 : 0);
     L.total = at;
     return L;
-}
-
-int64_t tiles_of(int64_t rows, int64_t cols, int64_t b) { return ((rows + b - 1) / b) * ((cols + b - 1) / b); }
-int64_t half_tiles_of(int64_t s, int64_t b) { return ((s + b - 1) / b) * ((s + b - 1) / b + 1) / 2; }
-
-// Pairs of CTAs or single ones for all products of a step: the smaller time by the rule of use_pairs, a product's waves
-// times its stages (and about 16 for filling the ring and storing the last tile).
-bool pairs_win(int m, int n, int s, int count) {
-    double cost[2];
-    for (int cg = 1; cg <= 2; ++cg) {
-        const int64_t b = 128 * cg, slots = kSms / cg, nl = (m + n - s + kTileK - 1) / kTileK, ns = (s + kTileK - 1) / kTileK;
-        const double sym = (double)((half_tiles_of(s, b) * count + slots - 1) / slots), app = (double)((tiles_of(m, n, b) * count + slots - 1) / slots);
-        const double unit = cg == 2 ? 2.0 : kSmallCost;
-        cost[cg - 1] = sym * (nl * unit + 32) + sym * (ns * unit + 32) + app * (ns * unit + 32);
-    }
-    return cost[1] <= cost[0];
 }
 
 template <int CG>
@@ -665,7 +807,7 @@ cudaError_t launch_steps(const StepsMaps& maps, const StepsArgs& p, cudaStream_t
         }
         slots = n;
     }
-    const int64_t b = 128 * CG, half = half_tiles_of(p.s, b) * p.count, whole = tiles_of(p.m, p.n, b) * p.count, most = half > whole ? half : whole;
+    const int64_t b = 128 * CG, half = half_tiles_of(p.s, b) * p.count * p.parts, whole = tiles_of(p.m, p.n, b) * p.count, most = half > whole ? half : whole;
     if (most > 0x7FFFFFFF) return cudaErrorInvalidValue;
     cfg.gridDim = dim3((unsigned)((most < slots ? most : slots) * CG));
     return cudaLaunchKernelEx(&cfg, kernel, maps, p);
@@ -709,7 +851,7 @@ int ones_orthogonalize(const void* d_g, int64_t ldg, int64_t stride, int32_t cou
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
     char* ws = static_cast<char*>(d_workspace);
     float2* factor = reinterpret_cast<float2*>(ws + L.factor);
-    double* part = reinterpret_cast<double*>(ws + L.part);
+    double* sums = reinterpret_cast<double*>(ws + L.sums);
     __half* x[2] = {reinterpret_cast<__half*>(ws + L.x0), reinterpret_cast<__half*>(ws + L.x1)};
     __half* gram = reinterpret_cast<__half*>(ws + L.gram);
     __half* poly = reinterpret_cast<__half*>(ws + L.poly);
@@ -722,7 +864,7 @@ int ones_orthogonalize(const void* d_g, int64_t ldg, int64_t stride, int32_t cou
     while ((int64_t)1 << (2 * (q + 1)) <= (m > n ? m : n)) ++q;
     const float unit = ldexpf(1.f, q);
     const bool wide_out = n % 8 == 0 && aligned(d_out, 16);
-    if (L.s <= kSmallSide && (m > n ? m : n) <= kSmallLong) {
+    if (stays_in_a_block(m, n)) {
         const SmallArgs sa = {steps, a, b, c, eps, unit, static_cast<uint16_t*>(d_out), wide_out};
         const int bytes = (((m > n ? m : n) + 63) / 64 + 4) * kBlockBytes + 1024;
         static std::atomic<uint64_t> ready{0};
@@ -733,10 +875,10 @@ int ones_orthogonalize(const void* d_g, int64_t ldg, int64_t stride, int32_t cou
     }
     int blocks = (m + kNormThreads / 32 - 1) / (kNormThreads / 32), most = kNormBlocks / count;
     if (blocks > most) blocks = most > 0 ? most : 1;
-    k_ns_norm<<<dim3(blocks, count), kNormThreads, 0, stream>>>(src, part, counter);
+    k_ns_norm<<<dim3(blocks, count), kNormThreads, 0, stream>>>(src, sums, counter);
     cudaError_t err = cudaGetLastError();
     if (err == cudaSuccess)
-        err = launch_after(k_ns_cast, dim3(blocks, count), dim3(kNormThreads), stream, src, static_cast<const double*>(part), blocks, eps,
+        err = launch_after(k_ns_cast, dim3(blocks, count), dim3(kNormThreads), stream, src, static_cast<const double*>(sums), blocks, eps,
                            x[0], L.ldx, factor);
     StepsArgs p = {};
     p.m = m, p.n = n, p.s = L.s, p.count = count, p.steps = steps, p.tall = m > n;
@@ -745,6 +887,10 @@ int ones_orthogonalize(const void* d_g, int64_t ldg, int64_t stride, int32_t cou
     p.x[0] = x[0], p.x[1] = x[1], p.gram = gram, p.poly = poly, p.out = static_cast<uint16_t*>(d_out);
     p.ldx = L.ldx, p.xs = (int64_t)m * L.ldx, p.lds = L.lds, p.ss = (int64_t)L.s * L.lds;
     p.factor = factor, p.counter = counter;
+    p.parts = L.plan.parts;
+    p.diag = reinterpret_cast<float*>(ws + L.diag), p.regain = reinterpret_cast<float*>(ws + L.regain);
+    p.part = L.plan.parts > 1 ? reinterpret_cast<float*>(ws + L.part) : nullptr;
+    p.ld_part = L.ld_part, p.part_stride = (int64_t)count * L.s * L.ld_part;
     p.wide = wide_out;
     StepsMaps maps;
     for (int i = 0; i < 2 && err == cudaSuccess; ++i) {
@@ -755,7 +901,7 @@ int ones_orthogonalize(const void* d_g, int64_t ldg, int64_t stride, int32_t cou
         err = make_map(&maps.gram[i], {gram, L.lds, p.ss, i == 1}, L.s, L.s, count, true);
         if (err == cudaSuccess) err = make_map(&maps.poly[i], {poly, L.lds, p.ss, i == 1}, L.s, L.s, count, true);
     }
-    if (err == cudaSuccess) err = pairs_win(m, n, L.s, count) ? launch_steps<2>(maps, p, stream) : launch_steps<1>(maps, p, stream);
+    if (err == cudaSuccess) err = L.plan.pairs ? launch_steps<2>(maps, p, stream) : launch_steps<1>(maps, p, stream);
     return err == cudaSuccess ? ONES_OK : ONES_ERR_CUDA;
 }
 

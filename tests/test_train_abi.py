@@ -45,7 +45,8 @@ def test_workspace_sizes():
     small = L.ones_linear_ce_backward_workspace_bytes(8192, 2048, 128000, 1024)
     assert 0 < small < whole < 8192 * 128000 * 2
     assert L.ones_orthogonalize_workspace_bytes(0, 8, 8) == 0 and L.ones_orthogonalize_workspace_bytes(1, 0, 8) == 0
-    assert L.ones_orthogonalize_workspace_bytes(2, 64, 96) > 2 * 64 * 96 * 2
+    assert L.ones_orthogonalize_workspace_bytes(2, 200, 300) > 2 * 200 * 300 * 2
+    assert 0 < L.ones_orthogonalize_workspace_bytes(1000, 128, 512) < 1024  # such matrices stay on the chip
     big = L.ones_orthogonalize_workspace_bytes(16, 65536, 4096)  # past 32 bits
     assert big > 2 * 16 * 65536 * 4096 * 2
 
@@ -99,10 +100,10 @@ def test_linear_ce_backward_refuses(change, want):
 
 @pytest.mark.parametrize("change, want", [
     ({"count": 0}, PARAM), ({"m": 0}, PARAM), ({"n": 1 << 21}, PARAM), ({"type": 5}, PARAM), ({"steps": 0}, PARAM), ({"eps": -1.0}, PARAM),
-    ({"a": float("inf")}, PARAM), ({"ldg": 63}, PARAM), ({"stride": -1, "count": 2}, PARAM), ({"g": None}, NULL), ({"out": None}, NULL),
+    ({"a": float("inf")}, PARAM), ({"ldg": 199}, PARAM), ({"stride": -1, "count": 2}, PARAM), ({"g": None}, NULL), ({"out": None}, NULL),
     ({"g": P + 2}, ALIGN), ({"out": P + 1}, ALIGN), ({"ws": P + 16}, ALIGN), ({"size": 1024}, SPACE)])
 def test_orthogonalize_refuses(change, want):
-    a = dict(g=P, ldg=64, stride=64 * 64, count=1, m=64, n=64, type=0, steps=5, a=3.4445, b=-4.775, c=2.0315, eps=1e-7, out=P, ws=P,
+    a = dict(g=P, ldg=200, stride=200 * 200, count=1, m=200, n=200, type=0, steps=5, a=3.4445, b=-4.775, c=2.0315, eps=1e-7, out=P, ws=P,
              size=1 << 24) | change
     assert _lib().ones_orthogonalize(a["g"], a["ldg"], a["stride"], a["count"], a["m"], a["n"], a["type"], a["steps"], a["a"], a["b"],
                                      a["c"], a["eps"], a["out"], a["ws"], a["size"], None) == want

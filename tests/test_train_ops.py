@@ -455,7 +455,7 @@ def check_ns(g, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7):
 
 
 NS = [(1, 1), (1, 50), (50, 1), (7, 33), (64, 64), (100, 200), (200, 100), (128, 128), (128, 512), (512, 128), (129, 129), (128, 513),
-      (130, 70), (513, 64), (255, 257), (500, 300), (256, 1024), (1000, 1368), (1111, 555), (32, 4096), (4100, 40)]
+      (130, 70), (513, 64), (255, 257), (500, 300), (256, 1024), (1000, 1368), (1111, 555), (32, 4096), (4100, 40), (247, 6276), (5000, 130), (71, 2063), (513, 8000)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
