@@ -36,6 +36,7 @@ struct EpiStats {
     static __device__ __forceinline__ void tile(const Args& a, const MatShape& g, uint32_t acc, int row, int col,
                                                 const TileAt& at, int half, const Turn&) {
         const float up = regain(g.K), to2 = kLog2e * up;
+        const int end = min(a.vocab, (at.n + 1) * g.width);
         const int64_t t64 = row < a.rows ? a.target[row] : -1;
         const int t = t64 >= 0 && t64 < a.vocab ? (int)t64 : -1;
         float m = -INFINITY, s = 0.f;
@@ -43,7 +44,7 @@ struct EpiStats {
         for (int c = 0; c < W; c += 32) {
             float v[32];
             tmem_load(acc + c, v);
-            const int left = a.vocab - (col + c);
+            const int left = end - (col + c);
             if (left <= 0) break;
             if (left < 32) {
 #pragma unroll
@@ -51,7 +52,7 @@ struct EpiStats {
                     if (i >= left) v[i] = -INFINITY;
             }
             const unsigned at_i = (unsigned)(t - (col + c));
-            if (at_i < 32u) {
+            if (at_i < 32u && t < end) {
                 float lt = 0.f;
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
@@ -395,8 +396,16 @@ __global__ void __launch_bounds__(256) k_ce_rows(const float* sum, int parts, in
 
 inline size_t up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
+// Columns of a tile of logits where the rows fill one tile at most (0: the usual): the weight's rows pass once and that is
+// all the time, so they are spread evenly over the SMs, in as few rounds of tiles as there have to be.
+inline int width_of(int32_t rows, int32_t vocab) {
+    if (rows > 128) return 0;
+    const int rounds = (vocab + 128 * kSms - 1) / (128 * kSms);
+    return (int)up((size_t)((vocab + kSms * rounds - 1) / (kSms * rounds)), 16);
+}
+
 inline int slots_of(int32_t rows, int32_t vocab) {
-    const int w = use_pairs(rows, vocab, 1, false) ? 256 : 128;
+    const int narrow = width_of(rows, vocab), w = narrow ? narrow : use_pairs(rows, vocab, 1, false) ? 256 : 128;
     return (vocab + w - 1) / w * 2;
 }
 
@@ -489,7 +498,8 @@ int ones_linear_ce(const void* d_hidden, int64_t ldh, const void* d_weight, int6
     float* at_target = reinterpret_cast<float*>(ws + L.at_target);
     const Operand h = {d_hidden, ldh, 0, false}, w = {d_weight, ldw, 0, false};
     const EpiStats::Args ea = {d_target, part, at_target, rows, vocab};
-    cudaError_t err = launch_matmul<false, false, EpiStats>(h, w, rows, vocab, cols, 1, false, type == ONES_F16, ea, stream, false);
+    cudaError_t err = launch_matmul<false, false, EpiStats>(h, w, rows, vocab, cols, 1, false, type == ONES_F16, ea, stream, false,
+                                                                  nullptr, nullptr, width_of(rows, vocab));
     const int r = rows > 4 * kSms ? 8 : 4;
     if (err == cudaSuccess)
         err = launch_after(r == 8 ? k_ce_join<8> : k_ce_join<4>, dim3((rows + r - 1) / r), dim3(kJoinThreads), stream, part,

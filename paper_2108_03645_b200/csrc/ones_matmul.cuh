@@ -41,6 +41,8 @@ struct MatShape {
     const int *live_m, *live_k;  // where M or K is known on the device only (at most the value above)
     int group;  // row tiles that run through the columns together, so that both operands' tiles are met again in L2
     bool f16;
+    int width;         // columns of a tile: 128 * CG, or fewer where N is to be spread evenly over single CTAs (multiple of 16)
+    int stage_a, stage_b;  // bytes of the operands' boxes per stage and CTA
 };
 
 struct TileAt {
@@ -111,12 +113,12 @@ __device__ __forceinline__ void fill_operand(uint32_t at, const View& v, int row
 // Fills the stages of one tile: K from stage k0 to k1, rows am of A and bn of B. Run by a whole warp; false: gave up.
 template <int CG>
 __device__ __forceinline__ bool fill_tile(Ring& r, const View& va, const View& vb, int am, int bn, int z, int k0, int k1, uint32_t rank,
-                                          uint32_t full_at) {
+                                          uint32_t full_at, uint32_t bytes = kStageBytes) {
     for (int k = k0; k < k1; ++k) {
         if (!bar_wait(r.empty + 8 * r.s, r.ph ^ 1, &g_wait_expired)) return false;
         const uint32_t a = r.base + r.s * kStageBytes, bar = full_at + 8 * r.s;
         if (elect_one()) {
-            if (rank == 0) bar_expect(r.full + 8 * r.s, CG * kStageBytes);
+            if (rank == 0) bar_expect(r.full + 8 * r.s, CG * bytes);
             fill_operand<CG>(a, va, am, k, z, bar);
             fill_operand<CG>(a + kHalf, vb, bn, k, z, bar);
         }
@@ -126,15 +128,16 @@ __device__ __forceinline__ bool fill_tile(Ring& r, const View& va, const View& v
     return true;
 }
 
-__host__ __device__ inline uint32_t instruction_desc(int cg, bool f16, bool amn, bool bmn) {
+__host__ __device__ inline uint32_t instruction_desc(int cg, bool f16, bool amn, bool bmn, int width) {
     const uint32_t type = f16 ? 0u : 1u;
     return (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)amn << 15) | ((uint32_t)bmn << 16) |
-           ((uint32_t)(128 * cg / 8) << 17) | ((uint32_t)(128 * cg / 16) << 24);
+           ((uint32_t)(width / 8) << 17) | ((uint32_t)(128 * cg / 16) << 24);
 }
 
 // Multiplies the nk stages of one tile into the accumulator at `acc` and lets barrier `done` know when that is through.
 template <int CG>
-__device__ __forceinline__ bool multiply_tile(Ring& r, uint32_t acc, int nk, const View& va, const View& vb, bool f16, uint32_t done) {
+__device__ __forceinline__ bool multiply_tile(Ring& r, uint32_t acc, int nk, const View& va, const View& vb, bool f16, uint32_t done,
+                                              int width = 128 * CG) {
     const uint64_t a_k = operand_desc(r.base, false, kHalf / 2), a_mn = operand_desc(r.base, true, kHalf / 2);
     const uint64_t to_b = kHalf >> 4;
     for (int k = 0; k < nk; ++k) {
@@ -144,7 +147,7 @@ __device__ __forceinline__ bool multiply_tile(Ring& r, uint32_t acc, int nk, con
         const uint64_t off = (uint64_t)(r.s * (kStageBytes >> 4));
         const uint64_t a = (amn ? a_mn : a_k) + off, b = (bmn ? a_mn : a_k) + off + to_b;
         const uint64_t step_a = (amn ? 2048 : 32) >> 4, step_b = (bmn ? 2048 : 32) >> 4;  // 16 values along K
-        const uint32_t idesc = instruction_desc(CG, f16, amn, bmn);
+        const uint32_t idesc = instruction_desc(CG, f16, amn, bmn, width);
         if (elect_one()) {
 #pragma unroll
             for (int i = 0; i < kTileK / 16; ++i) mma_f16<CG>(acc, a + i * step_a, b + i * step_b, idesc, (k | i) != 0);
@@ -379,9 +382,9 @@ __global__ void __launch_bounds__(kMatThreads, 1)
         Ring r = {w.base, w.full, w.empty};
         for (int t = first; ok && t < total; t += step) {
             const TileAt at = tile_at(g, t, per);
-            const int am = at.m * 128 * CG + (int)rank * 128, bn = at.n * BN + (int)rank * 128;
+            const int am = at.m * 128 * CG + (int)rank * 128, bn = at.n * g.width + (int)rank * 128;
             const int k0 = g.splits > 1 ? at.b * nk_part : 0, k1 = min(k0 + nk_part, nk_all), z = g.splits > 1 ? 0 : at.b;
-            ok = fill_tile<CG>(r, va, vb, am, bn, z, k0, k1, rank, full_at);
+            ok = fill_tile<CG>(r, va, vb, am, bn, z, k0, k1, rank, full_at, g.stage_a + g.stage_b);
         }
     } else if (warp == 1 && rank == 0) {
         // multiply
@@ -393,7 +396,7 @@ __global__ void __launch_bounds__(kMatThreads, 1)
             if (g.splits > 1 && nk <= 0) continue;  // nothing of K is left for this part
             if (!(ok = bar_wait(w.free_ + 8 * acc, aph ^ 1, &g_wait_expired))) break;
             mma_fence_after();
-            ok = multiply_tile<CG>(r, w.tmem + acc * BN, nk, va, vb, g.f16, w.done + 8 * acc);
+            ok = multiply_tile<CG>(r, w.tmem + acc * BN, nk, va, vb, g.f16, w.done + 8 * acc, g.width);
             if (++acc == 2) acc = 0, aph ^= 1;
         }
     } else if (warp >= 4) {
@@ -410,7 +413,7 @@ __global__ void __launch_bounds__(kMatThreads, 1)
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
             mma_fence_after();
             const int row = at.m * 128 * CG + (int)rank * 128 + quad * 32 + lane;
-            const int col = at.n * BN + half * (BN / 2);
+            const int col = at.n * g.width + half * (BN / 2);
             Epi::template tile<BN / 2>(ea, g, w.tmem + acc * BN + half * (BN / 2) + ((uint32_t)quad << 21), row, col, at, half, turn);
             free_accumulator<CG>(free_at + 8 * acc, lane);
             if (++acc == 2) acc = 0, aph ^= 1;
@@ -428,7 +431,7 @@ struct Operand {
     bool mn;          // memory rows run along K, and hold the operand's rows (M or N)
 };
 
-cudaError_t make_map(CUtensorMap* out, const Operand& o, int rows, int k, int batch, bool f16);
+cudaError_t make_map(CUtensorMap* out, const Operand& o, int rows, int k, int batch, bool f16, int box = 128);  // box: rows (K contiguous)
 
 int device_sms();  // of the current device; 148 where that cannot be asked
 
@@ -452,12 +455,16 @@ template <int CG, bool AMN, bool BMN, class Epi>
 cudaError_t launch_matmul_cg(const Operand& a, const Operand& b, MatShape g, bool f16, const typename Epi::Args& ea,
                              cudaStream_t stream, bool dependent) {
     CUtensorMap ma, mb;
+    if (!g.width) g.width = 128 * CG;
     const int matrices = g.splits > 1 ? 1 : g.batch;
-    cudaError_t err = make_map(&ma, a, g.M, g.K, matrices, f16);
-    if (err == cudaSuccess) err = make_map(&mb, b, g.N, g.K, matrices, f16);
+    // Where the rows do not fill one tile, only their part of it is loaded; what the rest of the tile's rows hold does not matter.
+    const int box_a = !AMN && CG == 1 && g.M < 128 ? (g.M + 7) / 8 * 8 : 128, box_b = g.width / CG;
+    g.stage_a = box_a * kTileK * 2, g.stage_b = box_b * kTileK * 2;
+    cudaError_t err = make_map(&ma, a, g.M, g.K, matrices, f16, box_a);
+    if (err == cudaSuccess) err = make_map(&mb, b, g.N, g.K, matrices, f16, box_b);
     if (err != cudaSuccess) return err;
     g.tiles_m = (g.M + 128 * CG - 1) / (128 * CG);
-    g.tiles_n = (g.N + 128 * CG - 1) / (128 * CG);
+    g.tiles_n = (g.N + g.width - 1) / g.width;
     g.group = 8 * (CG == 1 ? 2 : 1);
     g.f16 = f16;
     const int64_t per = g.sym ? (int64_t)g.tiles_m * (g.tiles_m + 1) / 2 : (int64_t)g.tiles_m * g.tiles_n;
@@ -494,10 +501,11 @@ cudaError_t launch_matmul_cg(const Operand& a, const Operand& b, MatShape g, boo
 template <bool AMN, bool BMN, class Epi>
 cudaError_t launch_matmul(const Operand& a, const Operand& b, int M, int N, int K, int batch, bool sym, bool f16,
                           const typename Epi::Args& ea, cudaStream_t stream, bool dependent, const int* live_m = nullptr,
-                          const int* live_k = nullptr) {
+                          const int* live_k = nullptr, int width = 0) {
     MatShape g = {};
+    g.width = width;
     g.M = M, g.N = N, g.K = K, g.batch = batch, g.splits = 1, g.sym = sym, g.live_m = live_m, g.live_k = live_k;
-    return use_pairs(M, N, batch, sym) ? launch_matmul_cg<2, AMN, BMN, Epi>(a, b, g, f16, ea, stream, dependent)
+    return !width && use_pairs(M, N, batch, sym) ? launch_matmul_cg<2, AMN, BMN, Epi>(a, b, g, f16, ea, stream, dependent)
                                        : launch_matmul_cg<1, AMN, BMN, Epi>(a, b, g, f16, ea, stream, dependent);
 }
 

@@ -148,7 +148,7 @@ __device__ __forceinline__ bool wait_all(const unsigned* counter, unsigned targe
         uint64_t begin = 0;
         for (;;) {
             unsigned v;
-            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(counter) : "memory");
+            asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(counter) : "memory");
             if ((int)(v - target) >= 0) break;
             const uint64_t now = now_ns();
             if (!begin) begin = now;
@@ -159,6 +159,7 @@ __device__ __forceinline__ bool wait_all(const unsigned* counter, unsigned targe
             }
         }
     }
+    __threadfence();  // once, not with every look at the counter
     ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
     asm volatile("fence.proxy.async;" ::: "memory");
     return ok;

@@ -22,7 +22,7 @@ using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, voi
                               const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                               CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-cudaError_t make_map(CUtensorMap* out, const Operand& o, int rows, int k, int batch, bool f16) {
+cudaError_t make_map(CUtensorMap* out, const Operand& o, int rows, int k, int batch, bool f16, int box_rows) {
     static std::atomic<EncodeFn> encode{nullptr};
     EncodeFn fn = encode.load(std::memory_order_relaxed);
     if (!fn) {
@@ -37,7 +37,7 @@ cudaError_t make_map(CUtensorMap* out, const Operand& o, int rows, int k, int ba
     const cuuint64_t inner = o.mn ? rows : k, outer = o.mn ? k : rows;
     const cuuint64_t dims[3] = {inner, outer, (cuuint64_t)batch};
     const cuuint64_t strides[2] = {(cuuint64_t)o.ld * 2, (cuuint64_t)(batch > 1 ? o.batch_ld : o.ld * (int64_t)outer) * 2};
-    const cuuint32_t box[3] = {64, o.mn ? (cuuint32_t)kTileK : 128u, 1};
+    const cuuint32_t box[3] = {64, o.mn ? (cuuint32_t)kTileK : (cuuint32_t)box_rows, 1};
     const cuuint32_t unit[3] = {1, 1, 1};
     const CUresult res = fn(out, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
                             const_cast<void*>(o.p), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,

@@ -577,7 +577,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, c
 
     const int quad = warp % 4, part = warp / 4, row = quad * 32 + lane;  // a thread has 32 columns of a row at a time
     const uint32_t lanes = (uint32_t)quad << 21;
-    const uint32_t idesc128 = instruction_desc(1, true, false, false);
+    const uint32_t idesc128 = instruction_desc(1, true, false, false, 128);
     uint32_t ph = 0;
     bool ok = true;
     // What the threads wrote to shared memory is there for the tensor cores; one warp issues, all wait for the end.
