@@ -158,8 +158,9 @@ __device__ __forceinline__ bool wait_all(const unsigned* counter, unsigned targe
                 break;
             }
         }
+        __threadfence();  // once, not with every look at the counter
     }
-    __threadfence();  // once, not with every look at the counter
+    __syncwarp();
     ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
     asm volatile("fence.proxy.async;" ::: "memory");
     return ok;

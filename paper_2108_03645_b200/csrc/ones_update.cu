@@ -144,9 +144,9 @@ struct EpiGram {
         float* part;          // where K is cut: the sums of this part [count][s][ld_part], else NULL
         int64_t ld_part;
     };
-    template <int W>
+    template <int W, bool CUT>
     static __device__ __forceinline__ void tile(const Args& a, uint32_t acc, int row, int col, const TileAt& at, const Turn& turn) {
-        if (a.part) {
+        if constexpr (CUT) {
             float* out = a.part + (int64_t)at.b * a.s * a.ld_part;
 #pragma unroll 1
             for (int c = 0; c < W && col + c < a.s; c += 32) {
@@ -279,16 +279,16 @@ struct EpiApply {
         float factor;
         const float2* first;  // the first step's f, or NULL
         const float* regain;  // [count][s]: of the rows, or (tall) of the columns
-        bool tall, f16, wide;
+        bool f16, wide;
     };
-    template <int W>
+    template <int W, bool TALL>
     static __device__ __forceinline__ void tile(const Args& a, uint32_t acc, int row, int col, const TileAt& at, const Turn& turn, float own) {
         const float* regain = a.regain + (int64_t)at.b * a.n;
         const float f = (a.first ? a.factor * a.first[at.b].x : a.factor) * own;
 #pragma unroll 1
         for (int c = 0; c < W && col + c < a.n; c += 64) {
             float v[64], r0 = 1.f, r1 = 1.f;
-            if (a.tall) {
+            if constexpr (TALL) {
                 const int k = col + c + 2 * turn.lane;
                 if (k < a.n) r0 = __ldcg(regain + k);
                 if (k + 1 < a.n) r1 = __ldcg(regain + k + 1);
@@ -296,7 +296,7 @@ struct EpiApply {
             tmem_load(acc + c, v);
 #pragma unroll
             for (int i = 0; i < 64; ++i) v[i] *= f;
-            if (a.tall) {
+            if constexpr (TALL) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
                     v[2 * i] *= __shfl_sync(0xFFFFFFFFu, r0, i);
@@ -318,7 +318,7 @@ struct StepsArgs {
     int parts;  // > 1: K of the Gram matrix is cut into so many parts, joined in a round of its own
     float *diag, *regain, *part;
     int64_t ld_part, part_stride;
-    bool tall;  // more rows than columns: the Gram matrix is X^T X and X takes the polynomial from the right
+    bool tall;
     float a, b, c, unit;  // unit: X is kept times this between the steps
     __half *x[2], *gram, *poly;
     uint16_t* out;
@@ -351,7 +351,10 @@ __device__ __forceinline__ void operands(const StepsMaps& maps, bool tall, int w
     }
 }
 
-template <int CG>
+// CUT: the Gram matrix's K is cut into parts; TALL: more rows than columns, the Gram matrix is X^T X and X takes the
+// polynomial from the right. Both as kernels of their own: code that is not run still costs (12 of 189 us for twelve of
+// 768 x 768).
+template <int CG, bool CUT, bool TALL>
 __global__ void __launch_bounds__(kMatThreads, 1) k_ns_steps(const __grid_constant__ StepsMaps maps, const StepsArgs p) {
     constexpr int BN = 128 * CG;
     extern __shared__ uint8_t smem_raw[];
@@ -371,25 +374,25 @@ __global__ void __launch_bounds__(kMatThreads, 1) k_ns_steps(const __grid_consta
     app.M = p.m, app.N = p.n, app.K = p.s, app.batch = p.count, app.tiles_m = (p.m + BN - 1) / BN, app.tiles_n = (p.n + BN - 1) / BN;
     app.group = 16 / CG;
     const int per_sym = tiles_per_matrix(sym), per_app = tiles_per_matrix(app);
-    const int long_side = p.tall ? p.m : p.n;
+    const int long_side = TALL ? p.m : p.n;
     const int nk_gram = (long_side + kTileK - 1) / kTileK, nk_s = (p.s + kTileK - 1) / kTileK;
     // a step's rounds: Gram matrix, (3: its parts joined,) polynomial, application
-    const int per_step = p.parts > 1 ? 4 : 3, rounds = per_step * p.steps;
-    const int gram_part = (nk_gram + p.parts - 1) / p.parts;
+    constexpr int per_step = CUT ? 4 : 3;
+    const int rounds = per_step * p.steps;
+    const int gram_part = CUT ? (nk_gram + p.parts - 1) / p.parts : nk_gram;
     auto which_of = [&](int round) {
         const int i = round % per_step;
-        return per_step == 3 ? i : i == 0 ? 0 : i == 1 ? 3 : i - 1;
+        return !CUT || i == 0 ? i : i == 1 ? 3 : i - 1;
     };
-    auto tiles_in = [&](int which) { return which == 0 ? per_sym * p.count * p.parts : which == 1 ? per_sym * p.count : which == 2 ? per_app * p.count : 0; };
+    auto tiles_in = [&](int which) { return which == 0 ? per_sym * p.count * (CUT ? p.parts : 1) : which == 1 ? per_sym * p.count : which == 2 ? per_app * p.count : 0; };
     // tile t of a round, the part of K that it takes and what that is
     auto tile_of = [&](int which, int t, int& k0, int& nk, int& cut) {
         cut = 0;
-        if (which == 0) {
+        k0 = 0, nk = which == 0 ? nk_gram : nk_s;
+        if (CUT && which == 0) {
             cut = t / (per_sym * p.count);
             t -= cut * per_sym * p.count;
             k0 = cut * gram_part, nk = min(gram_part, nk_gram - k0);
-        } else {
-            k0 = 0, nk = nk_s;
         }
         return tile_at(which == 2 ? app : sym, t, which == 2 ? per_app : per_sym);
     };
@@ -406,7 +409,7 @@ __global__ void __launch_bounds__(kMatThreads, 1) k_ns_steps(const __grid_consta
                 int k0, nk, cut;
                 const TileAt at = tile_of(which, t, k0, nk, cut);
                 View va, vb;
-                operands(maps, p.tall, which, buf, at, va, vb);
+                operands(maps, TALL, which, buf, at, va, vb);
                 ok = fill_tile<CG>(r, va, vb, at.m * BN + (int)rank * 128, at.n * BN + (int)rank * 128, at.b, k0, k0 + nk, rank, full_at);
             }
         }
@@ -419,7 +422,7 @@ __global__ void __launch_bounds__(kMatThreads, 1) k_ns_steps(const __grid_consta
             for (int t = first; ok && t < total; t += step) {
                 int k0, nk, cut;
                 View va, vb;
-                operands(maps, p.tall, which, 0, tile_of(which, t, k0, nk, cut), va, vb);
+                operands(maps, TALL, which, 0, tile_of(which, t, k0, nk, cut), va, vb);
                 if (!(ok = bar_wait(w.free_ + 8 * acc, aph ^ 1, &g_wait_expired))) break;
                 mma_fence_after();
                 ok = multiply_tile<CG>(r, w.tmem + acc * BN, nk, va, vb, true, w.done + 8 * acc);
@@ -437,7 +440,7 @@ __global__ void __launch_bounds__(kMatThreads, 1) k_ns_steps(const __grid_consta
             if (ok && round) ok = __all_sync(0xFFFFFFFFu, bar_wait(round_bar, (round - 1) & 1, &g_wait_expired));
             const float2* start = k == 0 ? p.factor : nullptr;
             EpiGram::Args eg = {p.gram, p.diag, p.lds, p.ss, p.s, 1.f / (p.unit * p.unit), start, p.part, p.ld_part};
-            if (ok && which == 3)
+            if (CUT && ok && which == 3)
                 for (int i = blockIdx.x * kEpiWarps + warp - 4; i < p.count * p.s; i += gridDim.x * kEpiWarps)
                     EpiGram::join(eg, p.parts, p.part_stride, i / p.s, i % p.s, BN, lane);
             for (int t = first; ok && t < total; t += step) {
@@ -450,25 +453,25 @@ __global__ void __launch_bounds__(kMatThreads, 1) k_ns_steps(const __grid_consta
                 // what the epilogue needs of the round before, asked for while the tile is multiplied
                 float own = 1.f;
                 if (which == 1) EpiPoly::load(ep, row, col, at, turn, q);
-                if (row < p.s && (which == 1 || (which == 2 && !p.tall)))
+                if (row < p.s && (which == 1 || (which == 2 && !TALL)))
                     own = __ldcg((which == 1 ? p.diag : p.regain) + (int64_t)at.b * p.s + row);
                 ok = bar_wait(w.done + 8 * acc, aph, &g_wait_expired);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 mma_fence_after();
                 if (which == 0) {
-                    if (p.part) eg.part = p.part + cut * p.part_stride;
-                    EpiGram::tile<BN / 2>(eg, tmem, row, col, at, turn);
+                    if (CUT) eg.part = p.part + cut * p.part_stride;
+                    EpiGram::tile<BN / 2, CUT>(eg, tmem, row, col, at, turn);
                 } else if (which == 1) {
                     EpiPoly::tile<BN / 2>(ep, tmem, row, col, at, turn, q, own);
                 } else {
-                    EpiApply::Args e = {reinterpret_cast<uint16_t*>(p.x[1 - buf]), p.ldx, p.xs, p.m, p.n, start ? p.unit : 1.f, start, p.regain, p.tall, true, true};
+                    EpiApply::Args e = {reinterpret_cast<uint16_t*>(p.x[1 - buf]), p.ldx, p.xs, p.m, p.n, start ? p.unit : 1.f, start, p.regain, true, true};
                     if (k + 1 == p.steps) {
                         e.out = p.out, e.ld = p.n, e.batch_ld = (int64_t)p.m * p.n;
                         e.factor = start ? 1.f : 1.f / p.unit;
                         e.f16 = false, e.wide = p.wide;
                     }
-                    EpiApply::tile<BN / 2>(e, tmem, row, col, at, turn, own);
+                    EpiApply::tile<BN / 2, TALL>(e, tmem, row, col, at, turn, own);
                 }
                 free_accumulator<CG>(free_at + 8 * acc, lane);
                 if (++acc == 2) acc = 0, aph ^= 1;
@@ -769,9 +772,9 @@ Layout layout(int32_t count, int32_t m, int32_t n) {
     return L;
 }
 
-template <int CG>
+template <int CG, bool CUT, bool TALL>
 cudaError_t launch_steps(const StepsMaps& maps, const StepsArgs& p, cudaStream_t stream) {
-    auto kernel = k_ns_steps<CG>;
+    auto kernel = k_ns_steps<CG, CUT, TALL>;
     static std::atomic<uint64_t> ready{0};
     cudaError_t err = allow_smem(kernel, kMatSmem, ready);
     if (err != cudaSuccess) return err;
@@ -811,6 +814,12 @@ cudaError_t launch_steps(const StepsMaps& maps, const StepsArgs& p, cudaStream_t
     if (most > 0x7FFFFFFF) return cudaErrorInvalidValue;
     cfg.gridDim = dim3((unsigned)((most < slots ? most : slots) * CG));
     return cudaLaunchKernelEx(&cfg, kernel, maps, p);
+}
+
+template <int CG>
+cudaError_t launch_steps_cg(const StepsMaps& maps, const StepsArgs& p, cudaStream_t stream) {
+    if (p.parts > 1) return p.tall ? launch_steps<CG, true, true>(maps, p, stream) : launch_steps<CG, true, false>(maps, p, stream);
+    return p.tall ? launch_steps<CG, false, true>(maps, p, stream) : launch_steps<CG, false, false>(maps, p, stream);
 }
 
 bool bad_sizes(int32_t count, int32_t m, int32_t n) {
@@ -901,7 +910,7 @@ int ones_orthogonalize(const void* d_g, int64_t ldg, int64_t stride, int32_t cou
         err = make_map(&maps.gram[i], {gram, L.lds, p.ss, i == 1}, L.s, L.s, count, true);
         if (err == cudaSuccess) err = make_map(&maps.poly[i], {poly, L.lds, p.ss, i == 1}, L.s, L.s, count, true);
     }
-    if (err == cudaSuccess) err = L.plan.pairs ? launch_steps<2>(maps, p, stream) : launch_steps<1>(maps, p, stream);
+    if (err == cudaSuccess) err = L.plan.pairs ? launch_steps_cg<2>(maps, p, stream) : launch_steps_cg<1>(maps, p, stream);
     return err == cudaSuccess ? ONES_OK : ONES_ERR_CUDA;
 }
 
