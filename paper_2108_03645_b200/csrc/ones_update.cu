@@ -483,35 +483,42 @@ __global__ void __launch_bounds__(kMatThreads, 1) k_ns_steps(const __grid_consta
     clear_up<CG>(w, warp, ok);
 }
 
-// A matrix whose shorter side is at most 128 and longer side at most 512 stays in one block's shared memory from its
-// first reading to its result: X lies there as blocks of 64 columns (of the longer side) x 128 rows with the 128-byte
-// swizzle, which serves both as the operand with K along the longer side (X X^T) and as the one with its rows along it
-// (B X). Nothing but the input and the result touches memory and nobody waits for another block: 128 x 256 takes 69 us in
-// k_ns_steps, most of it in the meetings of the blocks.
+// A matrix whose shorter side is at most 128 stays in shared memory from its first reading to its result: of one CTA up
+// to 512 on the longer side, of a cluster of CTAs up to 8192. X lies there as blocks of 64 columns (of the longer side)
+// x 128 rows with the 128-byte swizzle, which serves both as the operand with K along the longer side (X X^T) and as the
+// one with its rows along it (B X). Nothing but the input and the result touches memory. In a cluster each CTA has some
+// of the columns; the CTAs' shares of the Gram matrix are added up over distributed shared memory, each CTA summing some
+// of the rows for all of them, and the 128 x 128 polynomial is computed by each. 128 x 256 takes 69 us in k_ns_steps, most
+// of it in the meetings of all blocks of the GPU, and 30 us here.
 constexpr int kSmallSide = 128, kSmallLong = 512, kSmallThreads = 512, kBlockBytes = 128 * 128;
 
 struct SmallArgs {
+    int cluster, own;  // CTAs of a matrix, and blocks of columns that a CTA has (the last one may have fewer)
     int steps;
     float a, b, c, eps, unit;
     uint16_t* out;
     bool wide;
 };
 
+template <bool CL>
 __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, const SmallArgs p) {
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t s_bar;
     __shared__ uint32_t s_tmem;
     __shared__ double s_sum[kSmallThreads / 32];
-    __shared__ float s_scale, s_factor, s_regain[128];
+    __shared__ float s_scale, s_factor, s_regain[128], s_diag[128];
+    __shared__ double s_share;
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const bool tall = g.m > g.n;
-    const int blocks = ((tall ? g.m : g.n) + 63) / 64;
+    const int rank = CL ? (int)cluster_rank() : 0, matrix = CL ? blockIdx.x / p.cluster : blockIdx.x;
+    const int lng = tall ? g.m : g.n, c0 = rank * p.own * 64, mine = min(p.own * 64, lng - c0);  // columns c0 .. c0 + mine - 1
+    const int blocks = (mine + 63) / 64;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, bar = smem_u32(&s_bar);
     uint8_t* x = smem_raw + (base - smem_u32(smem_raw));
-    uint8_t* gram = x + blocks * kBlockBytes;
+    uint8_t* gram = x + p.own * kBlockBytes;
     uint8_t* poly = gram + 2 * kBlockBytes;
-    const uint32_t x_at = base, gram_at = base + blocks * kBlockBytes, poly_at = gram_at + 2 * kBlockBytes;
-    const uint32_t cols = blocks <= 2 ? 128 : blocks <= 4 ? 256 : 512;  // with this shared memory, what an SM's blocks take together fits
+    const uint32_t x_at = base, gram_at = base + p.own * kBlockBytes, poly_at = gram_at + 2 * kBlockBytes;
+    const uint32_t cols = p.own <= 2 ? 128 : p.own <= 4 ? 256 : 512;  // with this shared memory, what an SM's blocks take together fits
     if (threadIdx.x == 0) {
         bar_init(bar, 1);
         bar_init_done();
@@ -519,19 +526,21 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, c
     if (warp == 0) tmem_alloc<1>(smem_u32(&s_tmem), cols);
 
     // X0 as in k_ns_norm and k_ns_cast
-    const int64_t from = blockIdx.x * g.stride;
+    // (this CTA's columns of X: rows of the matrix if it is tall)
+    const int64_t from = matrix * g.stride + (tall ? c0 * g.ld : c0);
+    const int my_rows = tall ? mine : g.m, my_cols = tall ? g.n : mine;
     double sum = 0.0;
 #pragma unroll 4
-    for (int r = warp; r < g.m; r += kSmallThreads / 32) {
+    for (int r = warp; r < my_rows; r += kSmallThreads / 32) {
         if (g.wide) {
-            for (int c = lane * 8; c < g.n; c += 256) {
+            for (int c = lane * 8; c < my_cols; c += 256) {
                 float v[8];
                 load8(g.p, from + r * g.ld + c, g.type, v);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum = fma((double)v[i], (double)v[i], sum);
             }
         } else {
-            for (int c = lane; c < g.n; c += 32) {
+            for (int c = lane; c < my_cols; c += 32) {
                 const double v = load_as_float(g.p, from + r * g.ld + c, g.type);
                 sum = fma(v, v, sum);
             }
@@ -539,13 +548,25 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, c
     }
     for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
     if (lane == 0) s_sum[warp] = sum;
-    for (int i = threadIdx.x; i < blocks * kBlockBytes / 16; i += kSmallThreads) reinterpret_cast<uint4*>(x)[i] = make_uint4(0, 0, 0, 0);
+    for (int i = threadIdx.x; i < p.own * kBlockBytes / 16; i += kSmallThreads) reinterpret_cast<uint4*>(x)[i] = make_uint4(0, 0, 0, 0);
     mma_fence_before();
     __syncthreads();
     mma_fence_after();
     const uint32_t tmem = s_tmem;
     if (threadIdx.x == 0) {
         for (int i = 1; i < kSmallThreads / 32; ++i) sum += s_sum[i];
+        s_share = sum;
+    }
+    if constexpr (CL) cluster_sync_all();
+    if (threadIdx.x == 0) {
+        if constexpr (CL) {
+            sum = 0.0;
+            for (int q = 0; q < p.cluster; ++q) {
+                double share;
+                asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(share) : "r"(map_to_rank(smem_u32(&s_share), q)) : "memory");
+                sum += share;
+            }
+        }
         const double norm = sqrt(sum), rms = norm / sqrt((double)g.m * g.n);
         int k = rms > 0.0 && rms < 1e300 ? ilogb(rms) : 0;
         k = k < -120 ? -120 : k > 120 ? 120 : k;
@@ -555,14 +576,14 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, c
     __syncthreads();
     const float scale = s_scale, factor = s_factor;
 #pragma unroll 4
-    for (int r = warp; r < g.m; r += kSmallThreads / 32) {
+    for (int r = warp; r < my_rows; r += kSmallThreads / 32) {
         if (tall) {  // row r of the matrix is column r of X
             uint8_t* to = x + (r / 64) * kBlockBytes + (r % 8) * 2;
-            for (int c = lane; c < g.n; c += 32)
+            for (int c = lane; c < my_cols; c += 32)
                 *reinterpret_cast<__half*>(to + c * 128 + (((r % 64 / 8) ^ (c & 7)) << 4)) =
                     __float2half_rn(load_as_float(g.p, from + r * g.ld + c, g.type) * scale);
         } else if (g.wide) {
-            for (int c = lane * 8; c < g.n; c += 256) {
+            for (int c = lane * 8; c < my_cols; c += 256) {
                 float v[8];
                 load8(g.p, from + r * g.ld + c, g.type, v);
 #pragma unroll
@@ -572,7 +593,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, c
                                Half16::pack(v[6], v[7], true));
             }
         } else {
-            for (int c = lane; c < g.n; c += 32)
+            for (int c = lane; c < my_cols; c += 32)
                 *reinterpret_cast<__half*>(x + (c / 64) * kBlockBytes + r * 128 + (((c % 64 / 8) ^ (r & 7)) << 4) + (c % 8) * 2) =
                     __float2half_rn(load_as_float(g.p, from + r * g.ld + c, g.type) * scale);
         }
@@ -629,15 +650,60 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, c
         tmem_load(tmem + part * 32 + lanes, v);
         const unsigned d = (unsigned)(row - part * 32);
         float exact = 0.f;
-        if (d < 32u) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) exact = d == (unsigned)i ? v[i] : exact;
-            exact *= f;
-        }
         // the polynomial takes both its terms from the rounded A: their errors then go against each other
+        if constexpr (CL) {
+            // this CTA's share of the sums, in 32 bits, in the place of the polynomial and the two blocks behind it
+            uint8_t* share = poly + row * 512 + part * 128;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = __half2float(__float2half_rn(v[i] * f));
-        put(gram, row, part, v, true);
+            for (int c = 0; c < 8; ++c)
+                *reinterpret_cast<float4*>(share + ((c ^ (row & 7)) << 4)) = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+            cluster_sync_all();
+            const int each = (4096 + p.cluster - 1) / p.cluster, end = min(4096, (rank + 1) * each);
+            for (int u = rank * each + threadIdx.x; u < end; u += kSmallThreads) {
+                const int r = u / 32, c = u % 32;  // four columns from 4 * c
+                const uint32_t off = poly_at + r * 512 + (c / 8) * 128 + (((c % 8) ^ (r & 7)) << 4);
+                float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+                for (int q = 0; q < p.cluster; ++q) {
+                    float4 e;
+                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                 : "=f"(e.x), "=f"(e.y), "=f"(e.z), "=f"(e.w)
+                                 : "r"(map_to_rank(off, q))
+                                 : "memory");
+                    t.x += e.x, t.y += e.y, t.z += e.z, t.w += e.w;
+                }
+                t.x *= f, t.y *= f, t.z *= f, t.w *= f;
+                const uint32_t to = gram_at + (c / 16) * kBlockBytes + r * 128 + (((c % 16 / 2) ^ (r & 7)) << 4) + (c & 1) * 8;
+                const uint32_t lo = Half16::pack(t.x, t.y, true), hi = Half16::pack(t.z, t.w, true);
+                const bool diagonal = r / 4 == c;
+                const float own = r % 4 == 0 ? t.x : r % 4 == 1 ? t.y : r % 4 == 2 ? t.z : t.w;
+                for (int q = 0; q < p.cluster; ++q) {
+                    asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(map_to_rank(to, q)), "r"(lo), "r"(hi) : "memory");
+                    if (diagonal) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(map_to_rank(smem_u32(&s_diag[r]), q)), "f"(own) : "memory");
+                }
+            }
+            cluster_sync_all();
+            exact = s_diag[row];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const uint4 e = *reinterpret_cast<const uint4*>(gram + (part / 2) * kBlockBytes + row * 128 + ((((part & 1) * 4 + c) ^ (row & 7)) << 4));
+                const uint32_t w[4] = {e.x, e.y, e.z, e.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+                    v[8 * c + 2 * i] = h.x, v[8 * c + 2 * i + 1] = h.y;
+                }
+            }
+        } else {
+            if (d < 32u) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) exact = d == (unsigned)i ? v[i] : exact;
+                exact *= f;
+            }
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __half2float(__float2half_rn(v[i] * f));
+            put(gram, row, part, v, true);
+        }
         ready();
         square(gram_at, 2);
         wait();
@@ -685,18 +751,19 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, c
         ready();
     }
     // the result lies in the place of X, as bfloat16
-    uint16_t* out = p.out + (int64_t)blockIdx.x * g.m * g.n;
+    uint16_t* out = p.out + (int64_t)matrix * g.m * g.n + (tall ? (int64_t)c0 * g.n : c0);
     auto at = [&](int r, int c) { return x + (c / 64) * kBlockBytes + r * 128 + (((c % 64 / 8) ^ (r & 7)) << 4) + (c % 8) * 2; };
-    for (int r = warp; r < g.m; r += kSmallThreads / 32) {
+    for (int r = warp; r < my_rows; r += kSmallThreads / 32) {
         if (p.wide && !tall) {
-            for (int c = lane * 8; c < g.n; c += 256) *reinterpret_cast<uint4*>(out + (int64_t)r * g.n + c) = *reinterpret_cast<const uint4*>(at(r, c));
+            for (int c = lane * 8; c < my_cols; c += 256) *reinterpret_cast<uint4*>(out + (int64_t)r * g.n + c) = *reinterpret_cast<const uint4*>(at(r, c));
         } else {
-            for (int c = lane; c < g.n; c += 32) out[(int64_t)r * g.n + c] = *reinterpret_cast<const uint16_t*>(tall ? at(c, r) : at(r, c));
+            for (int c = lane; c < my_cols; c += 32) out[(int64_t)r * g.n + c] = *reinterpret_cast<const uint16_t*>(tall ? at(c, r) : at(r, c));
         }
     }
     if (!ok) let_copies_end();
     __syncthreads();
     if (warp == 0) tmem_free<1>(tmem, cols);
+    if constexpr (CL) cluster_sync_all();
 }
 
 inline size_t up(size_t x, size_t a) { return (x + a - 1) / a * a; }
@@ -704,7 +771,21 @@ inline size_t up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 int64_t tiles_of(int64_t rows, int64_t cols, int64_t b) { return ((rows + b - 1) / b) * ((cols + b - 1) / b); }
 int64_t half_tiles_of(int64_t s, int64_t b) { return ((s + b - 1) / b) * ((s + b - 1) / b + 1) / 2; }
 
-bool stays_in_a_block(int m, int n) { return (m < n ? m : n) <= kSmallSide && (m < n ? n : m) <= kSmallLong; }
+// How a matrix whose shorter side is at most 128 is spread over a cluster: CTAs, and blocks of 64 columns of the longer side
+// that a CTA has; {0, 0} where it does not fit, or where there are so many that k_ns_steps has work for the whole GPU.
+struct Spread {
+    int cluster, own;
+};
+Spread spread_of(int m, int n, int count) {
+    const int s = m < n ? m : n, blocks = ((m < n ? n : m) + 63) / 64, most = kSmallLong / 64;
+    if (s > kSmallSide) return {0, 0};
+    if (blocks <= most) return {1, blocks};
+    int own = 4;  // a CTA with 4 blocks has a shorter step than one with 8
+    while (own < most && ((blocks + own - 1) / own > 16 || (int64_t)count * ((blocks + own - 1) / own) > kSms)) own *= 2;
+    const int cluster = (blocks + own - 1) / own;
+    if (cluster > 16 || (int64_t)count * cluster > kSms) return {0, 0};
+    return {cluster, own};
+}
 
 // Pairs of CTAs or single ones, and the parts of the Gram matrix's K: the smallest time by the rule of use_pairs. In units
 // of 256 cycles, a product takes its waves times its stages (and about 32 for the meeting of the blocks, filling the ring
@@ -743,7 +824,7 @@ struct Layout {
 };
 Layout layout(int32_t count, int32_t m, int32_t n) {
     Layout L = {};
-    if (stays_in_a_block(m, n)) {
+    if (spread_of(m, n, count).cluster) {
         L.total = 256;  // nothing, but never a size of zero
         return L;
     }
@@ -822,6 +903,30 @@ cudaError_t launch_steps_cg(const StepsMaps& maps, const StepsArgs& p, cudaStrea
     return p.tall ? launch_steps<CG, false, true>(maps, p, stream) : launch_steps<CG, false, false>(maps, p, stream);
 }
 
+cudaError_t launch_small(const Source& src, const SmallArgs& sa, int count, cudaStream_t stream) {
+    const bool cl = sa.cluster > 1;
+    auto kernel = cl ? k_ns_small<true> : k_ns_small<false>;
+    static std::atomic<uint64_t> ready[2];
+    cudaError_t err = allow_smem(kernel, (kSmallLong / 64 + 6) * kBlockBytes + 1024, ready[cl]);
+    if (err != cudaSuccess) return err;
+    if (sa.cluster > 8) {  // more CTAs than a portable cluster has
+        err = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (err != cudaSuccess) return err;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(count * sa.cluster));
+    cfg.blockDim = dim3(kSmallThreads);
+    cfg.dynamicSmemBytes = (sa.own + (cl ? 6 : 4)) * kBlockBytes + 1024;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = sa.cluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cl ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, src, sa);
+}
+
 bool bad_sizes(int32_t count, int32_t m, int32_t n) {
     return count < 1 || m < 1 || n < 1 || count > 65535 || m > (1 << 20) || n > (1 << 20);
 }
@@ -873,14 +978,10 @@ int ones_orthogonalize(const void* d_g, int64_t ldg, int64_t stride, int32_t cou
     while ((int64_t)1 << (2 * (q + 1)) <= (m > n ? m : n)) ++q;
     const float unit = ldexpf(1.f, q);
     const bool wide_out = n % 8 == 0 && aligned(d_out, 16);
-    if (stays_in_a_block(m, n)) {
-        const SmallArgs sa = {steps, a, b, c, eps, unit, static_cast<uint16_t*>(d_out), wide_out};
-        const int bytes = (((m > n ? m : n) + 63) / 64 + 4) * kBlockBytes + 1024;
-        static std::atomic<uint64_t> ready{0};
-        cudaError_t err = allow_smem(k_ns_small, (kSmallLong / 64 + 4) * kBlockBytes + 1024, ready);
-        if (err != cudaSuccess) return ONES_ERR_CUDA;
-        k_ns_small<<<count, kSmallThreads, bytes, stream>>>(src, sa);
-        return cudaGetLastError() == cudaSuccess ? ONES_OK : ONES_ERR_CUDA;
+    const Spread on = spread_of(m, n, count);
+    if (on.cluster) {
+        const SmallArgs sa = {on.cluster, on.own, steps, a, b, c, eps, unit, static_cast<uint16_t*>(d_out), wide_out};
+        return launch_small(src, sa, count, stream) == cudaSuccess ? ONES_OK : ONES_ERR_CUDA;
     }
     int blocks = (m + kNormThreads / 32 - 1) / (kNormThreads / 32), most = kNormBlocks / count;
     if (blocks > most) blocks = most > 0 ? most : 1;

@@ -455,7 +455,7 @@ def check_ns(g, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7):
 
 
 NS = [(1, 1), (1, 50), (50, 1), (7, 33), (64, 64), (100, 200), (200, 100), (128, 128), (128, 512), (512, 128), (129, 129), (128, 513),
-      (130, 70), (513, 64), (255, 257), (500, 300), (256, 1024), (1000, 1368), (1111, 555), (32, 4096), (4100, 40), (247, 6276), (5000, 130), (71, 2063), (513, 8000)]
+      (130, 70), (513, 64), (255, 257), (500, 300), (256, 1024), (1000, 1368), (1111, 555), (32, 4096), (4100, 40), (247, 6276), (5000, 130), (71, 2063), (513, 8000), (128, 520), (600, 100), (77, 1025), (128, 4096), (8192, 128), (8000, 33), (20, 8191), (5, 8200), (9000, 128)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
@@ -464,7 +464,7 @@ def test_orthogonalize(m, n, dtype):
     check_ns((randn(m, n, seed=m + n) * 1e-2).to(dtype))
 
 
-@pytest.mark.parametrize("count,m,n", [(2, 40, 30), (300, 16, 24), (3, 200, 333), (12, 768, 768), (5, 300, 129), (160, 140, 130)])
+@pytest.mark.parametrize("count,m,n", [(2, 40, 30), (300, 16, 24), (3, 200, 333), (12, 90, 1188), (40, 2000, 64), (200, 30, 700), (7, 128, 1344), (12, 768, 768), (5, 300, 129), (160, 140, 130)])
 def test_orthogonalize_many(count, m, n):
     g = randn(count, m, n).bfloat16()
     o = check_ns(g)
