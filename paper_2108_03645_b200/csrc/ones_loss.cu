@@ -36,7 +36,7 @@ struct EpiStats {
     static __device__ __forceinline__ void tile(const Args& a, const MatShape& g, uint32_t acc, int row, int col,
                                                 const TileAt& at, int half, const Turn&) {
         const float up = regain(g.K), to2 = kLog2e * up;
-        const int end = min(a.vocab, (at.n + 1) * g.width);
+        const int end = min(a.vocab, col + g.width / 2);
         const int64_t t64 = row < a.rows ? a.target[row] : -1;
         const int t = t64 >= 0 && t64 < a.vocab ? (int)t64 : -1;
         float m = -INFINITY, s = 0.f;
@@ -106,14 +106,16 @@ struct EpiDlogits {
         const int t = r.target - a.first;
         // the product with the hidden rows runs over whole stages of rows: those after the last one are zero
         const int rows = min(a.rows, (shape.M + kTileK - 1) / kTileK * kTileK);
+        const int end = min(a.cols, col + shape.width / 2);
 #pragma unroll 1
-        for (int c = 0; c < W && col + c < a.cols; c += 64) {
+        for (int c = 0; c < W && col + c < end; c += 64) {
             float v[64];
             tmem_load(acc + c, v);
 #pragma unroll
-            for (int i = 0; i < 64; ++i) {
-                const float p = exp2_fast(fmaf(v[i], to2, r.shift));
-                v[i] = live ? p * r.g : 0.f;
+            for (int i = 0; i < 64; i += 2) {  // rows behind the last one that takes part are zero: exp(0) * 0
+                const float2 x = split(fma2(pair(v[i], v[i + 1]), both(to2), both(r.shift)));
+                const float2 y = split(pair(exp2_fast(x.x), exp2_fast(x.y)) * both(r.g));
+                v[i] = y.x, v[i + 1] = y.y;
             }
             const unsigned at_i = (unsigned)(t - (col + c));
             if (live && at_i < 64u) {
@@ -121,8 +123,7 @@ struct EpiDlogits {
                 for (int i = 0; i < 64; ++i)
                     if (at_i == (unsigned)i) v[i] -= r.g;
             }
-            turn.put16(v, a.f16);
-            turn.store16(a.out, a.ld, row - turn.lane, col + c, rows, a.cols, true);
+            turn.write16(v, a.f16, a.out, a.ld, row - turn.lane, col + c, rows, end, true);
         }
     }
 };
@@ -157,15 +158,16 @@ struct EpiSum {
                                                 const TileAt& at, int, const Turn& turn) {
         const float unscale = a.last ? 1.f / *a.scale : 1.f;  // a power of two
         const int r0 = row - turn.lane + turn.lane / 8, k = turn.lane & 7;
+        const int end = min(a.cols, col + shape.width / 2);
 #pragma unroll 1
-        for (int c = 0; c < W && col + c < a.cols; c += 32) {
-            const int at_col = col + c + 4 * k, left = a.cols - at_col;
-            float* sum = a.sum + ((int64_t)at.b * a.rows + r0) * a.ld_sum + at_col;  // has whole chunks of 32 columns
+        for (int c = 0; c < W && col + c < end; c += 32) {
+            const int at_col = col + c + 4 * k, left = end - at_col;
+            float* sum = a.sum + ((int64_t)at.b * a.rows + r0) * a.ld_sum + at_col;  // has whole chunks of 4 columns
             float4 old[8];
             if (!a.first) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (r0 + 4 * i < shape.M) old[i] = *reinterpret_cast<const float4*>(sum + 4 * i * a.ld_sum);
+                    if (r0 + 4 * i < shape.M && left > 0) old[i] = *reinterpret_cast<const float4*>(sum + 4 * i * a.ld_sum);
             }
             float v[32];
             tmem_load(acc + c, v);
@@ -177,7 +179,7 @@ struct EpiSum {
             for (int i = 0; i < 8; ++i) {
                 float4 f = make_float4(__uint_as_float(q[i].x), __uint_as_float(q[i].y), __uint_as_float(q[i].z), __uint_as_float(q[i].w));
                 if (!a.first) f.x += old[i].x, f.y += old[i].y, f.z += old[i].z, f.w += old[i].w;
-                if (r0 + 4 * i >= shape.M) continue;
+                if (r0 + 4 * i >= shape.M || left <= 0) continue;
                 if (!a.last) {
                     *reinterpret_cast<float4*>(sum + 4 * i * a.ld_sum) = f;
                     continue;
@@ -204,8 +206,9 @@ struct EpiGrad {
         const float unscale = 1.f / *a.scale;
         const bool none = shape.K == 0;  // no row takes part: nothing was multiplied
         const int row0 = row - turn.lane;
+        const int end = min(a.cols, col + shape.width / 2);
 #pragma unroll 1
-        for (int c = 0; c < W && col + c < a.cols; c += 64) {
+        for (int c = 0; c < W && col + c < end; c += 64) {
             float v[64];
             tmem_load(acc + c, v);
 #pragma unroll
@@ -217,11 +220,10 @@ struct EpiGrad {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) u[i] = v[h + i];
                     turn.put32(u);
-                    turn.store32(static_cast<float*>(a.out), a.ld, row0, col + c + h, a.rows, a.cols, a.wide);
+                    turn.store32(static_cast<float*>(a.out), a.ld, row0, col + c + h, a.rows, end, a.wide);
                 }
             } else {
-                turn.put16(v, a.f16);
-                turn.store16(static_cast<uint16_t*>(a.out), a.ld, row0, col + c, a.rows, a.cols, a.wide);
+                turn.write16(v, a.f16, static_cast<uint16_t*>(a.out), a.ld, row0, col + c, a.rows, end, a.wide);
             }
         }
     }
@@ -372,12 +374,13 @@ __global__ void __launch_bounds__(256) k_ce_gather(const uint16_t* hidden, int64
 }
 
 // Joins the parts of the sums over the vocabulary, in order, and rounds them into the caller's rows. A warp takes a row.
-__global__ void __launch_bounds__(256) k_ce_rows(const float* sum, int parts, int64_t ld_sum, int rows, int cols, const Header* head,
+__global__ void __launch_bounds__(256) k_ce_rows(const float* sum, Cut cut, int plan_nk, int64_t ld_sum, int rows, int cols, const Header* head,
                                                  const RowInfo* info, uint16_t* out, int64_t ld_out, bool f16, bool wide) {
     wait_for_predecessor();
     const int lane = threadIdx.x % 32;
     const float unscale = 1.f / head->scale;
     const int64_t part = (int64_t)rows * ld_sum;
+    const int parts = parts_of(cut, head->live, cols, plan_nk);
     for (int i = blockIdx.x * 8 + threadIdx.x / 32; i < head->live; i += gridDim.x * 8) {
         const float* p = sum + (int64_t)i * ld_sum;
         uint16_t* to = out + (int64_t)info[i].row * ld_out;
@@ -542,6 +545,7 @@ int ones_linear_ce_backward(const float* d_dloss, const void* d_hidden, int64_t 
     const bool f16 = type == ONES_F16;
     const bool wide_h = aligned(d_dhidden, 16) && lddh % 8 == 0, wide_w = aligned(d_dweight, 16) && lddw % 8 == 0;
     const bool wide_in = aligned(d_hidden, 16) && ldh % 8 == 0;
+    const int plan_nk = ((vocab < L.piece ? vocab : L.piece) + kTileK - 1) / kTileK;  // of the first piece: later ones are no longer
     const unsigned row_blocks = (unsigned)((rows + 7) / 8 < 8 * kSms ? (rows + 7) / 8 : 8 * kSms);
 
     k_ce_scan<<<1, 1024, 0, stream>>>(d_dloss, d_target, rows, vocab, info, head);
@@ -559,7 +563,7 @@ int ones_linear_ce_backward(const float* d_dloss, const void* d_hidden, int64_t 
         if (err != cudaSuccess) break;
         const EpiSum::Args e2 = {sum, L.ld_sum, dh, lddh, &head->scale, info, rows, cols, v0 == 0, last && L.cut.splits == 1, f16, wide_h};
         err = launch_matmul_cut<false, true, EpiSum>({dl, L.piece, 0, false}, {w0, ldw, 0, true}, rows, cols, n, L.cut, f16,
-                                                     e2, stream, true, &head->live);
+                                                     e2, stream, true, &head->live, plan_nk);
         if (err != cudaSuccess) break;
         const EpiGrad::Args e3 = {static_cast<char*>(d_dweight) + (int64_t)v0 * lddw * (int64_t)wsize, lddw, &head->scale, n, cols,
                                   wtype == ONES_F32, f16, wide_w};
@@ -567,7 +571,7 @@ int ones_linear_ce_backward(const float* d_dloss, const void* d_hidden, int64_t 
                                                  e3, stream, true, nullptr, &head->live);
     }
     if (err == cudaSuccess && L.cut.splits > 1)
-        err = launch_after(k_ce_rows, dim3(row_blocks), dim3(256), stream, static_cast<const float*>(sum), L.cut.splits, L.ld_sum, rows, cols,
+        err = launch_after(k_ce_rows, dim3(row_blocks), dim3(256), stream, static_cast<const float*>(sum), L.cut, plan_nk, L.ld_sum, rows, cols,
                            static_cast<const Header*>(head), static_cast<const RowInfo*>(info), dh, lddh, f16, wide_h);
     return err == cudaSuccess ? ONES_OK : ONES_ERR_CUDA;
 }

@@ -21,6 +21,7 @@
 
 namespace ones {
 
+constexpr int kSms = 148;  // launch rules reckon with a B200's SMs, so that workspace sizes need no device
 constexpr int kTileK = 64;       // values along K per stage: one 128-byte swizzle row
 constexpr int kStages = 6;
 constexpr int kHalf = 128 * kTileK * 2;  // bytes of one operand's box(es) per stage and CTA
@@ -36,12 +37,13 @@ static __device__ unsigned g_wait_expired;
 struct MatShape {
     int M, N, K;
     int tiles_m, tiles_n, batch;
-    int splits;  // > 1: K is cut into so many parts, each with a C of its own in the place of a matrix of the batch
+    int splits;  // > 1: K is cut into parts, at most so many, each with a C of its own in the place of a matrix of the batch
+    int plan_nk; // stages of K that the number of parts goes by (K itself may be shorter)
     int sym;     // only tiles on and above the diagonal are computed (C is symmetric)
     const int *live_m, *live_k;  // where M or K is known on the device only (at most the value above)
     int group;  // row tiles that run through the columns together, so that both operands' tiles are met again in L2
     bool f16;
-    int width;         // columns of a tile: 128 * CG, or fewer where N is to be spread evenly over single CTAs (multiple of 16)
+    int width;         // columns of a tile: 128 * CG, or fewer where N is to be spread evenly (multiple of 16)
     int stage_a, stage_b;  // bytes of the operands' boxes per stage and CTA
 };
 
@@ -252,10 +254,12 @@ struct Turn {
         return *reinterpret_cast<const float*>(at + row * 128 + (((c >> 2) ^ (row & 7)) << 4) + (c & 3) * 4);
     }
 
-    // The 64 x 16-bit (32 x 32-bit) columns from `col` of rows row0..row0+31, as far as they lie inside rows x cols, to
-    // `out` (row 0's first value). wide: rows start on 16-byte boundaries; otherwise single values, a row at a time.
-    __device__ __forceinline__ void store16(uint16_t* out, int64_t ld, int row0, int col, int rows, int cols, bool wide) const {
+    // The calling thread's 64 values as 16 bits, and with them the warp's 32 rows from row0, into columns from `col` of
+    // `out` (row 0's first value), as far as they lie inside rows x cols. wide: rows start on 16-byte boundaries.
+    __device__ __forceinline__ void write16(float (&v)[64], bool f16, uint16_t* out, int64_t ld, int row0, int col, int rows, int cols,
+                                            bool wide) const {
         if (wide) {
+            put16(v, f16);
             const int c = lane & 7, left = cols - (col + 8 * c);
             uint16_t* p = out + (int64_t)(row0 + lane / 8) * ld + col + 8 * c;
             uint4 q[8];
@@ -272,33 +276,34 @@ struct Turn {
                 }
             }
         } else {
-            // Two values at a time, from the first place in a row that lies on a 4-byte boundary; what is left over before
-            // and after the pairs goes alone.
-            // Eight rows are read before they are written, since the compiler cannot tell the two memories apart.
+            // Two values at a time: a row that starts on an odd 2-byte place is put one value further to the left, so that
+            // its pairs lie on 4-byte boundaries on both sides; its first value goes by itself.
             const int n = min(32, rows - row0), width = min(64, cols - col);
             uint16_t* p = out + (int64_t)row0 * ld + col;
+            const bool odd = (reinterpret_cast<uintptr_t>(p + lane * ld) >> 1) & 1;
+            if (odd && lane < n) p[lane * ld] = (uint16_t)Half16::pack(v[0], 0.f, f16);
+#pragma unroll
+            for (int i = 0; i < 63; ++i) v[i] = odd ? v[i + 1] : v[i];
+            put16(v, f16);
+            // Eight rows are read before they are written, since the compiler cannot tell the two memories apart.
 #pragma unroll 1
             for (int r = 0; r < n; r += 8) {
-                uint32_t v[8], lone[8];
+                uint32_t q[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int c = 2 * lane + ((int)(reinterpret_cast<uintptr_t>(p + j * ld) >> 1) & 1);
-                    v[j] = half_at(r + j, c) | (uint32_t)half_at(r + j, min(c + 1, 63)) << 16;
-                    lone[j] = half_at(r + j, 0);
-                }
+                for (int j = 0; j < 8; ++j) q[j] = *reinterpret_cast<const uint32_t*>(at + (r + j) * 128 + (((lane >> 2) ^ ((r + j) & 7)) << 4) + (lane & 3) * 4);
 #pragma unroll
                 for (int j = 0; j < 8; ++j, p += ld) {
                     if (r + j >= n) break;
-                    const int odd = (int)(reinterpret_cast<uintptr_t>(p) >> 1) & 1, c = 2 * lane + odd;
+                    const int c = 2 * lane + ((int)(reinterpret_cast<uintptr_t>(p) >> 1) & 1);
                     if (c + 1 < width)
-                        *reinterpret_cast<uint32_t*>(p + c) = v[j];
+                        *reinterpret_cast<uint32_t*>(p + c) = q[j];
                     else if (c < width)
-                        p[c] = (uint16_t)v[j];
-                    if (odd && lane == 0) p[0] = (uint16_t)lone[j];
+                        p[c] = (uint16_t)q[j];
                 }
             }
         }
     }
+    // The same for 32 x 32-bit columns that have been put.
     __device__ __forceinline__ void store32(float* out, int64_t ld, int row0, int col, int rows, int cols, bool wide) const {
         if (wide) {
             const int c = lane & 7, left = cols - (col + 4 * c);
@@ -349,6 +354,14 @@ __device__ __forceinline__ void free_accumulator(uint32_t bar, int lane) {
     }
 }
 
+// Parts that K is cut into: as many as give every SM or pair (slots) a tile, none of them empty.
+__host__ __device__ inline int parts_of_k(int most, int tiles, int slots, int nk) {
+    int parts = tiles > 0 ? slots / tiles : 1;
+    parts = parts < 1 ? 1 : parts > most ? most : parts;
+    const int part = (nk + parts - 1) / parts;
+    return (nk + part - 1) / part;
+}
+
 template <int CG, bool AMN, bool BMN, class Epi>
 __global__ void __launch_bounds__(kMatThreads, 1)
     k_matmul(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MatShape shape,
@@ -370,7 +383,9 @@ __global__ void __launch_bounds__(kMatThreads, 1)
     MatShape g = shape;
     if (g.live_m) g.M = *g.live_m, g.tiles_m = (g.M + 128 * CG - 1) / (128 * CG);
     if (g.live_k) g.K = *g.live_k;
-    const int per = tiles_per_matrix(g), total = per * g.batch;
+    const int per = tiles_per_matrix(g);
+    if (g.splits > 1) g.splits = g.batch = parts_of_k(g.splits, per, kSms / CG, g.plan_nk);
+    const int total = per * g.batch;
     const int first = blockIdx.x / CG, step = gridDim.x / CG;
     const int nk_all = (g.K + kTileK - 1) / kTileK, nk_part = (nk_all + g.splits - 1) / g.splits;
     const View va = {&map_a, &map_a, AMN ? Lie::mn : Lie::k, 0}, vb = {&map_b, &map_b, BMN ? Lie::mn : Lie::k, 0};
@@ -382,7 +397,7 @@ __global__ void __launch_bounds__(kMatThreads, 1)
         Ring r = {w.base, w.full, w.empty};
         for (int t = first; ok && t < total; t += step) {
             const TileAt at = tile_at(g, t, per);
-            const int am = at.m * 128 * CG + (int)rank * 128, bn = at.n * g.width + (int)rank * 128;
+            const int am = at.m * 128 * CG + (int)rank * 128, bn = at.n * g.width + (int)rank * (g.width / CG);
             const int k0 = g.splits > 1 ? at.b * nk_part : 0, k1 = min(k0 + nk_part, nk_all), z = g.splits > 1 ? 0 : at.b;
             ok = fill_tile<CG>(r, va, vb, am, bn, z, k0, k1, rank, full_at, g.stage_a + g.stage_b);
         }
@@ -413,8 +428,8 @@ __global__ void __launch_bounds__(kMatThreads, 1)
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
             mma_fence_after();
             const int row = at.m * 128 * CG + (int)rank * 128 + quad * 32 + lane;
-            const int col = at.n * g.width + half * (BN / 2);
-            Epi::template tile<BN / 2>(ea, g, w.tmem + acc * BN + half * (BN / 2) + ((uint32_t)quad << 21), row, col, at, half, turn);
+            const int hw = g.width / 2, col = at.n * g.width + half * hw;
+            Epi::template tile<BN / 2>(ea, g, w.tmem + acc * BN + half * hw + ((uint32_t)quad << 21), row, col, at, half, turn);
             free_accumulator<CG>(free_at + 8 * acc, lane);
             if (++acc == 2) acc = 0, aph ^= 1;
         }
@@ -435,7 +450,6 @@ cudaError_t make_map(CUtensorMap* out, const Operand& o, int rows, int k, int ba
 
 int device_sms();  // of the current device; 148 where that cannot be asked
 
-constexpr int kSms = 148;  // the launch rules below reckon with a B200's SMs, so that workspace sizes need no device
 
 // Pairs of CTAs with tiles of 256 x 256 multiply at the tensor cores' rate (511 cycles per stage of K = 64, of 512);
 // tiles of 128 x 128 are held up by what an SM gets from L2 (450 cycles of 256), but leave fewer SMs idle. A tile of the
@@ -455,10 +469,13 @@ template <int CG, bool AMN, bool BMN, class Epi>
 cudaError_t launch_matmul_cg(const Operand& a, const Operand& b, MatShape g, bool f16, const typename Epi::Args& ea,
                              cudaStream_t stream, bool dependent) {
     CUtensorMap ma, mb;
-    if (!g.width) g.width = 128 * CG;
+    if (!g.width) {  // tiles as wide as each other: 777 columns are 4 x 208, not 3 x 256 + 9
+        const int n = (g.N + 128 * CG - 1) / (128 * CG);
+        g.width = ((g.N + n - 1) / n + 15) / 16 * 16;
+    }
     const int matrices = g.splits > 1 ? 1 : g.batch;
     // Where the rows do not fill one tile, only their part of it is loaded; what the rest of the tile's rows hold does not matter.
-    const int box_a = !AMN && CG == 1 && g.M < 128 ? (g.M + 7) / 8 * 8 : 128, box_b = g.width / CG;
+    const int box_a = !AMN && CG == 1 && g.M < 128 ? (g.M + 7) / 8 * 8 : 128, box_b = BMN ? 128 : g.width / CG;
     g.stage_a = box_a * kTileK * 2, g.stage_b = box_b * kTileK * 2;
     cudaError_t err = make_map(&ma, a, g.M, g.K, matrices, f16, box_a);
     if (err == cudaSuccess) err = make_map(&mb, b, g.N, g.K, matrices, f16, box_b);
@@ -509,8 +526,9 @@ cudaError_t launch_matmul(const Operand& a, const Operand& b, int M, int N, int 
                                        : launch_matmul_cg<1, AMN, BMN, Epi>(a, b, g, f16, ea, stream, dependent);
 }
 
-// How a product with few tiles and a long K is cut: `splits` parts of K, on pairs of CTAs or single ones. The time of a
-// way is its waves times the stages of a part (and about 16 stages' time for filling the ring and storing a tile).
+// How a product with few tiles and a long K is cut: into at most `splits` parts of K, on pairs of CTAs or single ones. The
+// time of a way is its waves times the stages of a part (and about 16 stages' time for filling the ring and storing a
+// tile). Twice as many parts as M asks for are allowed, because fewer rows may take part than M.
 struct Cut {
     bool pairs;
     int splits;
@@ -530,14 +548,20 @@ inline Cut cut_of(int M, int N, int K) {
             if (least == 0 || cost < least) least = cost, best = {pairs != 0, s};
         }
     }
+    if (best.splits > 1) best.splits = 2 * best.splits < nk ? 2 * best.splits : nk;
     return best;
+}
+// The parts that a product over `live` rows is cut into.
+__host__ __device__ inline int parts_of(const Cut& cut, int live, int N, int plan_nk) {
+    const int b = cut.pairs ? 256 : 128, tiles = ((live + b - 1) / b) * ((N + b - 1) / b);
+    return cut.splits > 1 ? parts_of_k(cut.splits, tiles, cut.pairs ? kSms / 2 : kSms, plan_nk) : 1;
 }
 
 template <bool AMN, bool BMN, class Epi>
 cudaError_t launch_matmul_cut(const Operand& a, const Operand& b, int M, int N, int K, Cut cut, bool f16,
-                              const typename Epi::Args& ea, cudaStream_t stream, bool dependent, const int* live_m) {
+                              const typename Epi::Args& ea, cudaStream_t stream, bool dependent, const int* live_m, int plan_nk) {
     MatShape g = {};
-    g.M = M, g.N = N, g.K = K, g.batch = g.splits = cut.splits, g.live_m = live_m;
+    g.M = M, g.N = N, g.K = K, g.batch = g.splits = cut.splits, g.live_m = live_m, g.plan_nk = plan_nk;
     return cut.pairs ? launch_matmul_cg<2, AMN, BMN, Epi>(a, b, g, f16, ea, stream, dependent)
                      : launch_matmul_cg<1, AMN, BMN, Epi>(a, b, g, f16, ea, stream, dependent);
 }

@@ -172,8 +172,7 @@ struct EpiGram {
             }
 #pragma unroll
             for (int i = 0; i < 64; ++i) v[i] *= f;
-            turn.put16(v, true);
-            turn.store16(out, a.ld, row - turn.lane, col + c, a.s, a.s, true);
+            turn.write16(v, true, out, a.ld, row - turn.lane, col + c, a.s, a.s, true);
         }
     }
     // Joins the parts of a row's sums, in order, from the diagonal's block on. Run by a warp.
@@ -264,8 +263,7 @@ struct EpiPoly {
                 for (int i = 0; i < 64; ++i) v[i] = d == (unsigned)i ? own : v[i];
                 a.regain[(int64_t)at.b * a.s + row] = regain_row(own);
             }
-            turn.put16(v, true);
-            turn.store16(out, a.ld, row - turn.lane, col + c, a.s, a.s, true);
+            turn.write16(v, true, out, a.ld, row - turn.lane, col + c, a.s, a.s, true);
         }
     }
 };
@@ -303,8 +301,7 @@ struct EpiApply {
                     v[2 * i + 1] *= __shfl_sync(0xFFFFFFFFu, r1, i);
                 }
             }
-            turn.put16(v, a.f16);
-            turn.store16(a.out + at.b * a.batch_ld, a.ld, row - turn.lane, col + c, a.m, a.n, a.wide);
+            turn.write16(v, a.f16, a.out + at.b * a.batch_ld, a.ld, row - turn.lane, col + c, a.m, a.n, a.wide);
         }
     }
 };
