@@ -458,11 +458,14 @@ __global__ void __launch_bounds__(TPR < 512 ? 512 : TPR) k_norm_back(const NormB
     let_successor_start();
 }
 
-// The same for rows on 16-byte boundaries, as k_norm_ring: x and dy come by bulk copies.
+// The same for rows on 16-byte boundaries, as k_norm_ring: x and dy come by bulk copies. With 32 values a thread the
+// registers do not hold the weights too: they lie in shared memory before the ring then.
 template <class T, int TPR, int NV>
 __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_ring(const NormBack a, int stages) {
     constexpr int P = Chunk<T>::kPairs, kGroups = kRingThreads / TPR;
-    extern __shared__ __align__(128) uint8_t ring[];
+    constexpr bool kShared = 2 * P * NV > 16;
+    extern __shared__ __align__(128) uint8_t smem[];
+    uint8_t* ring = smem + (kShared ? a.cols * 4 : 0);
     __shared__ __align__(8) uint64_t s_full[kGroups * kMaxStages];
     __shared__ float s[2][2 * kRingThreads / 32];
     const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
@@ -481,10 +484,30 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_ring(const NormBa
         bar_init_done();
         for (int i = 0; i < stages && first + (int64_t)i * step < a.rows; ++i) fetch(first + (int64_t)i * step, i);
     }
-    Pair w[NV][P], dw[NV][P], db[NV][P];
+    Pair w[kShared ? 1 : NV][P], dw[NV][P], db[NV][P];
+    // the weights of chunk i: in registers, or read from shared memory each time
+    auto weights = [&](int i) -> Pair(&)[P] {
+        if constexpr (kShared) {
+            const float4* q = reinterpret_cast<const float4*>(smem) + (t + i * TPR) * (P / 2);
+#pragma unroll
+            for (int j = 0; j < P / 2; ++j) {
+                const float4 f = q[j];
+                w[0][2 * j] = pair(f.x, f.y), w[0][2 * j + 1] = pair(f.z, f.w);
+            }
+            return w[0];
+        } else {
+            return w[i];
+        }
+    };
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        if (t + i * TPR < cols16) load_param_pairs<T>(a.w, a.w32, (t + i * TPR) * 2 * P, 1.f, w[i]);
+        if (t + i * TPR < cols16) {
+            load_param_pairs<T>(a.w, a.w32, (t + i * TPR) * 2 * P, 1.f, w[kShared ? 0 : i]);
+            if constexpr (kShared) {  // every thread reads what it wrote itself
+#pragma unroll
+                for (int j = 0; j < P; ++j) reinterpret_cast<float2*>(smem)[(t + i * TPR) * P + j] = split(w[0][j]);
+            }
+        }
 #pragma unroll
         for (int j = 0; j < P; ++j) dw[i][j] = db[i][j] = both(0.f);
     }
@@ -509,13 +532,14 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_ring(const NormBa
             if (c >= cols16) break;
             x[i].raw = at[c];
             dy[i].raw = at[cols16 + c];
+            Pair(&wi)[P] = weights(i);
 #pragma unroll
             for (int j = 0; j < P; ++j) {
                 const Pair d = dy[i].get(j), e = d * ((x[i].get(j) + minus) * scale);  // dy * xh
                 db[i][j] = db[i][j] + d;
                 dw[i][j] = dw[i][j] + e;
-                acc1 = fma2(d, w[i][j], acc1);
-                acc2 = fma2(e, w[i][j], acc2);
+                acc1 = fma2(d, wi[j], acc1);
+                acc2 = fma2(e, wi[j], acc2);
             }
         }
         float sum[2] = {total(acc1), total(acc2)};
@@ -530,9 +554,10 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_ring(const NormBa
             const int c = t + i * TPR;
             if (c >= cols16) break;
             Chunk<T> q;
+            Pair(&wi)[P] = weights(i);
 #pragma unroll
             for (int j = 0; j < P; ++j)
-                q.set(j, fma2(x[i].get(j) + minus, c2, fma2(dy[i].get(j) * w[i][j], scale, c1)));
+                q.set(j, fma2(x[i].get(j) + minus, c2, fma2(dy[i].get(j) * wi[j], scale, c1)));
             dx[c] = q.raw;
         }
         if (++st == stages) st = 0, ph ^= 1;
@@ -705,12 +730,13 @@ cudaError_t back_ring(const NormBack& a, int* parts, cudaStream_t stream) {
     const int need = (a.rows + kGroups - 1) / kGroups;
     *parts = need < kNormSms ? need : kNormSms;
     const size_t stage = (size_t)a.cols * sizeof(T) * 2;
-    const int stages = ring_stages(kGroups, stage, kRingBytes);
+    const size_t weights = NV * (16 / sizeof(T)) > 16 ? (size_t)a.cols * 4 : 0;
+    const int stages = ring_stages(kGroups, stage, kRingBytes - weights);
     auto kernel = k_norm_back_ring<T, TPR, NV>;
     static std::atomic<uint64_t> ready{0};
     cudaError_t err = allow_smem(kernel, kRingBytes, ready);
     if (err != cudaSuccess) return err;
-    size_t smem = kGroups * stages * stage;
+    size_t smem = kGroups * stages * stage + weights;
     if (smem < (size_t)2 * a.cols * 4) smem = (size_t)2 * a.cols * 4;  // the ring's place also joins the groups' sums
     kernel<<<*parts, kRingThreads, smem, stream>>>(a, stages);
     return cudaGetLastError();
@@ -728,6 +754,9 @@ cudaError_t back_of(const NormBack& a, int* parts, bool wide, cudaStream_t strea
         if (n <= 128 * 16) return back_ring<T, 128, N>(a, parts, stream);
         if (n <= 256 * 16) return back_ring<T, 256, N>(a, parts, stream);
         if (n <= 512 * 16) return back_ring<T, 512, N>(a, parts, stream);
+        if constexpr (sizeof(T) == 2) {
+            if (n <= 512 * 32) return back_ring<T, 512, 2 * N>(a, parts, stream);
+        }
     } else {
         if (n <= 32 * 8) return back<T, 32, 8>(a, parts, stream);
         if (n <= 128 * 8) return back<T, 128, 8>(a, parts, stream);

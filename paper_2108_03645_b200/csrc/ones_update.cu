@@ -59,10 +59,10 @@ __global__ void __launch_bounds__(kNormThreads) k_ns_norm(Source g, double* part
             for (int c = lane * 8; c < g.n; c += 256) {
                 float v[8];
                 load8(g.p, at + c, g.type, v);
-                double e = 0.0;
+                double e[4] = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll
-                for (int i = 0; i < 8; ++i) e = fma((double)v[i], (double)v[i], e);
-                sum += e;
+                for (int i = 0; i < 8; ++i) e[i & 3] = fma((double)v[i], (double)v[i], e[i & 3]);
+                sum += (e[0] + e[1]) + (e[2] + e[3]);
             }
         } else {
 #pragma unroll 8
@@ -526,7 +526,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, c
     // (this CTA's columns of X: rows of the matrix if it is tall)
     const int64_t from = matrix * g.stride + (tall ? c0 * g.ld : c0);
     const int my_rows = tall ? mine : g.m, my_cols = tall ? g.n : mine;
-    double sum = 0.0;
+    double sums[4] = {0.0, 0.0, 0.0, 0.0};  // chains of additions in 64 bits are long: four of them
 #pragma unroll 4
     for (int r = warp; r < my_rows; r += kSmallThreads / 32) {
         if (g.wide) {
@@ -534,15 +534,17 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, c
                 float v[8];
                 load8(g.p, from + r * g.ld + c, g.type, v);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum = fma((double)v[i], (double)v[i], sum);
+                for (int i = 0; i < 8; ++i) sums[i & 3] = fma((double)v[i], (double)v[i], sums[i & 3]);
             }
         } else {
+#pragma unroll 4
             for (int c = lane; c < my_cols; c += 32) {
                 const double v = load_as_float(g.p, from + r * g.ld + c, g.type);
-                sum = fma(v, v, sum);
+                sums[0] = fma(v, v, sums[0]);
             }
         }
     }
+    double sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
     for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
     if (lane == 0) s_sum[warp] = sum;
     for (int i = threadIdx.x; i < p.own * kBlockBytes / 16; i += kSmallThreads) reinterpret_cast<uint4*>(x)[i] = make_uint4(0, 0, 0, 0);
