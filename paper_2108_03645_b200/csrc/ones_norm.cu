@@ -209,6 +209,11 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR)
 // registers nor on how many threads wait. What is left to bound the kernels is the issue of instructions, so a thread has
 // many values (the shuffles and the barrier of a sum cost as much for few) and does arithmetic on pairs.
 constexpr int kRingThreads = 512, kRingBytes = 196 * 1024, kMaxStages = 16;
+// Rows that a group takes together: short ones share the latency of their sums (their values go through one butterfly).
+template <int TPR, int kValues>
+constexpr int kRingRows = TPR == 32 ? (kValues <= 8 ? 4 : kValues <= 16 ? 2 : 1) : 1;
+template <int TPR, int kValues>
+constexpr int kRingBackRows = TPR == 32 && kValues <= 8 ? 2 : 1;
 
 template <int TPR>
 __device__ __forceinline__ void group_sync(int group) {
@@ -223,18 +228,20 @@ __device__ unsigned g_wait_expired;
 template <class T, int TPR, int NV>
 __global__ void __launch_bounds__(kRingThreads, 1)
     k_norm_ring(const NormIn a, void* y_, int64_t ldy, float* mean_out, float* rstd_out, int stages) {
-    constexpr int P = Chunk<T>::kPairs, kGroups = kRingThreads / TPR;
+    constexpr int P = Chunk<T>::kPairs, kGroups = kRingThreads / TPR, R = kRingRows<TPR, 2 * P * NV>;
     extern __shared__ __align__(128) uint8_t ring[];
     __shared__ __align__(8) uint64_t s_full[kGroups * kMaxStages];
-    __shared__ float s[2][2][kRingThreads / 32];
+    __shared__ float s[2][2][R * kRingThreads / 32];
     const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
     const int cols16 = a.cols / (2 * P);  // chunks of a row
     const uint32_t bytes = a.cols * sizeof(T), full = smem_u32(s_full + group * kMaxStages);
-    uint8_t* mine = ring + (size_t)group * stages * bytes;
-    const int first = blockIdx.x * kGroups + group, step = gridDim.x * kGroups;
+    uint8_t* mine = ring + (size_t)group * stages * R * bytes;
+    const int first = (blockIdx.x * kGroups + group) * R, step = gridDim.x * kGroups * R;
     auto fetch = [&](int64_t row, int st) {
-        bar_expect(full + 8 * st, bytes);
-        bulk_load(smem_u32(mine + st * bytes), static_cast<const T*>(a.x) + row * a.ldx, bytes, full + 8 * st);
+        const int n = (int)(a.rows - row < R ? a.rows - row : R);
+        bar_expect(full + 8 * st, n * bytes);
+        for (int r = 0; r < n; ++r)
+            bulk_load(smem_u32(mine + (st * R + r) * bytes), static_cast<const T*>(a.x) + (row + r) * a.ldx, bytes, full + 8 * st);
     };
     if (t == 0) {
         for (int i = 0; i < stages; ++i) bar_init(full + 8 * i, 1);
@@ -257,50 +264,62 @@ __global__ void __launch_bounds__(kRingThreads, 1)
     for (int64_t row = first; row < a.rows; row += step, turn ^= 1) {
         const bool ok = bar_wait(full + 8 * st, ph, &g_wait_expired);
         bad = bad || !ok;
-        const uint4* at = reinterpret_cast<const uint4*>(mine + st * bytes);
-        Pair v[NV][P], acc = both(0.f);
+        Pair v[R][NV][P];
+        float sum[R], sq[R];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            if (t + i * TPR < cols16) {
-                const Chunk<T> q = {at[t + i * TPR]};
+        for (int r = 0; r < R; ++r) {
+            const uint4* at = reinterpret_cast<const uint4*>(mine + (st * R + r) * bytes);
+            Pair acc = both(0.f);
 #pragma unroll
-                for (int j = 0; j < P; ++j) acc = acc + (v[i][j] = q.get(j));
-            }
-        }
-        float sum[1] = {total(acc)};
-        row_sums<TPR, 1>(sum, s[turn][0], group);
-        // everybody has read this row: its place is free
-        if (t == 0 && ok && row + (int64_t)stages * step < a.rows) fetch(row + (int64_t)stages * step, st);
-        const float mean = sum[0] * inv;
-        const Pair minus = both(-mean);
-        acc = both(0.f);
+            for (int i = 0; i < NV; ++i) {
+                if (t + i * TPR < cols16 && (R == 1 || row + r < a.rows)) {
+                    const Chunk<T> q = {at[t + i * TPR]};
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            if (t + i * TPR < cols16) {
-#pragma unroll
-                for (int j = 0; j < P; ++j) {
-                    v[i][j] = v[i][j] + minus;
-                    acc = fma2(v[i][j], v[i][j], acc);
+                    for (int j = 0; j < P; ++j) acc = acc + (v[r][i][j] = q.get(j));
                 }
             }
+            sum[r] = total(acc);
         }
-        float sq[1] = {total(acc)};
-        row_sums<TPR, 1>(sq, s[turn][1], group);
-        const float rstd = inv_sqrt(fmaf(sq[0], inv, a.eps));
-        if (t == 0) {
-            if (mean_out) mean_out[row] = mean;
-            if (rstd_out) rstd_out[row] = rstd;
+        row_sums<TPR, R>(sum, s[turn][0], group);
+        // everybody has read these rows: their place is free
+        if (t == 0 && ok && row + (int64_t)stages * step < a.rows) fetch(row + (int64_t)stages * step, st);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            sum[r] *= inv;
+            const Pair minus = both(-sum[r]);
+            Pair acc = both(0.f);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                if (t + i * TPR < cols16) {
+#pragma unroll
+                    for (int j = 0; j < P; ++j) {
+                        v[r][i][j] = v[r][i][j] + minus;
+                        acc = fma2(v[r][i][j], v[r][i][j], acc);
+                    }
+                }
+            }
+            sq[r] = total(acc);
         }
-        uint4* y = reinterpret_cast<uint4*>(static_cast<T*>(y_) + row * ldy);
-        const Pair scale = both(rstd);
+        row_sums<TPR, R>(sq, s[turn][1], group);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = t + i * TPR;
-            if (c >= cols16) break;
-            Chunk<T> q;
+        for (int r = 0; r < R; ++r) {
+            if (R > 1 && row + r >= a.rows) break;
+            const float rstd = inv_sqrt(fmaf(sq[r], inv, a.eps));
+            if (t == 0) {
+                if (mean_out) mean_out[row + r] = sum[r];
+                if (rstd_out) rstd_out[row + r] = rstd;
+            }
+            uint4* y = reinterpret_cast<uint4*>(static_cast<T*>(y_) + (row + r) * ldy);
+            const Pair scale = both(rstd);
 #pragma unroll
-            for (int j = 0; j < P; ++j) q.set(j, fma2(v[i][j] * scale, w[i][j], b[i][j]));
-            y[c] = q.raw;
+            for (int i = 0; i < NV; ++i) {
+                const int c = t + i * TPR;
+                if (c >= cols16) break;
+                Chunk<T> q;
+#pragma unroll
+                for (int j = 0; j < P; ++j) q.set(j, fma2(v[r][i][j] * scale, w[i][j], b[i][j]));
+                y[c] = q.raw;
+            }
         }
         if (++st == stages) st = 0, ph ^= 1;
     }
@@ -462,22 +481,25 @@ __global__ void __launch_bounds__(TPR < 512 ? 512 : TPR) k_norm_back(const NormB
 // registers do not hold the weights too: they lie in shared memory before the ring then.
 template <class T, int TPR, int NV>
 __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_ring(const NormBack a, int stages) {
-    constexpr int P = Chunk<T>::kPairs, kGroups = kRingThreads / TPR;
+    constexpr int P = Chunk<T>::kPairs, kGroups = kRingThreads / TPR, R = kRingBackRows<TPR, 2 * P * NV>;
     constexpr bool kShared = 2 * P * NV > 16;
     extern __shared__ __align__(128) uint8_t smem[];
     uint8_t* ring = smem + (kShared ? a.cols * 4 : 0);
     __shared__ __align__(8) uint64_t s_full[kGroups * kMaxStages];
-    __shared__ float s[2][2 * kRingThreads / 32];
+    __shared__ float s[2][2 * R * kRingThreads / 32];
     const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
     const int cols16 = a.cols / (2 * P);
     const uint32_t bytes = a.cols * sizeof(T), full = smem_u32(s_full + group * kMaxStages);
-    uint8_t* mine = ring + (size_t)group * stages * 2 * bytes;
-    const int first = blockIdx.x * kGroups + group, step = gridDim.x * kGroups;
+    uint8_t* mine = ring + (size_t)group * stages * R * 2 * bytes;
+    const int first = (blockIdx.x * kGroups + group) * R, step = gridDim.x * kGroups * R;
     auto fetch = [&](int64_t row, int st) {
-        const uint32_t at = smem_u32(mine + st * 2 * bytes);
-        bar_expect(full + 8 * st, 2 * bytes);
-        bulk_load(at, static_cast<const T*>(a.x) + row * a.ldx, bytes, full + 8 * st);
-        bulk_load(at + bytes, static_cast<const T*>(a.dy) + row * a.lddy, bytes, full + 8 * st);
+        const int n = (int)(a.rows - row < R ? a.rows - row : R);
+        bar_expect(full + 8 * st, 2 * n * bytes);
+        for (int r = 0; r < n; ++r) {
+            const uint32_t at = smem_u32(mine + (st * R + r) * 2 * bytes);
+            bulk_load(at, static_cast<const T*>(a.x) + (row + r) * a.ldx, bytes, full + 8 * st);
+            bulk_load(at + bytes, static_cast<const T*>(a.dy) + (row + r) * a.lddy, bytes, full + 8 * st);
+        }
     };
     if (t == 0) {
         for (int i = 0; i < stages; ++i) bar_init(full + 8 * i, 1);
@@ -516,49 +538,65 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_ring(const NormBa
     int st = 0, turn = 0;
     uint32_t ph = 0;
     bool bad = false;
-    float nmean = first < a.rows ? a.mean[first] : 0.f, nrstd = first < a.rows ? a.rstd[first] : 0.f;
+    float nmean[R], nrstd[R];
+    auto statistics = [&](int64_t row) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (row + r < a.rows) nmean[r] = a.mean[row + r], nrstd[r] = a.rstd[row + r];
+    };
+    statistics(first);
     for (int64_t row = first; row < a.rows; row += step, turn ^= 1) {
-        const float mean = nmean, rstd = nrstd;
-        if (row + step < a.rows) nmean = a.mean[row + step], nrstd = a.rstd[row + step];
+        float mean[R], rstd[R], sum[2 * R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) mean[r] = nmean[r], rstd[r] = nrstd[r];
+        statistics(row + step);
         const bool ok = bar_wait(full + 8 * st, ph, &g_wait_expired);
         bad = bad || !ok;
-        const uint4* at = reinterpret_cast<const uint4*>(mine + st * 2 * bytes);
-        const Pair scale = both(rstd), minus = both(-mean);
-        Pair acc1 = both(0.f), acc2 = both(0.f);
-        Chunk<T> x[NV], dy[NV];
+        Chunk<T> x[R][NV], dy[R][NV];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = t + i * TPR;
-            if (c >= cols16) break;
-            x[i].raw = at[c];
-            dy[i].raw = at[cols16 + c];
-            Pair(&wi)[P] = weights(i);
+        for (int r = 0; r < R; ++r) {
+            const uint4* at = reinterpret_cast<const uint4*>(mine + (st * R + r) * 2 * bytes);
+            const Pair scale = both(rstd[r]), minus = both(-mean[r]);
+            Pair acc1 = both(0.f), acc2 = both(0.f);
 #pragma unroll
-            for (int j = 0; j < P; ++j) {
-                const Pair d = dy[i].get(j), e = d * ((x[i].get(j) + minus) * scale);  // dy * xh
-                db[i][j] = db[i][j] + d;
-                dw[i][j] = dw[i][j] + e;
-                acc1 = fma2(d, wi[j], acc1);
-                acc2 = fma2(e, wi[j], acc2);
+            for (int i = 0; i < NV; ++i) {
+                const int c = t + i * TPR;
+                if (c >= cols16 || (R > 1 && row + r >= a.rows)) break;
+                x[r][i].raw = at[c];
+                dy[r][i].raw = at[cols16 + c];
+                Pair(&wi)[P] = weights(i);
+#pragma unroll
+                for (int j = 0; j < P; ++j) {
+                    const Pair d = dy[r][i].get(j), e = d * ((x[r][i].get(j) + minus) * scale);  // dy * xh
+                    db[i][j] = db[i][j] + d;
+                    dw[i][j] = dw[i][j] + e;
+                    acc1 = fma2(d, wi[j], acc1);
+                    acc2 = fma2(e, wi[j], acc2);
+                }
             }
+            sum[2 * r] = total(acc1), sum[2 * r + 1] = total(acc2);
         }
-        float sum[2] = {total(acc1), total(acc2)};
-        row_sums<TPR, 2>(sum, s[turn], group);
+        row_sums<TPR, 2 * R>(sum, s[turn], group);
         // everybody has read these rows: their place is free
         if (t == 0 && ok && row + (int64_t)stages * step < a.rows) fetch(row + (int64_t)stages * step, st);
-        // dx = rstd * (dy * w - c1 - xh * c2)
-        const Pair c1 = both(-rstd * sum[0] * inv), c2 = both(-rstd * rstd * sum[1] * inv);
-        uint4* dx = reinterpret_cast<uint4*>(static_cast<T*>(a.dx) + row * a.lddx);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = t + i * TPR;
-            if (c >= cols16) break;
-            Chunk<T> q;
-            Pair(&wi)[P] = weights(i);
+        for (int r = 0; r < R; ++r) {
+            if (R > 1 && row + r >= a.rows) break;
+            // dx = rstd * (dy * w - c1 - xh * c2)
+            const Pair c1 = both(-rstd[r] * sum[2 * r] * inv), c2 = both(-rstd[r] * rstd[r] * sum[2 * r + 1] * inv);
+            const Pair scale = both(rstd[r]), minus = both(-mean[r]);
+            uint4* dx = reinterpret_cast<uint4*>(static_cast<T*>(a.dx) + (row + r) * a.lddx);
 #pragma unroll
-            for (int j = 0; j < P; ++j)
-                q.set(j, fma2(x[i].get(j) + minus, c2, fma2(dy[i].get(j) * wi[j], scale, c1)));
-            dx[c] = q.raw;
+            for (int i = 0; i < NV; ++i) {
+                const int c = t + i * TPR;
+                if (c >= cols16) break;
+                Chunk<T> q;
+                Pair(&wi)[P] = weights(i);
+#pragma unroll
+                for (int j = 0; j < P; ++j)
+                    q.set(j, fma2(x[r][i].get(j) + minus, c2, fma2(dy[r][i].get(j) * wi[j], scale, c1)));
+                dx[c] = q.raw;
+            }
         }
         if (++st == stages) st = 0, ph ^= 1;
     }
@@ -679,9 +717,9 @@ inline int ring_stages(int groups, size_t stage_bytes, size_t most) {
 
 template <class T, int TPR, int NV>
 cudaError_t norm_ring(const NormIn& a, void* y, int64_t ldy, float* mean, float* rstd, cudaStream_t stream) {
-    constexpr int kGroups = kRingThreads / TPR;
-    const int need = (a.rows + kGroups - 1) / kGroups, blocks = need < kNormSms ? need : kNormSms;
-    const size_t row = (size_t)a.cols * sizeof(T);
+    constexpr int kGroups = kRingThreads / TPR, R = kRingRows<TPR, NV * 16 / (int)sizeof(T)>;
+    const int need = (a.rows + kGroups * R - 1) / (kGroups * R), blocks = need < kNormSms ? need : kNormSms;
+    const size_t row = (size_t)a.cols * sizeof(T) * R;
     const int stages = ring_stages(kGroups, row, kRingBytes);
     auto kernel = k_norm_ring<T, TPR, NV>;
     static std::atomic<uint64_t> ready{0};
@@ -726,10 +764,10 @@ cudaError_t back(const NormBack& a, int* parts, cudaStream_t stream) {
 
 template <class T, int TPR, int NV>
 cudaError_t back_ring(const NormBack& a, int* parts, cudaStream_t stream) {
-    constexpr int kGroups = kRingThreads / TPR;
-    const int need = (a.rows + kGroups - 1) / kGroups;
+    constexpr int kGroups = kRingThreads / TPR, R = kRingBackRows<TPR, NV * 16 / (int)sizeof(T)>;
+    const int need = (a.rows + kGroups * R - 1) / (kGroups * R);
     *parts = need < kNormSms ? need : kNormSms;
-    const size_t stage = (size_t)a.cols * sizeof(T) * 2;
+    const size_t stage = (size_t)a.cols * sizeof(T) * 2 * R;
     const size_t weights = NV * (16 / sizeof(T)) > 16 ? (size_t)a.cols * 4 : 0;
     const int stages = ring_stages(kGroups, stage, kRingBytes - weights);
     auto kernel = k_norm_back_ring<T, TPR, NV>;
