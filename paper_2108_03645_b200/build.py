@@ -1,4 +1,5 @@
-"""Build libones.so (CUDA kernels + C ABI) in-tree with nvcc for sm_100a."""
+"""Build libones.so (CUDA kernels + C ABI) in-tree with nvcc for sm_100a, and the torch marshalling of its training-step
+operators with g++."""
 from __future__ import annotations
 
 import glob
@@ -11,6 +12,7 @@ _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 INCLUDE = os.path.join(_ROOT, "include")
 LIB = os.path.join(_HERE, "libones.so")
+TORCH_LIB = os.path.join(_HERE, "_train_torch.so")  # marshalling of the training-step operators for torch tensors
 
 
 def sources() -> list[str]:
@@ -22,11 +24,30 @@ def _deps() -> list[str]:
         glob.glob(os.path.join(INCLUDE, "*.h"))
 
 
+def _torch_source() -> str:
+    return os.path.join(CSRC, "ones_train_torch.cpp")
+
+
+def _newer(lib: str, deps: list[str]) -> bool:
+    return os.path.exists(lib) and all(os.path.getmtime(f) <= os.path.getmtime(lib) for f in deps)
+
+
 def up_to_date() -> bool:
-    if not os.path.exists(LIB):
-        return False
-    t = os.path.getmtime(LIB)
-    return all(os.path.getmtime(f) <= t for f in _deps())
+    return _newer(LIB, _deps()) and _newer(TORCH_LIB, [_torch_source()] + glob.glob(os.path.join(INCLUDE, "*.h")))
+
+
+def _torch_command(out: str) -> list[str]:
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include")
+    includes = [INCLUDE, os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), cuda,
+                sysconfig.get_paths()["include"]]
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-DTORCH_EXTENSION_NAME=_train_torch",
+            "-DTORCH_API_INCLUDE_EXTENSION_H", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+            *[x for i in includes for x in ("-isystem", i)], _torch_source(), "-o", out, "-L", os.path.join(root, "lib"), "-ltorch",
+            "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python", "-lc10", "-lc10_cuda", "-L", _HERE, "-l:libones.so", "-Wl,-rpath,$ORIGIN"]
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -45,6 +66,11 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if verbose:
         print(res.stderr)
     os.replace(tmp, LIB)
+    tmp = TORCH_LIB + f".tmp{os.getpid()}"
+    res = subprocess.run(_torch_command(tmp), capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("g++ failed:\n" + res.stdout + res.stderr)
+    os.replace(tmp, TORCH_LIB)
     return LIB
 
 
