@@ -94,7 +94,7 @@ struct EpiDlogits {
         uint16_t* out;
         int64_t ld;
         int rows, first, cols;  // the piece: `cols` entries from `first`
-        bool f16;
+        bool f16, twice;        // twice: what the rounding left goes into a second row of ld / 2 values
     };
     template <int W>
     static __device__ __forceinline__ void tile(const Args& a, const MatShape& shape, uint32_t acc, int row, int col,
@@ -124,6 +124,12 @@ struct EpiDlogits {
                     if (at_i == (unsigned)i) v[i] -= r.g;
             }
             turn.write16(v, a.f16, a.out, a.ld, row - turn.lane, col + c, rows, end, true);
+            if (a.twice) {
+#pragma unroll
+                for (int i = 0; i < 64; ++i)
+                    v[i] -= a.f16 ? __half2float(__float2half_rn(v[i])) : __bfloat162float(__float2bfloat16_rn(v[i]));
+                turn.write16(v, a.f16, a.out + a.ld / 2, a.ld, row - turn.lane, col + c, rows, end, true);
+            }
         }
     }
 };
@@ -338,7 +344,8 @@ __global__ void __launch_bounds__(1024) k_ce_scan(const float* dloss, const int6
 // them, and clears the gradients of the rows that take none. A warp takes a row at a time.
 __global__ void __launch_bounds__(256) k_ce_gather(const uint16_t* hidden, int64_t ldh, const int64_t* target, const float* dloss,
                                                    const float* lse, int rows, int cols, int vocab, const Header* head, RowInfo* info,
-                                                   uint16_t* out, int64_t ld_out, uint16_t* dhidden, int64_t lddh, bool wide_in, bool wide_dh) {
+                                                   uint16_t* out, int64_t ld_out, int times, uint16_t* dhidden, int64_t lddh, bool wide_in,
+                                                   bool wide_dh) {
     wait_for_predecessor();
     let_successor_start();
     const int lane = threadIdx.x % 32, live = head->live;
@@ -346,13 +353,15 @@ __global__ void __launch_bounds__(256) k_ce_gather(const uint16_t* hidden, int64
     const int padded = min(rows, (live + kTileK - 1) / kTileK * kTileK);
     for (int i = blockIdx.x * 8 + threadIdx.x / 32; i < rows; i += gridDim.x * 8) {
         if (i < padded) {
-            uint16_t* to = out + (int64_t)i * ld_out;
             const int row = i < live ? info[i].row : -1;
             const uint16_t* from = hidden + (int64_t)row * ldh;
             const int whole = wide_in || row < 0 ? cols / 8 : 0;  // ld_out is a multiple of 8
-            for (int c = lane; c < whole; c += 32)
-                reinterpret_cast<uint4*>(to)[c] = row >= 0 ? reinterpret_cast<const uint4*>(from)[c] : make_uint4(0, 0, 0, 0);
-            for (int c = whole * 8 + lane; c < cols; c += 32) to[c] = row >= 0 ? from[c] : 0;
+            for (int k = 0; k < times; ++k) {
+                uint16_t* to = out + ((int64_t)i * times + k) * ld_out;
+                for (int c = lane; c < whole; c += 32)
+                    reinterpret_cast<uint4*>(to)[c] = row >= 0 ? reinterpret_cast<const uint4*>(from)[c] : make_uint4(0, 0, 0, 0);
+                for (int c = whole * 8 + lane; c < cols; c += 32) to[c] = row >= 0 ? from[c] : 0;
+            }
             __syncwarp();
             if (lane == 0 && row >= 0) {
                 RowInfo r;
@@ -433,16 +442,25 @@ int32_t piece_of(int32_t rows, int32_t vocab, int32_t piece) {
     return (int32_t)up((size_t)((vocab + n - 1) / n), 256);
 }
 
+// With few rows an error is not averaged over many products, and the time goes by the weight's bytes: the gradients of the
+// logits are kept as two 16-bit terms then, the rounded value and what the rounding left (each row twice in the gathered
+// rows, so that both terms meet it), and nothing but the roundings of the results is left of the 16 bits: 1.7e-3 of the
+// norm for bfloat16 instead of up to 3.9e-3.
+constexpr int32_t kFewRows = 64;
+inline int fold_of(int32_t rows) { return rows <= kFewRows ? 2 : 1; }
+
 struct BackwardLayout {
     size_t head, info, hidden, dlogits, sum, total;
     int64_t ld_sum, ld_hidden;
     int32_t piece;
+    int fold;
     Cut cut;  // of the product over a piece of the vocabulary
 };
 BackwardLayout backward_layout(int32_t rows, int32_t cols, int32_t vocab, int32_t piece) {
     BackwardLayout L;
     L.piece = piece_of(rows, vocab, piece);
-    L.cut = cut_of(rows, cols, vocab < L.piece ? vocab : L.piece);
+    L.fold = fold_of(rows);
+    L.cut = cut_of(rows, cols, (int)up(vocab < L.piece ? vocab : L.piece, kTileK) * L.fold);
     L.ld_sum = (int64_t)up(cols, 32);
     L.ld_hidden = (int64_t)up(cols, 8);
     size_t at = 0;
@@ -453,8 +471,8 @@ BackwardLayout backward_layout(int32_t rows, int32_t cols, int32_t vocab, int32_
     };
     L.head = take(sizeof(Header));
     L.info = take((size_t)rows * sizeof(RowInfo));
-    L.hidden = take((size_t)rows * L.ld_hidden * 2);
-    L.dlogits = take((size_t)rows * L.piece * 2);
+    L.hidden = take((size_t)rows * L.fold * L.ld_hidden * 2);
+    L.dlogits = take((size_t)rows * L.fold * L.piece * 2);
     L.sum = take(L.piece < vocab || L.cut.splits > 1 ? (size_t)L.cut.splits * rows * L.ld_sum * 4 : 0);
     L.total = at;
     return L;
@@ -545,30 +563,30 @@ int ones_linear_ce_backward(const float* d_dloss, const void* d_hidden, int64_t 
     const bool f16 = type == ONES_F16;
     const bool wide_h = aligned(d_dhidden, 16) && lddh % 8 == 0, wide_w = aligned(d_dweight, 16) && lddw % 8 == 0;
     const bool wide_in = aligned(d_hidden, 16) && ldh % 8 == 0;
-    const int plan_nk = ((vocab < L.piece ? vocab : L.piece) + kTileK - 1) / kTileK;  // of the first piece: later ones are no longer
+    const int fold = L.fold, plan_nk = ((vocab < L.piece ? vocab : L.piece) + kTileK - 1) / kTileK * fold;  // of the first piece: later ones are no longer
     const unsigned row_blocks = (unsigned)((rows + 7) / 8 < 8 * kSms ? (rows + 7) / 8 : 8 * kSms);
 
     k_ce_scan<<<1, 1024, 0, stream>>>(d_dloss, d_target, rows, vocab, info, head);
     cudaError_t err = cudaGetLastError();
     if (err == cudaSuccess)
         err = launch_after(k_ce_gather, dim3(row_blocks), dim3(256), stream, static_cast<const uint16_t*>(d_hidden), ldh, d_target, d_dloss,
-                           d_lse, rows, cols, vocab, static_cast<const Header*>(head), info, hidden, L.ld_hidden, dh, lddh, wide_in, wide_h);
+                           d_lse, rows, cols, vocab, static_cast<const Header*>(head), info, hidden, L.ld_hidden, fold, dh, lddh, wide_in, wide_h);
     for (int32_t v0 = 0; err == cudaSuccess && v0 < vocab; v0 += L.piece) {
         const int32_t n = vocab - v0 < L.piece ? vocab - v0 : L.piece;
         const bool last = v0 + n == vocab;
         const uint16_t* w0 = static_cast<const uint16_t*>(d_weight) + (int64_t)v0 * ldw;
-        const EpiDlogits::Args e1 = {info, dl, L.piece, rows, v0, n, f16};
-        err = launch_matmul<false, false, EpiDlogits>({hidden, L.ld_hidden, 0, false}, {w0, ldw, 0, false}, rows, n, cols, 1, false,
+        const EpiDlogits::Args e1 = {info, dl, (int64_t)L.piece * fold, rows, v0, n, f16, fold == 2};
+        err = launch_matmul<false, false, EpiDlogits>({hidden, L.ld_hidden * fold, 0, false}, {w0, ldw, 0, false}, rows, n, cols, 1, false,
                                                       f16, e1, stream, true, &head->live);
         if (err != cudaSuccess) break;
         const EpiSum::Args e2 = {sum, L.ld_sum, dh, lddh, &head->scale, info, rows, cols, v0 == 0, last && L.cut.splits == 1, f16, wide_h};
-        err = launch_matmul_cut<false, true, EpiSum>({dl, L.piece, 0, false}, {w0, ldw, 0, true}, rows, cols, n, L.cut, f16,
-                                                     e2, stream, true, &head->live, plan_nk);
+        err = launch_matmul_cut<false, true, EpiSum>({dl, (int64_t)L.piece * fold, L.piece, false}, {w0, ldw, 0, true}, rows, cols, n, L.cut, f16,
+                                                     e2, stream, true, &head->live, plan_nk, fold);
         if (err != cudaSuccess) break;
         const EpiGrad::Args e3 = {static_cast<char*>(d_dweight) + (int64_t)v0 * lddw * (int64_t)wsize, lddw, &head->scale, n, cols,
                                   wtype == ONES_F32, f16, wide_w};
-        err = launch_matmul<true, true, EpiGrad>({dl, L.piece, 0, true}, {hidden, L.ld_hidden, 0, true}, n, cols, rows, 1, false, f16,
-                                                 e3, stream, true, nullptr, &head->live);
+        err = launch_matmul<true, true, EpiGrad>({dl, L.piece, 0, true}, {hidden, L.ld_hidden, 0, true}, n, cols, rows * fold, 1, false, f16,
+                                                 e3, stream, true, nullptr, &head->live, 0, fold);
     }
     if (err == cudaSuccess && L.cut.splits > 1)
         err = launch_after(k_ce_rows, dim3(row_blocks), dim3(256), stream, static_cast<const float*>(sum), L.cut, plan_nk, L.ld_sum, rows, cols,

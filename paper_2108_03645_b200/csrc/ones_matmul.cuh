@@ -39,8 +39,10 @@ struct MatShape {
     int tiles_m, tiles_n, batch;
     int splits;  // > 1: K is cut into parts, at most so many, each with a C of its own in the place of a matrix of the batch
     int plan_nk; // stages of K that the number of parts goes by (K itself may be shorter)
+    int fold;    // 2: A has two terms (a matrix of the batch each) that meet the same B: K runs over it twice
     int sym;     // only tiles on and above the diagonal are computed (C is symmetric)
     const int *live_m, *live_k;  // where M or K is known on the device only (at most the value above)
+    int live_times;              // K is so many times what live_k says
     int group;  // row tiles that run through the columns together, so that both operands' tiles are met again in L2
     bool f16;
     int width;         // columns of a tile: 128 * CG, or fewer where N is to be spread evenly (multiple of 16)
@@ -115,14 +117,15 @@ __device__ __forceinline__ void fill_operand(uint32_t at, const View& v, int row
 // Fills the stages of one tile: K from stage k0 to k1, rows am of A and bn of B. Run by a whole warp; false: gave up.
 template <int CG>
 __device__ __forceinline__ bool fill_tile(Ring& r, const View& va, const View& vb, int am, int bn, int z, int k0, int k1, uint32_t rank,
-                                          uint32_t full_at, uint32_t bytes = kStageBytes) {
+                                          uint32_t full_at, uint32_t bytes = kStageBytes, int nk_one = 1 << 30) {
     for (int k = k0; k < k1; ++k) {
+        const int term = k >= nk_one, kb = term ? k - nk_one : k;
         if (!bar_wait(r.empty + 8 * r.s, r.ph ^ 1, &g_wait_expired)) return false;
         const uint32_t a = r.base + r.s * kStageBytes, bar = full_at + 8 * r.s;
         if (elect_one()) {
             if (rank == 0) bar_expect(r.full + 8 * r.s, CG * bytes);
-            fill_operand<CG>(a, va, am, k, z, bar);
-            fill_operand<CG>(a + kHalf, vb, bn, k, z, bar);
+            fill_operand<CG>(a, va, am, kb, z + term, bar);
+            fill_operand<CG>(a + kHalf, vb, bn, kb, z, bar);
         }
         __syncwarp();
         r.next();
@@ -382,12 +385,12 @@ __global__ void __launch_bounds__(kMatThreads, 1)
 
     MatShape g = shape;
     if (g.live_m) g.M = *g.live_m, g.tiles_m = (g.M + 128 * CG - 1) / (128 * CG);
-    if (g.live_k) g.K = *g.live_k;
+    if (g.live_k) g.K = *g.live_k * g.live_times;
     const int per = tiles_per_matrix(g);
     if (g.splits > 1) g.splits = g.batch = parts_of_k(g.splits, per, kSms / CG, g.plan_nk);
     const int total = per * g.batch;
     const int first = blockIdx.x / CG, step = gridDim.x / CG;
-    const int nk_all = (g.K + kTileK - 1) / kTileK, nk_part = (nk_all + g.splits - 1) / g.splits;
+    const int nk_one = (g.K + kTileK - 1) / kTileK, nk_all = nk_one * g.fold, nk_part = (nk_all + g.splits - 1) / g.splits;
     const View va = {&map_a, &map_a, AMN ? Lie::mn : Lie::k, 0}, vb = {&map_b, &map_b, BMN ? Lie::mn : Lie::k, 0};
     bool ok = true;
 
@@ -399,7 +402,7 @@ __global__ void __launch_bounds__(kMatThreads, 1)
             const TileAt at = tile_at(g, t, per);
             const int am = at.m * 128 * CG + (int)rank * 128, bn = at.n * g.width + (int)rank * (g.width / CG);
             const int k0 = g.splits > 1 ? at.b * nk_part : 0, k1 = min(k0 + nk_part, nk_all), z = g.splits > 1 ? 0 : at.b;
-            ok = fill_tile<CG>(r, va, vb, am, bn, z, k0, k1, rank, full_at, g.stage_a + g.stage_b);
+            ok = fill_tile<CG>(r, va, vb, am, bn, z, k0, k1, rank, full_at, g.stage_a + g.stage_b, nk_one);
         }
     } else if (warp == 1 && rank == 0) {
         // multiply
@@ -477,7 +480,8 @@ cudaError_t launch_matmul_cg(const Operand& a, const Operand& b, MatShape g, boo
     // Where the rows do not fill one tile, only their part of it is loaded; what the rest of the tile's rows hold does not matter.
     const int box_a = !AMN && CG == 1 && g.M < 128 ? (g.M + 7) / 8 * 8 : 128, box_b = BMN ? 128 : g.width / CG;
     g.stage_a = box_a * kTileK * 2, g.stage_b = box_b * kTileK * 2;
-    cudaError_t err = make_map(&ma, a, g.M, g.K, matrices, f16, box_a);
+    if (!g.fold) g.fold = 1;
+    cudaError_t err = make_map(&ma, a, g.M, g.K, g.fold > 1 ? g.fold : matrices, f16, box_a);
     if (err == cudaSuccess) err = make_map(&mb, b, g.N, g.K, matrices, f16, box_b);
     if (err != cudaSuccess) return err;
     g.tiles_m = (g.M + 128 * CG - 1) / (128 * CG);
@@ -518,9 +522,9 @@ cudaError_t launch_matmul_cg(const Operand& a, const Operand& b, MatShape g, boo
 template <bool AMN, bool BMN, class Epi>
 cudaError_t launch_matmul(const Operand& a, const Operand& b, int M, int N, int K, int batch, bool sym, bool f16,
                           const typename Epi::Args& ea, cudaStream_t stream, bool dependent, const int* live_m = nullptr,
-                          const int* live_k = nullptr, int width = 0) {
+                          const int* live_k = nullptr, int width = 0, int live_times = 1) {
     MatShape g = {};
-    g.width = width;
+    g.width = width, g.live_times = live_times;
     g.M = M, g.N = N, g.K = K, g.batch = batch, g.splits = 1, g.sym = sym, g.live_m = live_m, g.live_k = live_k;
     return !width && use_pairs(M, N, batch, sym) ? launch_matmul_cg<2, AMN, BMN, Epi>(a, b, g, f16, ea, stream, dependent)
                                        : launch_matmul_cg<1, AMN, BMN, Epi>(a, b, g, f16, ea, stream, dependent);
@@ -559,8 +563,9 @@ __host__ __device__ inline int parts_of(const Cut& cut, int live, int N, int pla
 
 template <bool AMN, bool BMN, class Epi>
 cudaError_t launch_matmul_cut(const Operand& a, const Operand& b, int M, int N, int K, Cut cut, bool f16,
-                              const typename Epi::Args& ea, cudaStream_t stream, bool dependent, const int* live_m, int plan_nk) {
+                              const typename Epi::Args& ea, cudaStream_t stream, bool dependent, const int* live_m, int plan_nk, int fold) {
     MatShape g = {};
+    g.fold = fold;
     g.M = M, g.N = N, g.K = K, g.batch = g.splits = cut.splits, g.live_m = live_m, g.plan_nk = plan_nk;
     return cut.pairs ? launch_matmul_cg<2, AMN, BMN, Epi>(a, b, g, f16, ea, stream, dependent)
                      : launch_matmul_cg<1, AMN, BMN, Epi>(a, b, g, f16, ea, stream, dependent);

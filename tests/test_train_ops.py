@@ -305,6 +305,19 @@ def test_linear_cross_entropy_strides(dtype, pad):
     check_ce(wide(h, pad)[:, 1:60], wide(w, pad)[:, 1:60], t, g)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("n,d,v,piece", [(1, 64, 500, 0), (2, 1000, 3000, 512), (5, 1856, 4086, 0), (17, 72, 9000, 0), (64, 256, 2000, 256)])
+def test_linear_cross_entropy_few_rows(n, d, v, piece, dtype):
+    # no error is averaged over many products here: both terms of the gradients of the logits are kept, and only the
+    # results' own roundings remain, 2^-8 (2^-11) / sqrt(3) of the norm in the mean at most
+    from paper_2108_03645_b200 import train
+    h, w, t, g = ce_inputs(n, d, v, dtype, 0.0, seed=n)
+    loss, lse, dh, dw = check_ce(h, w, t, g, piece=piece)
+    r = ce_reference(h, w, t, g)
+    for got, want in ((dh, r["dh"]), (dw, r["dw"])):
+        assert float((got.double() - want).norm() / want.norm()) <= 0.6 * U[dtype]
+
+
 def test_linear_cross_entropy_no_row_takes_part():
     from paper_2108_03645_b200 import train
     h, w, t, g = ce_inputs(150, 64, 300, BF16, 0.0)
