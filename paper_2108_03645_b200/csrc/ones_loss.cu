@@ -26,6 +26,7 @@ __device__ __forceinline__ float regain(int k) { return 1.f + (float)k * 9.31322
 // Softmax statistics of a tile of logits: each thread takes the maximum m and s = sum exp(l - m) of its row's columns
 // here, and the logit of the row's target if it meets it.
 struct EpiStats {
+    static constexpr int kWarps = 8;
     struct Args {
         const int64_t* target;
         float2* part;  // [slots][rows], one slot per half tile
@@ -33,10 +34,10 @@ struct EpiStats {
         int rows, vocab;
     };
     template <int W>
-    static __device__ __forceinline__ void tile(const Args& a, const MatShape& g, uint32_t acc, int row, int col,
-                                                const TileAt& at, int half, const Turn&) {
+    static __device__ __forceinline__ void tile(const Args& a, const MatShape& g, uint32_t acc, int row, int col, int limit,
+                                                const TileAt& at, int half, const Turn<kWarps>&) {
         const float up = regain(g.K), to2 = kLog2e * up;
-        const int end = min(a.vocab, col + g.width / 2);
+        const int end = min(a.vocab, limit);
         const int64_t t64 = row < a.rows ? a.target[row] : -1;
         const int t = t64 >= 0 && t64 < a.vocab ? (int)t64 : -1;
         float m = -INFINITY, s = 0.f;
@@ -89,6 +90,7 @@ struct RowInfo {
 
 // Gradient of a piece's logits, as 16 bits: (exp(l - lse) - [target]) * dloss * scale.
 struct EpiDlogits {
+    static constexpr int kWarps = 16;
     struct Args {
         const RowInfo* info;
         uint16_t* out;
@@ -97,8 +99,9 @@ struct EpiDlogits {
         bool f16, twice;        // twice: what the rounding left goes into a second row of ld / 2 values
     };
     template <int W>
-    static __device__ __forceinline__ void tile(const Args& a, const MatShape& shape, uint32_t acc, int row, int col,
-                                                const TileAt&, int, const Turn& turn) {
+    static __device__ __forceinline__ void tile(const Args& a, const MatShape& shape, uint32_t acc, int row, int col, int limit,
+                                                const TileAt&, int, const Turn<kWarps>& turn) {
+        constexpr int N = Turn<kWarps>::kHalves;
         const float to2 = kLog2e * regain(shape.K);
         const bool live = row < shape.M;
         RowInfo r = {-1, 0.f, 0.f, 0};
@@ -106,27 +109,27 @@ struct EpiDlogits {
         const int t = r.target - a.first;
         // the product with the hidden rows runs over whole stages of rows: those after the last one are zero
         const int rows = min(a.rows, (shape.M + kTileK - 1) / kTileK * kTileK);
-        const int end = min(a.cols, col + shape.width / 2);
+        const int end = min(a.cols, limit);
 #pragma unroll 1
-        for (int c = 0; c < W && col + c < end; c += 64) {
-            float v[64];
+        for (int c = 0; c < W && col + c < end; c += N) {
+            float v[N];
             tmem_load(acc + c, v);
 #pragma unroll
-            for (int i = 0; i < 64; i += 2) {  // rows behind the last one that takes part are zero: exp(0) * 0
+            for (int i = 0; i < N; i += 2) {  // rows behind the last one that takes part are zero: exp(0) * 0
                 const float2 x = split(fma2(pair(v[i], v[i + 1]), both(to2), both(r.shift)));
                 const float2 y = split(pair(exp2_fast(x.x), exp2_fast(x.y)) * both(r.g));
                 v[i] = y.x, v[i + 1] = y.y;
             }
             const unsigned at_i = (unsigned)(t - (col + c));
-            if (live && at_i < 64u) {
+            if (live && at_i < (unsigned)N) {
 #pragma unroll
-                for (int i = 0; i < 64; ++i)
+                for (int i = 0; i < N; ++i)
                     if (at_i == (unsigned)i) v[i] -= r.g;
             }
             turn.write16(v, a.f16, a.out, a.ld, row - turn.lane, col + c, rows, end, true);
             if (a.twice) {
 #pragma unroll
-                for (int i = 0; i < 64; ++i)
+                for (int i = 0; i < N; ++i)
                     v[i] -= a.f16 ? __half2float(__float2half_rn(v[i])) : __bfloat162float(__float2bfloat16_rn(v[i]));
                 turn.write16(v, a.f16, a.out + a.ld / 2, a.ld, row - turn.lane, col + c, rows, end, true);
             }
@@ -149,6 +152,7 @@ __device__ __forceinline__ void store_grad4(uint16_t* out, float4 f, int left, b
 // Sum over the pieces: the product is added to (first piece: put into) 32-bit sums; the last piece rounds them into the
 // caller's rows, unless the sums come in several parts (k_ce_rows joins those).
 struct EpiSum {
+    static constexpr int kWarps = 8;
     struct Args {
         float* sum;  // [parts][rows][ld_sum]
         int64_t ld_sum;
@@ -160,11 +164,11 @@ struct EpiSum {
         bool first, last, f16, wide;
     };
     template <int W>
-    static __device__ __forceinline__ void tile(const Args& a, const MatShape& shape, uint32_t acc, int row, int col,
-                                                const TileAt& at, int, const Turn& turn) {
+    static __device__ __forceinline__ void tile(const Args& a, const MatShape& shape, uint32_t acc, int row, int col, int limit,
+                                                const TileAt& at, int, const Turn<kWarps>& turn) {
         const float unscale = a.last ? 1.f / *a.scale : 1.f;  // a power of two
-        const int r0 = row - turn.lane + turn.lane / 8, k = turn.lane & 7;
-        const int end = min(a.cols, col + shape.width / 2);
+        const int r0 = row - turn.lane + turn.row_of(0), k = turn.chunk_of();
+        const int end = min(a.cols, limit);
 #pragma unroll 1
         for (int c = 0; c < W && col + c < end; c += 32) {
             const int at_col = col + c + 4 * k, left = end - at_col;
@@ -180,7 +184,7 @@ struct EpiSum {
             turn.put32(v);
             uint4 q[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) q[i] = turn.chunk(4 * i + turn.lane / 8, k);
+            for (int i = 0; i < 8; ++i) q[i] = turn.chunk(turn.row_of(i), k);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 float4 f = make_float4(__uint_as_float(q[i].x), __uint_as_float(q[i].y), __uint_as_float(q[i].z), __uint_as_float(q[i].w));
@@ -199,6 +203,7 @@ struct EpiSum {
 
 // A piece's rows of dweight, complete: scaled back and rounded.
 struct EpiGrad {
+    static constexpr int kWarps = 16;
     struct Args {
         void* out;
         int64_t ld;
@@ -207,26 +212,26 @@ struct EpiGrad {
         bool f32, f16, wide;
     };
     template <int W>
-    static __device__ __forceinline__ void tile(const Args& a, const MatShape& shape, uint32_t acc, int row, int col,
-                                                const TileAt&, int, const Turn& turn) {
+    static __device__ __forceinline__ void tile(const Args& a, const MatShape& shape, uint32_t acc, int row, int col, int limit,
+                                                const TileAt&, int, const Turn<kWarps>& turn) {
         const float unscale = 1.f / *a.scale;
         const bool none = shape.K == 0;  // no row takes part: nothing was multiplied
         const int row0 = row - turn.lane;
-        const int end = min(a.cols, col + shape.width / 2);
+        const int end = min(a.cols, limit);
+        constexpr int N = Turn<kWarps>::kHalves;
 #pragma unroll 1
-        for (int c = 0; c < W && col + c < end; c += 64) {
-            float v[64];
+        for (int c = 0; c < W && col + c < end; c += N) {
+            float v[N];
             tmem_load(acc + c, v);
 #pragma unroll
-            for (int i = 0; i < 64; ++i) v[i] = none ? 0.f : v[i] * unscale;
+            for (int i = 0; i < N; ++i) v[i] = none ? 0.f : v[i] * unscale;
             if (a.f32) {
-                float u[32];
+                float u[N / 2];
 #pragma unroll
-                for (int h = 0; h < 64; h += 32) {
+                for (int h = 0; h < N; h += N / 2) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) u[i] = v[h + i];
-                    turn.put32(u);
-                    turn.store32(static_cast<float*>(a.out), a.ld, row0, col + c + h, a.rows, end, a.wide);
+                    for (int i = 0; i < N / 2; ++i) u[i] = v[h + i];
+                    turn.write32(u, static_cast<float*>(a.out), a.ld, row0, col + c + h, a.rows, end, a.wide);
                 }
             } else {
                 turn.write16(v, a.f16, static_cast<uint16_t*>(a.out), a.ld, row0, col + c, a.rows, end, a.wide);
@@ -382,27 +387,27 @@ __global__ void __launch_bounds__(256) k_ce_gather(const uint16_t* hidden, int64
     }
 }
 
-// Joins the parts of the sums over the vocabulary, in order, and rounds them into the caller's rows. A warp takes a row.
+// Joins the parts of the sums over the vocabulary, in order, and rounds them into the caller's rows. A warp takes 128
+// columns of a row, so that few rows fill the SMs too.
 __global__ void __launch_bounds__(256) k_ce_rows(const float* sum, Cut cut, int plan_nk, int64_t ld_sum, int rows, int cols, const Header* head,
                                                  const RowInfo* info, uint16_t* out, int64_t ld_out, bool f16, bool wide) {
     wait_for_predecessor();
-    const int lane = threadIdx.x % 32;
+    const int groups = (cols + 127) / 128;
     const float unscale = 1.f / head->scale;
-    const int64_t part = (int64_t)rows * ld_sum;
+    const int64_t part = (int64_t)rows * ld_sum, items = (int64_t)head->live * groups;
     const int parts = parts_of(cut, head->live, cols, plan_nk);
-    for (int i = blockIdx.x * 8 + threadIdx.x / 32; i < head->live; i += gridDim.x * 8) {
-        const float* p = sum + (int64_t)i * ld_sum;
-        uint16_t* to = out + (int64_t)info[i].row * ld_out;
-        for (int c = lane * 4; c < cols; c += 128) {
-            float4 f = *reinterpret_cast<const float4*>(p + c);
-#pragma unroll 4
-            for (int k = 1; k < parts; ++k) {
-                const float4 q = *reinterpret_cast<const float4*>(p + k * part + c);
-                f.x += q.x, f.y += q.y, f.z += q.z, f.w += q.w;
-            }
-            f.x *= unscale, f.y *= unscale, f.z *= unscale, f.w *= unscale;
-            store_grad4(to + c, f, cols - c, f16, wide);
+    for (int64_t w = blockIdx.x * 8 + threadIdx.x / 32; w < items; w += gridDim.x * 8) {
+        const int i = (int)(w / groups), c = (int)(w % groups) * 128 + threadIdx.x % 32 * 4;
+        if (c >= cols) continue;
+        const float* p = sum + (int64_t)i * ld_sum + c;
+        float4 f = *reinterpret_cast<const float4*>(p);
+#pragma unroll 8
+        for (int k = 1; k < parts; ++k) {
+            const float4 q = *reinterpret_cast<const float4*>(p + k * part);
+            f.x += q.x, f.y += q.y, f.z += q.z, f.w += q.w;
         }
+        f.x *= unscale, f.y *= unscale, f.z *= unscale, f.w *= unscale;
+        store_grad4(out + (int64_t)info[i].row * ld_out + c, f, cols - c, f16, wide);
     }
 }
 
@@ -588,8 +593,9 @@ int ones_linear_ce_backward(const float* d_dloss, const void* d_hidden, int64_t 
         err = launch_matmul<true, true, EpiGrad>({dl, L.piece, 0, true}, {hidden, L.ld_hidden, 0, true}, n, cols, rows * fold, 1, false, f16,
                                                  e3, stream, true, nullptr, &head->live, 0, fold);
     }
+    const int64_t join_blocks = ((int64_t)rows * ((cols + 127) / 128) + 7) / 8;
     if (err == cudaSuccess && L.cut.splits > 1)
-        err = launch_after(k_ce_rows, dim3(row_blocks), dim3(256), stream, static_cast<const float*>(sum), L.cut, plan_nk, L.ld_sum, rows, cols,
+        err = launch_after(k_ce_rows, dim3((unsigned)(join_blocks < 8 * kSms ? join_blocks : 8 * kSms)), dim3(256), stream, static_cast<const float*>(sum), L.cut, plan_nk, L.ld_sum, rows, cols,
                            static_cast<const Header*>(head), static_cast<const RowInfo*>(info), dh, lddh, f16, wide_h);
     return err == cudaSuccess ? ONES_OK : ONES_ERR_CUDA;
 }

@@ -26,10 +26,13 @@ constexpr int kTileK = 64;       // values along K per stage: one 128-byte swizz
 constexpr int kStages = 6;
 constexpr int kHalf = 128 * kTileK * 2;  // bytes of one operand's box(es) per stage and CTA
 constexpr int kStageBytes = 2 * kHalf;
-constexpr int kEpiWarps = 8;
-constexpr int kMatThreads = 128 + 32 * kEpiWarps;
-constexpr int kEpiBytes = 32 * 128;  // what a warp of the epilogue has to turn rows round: 32 rows of 128 bytes
-constexpr int kMatSmem = kStages * kStageBytes + kEpiWarps * kEpiBytes + 1024;
+// Warps of the epilogue: 16 where a tile's way out is what short products wait for (the gradients of the cross entropy:
+// 32001 x 777 out of K = 1023 in 98 us with 8 and 86 us with 16, 32000 x 1024 out of K = 10 in 36 and 25 us), 8 where
+// each thread needs more registers or little leaves.
+template <int WARPS>
+constexpr int kMatThreads = 128 + 32 * WARPS;
+constexpr int kTurnBytes = 32 * 1024;  // what they have between them to turn rows round
+constexpr int kMatSmem = kStages * kStageBytes + kTurnBytes + 1024;
 
 // Set when a wait inside a kernel of this translation unit ran out of time.
 static __device__ unsigned g_wait_expired;
@@ -174,7 +177,7 @@ struct BenchShared {
     uint64_t full[kStages], empty[kStages], done[2], free_[2];
     uint32_t tmem;
 };
-template <int CG>
+template <int CG, int WARPS>
 __device__ __forceinline__ Bench set_up(BenchShared& s, uint8_t* smem_raw, int warp) {
     Bench w;
     w.base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -186,7 +189,7 @@ __device__ __forceinline__ Bench set_up(BenchShared& s, uint8_t* smem_raw, int w
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(w.done + 8 * i, 1);
-            bar_init(w.free_ + 8 * i, kEpiWarps * CG);
+            bar_init(w.free_ + 8 * i, WARPS * CG);
         }
         bar_init_done();
     }
@@ -223,81 +226,89 @@ struct Half16 {  // two 16-bit values of the run-time type, in one word
     }
 };
 
-// A thread has 128 bytes of one row; stored like that, a warp's store would touch 32 rows at once. They go through
-// shared memory instead, the 16-byte chunks of a row permuted by the row so that neither side meets a bank twice, and
-// leave with 8 lanes on one row.
+// A thread has one row's values; stored like that, a warp's store would touch 32 rows at once. They go through shared
+// memory instead, 64 (16 warps) or 128 bytes (8 warps) of a row at a time, the 16-byte chunks of a row permuted by the row
+// so that neither side meets a bank twice, and leave with 4 or 8 lanes on one row.
+template <int WARPS>
 struct Turn {
-    uint8_t* at;  // 32 rows of 128 bytes, this warp's own
+    static constexpr int kBytes = kTurnBytes / WARPS / 32;                   // of a row
+    static constexpr int kHalves = kBytes / 2, kWords = kBytes / 4;          // values of 16 and of 32 bits in them
+    static constexpr int kChunks = kBytes / 16, kRowsAtOnce = 32 / kChunks;  // a warp's 16-byte accesses cover so many rows
+    uint8_t* at;  // this warp's own 32 rows
     int lane;
 
-    __device__ __forceinline__ uint4& chunk(int row, int c) const {
-        return *reinterpret_cast<uint4*>(at + row * 128 + ((c ^ (row & 7)) << 4));
-    }
-    __device__ __forceinline__ void put16(const float (&v)[64], bool f16) const {
+    static __device__ __forceinline__ int place(int row, int c) { return kChunks == 8 ? c ^ (row & 7) : c ^ (row >> 1 & 3); }
+    __device__ __forceinline__ uint4& chunk(int row, int c) const { return *reinterpret_cast<uint4*>(at + row * kBytes + (place(row, c) << 4)); }
+    // the row and chunk of this lane's i-th access, of kChunks, to all 32 rows
+    __device__ __forceinline__ int row_of(int i) const { return kRowsAtOnce * i + lane / kChunks; }
+    __device__ __forceinline__ int chunk_of() const { return lane % kChunks; }
+
+    __device__ __forceinline__ void put16(const float (&v)[kHalves], bool f16) const {
         __syncwarp();
 #pragma unroll
-        for (int c = 0; c < 8; ++c)
+        for (int c = 0; c < kChunks; ++c)
             chunk(lane, c) = make_uint4(Half16::pack(v[8 * c], v[8 * c + 1], f16), Half16::pack(v[8 * c + 2], v[8 * c + 3], f16),
                                         Half16::pack(v[8 * c + 4], v[8 * c + 5], f16), Half16::pack(v[8 * c + 6], v[8 * c + 7], f16));
         __syncwarp();
     }
-    __device__ __forceinline__ void put32(const float (&v)[32]) const {
+    __device__ __forceinline__ void put32(const float (&v)[kWords]) const {
         __syncwarp();
 #pragma unroll
-        for (int c = 0; c < 8; ++c)
+        for (int c = 0; c < kChunks; ++c)
             chunk(lane, c) = make_uint4(__float_as_uint(v[4 * c]), __float_as_uint(v[4 * c + 1]), __float_as_uint(v[4 * c + 2]),
                                         __float_as_uint(v[4 * c + 3]));
         __syncwarp();
     }
-    // One 16-bit / 32-bit value of what was put.
+    // A 16-bit or 32-bit value of what was put.
     __device__ __forceinline__ uint16_t half_at(int row, int c) const {
-        return *reinterpret_cast<const uint16_t*>(at + row * 128 + (((c >> 3) ^ (row & 7)) << 4) + (c & 7) * 2);
+        return *reinterpret_cast<const uint16_t*>(at + row * kBytes + (place(row, c >> 3) << 4) + (c & 7) * 2);
     }
-    __device__ __forceinline__ float word_at(int row, int c) const {
-        return *reinterpret_cast<const float*>(at + row * 128 + (((c >> 2) ^ (row & 7)) << 4) + (c & 3) * 4);
+    __device__ __forceinline__ uint32_t word_at(int row, int c) const {
+        return *reinterpret_cast<const uint32_t*>(at + row * kBytes + (place(row, c >> 2) << 4) + (c & 3) * 4);
     }
 
-    // The calling thread's 64 values as 16 bits, and with them the warp's 32 rows from row0, into columns from `col` of
+    // The calling thread's values as 16 bits, and with them the warp's 32 rows from row0, into columns from `col` of
     // `out` (row 0's first value), as far as they lie inside rows x cols. wide: rows start on 16-byte boundaries.
-    __device__ __forceinline__ void write16(float (&v)[64], bool f16, uint16_t* out, int64_t ld, int row0, int col, int rows, int cols,
+    // What is written is read first, all of it or of eight rows, since the compiler cannot tell the two memories apart.
+    __device__ __forceinline__ void write16(float (&v)[kHalves], bool f16, uint16_t* out, int64_t ld, int row0, int col, int rows, int cols,
                                             bool wide) const {
         if (wide) {
             put16(v, f16);
-            const int c = lane & 7, left = cols - (col + 8 * c);
-            uint16_t* p = out + (int64_t)(row0 + lane / 8) * ld + col + 8 * c;
-            uint4 q[8];
+            const int c = chunk_of(), left = cols - (col + 8 * c);
+            uint16_t* p = out + (int64_t)(row0 + row_of(0)) * ld + col + 8 * c;
+            uint4 q[kChunks];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) q[i] = chunk(4 * i + lane / 8, c);
+            for (int i = 0; i < kChunks; ++i) q[i] = chunk(row_of(i), c);
 #pragma unroll
-            for (int i = 0; i < 8; ++i, p += 4 * ld) {
-                const int r = 4 * i + lane / 8;
-                if (row0 + r >= rows || left <= 0) continue;
+            for (int i = 0; i < kChunks; ++i, p += kRowsAtOnce * ld) {
+                if (row0 + row_of(i) >= rows || left <= 0) continue;
                 if (left >= 8) {
                     *reinterpret_cast<uint4*>(p) = q[i];
                 } else {
-                    for (int j = 0; j < left; ++j) p[j] = half_at(r, 8 * c + j);
+                    for (int j = 0; j < left; ++j) p[j] = half_at(row_of(i), 8 * c + j);
                 }
             }
         } else {
             // Two values at a time: a row that starts on an odd 2-byte place is put one value further to the left, so that
             // its pairs lie on 4-byte boundaries on both sides; its first value goes by itself.
-            const int n = min(32, rows - row0), width = min(64, cols - col);
+            constexpr int kLanes = kWords, kStep = 32 / kLanes;  // lanes on a row, rows at once
+            const int n = min(32, rows - row0), width = min(kHalves, cols - col);
             uint16_t* p = out + (int64_t)row0 * ld + col;
             const bool odd = (reinterpret_cast<uintptr_t>(p + lane * ld) >> 1) & 1;
             if (odd && lane < n) p[lane * ld] = (uint16_t)Half16::pack(v[0], 0.f, f16);
 #pragma unroll
-            for (int i = 0; i < 63; ++i) v[i] = odd ? v[i + 1] : v[i];
+            for (int i = 0; i < kHalves - 1; ++i) v[i] = odd ? v[i + 1] : v[i];
             put16(v, f16);
-            // Eight rows are read before they are written, since the compiler cannot tell the two memories apart.
+            p += lane / kLanes * ld;
 #pragma unroll 1
-            for (int r = 0; r < n; r += 8) {
+            for (int r = lane / kLanes; r - lane / kLanes < n; r += 8 * kStep) {
                 uint32_t q[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) q[j] = *reinterpret_cast<const uint32_t*>(at + (r + j) * 128 + (((lane >> 2) ^ ((r + j) & 7)) << 4) + (lane & 3) * 4);
+                for (int j = 0; j < 8; ++j) q[j] = word_at((r + j * kStep) & 31, lane % kLanes);
 #pragma unroll
-                for (int j = 0; j < 8; ++j, p += ld) {
-                    if (r + j >= n) break;
-                    const int c = 2 * lane + ((int)(reinterpret_cast<uintptr_t>(p) >> 1) & 1);
+                for (int j = 0; j < 8; ++j, p += kStep * ld) {
+                    if (r + j * kStep >= n) continue;
+                    const int c = 2 * (lane % kLanes) + ((int)(reinterpret_cast<uintptr_t>(p) >> 1) & 1);
                     if (c + 1 < width)
                         *reinterpret_cast<uint32_t*>(p + c) = q[j];
                     else if (c < width)
@@ -306,42 +317,44 @@ struct Turn {
             }
         }
     }
-    // The same for 32 x 32-bit columns that have been put.
-    __device__ __forceinline__ void store32(float* out, int64_t ld, int row0, int col, int rows, int cols, bool wide) const {
+    // The same as 32 bits.
+    __device__ __forceinline__ void write32(const float (&v)[kWords], float* out, int64_t ld, int row0, int col, int rows, int cols, bool wide) const {
+        put32(v);
         if (wide) {
-            const int c = lane & 7, left = cols - (col + 4 * c);
-            float* p = out + (int64_t)(row0 + lane / 8) * ld + col + 4 * c;
-            uint4 q[8];
+            const int c = chunk_of(), left = cols - (col + 4 * c);
+            float* p = out + (int64_t)(row0 + row_of(0)) * ld + col + 4 * c;
+            uint4 q[kChunks];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) q[i] = chunk(4 * i + lane / 8, c);
+            for (int i = 0; i < kChunks; ++i) q[i] = chunk(row_of(i), c);
 #pragma unroll
-            for (int i = 0; i < 8; ++i, p += 4 * ld) {
-                const int r = 4 * i + lane / 8;
-                if (row0 + r >= rows || left <= 0) continue;
+            for (int i = 0; i < kChunks; ++i, p += kRowsAtOnce * ld) {
+                if (row0 + row_of(i) >= rows || left <= 0) continue;
                 if (left >= 4) {
                     *reinterpret_cast<uint4*>(p) = q[i];
                 } else {
-                    for (int j = 0; j < left; ++j) p[j] = word_at(r, 4 * c + j);
+                    for (int j = 0; j < left; ++j) p[j] = __uint_as_float(word_at(row_of(i), 4 * c + j));
                 }
             }
         } else {
-            const int n = min(32, rows - row0);
-            float* p = out + (int64_t)row0 * ld + col + lane;
+            constexpr int kStep = 32 / kWords;
+            const int n = min(32, rows - row0), c = lane % kWords;
+            float* p = out + (int64_t)(row0 + lane / kWords) * ld + col + c;
 #pragma unroll 1
-            for (int r = 0; r < n; r += 8) {
-                float v[8];
+            for (int r = lane / kWords; r - lane / kWords < n; r += 8 * kStep) {
+                uint32_t q[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = word_at(r + j, lane);
+                for (int j = 0; j < 8; ++j) q[j] = word_at((r + j * kStep) & 31, c);
 #pragma unroll
-                for (int j = 0; j < 8; ++j, p += ld)
-                    if (r + j < n && col + lane < cols) *p = v[j];
+                for (int j = 0; j < 8; ++j, p += kStep * ld)
+                    if (r + j * kStep < n && col + c < cols) *p = __uint_as_float(q[j]);
             }
         }
     }
 };
 
-__device__ __forceinline__ Turn turn_of(uint8_t* smem_raw, uint32_t base, int warp, int lane) {
-    return {smem_raw + (base - smem_u32(smem_raw)) + kStages * kStageBytes + (warp - 4) * kEpiBytes, lane};
+template <int WARPS>
+__device__ __forceinline__ Turn<WARPS> turn_of(uint8_t* smem_raw, uint32_t base, int warp, int lane) {
+    return {smem_raw + (base - smem_u32(smem_raw)) + kStages * kStageBytes + (warp - 4) * (kTurnBytes / WARPS), lane};
 }
 
 // The warp has read its part of an accumulator.
@@ -366,10 +379,11 @@ __host__ __device__ inline int parts_of_k(int most, int tiles, int slots, int nk
 }
 
 template <int CG, bool AMN, bool BMN, class Epi>
-__global__ void __launch_bounds__(kMatThreads, 1)
+__global__ void __launch_bounds__(kMatThreads<Epi::kWarps>, 1)
     k_matmul(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MatShape shape,
              const typename Epi::Args ea) {
-    constexpr int BN = 128 * CG;  // columns of a tile
+    constexpr int BN = 128 * CG, kWarps = Epi::kWarps;  // columns of a tile
+    constexpr int W = BN / (kWarps / 4);                // and of a warp's part of it, at most
     extern __shared__ uint8_t smem_raw[];
     __shared__ BenchShared shared;
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
@@ -378,7 +392,7 @@ __global__ void __launch_bounds__(kMatThreads, 1)
         tma_prefetch(&map_a);
         tma_prefetch(&map_b);
     }
-    const Bench w = set_up<CG>(shared, smem_raw, warp);
+    const Bench w = set_up<CG, kWarps>(shared, smem_raw, warp);
 
     wait_for_predecessor();
     let_successor_start();
@@ -419,8 +433,9 @@ __global__ void __launch_bounds__(kMatThreads, 1)
         }
     } else if (warp >= 4) {
         // hand the accumulators on
-        const int quad = warp % 4, half = (warp - 4) / 4;
-        const Turn turn = turn_of(smem_raw, w.base, warp, lane);
+        const int quad = warp % 4, part = (warp - 4) / 4;
+        const auto turn = turn_of<kWarps>(smem_raw, w.base, warp, lane);
+        const int share = kWarps == 8 ? g.width / 2 : W;  // of a tile's columns (16 bytes of 16 bits at least)
         const uint32_t free_at = CG == 2 ? map_to_rank(w.free_, 0) : w.free_;
         int acc = 0;
         uint32_t aph = 0;
@@ -431,8 +446,8 @@ __global__ void __launch_bounds__(kMatThreads, 1)
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
             mma_fence_after();
             const int row = at.m * 128 * CG + (int)rank * 128 + quad * 32 + lane;
-            const int hw = g.width / 2, col = at.n * g.width + half * hw;
-            Epi::template tile<BN / 2>(ea, g, w.tmem + acc * BN + half * hw + ((uint32_t)quad << 21), row, col, at, half, turn);
+            const int col = at.n * g.width + part * share, end = min(col + share, (at.n + 1) * g.width);
+            Epi::template tile<W>(ea, g, w.tmem + acc * BN + part * share + ((uint32_t)quad << 21), row, col, end, at, part, turn);
             free_accumulator<CG>(free_at + 8 * acc, lane);
             if (++acc == 2) acc = 0, aph ^= 1;
         }
@@ -497,7 +512,7 @@ cudaError_t launch_matmul_cg(const Operand& a, const Operand& b, MatShape g, boo
     if (err != cudaSuccess) return err;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((total < slots ? total : slots) * CG));
-    cfg.blockDim = dim3(kMatThreads);
+    cfg.blockDim = dim3(kMatThreads<Epi::kWarps>);
     cfg.dynamicSmemBytes = kMatSmem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];

@@ -132,6 +132,11 @@ __global__ void __launch_bounds__(kNormThreads) k_ns_cast(Source g, const double
 // The symmetric products have only their blocks on and above the diagonal computed and stored. The products that read
 // them take what lies below from above, as an operand with its rows contiguous (Lie::upper).
 
+// Eight warps: with 16, rounds of long products gain (2048 x 8192: 586 -> 571 us), but the many short ones lose more
+// to the larger barrier and the smaller register share (8192 x 300: 179 -> 195 us).
+constexpr int kStepWarps = 8;
+using StepTurn = Turn<kStepWarps>;
+
 // A = factor * X X^T, and its diagonal in 32 bits.
 struct EpiGram {
     struct Args {
@@ -145,15 +150,14 @@ struct EpiGram {
         int64_t ld_part;
     };
     template <int W, bool CUT>
-    static __device__ __forceinline__ void tile(const Args& a, uint32_t acc, int row, int col, const TileAt& at, const Turn& turn) {
+    static __device__ __forceinline__ void tile(const Args& a, uint32_t acc, int row, int col, const TileAt& at, const StepTurn& turn) {
         if constexpr (CUT) {
             float* out = a.part + (int64_t)at.b * a.s * a.ld_part;
 #pragma unroll 1
             for (int c = 0; c < W && col + c < a.s; c += 32) {
                 float v[32];
                 tmem_load(acc + c, v);
-                turn.put32(v);
-                turn.store32(out, a.ld_part, row - turn.lane, col + c, a.s, a.s, true);
+                turn.write32(v, out, a.ld_part, row - turn.lane, col + c, a.s, a.s, true);
             }
             return;
         }
@@ -220,17 +224,17 @@ struct EpiPoly {
         float a, b, c;
     };
     // A's values of 64 columns, 8 lanes to a row, as the result leaves; asked for before they are needed.
-    static __device__ __forceinline__ void load(const Args& a, int row, int col, const TileAt& at, const Turn& turn, uint4 (&q)[8]) {
-        const int c = col + 8 * (turn.lane & 7);
+    static __device__ __forceinline__ void load(const Args& a, int row, int col, const TileAt& at, const StepTurn& turn, uint4 (&q)[8]) {
+        const int c = col + 8 * turn.chunk_of();
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int r = row - turn.lane + 4 * i + turn.lane / 8;  // rows of A are padded to whole 16 bytes
+            const int r = row - turn.lane + turn.row_of(i);  // rows of A are padded to whole 16 bytes
             q[i] = r < a.s && c < a.s ? __ldcg(reinterpret_cast<const uint4*>(a.gram + at.b * a.batch_ld + (int64_t)r * a.ld + c))
                                       : make_uint4(0, 0, 0, 0);
         }
     }
     template <int W>
-    static __device__ __forceinline__ void tile(const Args& a, uint32_t acc, int row, int col, const TileAt& at, const Turn& turn, uint4 (&q)[8],
+    static __device__ __forceinline__ void tile(const Args& a, uint32_t acc, int row, int col, const TileAt& at, const StepTurn& turn, uint4 (&q)[8],
                                                 float exact) {
         uint16_t* out = reinterpret_cast<uint16_t*>(a.out + at.b * a.batch_ld);
 #pragma unroll 1
@@ -239,7 +243,7 @@ struct EpiPoly {
             tmem_load(acc + c, v);
             __syncwarp();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) turn.chunk(4 * i + turn.lane / 8, turn.lane & 7) = q[i];
+            for (int i = 0; i < 8; ++i) turn.chunk(turn.row_of(i), turn.chunk_of()) = q[i];
             __syncwarp();
             if (c + 64 < W) load(a, row, col + c + 64, at, turn, q);
 #pragma unroll
@@ -280,7 +284,7 @@ struct EpiApply {
         bool f16, wide;
     };
     template <int W, bool TALL>
-    static __device__ __forceinline__ void tile(const Args& a, uint32_t acc, int row, int col, const TileAt& at, const Turn& turn, float own) {
+    static __device__ __forceinline__ void tile(const Args& a, uint32_t acc, int row, int col, const TileAt& at, const StepTurn& turn, float own) {
         const float* regain = a.regain + (int64_t)at.b * a.n;
         const float f = (a.first ? a.factor * a.first[at.b].x : a.factor) * own;
 #pragma unroll 1
@@ -352,7 +356,7 @@ __device__ __forceinline__ void operands(const StepsMaps& maps, bool tall, int w
 // polynomial from the right. Both as kernels of their own: code that is not run still costs (12 of 189 us for twelve of
 // 768 x 768).
 template <int CG, bool CUT, bool TALL>
-__global__ void __launch_bounds__(kMatThreads, 1) k_ns_steps(const __grid_constant__ StepsMaps maps, const StepsArgs p) {
+__global__ void __launch_bounds__(kMatThreads<kStepWarps>, 1) k_ns_steps(const __grid_constant__ StepsMaps maps, const StepsArgs p) {
     constexpr int BN = 128 * CG;
     extern __shared__ uint8_t smem_raw[];
     __shared__ BenchShared shared;
@@ -361,7 +365,7 @@ __global__ void __launch_bounds__(kMatThreads, 1) k_ns_steps(const __grid_consta
     __shared__ __align__(8) uint64_t s_round;  // tells the epilogue that the product before is complete: one poller a block
     const uint32_t round_bar = smem_u32(&s_round);
     if (threadIdx.x == 0) bar_init(round_bar, 1);
-    const Bench w = set_up<CG>(shared, smem_raw, warp);
+    const Bench w = set_up<CG, kStepWarps>(shared, smem_raw, warp);
     wait_for_predecessor();
 
     const int first = blockIdx.x / CG, step = gridDim.x / CG;
@@ -428,7 +432,7 @@ __global__ void __launch_bounds__(kMatThreads, 1) k_ns_steps(const __grid_consta
         }
     } else if (warp >= 4) {
         const int quad = warp % 4, half = (warp - 4) / 4;
-        const Turn turn = turn_of(smem_raw, w.base, warp, lane);
+        const StepTurn turn = turn_of<kStepWarps>(smem_raw, w.base, warp, lane);
         const uint32_t free_at = CG == 2 ? map_to_rank(w.free_, 0) : w.free_;
         int acc = 0;
         uint32_t aph = 0;
@@ -438,7 +442,7 @@ __global__ void __launch_bounds__(kMatThreads, 1) k_ns_steps(const __grid_consta
             const float2* start = k == 0 ? p.factor : nullptr;
             EpiGram::Args eg = {p.gram, p.diag, p.lds, p.ss, p.s, 1.f / (p.unit * p.unit), start, p.part, p.ld_part};
             if (CUT && ok && which == 3)
-                for (int i = blockIdx.x * kEpiWarps + warp - 4; i < p.count * p.s; i += gridDim.x * kEpiWarps)
+                for (int i = blockIdx.x * kStepWarps + warp - 4; i < p.count * p.s; i += gridDim.x * kStepWarps)
                     EpiGram::join(eg, p.parts, p.part_stride, i / p.s, i % p.s, BN, lane);
             for (int t = first; ok && t < total; t += step) {
                 int k0, nk, cut;
@@ -473,7 +477,7 @@ __global__ void __launch_bounds__(kMatThreads, 1) k_ns_steps(const __grid_consta
                 free_accumulator<CG>(free_at + 8 * acc, lane);
                 if (++acc == 2) acc = 0, aph ^= 1;
             }
-            asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpiWarps) : "memory");
+            asm volatile("bar.sync 1, %0;" ::"n"(32 * kStepWarps) : "memory");
             if (warp == 4 && lane == 0) arrive_all(p.counter);
         }
     }
@@ -859,7 +863,7 @@ cudaError_t launch_steps(const StepsMaps& maps, const StepsArgs& p, cudaStream_t
     cudaError_t err = allow_smem(kernel, kMatSmem, ready);
     if (err != cudaSuccess) return err;
     cudaLaunchConfig_t cfg = {};
-    cfg.blockDim = dim3(kMatThreads);
+    cfg.blockDim = dim3(kMatThreads<kStepWarps>);
     cfg.dynamicSmemBytes = kMatSmem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
