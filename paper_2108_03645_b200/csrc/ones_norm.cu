@@ -158,8 +158,8 @@ struct NormIn {
     bool w32;
 };
 
-// Rows that do not start on 16-byte boundaries: a row is held in registers by TPR threads, read once a value at a time,
-// the mean first and the squares of the differences from it second, so that no cancellation spoils the variance.
+// Short rows that do not start on 16-byte boundaries: a row is held in registers by TPR threads, read once a value at a
+// time, the mean first and the squares of the differences from it second, so that no cancellation spoils the variance.
 template <class T, int TPR, int N>
 __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR)
     k_norm(const NormIn a, void* y_, int64_t ldy, float* mean_out, float* rstd_out) {
@@ -326,6 +326,269 @@ __global__ void __launch_bounds__(kRingThreads, 1)
     if (bad) let_copies_end();
 }
 
+// ---- rows on other boundaries ----
+// The same ring, filled with whole 16-byte blocks around a row: it starts up to 14 bytes into its place. From there a
+// warp reads 32-bit words, one after the other over its lanes; where a 16-bit row starts on an odd half word, a pair of
+// columns is shifted together out of two. The result leaves the same way: a word is put together from the pairs of two
+// lanes. A warp has 64 * NU columns in a row, so that only their ends are written as halves.
+// A row whose first or last block reaches over the ends of the tensor is not copied: its values are read one by one.
+template <class T>
+struct Unit {  // two columns of a row: neighbours for 16 bits, 32 apart for 32 bits
+    static constexpr bool k16 = sizeof(T) == 2;
+    static constexpr int kWords = k16 ? 1 : 2, kNext = k16 ? 1 : 32;
+    uint32_t raw[kWords];
+    static __device__ __forceinline__ int column(int span, int u, int lane) { return span + 64 * u + (k16 ? 2 * lane : lane); }
+    __device__ __forceinline__ Pair get() const {
+        if constexpr (!k16) {
+            return pair(__uint_as_float(raw[0]), __uint_as_float(raw[1]));
+        } else if constexpr (std::is_same<T, __half>::value) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(raw));
+            return pair(f.x, f.y);
+        } else {
+            return pair(__uint_as_float(raw[0] << 16), __uint_as_float(raw[0] & 0xFFFF0000u));
+        }
+    }
+};
+
+// Rows of a tensor [rows][cols], `ld` values apart, as they go through a ring.
+template <class T>
+struct OddRows {
+    using U = Unit<T>;
+    const T* p;
+    int64_t ld;
+    int head, tail;  // the rows from head up to tail are copied
+    __device__ __forceinline__ OddRows(const void* base, int64_t ld_, int rows, int cols) : p(static_cast<const T*>(base)), ld(ld_) {
+        // rows that begin in a block before `base`'s end, or end in the block in which the tensor ends
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p), end = reinterpret_cast<uintptr_t>(p + (rows - 1) * ld + cols);
+        const int step = (int)(ld < 16 ? ld : 16) * (int)sizeof(T);
+        head = ((int)(-at & 15) + step - 1) / step;
+        tail = rows - ((int)(end & 15) + step - 1) / step;
+    }
+    __device__ __forceinline__ bool copied(int r) const { return r >= head && r < tail; }
+    // where row r starts in its first block
+    __device__ __forceinline__ uint32_t offset(int r) const {
+        return ((uint32_t)reinterpret_cast<uintptr_t>(p) + (uint32_t)r * (uint32_t)ld * (uint32_t)sizeof(T)) & 15;
+    }
+    // bytes of the blocks around row r
+    __device__ __forceinline__ uint32_t bytes(int r, int cols) const {
+        return copied(r) ? (offset(r) + cols * (uint32_t)sizeof(T) + 15) & ~15u : 0;
+    }
+    __device__ __forceinline__ const void* blocks(int r) const { return reinterpret_cast<const uint8_t*>(p + r * ld) - offset(r); }
+
+    // The calling thread's columns of row r, out of its place in the ring; zeros behind the last column.
+    template <int NU>
+    __device__ __forceinline__ void read(int r, const uint8_t* place, int span, int lane, int cols, U (&q)[NU]) const {
+        if (!copied(r)) {
+            const T* x = p + r * ld;
+#pragma unroll
+            for (int u = 0; u < NU; ++u) {
+                const int c = U::column(span, u, lane);
+                T v[2] = {from_f<T>(0.f), from_f<T>(0.f)};
+                if (c < cols) v[0] = x[c];
+                if (c + U::kNext < cols) v[1] = x[c + U::kNext];
+                if constexpr (U::k16)
+                    q[u].raw[0] = (uint32_t)*reinterpret_cast<const uint16_t*>(v) | (uint32_t)*reinterpret_cast<const uint16_t*>(v + 1) << 16;
+                else
+                    q[u].raw[0] = *reinterpret_cast<const uint32_t*>(v), q[u].raw[1] = *reinterpret_cast<const uint32_t*>(v + 1);
+            }
+            return;
+        }
+        const uint32_t off = offset(r);
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(place + (off & ~3u)) + U::column(span, 0, lane) * sizeof(T) / 4;
+        if (span + 64 * NU <= cols) {
+#pragma unroll
+            for (int u = 0; u < NU; ++u) {
+                q[u].raw[0] = w[(U::k16 ? 32 : 64) * u];
+                if constexpr (!U::k16) q[u].raw[1] = w[64 * u + 32];
+            }
+            if constexpr (U::k16) {
+                if (off & 2) {
+#pragma unroll
+                    for (int u = 0; u < NU; ++u) q[u].raw[0] = __funnelshift_r(q[u].raw[0], w[32 * u + 1], 16);
+                }
+            }
+            return;
+        }
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+            const int c = U::column(span, u, lane);
+            if constexpr (U::k16) {
+                uint32_t v = c < cols ? w[32 * u] : 0;
+                if (off & 2) v = __funnelshift_r(v, c + 1 < cols ? w[32 * u + 1] : 0, 16);
+                q[u].raw[0] = c + 1 < cols ? v : v & 0xFFFFu;
+            } else {
+                q[u].raw[0] = c < cols ? w[64 * u] : 0;
+                q[u].raw[1] = c + 32 < cols ? w[64 * u + 32] : 0;
+            }
+        }
+    }
+};
+
+// Writes a warp's columns of a row: f(u) is the u-th pair. Called by whole warps.
+template <class T, int NU, class F>
+__device__ __forceinline__ void write_units(T* y, int span, int lane, int cols, F f) {
+    using U = Unit<T>;
+    const bool whole = span + 64 * NU <= cols;
+    y += U::column(span, 0, lane);
+    cols -= U::column(span, 0, lane);
+    if constexpr (!U::k16) {
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+            const float2 v = split(f(u));
+            if (whole || 64 * u < cols) y[64 * u] = v.x;
+            if (whole || 64 * u + 32 < cols) y[64 * u + 32] = v.y;
+        }
+    } else {
+        uint16_t* half = reinterpret_cast<uint16_t*>(y);
+        auto packed = [&](int u) {
+            const float2 v = split(f(u));
+            if constexpr (std::is_same<T, __half>::value) {
+                const __half2 h = __floats2half2_rn(v.x, v.y);
+                return *reinterpret_cast<const uint32_t*>(&h);
+            } else {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(v.x, v.y);
+                return *reinterpret_cast<const uint32_t*>(&h);
+            }
+        };
+        if (!(reinterpret_cast<uintptr_t>(y) & 2)) {
+#pragma unroll
+            for (int u = 0; u < NU; ++u) {
+                const uint32_t v = packed(u);
+                if (whole || 64 * u + 1 < cols)
+                    *reinterpret_cast<uint32_t*>(half + 64 * u) = v;
+                else if (64 * u < cols)
+                    half[64 * u] = (uint16_t)v;
+            }
+            return;
+        }
+        // an odd half word: the lane's word ends with its pair's first column and begins with the second of the lane
+        // before, or of lane 31 in the unit before
+        uint32_t carry = 0;
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+            const uint32_t v = packed(u), left = __shfl_sync(0xFFFFFFFFu, v, (lane + 31) & 31), before = lane ? left : carry;
+            carry = left;
+            if (u == 0 && lane == 0) {
+                if (0 < cols) half[0] = (uint16_t)v;
+            } else if (whole || 64 * u < cols) {
+                *reinterpret_cast<uint32_t*>(half + 64 * u - 1) = __funnelshift_r(before, v, 16);
+            } else if (64 * u == cols) {
+                half[64 * u - 1] = (uint16_t)(before >> 16);
+            }
+            if (u == NU - 1 && lane == 31 && 64 * u + 1 < cols) half[64 * u + 1] = (uint16_t)(v >> 16);
+        }
+    }
+}
+
+// weight or bias of a thread's columns
+template <class T, int NU>
+__device__ __forceinline__ void load_units(const void* p, bool f32, int span, int lane, int cols, float none, Pair (&out)[NU]) {
+    using U = Unit<T>;
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+        const int c = U::column(span, u, lane);
+        float v[2][1] = {{0.f}, {0.f}};
+        if (c < cols) load_param<T, 1>(p, f32, c, none, v[0]);
+        if (c + U::kNext < cols) load_param<T, 1>(p, f32, c + U::kNext, none, v[1]);
+        out[u] = pair(v[0][0], v[1][0]);
+    }
+}
+
+// Rows that a group takes together, as above: they share the latency of their sums.
+template <int NU>
+constexpr int kOddRows = NU <= 8 ? 2 : 1;
+constexpr int kBackOddUnits = 8, kBackOddRows = 8 * kNormSms;
+
+// Bytes of a row's place in a ring.
+inline uint32_t odd_place(int cols, int size) { return (uint32_t)((cols * size + 14 + 15) / 16 * 16); }
+
+template <class T, int TPR, int NU>
+__global__ void __launch_bounds__(kRingThreads, 1)
+    k_norm_odd(const NormIn a, void* y_, int64_t ldy, float* mean_out, float* rstd_out, int stages, uint32_t place) {
+    constexpr int kGroups = kRingThreads / TPR, R = kOddRows<NU>;
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ __align__(8) uint64_t s_full[kGroups * kMaxStages];
+    __shared__ float s[2][2][R * kRingThreads / 32];
+    const int group = threadIdx.x / TPR, t = threadIdx.x % TPR, lane = t % 32, span = t / 32 * (64 * NU);
+    const uint32_t full = smem_u32(s_full + group * kMaxStages);
+    uint8_t* mine = ring + (size_t)group * stages * R * place;
+    const int first = (blockIdx.x * kGroups + group) * R, step = gridDim.x * kGroups * R;
+    const OddRows<T> x(a.x, a.ldx, a.rows, a.cols);
+    auto fetch = [&](int64_t row, int st) {
+        uint32_t bytes[R], sum = 0;
+#pragma unroll
+        for (int r = 0; r < R; ++r) sum += bytes[r] = x.bytes((int)row + r, a.cols);
+        bar_expect(full + 8 * st, sum);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (bytes[r]) bulk_load(smem_u32(mine + (st * R + r) * place), x.blocks((int)row + r), bytes[r], full + 8 * st);
+    };
+    if (t == 0) {
+        for (int i = 0; i < stages; ++i) bar_init(full + 8 * i, 1);
+        bar_init_done();
+        for (int i = 0; i < stages && first + (int64_t)i * step < a.rows; ++i) fetch(first + (int64_t)i * step, i);
+    }
+    Pair w[NU], b[NU];
+    load_units<T, NU>(a.w, a.w32, span, lane, a.cols, 1.f, w);
+    load_units<T, NU>(a.b, a.w32, span, lane, a.cols, 0.f, b);
+    const bool whole = span + 64 * NU <= a.cols;
+    group_sync<TPR>(group);
+    const float inv = 1.f / a.cols;
+    int st = 0, turn = 0;
+    uint32_t ph = 0;
+    bool bad = false;
+    for (int64_t row = first; row < a.rows; row += step, turn ^= 1) {
+        const bool ok = bar_wait(full + 8 * st, ph, &g_wait_expired);
+        bad = bad || !ok;
+        Pair v[R][NU];
+        float sum[R], sq[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            sum[r] = 0.f;
+            if (R > 1 && row + r >= a.rows) continue;
+            Unit<T> q[NU];
+            x.read((int)row + r, mine + (st * R + r) * place, span, lane, a.cols, q);
+            Pair acc = both(0.f);
+#pragma unroll
+            for (int u = 0; u < NU; ++u) acc = acc + (v[r][u] = q[u].get());
+            sum[r] = total(acc);
+        }
+        row_sums<TPR, R>(sum, s[turn][0], group);
+        // everybody has read these rows: their place is free
+        if (t == 0 && ok && row + (int64_t)stages * step < a.rows) fetch(row + (int64_t)stages * step, st);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            sum[r] *= inv;
+            Pair acc = both(0.f);
+#pragma unroll
+            for (int u = 0; u < NU; ++u) {
+                v[r][u] = v[r][u] + both(-sum[r]);
+                if (!whole) {
+                    const int c = Unit<T>::column(span, u, lane);
+                    const float2 f = split(v[r][u]);
+                    v[r][u] = pair(c < a.cols ? f.x : 0.f, c + Unit<T>::kNext < a.cols ? f.y : 0.f);
+                }
+                acc = fma2(v[r][u], v[r][u], acc);
+            }
+            sq[r] = total(acc);
+        }
+        row_sums<TPR, R>(sq, s[turn][1], group);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (R > 1 && row + r >= a.rows) break;
+            const float rstd = inv_sqrt(fmaf(sq[r], inv, a.eps));
+            if (t == 0) {
+                if (mean_out) mean_out[row + r] = sum[r];
+                if (rstd_out) rstd_out[row + r] = rstd;
+            }
+            write_units<T, NU>(static_cast<T*>(y_) + (row + r) * ldy, span, lane, a.cols,
+                               [&](int u) { return fma2(v[r][u] * both(rstd), w[u], b[u]); });
+        }
+        if (++st == stages) st = 0, ph ^= 1;
+    }
+    if (bad) let_copies_end();
+}
+
 // Rows longer than the registers of a block hold: three passes, the second and third from the caches.
 constexpr int kLongThreads = 1024;
 template <class T>
@@ -368,13 +631,25 @@ struct NormBack {
 
 constexpr int kBackParts = 2 * 148;  // at most so many blocks, and parts of the sums over rows: two on every SM of a B200
 
+// The block's share of dweight and dbias out of its groups', [groups][2][cols] in shared memory, in their order.
+template <int kGroups>
+__device__ __forceinline__ void join_groups(const float* part, int cols, float* out) {
+    __syncthreads();
+    for (int c = threadIdx.x; c < 2 * cols; c += blockDim.x) {
+        float v = part[c];
+#pragma unroll
+        for (int k = 1; k < kGroups; ++k) v += part[(int64_t)k * 2 * cols + c];
+        out[c] = v;
+    }
+}
+
 // Each thread keeps the same columns for all rows of its block, and with them the block's share of dweight and dbias
 // in registers; the next row's dy and x are on their way while a row is summed and written.
 template <class T, int TPR, int NV, int V>
 __global__ void __launch_bounds__(TPR < 512 ? 512 : TPR) k_norm_back(const NormBack a) {
     constexpr int kThreads = TPR < 512 ? 512 : TPR, kGroups = kThreads / TPR;
     __shared__ float s[2][2 * kThreads / 32];
-    extern __shared__ float s_part[];  // [2][cols] when a block has several groups
+    extern __shared__ float s_part[];  // [groups][2][cols] when a block has several groups
     const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
     const float inv = 1.f / a.cols;
     float w[NV][V], dw[NV][V], db[NV][V];
@@ -444,35 +719,18 @@ __global__ void __launch_bounds__(TPR < 512 ? 512 : TPR) k_norm_back(const NormB
     }
     if (a.part) {
         float* out = a.part + (int64_t)blockIdx.x * 2 * a.cols;
-        if constexpr (kGroups > 1) {
-            for (int k = 0; k < kGroups; ++k) {
-                if (group == k) {
+        float* own = kGroups > 1 ? s_part + group * 2 * a.cols : out;
 #pragma unroll
-                    for (int i = 0; i < NV; ++i) {
-                        const int c = (t + i * TPR) * V;
-                        if (c >= a.cols) break;
+        for (int i = 0; i < NV; ++i) {
+            const int c = (t + i * TPR) * V;
+            if (c >= a.cols) break;
 #pragma unroll
-                        for (int j = 0; j < V; ++j) {
-                            s_part[c + j] = k ? s_part[c + j] + dw[i][j] : dw[i][j];
-                            s_part[a.cols + c + j] = k ? s_part[a.cols + c + j] + db[i][j] : db[i][j];
-                        }
-                    }
-                }
-                __syncthreads();
-            }
-            for (int c = threadIdx.x; c < 2 * a.cols; c += kThreads) out[c] = s_part[c];
-        } else {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int c = (t + i * TPR) * V;
-                if (c >= a.cols) break;
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    out[c + j] = dw[i][j];
-                    out[a.cols + c + j] = db[i][j];
-                }
+            for (int j = 0; j < V; ++j) {
+                own[c + j] = dw[i][j];
+                own[a.cols + c + j] = db[i][j];
             }
         }
+        if (kGroups > 1) join_groups<kGroups>(s_part, a.cols, out);
     }
     let_successor_start();
 }
@@ -603,30 +861,102 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_ring(const NormBa
     if (bad) let_copies_end();
     if (a.part) {
         float* out = a.part + (int64_t)blockIdx.x * 2 * a.cols;
-        float* s_part = kGroups > 1 ? reinterpret_cast<float*>(ring) : out;  // [2][cols]; the ring has done its work
+        float* own = kGroups > 1 ? reinterpret_cast<float*>(ring) + group * 2 * a.cols : out;  // the ring has done its work
         __syncthreads();
-        for (int k = 0; k < kGroups; ++k) {
-            if (group == k) {
 #pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    if (t + i * TPR >= cols16) break;
+        for (int i = 0; i < NV; ++i) {
+            if (t + i * TPR >= cols16) break;
 #pragma unroll
-                    for (int j = 0; j < P; ++j) {
-                        float2* p = reinterpret_cast<float2*>(s_part) + (t + i * TPR) * P + j;
-                        float2 u = split(dw[i][j]), v = split(db[i][j]);
-                        if (k) {
-                            const float2 pu = p[0], pv = p[a.cols / 2];
-                            u.x += pu.x, u.y += pu.y, v.x += pv.x, v.y += pv.y;
-                        }
-                        p[0] = u;
-                        p[a.cols / 2] = v;
-                    }
-                }
+            for (int j = 0; j < P; ++j) {
+                float2* p = reinterpret_cast<float2*>(own) + (t + i * TPR) * P + j;
+                p[0] = split(dw[i][j]);
+                p[a.cols / 2] = split(db[i][j]);
             }
-            __syncthreads();
         }
-        if (kGroups > 1)
-            for (int c = threadIdx.x; c < 2 * a.cols; c += kRingThreads) out[c] = s_part[c];
+        if (kGroups > 1) join_groups<kGroups>(reinterpret_cast<const float*>(ring), a.cols, out);
+    }
+    let_successor_start();
+}
+
+// The same for many 32-bit rows on other boundaries, as k_norm_odd.
+template <int TPR>
+__global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_odd(const NormBack a, int stages, uint32_t place) {
+    constexpr int kGroups = kRingThreads / TPR, NU = kBackOddUnits;
+    using T = float;
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ __align__(8) uint64_t s_full[kGroups * kMaxStages];
+    __shared__ float s[2][2 * kRingThreads / 32];
+    const int group = threadIdx.x / TPR, t = threadIdx.x % TPR, lane = t % 32, span = t / 32 * (64 * NU);
+    const uint32_t full = smem_u32(s_full + group * kMaxStages);
+    uint8_t* mine = ring + (size_t)group * stages * 2 * place;
+    const int first = blockIdx.x * kGroups + group, step = gridDim.x * kGroups;
+    const OddRows<T> x(a.x, a.ldx, a.rows, a.cols), dy(a.dy, a.lddy, a.rows, a.cols);
+    auto fetch = [&](int64_t row, int st) {
+        const uint32_t bx = x.bytes((int)row, a.cols), bd = dy.bytes((int)row, a.cols), at = smem_u32(mine + st * 2 * place);
+        bar_expect(full + 8 * st, bx + bd);
+        if (bx) bulk_load(at, x.blocks((int)row), bx, full + 8 * st);
+        if (bd) bulk_load(at + place, dy.blocks((int)row), bd, full + 8 * st);
+    };
+    if (t == 0) {
+        for (int i = 0; i < stages; ++i) bar_init(full + 8 * i, 1);
+        bar_init_done();
+        for (int i = 0; i < stages && first + (int64_t)i * step < a.rows; ++i) fetch(first + (int64_t)i * step, i);
+    }
+    Pair w[NU], dw[NU], db[NU];
+    load_units<T, NU>(a.w, a.w32, span, lane, a.cols, 1.f, w);
+#pragma unroll
+    for (int u = 0; u < NU; ++u) dw[u] = db[u] = both(0.f);
+    group_sync<TPR>(group);
+    const float inv = 1.f / a.cols;
+    int st = 0, turn = 0;
+    uint32_t ph = 0;
+    bool bad = false;
+    float nmean = 0.f, nrstd = 0.f;
+    auto statistics = [&](int64_t row) {
+        if (row < a.rows) nmean = a.mean[row], nrstd = a.rstd[row];
+    };
+    statistics(first);
+    for (int64_t row = first; row < a.rows; row += step, turn ^= 1) {
+        const float mean = nmean, rstd = nrstd;
+        statistics(row + step);
+        const bool ok = bar_wait(full + 8 * st, ph, &g_wait_expired);
+        bad = bad || !ok;
+        Unit<T> xq[NU], dq[NU];
+        x.read((int)row, mine + st * 2 * place, span, lane, a.cols, xq);
+        dy.read((int)row, mine + st * 2 * place + place, span, lane, a.cols, dq);
+        const Pair scale = both(rstd), minus = both(-mean);
+        Pair acc1 = both(0.f), acc2 = both(0.f);
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {  // behind the last column dy and the weight are zero
+            const Pair d = dq[u].get(), e = d * ((xq[u].get() + minus) * scale);  // e: dy * xh
+            db[u] = db[u] + d;
+            dw[u] = dw[u] + e;
+            acc1 = fma2(d, w[u], acc1);
+            acc2 = fma2(e, w[u], acc2);
+        }
+        float sum[2] = {total(acc1), total(acc2)};
+        row_sums<TPR, 2>(sum, s[turn], group);
+        // everybody has read this row: its place is free
+        if (t == 0 && ok && row + (int64_t)stages * step < a.rows) fetch(row + (int64_t)stages * step, st);
+        // dx = rstd * (dy * w - c1 - xh * c2)
+        const Pair c1 = both(-rstd * sum[0] * inv), c2 = both(-rstd * rstd * sum[1] * inv);
+        write_units<T, NU>(static_cast<T*>(a.dx) + row * a.lddx, span, lane, a.cols,
+                           [&](int u) { return fma2(xq[u].get() + minus, c2, fma2(dq[u].get() * w[u], scale, c1)); });
+        if (++st == stages) st = 0, ph ^= 1;
+    }
+    if (bad) let_copies_end();
+    if (a.part) {
+        float* out = a.part + (int64_t)blockIdx.x * 2 * a.cols;
+        float* own = kGroups > 1 ? reinterpret_cast<float*>(ring) + group * 2 * a.cols : out;  // the ring has done its work
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+            const float2 f = split(dw[u]), g = split(db[u]);
+            const int c = Unit<T>::column(span, u, lane), d = c + Unit<T>::kNext;
+            if (c < a.cols) own[c] = f.x, own[a.cols + c] = g.x;
+            if (d < a.cols) own[d] = f.y, own[a.cols + d] = g.y;
+        }
+        if (kGroups > 1) join_groups<kGroups>(reinterpret_cast<const float*>(ring), a.cols, out);
     }
     let_successor_start();
 }
@@ -729,6 +1059,20 @@ cudaError_t norm_ring(const NormIn& a, void* y, int64_t ldy, float* mean, float*
     return cudaGetLastError();
 }
 
+template <class T, int TPR, int NU>
+cudaError_t norm_odd(const NormIn& a, void* y, int64_t ldy, float* mean, float* rstd, cudaStream_t stream) {
+    constexpr int kGroups = kRingThreads / TPR, R = kOddRows<NU>;
+    const int need = (a.rows + kGroups * R - 1) / (kGroups * R), blocks = need < kNormSms ? need : kNormSms;
+    const uint32_t place = odd_place(a.cols, sizeof(T));
+    const int stages = ring_stages(kGroups, (size_t)place * R, kRingBytes);
+    auto kernel = k_norm_odd<T, TPR, NU>;
+    static std::atomic<uint64_t> ready{0};
+    cudaError_t err = allow_smem(kernel, kRingBytes, ready);
+    if (err != cudaSuccess) return err;
+    kernel<<<blocks, kRingThreads, (size_t)kGroups * stages * R * place, stream>>>(a, y, ldy, mean, rstd, stages, place);
+    return cudaGetLastError();
+}
+
 template <class T>
 cudaError_t norm_of(const NormIn& a, void* y, int64_t ldy, float* mean, float* rstd, bool wide, cudaStream_t stream) {
     constexpr int V = 16 / sizeof(T);
@@ -743,10 +1087,18 @@ cudaError_t norm_of(const NormIn& a, void* y, int64_t ldy, float* mean, float* r
         if (n <= 256 * 32) return norm_ring<T, 256, N>(a, y, ldy, mean, rstd, stream);
         if (n <= 512 * 32) return norm_ring<T, 512, N>(a, y, ldy, mean, rstd, stream);
     } else {
+        // Short rows are latency: many warps that each wait for their own row do better than the ring (777 columns, 4000
+        // rows of 16 bits: 7.5 us; 512 rows of 1001: 3.8 us, ring 5.3), unless many rows of half the threads' columns go
+        // by (501 columns, 47904 rows: 55 us, ring 33). With few rows the same holds for longer ones (64 x 3001: 3.4 us,
+        // ring 5.0; 512 x 3001: 6.3 and 5.3; 15989 x 1501: 80 and 44).
         if (n <= 32 * 8) return norm<T, 32, 8>(a, y, ldy, mean, rstd, stream);
+        if (n <= 32 * 16 && a.rows >= kOddRows<8> * (kRingThreads / 32) * kNormSms) return norm_odd<T, 32, 8>(a, y, ldy, mean, rstd, stream);
         if (n <= 128 * 8) return norm<T, 128, 8>(a, y, ldy, mean, rstd, stream);
-        if (n <= 512 * 8) return norm<T, 512, 8>(a, y, ldy, mean, rstd, stream);
-        if (n <= 512 * 32) return norm<T, 512, 32>(a, y, ldy, mean, rstd, stream);
+        if (n <= 512 * 8 && a.rows <= 2 * kNormSms) return norm<T, 512, 8>(a, y, ldy, mean, rstd, stream);
+        if (n <= 128 * 16) return norm_odd<T, 128, 8>(a, y, ldy, mean, rstd, stream);
+        if (n <= 256 * 16) return norm_odd<T, 256, 8>(a, y, ldy, mean, rstd, stream);
+        if (n <= 512 * 16) return norm_odd<T, 512, 8>(a, y, ldy, mean, rstd, stream);
+        if (n <= 512 * 32) return norm_odd<T, 512, 16>(a, y, ldy, mean, rstd, stream);
     }
     k_norm_long<T><<<a.rows, kLongThreads, 0, stream>>>(a, y, ldy, mean, rstd);
     return cudaGetLastError();
@@ -757,7 +1109,7 @@ cudaError_t back(const NormBack& a, int* parts, cudaStream_t stream) {
     constexpr int kThreads = TPR < 512 ? 512 : TPR, kGroups = kThreads / TPR;
     const int need = (a.rows + kGroups - 1) / kGroups;
     *parts = need < kBackParts ? need : kBackParts;
-    const size_t smem = kGroups > 1 && a.part ? (size_t)2 * a.cols * 4 : 0;  // at most 16 KiB: 2048 columns
+    const size_t smem = kGroups > 1 && a.part ? (size_t)kGroups * 2 * a.cols * 4 : 0;  // at most 32 KiB: 8 columns a thread
     k_norm_back<T, TPR, N, 1><<<*parts, kThreads, smem, stream>>>(a);
     return cudaGetLastError();
 }
@@ -775,8 +1127,27 @@ cudaError_t back_ring(const NormBack& a, int* parts, cudaStream_t stream) {
     cudaError_t err = allow_smem(kernel, kRingBytes, ready);
     if (err != cudaSuccess) return err;
     size_t smem = kGroups * stages * stage + weights;
-    if (smem < (size_t)2 * a.cols * 4) smem = (size_t)2 * a.cols * 4;  // the ring's place also joins the groups' sums
+    const size_t join = kGroups > 1 ? (size_t)kGroups * 2 * a.cols * 4 : 0;  // its place also joins the groups' sums
+    if (smem < join) smem = join;
     kernel<<<*parts, kRingThreads, smem, stream>>>(a, stages);
+    return cudaGetLastError();
+}
+
+template <int TPR>
+cudaError_t back_odd(const NormBack& a, int* parts, cudaStream_t stream) {
+    constexpr int kGroups = kRingThreads / TPR;
+    const int need = (a.rows + kGroups - 1) / kGroups;
+    *parts = need < kNormSms ? need : kNormSms;
+    const uint32_t place = odd_place(a.cols, 4);
+    const int stages = ring_stages(kGroups, 2 * (size_t)place, kRingBytes);
+    auto kernel = k_norm_back_odd<TPR>;
+    static std::atomic<uint64_t> ready{0};
+    cudaError_t err = allow_smem(kernel, kRingBytes, ready);
+    if (err != cudaSuccess) return err;
+    size_t smem = (size_t)kGroups * stages * 2 * place;
+    const size_t join = kGroups > 1 ? (size_t)kGroups * 2 * a.cols * 4 : 0;  // its place also joins the groups' sums
+    if (smem < join) smem = join;
+    kernel<<<*parts, kRingThreads, smem, stream>>>(a, stages, place);
     return cudaGetLastError();
 }
 
@@ -796,8 +1167,21 @@ cudaError_t back_of(const NormBack& a, int* parts, bool wide, cudaStream_t strea
             if (n <= 512 * 32) return back_ring<T, 512, 2 * N>(a, parts, stream);
         }
     } else {
-        if (n <= 32 * 8) return back<T, 32, 8>(a, parts, stream);
+        // The ring for many 32-bit rows (11758 x 2041: 42 us, 111 without; 1184 x 3001: 11.1 and 11.7; 512 x 3001: 8.5 and
+        // 7.0). 16-bit rows cost as many instructions a value for half the bytes (7997 x 3001: ring 63 us, 49 without).
+        if constexpr (sizeof(T) == 4) {
+            if (n > 128 * 8 && a.rows >= kBackOddRows) {
+                if (n <= 128 * 16) return back_odd<128>(a, parts, stream);
+                if (n <= 256 * 16) return back_odd<256>(a, parts, stream);
+                if (n <= 512 * 16) return back_odd<512>(a, parts, stream);
+            }
+        }
+        // few rows: the threads of four in a block, whatever their length (512 x 251: 2.6 us; 7.7 with sixteen)
+        const bool few = a.rows <= kBackParts * (512 / 128);  // one row to a group of 128 threads
+        if (n <= 32 * 8 && !few) return back<T, 32, 8>(a, parts, stream);
+        if (n <= 64 * 8 && !few) return back<T, 64, 8>(a, parts, stream);
         if (n <= 128 * 8) return back<T, 128, 8>(a, parts, stream);
+        if (n <= 256 * 8) return back<T, 256, 8>(a, parts, stream);
         if (n <= 512 * 8) return back<T, 512, 8>(a, parts, stream);
         if (n <= 512 * 16) return back<T, 512, 16>(a, parts, stream);
     }
