@@ -57,6 +57,10 @@ int ones_layer_norm_backward(const void* d_dy, int64_t lddy, const void* d_x, in
  *   d_workspace  at least ones_linear_ce_workspace_bytes(rows, vocab) bytes, 256-byte aligned.
  * Logits are accumulated and reduced in 32 bits. */
 size_t ones_linear_ce_workspace_bytes(int32_t rows, int32_t vocab);
+/* Copies rows that start anywhere to rows on 16-byte boundaries, as ones_linear_ce needs them: d_dst 16-byte aligned, ldd
+ * a multiple of 8, both [rows][cols] of ONES_BF16 or ONES_F16.  Zeros follow each row up to the next multiple of 8. */
+int ones_align_rows(const void* d_src, int64_t lds, int32_t rows, int32_t cols, int32_t type, void* d_dst, int64_t ldd,
+                    void* cuda_stream);
 int ones_linear_ce(const void* d_hidden, int64_t ldh, const void* d_weight, int64_t ldw, const int64_t* d_target,
                    int32_t rows, int32_t cols, int32_t vocab, int32_t type, float* d_loss, float* d_lse,
                    void* d_workspace, size_t workspace_bytes, void* cuda_stream);

@@ -411,6 +411,66 @@ __global__ void __launch_bounds__(256) k_ce_rows(const float* sum, Cut cut, int 
     }
 }
 
+// Rows that start anywhere, copied to rows on 16-byte boundaries. A thread puts together 16 bytes out of the two aligned
+// blocks that hold them: four words from a distance that is the same along a row, shifted by half a word where that is
+// odd. Bytes bound it (75300 x 871: 131 MB each way).
+constexpr int kAlignThreads = 256, kAlignEach = 4;
+__global__ void __launch_bounds__(kAlignThreads) k_align_rows(const uint16_t* src, int64_t lds, int64_t rows, int cols, uint16_t* dst, int64_t ldd) {
+    const int chunks = (cols + 7) / 8;
+    const int64_t total = rows * chunks, step = (int64_t)gridDim.x * kAlignThreads * kAlignEach;
+    const uintptr_t begin = reinterpret_cast<uintptr_t>(src), end = reinterpret_cast<uintptr_t>(src + (rows - 1) * lds + cols);
+    for (int64_t at = (int64_t)blockIdx.x * kAlignThreads * kAlignEach + threadIdx.x; at < total; at += step) {
+        int64_t row = at / chunks;
+        int k = (int)(at - row * chunks);
+        uint4 lo[kAlignEach], hi[kAlignEach];
+        const uint16_t* from[kAlignEach];
+        uint16_t* to[kAlignEach];
+        int left[kAlignEach];
+#pragma unroll
+        for (int i = 0; i < kAlignEach; ++i) {
+            from[i] = src + row * lds + 8 * k;
+            to[i] = dst + row * ldd + 8 * k;
+            left[i] = at + i * kAlignThreads < total ? min(8, cols - 8 * k) : 0;
+            const uintptr_t a = reinterpret_cast<uintptr_t>(from[i]), block = a & ~(uintptr_t)15;
+            lo[i] = hi[i] = make_uint4(0, 0, 0, 0);
+            if (left[i] > 0) {
+                if (block >= begin && block + 32 <= end) {
+                    lo[i] = __ldg(reinterpret_cast<const uint4*>(block));
+                    hi[i] = __ldg(reinterpret_cast<const uint4*>(block) + 1);
+                } else {  // a block that reaches over the ends
+                    uint32_t w[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const uintptr_t p = block + 4 * j;
+                        const uint32_t x = p >= begin && p + 2 <= end ? *reinterpret_cast<const uint16_t*>(p) : 0;
+                        const uint32_t y = p + 2 >= begin && p + 4 <= end ? *reinterpret_cast<const uint16_t*>(p + 2) : 0;
+                        w[j] = x | y << 16;
+                    }
+                    lo[i] = make_uint4(w[0], w[1], w[2], w[3]), hi[i] = make_uint4(w[4], w[5], w[6], w[7]);
+                }
+            }
+            k += kAlignThreads;
+            if (k >= chunks) row += k / chunks, k %= chunks;
+        }
+#pragma unroll
+        for (int i = 0; i < kAlignEach; ++i) {
+            if (left[i] <= 0) continue;
+            const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(from[i]) & 15;
+            uint32_t w[8] = {lo[i].x, lo[i].y, lo[i].z, lo[i].w, hi[i].x, hi[i].y, hi[i].z, hi[i].w};
+#pragma unroll
+            for (int j = 0; j < 6; ++j) w[j] = off & 8 ? w[j + 2] : w[j];
+#pragma unroll
+            for (int j = 0; j < 5; ++j) w[j] = off & 4 ? w[j + 1] : w[j];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                w[j] = __funnelshift_r(w[j], w[j + 1], off & 2 ? 16 : 0);
+                if (left[i] < 2 * j + 2) w[j] &= left[i] <= 2 * j ? 0u : 0xFFFFu;  // zeros behind the last column
+            }
+            *reinterpret_cast<uint4*>(to[i]) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+}
+
 inline size_t up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // Columns of a tile of logits where the rows fill one tile at most (0: the usual): the weight's rows pass once and that is
@@ -501,6 +561,17 @@ cudaError_t loss_wait_expired(unsigned* out) {
 using namespace ones;
 
 extern "C" {
+
+int ones_align_rows(const void* d_src, int64_t lds, int32_t rows, int32_t cols, int32_t type, void* d_dst, int64_t ldd, void* cuda_stream) {
+    if (rows < 0 || cols < 0 || (type != ONES_BF16 && type != ONES_F16) || lds < cols || ldd < cols) return ONES_ERR_BAD_PARAM;
+    if (rows == 0 || cols == 0) return ONES_OK;
+    if (!d_src || !d_dst) return ONES_ERR_NULL;
+    if (!aligned(d_src, 2) || !aligned(d_dst, 16) || ldd % 8) return ONES_ERR_ALIGN;
+    const int64_t need = ((int64_t)rows * ((cols + 7) / 8) + kAlignThreads * kAlignEach - 1) / (kAlignThreads * kAlignEach);
+    k_align_rows<<<(unsigned)(need < 8 * kSms ? need : 8 * kSms), kAlignThreads, 0, reinterpret_cast<cudaStream_t>(cuda_stream)>>>(
+        static_cast<const uint16_t*>(d_src), lds, rows, cols, static_cast<uint16_t*>(d_dst), ldd);
+    return cudaGetLastError() == cudaSuccess ? ONES_OK : ONES_ERR_CUDA;
+}
 
 size_t ones_linear_ce_workspace_bytes(int32_t rows, int32_t vocab) {
     if (bad_sizes(rows, 1, vocab)) return 0;

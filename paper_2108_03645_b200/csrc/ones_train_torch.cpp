@@ -28,11 +28,13 @@ Tensor fresh(at::IntArrayRef shape, const Tensor& like, at::ScalarType type) { r
 struct Rows {
     Tensor t;
     int64_t n, c, ld;
+    int rc = 0;  // of a copy
 };
 Rows rows_of(const Tensor& x, int64_t align = 0) {
     Rows r{x.dim() == 2 ? x : x.reshape({-1, x.size(-1)}), 0, 0, 0};
     r.n = r.t.size(0), r.c = r.t.size(1);
     r.ld = r.t.stride(0);
+    TORCH_CHECK_VALUE(r.n <= INT32_MAX && r.c <= INT32_MAX, "more than 2^31 - 1 rows or columns");
     const int64_t least = std::max<int64_t>(r.c, 1);
     if (r.n <= 1) r.ld = align ? (least + align - 1) / align * align : least;  // there is no second row
     if ((r.t.stride(1) != 1 && r.c > 1) || r.ld < r.c) {
@@ -40,13 +42,11 @@ Rows rows_of(const Tensor& x, int64_t align = 0) {
         r.ld = r.c;
     }
     if (align && (r.ld % align || reinterpret_cast<uintptr_t>(r.t.data_ptr()) % 16)) {
-        r.ld = (r.c + align - 1) / align * align;
-        Tensor wide = fresh({r.n, r.ld}, r.t, r.t.scalar_type());
-        Tensor part = wide.narrow(1, 0, r.c);
-        part.copy_(r.t);
-        r.t = part;
+        const int64_t ld = (r.c + align - 1) / align * align;
+        Tensor wide = fresh({r.n, ld}, r.t, r.t.scalar_type());
+        r.rc = ones_align_rows(r.t.data_ptr(), r.ld, (int)r.n, (int)r.c, kind_of(r.t.scalar_type()), wide.data_ptr(), ld, stream());
+        r.t = wide, r.ld = ld;
     }
-    TORCH_CHECK_VALUE(r.n <= INT32_MAX && r.c <= INT32_MAX, "more than 2^31 - 1 rows or columns");
     return r;
 }
 
@@ -120,6 +120,7 @@ py::object linear_cross_entropy(const Tensor& hidden, const Tensor& weight, cons
     const at::NoGradGuard no_grad;
     const c10::cuda::CUDAGuard guard(hidden.device());
     const Rows h = rows_of(hidden, 8), w = rows_of(weight, 8);
+    if (h.rc || w.rc) return py::int_(h.rc ? h.rc : w.rc);
     const Tensor t = target.contiguous();
     Tensor loss = fresh(target.sizes(), hidden, at::kFloat), lse = fresh(target.sizes(), hidden, at::kFloat);
     const size_t nbytes = ones_linear_ce_workspace_bytes((int)h.n, (int)w.n);
@@ -139,6 +140,7 @@ py::object linear_cross_entropy_backward(const Tensor& dloss, const Tensor& hidd
     const c10::cuda::CUDAGuard guard(hidden.device());
     const at::ScalarType wt = weight_gradient_f32 ? at::kFloat : weight.scalar_type();
     const Rows h = rows_of(hidden), w = rows_of(weight, 8);
+    if (w.rc) return py::int_(w.rc);
     const Tensor t = target.contiguous(), g = dloss.contiguous(), l = lse.contiguous();
     Tensor dh = fresh(hidden.sizes(), hidden, hidden.scalar_type()), dw = fresh(weight.sizes(), weight, wt);
     const int32_t entries = piece < 0 || piece > INT32_MAX ? -1 : (int32_t)piece;

@@ -20,7 +20,7 @@ def test_library_exports_and_binding_covers_every_declared_symbol():
     from paper_2108_03645_b200 import build, train
     lib = ctypes.CDLL(build.build())
     names = _declared()
-    assert len(names) == 10
+    assert len(names) == 11
     for n in names:
         assert hasattr(lib, n), n
     assert sorted(train._SIGNATURES) == names
@@ -142,3 +142,12 @@ def test_profile_fit():
             pj.fit(b, bad)
     row = pj.job_row(8, 4, 64, 0.003, 2e-4, 0.01)
     assert row.dtype.itemsize == 48 and row["kmax"][0] == 4
+
+
+@pytest.mark.parametrize("change, want", [
+    ({"rows": -1}, PARAM), ({"cols": -1}, PARAM), ({"type": 0}, PARAM), ({"lds": 63}, PARAM), ({"ldd": 63}, PARAM), ({"src": None}, NULL),
+    ({"dst": None}, NULL), ({"src": P + 1}, ALIGN), ({"dst": P + 8}, ALIGN), ({"ldd": 68}, ALIGN)])
+def test_align_rows_refuses(change, want):
+    a = {"src": P, "lds": 64, "rows": 4, "cols": 64, "type": 1, "dst": P, "ldd": 64, "stream": None}
+    a.update(change)
+    assert _lib().ones_align_rows(*a.values()) == want
