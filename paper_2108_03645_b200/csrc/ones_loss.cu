@@ -293,7 +293,7 @@ struct Header {
 
 // Finds the rows that take part, in order, and the power of two that brings their largest |dloss| into [1, 2), so that
 // the 16-bit gradients of the logits neither overflow nor lose their small values, whatever the scale of the loss.
-constexpr int kScan = 4;
+constexpr int kScan = 8;
 __global__ void __launch_bounds__(1024) k_ce_scan(const float* dloss, const int64_t* target, int rows, int vocab, RowInfo* info, Header* head) {
     __shared__ int s_count[32];
     __shared__ float s_top[32];
@@ -301,33 +301,37 @@ __global__ void __launch_bounds__(1024) k_ce_scan(const float* dloss, const int6
     float top = 0.f;
     int base = 0;
     for (int r0 = 0; r0 < rows; r0 += 1024 * kScan) {
-        const int first = r0 + threadIdx.x * kScan;
-        bool in[kScan];
+        const int first = r0 + warp * 32 * kScan + lane;
+        int64_t t[kScan];
+        float g[kScan];
+#pragma unroll
+        for (int i = 0; i < kScan; ++i) {
+            t[i] = first + 32 * i < rows ? target[first + 32 * i] : -1;
+            g[i] = first + 32 * i < rows ? dloss[first + 32 * i] : 0.f;
+        }
+        unsigned in[kScan];
         int n = 0;
 #pragma unroll
         for (int i = 0; i < kScan; ++i) {
-            const int64_t t = first + i < rows ? target[first + i] : -1;
-            in[i] = t >= 0 && t < vocab;
-            n += in[i];
-            if (in[i]) top = fmaxf(top, fabsf(dloss[first + i]));
+            const bool live = t[i] >= 0 && t[i] < vocab;
+            if (live) top = fmaxf(top, fabsf(g[i]));
+            in[i] = __ballot_sync(0xFFFFFFFFu, live);
+            n += __popc(in[i]);
         }
-        int up_to = n;
+        if (lane == 0) s_count[warp] = n;
+        __syncthreads();
+        int up_to = s_count[lane];  // by the warps up to the lane's
         for (int o = 1; o < 32; o *= 2) {
             const int u = __shfl_up_sync(0xFFFFFFFFu, up_to, o);
             if (lane >= o) up_to += u;
         }
-        if (lane == 31) s_count[warp] = up_to;
-        __syncthreads();
-        int before = 0, all = 0;
-        for (int w = 0; w < 32; ++w) {
-            if (w < warp) before += s_count[w];
-            all += s_count[w];
-        }
-        int at = base + before + up_to - n;
+        int at = base + __shfl_sync(0xFFFFFFFFu, up_to, warp) - n;
+        base += __shfl_sync(0xFFFFFFFFu, up_to, 31);
 #pragma unroll
-        for (int i = 0; i < kScan; ++i)
-            if (in[i]) info[at++].row = first + i;
-        base += all;
+        for (int i = 0; i < kScan; ++i) {
+            if (in[i] >> lane & 1) info[at + __popc(in[i] & ((1u << lane) - 1))].row = first + 32 * i;
+            at += __popc(in[i]);
+        }
         __syncthreads();
     }
     for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
@@ -387,8 +391,20 @@ __global__ void __launch_bounds__(256) k_ce_gather(const uint16_t* hidden, int64
     }
 }
 
-// Joins the parts of the sums over the vocabulary, in order, and rounds them into the caller's rows. A warp takes 128
-// columns of a row, so that few rows fill the SMs too.
+// Four values of a row out of the parts of a product, in their order.
+__device__ __forceinline__ float4 join_parts(const float* p, int64_t part, int parts, float scale) {
+    float4 f = *reinterpret_cast<const float4*>(p);
+#pragma unroll 8
+    for (int k = 1; k < parts; ++k) {
+        const float4 q = *reinterpret_cast<const float4*>(p + k * part);
+        f.x += q.x, f.y += q.y, f.z += q.z, f.w += q.w;
+    }
+    f.x *= scale, f.y *= scale, f.z *= scale, f.w *= scale;
+    return f;
+}
+
+// Joins the parts of the sums over the vocabulary and rounds them into the caller's rows. A warp takes 128 columns of a
+// row, so that few rows fill the SMs too.
 __global__ void __launch_bounds__(256) k_ce_rows(const float* sum, Cut cut, int plan_nk, int64_t ld_sum, int rows, int cols, const Header* head,
                                                  const RowInfo* info, uint16_t* out, int64_t ld_out, bool f16, bool wide) {
     wait_for_predecessor();
@@ -399,15 +415,32 @@ __global__ void __launch_bounds__(256) k_ce_rows(const float* sum, Cut cut, int 
     for (int64_t w = blockIdx.x * 8 + threadIdx.x / 32; w < items; w += gridDim.x * 8) {
         const int i = (int)(w / groups), c = (int)(w % groups) * 128 + threadIdx.x % 32 * 4;
         if (c >= cols) continue;
-        const float* p = sum + (int64_t)i * ld_sum + c;
-        float4 f = *reinterpret_cast<const float4*>(p);
-#pragma unroll 8
-        for (int k = 1; k < parts; ++k) {
-            const float4 q = *reinterpret_cast<const float4*>(p + k * part);
-            f.x += q.x, f.y += q.y, f.z += q.z, f.w += q.w;
+        store_grad4(out + (int64_t)info[i].row * ld_out + c, join_parts(sum + (int64_t)i * ld_sum + c, part, parts, unscale), cols - c, f16, wide);
+    }
+}
+
+// The same for dweight's parts, over the rows that take part.
+__global__ void __launch_bounds__(256) k_ce_weight_rows(const float* sum, Cut cut, int fold, int64_t ld_sum, int rows, int cols, const Header* head,
+                                                        void* out, int64_t ld_out, bool f32, bool f16, bool wide) {
+    wait_for_predecessor();
+    let_successor_start();
+    const int groups = (cols + 127) / 128, nk = (head->live * fold + kTileK - 1) / kTileK;
+    const float unscale = 1.f / head->scale;
+    const int64_t part = (int64_t)rows * ld_sum, items = (int64_t)rows * groups;
+    const int parts = nk ? parts_of(cut, rows, cols, nk) : 0;
+    for (int64_t w = blockIdx.x * 8 + threadIdx.x / 32; w < items; w += gridDim.x * 8) {
+        const int i = (int)(w / groups), c = (int)(w % groups) * 128 + threadIdx.x % 32 * 4, left = cols - c;
+        if (left <= 0) continue;
+        const float4 f = parts ? join_parts(sum + (int64_t)i * ld_sum + c, part, parts, unscale) : make_float4(0.f, 0.f, 0.f, 0.f);
+        if (f32) {
+            float* to = static_cast<float*>(out) + (int64_t)i * ld_out + c;
+            to[0] = f.x;
+            if (left > 1) to[1] = f.y;
+            if (left > 2) to[2] = f.z;
+            if (left > 3) to[3] = f.w;
+        } else {
+            store_grad4(static_cast<uint16_t*>(out) + (int64_t)i * ld_out + c, f, left, f16, wide);
         }
-        f.x *= unscale, f.y *= unscale, f.z *= unscale, f.w *= unscale;
-        store_grad4(out + (int64_t)info[i].row * ld_out + c, f, cols - c, f16, wide);
     }
 }
 
@@ -515,17 +548,22 @@ constexpr int32_t kFewRows = 64;
 inline int fold_of(int32_t rows) { return rows <= kFewRows ? 2 : 1; }
 
 struct BackwardLayout {
-    size_t head, info, hidden, dlogits, sum, total;
+    size_t head, info, hidden, dlogits, sum, wsum, total;
     int64_t ld_sum, ld_hidden;
     int32_t piece;
     int fold;
-    Cut cut;  // of the product over a piece of the vocabulary
+    Cut cut;   // of the product over a piece of the vocabulary
+    Cut wcut;  // of a piece's product over the rows: many rows and a small weight are few tiles with a long K
 };
 BackwardLayout backward_layout(int32_t rows, int32_t cols, int32_t vocab, int32_t piece) {
     BackwardLayout L;
     L.piece = piece_of(rows, vocab, piece);
     L.fold = fold_of(rows);
     L.cut = cut_of(rows, cols, (int)up(vocab < L.piece ? vocab : L.piece, kTileK) * L.fold);
+    const int32_t entries = vocab < L.piece ? vocab : L.piece;
+    L.wcut = cut_of(entries, cols, rows * L.fold);
+    const int64_t edge = L.wcut.pairs ? 256 : 128, tiles = (entries + edge - 1) / edge * ((cols + edge - 1) / edge), most = (L.wcut.pairs ? kSms / 2 : kSms) / tiles;
+    if (L.wcut.splits > most) L.wcut.splits = most > 1 ? (int)most : 1;
     L.ld_sum = (int64_t)up(cols, 32);
     L.ld_hidden = (int64_t)up(cols, 8);
     size_t at = 0;
@@ -539,6 +577,7 @@ BackwardLayout backward_layout(int32_t rows, int32_t cols, int32_t vocab, int32_
     L.hidden = take((size_t)rows * L.fold * L.ld_hidden * 2);
     L.dlogits = take((size_t)rows * L.fold * L.piece * 2);
     L.sum = take(L.piece < vocab || L.cut.splits > 1 ? (size_t)L.cut.splits * rows * L.ld_sum * 4 : 0);
+    L.wsum = take(L.wcut.splits > 1 ? (size_t)L.wcut.splits * entries * L.ld_sum * 4 : 0);
     L.total = at;
     return L;
 }
@@ -659,6 +698,18 @@ int ones_linear_ce_backward(const float* d_dloss, const void* d_hidden, int64_t 
         err = launch_matmul_cut<false, true, EpiSum>({dl, (int64_t)L.piece * fold, L.piece, false}, {w0, ldw, 0, true}, rows, cols, n, L.cut, f16,
                                                      e2, stream, true, &head->live, plan_nk, fold);
         if (err != cudaSuccess) break;
+        if (L.wcut.splits > 1) {
+            float* wsum = reinterpret_cast<float*>(ws + L.wsum);
+            const EpiSum::Args e4 = {wsum, L.ld_sum, nullptr, 0, nullptr, nullptr, n, cols, true, false, f16, false};
+            err = launch_matmul_cut<true, true, EpiSum>({dl, L.piece, 0, true}, {hidden, L.ld_hidden, 0, true}, n, cols, rows * fold, L.wcut, f16,
+                                                        e4, stream, true, nullptr, 0, 1, &head->live, fold);
+            if (err != cudaSuccess) break;
+            const int64_t blocks = ((int64_t)n * ((cols + 127) / 128) + 7) / 8;
+            err = launch_after(k_ce_weight_rows, dim3((unsigned)(blocks < 8 * kSms ? blocks : 8 * kSms)), dim3(256), stream,
+                               static_cast<const float*>(wsum), L.wcut, fold, L.ld_sum, n, cols, static_cast<const Header*>(head),
+                               static_cast<void*>(static_cast<char*>(d_dweight) + (int64_t)v0 * lddw * (int64_t)wsize), lddw, wtype == ONES_F32, f16, wide_w);
+            continue;
+        }
         const EpiGrad::Args e3 = {static_cast<char*>(d_dweight) + (int64_t)v0 * lddw * (int64_t)wsize, lddw, &head->scale, n, cols,
                                   wtype == ONES_F32, f16, wide_w};
         err = launch_matmul<true, true, EpiGrad>({dl, L.piece, 0, true}, {hidden, L.ld_hidden, 0, true}, n, cols, rows * fold, 1, false, f16,

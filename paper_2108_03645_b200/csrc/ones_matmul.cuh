@@ -41,7 +41,7 @@ struct MatShape {
     int M, N, K;
     int tiles_m, tiles_n, batch;
     int splits;  // > 1: K is cut into parts, at most so many, each with a C of its own in the place of a matrix of the batch
-    int plan_nk; // stages of K that the number of parts goes by (K itself may be shorter)
+    int plan_nk; // stages of K that the number of parts goes by (K itself may be shorter); 0: K's own
     int fold;    // 2: A has two terms (a matrix of the batch each) that meet the same B: K runs over it twice
     int sym;     // only tiles on and above the diagonal are computed (C is symmetric)
     const int *live_m, *live_k;  // where M or K is known on the device only (at most the value above)
@@ -401,7 +401,7 @@ __global__ void __launch_bounds__(kMatThreads<Epi::kWarps>, 1)
     if (g.live_m) g.M = *g.live_m, g.tiles_m = (g.M + 128 * CG - 1) / (128 * CG);
     if (g.live_k) g.K = *g.live_k * g.live_times;
     const int per = tiles_per_matrix(g);
-    if (g.splits > 1) g.splits = g.batch = parts_of_k(g.splits, per, kSms / CG, g.plan_nk);
+    if (g.splits > 1) g.splits = g.batch = parts_of_k(g.splits, per, kSms / CG, g.plan_nk ? g.plan_nk : max(1, (g.K + kTileK - 1) / kTileK));
     const int total = per * g.batch;
     const int first = blockIdx.x / CG, step = gridDim.x / CG;
     const int nk_one = (g.K + kTileK - 1) / kTileK, nk_all = nk_one * g.fold, nk_part = (nk_all + g.splits - 1) / g.splits;
@@ -562,8 +562,8 @@ inline Cut cut_of(int M, int N, int K) {
             const int part = (nk + s - 1) / s;
             if (s > 1 && (s - 1) * part >= nk) continue;  // no part is empty
             const double waves = (double)((tiles * s + slots - 1) / slots);
-            // parts cost a pass over their sums: only where they win a tenth
-            const double cost = waves * (part * (pairs ? 2.0 : kSmallCost) + 32) * (s > 1 ? 1.1 : 1.0);
+            // a unit is 0.135 us; joining the parts is a launch of about 5 us and a pass over their sums at 5 TB/s
+            const double cost = waves * (part * (pairs ? 2.0 : kSmallCost) + 32) + (s > 1 ? 36 + (double)s * M * N * 8 / 675e3 : 0);
             if (least == 0 || cost < least) least = cost, best = {pairs != 0, s};
         }
     }
@@ -578,9 +578,10 @@ __host__ __device__ inline int parts_of(const Cut& cut, int live, int N, int pla
 
 template <bool AMN, bool BMN, class Epi>
 cudaError_t launch_matmul_cut(const Operand& a, const Operand& b, int M, int N, int K, Cut cut, bool f16,
-                              const typename Epi::Args& ea, cudaStream_t stream, bool dependent, const int* live_m, int plan_nk, int fold) {
+                              const typename Epi::Args& ea, cudaStream_t stream, bool dependent, const int* live_m, int plan_nk, int fold,
+                              const int* live_k = nullptr, int live_times = 1) {
     MatShape g = {};
-    g.fold = fold;
+    g.fold = fold, g.live_k = live_k, g.live_times = live_times;
     g.M = M, g.N = N, g.K = K, g.batch = g.splits = cut.splits, g.live_m = live_m, g.plan_nk = plan_nk;
     return cut.pairs ? launch_matmul_cg<2, AMN, BMN, Epi>(a, b, g, f16, ea, stream, dependent)
                      : launch_matmul_cg<1, AMN, BMN, Epi>(a, b, g, f16, ea, stream, dependent);

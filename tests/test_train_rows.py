@@ -108,3 +108,29 @@ def test_align_rows_past_32_bits():
 def test_linear_cross_entropy_odd_rows(n, d, v, dtype):
     h, w, t, g = ce_inputs(n, d, v, dtype, 0.1)
     check_ce(placed(h, d + 1, 3), placed(w, d + 3, 1), t, g)
+
+
+# many rows and a small weight: the rows are what is cut into parts, and how many of them take part is known late
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("n,d,v,ignored,piece", [(3000, 72, 300, 0.1, 0), (5000, 65, 111, 0.0, 0), (2000, 520, 260, 0.97, 0),
+                                                 (2500, 130, 1000, 0.3, 256), (9000, 96, 50, 0.999, 0), (4097, 8, 2, 0.5, 0)])
+def test_linear_cross_entropy_small_weight(n, d, v, ignored, piece, dtype):
+    h, w, t, g = ce_inputs(n, d, v, dtype, ignored)
+    check_ce(h, w, t, g, piece=piece)
+    check_ce(h, w, t, g, piece=piece, weight_gradient=F32)
+
+
+def test_linear_cross_entropy_small_weight_no_row_takes_part():
+    from paper_2108_03645_b200 import train
+    h, w, t, g = ce_inputs(3000, 72, 300, BF16, 0.0)
+    t[:] = -1
+    loss, lse = train.linear_cross_entropy(h, w, t)
+    dh, dw = train.linear_cross_entropy_backward(g, h, w, t, lse)
+    assert not bool(loss.any()) and not bool(dh.any()) and not bool(dw.any())
+
+
+@pytest.mark.parametrize("n", [1, 31, 33, 8191, 8192, 8193, 20000])
+def test_linear_cross_entropy_finds_the_rows_that_take_part(n):
+    """Whatever their number and place: their order shows in the gradients."""
+    h, w, t, g = ce_inputs(n, 64, 40, BF16, 0.4, seed=n)
+    check_ce(h, w, t, g)
