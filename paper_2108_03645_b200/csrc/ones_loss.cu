@@ -211,13 +211,86 @@ struct EpiGrad {
         int rows, cols;
         bool f32, f16, wide;
     };
+    // 16-bit rows that start anywhere. A window of 32 columns is moved back, for each row by itself, to where the row meets
+    // a 32-byte boundary; the up to 15 columns before its own are the neighbour's, and still in the accumulator. So only
+    // the ends of a tile's rows are written in less than 16 bytes. first, last: the tile's columns.
+    template <int W>
+    static __device__ __forceinline__ void odd_rows(const Args& a, float unscale, uint32_t acc, int row, int col, int first, int last,
+                                                    const Turn<kWarps>& turn) {
+        static_assert(Turn<kWarps>::kHalves == 32, "");
+        uint16_t* out = static_cast<uint16_t*>(a.out);
+        auto phase = [&](int r) { return (int)(reinterpret_cast<uintptr_t>(out + (int64_t)r * a.ld + col) >> 1) & 15; };
+        const int back = 16 - phase(row), row0 = row - turn.lane;
+        const bool ends = last <= col + W;  // the tile's last column is this warp's
+#pragma unroll 1
+        for (int c = 0; c < W + 32; c += 32) {
+            const bool extra = col + c >= last;  // what is moved back out of the last window
+            if ((c == W || extra) && (!ends || col + c >= last + 32)) break;
+            uint32_t w[24];
+            if (col + c > first) {
+                float v[16];
+                tmem_load(acc + c - 16, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = Half16::pack(v[2 * i] * unscale, v[2 * i + 1] * unscale, a.f16);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = 0;
+            }
+            if (!extra) {
+                float v[32];
+                tmem_load(acc + c, v);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) w[8 + i] = Half16::pack(v[2 * i] * unscale, v[2 * i + 1] * unscale, a.f16);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) w[8 + i] = 0;
+            }
+            // the 32 values from `back` (1 to 16) on
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = back & 16 ? w[i + 8] : w[i];
+#pragma unroll
+            for (int i = 0; i < 20; ++i) w[i] = back & 8 ? w[i + 4] : w[i];
+#pragma unroll
+            for (int i = 0; i < 18; ++i) w[i] = back & 4 ? w[i + 2] : w[i];
+#pragma unroll
+            for (int i = 0; i < 17; ++i) w[i] = back & 2 ? w[i + 1] : w[i];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], back & 1 ? 16 : 0);
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < 4; ++k) turn.chunk(turn.lane, k) = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+            __syncwarp();
+            uint4 q[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[i] = turn.chunk(turn.row_of(i), turn.chunk_of());
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = row0 + turn.row_of(i), at = col + c - phase(r) + 8 * turn.chunk_of();
+                if (r >= a.rows) continue;
+                uint16_t* p = out + (int64_t)r * a.ld + at;
+                if (at >= first && at + 8 <= last) {
+                    *reinterpret_cast<uint4*>(p) = q[i];
+                } else {
+                    const int to = min(last - at, 8);
+                    int k = max(first - at, 0);
+                    if (k < to && k & 1) p[k] = turn.half_at(turn.row_of(i), 8 * turn.chunk_of() + k), ++k;
+                    for (; k + 1 < to; k += 2) *reinterpret_cast<uint32_t*>(p + k) = turn.word_at(turn.row_of(i), 4 * turn.chunk_of() + k / 2);
+                    if (k < to) p[k] = turn.half_at(turn.row_of(i), 8 * turn.chunk_of() + k);
+                }
+            }
+        }
+    }
     template <int W>
     static __device__ __forceinline__ void tile(const Args& a, const MatShape& shape, uint32_t acc, int row, int col, int limit,
-                                                const TileAt&, int, const Turn<kWarps>& turn) {
+                                                const TileAt& at, int, const Turn<kWarps>& turn) {
         const float unscale = 1.f / *a.scale;
         const bool none = shape.K == 0;  // no row takes part: nothing was multiplied
         const int row0 = row - turn.lane;
         const int end = min(a.cols, limit);
+        if (!a.f32 && !a.wide && !none) {
+            if (col < end) odd_rows<W>(a, unscale, acc, row, col, at.n * shape.width, min(a.cols, (at.n + 1) * shape.width), turn);
+            return;
+        }
         constexpr int N = Turn<kWarps>::kHalves;
 #pragma unroll 1
         for (int c = 0; c < W && col + c < end; c += N) {

@@ -134,3 +134,31 @@ def test_linear_cross_entropy_finds_the_rows_that_take_part(n):
     """Whatever their number and place: their order shows in the gradients."""
     h, w, t, g = ce_inputs(n, 64, 40, BF16, 0.4, seed=n)
     check_ce(h, w, t, g)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("d", [1, 9, 15, 17, 33, 113, 130, 207, 255, 257, 271, 513, 777])
+def test_linear_cross_entropy_weight_gradient_rows_of_any_length(d, dtype):
+    """Whatever the lengths, starts and distances of its rows, and nothing beside them."""
+    from paper_2108_03645_b200 import train
+    L = train.lib()
+    n, v = 70, 700
+    h, w, t, g = ce_inputs(n, d, v, dtype, 0.1)
+    lse = train.linear_cross_entropy(h, w, t)[1]
+    dh, want = train.linear_cross_entropy_backward(g, h, w, t, lse, weight_gradient=F32)
+    check_ce(h, w, t, g)
+    kind, up = (1 if dtype == BF16 else 2), (d + 7) // 8 * 8
+    wa, ha = torch.zeros(v, up, dtype=dtype, device="cuda"), h.contiguous()
+    wa[:, :d] = w
+    nbytes = L.ones_linear_ce_backward_workspace_bytes(n, d, v, 0)
+    space = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    s = torch.cuda.current_stream().cuda_stream
+    for ld, start in ((d, 0), (d, 1), (d + 1, 3), (d + 2, 6), (up + 8, 2)):
+        buf = torch.full((start + v * ld + 16,), 77.0, dtype=dtype, device="cuda")
+        assert L.ones_linear_ce_backward(g.data_ptr(), ha.data_ptr(), d, wa.data_ptr(), up, t.data_ptr(), lse.data_ptr(), n, d, v, kind, kind,
+                                         0, dh.data_ptr(), d, buf.data_ptr() + 2 * start, ld, space.data_ptr(), nbytes, s) == 0
+        got = buf.as_strided((v, d), (ld, 1), start)
+        assert torch.equal(got, want.to(dtype))                        # the same sums, rounded once
+        inside = torch.zeros_like(buf, dtype=torch.bool)
+        inside.as_strided((v, d), (ld, 1), start).fill_(True)
+        assert bool((buf[~inside] == 77.0).all())
