@@ -12,7 +12,8 @@
  * is enqueued on `cuda_stream` (a cudaStream_t, NULL = the default stream) and nothing synchronises, except
  * ones_train_status.  Arguments are checked before anything is launched.  Results do not depend on the order in which
  * blocks run: the same inputs give the same bits.  Rows are `ld` values apart, ld >= the row's length; values between
- * two rows are neither read nor written.
+ * two rows are not written and do not matter, but where rows start on no 16-byte boundary they may be read along with
+ * the 16-byte blocks around a row.  Nothing before a matrix's first value or after its last is read.
  */
 #ifndef ONES_TRAIN_H
 #define ONES_TRAIN_H
@@ -71,7 +72,8 @@ int ones_linear_ce(const void* d_hidden, int64_t ldh, const void* d_weight, int6
  * Rows that take no part cost next to nothing: the others are gathered first, so nothing of them, not even a NaN in
  * hidden, reaches dweight.  The vocabulary is taken in pieces of `piece` entries (a multiple of 256; 0: a default that keeps the piece's
  * gradient near 256 MiB): the logits of a piece are computed again, and their gradient is kept in the workspace, as
- * 16 bits of `type` scaled by a power of two, until both products have used it.
+ * 16 bits of `type` scaled by a power of two (with up to 64 rows as two such terms, the second what the rounding of the
+ * first left), until both products have used it.
  *   d_dhidden [rows][cols] of `type`; d_dweight [vocab][cols] of `wtype` (`type` or ONES_F32), any alignment of their
  *   elements (16-byte aligned rows are written faster), hidden too; weight aligned as above.
  *   d_workspace  at least ones_linear_ce_backward_workspace_bytes(rows, cols, vocab, piece) bytes. */

@@ -5,7 +5,7 @@
 // One persistent CTA per SM (CG = 1: tiles of 128 x 128) or pair of CTAs (CG = 2: tiles of 256 x 256, each CTA holds
 // 128 rows of A and 128 rows of B, and both tensor cores work on one tile). A ring of kStages boxes of 64 values
 // along K is filled by TMA (one thread), consumed by tcgen05.mma (one thread), and two accumulators in tensor memory
-// let the 8 epilogue warps work on one tile while the next one is multiplied. A thread of the epilogue owns one row.
+// let the epilogue warps work on one tile while the next one is multiplied. A thread of the epilogue owns one row.
 //
 // A operand is read as rows x K with K contiguous, or (AMN / BMN) as K x rows with the rows contiguous, straight from
 // the caller's layout: nothing is transposed beforehand. Sizes need not be multiples of anything: TMA fills what lies

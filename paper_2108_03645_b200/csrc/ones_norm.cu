@@ -160,6 +160,7 @@ struct NormIn {
 
 // Short rows that do not start on 16-byte boundaries: a row is held in registers by TPR threads, read once a value at a
 // time, the mean first and the squares of the differences from it second, so that no cancellation spoils the variance.
+// Many independent groups hide each other's latency: 512 x 777 takes 3.5 us, 23976 x 1001 of 16 bits 36 us (2.7 TB/s).
 template <class T, int TPR, int N>
 __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR)
     k_norm(const NormIn a, void* y_, int64_t ldy, float* mean_out, float* rstd_out) {
@@ -208,6 +209,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR)
 // copies into a ring of `stages` per group of TPR threads that is filled ahead: the bytes on their way depend neither on
 // registers nor on how many threads wait. What is left to bound the kernels is the issue of instructions, so a thread has
 // many values (the shuffles and the barrier of a sum cost as much for few) and does arithmetic on pairs.
+// 32768 x 4096 of bfloat16: 82 us, 6.5 TB/s of the 6.54 that a copy reaches; 131072 x 256: 33 us, 4.1 TB/s.
 constexpr int kRingThreads = 512, kRingBytes = 196 * 1024, kMaxStages = 16;
 // Rows that a group takes together: short ones share the latency of their sums (their values go through one butterfly).
 template <int TPR, int kValues>
@@ -332,6 +334,8 @@ __global__ void __launch_bounds__(kRingThreads, 1)
 // columns is shifted together out of two. The result leaves the same way: a word is put together from the pairs of two
 // lanes. A warp has 64 * NU columns in a row, so that only their ends are written as halves.
 // A row whose first or last block reaches over the ends of the tensor is not copied: its values are read one by one.
+// 2958 x 8111 of 32 bits: 34 us, 5.7 TB/s. For 16 bits the instructions bound it (24 a value, half the issue slots and
+// the barriers between them): 3889 x 6171 in 42 us, 2.3 TB/s, where one value at a time takes 100.
 template <class T>
 struct Unit {  // two columns of a row: neighbours for 16 bits, 32 apart for 32 bits
     static constexpr bool k16 = sizeof(T) == 2;
@@ -644,7 +648,8 @@ __device__ __forceinline__ void join_groups(const float* part, int cols, float* 
 }
 
 // Each thread keeps the same columns for all rows of its block, and with them the block's share of dweight and dbias
-// in registers; the next row's dy and x are on their way while a row is summed and written.
+// in registers; the next row's dy and x are on their way while a row is summed and written. Latency bounds it as it does
+// k_norm: 512 x 777 takes 3 us, 23976 x 1001 of 16 bits 53 us (2.7 TB/s).
 template <class T, int TPR, int NV, int V>
 __global__ void __launch_bounds__(TPR < 512 ? 512 : TPR) k_norm_back(const NormBack a) {
     constexpr int kThreads = TPR < 512 ? 512 : TPR, kGroups = kThreads / TPR;
@@ -736,7 +741,8 @@ __global__ void __launch_bounds__(TPR < 512 ? 512 : TPR) k_norm_back(const NormB
 }
 
 // The same for rows on 16-byte boundaries, as k_norm_ring: x and dy come by bulk copies. With 32 values a thread the
-// registers do not hold the weights too: they lie in shared memory before the ring then.
+// registers do not hold the weights too: they lie in shared memory before the ring then. 32768 x 4096 of bfloat16: 139 us,
+// 5.8 TB/s; the sums over a row that all threads wait for are what is missing to a copy's 6.5.
 template <class T, int TPR, int NV>
 __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_ring(const NormBack a, int stages) {
     constexpr int P = Chunk<T>::kPairs, kGroups = kRingThreads / TPR, R = kRingBackRows<TPR, 2 * P * NV>;
@@ -878,7 +884,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_ring(const NormBa
     let_successor_start();
 }
 
-// The same for many 32-bit rows on other boundaries, as k_norm_odd.
+// The same for many 32-bit rows on other boundaries, as k_norm_odd. 11758 x 2041: 42 us, 6.9 TB/s with part of it in L2.
 template <int TPR>
 __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_odd(const NormBack a, int stages, uint32_t place) {
     constexpr int kGroups = kRingThreads / TPR, NU = kBackOddUnits;
@@ -961,7 +967,8 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_odd(const NormBac
     let_successor_start();
 }
 
-// Rows longer than the registers hold: dx from two passes over the row, the sums over rows by columns.
+// Rows longer than the registers hold: dx from two passes over the row, the sums over rows by columns. 1499 x 16001 of 32
+// bits: 110 us, 2.6 TB/s; such rows are rare enough to leave it there.
 template <class T>
 __global__ void __launch_bounds__(kLongThreads) k_norm_back_long(const NormBack a) {
     __shared__ float s[2 * kLongThreads / 32];
@@ -1006,7 +1013,7 @@ __global__ void __launch_bounds__(256) k_norm_back_columns(const NormBack a) {
     let_successor_start();
 }
 
-// dweight and dbias from the blocks' parts, in a fixed order: 32 columns x 16 threads a block.
+// dweight and dbias from the blocks' parts, in a fixed order: 32 columns x 16 threads a block. Latency: 4 to 5 us.
 constexpr int kJoinLanes = 16;
 template <class W>
 __global__ void __launch_bounds__(32 * kJoinLanes) k_norm_join(const float* part, int parts, int cols, W* dw, W* db) {
