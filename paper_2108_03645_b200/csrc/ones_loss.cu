@@ -645,7 +645,7 @@ BackwardLayout backward_layout(int32_t rows, int32_t cols, int32_t vocab, int32_
     const int64_t edge = L.wcut.pairs ? 256 : 128, tiles = (entries + edge - 1) / edge * ((cols + edge - 1) / edge), most = (L.wcut.pairs ? kSms / 2 : kSms) / tiles;
     if (L.wcut.splits > most) L.wcut.splits = most > 1 ? (int)most : 1;
     L.ld_sum = (int64_t)up(cols, 32);
-    L.ld_hidden = (int64_t)up(cols, 8);
+    L.ld_hidden = (int64_t)up(cols, 64);  // rows on 128-byte lines
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;

@@ -834,9 +834,11 @@ Layout layout(int32_t count, int32_t m, int32_t n) {
     }
     L.s = m < n ? m : n;
     L.plan = plan_of(m, n, count);
-    L.ldx = (int64_t)up(n, 8);
-    L.lds = (int64_t)up(L.s, 8);
-    L.ld_part = (int64_t)up(L.s, 4);
+    // Rows on 128-byte lines: on 16-byte boundaries alone, stores and loads split sectors and lines (5230 x 1832, two: 638
+    // us instead of 532; 200 x 200: 80 instead of 70).
+    L.ldx = (int64_t)up(n, 64);
+    L.lds = (int64_t)up(L.s, 64);
+    L.ld_part = (int64_t)up(L.s, 32);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
