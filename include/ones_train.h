@@ -72,8 +72,9 @@ int ones_linear_ce(const void* d_hidden, int64_t ldh, const void* d_weight, int6
  * Rows that take no part cost next to nothing: the others are gathered first, so nothing of them, not even a NaN in
  * hidden, reaches dweight.  The vocabulary is taken in pieces of `piece` entries (a multiple of 256; 0: a default that keeps the piece's
  * gradient near 256 MiB): the logits of a piece are computed again, and their gradient is kept in the workspace, as
- * 16 bits of `type` scaled so that the largest |dloss| is 1 (with up to 64 rows as two such terms, the second what the rounding of the
- * first left), until both products have used it.
+ * 16 bits of `type` scaled so that the largest |dloss| is 1, or 2^15 for ONES_F16 (with up to 64 rows as two such terms, the
+ * second what the rounding of the first left), until both products have used it.  ONES_F16 holds it in
+ * steps of 2^-39 of the largest |dloss| where those are larger than its 11 bits.
  *   d_dhidden [rows][cols] of `type`; d_dweight [vocab][cols] of `wtype` (`type` or ONES_F32), any alignment of their
  *   elements (16-byte aligned rows are written faster), hidden too; weight aligned as above.
  *   d_workspace  at least ones_linear_ce_backward_workspace_bytes(rows, cols, vocab, piece) bytes. */

@@ -369,13 +369,17 @@ struct Header {
     float scale;  // see below
 };
 
-// Finds the rows that take part, in order, and the factor that brings their largest |dloss| to 1, so that the 16-bit
+// Finds the rows that take part, in order, and the factor that brings their largest |dloss| to `goal`, so that the 16-bit
 // gradients of the logits neither overflow nor lose their small values, whatever the scale of the loss. Where all rows have
-// the same dloss, the entries at the targets, -(1 - p), then lie below 1 and are rounded by at most 2^-9 (bfloat16); scaled
-// by a power of two they would all lie at one place in [1, 2) and be off in one direction (error of the gradients against
-// 64 bits for 1/100 each: 2.5e-3 of their norm instead of 2.0e-3). One block, 8192 rows at a time: 3 us for so many.
+// the same dloss, the entries at the targets, -(1 - p), then lie below a power of two and are rounded by at most 2^-9 of it
+// (bfloat16); scaled by a power of two they would all lie at one place in [1, 2) and be off in one direction (error of the
+// gradients against 64 bits for 1/100 each: 2.5e-3 of their norm instead of 2.0e-3). The goal is 1 for bfloat16, whose range
+// is float32's, and 2^15 for float16, the most that its range holds: p * dloss of a large vocabulary reaches far down, and
+// further in rows that weigh less than others. With a goal of 1, 32001 entries and rows of 1/1000 of the weight, half of all
+// p * dloss would be nothing. One block, 8192 rows at a time: 3 us for so many.
 constexpr int kScan = 8;
-__global__ void __launch_bounds__(1024) k_ce_scan(const float* dloss, const int64_t* target, int rows, int vocab, RowInfo* info, Header* head) {
+__global__ void __launch_bounds__(1024) k_ce_scan(const float* dloss, const int64_t* target, int rows, int vocab, float goal, RowInfo* info,
+                                                     Header* head) {
     __shared__ int s_count[32];
     __shared__ float s_top[32];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -422,8 +426,8 @@ __global__ void __launch_bounds__(1024) k_ce_scan(const float* dloss, const int6
         top = s_top[threadIdx.x];
         for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
         if (threadIdx.x == 0) {
-            constexpr float kMost = 1.2676506e30f;  // 2^100
-            head->scale = !(top > 0.f && top < INFINITY) ? 1.f : top < 1.f / kMost ? kMost : top > kMost ? 1.f / kMost : 1.f / top;
+            constexpr float kMost = 8.507059e37f;  // 2^126: its inverse is a normal number, too
+            head->scale = top > 0.f && top < INFINITY ? fminf(goal / top, kMost) : 1.f;
             head->live = base;
         }
     }
@@ -763,7 +767,7 @@ int ones_linear_ce_backward(const float* d_dloss, const void* d_hidden, int64_t 
     const int fold = L.fold, plan_nk = ((vocab < L.piece ? vocab : L.piece) + kTileK - 1) / kTileK * fold;  // of the first piece: later ones are no longer
     const unsigned row_blocks = (unsigned)((rows + 7) / 8 < 8 * kSms ? (rows + 7) / 8 : 8 * kSms);
 
-    k_ce_scan<<<1, 1024, 0, stream>>>(d_dloss, d_target, rows, vocab, info, head);
+    k_ce_scan<<<1, 1024, 0, stream>>>(d_dloss, d_target, rows, vocab, f16 ? 32768.f : 1.f, info, head);
     cudaError_t err = cudaGetLastError();
     if (err == cudaSuccess)
         err = launch_after(k_ce_gather, dim3(row_blocks), dim3(256), stream, static_cast<const uint16_t*>(d_hidden), ldh, d_target, d_dloss,

@@ -1,0 +1,52 @@
+"""Training-step operators at the edges of what they accept, on the GPU: weights of the loss that differ by orders of
+magnitude, matrices that are small beside eps, infinities, second derivatives, waits that run out, row counts near 2^31; and
+the precision that the kernels claim. References are the definitions in 64 bits."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from test_train_ops import (BF16, F16, F32, TINY, U, _device, ce_inputs, ce_reference, check_ns, close, ns_reference,  # noqa: E402,F401
+                            randn)
+
+
+# ---------------------------------------------------------------- uneven weights of the loss
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("n", [48, 300])
+@pytest.mark.parametrize("least", [1.0, 1e-2, 1e-3, 1e-5])
+def test_linear_cross_entropy_uneven_weights(n, least, dtype):
+    """Rows that weigh little beside others keep their gradients: what a 16-bit gradient of a logit is off by is one rounding of
+    it, or of float16's smallest numbers with the largest |dloss| at 2^15: 2^-25 * 2^-15 of that."""
+    from paper_2108_03645_b200 import train
+    h, w, t, _ = ce_inputs(n, 96, 32001, dtype, 0.1, seed=n)
+    w = (w.float() + 0.1).to(dtype)                # a mean: what is lost does not average out
+    g = torch.full((n,), 1024.0, device="cuda")    # float16 training scales its loss
+    g[1::2] *= least
+    _, lse = train.linear_cross_entropy(h, w, t)
+    dh, dw = train.linear_cross_entropy_backward(g, h, w, t, lse)
+    r = ce_reference(h, w, t, g)
+    k, v = h.shape[1], w.shape[0]
+    tol = (k / 8 + 4) * 2.0 ** -23 * r["mass"] + 2.0 ** -20 * (1 + r["lse"].abs())   # of a logit, as in check_ce
+    live = r["live"].double() * g.double()
+    soft = torch.softmax(r["l"], 1) * live[:, None]
+    e = U[dtype] * r["p"].abs() + soft * (torch.expm1(2 * tol) + 2.0 ** -20)[:, None] + 2.0 ** -22 * live[:, None] * (r["p"] < 0)
+    e += TINY[dtype] * 2.0 ** -15 * float(g.max()) * r["live"][:, None]
+    close(dh, r["dh"], U[dtype] * r["dh"].abs() + 1.01 * (e @ r["w"].abs()) + (v / 8 + 8) * 2.0 ** -23 * (r["p"].abs() @ r["w"].abs()) + TINY[dtype])
+    close(dw, r["dw"], U[dtype] * r["dw"].abs() + 1.01 * (e.t() @ r["h"].abs()) + (n / 8 + 8) * 2.0 ** -23 * (r["p"].abs().t() @ r["h"].abs()) + TINY[dtype])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("scale", [2.0 ** -120, 2.0 ** -100, 2.0 ** -60, 2.0 ** 110])
+def test_linear_cross_entropy_weights_of_any_scale(scale, dtype):
+    """Far beyond float16's range: dweight in 32 bits."""
+    from paper_2108_03645_b200 import train
+    h, w, t, g = ce_inputs(100, 64, 500, dtype, 0.2)
+    g = (g * scale).float()
+    _, lse = train.linear_cross_entropy(h, w, t)
+    dw = train.linear_cross_entropy_backward(g, h, w, t, lse, weight_gradient=F32)[1]
+    want = ce_reference(h, w, t, g)["dw"]
+    # root mean square of the roundings below 2^-8; a result below 2^-126 is a multiple of 2^-149
+    assert float((dw.double() - want).norm()) <= 2.0 ** -8 * float(want.norm()) + 2.0 ** -148 * want.numel() ** 0.5
