@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(kNormThreads) k_ns_cast(Source g, const double
         k = k < -120 ? -120 : k > 120 ? 120 : k;
         s_scale = ldexpf(1.f, -k);
         if (blockIdx.x == 0) {
-            const double f = ldexp(1.0, k) / (norm + eps);
+            const double f = norm == 0.0 ? 0.0 : ldexp(1.0, k) / (norm + eps);  // of nothing: 1 / eps, whose square may pass 32 bits
             factor[blockIdx.y] = make_float2((float)f, (float)(f * f));
         }
     }
@@ -575,7 +575,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, c
         int k = rms > 0.0 && rms < 1e300 ? ilogb(rms) : 0;
         k = k < -120 ? -120 : k > 120 ? 120 : k;
         s_scale = ldexpf(1.f, -k);
-        s_factor = (float)(ldexp(1.0, k) / (norm + p.eps));
+        s_factor = norm == 0.0 ? 0.f : (float)(ldexp(1.0, k) / (norm + p.eps));  // as in k_ns_cast
     }
     __syncthreads();
     const float scale = s_scale, factor = s_factor;

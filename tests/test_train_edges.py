@@ -50,3 +50,20 @@ def test_linear_cross_entropy_weights_of_any_scale(scale, dtype):
     want = ce_reference(h, w, t, g)["dw"]
     # root mean square of the roundings below 2^-8; a result below 2^-126 is a multiple of 2^-149
     assert float((dw.double() - want).norm()) <= 2.0 ** -8 * float(want.norm()) + 2.0 ** -148 * want.numel() ** 0.5
+
+
+# ---------------------------------------------------------------- matrices that are small beside eps
+
+FORMS = [(30, 50), (40, 3000), (200, 150), (300, 2000), (150, 6000)]  # one block, a cluster, one launch of all blocks, cut along K
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m,n", FORMS)
+def test_orthogonalize_zero_at_any_eps(m, n, dtype):
+    from paper_2108_03645_b200 import train
+    for eps in (1e-38, 1e-30, 1e-20, 1e-7, 1.0):
+        g = torch.zeros(2, m, n, dtype=dtype, device="cuda")
+        g[1] = randn(m, n).to(dtype)
+        o = train.orthogonalize(g, eps=eps)
+        assert not bool(o[0].any()) and bool(torch.isfinite(o[1]).all()) and bool(o[1].any())
+        assert not bool(train.orthogonalize(g[0], eps=eps).any())
