@@ -82,10 +82,32 @@ __global__ void __launch_bounds__(kNormThreads) k_ns_norm(Source g, double* part
     let_successor_start();
 }
 
+// Between the steps X is kept as 16 bits, times a power of two. Where |G| is not small beside eps, that is `unit`, about the
+// square root of the longer side: it brings X's values near 1 once its singular values have arrived there. A matrix that is
+// small beside eps has |X|_F = n < 1 and is kept times up to 2^50 more, so that n * 2^j stays within (0.5, 1]; n grows in a
+// step by at most |a| + |b| n^2 + |c| n^4 (X's singular values are at most n).
+__device__ __forceinline__ float kept_times(float n, float unit) {
+    const int j = n > 0.f && n < 1.f ? 126 - (int)(__float_as_uint(n) >> 23) : 0;  // by the exponent's bits: 0 for n in [0.5, 1)
+    return __uint_as_float(__float_as_uint(unit) + ((uint32_t)(j < 50 ? j : 50) << 23));
+}
+__device__ __forceinline__ float inverse_of_power(float x) { return __uint_as_float((254u << 23) - __float_as_uint(x)); }
+__device__ __forceinline__ float bound_after(float n, float a, float b, float c) {
+    return n < 1.f ? n * (fabsf(a) + n * n * (fabsf(b) + n * n * fabsf(c))) : n;
+}
+// What the epilogues of a step multiply by, for each of the first kScaled steps, for those behind them (X is kept times
+// `unit` there) and for the last one: .x the Gram matrix, .y the application.
+constexpr int kScaled = 32;
+__device__ __forceinline__ int scales_of(int k, int steps) { return k + 1 == steps ? kScaled + 1 : k < kScaled ? k : kScaled; }
+
 // X0 = G * 2^-k in 11 significant bits, k such that the values' root mean square is about 1: exact for bfloat16 (8 bits)
-// down to 2^-14 of it. What is missing to G / (|G| + eps), f = 2^k / (|G| + eps), and f^2, go into the first step's epilogues.
+// down to 2^-14 of it. What is missing to G / (|G| + eps), f = 2^k / (|G| + eps), and f^2, go into the first step's epilogues:
+// scales [kScaled + 2][count] holds the factors of all steps.
+struct Polynomial {
+    int steps;
+    float a, b, c, unit;
+};
 __global__ void __launch_bounds__(kNormThreads) k_ns_cast(Source g, const double* part, int parts, float eps, __half* x, int64_t ldx,
-                                                          float2* factor) {
+                                                          Polynomial p, float2* scales) {
     wait_for_predecessor();
     let_successor_start();
     __shared__ double s_sum[kNormThreads / 32];
@@ -104,7 +126,16 @@ __global__ void __launch_bounds__(kNormThreads) k_ns_cast(Source g, const double
         s_scale = ldexpf(1.f, -k);
         if (blockIdx.x == 0) {
             const double f = norm == 0.0 ? 0.0 : ldexp(1.0, k) / (norm + eps);  // of nothing: 1 / eps, whose square may pass 32 bits
-            factor[blockIdx.y] = make_float2((float)f, (float)(f * f));
+            float2* to = scales + blockIdx.y;
+            float n = (float)(norm / (norm + eps)), gram = (float)(f * f), from = (float)f;  // from: 1 / what X is kept times
+            for (int i = 0; i < kScaled && i + 1 < p.steps; ++i) {
+                n = bound_after(n, p.a, p.b, p.c);
+                const float times = i + 1 < kScaled ? kept_times(n, p.unit) : p.unit;
+                to[(int64_t)i * gridDim.y] = make_float2(gram, from * times);
+                from = inverse_of_power(times), gram = from * from;
+            }
+            to[(int64_t)kScaled * gridDim.y] = make_float2(1.f / (p.unit * p.unit), 1.f);
+            to[(int64_t)(kScaled + 1) * gridDim.y] = make_float2(gram, from);
         }
     }
     __syncthreads();
@@ -144,13 +175,11 @@ struct EpiGram {
         float* diag;  // [count][s]
         int64_t ld, batch_ld;
         int s;
-        float factor;
-        const float2* first;  // the first step's f^2, or NULL
         float* part;          // where K is cut: the sums of this part [count][s][ld_part], else NULL
         int64_t ld_part;
     };
     template <int W, bool CUT>
-    static __device__ __forceinline__ void tile(const Args& a, uint32_t acc, int row, int col, const TileAt& at, const StepTurn& turn) {
+    static __device__ __forceinline__ void tile(const Args& a, uint32_t acc, int row, int col, const TileAt& at, const StepTurn& turn, float f) {
         if constexpr (CUT) {
             float* out = a.part + (int64_t)at.b * a.s * a.ld_part;
 #pragma unroll 1
@@ -161,7 +190,6 @@ struct EpiGram {
             }
             return;
         }
-        const float f = a.first ? a.first[at.b].y : a.factor;
         uint16_t* out = reinterpret_cast<uint16_t*>(a.out + at.b * a.batch_ld);
 #pragma unroll 1
         for (int c = 0; c < W && col + c < a.s; c += 64) {
@@ -180,8 +208,7 @@ struct EpiGram {
         }
     }
     // Joins the parts of a row's sums, in order, from the diagonal's block on. Run by a warp.
-    static __device__ __forceinline__ void join(const Args& a, int parts, int64_t stride, int b, int row, int block, int lane) {
-        const float f = a.first ? a.first[b].y : a.factor;
+    static __device__ __forceinline__ void join(const Args& a, int parts, int64_t stride, int b, int row, int block, int lane, float f) {
         const float* from = a.part + ((int64_t)b * a.s + row) * a.ld_part;
         __half* to = a.out + b * a.batch_ld + (int64_t)row * a.ld;
         for (int c = row / block * block + 4 * lane; c < a.s; c += 128) {
@@ -278,15 +305,12 @@ struct EpiApply {
         uint16_t* out;
         int64_t ld, batch_ld;
         int m, n;
-        float factor;
-        const float2* first;  // the first step's f, or NULL
         const float* regain;  // [count][s]: of the rows, or (tall) of the columns
         bool f16, wide;
     };
     template <int W, bool TALL>
-    static __device__ __forceinline__ void tile(const Args& a, uint32_t acc, int row, int col, const TileAt& at, const StepTurn& turn, float own) {
+    static __device__ __forceinline__ void tile(const Args& a, uint32_t acc, int row, int col, const TileAt& at, const StepTurn& turn, float f) {
         const float* regain = a.regain + (int64_t)at.b * a.n;
-        const float f = (a.first ? a.factor * a.first[at.b].x : a.factor) * own;
 #pragma unroll 1
         for (int c = 0; c < W && col + c < a.n; c += 64) {
             float v[64], r0 = 1.f, r1 = 1.f;
@@ -321,11 +345,11 @@ struct StepsArgs {
     float *diag, *regain, *part;
     int64_t ld_part, part_stride;
     bool tall;
-    float a, b, c, unit;  // unit: X is kept times this between the steps
+    float a, b, c;
     __half *x[2], *gram, *poly;
     uint16_t* out;
     int64_t ldx, xs, lds, ss;
-    const float2* factor;
+    const float2* scales;  // [kScaled + 2][count]
     unsigned* counter;
     bool wide;
 };
@@ -440,11 +464,11 @@ __global__ void __launch_bounds__(kMatThreads<kStepWarps>, 1) k_ns_steps(const _
         for (int round = 0; round < rounds; ++round) {  // a warp that gave up still comes to the barrier below
             const int which = which_of(round), k = round / per_step, buf = k & 1, total = tiles_in(which);
             if (ok && round) ok = __all_sync(0xFFFFFFFFu, bar_wait(round_bar, (round - 1) & 1, &g_wait_expired));
-            const float2* start = k == 0 ? p.factor : nullptr;
-            EpiGram::Args eg = {p.gram, p.diag, p.lds, p.ss, p.s, 1.f / (p.unit * p.unit), start, p.part, p.ld_part};
+            const float2* scales = p.scales + (int64_t)scales_of(k, p.steps) * p.count;
+            EpiGram::Args eg = {p.gram, p.diag, p.lds, p.ss, p.s, p.part, p.ld_part};
             if (CUT && ok && which == 3)
                 for (int i = blockIdx.x * kStepWarps + warp - 4; i < p.count * p.s; i += gridDim.x * kStepWarps)
-                    EpiGram::join(eg, p.parts, p.part_stride, i / p.s, i % p.s, BN, lane);
+                    EpiGram::join(eg, p.parts, p.part_stride, i / p.s, i % p.s, BN, lane, scales[i / p.s].x);
             for (int t = first; ok && t < total; t += step) {
                 int k0, nk, cut;
                 const TileAt at = tile_of(which, t, k0, nk, cut);
@@ -454,6 +478,7 @@ __global__ void __launch_bounds__(kMatThreads<kStepWarps>, 1) k_ns_steps(const _
                 uint4 q[8];
                 // what the epilogue needs of the round before, asked for while the tile is multiplied
                 float own = 1.f;
+                const float2 scale = scales[at.b];
                 if (which == 1) EpiPoly::load(ep, row, col, at, turn, q);
                 if (row < p.s && (which == 1 || (which == 2 && !TALL)))
                     own = __ldcg((which == 1 ? p.diag : p.regain) + (int64_t)at.b * p.s + row);
@@ -463,17 +488,16 @@ __global__ void __launch_bounds__(kMatThreads<kStepWarps>, 1) k_ns_steps(const _
                 mma_fence_after();
                 if (which == 0) {
                     if (CUT) eg.part = p.part + cut * p.part_stride;
-                    EpiGram::tile<BN / 2, CUT>(eg, tmem, row, col, at, turn);
+                    EpiGram::tile<BN / 2, CUT>(eg, tmem, row, col, at, turn, scale.x);
                 } else if (which == 1) {
                     EpiPoly::tile<BN / 2>(ep, tmem, row, col, at, turn, q, own);
                 } else {
-                    EpiApply::Args e = {reinterpret_cast<uint16_t*>(p.x[1 - buf]), p.ldx, p.xs, p.m, p.n, start ? p.unit : 1.f, start, p.regain, true, true};
+                    EpiApply::Args e = {reinterpret_cast<uint16_t*>(p.x[1 - buf]), p.ldx, p.xs, p.m, p.n, p.regain, true, true};
                     if (k + 1 == p.steps) {
                         e.out = p.out, e.ld = p.n, e.batch_ld = (int64_t)p.m * p.n;
-                        e.factor = start ? 1.f : 1.f / p.unit;
                         e.f16 = false, e.wide = p.wide;
                     }
-                    EpiApply::tile<BN / 2, TALL>(e, tmem, row, col, at, turn, own);
+                    EpiApply::tile<BN / 2, TALL>(e, tmem, row, col, at, turn, scale.y * own);
                 }
                 free_accumulator<CG>(free_at + 8 * acc, lane);
                 if (++acc == 2) acc = 0, aph ^= 1;
@@ -508,7 +532,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, c
     __shared__ __align__(8) uint64_t s_bar;
     __shared__ uint32_t s_tmem;
     __shared__ double s_sum[kSmallThreads / 32];
-    __shared__ float s_scale, s_factor, s_regain[128], s_diag[128];
+    __shared__ float s_scale, s_factor, s_bound, s_regain[128], s_diag[128];
     __shared__ double s_share;
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const bool tall = g.m > g.n;
@@ -576,6 +600,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, c
         k = k < -120 ? -120 : k > 120 ? 120 : k;
         s_scale = ldexpf(1.f, -k);
         s_factor = norm == 0.0 ? 0.f : (float)(ldexp(1.0, k) / (norm + p.eps));  // as in k_ns_cast
+        s_bound = (float)(norm / (norm + p.eps));
     }
     __syncthreads();
     const float scale = s_scale, factor = s_factor;
@@ -646,8 +671,9 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, c
                            Half16::pack(e[8 * c + 4], e[8 * c + 5], f16), Half16::pack(e[8 * c + 6], e[8 * c + 7], f16));
     };
     ready();
+    float bound = s_bound, back = factor;  // of |X|; 1 / what X is kept times
     for (int k = 0; k < p.steps; ++k) {
-        const float f = k == 0 ? factor * factor : 1.f / (p.unit * p.unit);
+        const float f = back * back;
         square(x_at, blocks);
         wait();
         float v[32];
@@ -743,9 +769,11 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, c
             }
             __syncwarp();
         }
-        wait();
         const bool last = k + 1 == p.steps;
-        const float fx = (k == 0 ? factor : 1.f / p.unit) * (last ? 1.f : p.unit) * s_regain[row];
+        bound = bound_after(bound, p.a, p.b, p.c);
+        const float times = last ? 1.f : kept_times(bound, p.unit), fx = back * times * s_regain[row];
+        back = inverse_of_power(times);
+        wait();
         for (int n = part; n < 2 * blocks; n += kSmallThreads / 128) {
             tmem_load(tmem + 32 * n + lanes, v);
 #pragma unroll
@@ -821,7 +849,7 @@ Plan plan_of(int m, int n, int count) {
 }
 
 struct Layout {
-    size_t counter, factor, sums, x0, x1, gram, poly, diag, regain, part, total;
+    size_t counter, scales, sums, x0, x1, gram, poly, diag, regain, part, total;
     int64_t ldx, lds, ld_part;
     int s;
     Plan plan;
@@ -846,7 +874,7 @@ Layout layout(int32_t count, int32_t m, int32_t n) {
         return here;
     };
     L.counter = take(256);
-    L.factor = take((size_t)count * sizeof(float2));
+    L.scales = take((size_t)(kScaled + 2) * count * sizeof(float2));
     L.sums = take((size_t)(count > kNormBlocks ? count : kNormBlocks) * 8);
     L.x0 = take((size_t)count * m * L.ldx * 2);
     L.x1 = take((size_t)count * m * L.ldx * 2);
@@ -970,7 +998,7 @@ int ones_orthogonalize(const void* d_g, int64_t ldg, int64_t stride, int32_t cou
     if (workspace_bytes < L.total) return ONES_ERR_WORKSPACE;
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
     char* ws = static_cast<char*>(d_workspace);
-    float2* factor = reinterpret_cast<float2*>(ws + L.factor);
+    float2* scales = reinterpret_cast<float2*>(ws + L.scales);
     double* sums = reinterpret_cast<double*>(ws + L.sums);
     __half* x[2] = {reinterpret_cast<__half*>(ws + L.x0), reinterpret_cast<__half*>(ws + L.x1)};
     __half* gram = reinterpret_cast<__half*>(ws + L.gram);
@@ -978,8 +1006,7 @@ int ones_orthogonalize(const void* d_g, int64_t ldg, int64_t stride, int32_t cou
     unsigned* counter = reinterpret_cast<unsigned*>(ws + L.counter);
     const bool wide = n % 8 == 0 && aligned(d_g, 16) && ldg * size % 16 == 0 && stride * size % 16 == 0;
     const Source src = {d_g, ldg, count > 1 ? stride : 0, m, n, type, wide};
-    // Between the steps X is kept times 2^q, about the square root of the longer side, which brings its values near 1:
-    // after the last step they are about 1 / 2^q, before the first about 1 / sqrt(m n).
+    // see kept_times: after the last step X's values are about 1 / 2^q, before the first about 1 / sqrt(m n)
     int q = 0;
     while ((int64_t)1 << (2 * (q + 1)) <= (m > n ? m : n)) ++q;
     const float unit = ldexpf(1.f, q);
@@ -995,14 +1022,13 @@ int ones_orthogonalize(const void* d_g, int64_t ldg, int64_t stride, int32_t cou
     cudaError_t err = cudaGetLastError();
     if (err == cudaSuccess)
         err = launch_after(k_ns_cast, dim3(blocks, count), dim3(kNormThreads), stream, src, static_cast<const double*>(sums), blocks, eps,
-                           x[0], L.ldx, factor);
+                           x[0], L.ldx, Polynomial{steps, a, b, c, unit}, scales);
     StepsArgs p = {};
     p.m = m, p.n = n, p.s = L.s, p.count = count, p.steps = steps, p.tall = m > n;
     p.a = a, p.b = b, p.c = c;
-    p.unit = unit;
     p.x[0] = x[0], p.x[1] = x[1], p.gram = gram, p.poly = poly, p.out = static_cast<uint16_t*>(d_out);
     p.ldx = L.ldx, p.xs = (int64_t)m * L.ldx, p.lds = L.lds, p.ss = (int64_t)L.s * L.lds;
-    p.factor = factor, p.counter = counter;
+    p.scales = scales, p.counter = counter;
     p.parts = L.plan.parts;
     p.diag = reinterpret_cast<float*>(ws + L.diag), p.regain = reinterpret_cast<float*>(ws + L.regain);
     p.part = L.plan.parts > 1 ? reinterpret_cast<float*>(ws + L.part) : nullptr;

@@ -67,3 +67,24 @@ def test_orthogonalize_zero_at_any_eps(m, n, dtype):
         o = train.orthogonalize(g, eps=eps)
         assert not bool(o[0].any()) and bool(torch.isfinite(o[1]).all()) and bool(o[1].any())
         assert not bool(train.orthogonalize(g[0], eps=eps).any())
+
+
+@pytest.mark.parametrize("m,n", FORMS)
+@pytest.mark.parametrize("ratio", [1e-3, 1e-5, 5e-7, 1e-9, 1e-12])
+def test_orthogonalize_small_beside_eps(m, n, ratio):
+    g = randn(m, n)
+    check_ns(g * (ratio * 1e-7 / g.norm()))
+    check_ns(g * (ratio / g.norm()), steps=2, eps=1.0)
+    check_ns(g * (ratio / g.norm()), steps=10, coefficients=(1.5, -0.5, 0.0), eps=1.0)
+
+
+def test_orthogonalize_each_matrix_has_its_own_scale():
+    from paper_2108_03645_b200 import train
+    for m, n in FORMS:
+        g = torch.stack([randn(m, n, seed=k) for k in range(4)])
+        g *= torch.tensor([1.0, 1e-11, 0.0, 1e-14], device="cuda")[:, None, None]
+        o = train.orthogonalize(g)
+        assert not bool(o[2].any())
+        for a, b in zip(g[[0, 1, 3]], o[[0, 1, 3]]):
+            want = ns_reference(a, 5, (3.4445, -4.7750, 2.0315), 1e-7)
+            assert float((b.double() - want).norm()) <= (2.0 ** -9 + 15 * 2.0 ** -11) * float(want.norm())
