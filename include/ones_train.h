@@ -88,10 +88,11 @@ int ones_linear_ce_backward(const float* d_dloss, const void* d_hidden, int64_t 
  *   X = G / (|G|_F + eps);   `steps` times:  A = X X^T,  X <- (a I + b A + c A^2) X      (on the shorter side)
  * which moves every singular value of G towards 1 (for the usual coefficients a, b, c: into about [0.7, 1.2]).
  *   d_g of `type` (any of the three), any alignment of its elements; d_out [count][m][n] of bfloat16, rows n apart.
- *   steps >= 1, eps > 0, finite coefficients, sizes >= 1.
+ *   1 <= steps <= ONES_UPDATE_MAX_STEPS (one launch runs them all), eps > 0, finite coefficients, sizes >= 1.
  * Products run on 16-bit operands (11 significant bits, scaled into range, also where |G| is down to 2^-50 of eps) with
  * 32-bit accumulators; the norm is summed in 64 bits.
  *   d_workspace  at least ones_orthogonalize_workspace_bytes(count, m, n) bytes, 256-byte aligned. */
+#define ONES_UPDATE_MAX_STEPS 1024
 size_t ones_orthogonalize_workspace_bytes(int32_t count, int32_t m, int32_t n);
 int ones_orthogonalize(const void* d_g, int64_t ldg, int64_t stride, int32_t count, int32_t m, int32_t n, int32_t type,
                        int32_t steps, float a, float b, float c, float eps, void* d_out, void* d_workspace,

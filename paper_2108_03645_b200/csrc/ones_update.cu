@@ -988,7 +988,7 @@ size_t ones_orthogonalize_workspace_bytes(int32_t count, int32_t m, int32_t n) {
 int ones_orthogonalize(const void* d_g, int64_t ldg, int64_t stride, int32_t count, int32_t m, int32_t n, int32_t type,
                        int32_t steps, float a, float b, float c, float eps, void* d_out, void* d_workspace,
                        size_t workspace_bytes, void* cuda_stream) {
-    if (bad_sizes(count, m, n) || type < ONES_F32 || type > ONES_F16 || steps < 1 || !(eps > 0.f) || !isfinite(eps) ||
+    if (bad_sizes(count, m, n) || type < ONES_F32 || type > ONES_F16 || steps < 1 || steps > ONES_UPDATE_MAX_STEPS || !(eps > 0.f) || !isfinite(eps) ||
         !isfinite(a) || !isfinite(b) || !isfinite(c) || ldg < n || (count > 1 && stride < 0))
         return ONES_ERR_BAD_PARAM;
     if (!d_g || !d_out || !d_workspace) return ONES_ERR_NULL;

@@ -88,3 +88,14 @@ def test_orthogonalize_each_matrix_has_its_own_scale():
         for a, b in zip(g[[0, 1, 3]], o[[0, 1, 3]]):
             want = ns_reference(a, 5, (3.4445, -4.7750, 2.0315), 1e-7)
             assert float((b.double() - want).norm()) <= (2.0 ** -9 + 15 * 2.0 ** -11) * float(want.norm())
+
+
+def test_orthogonalize_many_steps():
+    """As many as are taken, and none beyond: the small coefficients make X decay, the second set holds it at 1."""
+    from paper_2108_03645_b200 import binding, train
+    for m, n in FORMS:
+        check_ns(randn(m, n), steps=60, coefficients=(0.9, 0.0, 0.0))
+        s = torch.linalg.svdvals(train.orthogonalize(randn(m, n), steps=1024, coefficients=(1.5, -0.5, 0.0)).double())
+        assert float(s.max()) < 1.02
+        with pytest.raises(binding.OnesError):
+            train.orthogonalize(randn(m, n), steps=1025)

@@ -1,0 +1,10 @@
+"""Arguments that the training-step operators refuse, without a device: each is turned into an error before any launch."""
+import pytest
+
+from test_train_abi import ALIGN, P, PARAM, _lib  # noqa: F401
+
+
+@pytest.mark.parametrize("m,n", [(200, 200), (64, 64), (64, 4000)])
+@pytest.mark.parametrize("steps", [1025, 1 << 29, (1 << 31) - 1])
+def test_orthogonalize_refuses_steps_without_end(m, n, steps):
+    assert _lib().ones_orthogonalize(P, n, m * n, 1, m, n, 0, steps, 3.4445, -4.775, 2.0315, 1e-7, P, P, 1 << 24, None) == PARAM
