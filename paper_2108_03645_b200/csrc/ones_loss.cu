@@ -674,12 +674,7 @@ bool bad_sizes(int32_t rows, int32_t cols, int32_t vocab) {
 
 }  // namespace
 
-cudaError_t loss_wait_expired(unsigned* out) {
-    cudaError_t err = cudaMemcpyFromSymbol(out, g_wait_expired, sizeof(*out));
-    const unsigned zero = 0;
-    if (err == cudaSuccess && *out) err = cudaMemcpyToSymbol(g_wait_expired, &zero, sizeof(zero));
-    return err;
-}
+const WaitControl loss_waits = {take_expired, limit_waits, wait_for_nothing};
 
 }  // namespace ones
 

@@ -7,8 +7,12 @@
 
 namespace ones {
 
-// Every wait on an mbarrier ends: after this many nanoseconds without the phase completing, the waiter gives up.
-constexpr uint64_t kWaitLimitNs = 4000000000ull;
+// Every wait ends: after this many nanoseconds without what it waits for, the waiter gives up, and does not wait again in
+// its kernel. A translation unit has its own limit and its own flag, which kernels set when a wait has run out.
+constexpr unsigned long long kWaitLimitNs = 4000000000ull;
+static __device__ unsigned long long g_wait_limit = kWaitLimitNs;
+static __device__ unsigned g_wait_expired;
+constexpr uint64_t kShortWaitNs = 20000;  // the limit is not looked at before: that is an access to memory
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -116,18 +120,28 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     return ok != 0;
 }
 
-// Waits for the phase of the given parity; false (and *expired set) when it has not come within kWaitLimitNs.
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, unsigned* expired) {
+// Waits for the phase of the given parity; false (and the flag set) when it has not come within the limit.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
     if (bar_try(bar, parity)) return true;
     const uint64_t begin = now_ns();
     while (!bar_try(bar, parity)) {
-        if (now_ns() - begin > kWaitLimitNs) {
-            atomicExch(expired, 1u);
+        const uint64_t waited = now_ns() - begin;
+        if (waited > kShortWaitNs && waited > g_wait_limit) {
+            atomicExch(&g_wait_expired, 1u);
             return false;
         }
     }
     return true;
 }
+// The waits of a thread that comes by again and again: after one that ran out, a look is all. That is asked only where the
+// first look has found nothing: asked before it, a pass over 8192 rows of 2048 takes 22.4 us instead of 22.1.
+struct Waits {
+    bool ok = true;
+    __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) {
+        if (bar_try(bar, parity)) return true;
+        return ok = ok && bar_wait(bar, parity);
+    }
+};
 
 // After a wait that ran out, copies and products may still be on their way: gives them time before their memory goes.
 __device__ __forceinline__ void let_copies_end() {
@@ -142,8 +156,8 @@ __device__ __forceinline__ void arrive_all(unsigned* counter) {
     asm volatile("fence.proxy.async;" ::: "memory");  // the others read by TMA
     asm volatile("red.relaxed.gpu.global.add.u32 [%0], 1;" ::"l"(counter) : "memory");
 }
-// Waits (a whole warp) until the counter has reached `target`; false when that has not come within kWaitLimitNs.
-__device__ __forceinline__ bool wait_all(const unsigned* counter, unsigned target, unsigned* expired) {
+// Waits (a whole warp) until the counter has reached `target`; false when that has not come within the limit.
+__device__ __forceinline__ bool wait_all(const unsigned* counter, unsigned target) {
     bool ok = true;
     if (threadIdx.x % 32 == 0) {
         uint64_t begin = 0;
@@ -153,8 +167,8 @@ __device__ __forceinline__ bool wait_all(const unsigned* counter, unsigned targe
             if ((int)(v - target) >= 0) break;
             const uint64_t now = now_ns();
             if (!begin) begin = now;
-            if (now - begin > kWaitLimitNs) {
-                atomicExch(expired, 1u);
+            if (now - begin > kShortWaitNs && now - begin > g_wait_limit) {
+                atomicExch(&g_wait_expired, 1u);
                 ok = false;
                 break;
             }
@@ -166,6 +180,40 @@ __device__ __forceinline__ bool wait_all(const unsigned* counter, unsigned targe
     asm volatile("fence.proxy.async;" ::: "memory");
     return ok;
 }
+
+// One warp that waits `times` times for what nobody sends: shows that waits end, once for all, and that the flag is set.
+static __global__ void k_wait_for_nothing(int times) {
+    __shared__ __align__(8) uint64_t s_bar;
+    if (threadIdx.x == 0) {
+        bar_init(smem_u32(&s_bar), 1);
+        bar_init_done();
+    }
+    __syncwarp();
+    Waits wait;
+    for (int i = 0; i < times; ++i) wait(smem_u32(&s_bar), 0);
+}
+
+// A translation unit's waits, seen from the host.
+static inline cudaError_t take_expired(unsigned* out) {  // reads and clears the flag
+    cudaError_t err = cudaMemcpyFromSymbol(out, g_wait_expired, sizeof(*out));
+    const unsigned zero = 0;
+    if (err == cudaSuccess && *out) err = cudaMemcpyToSymbol(g_wait_expired, &zero, sizeof(zero));
+    return err;
+}
+static inline cudaError_t limit_waits(unsigned long long ns) {  // 0: the default
+    if (!ns) ns = kWaitLimitNs;
+    return cudaMemcpyToSymbol(g_wait_limit, &ns, sizeof(ns));
+}
+static inline cudaError_t wait_for_nothing(int times, cudaStream_t stream) {
+    k_wait_for_nothing<<<1, 32, 0, stream>>>(times);
+    return cudaGetLastError();
+}
+struct WaitControl {
+    cudaError_t (*expired)(unsigned*);
+    cudaError_t (*limit)(unsigned long long);
+    cudaError_t (*nothing)(int, cudaStream_t);
+};
+extern const WaitControl norm_waits, loss_waits, update_waits;
 
 // ---- TMA ----
 __device__ __forceinline__ void tma_prefetch(const CUtensorMap* map) {

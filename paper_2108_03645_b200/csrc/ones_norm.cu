@@ -225,8 +225,6 @@ __device__ __forceinline__ void group_sync(int group) {
         asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(TPR) : "memory");
 }
 
-__device__ unsigned g_wait_expired;
-
 template <class T, int TPR, int NV>
 __global__ void __launch_bounds__(kRingThreads, 1)
     k_norm_ring(const NormIn a, void* y_, int64_t ldy, float* mean_out, float* rstd_out, int stages) {
@@ -262,10 +260,9 @@ __global__ void __launch_bounds__(kRingThreads, 1)
     const float inv = 1.f / a.cols;
     int st = 0, turn = 0;
     uint32_t ph = 0;
-    bool bad = false;
+    Waits wait;
     for (int64_t row = first; row < a.rows; row += step, turn ^= 1) {
-        const bool ok = bar_wait(full + 8 * st, ph, &g_wait_expired);
-        bad = bad || !ok;
+        const bool ok = wait(full + 8 * st, ph);
         Pair v[R][NV][P];
         float sum[R], sq[R];
 #pragma unroll
@@ -325,7 +322,7 @@ __global__ void __launch_bounds__(kRingThreads, 1)
         }
         if (++st == stages) st = 0, ph ^= 1;
     }
-    if (bad) let_copies_end();
+    if (!wait.ok) let_copies_end();
 }
 
 // ---- rows on other boundaries ----
@@ -540,10 +537,9 @@ __global__ void __launch_bounds__(kRingThreads, 1)
     const float inv = 1.f / a.cols;
     int st = 0, turn = 0;
     uint32_t ph = 0;
-    bool bad = false;
+    Waits wait;
     for (int64_t row = first; row < a.rows; row += step, turn ^= 1) {
-        const bool ok = bar_wait(full + 8 * st, ph, &g_wait_expired);
-        bad = bad || !ok;
+        const bool ok = wait(full + 8 * st, ph);
         Pair v[R][NU];
         float sum[R], sq[R];
 #pragma unroll
@@ -590,7 +586,7 @@ __global__ void __launch_bounds__(kRingThreads, 1)
         }
         if (++st == stages) st = 0, ph ^= 1;
     }
-    if (bad) let_copies_end();
+    if (!wait.ok) let_copies_end();
 }
 
 // Rows longer than the registers of a block hold: three passes, the second and third from the caches.
@@ -801,7 +797,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_ring(const NormBa
     const float inv = 1.f / a.cols;
     int st = 0, turn = 0;
     uint32_t ph = 0;
-    bool bad = false;
+    Waits wait;
     float nmean[R], nrstd[R];
     auto statistics = [&](int64_t row) {
 #pragma unroll
@@ -814,8 +810,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_ring(const NormBa
 #pragma unroll
         for (int r = 0; r < R; ++r) mean[r] = nmean[r], rstd[r] = nrstd[r];
         statistics(row + step);
-        const bool ok = bar_wait(full + 8 * st, ph, &g_wait_expired);
-        bad = bad || !ok;
+        const bool ok = wait(full + 8 * st, ph);
         Chunk<T> x[R][NV], dy[R][NV];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -864,7 +859,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_ring(const NormBa
         }
         if (++st == stages) st = 0, ph ^= 1;
     }
-    if (bad) let_copies_end();
+    if (!wait.ok) let_copies_end();
     if (a.part) {
         float* out = a.part + (int64_t)blockIdx.x * 2 * a.cols;
         float* own = kGroups > 1 ? reinterpret_cast<float*>(ring) + group * 2 * a.cols : out;  // the ring has done its work
@@ -916,7 +911,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_odd(const NormBac
     const float inv = 1.f / a.cols;
     int st = 0, turn = 0;
     uint32_t ph = 0;
-    bool bad = false;
+    Waits wait;
     float nmean = 0.f, nrstd = 0.f;
     auto statistics = [&](int64_t row) {
         if (row < a.rows) nmean = a.mean[row], nrstd = a.rstd[row];
@@ -925,8 +920,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_odd(const NormBac
     for (int64_t row = first; row < a.rows; row += step, turn ^= 1) {
         const float mean = nmean, rstd = nrstd;
         statistics(row + step);
-        const bool ok = bar_wait(full + 8 * st, ph, &g_wait_expired);
-        bad = bad || !ok;
+        const bool ok = wait(full + 8 * st, ph);
         Unit<T> xq[NU], dq[NU];
         x.read((int)row, mine + st * 2 * place, span, lane, a.cols, xq);
         dy.read((int)row, mine + st * 2 * place + place, span, lane, a.cols, dq);
@@ -950,7 +944,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_odd(const NormBac
                            [&](int u) { return fma2(xq[u].get() + minus, c2, fma2(dq[u].get() * w[u], scale, c1)); });
         if (++st == stages) st = 0, ph ^= 1;
     }
-    if (bad) let_copies_end();
+    if (!wait.ok) let_copies_end();
     if (a.part) {
         float* out = a.part + (int64_t)blockIdx.x * 2 * a.cols;
         float* own = kGroups > 1 ? reinterpret_cast<float*>(ring) + group * 2 * a.cols : out;  // the ring has done its work
@@ -1221,12 +1215,7 @@ bool is_wide(const void* p, int64_t ld, int cols, int32_t type) {
 
 }  // namespace
 
-cudaError_t norm_wait_expired(unsigned* out) {
-    cudaError_t err = cudaMemcpyFromSymbol(out, g_wait_expired, sizeof(*out));
-    const unsigned zero = 0;
-    if (err == cudaSuccess && *out) err = cudaMemcpyToSymbol(g_wait_expired, &zero, sizeof(zero));
-    return err;
-}
+const WaitControl norm_waits = {take_expired, limit_waits, wait_for_nothing};
 
 }  // namespace ones
 

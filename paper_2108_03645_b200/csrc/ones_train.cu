@@ -47,11 +47,32 @@ cudaError_t make_map(CUtensorMap* out, const Operand& o, int rows, int k, int ba
 
 }  // namespace ones
 
-extern "C" int ones_train_status(void* cuda_stream) {
-    if (cudaStreamSynchronize(reinterpret_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) return ONES_ERR_CUDA;
-    unsigned a = 0, b = 0, c = 0;
-    if (ones::norm_wait_expired(&a) != cudaSuccess || ones::loss_wait_expired(&b) != cudaSuccess ||
-        ones::update_wait_expired(&c) != cudaSuccess)
-        return ONES_ERR_CUDA;
-    return a || b || c ? ONES_ERR_TIMEOUT : ONES_OK;
+namespace {
+const ones::WaitControl* const kWaits[] = {&ones::norm_waits, &ones::loss_waits, &ones::update_waits};
 }
+
+extern "C" {
+
+int ones_train_status(void* cuda_stream) {
+    if (cudaStreamSynchronize(reinterpret_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) return ONES_ERR_CUDA;
+    unsigned any = 0;
+    for (const ones::WaitControl* w : kWaits) {
+        unsigned expired = 0;
+        if (w->expired(&expired) != cudaSuccess) return ONES_ERR_CUDA;
+        any |= expired;
+    }
+    return any ? ONES_ERR_TIMEOUT : ONES_OK;
+}
+
+int ones_train_wait_limit(unsigned long long ns) {
+    for (const ones::WaitControl* w : kWaits)
+        if (w->limit(ns) != cudaSuccess) return ONES_ERR_CUDA;
+    return ONES_OK;
+}
+
+int ones_train_wait_for_nothing(int which, int times, void* cuda_stream) {
+    if (which < 0 || which > 2) return ONES_ERR_BAD_PARAM;
+    return kWaits[which]->nothing(times, reinterpret_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? ONES_OK : ONES_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -9,11 +9,6 @@ namespace ones {
 
 inline bool aligned(const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
-// Read and clear the flags that kernels set when they give up waiting.
-cudaError_t norm_wait_expired(unsigned* out);
-cudaError_t loss_wait_expired(unsigned* out);
-cudaError_t update_wait_expired(unsigned* out);
-
 // Lets the kernel use `bytes` of dynamic shared memory on the current device; `ready` holds the devices that know.
 template <class F>
 cudaError_t allow_smem(F kernel, int bytes, std::atomic<uint64_t>& ready) {
@@ -43,3 +38,8 @@ cudaError_t launch_after(void (*kernel)(P...), dim3 grid, dim3 block, cudaStream
 }
 
 }  // namespace ones
+
+// For tests, beside the public functions: the limit of every wait on the current device (0: the default), and a kernel of one
+// of the three files (0 to 2) that waits `times` times for what never comes.
+extern "C" int ones_train_wait_limit(unsigned long long ns);
+extern "C" int ones_train_wait_for_nothing(int which, int times, void* cuda_stream);

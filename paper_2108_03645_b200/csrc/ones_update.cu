@@ -429,7 +429,7 @@ __global__ void __launch_bounds__(kMatThreads<kStepWarps>, 1) k_ns_steps(const _
         Ring r = {w.base, w.full, w.empty};
         for (int round = 0; ok && round < rounds; ++round) {
             const int which = which_of(round), buf = round / per_step & 1, total = tiles_in(which);
-            if (round && !(ok = wait_all(p.counter, (unsigned)round * gridDim.x, &g_wait_expired))) break;
+            if (round && !(ok = wait_all(p.counter, (unsigned)round * gridDim.x))) break;
             if (round && lane == 0) bar_arrive(round_bar);
             for (int t = first; ok && t < total; t += step) {
                 int k0, nk, cut;
@@ -449,7 +449,7 @@ __global__ void __launch_bounds__(kMatThreads<kStepWarps>, 1) k_ns_steps(const _
                 int k0, nk, cut;
                 View va, vb;
                 operands(maps, TALL, which, 0, tile_of(which, t, k0, nk, cut), va, vb);
-                if (!(ok = bar_wait(w.free_ + 8 * acc, aph ^ 1, &g_wait_expired))) break;
+                if (!(ok = bar_wait(w.free_ + 8 * acc, aph ^ 1))) break;
                 mma_fence_after();
                 ok = multiply_tile<CG>(r, w.tmem + acc * BN, nk, va, vb, true, w.done + 8 * acc);
                 if (++acc == 2) acc = 0, aph ^= 1;
@@ -463,7 +463,7 @@ __global__ void __launch_bounds__(kMatThreads<kStepWarps>, 1) k_ns_steps(const _
         uint32_t aph = 0;
         for (int round = 0; round < rounds; ++round) {  // a warp that gave up still comes to the barrier below
             const int which = which_of(round), k = round / per_step, buf = k & 1, total = tiles_in(which);
-            if (ok && round) ok = __all_sync(0xFFFFFFFFu, bar_wait(round_bar, (round - 1) & 1, &g_wait_expired));
+            if (ok && round) ok = __all_sync(0xFFFFFFFFu, bar_wait(round_bar, (round - 1) & 1));
             const float2* scales = p.scales + (int64_t)scales_of(k, p.steps) * p.count;
             EpiGram::Args eg = {p.gram, p.diag, p.lds, p.ss, p.s, p.part, p.ld_part};
             if (CUT && ok && which == 3)
@@ -482,7 +482,7 @@ __global__ void __launch_bounds__(kMatThreads<kStepWarps>, 1) k_ns_steps(const _
                 if (which == 1) EpiPoly::load(ep, row, col, at, turn, q);
                 if (row < p.s && (which == 1 || (which == 2 && !TALL)))
                     own = __ldcg((which == 1 ? p.diag : p.regain) + (int64_t)at.b * p.s + row);
-                ok = bar_wait(w.done + 8 * acc, aph, &g_wait_expired);
+                ok = bar_wait(w.done + 8 * acc, aph);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 mma_fence_after();
@@ -632,7 +632,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, c
     const uint32_t lanes = (uint32_t)quad << 21;
     const uint32_t idesc128 = instruction_desc(1, true, false, false, 128);
     uint32_t ph = 0;
-    bool ok = true;
+    Waits arrived;
     // What the threads wrote to shared memory is there for the tensor cores; one warp issues, all wait for the end.
     auto ready = [&] {
         asm volatile("fence.proxy.async;" ::: "memory");
@@ -641,7 +641,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, c
         mma_fence_after();
     };
     auto wait = [&] {
-        ok = bar_wait(bar, ph, &g_wait_expired) && ok;
+        arrived(bar, ph);
         ph ^= 1;
         mma_fence_after();
     };
@@ -792,7 +792,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ns_small(const Source g, c
             for (int c = lane; c < my_cols; c += 32) out[(int64_t)r * g.n + c] = *reinterpret_cast<const uint16_t*>(tall ? at(c, r) : at(r, c));
         }
     }
-    if (!ok) let_copies_end();
+    if (!arrived.ok) let_copies_end();
     __syncthreads();
     if (warp == 0) tmem_free<1>(tmem, cols);
     if constexpr (CL) cluster_sync_all();
@@ -967,12 +967,7 @@ bool bad_sizes(int32_t count, int32_t m, int32_t n) {
 
 }  // namespace
 
-cudaError_t update_wait_expired(unsigned* out) {
-    cudaError_t err = cudaMemcpyFromSymbol(out, g_wait_expired, sizeof(*out));
-    const unsigned zero = 0;
-    if (err == cudaSuccess && *out) err = cudaMemcpyToSymbol(g_wait_expired, &zero, sizeof(zero));
-    return err;
-}
+const WaitControl update_waits = {take_expired, limit_waits, wait_for_nothing};
 
 }  // namespace ones
 

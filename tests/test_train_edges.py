@@ -1,6 +1,7 @@
 """Training-step operators at the edges of what they accept, on the GPU: weights of the loss that differ by orders of
 magnitude, matrices that are small beside eps, infinities, second derivatives, waits that run out, row counts near 2^31; and
 the precision that the kernels claim. References are the definitions in 64 bits."""
+import ctypes as C
 import math
 
 import pytest
@@ -99,3 +100,32 @@ def test_orthogonalize_many_steps():
         assert float(s.max()) < 1.02
         with pytest.raises(binding.OnesError):
             train.orthogonalize(randn(m, n), steps=1025)
+
+
+# ---------------------------------------------------------------- waits that run out
+
+@pytest.mark.parametrize("which", [0, 1, 2])
+def test_a_wait_that_runs_out_is_reported_once_and_waited_for_once(which):
+    """A kernel of each file that waits a thousand times for what nobody sends: it spends one limit, not a thousand, the
+    status says so once, and what comes after it is as before."""
+    import time
+    from paper_2108_03645_b200 import binding, train
+    L = train.lib()
+    x, h = randn(300, 512), ce_inputs(40, 64, 300, BF16, 0.2)
+    everything = lambda: (*train.layer_norm(x), *train.linear_cross_entropy(*h[:3]), train.orthogonalize(x))  # noqa: E731
+    want = everything()
+    train.check()
+    assert L.ones_train_wait_limit(C.c_ulonglong(20_000_000)) == 0
+    try:
+        begin = time.monotonic()
+        assert L.ones_train_wait_for_nothing(which, 1000, C.c_void_p(torch.cuda.current_stream().cuda_stream)) == 0
+        torch.cuda.synchronize()
+        assert 0.02 <= time.monotonic() - begin < 2.0
+    finally:
+        assert L.ones_train_wait_limit(C.c_ulonglong(0)) == 0
+    with pytest.raises(binding.OnesError) as e:
+        train.check()
+    assert e.value.code == -9
+    train.check()
+    assert all(torch.equal(a, b) for a, b in zip(want, everything()))
+    train.check()
