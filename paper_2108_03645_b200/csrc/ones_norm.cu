@@ -149,6 +149,7 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* s, int group) {
 }
 
 constexpr int kNormSms = 148;  // the ring kernels have one block per SM of a B200
+constexpr int64_t kNoMore = (int64_t)1 << 40;  // beyond all rows: after a wait that ran out nothing is sent for any more
 
 struct NormIn {
     const void *x, *w, *b;
@@ -261,8 +262,9 @@ __global__ void __launch_bounds__(kRingThreads, 1)
     int st = 0, turn = 0;
     uint32_t ph = 0;
     Waits wait;
+    int64_t ahead = (int64_t)stages * step;  // of the row whose place is free, the next one for it
     for (int64_t row = first; row < a.rows; row += step, turn ^= 1) {
-        const bool ok = wait(full + 8 * st, ph);
+        if (!wait(full + 8 * st, ph)) ahead = kNoMore;
         Pair v[R][NV][P];
         float sum[R], sq[R];
 #pragma unroll
@@ -281,7 +283,7 @@ __global__ void __launch_bounds__(kRingThreads, 1)
         }
         row_sums<TPR, R>(sum, s[turn][0], group);
         // everybody has read these rows: their place is free
-        if (t == 0 && ok && row + (int64_t)stages * step < a.rows) fetch(row + (int64_t)stages * step, st);
+        if (t == 0 && row + ahead < a.rows) fetch(row + ahead, st);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             sum[r] *= inv;
@@ -538,8 +540,9 @@ __global__ void __launch_bounds__(kRingThreads, 1)
     int st = 0, turn = 0;
     uint32_t ph = 0;
     Waits wait;
+    int64_t ahead = (int64_t)stages * step;  // of the row whose place is free, the next one for it
     for (int64_t row = first; row < a.rows; row += step, turn ^= 1) {
-        const bool ok = wait(full + 8 * st, ph);
+        if (!wait(full + 8 * st, ph)) ahead = kNoMore;
         Pair v[R][NU];
         float sum[R], sq[R];
 #pragma unroll
@@ -555,7 +558,7 @@ __global__ void __launch_bounds__(kRingThreads, 1)
         }
         row_sums<TPR, R>(sum, s[turn][0], group);
         // everybody has read these rows: their place is free
-        if (t == 0 && ok && row + (int64_t)stages * step < a.rows) fetch(row + (int64_t)stages * step, st);
+        if (t == 0 && row + ahead < a.rows) fetch(row + ahead, st);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             sum[r] *= inv;
@@ -798,6 +801,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_ring(const NormBa
     int st = 0, turn = 0;
     uint32_t ph = 0;
     Waits wait;
+    int64_t ahead = (int64_t)stages * step;  // of the row whose place is free, the next one for it
     float nmean[R], nrstd[R];
     auto statistics = [&](int64_t row) {
 #pragma unroll
@@ -810,7 +814,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_ring(const NormBa
 #pragma unroll
         for (int r = 0; r < R; ++r) mean[r] = nmean[r], rstd[r] = nrstd[r];
         statistics(row + step);
-        const bool ok = wait(full + 8 * st, ph);
+        if (!wait(full + 8 * st, ph)) ahead = kNoMore;
         Chunk<T> x[R][NV], dy[R][NV];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -837,7 +841,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_ring(const NormBa
         }
         row_sums<TPR, 2 * R>(sum, s[turn], group);
         // everybody has read these rows: their place is free
-        if (t == 0 && ok && row + (int64_t)stages * step < a.rows) fetch(row + (int64_t)stages * step, st);
+        if (t == 0 && row + ahead < a.rows) fetch(row + ahead, st);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (R > 1 && row + r >= a.rows) break;
@@ -912,6 +916,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_odd(const NormBac
     int st = 0, turn = 0;
     uint32_t ph = 0;
     Waits wait;
+    int64_t ahead = (int64_t)stages * step;  // of the row whose place is free, the next one for it
     float nmean = 0.f, nrstd = 0.f;
     auto statistics = [&](int64_t row) {
         if (row < a.rows) nmean = a.mean[row], nrstd = a.rstd[row];
@@ -920,7 +925,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_odd(const NormBac
     for (int64_t row = first; row < a.rows; row += step, turn ^= 1) {
         const float mean = nmean, rstd = nrstd;
         statistics(row + step);
-        const bool ok = wait(full + 8 * st, ph);
+        if (!wait(full + 8 * st, ph)) ahead = kNoMore;
         Unit<T> xq[NU], dq[NU];
         x.read((int)row, mine + st * 2 * place, span, lane, a.cols, xq);
         dy.read((int)row, mine + st * 2 * place + place, span, lane, a.cols, dq);
@@ -937,7 +942,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_odd(const NormBac
         float sum[2] = {total(acc1), total(acc2)};
         row_sums<TPR, 2>(sum, s[turn], group);
         // everybody has read this row: its place is free
-        if (t == 0 && ok && row + (int64_t)stages * step < a.rows) fetch(row + (int64_t)stages * step, st);
+        if (t == 0 && row + ahead < a.rows) fetch(row + ahead, st);
         // dx = rstd * (dy * w - c1 - xh * c2)
         const Pair c1 = both(-rstd * sum[0] * inv), c2 = both(-rstd * rstd * sum[1] * inv);
         write_units<T, NU>(static_cast<T*>(a.dx) + row * a.lddx, span, lane, a.cols,
