@@ -120,7 +120,7 @@ __device__ __forceinline__ bool fill_tile(Ring& r, const View& va, const View& v
                                           uint32_t full_at, uint32_t bytes = kStageBytes, int nk_one = 1 << 30) {
     for (int k = k0; k < k1; ++k) {
         const int term = k >= nk_one, kb = term ? k - nk_one : k;
-        if (!bar_wait(r.empty + 8 * r.s, r.ph ^ 1)) return false;
+        if (!warp_wait(r.empty + 8 * r.s, r.ph ^ 1)) return false;
         const uint32_t a = r.base + r.s * kStageBytes, bar = full_at + 8 * r.s;
         if (elect_one()) {
             if (rank == 0) bar_expect(r.full + 8 * r.s, CG * bytes);
@@ -146,7 +146,7 @@ __device__ __forceinline__ bool multiply_tile(Ring& r, uint32_t acc, int nk, con
     const uint64_t a_k = operand_desc(r.base, false, kHalf / 2), a_mn = operand_desc(r.base, true, kHalf / 2);
     const uint64_t to_b = kHalf >> 4;
     for (int k = 0; k < nk; ++k) {
-        if (!bar_wait(r.full + 8 * r.s, r.ph)) return false;
+        if (!warp_wait(r.full + 8 * r.s, r.ph)) return false;
         mma_fence_after();
         const bool amn = va.is_mn<128 * CG>(k), bmn = vb.is_mn<128 * CG>(k);
         const uint64_t off = (uint64_t)(r.s * (kStageBytes >> 4));
@@ -423,7 +423,7 @@ __global__ void __launch_bounds__(kMatThreads<Epi::kWarps>, 1)
         for (int t = first; ok && t < total; t += step) {
             const int k0 = g.splits > 1 ? tile_at(g, t, per).b * nk_part : 0, nk = min(nk_part, nk_all - k0);
             if (g.splits > 1 && nk <= 0) continue;  // nothing of K is left for this part
-            if (!(ok = bar_wait(w.free_ + 8 * acc, aph ^ 1))) break;
+            if (!(ok = warp_wait(w.free_ + 8 * acc, aph ^ 1))) break;
             mma_fence_after();
             ok = multiply_tile<CG>(r, w.tmem + acc * BN, nk, va, vb, g.f16, w.done + 8 * acc, g.width);
             if (++acc == 2) acc = 0, aph ^= 1;
@@ -439,8 +439,7 @@ __global__ void __launch_bounds__(kMatThreads<Epi::kWarps>, 1)
         for (int t = first; t < total; t += step) {
             const TileAt at = tile_at(g, t, per);
             if (g.splits > 1 && at.b * nk_part >= nk_all) continue;
-            ok = bar_wait(w.done + 8 * acc, aph);
-            if (!__all_sync(0xFFFFFFFFu, ok)) break;
+            if (!(ok = warp_wait(w.done + 8 * acc, aph))) break;
             mma_fence_after();
             const int row = at.m * 128 * CG + (int)rank * 128 + quad * 32 + lane;
             const int col = at.n * g.width + part * share, end = min(col + share, (at.n + 1) * g.width);

@@ -449,7 +449,7 @@ __global__ void __launch_bounds__(kMatThreads<kStepWarps>, 1) k_ns_steps(const _
                 int k0, nk, cut;
                 View va, vb;
                 operands(maps, TALL, which, 0, tile_of(which, t, k0, nk, cut), va, vb);
-                if (!(ok = bar_wait(w.free_ + 8 * acc, aph ^ 1))) break;
+                if (!(ok = warp_wait(w.free_ + 8 * acc, aph ^ 1))) break;
                 mma_fence_after();
                 ok = multiply_tile<CG>(r, w.tmem + acc * BN, nk, va, vb, true, w.done + 8 * acc);
                 if (++acc == 2) acc = 0, aph ^= 1;
@@ -463,7 +463,7 @@ __global__ void __launch_bounds__(kMatThreads<kStepWarps>, 1) k_ns_steps(const _
         uint32_t aph = 0;
         for (int round = 0; round < rounds; ++round) {  // a warp that gave up still comes to the barrier below
             const int which = which_of(round), k = round / per_step, buf = k & 1, total = tiles_in(which);
-            if (ok && round) ok = __all_sync(0xFFFFFFFFu, bar_wait(round_bar, (round - 1) & 1));
+            if (ok && round) ok = warp_wait(round_bar, (round - 1) & 1);
             const float2* scales = p.scales + (int64_t)scales_of(k, p.steps) * p.count;
             EpiGram::Args eg = {p.gram, p.diag, p.lds, p.ss, p.s, p.part, p.ld_part};
             if (CUT && ok && which == 3)
@@ -482,9 +482,7 @@ __global__ void __launch_bounds__(kMatThreads<kStepWarps>, 1) k_ns_steps(const _
                 if (which == 1) EpiPoly::load(ep, row, col, at, turn, q);
                 if (row < p.s && (which == 1 || (which == 2 && !TALL)))
                     own = __ldcg((which == 1 ? p.diag : p.regain) + (int64_t)at.b * p.s + row);
-                ok = bar_wait(w.done + 8 * acc, aph);
-                ok = __all_sync(0xFFFFFFFFu, ok);
-                if (!ok) break;
+                if (!(ok = warp_wait(w.done + 8 * acc, aph))) break;
                 mma_fence_after();
                 if (which == 0) {
                     if (CUT) eg.part = p.part + cut * p.part_stride;
