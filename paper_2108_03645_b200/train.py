@@ -16,6 +16,7 @@ from __future__ import annotations
 import ctypes as C
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as _b
 
@@ -135,6 +136,7 @@ class _LayerNorm(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, weight, mean, rstd = ctx.saved_tensors
         dx, dw, db = layer_norm_backward(dy, x, mean, rstd, weight, parameters=weight is not None or ctx.has_bias)
@@ -149,16 +151,17 @@ class _LinearCrossEntropy(torch.autograd.Function):
         return loss
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dloss):
         hidden, weight, target, lse = ctx.saved_tensors
         return (*linear_cross_entropy_backward(dloss, hidden, weight, target, lse), None)
 
 
 def layer_norm_autograd(x, weight=None, bias=None, eps: float = 1e-5) -> torch.Tensor:
-    """`layer_norm` as a differentiable function of x, weight and bias: y."""
+    """`layer_norm` as a (once) differentiable function of x, weight and bias: y."""
     return _LayerNorm.apply(x, weight, bias, eps)
 
 
 def linear_cross_entropy_autograd(hidden, weight, target) -> torch.Tensor:
-    """`linear_cross_entropy` as a differentiable function of hidden and weight: the loss of each row."""
+    """`linear_cross_entropy` as a (once) differentiable function of hidden and weight: the loss of each row."""
     return _LinearCrossEntropy.apply(hidden, weight, target)

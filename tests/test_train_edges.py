@@ -129,3 +129,21 @@ def test_a_wait_that_runs_out_is_reported_once_and_waited_for_once(which):
     train.check()
     assert all(torch.equal(a, b) for a, b in zip(want, everything()))
     train.check()
+
+
+# ---------------------------------------------------------------- automatic differentiation
+
+def test_second_derivatives_are_refused():
+    """The gradients are not differentiable themselves: a penalty on them is an error, not a constant."""
+    from paper_2108_03645_b200 import train
+    x, w = randn(6, 64).requires_grad_(), randn(64, seed=1).requires_grad_()
+    loss = train.layer_norm_autograd(x, w).pow(3).sum()
+    gx, gw = torch.autograd.grad(loss, (x, w), create_graph=True)
+    with pytest.raises(RuntimeError):
+        (loss + gx.pow(2).sum() + gw.pow(2).sum()).backward()
+    h, hw, t, _ = ce_inputs(10, 64, 50, BF16, 0.0)
+    h.requires_grad_(), hw.requires_grad_()
+    loss = train.linear_cross_entropy_autograd(h, hw, t).pow(2).sum()
+    gh, gw = torch.autograd.grad(loss, (h, hw), create_graph=True)
+    with pytest.raises(RuntimeError):
+        (loss + gh.float().pow(2).sum() + gw.float().pow(2).sum()).backward()
