@@ -5,6 +5,7 @@
 #include <c10/cuda/CUDAGuard.h>
 #include <torch/extension.h>
 
+#include <initializer_list>
 #include <optional>
 
 #include "ones_train.h"
@@ -17,6 +18,15 @@ using MaybeTensor = std::optional<Tensor>;
 int kind_of(at::ScalarType t) {
     return t == at::kFloat ? ONES_F32 : t == at::kBFloat16 ? ONES_BF16 : t == at::kHalf ? ONES_F16 : -1;
 }
+
+// Results have no graph: who asks for a gradient (or sends a tangent) through here would get none, without a word.
+void no_graph(std::initializer_list<const Tensor*> ts) {
+    for (const Tensor* t : ts)
+        TORCH_CHECK_VALUE(!(t->requires_grad() && at::GradMode::is_enabled()) && !t->_fw_grad(0).defined(),
+                          "an input requires a gradient, but this function is not differentiable: use layer_norm_autograd or "
+                          "linear_cross_entropy_autograd, or call it under torch.no_grad()");
+}
+const Tensor* given(const MaybeTensor& t, const Tensor& other) { return t ? &*t : &other; }
 
 void* ptr(const MaybeTensor& t) { return t ? t->data_ptr() : nullptr; }
 void* stream() { return at::cuda::getCurrentCUDAStream().stream(); }
@@ -58,6 +68,7 @@ bool is_param(const MaybeTensor& t, int64_t cols, const Tensor& x) {
 py::object result(int rc, py::object v) { return rc ? py::int_(rc) : std::move(v); }
 
 py::object layer_norm(const Tensor& x, const MaybeTensor& weight, const MaybeTensor& bias, double eps) {
+    no_graph({&x, given(weight, x), given(bias, x)});
     const int kind = kind_of(x.scalar_type());
     TORCH_CHECK_VALUE(x.is_cuda() && kind >= 0 && x.dim() >= 1, "x: a float32, bfloat16 or float16 CUDA tensor is needed");
     const int64_t cols = x.size(-1);
@@ -76,6 +87,7 @@ py::object layer_norm(const Tensor& x, const MaybeTensor& weight, const MaybeTen
 
 py::object layer_norm_backward(const Tensor& dy, const Tensor& x, const Tensor& mean, const Tensor& rstd, const MaybeTensor& weight,
                                bool parameters) {
+    no_graph({&dy, &x, &mean, &rstd, given(weight, x)});
     const int kind = kind_of(x.scalar_type());
     TORCH_CHECK_VALUE(x.is_cuda() && kind >= 0 && x.dim() >= 1, "x: a float32, bfloat16 or float16 CUDA tensor is needed");
     TORCH_CHECK_VALUE(dy.sizes() == x.sizes() && dy.scalar_type() == x.scalar_type() && dy.device() == x.device(),
@@ -116,6 +128,7 @@ void check_loss(const Tensor& hidden, const Tensor& weight, const Tensor& target
 }
 
 py::object linear_cross_entropy(const Tensor& hidden, const Tensor& weight, const Tensor& target) {
+    no_graph({&hidden, &weight});
     check_loss(hidden, weight, target);
     const at::NoGradGuard no_grad;
     const c10::cuda::CUDAGuard guard(hidden.device());
@@ -132,6 +145,7 @@ py::object linear_cross_entropy(const Tensor& hidden, const Tensor& weight, cons
 
 py::object linear_cross_entropy_backward(const Tensor& dloss, const Tensor& hidden, const Tensor& weight, const Tensor& target, const Tensor& lse,
                                          bool weight_gradient_f32, int64_t piece) {
+    no_graph({&dloss, &hidden, &weight, &lse});
     check_loss(hidden, weight, target);
     for (const Tensor* s : {&dloss, &lse})
         TORCH_CHECK_VALUE(s->scalar_type() == at::kFloat && s->device() == hidden.device() && s->sizes() == target.sizes(),
@@ -153,6 +167,7 @@ py::object linear_cross_entropy_backward(const Tensor& dloss, const Tensor& hidd
 }
 
 py::object orthogonalize(const Tensor& g, int64_t steps, double a, double b, double c, double eps) {
+    no_graph({&g});
     const int kind = kind_of(g.scalar_type());
     TORCH_CHECK_VALUE(g.is_cuda() && kind >= 0 && (g.dim() == 2 || g.dim() == 3), "g: a float32, bfloat16 or float16 CUDA matrix is needed, or several");
     const at::NoGradGuard no_grad;

@@ -10,6 +10,9 @@ workspaces come from torch's allocator on that stream.  Nothing synchronises exc
 
 The functions take rows with any stride between them (a slice of a wider buffer is read in place).  Other layouts, and
 for the cross entropy rows that do not start on 16-byte boundaries, are copied first.
+
+Their results have no graph, so they refuse inputs that require a gradient while gradients are recorded, and tangents of
+forward mode; `layer_norm_autograd` and `linear_cross_entropy_autograd` are differentiable, once.
 """
 from __future__ import annotations
 

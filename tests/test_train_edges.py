@@ -147,3 +147,28 @@ def test_second_derivatives_are_refused():
     gh, gw = torch.autograd.grad(loss, (h, hw), create_graph=True)
     with pytest.raises(RuntimeError):
         (loss + gh.float().pow(2).sum() + gw.float().pow(2).sum()).backward()
+
+
+def test_functions_outside_the_graph_refuse_what_asks_for_a_gradient():
+    from paper_2108_03645_b200 import train
+    x, w = randn(6, 64), randn(64, seed=1)
+    h, hw, t, g = ce_inputs(10, 64, 50, BF16, 0.0)
+    y, mean, rstd = train.layer_norm(x, w, w)
+    loss, lse = train.linear_cross_entropy(h, hw, t)
+    ask = lambda v: v.clone().requires_grad_()  # noqa: E731
+    # (orthogonalize is what an optimiser does with a gradient, under no_grad as a rule)
+    calls = [(train.layer_norm, (x, w, w), 3), (train.layer_norm_backward, (y, x, mean, rstd, w), 5), (train.linear_cross_entropy, (h, hw, t), 2),
+             (train.linear_cross_entropy_backward, (g, h, hw, t, lse), 3), (train.orthogonalize, (x,), 1)]
+    for f, args, n in calls:
+        for i in range(n):
+            mine = [ask(v) if j == i else v for j, v in enumerate(args)]
+            with pytest.raises(ValueError):
+                f(*mine)
+            with torch.no_grad():
+                f(*mine)
+    with torch.autograd.forward_ad.dual_level():
+        dual = torch.autograd.forward_ad.make_dual(x, torch.ones_like(x))
+        with pytest.raises(ValueError):
+            train.layer_norm(dual, w)
+        with pytest.raises((ValueError, RuntimeError, NotImplementedError)):
+            train.layer_norm_autograd(dual, w)

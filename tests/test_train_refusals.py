@@ -8,3 +8,17 @@ from test_train_abi import ALIGN, P, PARAM, _lib  # noqa: F401
 @pytest.mark.parametrize("steps", [1025, 1 << 29, (1 << 31) - 1])
 def test_orthogonalize_refuses_steps_without_end(m, n, steps):
     assert _lib().ones_orthogonalize(P, n, m * n, 1, m, n, 0, steps, 3.4445, -4.775, 2.0315, 1e-7, P, P, 1 << 24, None) == PARAM
+
+
+def test_functions_outside_the_graph_refuse_what_asks_for_a_gradient():
+    torch = pytest.importorskip("torch")
+    from paper_2108_03645_b200 import train
+    x = torch.zeros(4, 8)
+    for f, args in ((train.layer_norm, (x,)), (train.linear_cross_entropy, (x.bfloat16(), x.bfloat16(), torch.zeros(4, dtype=torch.int64))),
+                    (train.orthogonalize, (x,))):
+        with pytest.raises(ValueError, match="CUDA"):
+            f(*args)
+        with pytest.raises(ValueError, match="no_grad"):
+            f(args[0].clone().requires_grad_(), *args[1:])
+        with torch.no_grad(), pytest.raises(ValueError, match="CUDA"):
+            f(args[0].clone().requires_grad_(), *args[1:])
