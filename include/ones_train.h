@@ -32,7 +32,9 @@ extern "C" {
  *   mean = sum_c x / cols,  rstd = 1 / sqrt(sum_c (x - mean)^2 / cols + eps),  y = (x - mean) * rstd * weight + bias.
  *   d_x, d_y        [rows][cols] of `type`;  d_weight, d_bias [cols] of `wtype`, each NULL for 1 and 0.
  *   d_mean, d_rstd  float[rows], for the backward pass; either may be NULL.
- * rows >= 0, 1 <= cols <= ONES_NORM_MAX_COLS, eps > 0.  wtype is ONES_F32 or `type`.  Sums are in 32 bits. */
+ * 0 <= rows <= ONES_NORM_MAX_ROWS, 1 <= cols <= ONES_NORM_MAX_COLS, eps > 0.  wtype is ONES_F32 or `type`.  Sums are in 32
+ * bits. */
+#define ONES_NORM_MAX_ROWS 0x7FFF0000 /* 2^31 - 2^16 */
 #define ONES_NORM_MAX_COLS 65536
 int ones_layer_norm(const void* d_x, int64_t ldx, const void* d_weight, const void* d_bias, int32_t rows, int32_t cols,
                     float eps, int32_t type, int32_t wtype, void* d_y, int64_t ldy, float* d_mean, float* d_rstd,

@@ -172,3 +172,31 @@ def test_functions_outside_the_graph_refuse_what_asks_for_a_gradient():
             train.layer_norm(dual, w)
         with pytest.raises((ValueError, RuntimeError, NotImplementedError)):
             train.layer_norm_autograd(dual, w)
+
+
+# ---------------------------------------------------------------- as many rows as are taken
+
+def test_layer_norm_of_the_most_rows():
+    """2^31 - 2^16 rows of one value, through the C ABI: the last ones are reached, and nothing behind them."""
+    from paper_2108_03645_b200 import train
+    L = train.lib()
+    n = (1 << 31) - (1 << 16)
+    free = torch.cuda.mem_get_info()[0]
+    if free < 48 << 30:
+        pytest.skip("needs 48 GB")
+    x = torch.zeros(n + 64, dtype=BF16, device="cuda")
+    dy = torch.zeros(n + 64, dtype=BF16, device="cuda")
+    out = torch.full((n + 64,), 77.0, dtype=BF16, device="cuda")
+    x[n - 5:], dy[n - 5:n], dy[n:] = 3.0, 2.0, 1000.0
+    stat = torch.full((2, n + 64), 7.0, device="cuda")
+    shift, sums = torch.full((1,), 0.5, dtype=BF16, device="cuda"), torch.empty(2, device="cuda")
+    nbytes = L.ones_layer_norm_workspace_bytes(n, 1)
+    space = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    s = torch.cuda.current_stream().cuda_stream
+    assert L.ones_layer_norm(x.data_ptr(), 1, None, shift.data_ptr(), n, 1, 1e-5, 1, 1, out.data_ptr(), 1, stat.data_ptr(), stat[1].data_ptr(), s) == 0
+    assert float(out[:n].min()) == float(out[:n].max()) == 0.5 and bool((out[n:] == 77.0).all())
+    assert bool((stat[0, n - 5:n] == 3.0).all()) and bool((stat[:, n:] == 7.0).all()) and float(stat[0, :n - 5].abs().max()) == 0.0
+    assert L.ones_layer_norm_backward(dy.data_ptr(), 1, x.data_ptr(), 1, stat.data_ptr(), stat[1].data_ptr(), None, n, 1, 1, 0, out.data_ptr(), 1,
+                                      sums.data_ptr(), sums[1:].data_ptr(), space.data_ptr(), nbytes, s) == 0
+    assert float(out[:n].abs().max()) == 0.0 and bool((out[n:] == 77.0).all())
+    assert sums.tolist() == [0.0, 10.0]

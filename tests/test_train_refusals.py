@@ -22,3 +22,12 @@ def test_functions_outside_the_graph_refuse_what_asks_for_a_gradient():
             f(args[0].clone().requires_grad_(), *args[1:])
         with torch.no_grad(), pytest.raises(ValueError, match="CUDA"):
             f(args[0].clone().requires_grad_(), *args[1:])
+
+
+@pytest.mark.parametrize("rows", [(1 << 31) - (1 << 16) + 1, (1 << 31) - 1])
+@pytest.mark.parametrize("cols", [1, 8, 300])
+def test_layer_norm_refuses_more_rows_than_it_counts(rows, cols):
+    L = _lib()
+    assert L.ones_layer_norm(P, cols, None, None, rows, cols, 1e-5, 1, 1, P, cols, P, P, None) == PARAM
+    assert L.ones_layer_norm_workspace_bytes(rows, cols) == 0
+    assert L.ones_layer_norm_backward(P, cols, P, cols, P, P, None, rows, cols, 1, 0, P, cols, P, P, P, 1 << 30, None) == PARAM
