@@ -117,10 +117,14 @@ struct EpiDlogits {
             float v[N];
             tmem_load(acc + c, v);
 #pragma unroll
-            for (int i = 0; i < N; i += 2) {  // rows behind the last one that takes part are zero: exp(0) * 0
+            for (int i = 0; i < N; i += 2) {
                 const float2 x = split(fma2(pair(v[i], v[i + 1]), both(to2), both(r.shift)));
                 const float2 y = split(pair(exp2_fast(x.x), exp2_fast(x.y)) * both(r.g));
                 v[i] = y.x, v[i + 1] = y.y;
+            }
+            if (!live) {  // 0 * infinity, where the weight holds one, is no zero
+#pragma unroll
+                for (int i = 0; i < N; ++i) v[i] = 0.f;
             }
             const unsigned at_i = (unsigned)(t - (col + c));
             if (live && at_i < (unsigned)N) {

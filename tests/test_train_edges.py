@@ -200,3 +200,25 @@ def test_layer_norm_of_the_most_rows():
                                       sums.data_ptr(), sums[1:].data_ptr(), space.data_ptr(), nbytes, s) == 0
     assert float(out[:n].abs().max()) == 0.0 and bool((out[n:] == 77.0).all())
     assert sums.tolist() == [0.0, 10.0]
+
+
+# ---------------------------------------------------------------- infinities in the weight
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("n", [1, 40, 63, 64, 100, 300])
+def test_linear_cross_entropy_entry_that_never_comes(n, dtype):
+    """An entry whose logit is -inf in every row has probability 0: its row of dweight is 0, whatever the number of rows, and the
+    others are as if it were not there. Some rows take no part."""
+    from paper_2108_03645_b200 import train
+    h, w, t, g = ce_inputs(n, 64, 300, dtype, 0.3)
+    h[:, 3] = 1.0
+    t[t == 7] = 8
+    w[7, 3] = float("-inf")
+    loss, lse = train.linear_cross_entropy(h, w, t)
+    dw = train.linear_cross_entropy_backward(g, h, w, t, lse, weight_gradient=F32)[1]
+    keep = torch.arange(300, device="cuda") != 7
+    _, lse2 = train.linear_cross_entropy(h, w[keep].contiguous(), t - (t > 7).long())
+    want = train.linear_cross_entropy_backward(g, h, w[keep].contiguous(), t - (t > 7).long(), lse2, weight_gradient=F32)[1]
+    assert not bool(dw[7].any())
+    # lse of the same logits joined in another order: a few roundings of 2^-24, which can move a 16-bit rounding
+    assert float((dw[keep] - want).norm()) <= 2 * U[dtype] * float(want.norm())
