@@ -10,7 +10,8 @@
  * Conventions: those of ones.h.  Pointers named d_* are device memory of the current device; the caller owns every
  * buffer, the device workspace among them; nothing here allocates or frees device memory, prints or aborts.  All work
  * is enqueued on `cuda_stream` (a cudaStream_t, NULL = the default stream) and nothing synchronises, except
- * ones_train_status.  Arguments are checked before anything is launched.  Results do not depend on the order in which
+ * ones_train_status.  Arguments are checked before anything is launched, pointers for the alignment of their elements at
+ * least (ONES_ERR_ALIGN).  Results do not depend on the order in which
  * blocks run: the same inputs give the same bits.  Rows are `ld` values apart, ld >= the row's length; values between
  * two rows are not written and do not matter, but where rows start on no 16-byte boundary they may be read along with
  * the 16-byte blocks around a row.  Nothing before a matrix's first value or after its last is read.

@@ -709,7 +709,8 @@ int ones_linear_ce(const void* d_hidden, int64_t ldh, const void* d_weight, int6
         return ONES_ERR_BAD_PARAM;
     if (rows == 0) return ONES_OK;
     if (!d_hidden || !d_weight || !d_target || !d_loss || !d_lse || !d_workspace) return ONES_ERR_NULL;
-    if (!aligned(d_hidden, 16) || !aligned(d_weight, 16) || ldh % 8 || ldw % 8 || !aligned(d_workspace, 256))
+    if (!aligned(d_hidden, 16) || !aligned(d_weight, 16) || ldh % 8 || ldw % 8 || !aligned(d_workspace, 256) || !aligned(d_target, 8) ||
+        !aligned(d_loss, 4) || !aligned(d_lse, 4))
         return ONES_ERR_ALIGN;
     const ForwardLayout L = forward_layout(rows, vocab);
     if (workspace_bytes < L.total) return ONES_ERR_WORKSPACE;
@@ -749,7 +750,7 @@ int ones_linear_ce_backward(const float* d_dloss, const void* d_hidden, int64_t 
     if (!d_dloss || !d_hidden || !d_weight || !d_target || !d_lse || !d_dhidden || !d_workspace) return ONES_ERR_NULL;
     const size_t wsize = wtype == ONES_F32 ? 4 : 2;
     if (!aligned(d_hidden, 2) || !aligned(d_weight, 16) || ldw % 8 || !aligned(d_dhidden, 2) ||
-        !aligned(d_dweight, wsize) || !aligned(d_workspace, 256))
+        !aligned(d_dweight, wsize) || !aligned(d_workspace, 256) || !aligned(d_target, 8) || !aligned(d_dloss, 4) || !aligned(d_lse, 4))
         return ONES_ERR_ALIGN;
     const BackwardLayout L = backward_layout(rows, cols, vocab, piece);
     if (workspace_bytes < L.total) return ONES_ERR_WORKSPACE;

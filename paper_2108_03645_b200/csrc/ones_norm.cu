@@ -1237,7 +1237,8 @@ int ones_layer_norm(const void* d_x, int64_t ldx, const void* d_weight, const vo
     if (rows == 0) return ONES_OK;
     if (!d_x || !d_y) return ONES_ERR_NULL;
     const int size = size_of(type);
-    if (!aligned(d_x, size) || !aligned(d_y, size) || !aligned(d_weight, size_of(wtype)) || !aligned(d_bias, size_of(wtype)))
+    if (!aligned(d_x, size) || !aligned(d_y, size) || !aligned(d_weight, size_of(wtype)) || !aligned(d_bias, size_of(wtype)) ||
+        !aligned(d_mean, 4) || !aligned(d_rstd, 4))
         return ONES_ERR_ALIGN;
     const NormIn a = {d_x, d_weight, d_bias, ldx, rows, cols, eps, wtype == ONES_F32};
     const bool wide = is_wide(d_x, ldx, cols, type) && is_wide(d_y, ldy, cols, type) && aligned(d_weight, 16) && aligned(d_bias, 16);
@@ -1271,7 +1272,7 @@ int ones_layer_norm_backward(const void* d_dy, int64_t lddy, const void* d_x, in
     const bool sums = d_dweight || d_dbias;
     if (!d_dy || !d_x || !d_mean || !d_rstd || !d_dx || (sums && !d_workspace)) return ONES_ERR_NULL;
     if (!aligned(d_dy, size) || !aligned(d_x, size) || !aligned(d_dx, size) || !aligned(d_weight, wsize) ||
-        (sums && !aligned(d_workspace, 256)))
+        !aligned(d_mean, 4) || !aligned(d_rstd, 4) || (sums && !aligned(d_workspace, 256)))
         return ONES_ERR_ALIGN;
     if (sums && workspace_bytes < ones_layer_norm_workspace_bytes(rows, cols)) return ONES_ERR_WORKSPACE;
     float* part = sums ? static_cast<float*>(d_workspace) : nullptr;

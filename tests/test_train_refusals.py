@@ -31,3 +31,23 @@ def test_layer_norm_refuses_more_rows_than_it_counts(rows, cols):
     assert L.ones_layer_norm(P, cols, None, None, rows, cols, 1e-5, 1, 1, P, cols, P, P, None) == PARAM
     assert L.ones_layer_norm_workspace_bytes(rows, cols) == 0
     assert L.ones_layer_norm_backward(P, cols, P, cols, P, P, None, rows, cols, 1, 0, P, cols, P, P, P, 1 << 30, None) == PARAM
+
+
+@pytest.mark.parametrize("change", [{"t": P + 4}, {"loss": P + 2}, {"lse": P + 1}])
+def test_linear_ce_refuses_elements_off_their_alignment(change):
+    a = dict(h=P, ldh=64, w=P, ldw=64, t=P, loss=P, lse=P) | change
+    assert _lib().ones_linear_ce(a["h"], a["ldh"], a["w"], a["ldw"], a["t"], 4, 64, 100, 1, a["loss"], a["lse"], P, 1 << 20, None) == ALIGN
+
+
+@pytest.mark.parametrize("change", [{"g": P + 2}, {"t": P + 4}, {"lse": P + 2}])
+def test_linear_ce_backward_refuses_elements_off_their_alignment(change):
+    a = dict(g=P, t=P, lse=P) | change
+    assert _lib().ones_linear_ce_backward(a["g"], P, 64, P, 64, a["t"], a["lse"], 4, 64, 100, 1, 1, 0, P, 64, P, 64, P, 1 << 24, None) == ALIGN
+
+
+@pytest.mark.parametrize("change", [{"mean": P + 2}, {"rstd": P + 3}])
+def test_layer_norm_refuses_statistics_off_their_alignment(change):
+    a = dict(mean=P, rstd=P) | change
+    L = _lib()
+    assert L.ones_layer_norm(P, 64, P, P, 4, 64, 1e-5, 0, 0, P, 64, a["mean"], a["rstd"], None) == ALIGN
+    assert L.ones_layer_norm_backward(P, 64, P, 64, a["mean"], a["rstd"], P, 4, 64, 0, 0, P, 64, P, P, P, 1 << 20, None) == ALIGN
