@@ -59,7 +59,9 @@ int ones_layer_norm_backward(const void* d_dy, int64_t lddy, const void* d_x, in
  *   multiples of 8 (else ONES_ERR_ALIGN); d_target int64[rows]; d_loss, d_lse float[rows].
  *   rows >= 0, cols >= 1, vocab >= 1; any sizes otherwise.
  *   d_workspace  at least ones_linear_ce_workspace_bytes(rows, vocab) bytes, 256-byte aligned.
- * Logits are accumulated and reduced in 32 bits. */
+ * Logits are accumulated and reduced in 32 bits.  The tensor cores cut their sums off towards zero; what dense rows lose by
+ * that in the mean, 2^-30 of a logit per column, is given back for up to 4096 columns, whatever the row: a logit that comes
+ * from few columns is too large by up to 2^-18 of itself then, and dense rows of more columns are too small by the rest. */
 size_t ones_linear_ce_workspace_bytes(int32_t rows, int32_t vocab);
 /* Copies rows that start anywhere to rows on 16-byte boundaries, as ones_linear_ce needs them: d_dst 16-byte aligned, ldd
  * a multiple of 8, both [rows][cols] of ONES_BF16 or ONES_F16.  Zeros follow each row up to the next multiple of 8. */

@@ -21,7 +21,9 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // sum that grows evenly over K steps loses in the mean 2^-30 of itself per value of K (measured: 4.9e-7 at 512, 2.03e-6
 // at 2048, 4.07e-6 at 4096 columns, in proportion), and all large logits lose alike, so it is given back: the relative
 // error of the loss falls from 1.2e-6 to below 5e-7 at 2048 columns. It enters as part of the factor of the exponent.
-__device__ __forceinline__ float regain(int k) { return 1.f + (float)k * 9.3132257e-10f; }
+// It is a mean for dense rows: a logit that comes from a few columns, the others being zero, loses nothing and is given too
+// much. So nothing is given for more columns than were measured: a logit is never off by more than 2^-18 of itself for it.
+__device__ __forceinline__ float regain(int k) { return 1.f + (float)min(k, 4096) * 9.3132257e-10f; }
 
 // Softmax statistics of a tile of logits: each thread takes the maximum m and s = sum exp(l - m) of its row's columns
 // here, and the logit of the row's target if it meets it. 4096 x 1024 x 50000: 254 us while the card is cool, 1.65 PFLOP/s;

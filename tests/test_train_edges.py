@@ -222,3 +222,20 @@ def test_linear_cross_entropy_entry_that_never_comes(n, dtype):
     assert not bool(dw[7].any())
     # lse of the same logits joined in another order: a few roundings of 2^-24, which can move a 16-bit rounding
     assert float((dw[keep] - want).norm()) <= 2 * U[dtype] * float(want.norm())
+
+
+# ---------------------------------------------------------------- precision
+
+@pytest.mark.parametrize("d", [64, 1024, 4096, 16384])
+def test_linear_cross_entropy_logits_of_one_product(d):
+    """What is given back for the cut-off of evenly growing sums is at most 2^-30 * 4096 of a logit that had lost nothing."""
+    from paper_2108_03645_b200 import train
+    w = torch.zeros(300, d, dtype=BF16, device="cuda")
+    h = torch.zeros(3, d, dtype=BF16, device="cuda")
+    w[5, 0], w[9, d - 1] = 200.0, 200.0
+    h[0, 0], h[1, d - 1], h[2, 0] = 2.0, 2.0, 2.0
+    t = torch.tensor([7, 5, 5], device="cuda")
+    loss, lse = train.linear_cross_entropy(h, w, t)
+    bound = 400.0 * (4096 * 2.0 ** -30 + 2 * 2.0 ** -23)
+    assert bool(((lse.double() - 400.0).abs() <= bound).all())
+    assert bool(((loss[:2].double() - 400.0).abs() <= bound).all()) and float(loss[2]) == 0.0
