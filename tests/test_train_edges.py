@@ -239,3 +239,51 @@ def test_linear_cross_entropy_logits_of_one_product(d):
     bound = 400.0 * (4096 * 2.0 ** -30 + 2 * 2.0 ** -23)
     assert bool(((lse.double() - 400.0).abs() <= bound).all())
     assert bool(((loss[:2].double() - 400.0).abs() <= bound).all()) and float(loss[2]) == 0.0
+
+
+@pytest.mark.parametrize("d,bound", [(2048, 7.5e-7), (4096, 1.2e-6)])
+def test_linear_cross_entropy_precision(d, bound):
+    """Dense rows: losses and log-sums near their exact values. Logits that are cut off by 2^-30 of themselves per column, as in
+    the tensor cores, move both by 1.0e-6 of their norm at 2048 columns and by twice that at 4096, if it is not given back."""
+    from paper_2108_03645_b200 import train
+    n, v = 512, 32000
+    w = (randn(v, d) * (2 / math.sqrt(d))).bfloat16()
+    t = torch.randint(0, v, (n,), generator=torch.Generator(device="cuda").manual_seed(3), device="cuda")
+    h = (randn(n, d, seed=1) + w[t].float() * (4 * torch.rand(n, 1, generator=torch.Generator(device="cuda").manual_seed(4), device="cuda"))).bfloat16()
+    loss, lse = train.linear_cross_entropy(h, w, t)
+    r = ce_reference(h, w, t)
+    assert float((loss.double() - r["loss"]).norm()) <= bound * float(r["loss"].norm())
+    assert float((lse.double() - r["lse"]).norm()) <= bound * float(r["lse"].norm())
+
+
+def momentum(m, n, dtype):
+    """A part of low rank, and noise."""
+    r = max(1, min(m, n) // 4)
+    return ((randn(m, r) @ randn(r, n, seed=1) / math.sqrt(r) + 0.5 * randn(m, n, seed=2)) * 1e-3).to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m,n", [(768, 768), (1999, 1001), (128, 4096), (71, 2063), (128, 256), (32, 8192)])
+def test_orthogonalize_precision(m, n, dtype):
+    """Within 2.2e-3 of the norm, of which the rounding of the result is 1.66e-3."""
+    from paper_2108_03645_b200 import train
+    g = momentum(m, n, dtype)
+    want = ns_reference(g, 5, (3.4445, -4.7750, 2.0315), 1e-7)
+    assert float((train.orthogonalize(g).double() - want).norm()) <= 2.2e-3 * float(want.norm())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m,n,bound", [(32, 512, 3e-4), (71, 2063, 5e-4), (32, 8192, 2.5e-4), (200, 2500, 2e-4), (300, 4000, 2e-4)])
+def test_orthogonalize_rows_have_their_length(m, n, bound, dtype):
+    """The roundings of the result average out over a long row; what is left is the row's factor. A model of the arithmetic in 64
+    bits has it off (root mean square over the rows, at most over six inputs) by 2.0e-4, 3.2e-4, 1.5e-4, 1.2e-4 and 0.9e-4 for
+    these sizes, and by at least 4.1e-4, 7.0e-4, 3.6e-4, 2.8e-4 and 3.5e-4 without the Gram matrix's diagonal in 32 bits or
+    without the factors that give back the rounding of the polynomial's."""
+    from paper_2108_03645_b200 import train
+    g = momentum(m, n, dtype)
+    for flip in (False, True):
+        o = train.orthogonalize(g.mT if flip else g).double()
+        o = o.mT if flip else o
+        want = ns_reference(g, 5, (3.4445, -4.7750, 2.0315), 1e-7)
+        off = (o * want).sum(1) / want.square().sum(1) - 1
+        assert float(off.square().mean().sqrt()) <= bound
