@@ -124,7 +124,13 @@ class LanguageModelJob:
 
 
 def profile(job: LanguageModelJob, batches, *, steps: int = 10, warmup: int = 3) -> list[float]:
-    """Seconds per step at each batch (samples on this GPU), by CUDA events around `steps` steps."""
+    """Seconds per step at each batch (samples on the job's GPU), by CUDA events around `steps` steps."""
+    import torch
+    with torch.cuda.device(job.device):  # events and checks belong to the current device
+        return _profile(job, batches, steps, warmup)
+
+
+def _profile(job, batches, steps, warmup):
     import torch
     from . import train
     out = []

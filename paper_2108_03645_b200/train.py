@@ -123,9 +123,12 @@ def orthogonalize(g: torch.Tensor, *, steps: int = 5, coefficients=(3.4445, -4.7
     return _done((_ops or _load()).orthogonalize(g, steps, a, b, c, eps), "ones_orthogonalize")
 
 
-def check() -> None:
-    """Waits for the current stream and raises if a kernel gave up waiting since the last check (``ones_train_status``)."""
-    rc = lib().ones_train_status(torch.cuda.current_stream().cuda_stream)
+def check(device=None) -> None:
+    """Waits for the current stream of `device` (None: the current one) and raises if a kernel on it gave up waiting since the
+    last check (``ones_train_status``). Such a kernel's results are void, and nothing else says so: a program calls this before it
+    trusts what it computed, at a step that it waits for anyway."""
+    with torch.cuda.device(device):
+        rc = lib().ones_train_status(torch.cuda.current_stream().cuda_stream)
     if rc:
         raise _b.OnesError(rc, "ones_train_status")
 

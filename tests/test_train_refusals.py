@@ -51,3 +51,58 @@ def test_layer_norm_refuses_statistics_off_their_alignment(change):
     L = _lib()
     assert L.ones_layer_norm(P, 64, P, P, 4, 64, 1e-5, 0, 0, P, 64, a["mean"], a["rstd"], None) == ALIGN
     assert L.ones_layer_norm_backward(P, 64, P, 64, a["mean"], a["rstd"], P, 4, 64, 0, 0, P, 64, P, P, P, 1 << 20, None) == ALIGN
+
+
+def test_profile_runs_and_checks_on_the_jobs_device(monkeypatch):
+    """Events and the status of the waits are of the current device: the job's, whichever is current at the call."""
+    torch = pytest.importorskip("torch")
+    from paper_2108_03645_b200 import profile_job, train
+    current, seen = [0], []
+
+    class Device:
+        def __init__(self, device):
+            self.index = device if device is None or isinstance(device, int) else torch.device(device).index
+
+        def __enter__(self):
+            self.before = current[0]
+            current[0] = self.before if self.index is None else self.index
+
+        def __exit__(self, *a):
+            current[0] = self.before
+
+    class Event:
+        def __init__(self, enable_timing):
+            pass
+
+        def record(self):
+            seen.append(("record", current[0]))
+
+        def synchronize(self):
+            pass
+
+        def elapsed_time(self, other):
+            return 1.0
+
+    class Status:
+        def ones_train_status(self, stream):
+            seen.append(("status", current[0]))
+            return 0
+
+    class Job:
+        device = torch.device("cuda:1")
+
+        def batch(self, samples, seed):
+            return ()
+
+        def step(self):
+            seen.append(("step", current[0]))
+
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(torch.cuda, "Event", Event)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: type("S", (), {"cuda_stream": 0})())
+    monkeypatch.setattr(train, "lib", Status)
+    assert profile_job.profile(Job(), [8], steps=2, warmup=1) == [0.0005]
+    assert {name for name, _ in seen} == {"record", "status", "step"} and {index for _, index in seen} == {1}
+    seen.clear()
+    train.check("cuda:2"), train.check()
+    assert seen == [("status", 2), ("status", 0)]
