@@ -333,8 +333,9 @@ __global__ void __launch_bounds__(kRingThreads, 1)
 // columns is shifted together out of two. The result leaves the same way: a word is put together from the pairs of two
 // lanes. A warp has 64 * NU columns in a row, so that only their ends are written as halves.
 // A row whose first or last block reaches over the ends of the tensor is not copied: its values are read one by one.
-// 2958 x 8111 of 32 bits: 34 us, 5.7 TB/s. For 16 bits the instructions bound it (24 a value, half the issue slots and
-// the barriers between them): 3889 x 6171 in 42 us, 2.3 TB/s, where one value at a time takes 100.
+// 2958 x 8111 of 32 bits: 34 us, 5.7 TB/s. 16 bits take twice the instructions for a byte (23 a value), and the block's 16
+// warps issue in 47 % of the slots only: at the sums' two barriers of a row, for shared memory and for the instruction before
+// they wait 1.8, 1.0 and 1.8 cycles an issue. 3889 x 6171 in 42 us, 2.3 TB/s, where one value at a time takes 100.
 template <class T>
 struct Unit {  // two columns of a row: neighbours for 16 bits, 32 apart for 32 bits
     static constexpr bool k16 = sizeof(T) == 2;
@@ -966,8 +967,9 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_norm_back_odd(const NormBac
     let_successor_start();
 }
 
-// Rows longer than the registers hold: dx from two passes over the row, the sums over rows by columns. 1499 x 16001 of 32
-// bits: 110 us, 2.6 TB/s; such rows are rare enough to leave it there.
+// Rows longer than the registers hold: dx from two passes over the row, the sums over rows by columns, so that x and dy are
+// read three times (the second time from the caches). 1499 x 16001 of 32 bits: 150 us, 80 of them here and 64 in the kernel
+// below, where 288 MB once take 44: a block's registers do not hold more than 8192 such columns beside their sums.
 template <class T>
 __global__ void __launch_bounds__(kLongThreads) k_norm_back_long(const NormBack a) {
     __shared__ float s[2 * kLongThreads / 32];
