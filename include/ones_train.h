@@ -57,7 +57,7 @@ int ones_layer_norm_backward(const void* d_dy, int64_t lddy, const void* d_x, in
  * A row whose target lies outside [0, vocab) takes no part: its loss is 0 (its lse is still written).
  *   d_hidden [rows][cols], d_weight [vocab][cols] of `type` (ONES_BF16 or ONES_F16), 16-byte aligned, ldh and ldw
  *   multiples of 8 (else ONES_ERR_ALIGN); d_target int64[rows]; d_loss, d_lse float[rows].
- *   rows >= 0, cols >= 1, vocab >= 1; any sizes otherwise.
+ *   rows >= 0, cols >= 1, vocab >= 1, each at most 2^30; any sizes otherwise.
  *   d_workspace  at least ones_linear_ce_workspace_bytes(rows, vocab) bytes, 256-byte aligned.
  * Logits are accumulated and reduced in 32 bits.  The tensor cores cut their sums off towards zero; what dense rows lose by
  * that in the mean, 2^-30 of a logit per column, is given back for up to 4096 columns, whatever the row: a logit that comes
@@ -93,7 +93,8 @@ int ones_linear_ce_backward(const float* d_dloss, const void* d_hidden, int64_t 
  *   X = G / (|G|_F + eps);   `steps` times:  A = X X^T,  X <- (a I + b A + c A^2) X      (on the shorter side)
  * which moves every singular value of G towards 1 (for the usual coefficients a, b, c: into about [0.7, 1.2]).
  *   d_g of `type` (any of the three), any alignment of its elements; d_out [count][m][n] of bfloat16, rows n apart.
- *   1 <= steps <= ONES_UPDATE_MAX_STEPS (one launch runs them all), eps > 0, finite coefficients, sizes >= 1.
+ *   1 <= steps <= ONES_UPDATE_MAX_STEPS (one launch runs them all), eps > 0, finite coefficients, sizes >= 1;
+ *   count <= 65535, m and n <= 2^20.
  * Products run on 16-bit operands (11 significant bits, scaled into range, also where |G| is down to 2^-50 of eps) with
  * 32-bit accumulators; the norm is summed in 64 bits.
  *   d_workspace  at least ones_orthogonalize_workspace_bytes(count, m, n) bytes, 256-byte aligned. */
