@@ -24,8 +24,8 @@ def _deps() -> list[str]:
         glob.glob(os.path.join(INCLUDE, "*.h"))
 
 
-def _torch_source() -> str:
-    return os.path.join(CSRC, "ones_train_torch.cpp")
+def _torch_sources() -> list[str]:
+    return sorted(glob.glob(os.path.join(CSRC, "*.cpp")))
 
 
 def _newer(lib: str, deps: list[str]) -> bool:
@@ -33,7 +33,8 @@ def _newer(lib: str, deps: list[str]) -> bool:
 
 
 def up_to_date() -> bool:
-    return _newer(LIB, _deps()) and _newer(TORCH_LIB, [_torch_source()] + glob.glob(os.path.join(INCLUDE, "*.h")))
+    return _newer(LIB, _deps()) and _newer(TORCH_LIB, _torch_sources() + [os.path.join(CSRC, "ones_torch.h")] +
+                                           glob.glob(os.path.join(INCLUDE, "*.h")))
 
 
 def _torch_command(out: str) -> list[str]:
@@ -46,7 +47,7 @@ def _torch_command(out: str) -> list[str]:
                 sysconfig.get_paths()["include"]]
     return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-DTORCH_EXTENSION_NAME=_train_torch",
             "-DTORCH_API_INCLUDE_EXTENSION_H", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
-            *[x for i in includes for x in ("-isystem", i)], _torch_source(), "-o", out, "-L", os.path.join(root, "lib"), "-ltorch",
+            *[x for i in includes for x in ("-isystem", i)], *_torch_sources(), "-o", out, "-L", os.path.join(root, "lib"), "-ltorch",
             "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python", "-lc10", "-lc10_cuda", "-L", _HERE, "-l:libones.so", "-Wl,-rpath,$ORIGIN"]
 
 

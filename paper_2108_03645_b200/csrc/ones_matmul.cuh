@@ -462,9 +462,6 @@ struct Operand {
 
 cudaError_t make_map(CUtensorMap* out, const Operand& o, int rows, int k, int batch, bool f16, int box = 128);  // box: rows (K contiguous)
 
-int device_sms();  // of the current device; 148 where that cannot be asked
-
-
 // Pairs of CTAs with tiles of 256 x 256 multiply at the tensor cores' rate (511 cycles per stage of K = 64, of 512);
 // tiles of 128 x 128 are held up by what an SM gets from L2 (450 cycles of 256), but leave fewer SMs idle. A tile of the
 // pair keeps it busy for two units of time, a small tile its SM for kSmallCost: the smaller number of waves times cost wins.

@@ -221,6 +221,9 @@ struct WaitControl {
 extern const WaitControl norm_waits, loss_waits, update_waits;
 
 // ---- TMA ----
+// The map of a three-dimensional tensor of 16-bit values (strides in bytes) in boxes with the 128-byte swizzle.
+cudaError_t encode_box(CUtensorMap* out, const void* p, const uint64_t (&dims)[3], const uint64_t (&strides)[2], const uint32_t (&box)[3], bool f16);
+
 __device__ __forceinline__ void tma_prefetch(const CUtensorMap* map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }

@@ -7,6 +7,8 @@
 
 namespace ones {
 
+int device_sms();  // of the current device; 148 where that cannot be asked
+
 inline bool aligned(const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
 // Lets the kernel use `bytes` of dynamic shared memory on the current device; `ready` holds the devices that know.
@@ -40,6 +42,6 @@ cudaError_t launch_after(void (*kernel)(P...), dim3 grid, dim3 block, cudaStream
 }  // namespace ones
 
 // For tests, beside the public functions: the limit of every wait on the current device (0: the default), and a kernel of one
-// of the three files (0 to 2) that waits `times` times for what never comes.
+// of the five files (0 to 4) that waits `times` times for what never comes.
 extern "C" int ones_train_wait_limit(unsigned long long ns);
 extern "C" int ones_train_wait_for_nothing(int which, int times, void* cuda_stream);

@@ -1,37 +1,9 @@
 // Marshalling of the training-step operators for torch tensors: argument checks, outputs and workspaces from torch's
 // allocator, the current stream. All the work is behind the C ABI (ones_train.h). Small calls are bound by what the host
 // does before the launch: the same in Python takes 9 us of a layer norm's 13.
-#include <ATen/cuda/CUDAContext.h>
-#include <c10/cuda/CUDAGuard.h>
-#include <torch/extension.h>
-
-#include <initializer_list>
-#include <optional>
-
-#include "ones_train.h"
+#include "ones_torch.h"
 
 namespace {
-
-using at::Tensor;
-using MaybeTensor = std::optional<Tensor>;
-
-int kind_of(at::ScalarType t) {
-    return t == at::kFloat ? ONES_F32 : t == at::kBFloat16 ? ONES_BF16 : t == at::kHalf ? ONES_F16 : -1;
-}
-
-// Results have no graph: who asks for a gradient (or sends a tangent) through here would get none, without a word.
-void no_graph(std::initializer_list<const Tensor*> ts) {
-    for (const Tensor* t : ts)
-        TORCH_CHECK_VALUE(!(t->requires_grad() && at::GradMode::is_enabled()) && !t->_fw_grad(0).defined(),
-                          "an input requires a gradient, but this function is not differentiable: use layer_norm_autograd or "
-                          "linear_cross_entropy_autograd, or call it under torch.no_grad()");
-}
-const Tensor* given(const MaybeTensor& t, const Tensor& other) { return t ? &*t : &other; }
-
-void* ptr(const MaybeTensor& t) { return t ? t->data_ptr() : nullptr; }
-void* stream() { return at::cuda::getCurrentCUDAStream().stream(); }
-Tensor bytes(size_t n, const Tensor& like) { return at::empty({(int64_t)n}, like.options().dtype(at::kByte)); }
-Tensor fresh(at::IntArrayRef shape, const Tensor& like, at::ScalarType type) { return at::empty(shape, like.options().dtype(type)); }
 
 // A tensor [..][cols] as rows that can be read, and the distance of two rows in values. align: 8 for rows that have to
 // start on 16-byte boundaries (16-bit types).
@@ -64,8 +36,6 @@ bool is_param(const MaybeTensor& t, int64_t cols, const Tensor& x) {
     return !t || (t->dim() == 1 && t->size(0) == cols && t->device() == x.device() && t->is_contiguous() &&
                   (t->scalar_type() == at::kFloat || t->scalar_type() == x.scalar_type()));
 }
-
-py::object result(int rc, py::object v) { return rc ? py::int_(rc) : std::move(v); }
 
 py::object layer_norm(const Tensor& x, const MaybeTensor& weight, const MaybeTensor& bias, double eps) {
     no_graph({&x, given(weight, x), given(bias, x)});
@@ -194,4 +164,5 @@ PYBIND11_MODULE(_train_torch, m) {
     m.def("linear_cross_entropy", &linear_cross_entropy);
     m.def("linear_cross_entropy_backward", &linear_cross_entropy_backward);
     m.def("orthogonalize", &orthogonalize);
+    add_attention(m);
 }

@@ -1,18 +1,20 @@
-"""Training-step operators: binding of ``ones_train.h``.
+"""Training-step operators: binding of ``ones_train.h`` and ``ones_attention.h``.
 
 `lib()` is the C ABI through ctypes.  The functions below take torch tensors and go through ``_train_torch``, a small
 compiled module that checks arguments, allocates outputs and workspaces and calls the same C ABI: small calls are bound
 by the host, and the same marshalling in Python costs 9 us a call.
 
-Layer norm, the cross entropy of a projection on a large vocabulary, both with their gradients, and the orthogonalised
-update of matrix parameters, for CUDA tensors.  Work goes to torch's current stream of the tensors' device; outputs and
+Layer norm, the cross entropy of a projection on a large vocabulary, norms of queries and keys with their rotation, causal
+attention over packed sequences, all with their gradients, the orthogonalised update of matrix parameters and the clipping of
+gradients, for CUDA tensors.  Work goes to torch's current stream of the tensors' device; outputs and
 workspaces come from torch's allocator on that stream.  Nothing synchronises except `check`.
 
 The functions take rows with any stride between them (a slice of a wider buffer is read in place).  Other layouts, and
 for the cross entropy rows that do not start on 16-byte boundaries, are copied first.
 
 Their results have no graph, so they refuse inputs that require a gradient while gradients are recorded, and tangents of
-forward mode; `layer_norm_autograd` and `linear_cross_entropy_autograd` are differentiable, once.
+forward mode; `layer_norm_autograd`, `linear_cross_entropy_autograd`, `qk_norm_autograd` and `attention_autograd` are
+differentiable, once.
 """
 from __future__ import annotations
 
@@ -48,6 +50,34 @@ _SIGNATURES = {
     "ones_train_status": (C.c_int, [C.c_void_p]),
 }
 
+
+
+class Heads(C.Structure):
+    """``ones_heads``: vectors of a head for each token, strides in values."""
+    _fields_ = [("data", C.c_void_p), ("token", C.c_int64), ("head", C.c_int64), ("heads", C.c_int32)]
+
+
+_HEADS = C.POINTER(Heads)
+
+_ATTENTION_SIGNATURES = {
+    "ones_qk_norm": (C.c_int, [_HEADS, _HEADS, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
+                               C.c_int32, C.c_float, C.c_int32, C.c_int32, _HEADS, _HEADS, C.c_void_p]),
+    "ones_qk_norm_workspace_bytes": (C.c_size_t, [C.c_int32]),
+    "ones_qk_norm_backward": (C.c_int, [_HEADS, _HEADS, _HEADS, _HEADS, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32,
+                                        C.c_int32, C.c_int32, C.c_int32, C.c_float, C.c_int32, C.c_int32, _HEADS, _HEADS, C.c_void_p,
+                                        C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "ones_attention_workspace_bytes": (C.c_size_t, [C.c_int32] * 4),
+    "ones_attention": (C.c_int, [_HEADS, _HEADS, _HEADS, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_float, C.c_int32, _HEADS,
+                                 C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "ones_attention_backward_workspace_bytes": (C.c_size_t, [C.c_int32] * 5),
+    "ones_attention_backward": (C.c_int, [_HEADS, _HEADS, _HEADS, _HEADS, _HEADS, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
+                                          C.c_int32, C.c_float, C.c_int32, _HEADS, _HEADS, _HEADS, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "ones_gradient_norm_workspace_bytes": (C.c_size_t, [C.c_int32]),
+    "ones_gradient_norm": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "ones_clip_gradients": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_double, C.c_double, C.c_void_p,
+                                      C.c_void_p, C.c_size_t, C.c_void_p]),
+}
+
 _lib = None
 
 
@@ -56,7 +86,7 @@ def lib() -> C.CDLL:
     global _lib
     if _lib is None:
         L = _b.lib()
-        for name, (res, args) in _SIGNATURES.items():
+        for name, (res, args) in (_SIGNATURES | _ATTENTION_SIGNATURES).items():
             fn = getattr(L, name)
             fn.restype = res
             fn.argtypes = args
@@ -123,6 +153,56 @@ def orthogonalize(g: torch.Tensor, *, steps: int = 5, coefficients=(3.4445, -4.7
     return _done((_ops or _load()).orthogonalize(g, steps, a, b, c, eps), "ones_orthogonalize")
 
 
+def qk_norm(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, frequencies: torch.Tensor, q_weight=None, k_weight=None, *,
+            eps: float = 1e-6, interleaved: bool = False):
+    """Root-mean-square norm of every head's query and key, and the rotation of its position (``ones_qk_norm``): (q, k), new
+    tensors.  q, k [..][heads][dim]; positions int64 [..]; frequencies float64 (`rotary_frequencies`): the first twice as many
+    values of a head turn, pairs being i and i + rotary / 2, or neighbours where interleaved.  Weights: None, or vectors of q's
+    type or of float32."""
+    return _done((_ops or _load()).qk_norm(q, k, positions, frequencies, q_weight, k_weight, eps, interleaved), "ones_qk_norm")
+
+
+def qk_norm_backward(dq: torch.Tensor, dk: torch.Tensor, q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor,
+                     frequencies: torch.Tensor, q_weight=None, k_weight=None, *, eps: float = 1e-6, interleaved: bool = False,
+                     parameters: bool = True):
+    """Gradients of `qk_norm` (``ones_qk_norm_backward``) for the gradients dq, dk of its results: (dq, dk, dq_weight, dk_weight),
+    the latter two in the type of the weights (float32 where both are None), or None both with parameters=False."""
+    return _done((_ops or _load()).qk_norm_backward(dq, dk, q, k, positions, frequencies, q_weight, k_weight, eps, interleaved, parameters),
+                 "ones_qk_norm_backward")
+
+
+def rotary_frequencies(rotary: int, base: float = 10000.0, *, device="cuda") -> torch.Tensor:
+    """The frequencies base^(-2 i / rotary), i < rotary / 2, in float64, for `qk_norm`."""
+    if rotary < 0 or rotary % 2:
+        raise ValueError("rotary: an even number of values is needed")
+    return base ** (torch.arange(rotary // 2, dtype=torch.float64, device=device) * (-2.0 / max(rotary, 1)))
+
+
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets=None, *, scale: float | None = None):
+    """Causal attention (``ones_attention``): (out, lse), out with q's shape, lse float32 without its last dimension.
+    q [tokens][heads][dim], k and v [tokens][kv heads][dim] with the sequences packed one behind the other, bounds in `offsets`
+    (int64, on the device; None: one sequence), or all [batch][tokens][..] without offsets.  scale: None for 1 / sqrt(dim).
+    Tokens of no sequence have out = 0 and lse = 0."""
+    return _done((_ops or _load()).attention(q, k, v, offsets, scale), "ones_attention")
+
+
+def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
+                       offsets=None, *, scale: float | None = None):
+    """Gradients of `attention` (``ones_attention_backward``) for the gradient dout of out: (dq, dk, dv)."""
+    return _done((_ops or _load()).attention_backward(dout, q, k, v, out, lse, offsets, scale), "ones_attention_backward")
+
+
+def gradient_norm(gradients) -> torch.Tensor:
+    """Euclidean norm of all values of a list of tensors (``ones_gradient_norm``): float32, 0-d, on the device."""
+    return _done((_ops or _load()).clip(list(gradients), None, None, 0.0), "ones_gradient_norm")
+
+
+def clip_gradients(gradients, max_norm: float, *, out=None, eps: float = 1e-6) -> torch.Tensor:
+    """Scales all gradients by min(1, max_norm / (norm + eps)) (``ones_clip_gradients``), in place or into the tensors `out` (of the
+    same shapes, strides and types); returns the norm before, float32, 0-d.  Nothing synchronises."""
+    return _done((_ops or _load()).clip(list(gradients), None if out is None else list(out), max_norm, eps), "ones_clip_gradients")
+
+
 def check(device=None) -> None:
     """Waits for the current stream of `device` (None: the current one) and raises if a kernel on it gave up waiting since the
     last check (``ones_train_status``). Such a kernel's results are void, and nothing else says so: a program calls this before it
@@ -163,6 +243,38 @@ class _LinearCrossEntropy(torch.autograd.Function):
         return (*linear_cross_entropy_backward(dloss, hidden, weight, target, lse), None)
 
 
+class _QkNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, positions, frequencies, q_weight, k_weight, eps, interleaved):
+        ctx.save_for_backward(q, k, positions, frequencies, q_weight, k_weight)
+        ctx.form = (eps, interleaved)
+        return qk_norm(q, k, positions, frequencies, q_weight, k_weight, eps=eps, interleaved=interleaved)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dq, dk):
+        q, k, positions, frequencies, q_weight, k_weight = ctx.saved_tensors
+        eps, interleaved = ctx.form
+        dq, dk, dqw, dkw = qk_norm_backward(dq, dk, q, k, positions, frequencies, q_weight, k_weight, eps=eps, interleaved=interleaved,
+                                            parameters=q_weight is not None or k_weight is not None)
+        return dq, dk, None, None, dqw if q_weight is not None else None, dkw if k_weight is not None else None, None, None
+
+
+class _Attention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, offsets, scale):
+        out, lse = attention(q, k, v, offsets, scale=scale)
+        ctx.save_for_backward(q, k, v, out, lse, offsets)
+        ctx.scale = scale
+        return out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dout):
+        q, k, v, out, lse, offsets = ctx.saved_tensors
+        return (*attention_backward(dout, q, k, v, out, lse, offsets, scale=ctx.scale), None, None)
+
+
 def layer_norm_autograd(x, weight=None, bias=None, eps: float = 1e-5) -> torch.Tensor:
     """`layer_norm` as a (once) differentiable function of x, weight and bias: y."""
     return _LayerNorm.apply(x, weight, bias, eps)
@@ -171,3 +283,13 @@ def layer_norm_autograd(x, weight=None, bias=None, eps: float = 1e-5) -> torch.T
 def linear_cross_entropy_autograd(hidden, weight, target) -> torch.Tensor:
     """`linear_cross_entropy` as a (once) differentiable function of hidden and weight: the loss of each row."""
     return _LinearCrossEntropy.apply(hidden, weight, target)
+
+
+def qk_norm_autograd(q, k, positions, frequencies, q_weight=None, k_weight=None, *, eps: float = 1e-6, interleaved: bool = False):
+    """`qk_norm` as a (once) differentiable function of q, k and the weights: (q, k)."""
+    return _QkNorm.apply(q, k, positions, frequencies, q_weight, k_weight, eps, interleaved)
+
+
+def attention_autograd(q, k, v, offsets=None, *, scale: float | None = None) -> torch.Tensor:
+    """`attention` as a (once) differentiable function of q, k and v: out."""
+    return _Attention.apply(q, k, v, offsets, scale)
