@@ -101,6 +101,16 @@ __device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[32
 }
 __device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// Two columns of each lane, for what two warps of the same lanes tell each other.
+__device__ __forceinline__ void tmem_put(uint32_t addr, float a, float b) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1, %2};\n\ttcgen05.wait::st.sync.aligned;" ::"r"(addr), "f"(a), "f"(b) : "memory");
+}
+__device__ __forceinline__ float2 tmem_get(uint32_t addr) {
+    float2 r;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x2.b32 {%0, %1}, [%2];\n\ttcgen05.wait::ld.sync.aligned;" : "=f"(r.x), "=f"(r.y) : "r"(addr) : "memory");
+    return r;
+}
+
 __device__ __forceinline__ float exp2_of(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));

@@ -1,10 +1,18 @@
 // Gradients of the causal attention.
 //
 // Two passes over the pairs of tiles, each with sums that stay in tensor memory until they are whole: one for each tile of
-// keys (dk and dv: scores, dp and two products over the queries behind it, all heads of the group one after the other), one for
-// each tile of queries (dq: scores, dp and one product over the keys before it). Seven products where five would do if dq
-// were added up in memory: but that takes 64 KB of atomic additions for every pair of tiles, whose order would change the
-// results, or turns taken between blocks. A pair costs 2048 + 1536 cycles of products and 2 x 1024 of exponentials.
+// queries (dq: scores, dp and one product over the keys before it), then one for each tile of keys (dk and dv: scores, dp and
+// two products over the queries behind it, all heads of the group one after the other). Seven products where five would do
+// if dq were added up in memory: but that takes 64 KB of atomic additions for every pair of tiles, whose order would change
+// the results, or turns taken between blocks. A pair costs 1536 + 2048 cycles of products and 2 x 1024 of exponentials.
+//
+// What the rounding to 16 bits costs. The gradients of the scores meet q and k as float16, whatever the type of the tensors:
+// times a power of two they keep 11 bits where bfloat16 would keep 8 (error of dq 2.9e-3 of its norm, of which 1.66e-3 is the
+// rounding of the result, before; 1.7e-3 now). bfloat16 queries and keys are laid out as float16 times a power of two for
+// each head, which is exact for all that is not below 2^-32 of the largest. And delta = dout . out takes over the rounding of
+// out: an error that all pairs of a row share. The sum of a row's ds has to be 0: what the pass over the keys finds it to be is
+// spread over the keys of the row's last tile in proportion to their probabilities, and the delta that this amounts to is
+// left for the second pass.
 #include "ones_attention.cuh"
 
 #include <math.h>
@@ -18,89 +26,177 @@ constexpr int kThreads = 384;  // two groups of four warps that work on scores, 
 struct BackArgs {
     const Item* items;
     const PlanHead* head;
-    const float *lse, *delta;   // [tokens][heads]
-    const unsigned* largest;    // [2][kv]: bits of the largest |dout|^2 and |v|^2 of a head (float16)
+    const float* lse;           // [tokens][heads]
+    float* delta;               // the same; exact from the first pass on
+    const unsigned* largest;    // [4][kv]: bits of the largest finite |dout|, |v|, |q| and |k| of a head or group
     HeadsOut dq, dk, dv;
     int tokens, heads, kv, group, kt, dim;
     float scale;
 };
 
-// float16 holds the probabilities times 2^12, and the scores' gradients times a power of two that takes their bound
-// 2 max |dout| max |v| to 2^15: so that what is small beside it keeps its bits. bfloat16 has the range of 32 bits.
-constexpr float kLift = 12.f;
+// Powers of two. float16 tensors: probabilities times 2^12 for their product with dout, so that small ones keep their bits.
+// Gradients of the scores: times 2^sigma, which takes the bound 2 dim max |dout| max |v| of |dp - delta| to 2^15. bfloat16
+// queries and keys: times 2^q and 2^k, which takes their largest to 2^15.
+constexpr int kLift = 12;
+struct Powers {
+    int sigma, q, k;
+};
+__device__ __forceinline__ int above(unsigned bits) { return (int)(bits >> 23) - 126; }  // |x| < 2^above
+__device__ __forceinline__ int operand_power(unsigned bits) { return min(15 - above(bits), 100); }
 template <bool F16>
-__device__ __forceinline__ float gradient_scale(const BackArgs& g, int h) {
-    if (!F16) return 1.f;
-    const float bound = 2.f * sqrtf(__uint_as_float(g.largest[h])) * sqrtf(__uint_as_float(g.largest[g.kv + h]));
-    if (!(bound > 0.f)) return 1.f;
-    const int e = min(max(14 - ilogbf(bound), -100), 100);
-    return exp2f((float)e);
+__device__ __forceinline__ Powers powers_of(const BackArgs& g, int h) {
+    Powers p;
+    const int bound = 8 + above(g.largest[h]) + above(g.largest[g.kv + h]);  // 2^7 >= dim
+    p.sigma = min(max(15 - bound, -100), 100);
+    p.q = F16 ? 0 : operand_power(g.largest[2 * g.kv + h]);
+    p.k = F16 ? 0 : operand_power(g.largest[3 * g.kv + h]);
+    return p;
 }
 
-// ---- delta = dout . out, and the largest rows ----
+// ---- delta = dout . out, and the largest values ----
 
-struct DeltaArgs {
-    const uint16_t *dout, *out, *v;
-    int64_t dout_token, dout_head, out_token, out_head, v_token, v_head;
-    const PlanHead* head;
+struct SurveyArgs {
+    const uint16_t* p[5];  // dout, v, q, k, out
+    int64_t token[5], head[5];
+    const PlanHead* plan;
     float* delta;
     unsigned* largest;
-    int tokens, heads, kv, dim, wide;
+    int tokens, heads, kv, dim, wide;  // wide: out starts on 16-byte boundaries
 };
 
 template <bool F16>
 __device__ __forceinline__ float value16(uint16_t b) {
     return F16 ? __half2float(__ushort_as_half(b)) : __uint_as_float((uint32_t)b << 16);
 }
+__device__ __forceinline__ uint16_t half_of(const uint4& v, int i) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    return (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+}
 
-// 16 lanes for a row of up to 128 values: pieces of 8 where both rows have them, single values otherwise.
-template <bool F16>
-__global__ void __launch_bounds__(256) k_delta(const DeltaArgs g) {
+// Values c..c + 7 of a vector of dim values that starts on a 16-byte boundary; none behind its last is read.
+__device__ __forceinline__ uint4 eight_of(const uint16_t* p, int c, int dim) {
+    if (c + 8 <= dim) return *reinterpret_cast<const uint4*>(p + c);
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (c + i < dim) w[i / 2] |= (uint32_t)p[c + i] << (16 * (i & 1));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// LANES x 8 values are a vector. A group of lanes takes a token and goes through its heads, four at a time.
+template <bool F16, int LANES>
+__global__ void __launch_bounds__(256) k_survey(const SurveyArgs g) {
+    extern __shared__ unsigned top[];  // [4][kv]
+    constexpr int kGroups = 256 / LANES, kAtOnce = 4;
+    const int lane = threadIdx.x % LANES, c = 8 * lane;
+    for (int i = threadIdx.x; i < 4 * g.kv; i += 256) top[i] = 0;
+    __syncthreads();
     wait_for_predecessor();
     let_successor_start();
-    const int lane = threadIdx.x % 16;
-    const int64_t rows = (int64_t)g.tokens * (g.heads + (F16 ? g.kv : 0));
-    const int t0 = g.head->covered[0], t1 = g.head->covered[1];
-    for (int64_t r0 = (int64_t)blockIdx.x * 16; r0 < rows; r0 += (int64_t)gridDim.x * 16) {
-        const int64_t r = r0 + threadIdx.x / 16;
-        const bool is_v = r >= (int64_t)g.tokens * g.heads;
-        const int64_t q = is_v ? r - (int64_t)g.tokens * g.heads : r;
-        const int n = is_v ? g.kv : g.heads;
-        const int t = (int)(q / n), h = (int)(q - (int64_t)t * n);
-        float dot = 0.f, square = 0.f;
-        if (r < rows && t >= t0 && t < t1) {
-            const uint16_t* a = is_v ? g.v + t * g.v_token + h * g.v_head : g.dout + t * g.dout_token + h * g.dout_head;
-            const uint16_t* b = is_v ? a : g.out + t * g.out_token + h * g.out_head;
-            if (g.wide) {
-                const int c = 8 * lane;
-                if (c < g.dim) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(a + c), y = *reinterpret_cast<const uint4*>(b + c);
-                    const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
+    const int t0 = g.plan->covered[0], t1 = g.plan->covered[1], group = g.heads / g.kv;
+    auto fetch = [&](int which, int t, int h) { return eight_of(g.p[which] + t * g.token[which] + h * g.head[which], c, g.dim); };
+    auto note = [&](const uint4& v, int which, int h) {
+        unsigned m = 0;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float u = value16<F16>((uint16_t)(xw[i / 2] >> (16 * (i & 1)))), w = value16<F16>((uint16_t)(yw[i / 2] >> (16 * (i & 1))));
-                        dot = fmaf(u, w, dot), square = fmaf(u, u, square);
-                    }
+        for (int i = 0; i < 8; ++i) {
+            const unsigned b = __float_as_uint(value16<F16>(half_of(v, i))) & 0x7FFFFFFFu;
+            if (b < 0x7F800000u) m = max(m, b);
+        }
+        unsigned* const at = top + which * g.kv + h;
+        if (m > *at) atomicMax(at, m);
+    };
+    const int rounds = (t1 - t0 + kGroups * gridDim.x - 1) / (kGroups * gridDim.x);
+    for (int round = 0; round < rounds; ++round) {
+        const int t = t0 + (round * gridDim.x + blockIdx.x) * kGroups + threadIdx.x / LANES;
+        const bool live = t < t1;
+        for (int h0 = 0; h0 < g.heads; h0 += kAtOnce) {
+            uint4 a[kAtOnce], b[kAtOnce];
+            float dot[kAtOnce] = {};
+#pragma unroll
+            for (int x = 0; x < kAtOnce; ++x) {
+                a[x] = b[x] = make_uint4(0, 0, 0, 0);
+                if (!live || h0 + x >= g.heads) continue;
+                a[x] = fetch(0, t, h0 + x);
+                if (g.wide) b[x] = fetch(4, t, h0 + x);
+            }
+            if (!g.wide && live) {  // single values, in another order: dout is read again, from the first-level cache
+#pragma unroll
+                for (int x = 0; x < kAtOnce; ++x) {
+                    if (h0 + x >= g.heads) continue;
+                    const uint16_t* const u = g.p[0] + t * g.token[0] + (h0 + x) * g.head[0];
+                    const uint16_t* const w = g.p[4] + t * g.token[4] + (h0 + x) * g.head[4];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (lane + i * LANES < g.dim) dot[x] = fmaf(value16<F16>(u[lane + i * LANES]), value16<F16>(w[lane + i * LANES]), dot[x]);
                 }
-            } else {
-                for (int c = lane; c < g.dim; c += 16) {
-                    const float u = value16<F16>(a[c]), w = value16<F16>(b[c]);
-                    dot = fmaf(u, w, dot), square = fmaf(u, u, square);
+            }
+#pragma unroll
+            for (int x = 0; x < kAtOnce; ++x) {
+                if (live && h0 + x < g.heads) note(a[x], 0, (h0 + x) / group);
+                if (g.wide) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) dot[x] = fmaf(value16<F16>(half_of(a[x], i)), value16<F16>(half_of(b[x], i)), dot[x]);
+                }
+#pragma unroll
+                for (int m = LANES / 2; m; m >>= 1) dot[x] += __shfl_xor_sync(0xFFFFFFFFu, dot[x], m);
+                if (lane == 0 && live && h0 + x < g.heads) g.delta[(int64_t)t * g.heads + h0 + x] = dot[x];
+            }
+        }
+        for (int which = 1; live && which < (F16 ? 2 : 4); ++which) {
+            const int n = which == 2 ? g.heads : g.kv;
+            for (int h0 = 0; h0 < n; h0 += kAtOnce) {
+                uint4 a[kAtOnce];
+#pragma unroll
+                for (int x = 0; x < kAtOnce; ++x) a[x] = h0 + x < n ? fetch(which, t, h0 + x) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int x = 0; x < kAtOnce; ++x)
+                    if (h0 + x < n) note(a[x], which, which == 2 ? (h0 + x) / group : h0 + x);
+            }
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 4 * g.kv; i += 256)
+        if (top[i]) atomicMax(g.largest + i, top[i]);
+}
+
+// ---- bfloat16 queries and keys as float16 ----
+
+struct NarrowArgs {
+    const uint16_t* p[2];  // q, k
+    int64_t token[2], head[2];
+    uint16_t* out[2];      // [tokens][heads][row]
+    const PlanHead* plan;
+    const unsigned* largest;
+    int heads, kv, dim, row;
+};
+
+template <int LANES>
+__global__ void __launch_bounds__(256) k_narrow(const NarrowArgs g) {
+    constexpr int kGroups = 256 / LANES, kAtOnce = 4;
+    const int c = 8 * (threadIdx.x % LANES);
+    wait_for_predecessor();
+    let_successor_start();
+    const int t0 = g.plan->covered[0], t1 = g.plan->covered[1], group = g.heads / g.kv;
+    if (c >= g.row) return;
+    for (int t = t0 + blockIdx.x * kGroups + threadIdx.x / LANES; t < t1; t += gridDim.x * kGroups)
+        for (int which = 0; which < 2; ++which) {
+            const int n = which ? g.kv : g.heads;
+            for (int h0 = 0; h0 < n; h0 += kAtOnce) {
+                uint4 a[kAtOnce];
+#pragma unroll
+                for (int x = 0; x < kAtOnce; ++x)
+                    if (h0 + x < n) a[x] = eight_of(g.p[which] + t * g.token[which] + (h0 + x) * g.head[which], c, g.dim);
+#pragma unroll
+                for (int x = 0; x < kAtOnce; ++x) {
+                    if (h0 + x >= n) continue;
+                    const float f = exp2f((float)operand_power(g.largest[(2 + which) * g.kv + (which ? h0 + x : (h0 + x) / group)]));
+                    uint32_t w[4];
+#pragma unroll
+                    for (int i = 0; i < 8; i += 2) w[i / 2] = pack16<true>(value16<false>(half_of(a[x], i)) * f, value16<false>(half_of(a[x], i + 1)) * f);
+                    *reinterpret_cast<uint4*>(g.out[which] + ((int64_t)t * n + h0 + x) * g.row + c) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
         }
-#pragma unroll
-        for (int m = 8; m; m >>= 1) {
-            dot += __shfl_xor_sync(0xFFFFFFFFu, dot, m);
-            if (F16) square += __shfl_xor_sync(0xFFFFFFFFu, square, m);
-        }
-        if (lane || r >= rows) continue;
-        if (!is_v) g.delta[r] = dot;
-        if (F16 && square > 0.f && square < INFINITY) {
-            unsigned* at = g.largest + (is_v ? g.kv + h : h / (g.heads / g.kv));
-            if (__float_as_uint(square) > *reinterpret_cast<volatile unsigned*>(at)) atomicMax(at, __float_as_uint(square));
-        }
-    }
 }
 
 template <int HALVES>
@@ -118,7 +214,7 @@ struct Back {
 // ---- dq ----
 
 struct QueriesShared {
-    uint64_t q_full, q_free, k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[2], dp_full, dp_free, ds_full[2], acc_full;
+    uint64_t q_full, q_free, k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[2], dp_full, dp_free, ds_full[2], acc_full, met;
     uint32_t tmem;
 };
 
@@ -141,10 +237,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t at_q = base, at_do = base + B::kTile, at_k = base + 2 * B::kTile, at_v = at_k + kKS * B::kTile;
     const uint32_t q_full = smem_u32(&sh.q_full), q_free = smem_u32(&sh.q_free), k_full = smem_u32(sh.k_full), k_empty = smem_u32(sh.k_empty),
                    v_full = smem_u32(sh.v_full), v_empty = smem_u32(sh.v_empty), s_full = smem_u32(sh.s_full), dp_full = smem_u32(&sh.dp_full),
-                   dp_free = smem_u32(&sh.dp_free), ds_full = smem_u32(sh.ds_full), acc_full = smem_u32(&sh.acc_full);
+                   dp_free = smem_u32(&sh.dp_free), ds_full = smem_u32(sh.ds_full), acc_full = smem_u32(&sh.acc_full), met = smem_u32(&sh.met);
     if (threadIdx.x == 0) {
         tma_prefetch(&map_q), tma_prefetch(&map_do), tma_prefetch(&map_k), tma_prefetch(&map_v);
-        bar_init(q_full, 1), bar_init(q_free, 1), bar_init(dp_full, 1), bar_init(dp_free, 8), bar_init(acc_full, 1);
+        bar_init(q_full, 1), bar_init(q_free, 1), bar_init(dp_full, 1), bar_init(dp_free, 8), bar_init(acc_full, 1), bar_init(met, 8);
         for (int i = 0; i < 2; ++i) bar_init(s_full + 8 * i, 1), bar_init(ds_full + 8 * i, 8);
         for (int i = 0; i < 4; ++i) bar_init(k_full + 8 * i, 1), bar_init(k_empty + 8 * i, 1), bar_init(v_full + 8 * i, 1), bar_init(v_empty + 8 * i, 1);
         bar_init_done();
@@ -181,7 +277,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
             __syncwarp();
-            for (int j = 0; j < tiles; ++j) {
+            for (int j = tiles - 1; j >= 0; --j) {
                 if (!(ok = warp_wait(k_empty + 8 * ks, kph ^ 1))) break;
                 if (elect_one()) {
                     bar_expect(k_full + 8 * ks, B::kTile);
@@ -202,7 +298,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
     } else if (warp == 9) {
         // multiply
-        const uint32_t id_s = attend_desc(F16, false, kKeys), id_acc = attend_desc(F16, true, 64 * HALVES);
+        const uint32_t id_s = attend_desc(true, false, kKeys), id_dp = attend_desc(F16, false, kKeys), id_acc = attend_desc(true, true, 64 * HALVES);
         const int steps = (g.dim + 15) / 16;
         int ks = 0, vs = 0;
         uint32_t kph = 0, vph = 0, qph = 0, dpph = 0, t = 0;  // t: tiles so far
@@ -220,7 +316,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int slot = ks;
                 if (j < tiles) {
                     if (!(ok = warp_wait(k_full + 8 * ks, kph))) break;
-                    const int rest = it.end - it.begin - j * kKeys;
+                    const int rest = it.end - it.begin - (tiles - 1 - j) * kKeys;
                     if (rest < kKeys) clear_rows<HALVES>(smem + (2 + ks) * B::kTile, rest, lane);
                     mma_fence_after();
                     if (elect_one()) {
@@ -234,7 +330,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     dpph ^= 1;
                     mma_fence_after();
                     if (elect_one()) {
-                        product_rows(t_dp, at_do, at_v + vs * B::kTile, id_s, steps);
+                        product_rows(t_dp, at_do, at_v + vs * B::kTile, id_dp, steps);
                         mma_commit<1>(dp_full);
                         mma_commit<1>(v_empty + 8 * vs);
                     }
@@ -248,6 +344,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (elect_one()) {
                         const uint32_t a = tmem + 128 * (i & 1);
                         product_tmem(t_acc, a, a + 64, at_k + before * B::kTile, id_acc, j > 1);
+                        if (F16 && j == tiles) product_tmem(t_acc, a + 32, a + 96, at_k + before * B::kTile, id_acc, true);
                         mma_commit<1>(k_empty + 8 * before);
                     }
                     __syncwarp();
@@ -262,8 +359,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else if (warp < 8) {
         const int half = warp / 4, row = threadIdx.x % 128;
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;
-        const float c = g.scale * kLog2e;
-        uint32_t t = 0, dpph = 0, aph = 0;
+        uint32_t t = 0, dpph = 0, aph = 0, mph = 0;
         for (int turn = 0; ok; ++turn) {
             const int64_t w = work_at(turn);
             if ((int64_t)turn * gridDim.x >= total) break;
@@ -282,12 +378,15 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 continue;
             }
-            const float sigma = gradient_scale<F16>(g, h), sigma2 = F16 ? sigma * exp2f(-kLift) : 1.f;
+            const Powers pw = powers_of<F16>(g, h);
+            const int lift = F16 ? kLift : 0;
+            const float sigma = ldexpf(1.f, pw.sigma - lift);
             const int64_t at = (int64_t)token * g.heads + head;
-            const Pair l2 = both(live ? (F16 ? kLift : 0.f) - g.lse[at] * kLog2e : -INFINITY), d2 = both(live ? -g.delta[at] * sigma2 : 0.f);
-            const Pair c2 = both(c), s2 = both(sigma2);
+            const float delta = live ? g.delta[at] : 0.f;
+            const Pair c2 = both(ldexpf(g.scale * kLog2e, -pw.q - pw.k)), l2 = both(live ? lift - g.lse[at] * kLog2e : -INFINITY), s2 = both(sigma);
+            Pair d2 = both(-delta * sigma), sum = both(0.f), lost = both(0.f);  // lost: what the rounding of ds adds to its sum
             const int clean = (it.first - it.begin + 1) / kKeys;
-            for (int j = 0; j < tiles; ++j, ++t) {
+            for (int j = tiles - 1; j >= 0; --j, ++t) {
                 if (!(ok = warp_wait(s_full + 8 * (t & 1), (t >> 1) & 1))) break;
                 mma_fence_after();
                 const uint32_t ts = tmem + 128 * (t & 1) + 64 * half + lanes;
@@ -309,17 +408,71 @@ __global__ void __launch_bounds__(kThreads, 1)
                 mma_fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(dp_free);
-                const int last = token - it.begin - j * kKeys - 64 * half;  // the last key of this half that the row sees
-                uint32_t ds[32];
+                if (j >= clean) {
+                    const int last = token - it.begin - j * kKeys - 64 * half;  // the last key of this half that the row sees
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (32 * x + i > last) s[x][i] = dp[x][i] = 0;
+                }
+                auto p_at = [&](int x, int i) { return pair(__uint_as_float(s[x][i]), __uint_as_float(s[x][i + 1])); };
+                auto ds_at = [&](int x, int i) { return p_at(x, i) * fma2(pair(__uint_as_float(dp[x][i]), __uint_as_float(dp[x][i + 1])), s2, d2); };
+                Pair p2[2] = {both(0.f), both(0.f)};
+                if (j == 0) {
+                    // the last tile: what the row's ds add up to goes into its delta
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            sum = sum + ds_at(x, i);
+                            p2[x] = p2[x] + p_at(x, i);
+                        }
+                    // the other half of the columns is with the warp of the same lanes: they meet in columns that scores have left
+                    const float2 own = make_float2(total_of(sum), total_of(p2[0] + p2[1]));
+                    const float own_lost = F16 ? total_of(lost) : 0.f;
+                    tmem_put(ts + 32, own.x, own.y);
+                    if (F16) tmem_put(ts + 34, own_lost, 0.f);
+                    mma_fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(met);
+                    if (!(ok = warp_wait(met, mph))) break;
+                    mph ^= 1;
+                    mma_fence_after();
+                    const uint32_t there = tmem + 128 * (t & 1) + 64 * (1 - half) + 32 + lanes;
+                    const float2 other = tmem_get(there);
+                    const float r = own.x + other.x, p = own.y + other.y;
+                    if (half == 0 && live) g.delta[at] = delta + ldexpf(r, -pw.sigma);
+                    const float all = F16 ? r + own_lost + tmem_get(there + 2).x : r;
+                    if (p > 0x1p-100f) d2 = d2 + both(-all / p);
+                    if (F16) {  // both have read before either writes there again
+                        mma_fence_before();
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(met);
+                        if (!(ok = warp_wait(met, mph))) break;
+                        mph ^= 1;
+                        mma_fence_after();
+                    }
+                }
+                uint32_t ds[32], rest[32];
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
 #pragma unroll
                     for (int i = 0; i < 32; i += 2) {
-                        const Pair p = pair(__uint_as_float(s[x][i]), __uint_as_float(s[x][i + 1]));
-                        float2 v = split(p * fma2(pair(__uint_as_float(dp[x][i]), __uint_as_float(dp[x][i + 1])), s2, d2));
-                        if (j >= clean) v.x = 32 * x + i > last ? 0.f : v.x, v.y = 32 * x + i + 1 > last ? 0.f : v.y;
-                        ds[16 * x + i / 2] = pack16<F16>(v.x, v.y);
+                        const Pair v = ds_at(x, i);
+                        const float2 f = split(v);
+                        const uint32_t d = pack16<true>(f.x, f.y);
+                        ds[16 * x + i / 2] = d;
+                        sum = sum + v;
+                        if (F16) {
+                            const float2 e = __half22float2(*reinterpret_cast<const __half2*>(&d));
+                            const Pair off = fma2(both(-1.f), v, pair(e.x, e.y));
+                            lost = lost + off;
+                            const float2 o = split(off);
+                            rest[16 * x + i / 2] = pack16<true>(-o.x, -o.y);
+                        }
                     }
+                if (F16 && j == 0) tmem_store(ts + 32, rest);
                 tmem_store(ts, ds);
                 tmem_store_wait();
                 mma_fence_before();
@@ -330,7 +483,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!(ok = warp_wait(acc_full, aph))) break;
             aph ^= 1;
             mma_fence_after();
-            const float f = g.scale / sigma;
+            const float f = ldexpf(g.scale, -pw.sigma - pw.k);
             for (int x = 0; x < HALVES; ++x) {
                 const int col = 32 * (half * HALVES + x);
                 uint32_t o[32];
@@ -353,6 +506,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // ---- dk and dv ----
+
+// float16 tensors: where few tiles add up to dk, the rounding of ds would show beside that of the result (error of dk 1.52 times that of
+// one rounding at 195 queries of 5 heads): ds has two terms there, one product more. With more tiles it averages out (1.38 to 1.45).
+constexpr int kFineTiles = 16;
 
 struct KeysShared {
     uint64_t kv_full, kv_free, q_full[4], q_empty[4], do_full[4], do_empty[4], st_full[2], st_empty[2], s_full, p_full, dp_full, ds_full, acc_full;
@@ -449,7 +606,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
     } else if (warp == 9) {
         // multiply
-        const uint32_t id_s = attend_desc(F16, false, kRows), id_acc = attend_desc(F16, true, 64 * HALVES);
+        const uint32_t id_s = attend_desc(true, false, kRows), id_dp = attend_desc(F16, false, kRows), id_dk = attend_desc(true, true, 64 * HALVES),
+                       id_dv = attend_desc(F16, true, 64 * HALVES);
         const int steps = (g.dim + 15) / 16;
         int slot = 0;
         uint32_t ph = 0, kvph = 0, pph = 0, dsph = 0;
@@ -469,7 +627,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (rest < qrows) clear_rows<HALVES>(smem + (2 + (dp ? kS : 0) + s) * B::kTile, rest, lane);
                 mma_fence_after();
                 if (elect_one()) {
-                    product_rows(dp ? t_dp : tmem, dp ? at_v : at_k, (dp ? at_do : at_q) + s * B::kTile, id_s, steps);
+                    product_rows(dp ? t_dp : tmem, dp ? at_v : at_k, (dp ? at_do : at_q) + s * B::kTile, dp ? id_dp : id_s, steps);
                     mma_commit<1>(dp ? dp_full : s_full);
                 }
                 __syncwarp();
@@ -483,7 +641,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 pph ^= 1;
                 mma_fence_after();
                 if (elect_one()) {
-                    product_tmem(t_dv, tmem, tmem + 64, at_do + s * B::kTile, id_acc, i != 0);
+                    product_tmem(t_dv, tmem, tmem + 64, at_do + s * B::kTile, id_dv, i != 0);
                     mma_commit<1>(do_empty + 8 * s);
                 }
                 __syncwarp();
@@ -492,7 +650,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 dsph ^= 1;
                 mma_fence_after();
                 if (elect_one()) {
-                    product_tmem(t_dk, t_dp, t_dp + 64, at_q + s * B::kTile, id_acc, i != 0);
+                    product_tmem(t_dk, t_dp, t_dp + 64, at_q + s * B::kTile, id_dk, i != 0);
+                    if (F16 && q.tiles <= kFineTiles) product_tmem(t_dk, t_dp + 32, t_dp + 96, at_q + s * B::kTile, id_dk, true);
                     mma_commit<1>(q_empty + 8 * s);
                 }
                 __syncwarp();
@@ -514,7 +673,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int h = (int)(w % g.kv);
             const QuerySpan q = query_span(it, g.kt);
             if (!q.tiles) continue;
-            const float sigma2 = F16 ? gradient_scale<F16>(g, h) * exp2f(-kLift) : 1.f;
+            const float sigma = ldexpf(1.f, powers_of<F16>(g, h).sigma - (F16 ? kLift : 0));
             for (int i = 0; i < q.tiles; ++i) {
                 float l[4], d[4];
 #pragma unroll
@@ -522,8 +681,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const int row = 32 * x + lane, token = q.first + i * g.kt + row / g.group, head = h * g.group + row % g.group;
                     const bool live = row < qrows && token < it.end;
                     const int64_t at = (int64_t)token * g.heads + head;
-                    l[x] = live ? (F16 ? kLift : 0.f) - g.lse[at] * kLog2e : -INFINITY;
-                    d[x] = live ? -g.delta[at] * sigma2 : 0.f;
+                    l[x] = live ? (F16 ? kLift : 0) - g.lse[at] * kLog2e : -INFINITY;
+                    d[x] = live ? -g.delta[at] * sigma : 0.f;
                 }
                 if (!(ok = warp_wait(st_empty + 8 * stage, ph ^ 1))) break;
                 float* const to = stats + stage * 2 * kRows;
@@ -536,7 +695,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else if (warp < 8) {
         const int half = warp / 4, row = threadIdx.x % 128;
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;
-        const Pair c2 = both(g.scale * kLog2e);
         int stage = 0;
         uint32_t stph = 0, ph = 0, aph = 0;
         for (int turn = 0; ok; ++turn) {
@@ -559,8 +717,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 continue;
             }
-            const float sigma = gradient_scale<F16>(g, h);
-            const Pair s2 = both(F16 ? sigma * exp2f(-kLift) : 1.f);
+            const Powers pw = powers_of<F16>(g, h);
+            const Pair c2 = both(ldexpf(g.scale * kLog2e, -pw.q - pw.k)), s2 = both(ldexpf(1.f, pw.sigma - (F16 ? kLift : 0)));
             for (int i = 0; i < q.tiles; ++i) {
                 const int first = q.first + i * g.kt;  // token of the tile's first row
                 const bool masked = first < it.first + kRows - 1;
@@ -569,7 +727,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (!(ok = warp_wait(st_full + 8 * stage, stph))) break;
                 if (!(ok = warp_wait(s_full, ph))) break;
                 mma_fence_after();
-                uint32_t s[2][32], dp[2][32], e[32];
+                uint32_t s[2][32], dp[2][32], e[32], rest[32];
                 tmem_fetch(tmem + 64 * half + lanes, s[0]), tmem_fetch(tmem + 64 * half + 32 + lanes, s[1]);
                 tmem_wait(s[0]), tmem_wait(s[1]);
 #pragma unroll
@@ -611,9 +769,16 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                             for (int y = 0; y < 4; ++y) v[y] = 32 * x + j + y < from ? 0.f : v[y];
                         }
-                        e[16 * x + j / 2] = pack16<F16>(v[0], v[1]), e[16 * x + j / 2 + 1] = pack16<F16>(v[2], v[3]);
+                        e[16 * x + j / 2] = pack16<true>(v[0], v[1]), e[16 * x + j / 2 + 1] = pack16<true>(v[2], v[3]);
+                        if (F16 && q.tiles <= kFineTiles) {
+                            const float2 a16 = __half22float2(*reinterpret_cast<const __half2*>(&e[16 * x + j / 2]));
+                            const float2 b16 = __half22float2(*reinterpret_cast<const __half2*>(&e[16 * x + j / 2 + 1]));
+                            rest[16 * x + j / 2] = pack16<true>(v[0] - a16.x, v[1] - a16.y);
+                            rest[16 * x + j / 2 + 1] = pack16<true>(v[2] - b16.x, v[3] - b16.y);
+                        }
                     }
                 tmem_store(t_dp + 64 * half + lanes, e);
+                if (F16 && q.tiles <= kFineTiles) tmem_store(t_dp + 64 * half + 32 + lanes, rest);
                 tmem_store_wait();
                 mma_fence_before();
                 __syncwarp();
@@ -625,7 +790,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!(ok = warp_wait(acc_full, aph))) break;
             aph ^= 1;
             mma_fence_after();
-            const float f = half ? g.scale / sigma : F16 ? exp2f(-kLift) : 1.f;
+            const float f = half ? ldexpf(g.scale, -pw.sigma - pw.q) : ldexpf(1.f, F16 ? -kLift : 0);
             for (int x = 0; x < 2 * HALVES; ++x) {
                 uint32_t a[32];
                 tmem_fetch((half ? t_dk : t_dv) + 32 * x + lanes, a);
@@ -649,11 +814,11 @@ __global__ void __launch_bounds__(kThreads, 1)
 // ---- host side ----
 
 struct BackPlan {
-    int group, kt;
+    int group, kt, row;
     int64_t most[2];
-    size_t at_start, at_prefix[2], at_items[2], at_largest, at_delta, bytes;
+    size_t at_start, at_prefix[2], at_items[2], at_largest, at_delta, at_narrow[2], bytes;
 };
-BackPlan back_plan(int tokens, int sequences, int heads, int kv) {
+BackPlan back_plan(int tokens, int sequences, int heads, int kv, int dim) {
     BackPlan p;
     p.group = heads / kv, p.kt = kRows / p.group;
     p.most[0] = items_at_most(tokens, sequences, p.kt), p.most[1] = items_at_most(tokens, sequences, kKeys);
@@ -662,8 +827,10 @@ BackPlan back_plan(int tokens, int sequences, int heads, int kv) {
     const size_t bounds = ((size_t)sequences + 1) * 4;
     p.at_start = take(2 * bounds);
     for (int i = 0; i < 2; ++i) p.at_prefix[i] = take(bounds), p.at_items[i] = take((size_t)p.most[i] * sizeof(Item));
-    p.at_largest = take((size_t)2 * kv * 4);
+    p.at_largest = take((size_t)4 * kv * 4);
     p.at_delta = take((size_t)tokens * heads * 4);
+    p.row = (dim + 7) / 8 * 8;
+    p.at_narrow[0] = take((size_t)tokens * heads * p.row * 2), p.at_narrow[1] = take((size_t)tokens * kv * p.row * 2);  // for bfloat16
     p.bytes = at;
     return p;
 }
@@ -688,24 +855,34 @@ cudaError_t launch_pass(K kernel, int smem, std::atomic<uint64_t>& ready, int64_
 }
 
 template <int HALVES, bool F16>
-cudaError_t launch_back(const ones_heads& dout, const ones_heads& q, const ones_heads& k, const ones_heads& v, const DeltaArgs& d, BackArgs a,
-                        const PlanArgs& plan, const BackPlan& p, cudaStream_t stream) {
+cudaError_t launch_back(const ones_heads& dout, const ones_heads& q, const ones_heads& k, const ones_heads& v, const SurveyArgs& d,
+                        const NarrowArgs& n, BackArgs a, const PlanArgs& plan, const BackPlan& p, cudaStream_t stream) {
+    constexpr int kLanes = 8 * HALVES, kGroups = 256 / kLanes;
     CUtensorMap maps[4];
-    cudaError_t err = make_heads_map(&maps[0], q, a.dim, a.tokens, a.group, a.kt, F16);
+    ones_heads qs = q, ks = k;
+    if (!F16) qs = {n.out[0], (int64_t)a.heads * n.row, n.row, a.heads}, ks = {n.out[1], (int64_t)a.kv * n.row, n.row, a.kv};
+    cudaError_t err = make_heads_map(&maps[0], qs, a.dim, a.tokens, a.group, a.kt, true);
     if (err == cudaSuccess) err = make_heads_map(&maps[1], dout, a.dim, a.tokens, a.group, a.kt, F16);
-    if (err == cudaSuccess) err = make_heads_map(&maps[2], k, a.dim, a.tokens, 1, kKeys, F16);
+    if (err == cudaSuccess) err = make_heads_map(&maps[2], ks, a.dim, a.tokens, 1, kKeys, true);
     if (err == cudaSuccess) err = make_heads_map(&maps[3], v, a.dim, a.tokens, 1, kKeys, F16);
     if (err == cudaSuccess) err = launch_plan(plan, 2, stream);
     if (err != cudaSuccess) return err;
-    const int64_t rows = (int64_t)a.tokens * (a.heads + (F16 ? a.kv : 0)), blocks = (rows + 15) / 16, most = 8 * (int64_t)device_sms();
-    err = launch_after(k_delta<F16>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), stream, d);
+    const int blocks = (a.tokens + kGroups - 1) / kGroups, most = 8 * device_sms(), grid = blocks < most ? blocks : most;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid), cfg.blockDim = dim3(256), cfg.dynamicSmemBytes = (size_t)4 * a.kv * 4, cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr, cfg.numAttrs = 1;
+    err = cudaLaunchKernelEx(&cfg, k_survey<F16, kLanes>, d);
+    if (err == cudaSuccess && !F16) err = launch_after(k_narrow<kLanes>, dim3(grid), dim3(256), stream, n);
     if (err != cudaSuccess) return err;
     static std::atomic<uint64_t> ready[2];
-    a.items = plan.items[1], a.head = plan.head + 1;
-    err = launch_pass(k_attention_keys<HALVES, F16>, Back<HALVES>::kSmemKeys, ready[0], p.most[1] * a.kv, stream, maps, a);
-    if (err != cudaSuccess) return err;
     a.items = plan.items[0], a.head = plan.head;
-    return launch_pass(k_attention_queries<HALVES, F16>, Back<HALVES>::kSmemQueries, ready[1], p.most[0] * a.kv, stream, maps, a);
+    err = launch_pass(k_attention_queries<HALVES, F16>, Back<HALVES>::kSmemQueries, ready[0], p.most[0] * a.kv, stream, maps, a);
+    if (err != cudaSuccess) return err;
+    a.items = plan.items[1], a.head = plan.head + 1;
+    return launch_pass(k_attention_keys<HALVES, F16>, Back<HALVES>::kSmemKeys, ready[1], p.most[1] * a.kv, stream, maps, a);
 }
 
 }  // namespace
@@ -718,7 +895,7 @@ extern "C" {
 
 size_t ones_attention_backward_workspace_bytes(int32_t tokens, int32_t sequences, int32_t heads, int32_t kv, int32_t dim) {
     if (ones::bad_counts(tokens, sequences, heads, kv) || dim < 1 || dim > ONES_ATTENTION_MAX_DIM) return 0;
-    return ones::back_plan(tokens, sequences, heads, kv).bytes;
+    return ones::back_plan(tokens, sequences, heads, kv, dim).bytes;
 }
 
 int ones_attention_backward(const ones_heads* dout, const ones_heads* q, const ones_heads* k, const ones_heads* v,
@@ -733,7 +910,7 @@ int ones_attention_backward(const ones_heads* dout, const ones_heads* q, const o
     if (bad || !tokens) return bad;
     if (!d_lse || !d_workspace) return ONES_ERR_NULL;
     if (!aligned(d_lse, 4) || !aligned(d_workspace, 256)) return ONES_ERR_ALIGN;
-    const BackPlan p = back_plan(tokens, sequences, q->heads, k->heads);
+    const BackPlan p = back_plan(tokens, sequences, q->heads, k->heads, dim);
     if (workspace_bytes < p.bytes) return ONES_ERR_WORKSPACE;
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
     uint8_t* const ws = static_cast<uint8_t*>(d_workspace);
@@ -744,19 +921,26 @@ int ones_attention_backward(const ones_heads* dout, const ones_heads* q, const o
     for (int i = 0; i < 2; ++i)
         plan.prefix[i] = reinterpret_cast<int*>(ws + p.at_prefix[i]), plan.items[i] = reinterpret_cast<Item*>(ws + p.at_items[i]);
     unsigned* const largest = reinterpret_cast<unsigned*>(ws + p.at_largest);
-    plan.zero = largest, plan.zeros = 2 * k->heads;
+    plan.zero = largest, plan.zeros = 4 * k->heads;
     float* const delta = reinterpret_cast<float*>(ws + p.at_delta);
     const HeadsOut o = heads_out(*out, tokens);
-    const DeltaArgs d = {static_cast<const uint16_t*>(dout->d_data), o.p, static_cast<const uint16_t*>(v->d_data), dout->token, dout->head, o.token,
-                         o.head, v->token, v->head, plan.head, delta, largest, tokens, q->heads, k->heads, dim, o.wide && dim % 8 == 0};
+    const ones_heads* const five[5] = {dout, v, q, k, out};
+    SurveyArgs d = {};
+    for (int i = 0; i < 5; ++i) d.p[i] = static_cast<const uint16_t*>(five[i]->d_data), d.token[i] = five[i]->token, d.head[i] = five[i]->head;
+    d.plan = plan.head, d.delta = delta, d.largest = largest, d.tokens = tokens, d.heads = q->heads, d.kv = k->heads, d.dim = dim;
+    d.wide = o.wide && dim % 8 == 0;
+    NarrowArgs n = {};
+    for (int i = 0; i < 2; ++i)
+        n.p[i] = d.p[2 + i], n.token[i] = d.token[2 + i], n.head[i] = d.head[2 + i], n.out[i] = reinterpret_cast<uint16_t*>(ws + p.at_narrow[i]);
+    n.plan = plan.head, n.largest = largest, n.heads = q->heads, n.kv = k->heads, n.dim = dim, n.row = p.row;
     const BackArgs a = {nullptr, nullptr, d_lse, delta, largest, heads_out(*dq, tokens), heads_out(*dk, tokens), heads_out(*dv, tokens), tokens,
                         q->heads, k->heads, p.group, p.kt, dim, scale};
     const bool f16 = type == ONES_F16;
     cudaError_t err;
     if (dim > 64)
-        err = f16 ? launch_back<2, true>(*dout, *q, *k, *v, d, a, plan, p, stream) : launch_back<2, false>(*dout, *q, *k, *v, d, a, plan, p, stream);
+        err = f16 ? launch_back<2, true>(*dout, *q, *k, *v, d, n, a, plan, p, stream) : launch_back<2, false>(*dout, *q, *k, *v, d, n, a, plan, p, stream);
     else
-        err = f16 ? launch_back<1, true>(*dout, *q, *k, *v, d, a, plan, p, stream) : launch_back<1, false>(*dout, *q, *k, *v, d, a, plan, p, stream);
+        err = f16 ? launch_back<1, true>(*dout, *q, *k, *v, d, n, a, plan, p, stream) : launch_back<1, false>(*dout, *q, *k, *v, d, n, a, plan, p, stream);
     return err == cudaSuccess ? ONES_OK : ONES_ERR_CUDA;
 }
 

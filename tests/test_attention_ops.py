@@ -227,9 +227,11 @@ def attend64(q, k, v, lengths, scale, dout=None):
             # delta comes from out as it was rounded; dp and delta are sums of 128 products in 32 bits
             de = (do.abs() * out_e[rows, head]).sum(1, keepdim=True) + 2.0 ** -19 * ((do.abs() * o.abs()).sum(1, keepdim=True) + do.abs() @ c.abs().T)
             dse = p * de + ds.abs() * (u + 4 * se) + p * (dp - delta).abs() * length * 2.0 ** -22
-            if f16:  # steps of 2^-24 of a scale that the largest gradient, at most 4 |dout| |v|, uses up to 2^13 at least
-                most = 4 * dout[:sum(lengths)].double().norm(dim=2).max() * v64[:sum(lengths)].norm(dim=2).max()
-                dse = dse + mask * most * 2.0 ** -38
+            # ds is held as float16 times 2^sigma with sigma = 15 - 8 - e - f, where max |dout| >= 2^(e - 1), max |v| >= 2^(f - 1): its
+            # steps are 2^-24 at least, so it is off by 2^-25 2^-sigma = 2^-32 2^(e + f) <= 2^-30 max |dout| max |v|
+            most = dout[:sum(lengths)].double().abs().max() * v64[:sum(lengths)].abs().max()
+            dse = dse + mask * most * 2.0 ** -30
+            if f16:
                 ge["dv"][rows, kh] += 2.0 ** -37 * mask.double().T @ do.abs() + TINY[F16]
                 ge["dq"][rows, head] += TINY[F16]
                 ge["dk"][rows, kh] += TINY[F16]
