@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const PlanArgs a) {
 
 // ---- forward ----
 
-constexpr int kThreads = 384;  // two groups of softmax warps, then load, multiply and two idle warps
+constexpr int kThreads = 384;  // two groups of softmax warps, then load, two that multiply, and one that clears
 constexpr float kGrow = 8.f;   // a row's maximum may grow by so much (log2 of the exponentials) before it is followed
 
 struct ForwardArgs {
@@ -145,28 +145,35 @@ struct ForwardArgs {
     float scale;
 };
 
+// Heads of up to 64 values leave room for two sets of queries and of outputs: a lane then works on its next item's first scores
+// before it writes the last one's output.
 template <int HALVES>
 struct Forward {
     static constexpr int kTile = HALVES * kHalfTile;
+    static constexpr int kSets = HALVES == 2 ? 1 : 2;
     static constexpr int kSlots = HALVES == 2 ? 5 : 8;
-    static constexpr int kSmem = (2 + kSlots) * kTile + 1024;
+    // Warps that multiply: one for each lane, so that short items of one do not wait for those of the other; but where the ring is
+    // short, one warp that takes the lanes in turn: lanes that drift apart hold its slots for longer (16384 tokens, 16 heads of
+    // 128: 1100 us, and 890 in turn).
+    static constexpr int kLanes = HALVES == 2 ? 1 : 2;
+    static constexpr int kStage = HALVES == 2 ? 0 : 8 * kStageBytesOfWarp;  // for the way out
+    static constexpr int kSmem = (2 * kSets + kSlots) * kTile + kStage + 1024;
 };
 
 struct ForwardShared {
-    uint64_t q_full[2], q_free[2], full[8], empty[8], s_full[2], p_full[2], o_full[2];
+    uint64_t q_full[2][2], q_free[2][2], full[8], raw[8], empty[8], s_full[2], p_full[2], o_full[2], acc_full[2][2], acc_free[2][2];
     uint32_t tmem;
 };
 
-// A tile of queries of an item: its first token, how many tiles of keys it meets, where its masked ones begin.
+// A tile of queries of an item: its first token, how many tiles of keys it meets.
 struct QueryTile {
-    int first, tiles, clean;  // tiles of keys; those before `clean` need no mask
+    int first, tiles;
 };
-__device__ __forceinline__ QueryTile query_tile(const Item& it, int which, int kt) {
+__device__ __forceinline__ QueryTile query_tile(const Work& it, int which, int kt) {
     QueryTile q;
     q.first = it.first + which * kt;
     const int last = min(q.first + kt, it.end) - 1 - it.begin;  // of its tokens, from the sequence's begin
     q.tiles = it.begin < 0 || q.first >= it.end ? 0 : last / kKeys + 1;
-    q.clean = q.tiles ? (q.first - it.begin + 1) / kKeys : 0;
     return q;
 }
 
@@ -175,251 +182,359 @@ __global__ void __launch_bounds__(kThreads, 1)
     k_attention(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                 const ForwardArgs g) {
     using F = Forward<HALVES>;
+    using At = Slot<F::kSlots>;   // keys and values in turn; both lanes (tiles of queries) give every slot back
+    using Set = Slot<F::kSets>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ ForwardShared sh;
+    __shared__ WorkList list;
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* const smem = smem_raw + (base - smem_u32(smem_raw));
-    const uint32_t ring = base + 2 * F::kTile;
-    const uint32_t q_full = smem_u32(sh.q_full), q_free = smem_u32(sh.q_free), full = smem_u32(sh.full), empty = smem_u32(sh.empty),
-                   s_full = smem_u32(sh.s_full), p_full = smem_u32(sh.p_full), o_full = smem_u32(sh.o_full);
+    const uint32_t ring = base + 2 * F::kSets * F::kTile;
+    const uint32_t q_full = smem_u32(sh.q_full), q_free = smem_u32(sh.q_free), full = smem_u32(sh.full), raw = smem_u32(sh.raw),
+                   empty = smem_u32(sh.empty), s_full = smem_u32(sh.s_full), p_full = smem_u32(sh.p_full), o_full = smem_u32(sh.o_full),
+                   acc_full = smem_u32(sh.acc_full), acc_free = smem_u32(sh.acc_free);
     if (threadIdx.x == 0) {
         tma_prefetch(&map_q), tma_prefetch(&map_k), tma_prefetch(&map_v);
-        for (int i = 0; i < 2; ++i) {
-            bar_init(q_full + 8 * i, 1), bar_init(q_free + 8 * i, 1), bar_init(s_full + 8 * i, 1), bar_init(p_full + 8 * i, 4);
-            bar_init(o_full + 8 * i, 1);
-        }
-        for (int i = 0; i < F::kSlots; ++i) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
+        for (int i = 0; i < 2; ++i) bar_init(s_full + 8 * i, 1), bar_init(p_full + 8 * i, 4), bar_init(o_full + 8 * i, 1);
+        for (int i = 0; i < 4; ++i) bar_init(q_full + 8 * i, 1), bar_init(q_free + 8 * i, 1), bar_init(acc_full + 8 * i, 1), bar_init(acc_free + 8 * i, 4);
+        for (int i = 0; i < F::kSlots; ++i) bar_init(full + 8 * i, 1), bar_init(raw + 8 * i, 1), bar_init(empty + 8 * i, F::kLanes);
         bar_init_done();
     }
     if (warp == 9) tmem_alloc<1>(smem_u32(&sh.tmem), 512);
+    wait_for_predecessor();
+    let_successor_start();
+    list_work(list, g.items, g.head, g.kv);
     mma_fence_before();
     __syncthreads();
     mma_fence_after();
     const uint32_t tmem = sh.tmem;
-    wait_for_predecessor();
-    let_successor_start();
-    const int64_t total = (int64_t)g.head->count * g.kv;
+    Walk walk(list, g.items, g.kv);
     bool ok = true;
 
+    // The scores of a lane's tile j, and its product with the values; whole warps.
+    auto first_product = [&](int which, uint32_t item, int j, int tiles, uint32_t slot, uint32_t parity) {
+        const Set set(item);
+        const uint32_t bar = 8 * (2 * which + set.at);
+        if (j == 0 && !warp_wait(q_full + bar, set.parity)) return false;
+        if (!warp_wait(full + 8 * slot, parity)) return false;
+        mma_fence_after();
+        if (elect_one()) {
+            product_rows<HALVES>(tmem + 128 * which, base + (which * F::kSets + set.at) * F::kTile, ring + slot * F::kTile, attend_desc(F16, false, kKeys),
+                         (g.dim + 15) / 16);
+            mma_commit<1>(s_full + 8 * which);
+            if (j + 1 == tiles) mma_commit<1>(q_free + bar);
+        }
+        __syncwarp();
+        return true;
+    };
+    auto second_product = [&](int which, uint32_t item, int j, int tiles, uint32_t slot, uint32_t parity, uint32_t count) {
+        const Set set(item);
+        const uint32_t bar = 8 * (2 * which + set.at), to = tmem + 256 + 128 * which + 64 * set.at, ts = tmem + 128 * which;
+        if (!warp_wait(full + 8 * slot, parity)) return false;
+        if (j == 0 && !warp_wait(acc_free + bar, set.parity ^ 1)) return false;
+        if (!warp_wait(p_full + 8 * which, count & 1)) return false;
+        mma_fence_after();
+        if (elect_one()) {
+            product_tmem(to, ts, ts + 32, ring + slot * F::kTile, attend_desc(F16, true, 64 * HALVES), j != 0);
+            mma_commit<1>(o_full + 8 * which);
+            if (j + 1 == tiles) mma_commit<1>(acc_full + bar);
+        }
+        __syncwarp();
+        return true;
+    };
+
     if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (warp == 8) {
-            // load: queries of both tiles, then keys and values in turn
-            int slot = 0;
-            uint32_t ph = 0, qph[2] = {0, 0};
+            // load: keys and values in turn, each lane's queries before the first of them
+            uint32_t n = 0, items[2] = {0, 0};
             const uint32_t qbytes = HALVES * g.group * g.kt * 128;
-            for (int turn = 0; ok; ++turn) {
-                const int64_t w = work_at(turn);
-                if ((int64_t)turn * gridDim.x >= total) break;
-                if (w >= total) continue;
-                const Item it = g.items[w / g.kv];
-                const int h = (int)(w % g.kv);
-                const QueryTile q0 = query_tile(it, 0, g.kt), q1 = query_tile(it, 1, g.kt);
-                const int tiles = max(q0.tiles, q1.tiles);
-                for (int j = 0; ok && j < tiles; ++j) {
-                    for (int kind = 0; ok && kind < 2; ++kind) {
-                        if (kind == 0 && j == 0) {
-                            for (int i = 0; ok && i < 2; ++i) {
-                                if (!(i ? q1.tiles : q0.tiles)) continue;
-                                if (!(ok = warp_wait(q_free + 8 * i, qph[i] ^ 1))) break;
-                                qph[i] ^= 1;
-                                if (elect_one()) {
-                                    bar_expect(q_full + 8 * i, qbytes);
-                                    for (int x = 0; x < HALVES; ++x)
-                                        tma_load<1>(base + i * F::kTile + x * kHalfTile, &map_q, 64 * x, h * g.group, (i ? q1 : q0).first, q_full + 8 * i);
-                                }
-                                __syncwarp();
-                            }
-                            if (!ok) break;
-                        }
-                        if (!(ok = warp_wait(empty + 8 * slot, ph ^ 1))) break;
-                        if (elect_one()) {
-                            bar_expect(full + 8 * slot, F::kTile);
-                            for (int x = 0; x < HALVES; ++x)
-                                tma_load<1>(ring + slot * F::kTile + x * kHalfTile, kind ? &map_v : &map_k, 64 * x, h, it.begin + j * kKeys, full + 8 * slot);
-                        }
-                        __syncwarp();
-                        if (++slot == F::kSlots) slot = 0, ph ^= 1;
-                    }
-                }
-            }
-        } else if (warp == 9) {
-            // multiply
-            const uint32_t id_s = attend_desc(F16, false, kKeys), id_o = attend_desc(F16, true, 64 * HALVES);
-            const int steps = (g.dim + 15) / 16;
-            int slot = 0;
-            uint32_t ph = 0, qph[2] = {0, 0}, pph[2] = {0, 0};
-            for (int turn = 0; ok; ++turn) {
-                const int64_t w = work_at(turn);
-                if ((int64_t)turn * gridDim.x >= total) break;
-                if (w >= total) continue;
-                const Item it = g.items[w / g.kv];
+            while (ok && walk.next()) {
+                const Work it = walk.it;
                 const QueryTile q[2] = {query_tile(it, 0, g.kt), query_tile(it, 1, g.kt)};
                 const int tiles = max(q[0].tiles, q[1].tiles);
-                if (!tiles) continue;
-                // the first scores
-                if (!(ok = warp_wait(full + 8 * slot, ph))) break;
+                for (int i = 0; ok && i < 2 * tiles; ++i, ++n) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    if (!q[i].tiles || !ok) continue;
-                    if (!(ok = warp_wait(q_full + 8 * i, qph[i]))) break;
-                    qph[i] ^= 1;
-                    mma_fence_after();
-                    if (elect_one()) {
-                        product_rows(tmem + 128 * i, base + i * F::kTile, ring + slot * F::kTile, id_s, steps);
-                        mma_commit<1>(s_full + 8 * i);
-                        if (q[i].tiles == 1) mma_commit<1>(q_free + 8 * i);
-                    }
-                    __syncwarp();
-                }
-                if (!ok) break;
-                if (elect_one()) mma_commit<1>(empty + 8 * slot);
-                __syncwarp();
-                if (++slot == F::kSlots) slot = 0, ph ^= 1;
-                for (int j = 0; ok && j < tiles; ++j) {
-                    const int v = slot;
-                    if (!(ok = warp_wait(full + 8 * v, ph))) break;
-                    if (++slot == F::kSlots) slot = 0, ph ^= 1;
-                    const int rest = it.end - it.begin - j * kKeys;
-                    if (rest < kKeys) clear_rows<HALVES>(smem + (2 + v) * F::kTile, rest, lane);
-                    const bool more = j + 1 < tiles;
-                    if (more && !(ok = warp_wait(full + 8 * slot, ph))) break;
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        if (j >= q[i].tiles || !ok) continue;
-                        if (!(ok = warp_wait(p_full + 8 * i, pph[i]))) break;
-                        pph[i] ^= 1;
-                        mma_fence_after();
+                    for (int x = 0; x < 2; ++x) {
+                        if (i != x || !q[x].tiles || !ok) continue;
+                        const Set set(items[x]++);
+                        const uint32_t bar = 8 * (2 * x + set.at);
+                        if (!(ok = warp_wait(q_free + bar, set.parity ^ 1))) break;
                         if (elect_one()) {
-                            product_tmem(tmem + 256 + 128 * i, tmem + 128 * i, tmem + 128 * i + 32, ring + v * F::kTile, id_o, j != 0);
-                            mma_commit<1>(o_full + 8 * i);
-                            if (j + 1 < q[i].tiles) {
-                                product_rows(tmem + 128 * i, base + i * F::kTile, ring + slot * F::kTile, id_s, steps);
-                                mma_commit<1>(s_full + 8 * i);
-                                if (j + 2 == q[i].tiles) mma_commit<1>(q_free + 8 * i);
-                            }
+                            bar_expect(q_full + bar, qbytes);
+                            for (int y = 0; y < HALVES; ++y)
+                                tma_load<1>(base + (x * F::kSets + set.at) * F::kTile + y * kHalfTile, &map_q, 64 * y, walk.it.h * g.group, q[x].first,
+                                            q_full + bar);
                         }
                         __syncwarp();
                     }
                     if (!ok) break;
+                    const At slot(n);
+                    const bool values = i & 1, partial = values && it.end - it.begin < (i / 2 + 1) * kKeys;  // that tile is cleared first
+                    if (!(ok = warp_wait(empty + 8 * slot.at, slot.parity ^ 1))) break;
                     if (elect_one()) {
-                        mma_commit<1>(empty + 8 * v);
-                        if (more) mma_commit<1>(empty + 8 * slot);
+                        const uint32_t bar = (partial ? raw : full) + 8 * slot.at;
+                        bar_expect(bar, F::kTile);
+                        for (int y = 0; y < HALVES; ++y)
+                            tma_load<1>(ring + slot.at * F::kTile + y * kHalfTile, values ? &map_v : &map_k, 64 * y, walk.it.h, it.begin + i / 2 * kKeys, bar);
                     }
                     __syncwarp();
-                    if (more && ++slot == F::kSlots) slot = 0, ph ^= 1;
                 }
+            }
+        } else if (warp == 11) {
+            // clear what lies behind a sequence in its last values
+            uint32_t n = 0, parities = 0;
+            while (ok && walk.next()) {
+                const Work it = walk.it;
+                const int tiles = max(query_tile(it, 0, g.kt).tiles, query_tile(it, 1, g.kt).tiles);
+                if (!tiles) continue;
+                n += 2 * tiles;
+                const int rest = it.end - it.begin - (tiles - 1) * kKeys;
+                if (rest >= kKeys) continue;
+                const At slot(n - 1);
+                if (!(ok = warp_wait(raw + 8 * slot.at, parities >> slot.at & 1))) break;
+                parities ^= 1u << slot.at;
+                clear_rows<HALVES>(smem + (2 * F::kSets + slot.at) * F::kTile, rest, lane);
+                if (lane == 0) bar_arrive(full + 8 * slot.at);
+            }
+        } else if (F::kLanes == 2) {
+            // multiply for one tile of queries: its next scores right behind each product with the values
+            const int which = warp - 9;
+            uint32_t n = 0, items = 0, count = 0;  // slots before the present item, items and tiles of this lane so far
+            int tiles = 0, most = 0, j = -1;
+            int next_tiles = 0, next_most = 0;
+            bool next = false;
+            // The item after the present one: looked up while the softmax warps are at work, not when they are through.
+            auto look = [&]() {
+                next = walk.next();
+                next_tiles = next ? query_tile(walk.it, which, g.kt).tiles : 0;
+                next_most = next ? max(next_tiles, query_tile(walk.it, 1 - which, g.kt).tiles) : 0;
+            };
+            look();
+            // moves to this lane's next tile, past slots that it does not need
+            auto step = [&]() {
+                if (++j < tiles) return true;
+                for (;;) {
+                    for (int i = 2 * j; i < 2 * most; ++i) {
+                        const At slot(n + i);
+                        if (!(ok = warp_wait(full + 8 * slot.at, slot.parity))) return false;
+                        if (lane == 0) bar_arrive(empty + 8 * slot.at);
+                        __syncwarp();
+                    }
+                    n += 2 * most;
+                    if (!next) return false;
+                    j = 0, tiles = next_tiles, most = next_most;
+                    if (tiles) {
+                        ++items;
+                        return true;
+                    }
+                    look();
+                }
+            };
+            auto scores = [&]() {
+                const At slot(n + 2 * j);
+                if (!first_product(which, items - 1, j, tiles, slot.at, slot.parity)) return false;
+                if (elect_one()) mma_commit<1>(empty + 8 * slot.at);
+                __syncwarp();
+                return true;
+            };
+            bool more = step();
+            if (more) ok = scores();
+            while (ok && more) {
+                if (j == 0) look();
+                const At slot(n + 2 * j + 1);
+                if (!(ok = second_product(which, items - 1, j, tiles, slot.at, slot.parity, count))) break;
+                if (elect_one()) mma_commit<1>(empty + 8 * slot.at);
+                __syncwarp();
+                ++count;
+                more = step();
+                if (ok && more) ok = scores();
+            }
+        } else if (warp == 9) {
+            // multiply for both tiles of queries in turn
+            uint32_t n = 0, items[2] = {0, 0}, count[2] = {0, 0};
+            while (ok && walk.next()) {
+                const int tiles[2] = {query_tile(walk.it, 0, g.kt).tiles, query_tile(walk.it, 1, g.kt).tiles};
+                const int most = max(tiles[0], tiles[1]);
+                if (!most) continue;
+                {
+                    const At slot(n);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+                        if (ok && tiles[x]) ok = first_product(x, items[x], 0, tiles[x], slot.at, slot.parity);
+                    if (!ok) break;
+                    if (elect_one()) mma_commit<1>(empty + 8 * slot.at);
+                    __syncwarp();
+                }
+                for (int j = 0; ok && j < most; ++j) {
+                    const At values(n + 2 * j + 1), keys(n + 2 * j + 2);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        if (!ok || j >= tiles[x]) continue;
+                        if (!(ok = second_product(x, items[x], j, tiles[x], values.at, values.parity, count[x]++))) break;
+                        if (j + 1 < tiles[x]) ok = first_product(x, items[x], j + 1, tiles[x], keys.at, keys.parity);
+                    }
+                    if (!ok) break;
+                    if (elect_one()) {
+                        mma_commit<1>(empty + 8 * values.at);
+                        if (j + 1 < most) mma_commit<1>(empty + 8 * keys.at);
+                    }
+                    __syncwarp();
+                }
+                n += 2 * most;
+                items[0] += tiles[0] != 0, items[1] += tiles[1] != 0;
             }
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         const int which = warp / 4, row = threadIdx.x % 128;
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;
         const uint32_t ts = tmem + 128 * which + lanes, to = tmem + 256 + 128 * which + lanes;
         const float c = g.scale * kLog2e;
-        uint32_t sph = 0, oph = 0;  // oph: parity of the next product with the values that is to end
-        for (int turn = 0; ok; ++turn) {
-            const int64_t w = work_at(turn);
-            if ((int64_t)turn * gridDim.x >= total) break;
-            if (w >= total) continue;
-            const Item it = g.items[w / g.kv];
-            const int h = (int)(w % g.kv);
-            const QueryTile q = query_tile(it, which, g.kt);
-            const int token = q.first + row / g.group, head = h * g.group + row % g.group;
-            const bool live = row < g.group * g.kt && token < it.end;
-            uint16_t* const out = g.out.p + (int64_t)token * g.out.token + head * g.out.head;
-            if (it.begin < 0) {  // tokens of no sequence
-                if (live) {
-                    float zero[32];
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) zero[i] = 0.f;
-                    for (int x = 0; x < 2 * HALVES; ++x) write_columns<F16>(out, 32 * x, g.dim, g.out.wide, zero);
-                    g.lse[(int64_t)token * g.heads + head] = 0.f;
-                }
-                continue;
+        uint8_t* const stage = F::kStage ? smem + (2 * F::kSets + F::kSlots) * F::kTile + warp * kStageBytesOfWarp : nullptr;
+        uint32_t count = 0, items = 0;  // tiles and items so far
+        // the item whose output is still to be written
+        RowsOut out = {};
+        float* lse = nullptr;
+        float l = 0.f, top = 0.f;
+        bool pending = false;
+        auto write = [&](uint32_t item) {
+            const Set set(item);
+            const uint32_t bar = 8 * (2 * which + set.at);
+            if (!warp_wait(acc_full + bar, set.parity)) return false;
+            mma_fence_after();
+            const float inv = __frcp_rn(l);
+#pragma unroll 1
+            for (int x = 0; x < 2 * HALVES; ++x) {
+                if (32 * x >= g.dim) break;
+                uint32_t o[32];
+                tmem_fetch(to + 64 * set.at + 32 * x, o);
+                tmem_wait(o);
+                out.write<F16>(32 * x, g.dim, g.out.wide, o, inv, stage);
             }
-            float top = 0.f;
+            mma_fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(acc_free + bar);
+            if (out.own) *lse = top * g.scale + log2_of(l) * kLn2;
+            return true;
+        };
+        // of the row: its token in the tile and its head in the group; the tokens of the warp's first and last row
+        const int row_token = row / g.group, row_head = row - row_token * g.group, first_token = (row & ~31) / g.group, last_token = (row | 31) / g.group;
+        while (ok) {
+            const bool more = walk.next();
+            if (!more && !pending) break;
+            const Work it = walk.it;
+            const QueryTile q = query_tile(it, which, g.kt);
+            const int token = q.first + row_token, head = walk.it.h * g.group + row_head, tiles = more ? q.tiles : 0;
+            const bool live = row < g.group * g.kt && token < it.end;
+            uint16_t* const own = live ? g.out.p + (int64_t)token * g.out.token + head * g.out.head : nullptr;
+            float* const own_lse = g.lse + (int64_t)token * g.heads + head;
+            if (more && it.begin < 0) {  // tokens of no sequence
+                write_zeros(own, g.dim);
+                if (live) *own_lse = 0.f;
+            }
+            if (more && !tiles) continue;
+            float m_row = 0.f;
             Pair sum = both(0.f);
-            for (int j = 0; j < q.tiles; ++j) {
-                if (!(ok = warp_wait(s_full + 8 * which, sph))) break;
-                sph ^= 1;
+            for (int j = 0; j < max(tiles, 1); ++j) {
+                if (tiles) {
+                if (!(ok = warp_wait(s_full + 8 * which, count & 1))) break;
                 mma_fence_after();
+                // The last keys of the tile that the row and the warp's first row may see. Where all rows of the warp see the whole tile,
+                // the work is one run of code; elsewhere pieces of 32 keys that none sees are left out, and only those that not all
+                // see whole are masked.
+                const int reach = q.first - it.begin - j * kKeys, last = reach + row_token, low = reach + first_token;
+                const bool whole = low >= kKeys - 1;
+                const int seen = whole ? 4 : min(max((reach + last_token) / 32 + 1, 1), 4);
                 uint32_t s[4][32];
 #pragma unroll
                 for (int x = 0; x < 4; ++x) tmem_fetch(ts + 32 * x, s[x]);
 #pragma unroll
                 for (int x = 0; x < 4; ++x) tmem_wait(s[x]);
-                if (j >= q.clean) {
-                    const int last = token - it.begin - j * kKeys;  // the last key of the tile that the row may see
+                if (!whole) {
 #pragma unroll
-                    for (int x = 0; x < 4; ++x)
+                    for (int x = 0; x < 4; ++x) {
+                        if (32 * x + 31 <= low) continue;
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
                             if (32 * x + i > last) s[x][i] = 0xFF800000u;  // -infinity
+                    }
                 }
                 float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
+                for (int x = 0; x < 4; ++x)
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) m[x] = fmaxf(m[x], __uint_as_float(s[x][i]));
+                    for (int i = 0; i < 32; i += 8)
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) m[y] = max3(m[y], __uint_as_float(s[x][i + 2 * y]), __uint_as_float(s[x][i + 2 * y + 1]));
                 float tile_top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-                if (tile_top == -INFINITY) tile_top = j ? top : 0.f;
+                if (tile_top == -INFINITY) tile_top = j ? m_row : 0.f;
                 if (j == 0) {
-                    top = tile_top;
-                } else if (__any_sync(0xFFFFFFFFu, (tile_top - top) * c > kGrow)) {
-                    const float next = fmaxf(top, tile_top), f = exp2_of((top - next) * c);
-                    top = next;
+                    m_row = tile_top;
+                } else if (__any_sync(0xFFFFFFFFu, (tile_top - m_row) * c > kGrow)) {
+                    const float next = fmaxf(m_row, tile_top), f = exp2_of((m_row - next) * c);
+                    m_row = next;
                     sum = sum * both(f);
-                    if (!(ok = warp_wait(o_full + 8 * which, oph ^ 1))) break;  // the product of the tile before
+                    if (!(ok = warp_wait(o_full + 8 * which, (count & 1) ^ 1))) break;  // the product of the tile before
                     mma_fence_after();
+                    const uint32_t acc = to + 64 * Set(items).at;
                     for (int x = 0; x < 2 * HALVES; ++x) {
                         uint32_t o[32];
-                        tmem_fetch(to + 32 * x, o);
+                        tmem_fetch(acc + 32 * x, o);
                         tmem_wait(o);
 #pragma unroll
                         for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                        tmem_store(to + 32 * x, o);
+                        tmem_store(acc + 32 * x, o);
                     }
                     tmem_store_wait();
                 }
-                const Pair c2 = both(c), t2 = both(-top * c);
+                const Pair c2 = both(c), t2 = both(-m_row * c);
+                auto probability = [&](uint32_t lo, uint32_t hi) {
+                    const float2 e = split(fma2(pair(__uint_as_float(lo), __uint_as_float(hi)), c2, t2));
+                    const float a = exp2_of(e.x), b = exp2_of(e.y);
+                    sum = sum + pair(a, b);
+                    return pack16<F16>(a, b);
+                };
+                if (whole) {
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    uint32_t p[32];
+                    for (int half = 0; half < 2; ++half) {
+                        uint32_t p[32];
 #pragma unroll
-                    for (int x = 0; x < 2; ++x)
+                        for (int x = 0; x < 2; ++x)
 #pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            const float2 e = split(fma2(pair(__uint_as_float(s[2 * half + x][i]), __uint_as_float(s[2 * half + x][i + 1])), c2, t2));
-                            const float a = exp2_of(e.x), b = exp2_of(e.y);
-                            sum = sum + pair(a, b);
-                            p[16 * x + i / 2] = pack16<F16>(a, b);
+                            for (int i = 0; i < 32; i += 2) p[16 * x + i / 2] = probability(s[2 * half + x][i], s[2 * half + x][i + 1]);
+                        tmem_store(ts + 32 * half, p);
+                    }
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        uint32_t p[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) p[i] = 0;
+                        if (x < seen) {
+#pragma unroll
+                            for (int i = 0; i < 32; i += 2) p[i / 2] = probability(s[x][i], s[x][i + 1]);
                         }
-                    tmem_store(ts + 32 * half, p);
+                        tmem_store(ts + 16 * x, p);
+                    }
                 }
                 tmem_store_wait();
                 mma_fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(p_full + 8 * which);
-                oph ^= 1;
+                ++count;
+                }
+                if (j == 0 && pending) {  // behind the first tile of the next item, or the last item of all
+                    pending = false;
+                    if (!(ok = write(items - 1))) break;
+                }
             }
-            if (!ok) break;
-            if (!q.tiles) continue;
-            if (!(ok = warp_wait(o_full + 8 * which, oph ^ 1))) break;
-            mma_fence_after();
-            const float l = total_of(sum);
-            const float inv = 1.f / l;
-            for (int x = 0; x < 2 * HALVES; ++x) {
-                uint32_t o[32];
-                tmem_fetch(to + 32 * x, o);
-                tmem_wait(o);
-                float v[32];
-#pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(o[i]) * inv;
-                if (live && 32 * x < g.dim) write_columns<F16>(out, 32 * x, g.dim, g.out.wide, v);
-            }
-            if (live) g.lse[(int64_t)token * g.heads + head] = top * g.scale + logf(l);
+            if (!ok || !more) break;
+            out.set(own);
+            lse = own_lse, l = total_of(sum), top = m_row;
+            pending = true;
+            ++items;
         }
     }
     if (!ok) let_copies_end();
@@ -538,6 +653,7 @@ int ones_attention(const ones_heads* q, const ones_heads* k, const ones_heads* v
     if (!d_lse || !d_workspace) return ONES_ERR_NULL;
     if (!aligned(d_lse, 4) || !aligned(d_workspace, 256)) return ONES_ERR_ALIGN;
     const ForwardPlan p = forward_plan(tokens, sequences, q->heads, k->heads);
+    if (p.most * k->heads >= 1ll << 31) return ONES_ERR_BAD_PARAM;
     if (workspace_bytes < p.bytes) return ONES_ERR_WORKSPACE;
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
     uint8_t* const ws = static_cast<uint8_t*>(d_workspace);
@@ -548,7 +664,7 @@ int ones_attention(const ones_heads* q, const ones_heads* k, const ones_heads* v
     plan.items[0] = reinterpret_cast<Item*>(ws + p.at_items), plan.head = reinterpret_cast<PlanHead*>(ws);
     cudaError_t err = launch_plan(plan, 1, stream);
     if (err != cudaSuccess) return ONES_ERR_CUDA;
-    const ForwardArgs a = {plan.items[0], plan.head, heads_out(*out, tokens), d_lse, tokens, q->heads, k->heads, p.group, p.kt, dim, scale};
+    const ForwardArgs a = {plan.items[0], plan.head, heads_out(*out, dim, tokens), d_lse, tokens, q->heads, k->heads, p.group, p.kt, dim, scale};
     const bool f16 = type == ONES_F16;
     if (dim > 64)
         err = f16 ? launch_forward<2, true>(*q, *k, *v, a, p.most, stream) : launch_forward<2, false>(*q, *k, *v, a, p.most, stream);

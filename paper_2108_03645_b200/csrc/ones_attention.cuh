@@ -57,11 +57,23 @@ cudaError_t make_heads_map(CUtensorMap* out, const ones_heads& h, int dim, int t
 
 // ---- device side ----
 
-// D(tmem) (+)= A(tmem) * B(shared) for 16-bit operands: two neighbouring values along K in a 32-bit column.
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+// Operand descriptors differ in their low word only: the tile's place, and what lies between chunks of 64 values (rows taken
+// across). Put together where the instruction is issued, they cost one addition each.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_rows(uint32_t at) { return ((at & 0x3FFFF) >> 4) | (1u << 16); }
+__device__ __forceinline__ uint32_t desc_across(uint32_t at) { return ((at & 0x3FFFF) >> 4) | ((uint32_t)(kHalfTile >> 4) << 16); }
+// D(tmem) (+)= A * B for 16-bit operands: both in shared memory, or A in tensor memory, two neighbouring values along K in a
+// 32-bit column.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+        "{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tsetp.ne.u32 p, %4, 0;\n\tmov.b64 x, {%1, %5};\n\tmov.b64 y, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add), "r"(kDescHigh)
+        : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tsetp.ne.u32 p, %4, 0;\n\tmov.b64 y, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add), "r"(kDescHigh)
         : "memory");
 }
 
@@ -99,6 +111,13 @@ __device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[32
         "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
         : "memory");
 }
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
 __device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Two columns of each lane, for what two warps of the same lanes tell each other.
@@ -111,6 +130,16 @@ __device__ __forceinline__ float2 tmem_get(uint32_t addr) {
     return r;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float log2_of(float x) {
+    float r;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
 __device__ __forceinline__ float exp2_of(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -132,19 +161,21 @@ __device__ __forceinline__ uint32_t attend_desc(bool f16, bool bmn, int width) {
 }
 
 // D = A * B^T over `steps` x 16 columns of two tiles in shared memory, both with rows of columns. Run by one thread.
+template <int HALVES>
 __device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, int steps) {
-    const uint64_t da = operand_desc(a, false, 0), db = operand_desc(b, false, 0);
-    for (int i = 0; i < steps; ++i) {
-        const uint64_t off = (uint64_t)((i & 3) * 32 + (i >> 2) * kHalfTile) >> 4;
-        mma_f16<1>(d, da + off, db + off, idesc, i != 0);
+    const uint32_t da = desc_rows(a), db = desc_rows(b);
+#pragma unroll
+    for (int i = 0; i < 4 * HALVES; ++i) {
+        const uint32_t off = (uint32_t)((i & 3) * 32 + (i >> 2) * kHalfTile) >> 4;
+        if (i < steps) mma_ss(d, da + off, db + off, idesc, i != 0);
     }
 }
 // D (+)= A * B: A in tensor memory (16 rows of B take 8 columns of it; the second half of them starts at `a_second`), B a tile of
 // 128 rows in shared memory, taken along its rows. Run by one thread.
 __device__ __forceinline__ void product_tmem(uint32_t d, uint32_t a, uint32_t a_second, uint32_t b, uint32_t idesc, bool add) {
-    const uint64_t db = operand_desc(b, true, kHalfTile);
+    const uint32_t db = desc_across(b);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) mma_ts(d, (i < 4 ? a : a_second - 32) + 8 * i, db + (uint64_t)(i * (2048 >> 4)), idesc, add || i != 0);
+    for (int i = 0; i < 8; ++i) mma_ts(d, (i < 4 ? a : a_second - 32) + 8 * i, db + i * (2048 >> 4), idesc, add || i != 0);
 }
 
 // Zeros in rows [from, 128) of a tile, by a whole warp, before the tensor core reads it: what lies behind a sequence may hold
@@ -163,35 +194,153 @@ __device__ __forceinline__ void clear_rows(uint8_t* tile, int from, int lane) {
 struct HeadsOut {
     uint16_t* p;
     int64_t token, head;
-    int wide;  // rows start on 16-byte boundaries
+    int wide;  // rows start on 16-byte boundaries, and are pieces of 16 bytes
 };
-__host__ inline HeadsOut heads_out(const ones_heads& h, int tokens) {
+__host__ inline HeadsOut heads_out(const ones_heads& h, int dim, int tokens) {
     return {static_cast<uint16_t*>(h.d_data), h.token, h.head,
-            aligned(h.d_data, 16) && (h.heads <= 1 || h.head % 8 == 0) && (tokens <= 1 || h.token % 8 == 0)};
+            dim % 8 == 0 && aligned(h.d_data, 16) && (h.heads <= 1 || h.head % 8 == 0) && (tokens <= 1 || h.token % 8 == 0)};
 }
-// 32 columns of a row, from column c on, as 16 bits.
-template <bool F16>
-__device__ __forceinline__ void write_columns(uint16_t* row, int c, int dim, bool wide, const float (&v)[32]) {
+// The rows that the lanes of a warp own, on their way out: 32 columns at a time as 16 bits. A store of 16 bytes by each lane to its
+// own row would touch 32 lines at once, and the cache takes one a cycle: four lanes exchange pieces (through 2 KB of the warp's
+// own, or by shuffles where shared memory is full) until each has the same piece of four rows, and write 64 bytes of a row
+// together; predicated, since each branch around a store costs 100 cycles. Rows off 16-byte boundaries: 16 lanes exchange words,
+// and write a row by 2 bytes (15 heads of 77 values, 16 thousand tokens: 260 us for the forward pass with lanes that write
+// their own rows, 120 so).
+constexpr int kStageBytesOfWarp = 32 * 64;
+struct RowsOut {
+    unsigned long long own;   // 0: not there
+    unsigned long long to[4];  // of the four lanes
+    __device__ __forceinline__ void set(uint16_t* row) {
+        own = reinterpret_cast<unsigned long long>(row);
 #pragma unroll
-    for (int i = 0; i < 32; i += 8) {
-        const uint4 q = make_uint4(pack16<F16>(v[i], v[i + 1]), pack16<F16>(v[i + 2], v[i + 3]), pack16<F16>(v[i + 4], v[i + 5]),
-                                   pack16<F16>(v[i + 6], v[i + 7]));
-        if (wide && c + i + 8 <= dim) {
-            *reinterpret_cast<uint4*>(row + c + i) = q;
-        } else {
-            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+        for (int i = 0; i < 4; ++i) to[i] = __shfl_sync(0xFFFFFFFFu, own, (threadIdx.x & 28) + i);
+    }
+    // wide: rows start on 16-byte boundaries and have a multiple of 8 columns
+    template <bool F16>
+    __device__ __forceinline__ void write(int c, int dim, bool wide, const uint32_t (&o)[32], float factor, uint8_t* stage) const {
+        uint32_t w[16];
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (c + i + j < dim) row[c + i + j] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
+        for (int i = 0; i < 16; ++i) {
+            const float2 f = split(pair(__uint_as_float(o[2 * i]), __uint_as_float(o[2 * i + 1])) * both(factor));
+            w[i] = pack16<F16>(f.x, f.y);
+        }
+        const int lane = threadIdx.x % 32;
+        if (wide) {
+            const int at = c + 8 * (lane % 4);
+            if (stage) {
+                uint4* const s = reinterpret_cast<uint4*>(stage);
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[4 * lane + (i ^ (lane >> 1 & 3))] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = (lane & 28) + i;
+                    const uint4 q = s[4 * r + (lane % 4 ^ (r >> 1 & 3))];
+                    w[4 * i] = q.x, w[4 * i + 1] = q.y, w[4 * i + 2] = q.z, w[4 * i + 3] = q.w;
+                }
+            } else {
+#pragma unroll
+                for (int m = 2; m; m >>= 1) {  // piece i of lane l becomes piece l of lane i, for groups of four lanes
+                    const bool up = lane & m;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (i & m) continue;
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) {
+                            const uint32_t give = up ? w[4 * i + y] : w[4 * (i | m) + y], got = __shfl_xor_sync(0xFFFFFFFFu, give, m);
+                            if (up)
+                                w[4 * i + y] = got;
+                            else
+                                w[4 * (i | m) + y] = got;
+                        }
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\t@p st.global.v4.b32 [%0], {%1, %2, %3, %4};\n\t}" ::"l"(to[i] + 2 * at),
+                             "r"(w[4 * i]), "r"(w[4 * i + 1]), "r"(w[4 * i + 2]), "r"(w[4 * i + 3]), "r"((uint32_t)(to[i] != 0 && at < dim))
+                             : "memory");
+            return;
+        }
+        const int col = c + 2 * (lane % 16);
+#pragma unroll
+        for (int m = 8; m; m >>= 1) {  // word i of lane l becomes word l of lane i, for the 16 lanes of a half warp
+            const bool up = lane & m;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                if (i & m) continue;
+                const uint32_t give = up ? w[i] : w[i | m], got = __shfl_xor_sync(0xFFFFFFFFu, give, m);
+                if (up)
+                    w[i] = got;
+                else
+                    w[i | m] = got;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const unsigned long long at = __shfl_sync(0xFFFFFFFFu, own, (lane & 16) + i);
+            asm volatile(
+                "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %3, 0;\n\tsetp.ne.u32 q, %4, 0;\n\t@p st.global.b16 [%0], %1;\n\t@q st.global.b16 [%0 + 2], %2;\n\t}" ::"l"(
+                    at + 2 * col),
+                "h"((uint16_t)w[i]), "h"((uint16_t)(w[i] >> 16)), "r"((uint32_t)(at != 0 && col < dim)), "r"((uint32_t)(at != 0 && col + 1 < dim))
+                : "memory");
         }
     }
+};
+
+// Zeros in the own row, of tokens that belong to no sequence: rarely run, and so kept small.
+__device__ __forceinline__ void write_zeros(uint16_t* row, int dim) {
+#pragma unroll 1
+    for (int c = 0; row && c < dim; ++c) row[c] = 0;
 }
 
 // The items of this block: every gridDim.x-th, to and fro, so that a block that got the larger one of a turn gets the smaller
-// one of the next.
-__device__ __forceinline__ int64_t work_at(int turn) {
-    return (int64_t)turn * gridDim.x + (turn & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+// one of the next. The first of them are looked up once, by all threads, for all warps: fetched by each warp in its turn they
+// cost 1000 cycles apiece, which short items wait for.
+constexpr int kListed = 92;
+struct Work {
+    int first, begin, end, h;  // an item and its head of the keys
+};
+struct WorkList {  // in shared memory
+    int4 listed[kListed];
+    int turns;
+};
+__device__ __forceinline__ int4 fetch_work(const Item* items, uint32_t kv, int turn) {
+    const uint32_t w = turn * gridDim.x + (turn & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x), i = w / kv;
+    const Item a = items[i];
+    return make_int4(a.first, a.begin, a.end, (int)(w - i * kv));
 }
+// By all threads, before a barrier of the block. Items times heads are below 2^31.
+__device__ __forceinline__ void list_work(WorkList& list, const Item* items, const PlanHead* head, int kv) {
+    const uint32_t total = (uint32_t)head->count * kv, two = 2 * gridDim.x, pairs = total / two, left = total - pairs * two;
+    // of every two turns, the first goes to and the second fro
+    const int turns = 2 * pairs + (left > blockIdx.x) + (left > two - 1 - blockIdx.x);
+    for (int t = threadIdx.x; t < min(turns, kListed); t += blockDim.x) list.listed[t] = fetch_work(items, kv, t);
+    if (threadIdx.x == 0) list.turns = turns;
+}
+struct Walk {
+    const WorkList& list;
+    const Item* items;
+    int kv, turn = 0;
+    Work it = {};
+    __device__ __forceinline__ Walk(const WorkList& l, const Item* i, int heads) : list(l), items(i), kv(heads) {}
+    __device__ __forceinline__ bool next() {
+        if (turn >= list.turns) return false;
+        const int4 a = turn < kListed ? list.listed[turn] : fetch_work(items, kv, turn);
+        it = {a.x, a.y, a.z, a.w};
+        ++turn;
+        return true;
+    }
+};
+
+// Slots of a ring (or sets of buffers) by how many were taken before: where the n-th is, and the parity of its barriers' phase.
+template <int SLOTS>
+struct Slot {
+    uint32_t at, parity;
+    __device__ __forceinline__ explicit Slot(uint32_t n) : at(n % SLOTS), parity(n / SLOTS & 1) {}
+};
 
 __device__ __forceinline__ float total_of(Pair a) { return total(a); }
 

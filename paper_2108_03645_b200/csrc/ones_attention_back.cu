@@ -199,27 +199,32 @@ __global__ void __launch_bounds__(256) k_narrow(const NarrowArgs g) {
         }
 }
 
+// Heads of up to 64 values leave room for two sets of what belongs to an item (its tiles in shared memory, its sums in tensor
+// memory), so that the next item's first tile is begun before the sums of the last one are written.
 template <int HALVES>
 struct Back {
     static constexpr int kTile = HALVES * kHalfTile;
+    static constexpr int kSets = HALVES == 2 ? 1 : 2;
     // dq: queries and dout of the tile, rings of keys (needed until the last product) and values
     static constexpr int kKeySlots = HALVES == 2 ? 3 : 4, kValueSlots = HALVES == 2 ? 2 : 3;
-    static constexpr int kSmemQueries = (2 + kKeySlots + kValueSlots) * kTile + 1024;
+    static constexpr int kStage = HALVES == 2 ? 0 : 8 * kStageBytesOfWarp;  // for the way out
+    static constexpr int kSmemQueries = (2 * kSets + kKeySlots + kValueSlots) * kTile + kStage + 1024;
     // dk, dv: keys and values of the tile, rings of queries and dout, their statistics
     static constexpr int kSlots = HALVES == 2 ? 2 : 4;
     static constexpr int kStats = 2;
-    static constexpr int kSmemKeys = (2 + 2 * kSlots) * kTile + kStats * 2 * kRows * 4 + 1024;
+    static constexpr int kSmemKeys = (2 * kSets + 2 * kSlots) * kTile + kStats * 2 * kRows * 4 + kStage + 1024;
 };
 
 // ---- dq ----
 
 struct QueriesShared {
-    uint64_t q_full, q_free, k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[2], dp_full, dp_free, ds_full[2], acc_full, met;
+    uint64_t q_full[2], q_free[2], k_full[4], k_raw[4], k_empty[4], v_full[4], v_empty[4], s_full[2], dp_full, dp_free, ds_full[2], acc_full[2],
+        acc_free[2], met;
     uint32_t tmem;
 };
 
-// Tiles of keys that a tile of queries meets.
-__device__ __forceinline__ int key_tiles(const Item& it, int kt) {
+// Tiles of keys that a tile of queries meets; they are taken from the last to the first.
+__device__ __forceinline__ int key_tiles(const Work& it, int kt) {
     return it.begin < 0 ? 0 : (min(it.first + kt, it.end) - 1 - it.begin) / kKeys + 1;
 }
 
@@ -228,154 +233,202 @@ __global__ void __launch_bounds__(kThreads, 1)
     k_attention_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_do,
                         const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const BackArgs g) {
     using B = Back<HALVES>;
-    constexpr int kKS = B::kKeySlots, kVS = B::kValueSlots;
+    using KeySlot = Slot<B::kKeySlots>;
+    using ValueSlot = Slot<B::kValueSlots>;
+    using Set = Slot<B::kSets>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ QueriesShared sh;
+    __shared__ WorkList list;
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* const smem = smem_raw + (base - smem_u32(smem_raw));
-    const uint32_t at_q = base, at_do = base + B::kTile, at_k = base + 2 * B::kTile, at_v = at_k + kKS * B::kTile;
-    const uint32_t q_full = smem_u32(&sh.q_full), q_free = smem_u32(&sh.q_free), k_full = smem_u32(sh.k_full), k_empty = smem_u32(sh.k_empty),
-                   v_full = smem_u32(sh.v_full), v_empty = smem_u32(sh.v_empty), s_full = smem_u32(sh.s_full), dp_full = smem_u32(&sh.dp_full),
-                   dp_free = smem_u32(&sh.dp_free), ds_full = smem_u32(sh.ds_full), acc_full = smem_u32(&sh.acc_full), met = smem_u32(&sh.met);
+    const uint32_t at_k = base + 2 * B::kSets * B::kTile, at_v = at_k + B::kKeySlots * B::kTile;  // before: queries and dout of each set
+    const uint32_t q_full = smem_u32(sh.q_full), q_free = smem_u32(sh.q_free), k_full = smem_u32(sh.k_full), k_raw = smem_u32(sh.k_raw),
+                   k_empty = smem_u32(sh.k_empty), v_full = smem_u32(sh.v_full), v_empty = smem_u32(sh.v_empty), s_full = smem_u32(sh.s_full),
+                   dp_full = smem_u32(&sh.dp_full), dp_free = smem_u32(&sh.dp_free), ds_full = smem_u32(sh.ds_full),
+                   acc_full = smem_u32(sh.acc_full), acc_free = smem_u32(sh.acc_free), met = smem_u32(&sh.met);
     if (threadIdx.x == 0) {
         tma_prefetch(&map_q), tma_prefetch(&map_do), tma_prefetch(&map_k), tma_prefetch(&map_v);
-        bar_init(q_full, 1), bar_init(q_free, 1), bar_init(dp_full, 1), bar_init(dp_free, 8), bar_init(acc_full, 1), bar_init(met, 8);
-        for (int i = 0; i < 2; ++i) bar_init(s_full + 8 * i, 1), bar_init(ds_full + 8 * i, 8);
-        for (int i = 0; i < 4; ++i) bar_init(k_full + 8 * i, 1), bar_init(k_empty + 8 * i, 1), bar_init(v_full + 8 * i, 1), bar_init(v_empty + 8 * i, 1);
+        bar_init(dp_full, 1), bar_init(dp_free, 8), bar_init(met, 8);
+        for (int i = 0; i < 2; ++i) {
+            bar_init(q_full + 8 * i, 1), bar_init(q_free + 8 * i, 1), bar_init(s_full + 8 * i, 1), bar_init(ds_full + 8 * i, 8);
+            bar_init(acc_full + 8 * i, 1), bar_init(acc_free + 8 * i, 8);
+        }
+        for (int i = 0; i < 4; ++i) {
+            bar_init(k_full + 8 * i, 1), bar_init(k_raw + 8 * i, 1), bar_init(k_empty + 8 * i, 1);
+            bar_init(v_full + 8 * i, 1), bar_init(v_empty + 8 * i, 1);
+        }
         bar_init_done();
     }
     if (warp == 9) tmem_alloc<1>(smem_u32(&sh.tmem), 512);
+    wait_for_predecessor();
+    let_successor_start();
+    list_work(list, g.items, g.head, g.kv);
     mma_fence_before();
     __syncthreads();
     mma_fence_after();
     const uint32_t tmem = sh.tmem, t_dp = tmem + 256, t_acc = tmem + 384;
-    wait_for_predecessor();
-    let_successor_start();
-    const int64_t total = (int64_t)g.head->count * g.kv;
+    Walk walk(list, g.items, g.kv);
     bool ok = true;
 
+    if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (warp == 8) {
         // load
-        int ks = 0, vs = 0;
-        uint32_t kph = 0, vph = 0, qph = 0;
+        uint32_t n = 0, items = 0;
         const uint32_t qbytes = HALVES * g.group * g.kt * 128;
-        for (int turn = 0; ok; ++turn) {
-            const int64_t w = work_at(turn);
-            if ((int64_t)turn * gridDim.x >= total) break;
-            if (w >= total) continue;
-            const Item it = g.items[w / g.kv];
-            const int h = (int)(w % g.kv), tiles = key_tiles(it, g.kt);
-            if (!tiles) continue;
-            if (!(ok = warp_wait(q_free, qph ^ 1))) break;
-            qph ^= 1;
-            if (elect_one()) {
-                bar_expect(q_full, 2 * qbytes);
-                for (int x = 0; x < HALVES; ++x) {
-                    tma_load<1>(at_q + x * kHalfTile, &map_q, 64 * x, h * g.group, it.first, q_full);
-                    tma_load<1>(at_do + x * kHalfTile, &map_do, 64 * x, h * g.group, it.first, q_full);
-                }
-            }
-            __syncwarp();
-            for (int j = tiles - 1; j >= 0; --j) {
-                if (!(ok = warp_wait(k_empty + 8 * ks, kph ^ 1))) break;
-                if (elect_one()) {
-                    bar_expect(k_full + 8 * ks, B::kTile);
-                    for (int x = 0; x < HALVES; ++x)
-                        tma_load<1>(at_k + ks * B::kTile + x * kHalfTile, &map_k, 64 * x, h, it.begin + j * kKeys, k_full + 8 * ks);
-                }
-                __syncwarp();
-                if (++ks == kKS) ks = 0, kph ^= 1;
-                if (!(ok = warp_wait(v_empty + 8 * vs, vph ^ 1))) break;
-                if (elect_one()) {
-                    bar_expect(v_full + 8 * vs, B::kTile);
-                    for (int x = 0; x < HALVES; ++x)
-                        tma_load<1>(at_v + vs * B::kTile + x * kHalfTile, &map_v, 64 * x, h, it.begin + j * kKeys, v_full + 8 * vs);
-                }
-                __syncwarp();
-                if (++vs == kVS) vs = 0, vph ^= 1;
-            }
-        }
-    } else if (warp == 9) {
-        // multiply
-        const uint32_t id_s = attend_desc(true, false, kKeys), id_dp = attend_desc(F16, false, kKeys), id_acc = attend_desc(true, true, 64 * HALVES);
-        const int steps = (g.dim + 15) / 16;
-        int ks = 0, vs = 0;
-        uint32_t kph = 0, vph = 0, qph = 0, dpph = 0, t = 0;  // t: tiles so far
-        for (int turn = 0; ok; ++turn) {
-            const int64_t w = work_at(turn);
-            if ((int64_t)turn * gridDim.x >= total) break;
-            if (w >= total) continue;
-            const Item it = g.items[w / g.kv];
+        while (ok && walk.next()) {
+            const Work it = walk.it;
             const int tiles = key_tiles(it, g.kt);
             if (!tiles) continue;
-            if (!(ok = warp_wait(q_full, qph))) break;
-            qph ^= 1;
-            int before = 0;  // the slot of the keys whose dq comes next
-            for (int j = 0; ok && j <= tiles; ++j) {
-                const int slot = ks;
-                if (j < tiles) {
-                    if (!(ok = warp_wait(k_full + 8 * ks, kph))) break;
-                    const int rest = it.end - it.begin - (tiles - 1 - j) * kKeys;
-                    if (rest < kKeys) clear_rows<HALVES>(smem + (2 + ks) * B::kTile, rest, lane);
-                    mma_fence_after();
-                    if (elect_one()) {
-                        product_rows(tmem + 128 * ((t + j) & 1), at_q, at_k + ks * B::kTile, id_s, steps);
-                        mma_commit<1>(s_full + 8 * ((t + j) & 1));
-                    }
-                    __syncwarp();
-                    if (++ks == kKS) ks = 0, kph ^= 1;
-                    if (!(ok = warp_wait(v_full + 8 * vs, vph))) break;
-                    if (!(ok = warp_wait(dp_free, dpph ^ 1))) break;  // what was there has been read
-                    dpph ^= 1;
-                    mma_fence_after();
-                    if (elect_one()) {
-                        product_rows(t_dp, at_do, at_v + vs * B::kTile, id_dp, steps);
-                        mma_commit<1>(dp_full);
-                        mma_commit<1>(v_empty + 8 * vs);
-                    }
-                    __syncwarp();
-                    if (++vs == kVS) vs = 0, vph ^= 1;
+            const Set set(items++);
+            if (!(ok = warp_wait(q_free + 8 * set.at, set.parity ^ 1))) break;
+            if (elect_one()) {
+                const uint32_t to = base + 2 * set.at * B::kTile, bar = q_full + 8 * set.at;
+                bar_expect(bar, 2 * qbytes);
+                for (int x = 0; x < HALVES; ++x) {
+                    tma_load<1>(to + x * kHalfTile, &map_q, 64 * x, walk.it.h * g.group, it.first, bar);
+                    tma_load<1>(to + B::kTile + x * kHalfTile, &map_do, 64 * x, walk.it.h * g.group, it.first, bar);
                 }
-                if (j > 0) {
-                    const uint32_t i = t + j - 1;
-                    if (!(ok = warp_wait(ds_full + 8 * (i & 1), (i >> 1) & 1))) break;
-                    mma_fence_after();
-                    if (elect_one()) {
-                        const uint32_t a = tmem + 128 * (i & 1);
-                        product_tmem(t_acc, a, a + 64, at_k + before * B::kTile, id_acc, j > 1);
-                        if (F16 && j == tiles) product_tmem(t_acc, a + 32, a + 96, at_k + before * B::kTile, id_acc, true);
-                        mma_commit<1>(k_empty + 8 * before);
-                    }
-                    __syncwarp();
-                }
-                before = slot;
             }
-            if (!ok) break;
-            t += tiles;
-            if (elect_one()) mma_commit<1>(acc_full), mma_commit<1>(q_free);
             __syncwarp();
+            for (int j = tiles - 1; j >= 0; --j, ++n) {
+                const KeySlot ks(n);
+                const bool partial = it.end - it.begin < (j + 1) * kKeys;  // that tile is cleared first
+                if (!(ok = warp_wait(k_empty + 8 * ks.at, ks.parity ^ 1))) break;
+                if (elect_one()) {
+                    const uint32_t bar = (partial ? k_raw : k_full) + 8 * ks.at;
+                    bar_expect(bar, B::kTile);
+                    for (int x = 0; x < HALVES; ++x)
+                        tma_load<1>(at_k + ks.at * B::kTile + x * kHalfTile, &map_k, 64 * x, walk.it.h, it.begin + j * kKeys, bar);
+                }
+                __syncwarp();
+                const ValueSlot vs(n);
+                if (!(ok = warp_wait(v_empty + 8 * vs.at, vs.parity ^ 1))) break;
+                if (elect_one()) {
+                    const uint32_t bar = v_full + 8 * vs.at;
+                    bar_expect(bar, B::kTile);
+                    for (int x = 0; x < HALVES; ++x)
+                        tma_load<1>(at_v + vs.at * B::kTile + x * kHalfTile, &map_v, 64 * x, walk.it.h, it.begin + j * kKeys, bar);
+                }
+                __syncwarp();
+            }
         }
-    } else if (warp < 8) {
+    } else if (warp == 10) {
+        // clear what lies behind a sequence in its last keys
+        uint32_t n = 0, parities = 0;
+        while (ok && walk.next()) {
+            const Work it = walk.it;
+            const int tiles = key_tiles(it, g.kt), rest = it.end - it.begin - (tiles - 1) * kKeys;
+            if (tiles && rest < kKeys) {
+                const KeySlot ks(n);
+                if (!(ok = warp_wait(k_raw + 8 * ks.at, parities >> ks.at & 1))) break;
+                parities ^= 1u << ks.at;
+                clear_rows<HALVES>(smem + (2 * B::kSets + ks.at) * B::kTile, rest, lane);
+                if (lane == 0) bar_arrive(k_full + 8 * ks.at);
+            }
+            n += tiles;
+        }
+    } else if (warp == 9) {
+        // multiply: scores and dp of a tile, then dq of the one before, through all items
+        const uint32_t id_s = attend_desc(true, false, kKeys), id_dp = attend_desc(F16, false, kKeys), id_acc = attend_desc(true, true, 64 * HALVES);
+        const int steps = (g.dim + 15) / 16;
+        uint32_t t = 0, items = 0;  // tiles and items begun
+        int tiles = 0, j = 0;       // of the present item, tile j from the last on
+        struct {
+            bool any, first, last;
+            uint32_t item;
+        } before = {false, false, false, 0};
+        for (;;) {
+            bool any = true;
+            if (--j < 0) {
+                while ((any = walk.next()) && !(tiles = key_tiles(walk.it, g.kt))) {}
+                j = any ? tiles - 1 : 0;
+                items += any;
+            }
+            if (!any && !before.any) break;
+            if (any) {
+                const Set set(items - 1);
+                const KeySlot ks(t);
+                const ValueSlot vs(t);
+                const uint32_t at_q = base + 2 * set.at * B::kTile;
+                if (j == tiles - 1 && !(ok = warp_wait(q_full + 8 * set.at, set.parity))) break;
+                if (!(ok = warp_wait(k_full + 8 * ks.at, ks.parity))) break;
+                mma_fence_after();
+                if (elect_one()) {
+                    product_rows<HALVES>(tmem + 128 * (t & 1), at_q, at_k + ks.at * B::kTile, id_s, steps);
+                    mma_commit<1>(s_full + 8 * (t & 1));
+                }
+                __syncwarp();
+                if (!(ok = warp_wait(v_full + 8 * vs.at, vs.parity))) break;
+                if (!(ok = warp_wait(dp_free, (t & 1) ^ 1))) break;  // what was there has been read
+                mma_fence_after();
+                if (elect_one()) {
+                    product_rows<HALVES>(t_dp, at_q + B::kTile, at_v + vs.at * B::kTile, id_dp, steps);
+                    mma_commit<1>(dp_full);
+                    mma_commit<1>(v_empty + 8 * vs.at);
+                    if (j == 0) mma_commit<1>(q_free + 8 * set.at);
+                }
+                __syncwarp();
+            }
+            if (before.any) {
+                const uint32_t i = t - 1;
+                const Set set(before.item);
+                const KeySlot ks(i);
+                if (!(ok = warp_wait(ds_full + 8 * (i & 1), (i >> 1) & 1))) break;
+                if (before.first && !(ok = warp_wait(acc_free + 8 * set.at, set.parity ^ 1))) break;
+                mma_fence_after();
+                if (elect_one()) {
+                    const uint32_t a = tmem + 128 * (i & 1), k = at_k + ks.at * B::kTile, acc = t_acc + 64 * set.at;
+                    product_tmem(acc, a, a + 64, k, id_acc, !before.first);
+                    if (F16 && before.last) product_tmem(acc, a + 32, a + 96, k, id_acc, true);
+                    mma_commit<1>(k_empty + 8 * ks.at);
+                    if (before.last) mma_commit<1>(acc_full + 8 * set.at);
+                }
+                __syncwarp();
+            }
+            before = {any, j == tiles - 1, j == 0, items - 1};
+            t += any;
+        }
+    }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         const int half = warp / 4, row = threadIdx.x % 128;
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;
-        uint32_t t = 0, dpph = 0, aph = 0, mph = 0;
-        for (int turn = 0; ok; ++turn) {
-            const int64_t w = work_at(turn);
-            if ((int64_t)turn * gridDim.x >= total) break;
-            if (w >= total) continue;
-            const Item it = g.items[w / g.kv];
-            const int h = (int)(w % g.kv), tiles = key_tiles(it, g.kt);
-            const int token = it.first + row / g.group, head = h * g.group + row % g.group;
+        uint32_t t = 0, items = 0, mph = 0;
+        uint8_t* const stage = B::kStage ? smem + (2 * B::kSets + B::kKeySlots + B::kValueSlots) * B::kTile + warp * kStageBytesOfWarp : nullptr;
+        // of the row: its token in the tile and its head in the group
+        const int row_token = row / g.group, row_head = row - row_token * g.group;
+        // the item whose dq is still to be written
+        RowsOut out = {};
+        float factor = 0.f;
+        bool pending = false;
+        auto write = [&](uint32_t item) {
+            const Set set(item);
+            if (!warp_wait(acc_full + 8 * set.at, set.parity)) return false;
+            mma_fence_after();
+#pragma unroll 1
+            for (int x = 0; x < HALVES; ++x) {
+                const int col = 32 * (half * HALVES + x);
+                if (col >= g.dim) break;
+                uint32_t o[32];
+                tmem_fetch(t_acc + 64 * set.at + col + lanes, o);
+                tmem_wait(o);
+                out.write<F16>(col, g.dim, g.dq.wide, o, factor, stage);
+            }
+            mma_fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(acc_free + 8 * set.at);
+            return true;
+        };
+        while (ok && walk.next()) {
+            const Work it = walk.it;
+            const int h = walk.it.h, tiles = key_tiles(it, g.kt);
+            const int token = it.first + row_token, head = h * g.group + row_head;
             const bool live = row < g.group * g.kt && token < it.end;
-            uint16_t* const out = g.dq.p + (int64_t)token * g.dq.token + head * g.dq.head;
+            uint16_t* const own = live ? g.dq.p + (int64_t)token * g.dq.token + head * g.dq.head : nullptr;
             if (it.begin < 0) {
-                if (live) {
-                    float zero[32];
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) zero[i] = 0.f;
-                    for (int x = 0; x < HALVES; ++x) write_columns<F16>(out, 32 * (half * HALVES + x), g.dim, g.dq.wide, zero);
-                }
+                if (half == 0) write_zeros(own, g.dim);
                 continue;
             }
             const Powers pw = powers_of<F16>(g, h);
@@ -400,8 +453,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         const float2 e = split(fma2(pair(__uint_as_float(s[x][i]), __uint_as_float(s[x][i + 1])), c2, l2));
                         s[x][i] = __float_as_uint(exp2_of(e.x)), s[x][i + 1] = __float_as_uint(exp2_of(e.y));
                     }
-                if (!(ok = warp_wait(dp_full, dpph))) break;
-                dpph ^= 1;
+                if (!(ok = warp_wait(dp_full, t & 1))) break;
                 mma_fence_after();
                 tmem_fetch(t_dp + 64 * half + lanes, dp[0]), tmem_fetch(t_dp + 64 * half + 32 + lanes, dp[1]);
                 tmem_wait(dp[0]), tmem_wait(dp[1]);
@@ -418,20 +470,20 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 auto p_at = [&](int x, int i) { return pair(__uint_as_float(s[x][i]), __uint_as_float(s[x][i + 1])); };
                 auto ds_at = [&](int x, int i) { return p_at(x, i) * fma2(pair(__uint_as_float(dp[x][i]), __uint_as_float(dp[x][i + 1])), s2, d2); };
-                Pair p2[2] = {both(0.f), both(0.f)};
                 if (j == 0) {
                     // the last tile: what the row's ds add up to goes into its delta
+                    Pair p2 = both(0.f);
 #pragma unroll
                     for (int x = 0; x < 2; ++x)
 #pragma unroll
                         for (int i = 0; i < 32; i += 2) {
                             sum = sum + ds_at(x, i);
-                            p2[x] = p2[x] + p_at(x, i);
+                            p2 = p2 + p_at(x, i);
                         }
                     // the other half of the columns is with the warp of the same lanes: they meet in columns that scores have left
-                    const float2 own = make_float2(total_of(sum), total_of(p2[0] + p2[1]));
+                    const float2 own_sums = make_float2(total_of(sum), total_of(p2));
                     const float own_lost = F16 ? total_of(lost) : 0.f;
-                    tmem_put(ts + 32, own.x, own.y);
+                    tmem_put(ts + 32, own_sums.x, own_sums.y);
                     if (F16) tmem_put(ts + 34, own_lost, 0.f);
                     mma_fence_before();
                     __syncwarp();
@@ -441,7 +493,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     mma_fence_after();
                     const uint32_t there = tmem + 128 * (t & 1) + 64 * (1 - half) + 32 + lanes;
                     const float2 other = tmem_get(there);
-                    const float r = own.x + other.x, p = own.y + other.y;
+                    const float r = own_sums.x + other.x, p = own_sums.y + other.y;
                     if (half == 0 && live) g.delta[at] = delta + ldexpf(r, -pw.sigma);
                     const float all = F16 ? r + own_lost + tmem_get(there + 2).x : r;
                     if (p > 0x1p-100f) d2 = d2 + both(-all / p);
@@ -472,30 +524,25 @@ __global__ void __launch_bounds__(kThreads, 1)
                             rest[16 * x + i / 2] = pack16<true>(-o.x, -o.y);
                         }
                     }
+                // float16 tensors: the last tile, which is the only one of short rows, has two terms
                 if (F16 && j == 0) tmem_store(ts + 32, rest);
                 tmem_store(ts, ds);
                 tmem_store_wait();
                 mma_fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(ds_full + 8 * (t & 1));
+                if (j == tiles - 1 && pending) {
+                    pending = false;
+                    if (!(ok = write(items - 1))) break;
+                }
             }
             if (!ok) break;
-            if (!(ok = warp_wait(acc_full, aph))) break;
-            aph ^= 1;
-            mma_fence_after();
-            const float f = ldexpf(g.scale, -pw.sigma - pw.k);
-            for (int x = 0; x < HALVES; ++x) {
-                const int col = 32 * (half * HALVES + x);
-                uint32_t o[32];
-                tmem_fetch(t_acc + col + lanes, o);
-                tmem_wait(o);
-                float v[32];
-#pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(o[i]) * f;
-                if (live && col < g.dim) write_columns<F16>(out, col, g.dim, g.dq.wide, v);
-            }
-            mma_fence_before();
+            out.set(own);
+            factor = ldexpf(g.scale, -pw.sigma - pw.k);
+            pending = true;
+            ++items;
         }
+        if (ok && pending) ok = write(items - 1);
     }
     if (!ok) let_copies_end();
     __syncwarp();
@@ -512,7 +559,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 constexpr int kFineTiles = 16;
 
 struct KeysShared {
-    uint64_t kv_full, kv_free, q_full[4], q_empty[4], do_full[4], do_empty[4], st_full[2], st_empty[2], s_full, p_full, dp_full, ds_full, acc_full;
+    uint64_t kv_full[2], kv_free[2], q_full[4], q_raw[4], q_empty[4], do_full[4], do_raw[4], do_empty[4], st_full[2], st_empty[2], s_full, p_full, dp_full,
+        ds_full, acc_full[2], acc_free[2];
     uint32_t tmem;
 };
 
@@ -520,7 +568,7 @@ struct KeysShared {
 struct QuerySpan {
     int first, tiles;  // first token of the first tile
 };
-__device__ __forceinline__ QuerySpan query_span(const Item& it, int kt) {
+__device__ __forceinline__ QuerySpan query_span(const Work& it, int kt) {
     if (it.begin < 0) return {0, 0};
     const int f = (it.first - it.begin) / kt;
     return {it.begin + f * kt, (it.end - it.begin + kt - 1) / kt - f};
@@ -531,201 +579,247 @@ __global__ void __launch_bounds__(kThreads, 1)
     k_attention_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_do,
                      const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const BackArgs g) {
     using B = Back<HALVES>;
-    constexpr int kS = B::kSlots;
+    using At = Slot<B::kSlots>;
+    using Set = Slot<B::kSets>;
+    using Stat = Slot<B::kStats>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ KeysShared sh;
+    __shared__ WorkList list;
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* const smem = smem_raw + (base - smem_u32(smem_raw));
-    const uint32_t at_k = base, at_v = base + B::kTile, at_q = base + 2 * B::kTile, at_do = at_q + kS * B::kTile;
-    float* const stats = reinterpret_cast<float*>(smem + (2 + 2 * kS) * B::kTile);  // [stage][2][128]
-    const uint32_t kv_full = smem_u32(&sh.kv_full), kv_free = smem_u32(&sh.kv_free), q_full = smem_u32(sh.q_full), q_empty = smem_u32(sh.q_empty),
-                   do_full = smem_u32(sh.do_full), do_empty = smem_u32(sh.do_empty), st_full = smem_u32(sh.st_full), st_empty = smem_u32(sh.st_empty),
-                   s_full = smem_u32(&sh.s_full), p_full = smem_u32(&sh.p_full), dp_full = smem_u32(&sh.dp_full), ds_full = smem_u32(&sh.ds_full),
-                   acc_full = smem_u32(&sh.acc_full);
+    constexpr int kRing = 2 * B::kSets;  // tiles before the rings: keys and values of each set
+    const uint32_t at_q = base + kRing * B::kTile, at_do = at_q + B::kSlots * B::kTile;
+    float* const stats = reinterpret_cast<float*>(smem + (kRing + 2 * B::kSlots) * B::kTile);  // [stage][2][128]
+    const uint32_t kv_full = smem_u32(sh.kv_full), kv_free = smem_u32(sh.kv_free), q_full = smem_u32(sh.q_full), q_raw = smem_u32(sh.q_raw),
+                   q_empty = smem_u32(sh.q_empty), do_full = smem_u32(sh.do_full), do_raw = smem_u32(sh.do_raw), do_empty = smem_u32(sh.do_empty),
+                   st_full = smem_u32(sh.st_full), st_empty = smem_u32(sh.st_empty), s_full = smem_u32(&sh.s_full), p_full = smem_u32(&sh.p_full),
+                   dp_full = smem_u32(&sh.dp_full), ds_full = smem_u32(&sh.ds_full), acc_full = smem_u32(sh.acc_full), acc_free = smem_u32(sh.acc_free);
     const int qrows = g.group * g.kt;
     if (threadIdx.x == 0) {
         tma_prefetch(&map_q), tma_prefetch(&map_do), tma_prefetch(&map_k), tma_prefetch(&map_v);
-        bar_init(kv_full, 1), bar_init(kv_free, 1), bar_init(s_full, 1), bar_init(p_full, 8), bar_init(dp_full, 1), bar_init(ds_full, 8), bar_init(acc_full, 1);
-        for (int i = 0; i < 4; ++i) bar_init(q_full + 8 * i, 1), bar_init(q_empty + 8 * i, 1), bar_init(do_full + 8 * i, 1), bar_init(do_empty + 8 * i, 1);
-        for (int i = 0; i < 2; ++i) bar_init(st_full + 8 * i, 32), bar_init(st_empty + 8 * i, 8);
+        bar_init(s_full, 1), bar_init(p_full, 8), bar_init(dp_full, 1), bar_init(ds_full, 8);
+        for (int i = 0; i < 4; ++i) {
+            bar_init(q_full + 8 * i, 1), bar_init(q_raw + 8 * i, 1), bar_init(q_empty + 8 * i, 1);
+            bar_init(do_full + 8 * i, 1), bar_init(do_raw + 8 * i, 1), bar_init(do_empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(kv_full + 8 * i, 1), bar_init(kv_free + 8 * i, 1), bar_init(st_full + 8 * i, 32), bar_init(st_empty + 8 * i, 8);
+            bar_init(acc_full + 8 * i, 1), bar_init(acc_free + 8 * i, 8);
+        }
         bar_init_done();
     }
     // rows that no load fills, where the heads of a group do not divide 128: zeros
-    for (int s = 0; s < 2 * kS && qrows < kRows; ++s)
+    for (int s = 0; s < 2 * B::kSlots && qrows < kRows; ++s)
         for (int i = qrows * 8 + threadIdx.x; i < kRows * 8; i += kThreads)
             for (int x = 0; x < HALVES; ++x)
-                *reinterpret_cast<uint4*>(smem + (2 + s) * B::kTile + x * kHalfTile + i * 16) = make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4*>(smem + (kRing + s) * B::kTile + x * kHalfTile + i * 16) = make_uint4(0, 0, 0, 0);
     asm volatile("fence.proxy.async;" ::: "memory");
     if (warp == 9) tmem_alloc<1>(smem_u32(&sh.tmem), 512);
+    wait_for_predecessor();
+    let_successor_start();
+    list_work(list, g.items, g.head, g.kv);
     mma_fence_before();
     __syncthreads();
     mma_fence_after();
     const uint32_t tmem = sh.tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 384;
-    wait_for_predecessor();
-    let_successor_start();
-    const int64_t total = (int64_t)g.head->count * g.kv;
+    Walk walk(list, g.items, g.kv);
     bool ok = true;
 
+    if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (warp == 8) {
         // load
-        int slot = 0;
-        uint32_t ph = 0, kvph = 0;
+        uint32_t n = 0, items = 0;
         const uint32_t qbytes = HALVES * qrows * 128;
-        for (int turn = 0; ok; ++turn) {
-            const int64_t w = work_at(turn);
-            if ((int64_t)turn * gridDim.x >= total) break;
-            if (w >= total) continue;
-            const Item it = g.items[w / g.kv];
-            const int h = (int)(w % g.kv);
+        while (ok && walk.next()) {
+            const Work it = walk.it;
             const QuerySpan q = query_span(it, g.kt);
             if (!q.tiles) continue;
-            if (!(ok = warp_wait(kv_free, kvph ^ 1))) break;
-            kvph ^= 1;
+            const Set set(items++);
+            if (!(ok = warp_wait(kv_free + 8 * set.at, set.parity ^ 1))) break;
             if (elect_one()) {
-                bar_expect(kv_full, 2 * B::kTile);
+                const uint32_t to = base + 2 * set.at * B::kTile, bar = kv_full + 8 * set.at;
+                bar_expect(bar, 2 * B::kTile);
                 for (int x = 0; x < HALVES; ++x) {
-                    tma_load<1>(at_k + x * kHalfTile, &map_k, 64 * x, h, it.first, kv_full);
-                    tma_load<1>(at_v + x * kHalfTile, &map_v, 64 * x, h, it.first, kv_full);
+                    tma_load<1>(to + x * kHalfTile, &map_k, 64 * x, walk.it.h, it.first, bar);
+                    tma_load<1>(to + B::kTile + x * kHalfTile, &map_v, 64 * x, walk.it.h, it.first, bar);
                 }
             }
             __syncwarp();
-            for (int i = 0; ok && i < q.tiles; ++i) {
-                for (int kind = 0; ok && kind < 2; ++kind) {
-                    const uint32_t full = (kind ? do_full : q_full) + 8 * slot, to = (kind ? at_do : at_q) + slot * B::kTile;
-                    if (!(ok = warp_wait((kind ? do_empty : q_empty) + 8 * slot, ph ^ 1))) break;
+            for (int i = 0; ok && i < q.tiles; ++i, ++n) {
+                const At slot(n);
+                const int first = q.first + i * g.kt;
+                const bool partial = it.end - first < g.kt;  // that tile is cleared first
+                for (int kind = 0; kind < 2; ++kind) {
+                    const uint32_t full = (kind ? partial ? do_raw : do_full : partial ? q_raw : q_full) + 8 * slot.at;
+                    const uint32_t to = (kind ? at_do : at_q) + slot.at * B::kTile;
+                    if (!(ok = warp_wait((kind ? do_empty : q_empty) + 8 * slot.at, slot.parity ^ 1))) break;
                     if (elect_one()) {
                         bar_expect(full, qbytes);
                         for (int x = 0; x < HALVES; ++x)
-                            tma_load<1>(to + x * kHalfTile, kind ? &map_do : &map_q, 64 * x, h * g.group, q.first + i * g.kt, full);
+                            tma_load<1>(to + x * kHalfTile, kind ? &map_do : &map_q, 64 * x, walk.it.h * g.group, first, full);
                     }
                     __syncwarp();
                 }
-                if (++slot == kS) slot = 0, ph ^= 1;
             }
         }
+    } else if (warp == 11) {
+        // clear what lies behind a sequence in its last queries
+        uint32_t n = 0, parities = 0;
+        while (ok && walk.next()) {
+            const Work it = walk.it;
+            const QuerySpan q = query_span(it, g.kt);
+            n += q.tiles;
+            const int rest = it.end - q.first - (q.tiles - 1) * g.kt;
+            if (!q.tiles || rest >= g.kt) continue;
+            const At slot(n - 1);
+            for (int kind = 0; kind < 2; ++kind) {
+                if (!(ok = warp_wait((kind ? do_raw : q_raw) + 8 * slot.at, parities >> slot.at & 1))) break;
+                clear_rows<HALVES>(smem + (kRing + (kind ? B::kSlots : 0) + slot.at) * B::kTile, rest * g.group, lane);
+                if (lane == 0) bar_arrive((kind ? do_full : q_full) + 8 * slot.at);
+            }
+            parities ^= 1u << slot.at;
+        }
     } else if (warp == 9) {
-        // multiply
+        // multiply: each product with the queries or dout, and behind it the next tile's scores or dp in the place of what it used
         const uint32_t id_s = attend_desc(true, false, kRows), id_dp = attend_desc(F16, false, kRows), id_dk = attend_desc(true, true, 64 * HALVES),
                        id_dv = attend_desc(F16, true, 64 * HALVES);
         const int steps = (g.dim + 15) / 16;
-        int slot = 0;
-        uint32_t ph = 0, kvph = 0, pph = 0, dsph = 0;
-        for (int turn = 0; ok; ++turn) {
-            const int64_t w = work_at(turn);
-            if ((int64_t)turn * gridDim.x >= total) break;
-            if (w >= total) continue;
-            const Item it = g.items[w / g.kv];
-            const QuerySpan q = query_span(it, g.kt);
-            if (!q.tiles) continue;
-            if (!(ok = warp_wait(kv_full, kvph))) break;
-            kvph ^= 1;
-            // scores or dp of the tile i, in the slot s
-            auto rows = [&](int i, int s, uint32_t parity, bool dp) {
-                if (!warp_wait((dp ? do_full : q_full) + 8 * s, parity)) return false;
-                const int rest = (it.end - q.first - i * g.kt) * g.group;
-                if (rest < qrows) clear_rows<HALVES>(smem + (2 + (dp ? kS : 0) + s) * B::kTile, rest, lane);
-                mma_fence_after();
-                if (elect_one()) {
-                    product_rows(dp ? t_dp : tmem, dp ? at_v : at_k, (dp ? at_do : at_q) + s * B::kTile, dp ? id_dp : id_s, steps);
-                    mma_commit<1>(dp ? dp_full : s_full);
-                }
-                __syncwarp();
+        uint32_t t = 0, items = 0;  // the present tile, counted through all items; items begun
+        int i = 0, tiles = 0;
+        auto step = [&]() {
+            if (++i < tiles) return true;
+            while (walk.next()) {
+                tiles = query_span(walk.it, g.kt).tiles;
+                if (!tiles) continue;
+                i = 0;
+                ++items;
                 return true;
-            };
-            if (!(ok = rows(0, slot, ph, false) && rows(0, slot, ph, true))) break;
-            for (int i = 0; ok && i < q.tiles; ++i) {
-                const int s = slot;
-                if (++slot == kS) slot = 0, ph ^= 1;
-                if (!(ok = warp_wait(p_full, pph))) break;
-                pph ^= 1;
-                mma_fence_after();
-                if (elect_one()) {
-                    product_tmem(t_dv, tmem, tmem + 64, at_do + s * B::kTile, id_dv, i != 0);
-                    mma_commit<1>(do_empty + 8 * s);
-                }
-                __syncwarp();
-                if (i + 1 < q.tiles && !(ok = rows(i + 1, slot, ph, false))) break;
-                if (!(ok = warp_wait(ds_full, dsph))) break;
-                dsph ^= 1;
-                mma_fence_after();
-                if (elect_one()) {
-                    product_tmem(t_dk, t_dp, t_dp + 64, at_q + s * B::kTile, id_dk, i != 0);
-                    if (F16 && q.tiles <= kFineTiles) product_tmem(t_dk, t_dp + 32, t_dp + 96, at_q + s * B::kTile, id_dk, true);
-                    mma_commit<1>(q_empty + 8 * s);
-                }
-                __syncwarp();
-                if (i + 1 < q.tiles && !(ok = rows(i + 1, slot, ph, true))) break;
             }
-            if (!ok) break;
-            if (elect_one()) mma_commit<1>(acc_full), mma_commit<1>(kv_free);
+            return false;
+        };
+        // scores or dp of tile n, the i-th of its item
+        auto rows = [&](uint32_t n, bool dp) {
+            const At slot(n);
+            const Set set(items - 1);
+            if (!dp && i == 0 && !warp_wait(kv_full + 8 * set.at, set.parity)) return false;
+            if (!warp_wait((dp ? do_full : q_full) + 8 * slot.at, slot.parity)) return false;
+            mma_fence_after();
+            if (elect_one()) {
+                product_rows<HALVES>(dp ? t_dp : tmem, base + (2 * set.at + dp) * B::kTile, (dp ? at_do : at_q) + slot.at * B::kTile, dp ? id_dp : id_s, steps);
+                mma_commit<1>(dp ? dp_full : s_full);
+                if (dp && i + 1 == tiles) mma_commit<1>(kv_free + 8 * set.at);
+            }
             __syncwarp();
+            return true;
+        };
+        bool any = step();
+        if (any) ok = rows(0, false) && rows(0, true);
+        while (ok && any) {
+            const At slot(t);
+            const Set set(items - 1);
+            const bool first = i == 0, last = i + 1 == tiles, fine = F16 && tiles <= kFineTiles;
+            if (!(ok = warp_wait(p_full, t & 1))) break;
+            if (first && !(ok = warp_wait(acc_free + 8 * set.at, set.parity ^ 1))) break;
+            mma_fence_after();
+            if (elect_one()) {
+                product_tmem(t_dv + 64 * set.at, tmem, tmem + 64, at_do + slot.at * B::kTile, id_dv, !first);
+                mma_commit<1>(do_empty + 8 * slot.at);
+            }
+            __syncwarp();
+            any = step();
+            if (any && !(ok = rows(t + 1, false))) break;
+            if (!(ok = warp_wait(ds_full, t & 1))) break;
+            mma_fence_after();
+            if (elect_one()) {
+                const uint32_t acc = t_dk + 64 * set.at, b = at_q + slot.at * B::kTile;
+                product_tmem(acc, t_dp, t_dp + 64, b, id_dk, !first);
+                if (fine) product_tmem(acc, t_dp + 32, t_dp + 96, b, id_dk, true);
+                mma_commit<1>(q_empty + 8 * slot.at);
+                if (last) mma_commit<1>(acc_full + 8 * set.at);
+            }
+            __syncwarp();
+            if (any && !(ok = rows(t + 1, true))) break;
+            ++t;
         }
     } else if (warp == 10) {
         // statistics of the rows of queries: what the exponent subtracts, and delta
-        int stage = 0;
-        uint32_t ph = 0;
-        for (int turn = 0; ok; ++turn) {
-            const int64_t w = work_at(turn);
-            if ((int64_t)turn * gridDim.x >= total) break;
-            if (w >= total) continue;
-            const Item it = g.items[w / g.kv];
-            const int h = (int)(w % g.kv);
+        uint32_t n = 0;
+        while (ok && walk.next()) {
+            const Work it = walk.it;
             const QuerySpan q = query_span(it, g.kt);
             if (!q.tiles) continue;
-            const float sigma = ldexpf(1.f, powers_of<F16>(g, h).sigma - (F16 ? kLift : 0));
-            for (int i = 0; i < q.tiles; ++i) {
+            const float sigma = ldexpf(1.f, powers_of<F16>(g, walk.it.h).sigma - (F16 ? kLift : 0));
+            for (int i = 0; i < q.tiles; ++i, ++n) {
+                const Stat stage(n);
                 float l[4], d[4];
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    const int row = 32 * x + lane, token = q.first + i * g.kt + row / g.group, head = h * g.group + row % g.group;
+                    const int row = 32 * x + lane, token = q.first + i * g.kt + row / g.group, head = walk.it.h * g.group + row % g.group;
                     const bool live = row < qrows && token < it.end;
                     const int64_t at = (int64_t)token * g.heads + head;
                     l[x] = live ? (F16 ? kLift : 0) - g.lse[at] * kLog2e : -INFINITY;
                     d[x] = live ? -g.delta[at] * sigma : 0.f;
                 }
-                if (!(ok = warp_wait(st_empty + 8 * stage, ph ^ 1))) break;
-                float* const to = stats + stage * 2 * kRows;
+                if (!(ok = warp_wait(st_empty + 8 * stage.at, stage.parity ^ 1))) break;
+                float* const to = stats + stage.at * 2 * kRows;
 #pragma unroll
                 for (int x = 0; x < 4; ++x) to[32 * x + lane] = l[x], to[kRows + 32 * x + lane] = d[x];
-                bar_arrive(st_full + 8 * stage);
-                if (++stage == B::kStats) stage = 0, ph ^= 1;
+                bar_arrive(st_full + 8 * stage.at);
             }
         }
-    } else if (warp < 8) {
+    }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         const int half = warp / 4, row = threadIdx.x % 128;
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;
-        int stage = 0;
-        uint32_t stph = 0, ph = 0, aph = 0;
-        for (int turn = 0; ok; ++turn) {
-            const int64_t w = work_at(turn);
-            if ((int64_t)turn * gridDim.x >= total) break;
-            if (w >= total) continue;
-            const Item it = g.items[w / g.kv];
-            const int h = (int)(w % g.kv);
+        uint32_t t = 0, items = 0;
+        uint8_t* const stage = B::kStage ? smem + (kRing + 2 * B::kSlots) * B::kTile + B::kStats * 2 * kRows * 4 + warp * kStageBytesOfWarp : nullptr;
+        // the item whose sums are still to be written: one half of the warps has dv, the other dk
+        RowsOut out = {};
+        float factor = 0.f;
+        bool pending = false;
+        const bool wide = half ? g.dk.wide : g.dv.wide;
+        auto write = [&](uint32_t item) {
+            const Set set(item);
+            if (!warp_wait(acc_full + 8 * set.at, set.parity)) return false;
+            mma_fence_after();
+#pragma unroll 1
+            for (int x = 0; x < 2 * HALVES; ++x) {
+                if (32 * x >= g.dim) break;
+                uint32_t a[32];
+                tmem_fetch((half ? t_dk : t_dv) + 64 * set.at + 32 * x + lanes, a);
+                tmem_wait(a);
+                out.write<F16>(32 * x, g.dim, wide, a, factor, stage);
+            }
+            mma_fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(acc_free + 8 * set.at);
+            return true;
+        };
+        while (ok && walk.next()) {
+            const Work it = walk.it;
+            const int h = walk.it.h;
             const QuerySpan q = query_span(it, g.kt);
             const int token = it.first + row;
-            const bool live = token < it.end;
             const HeadsOut& o = half ? g.dk : g.dv;
-            uint16_t* const out = o.p + (int64_t)token * o.token + h * o.head;
+            uint16_t* const own = token < it.end ? o.p + (int64_t)token * o.token + h * o.head : nullptr;
             if (it.begin < 0) {
-                if (live) {
-                    float zero[32];
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) zero[i] = 0.f;
-                    for (int x = 0; x < 2 * HALVES; ++x) write_columns<F16>(out, 32 * x, g.dim, o.wide, zero);
-                }
+                write_zeros(own, g.dim);
                 continue;
             }
             const Powers pw = powers_of<F16>(g, h);
             const Pair c2 = both(ldexpf(g.scale * kLog2e, -pw.q - pw.k)), s2 = both(ldexpf(1.f, pw.sigma - (F16 ? kLift : 0)));
-            for (int i = 0; i < q.tiles; ++i) {
+            const bool fine = F16 && q.tiles <= kFineTiles;
+            for (int i = 0; i < q.tiles; ++i, ++t) {
+                const Stat step(t);
                 const int first = q.first + i * g.kt;  // token of the tile's first row
                 const bool masked = first < it.first + kRows - 1;
                 const int from = (token - first) * g.group - 64 * half;  // the first column of this half that sees this key
-                const float* const st = stats + stage * 2 * kRows + 64 * half;
-                if (!(ok = warp_wait(st_full + 8 * stage, stph))) break;
-                if (!(ok = warp_wait(s_full, ph))) break;
+                const float* const st = stats + step.at * 2 * kRows + 64 * half;
+                if (!(ok = warp_wait(st_full + 8 * step.at, step.parity))) break;
+                if (!(ok = warp_wait(s_full, t & 1))) break;
                 mma_fence_after();
                 uint32_t s[2][32], dp[2][32], e[32], rest[32];
                 tmem_fetch(tmem + 64 * half + lanes, s[0]), tmem_fetch(tmem + 64 * half + 32 + lanes, s[1]);
@@ -751,7 +845,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 mma_fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(p_full);
-                if (!(ok = warp_wait(dp_full, ph))) break;
+                if (!(ok = warp_wait(dp_full, t & 1))) break;
                 mma_fence_after();
                 tmem_fetch(t_dp + 64 * half + lanes, dp[0]), tmem_fetch(t_dp + 64 * half + 32 + lanes, dp[1]);
                 tmem_wait(dp[0]), tmem_wait(dp[1]);
@@ -770,7 +864,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             for (int y = 0; y < 4; ++y) v[y] = 32 * x + j + y < from ? 0.f : v[y];
                         }
                         e[16 * x + j / 2] = pack16<true>(v[0], v[1]), e[16 * x + j / 2 + 1] = pack16<true>(v[2], v[3]);
-                        if (F16 && q.tiles <= kFineTiles) {
+                        if (fine) {
                             const float2 a16 = __half22float2(*reinterpret_cast<const __half2*>(&e[16 * x + j / 2]));
                             const float2 b16 = __half22float2(*reinterpret_cast<const __half2*>(&e[16 * x + j / 2 + 1]));
                             rest[16 * x + j / 2] = pack16<true>(v[0] - a16.x, v[1] - a16.y);
@@ -778,30 +872,23 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                     }
                 tmem_store(t_dp + 64 * half + lanes, e);
-                if (F16 && q.tiles <= kFineTiles) tmem_store(t_dp + 64 * half + 32 + lanes, rest);
+                if (fine) tmem_store(t_dp + 64 * half + 32 + lanes, rest);
                 tmem_store_wait();
                 mma_fence_before();
                 __syncwarp();
-                if (lane == 0) bar_arrive(ds_full), bar_arrive(st_empty + 8 * stage);
-                ph ^= 1;
-                if (++stage == B::kStats) stage = 0, stph ^= 1;
+                if (lane == 0) bar_arrive(ds_full), bar_arrive(st_empty + 8 * step.at);
+                if (i == 0 && pending) {
+                    pending = false;
+                    if (!(ok = write(items - 1))) break;
+                }
             }
             if (!ok) break;
-            if (!(ok = warp_wait(acc_full, aph))) break;
-            aph ^= 1;
-            mma_fence_after();
-            const float f = half ? ldexpf(g.scale, -pw.sigma - pw.q) : ldexpf(1.f, F16 ? -kLift : 0);
-            for (int x = 0; x < 2 * HALVES; ++x) {
-                uint32_t a[32];
-                tmem_fetch((half ? t_dk : t_dv) + 32 * x + lanes, a);
-                tmem_wait(a);
-                float v[32];
-#pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(a[i]) * f;
-                if (live && 32 * x < g.dim) write_columns<F16>(out, 32 * x, g.dim, o.wide, v);
-            }
-            mma_fence_before();
+            out.set(own);
+            factor = half ? ldexpf(g.scale, -pw.sigma - pw.q) : ldexpf(1.f, F16 ? -kLift : 0);
+            pending = true;
+            ++items;
         }
+        if (ok && pending) ok = write(items - 1);
     }
     if (!ok) let_copies_end();
     __syncwarp();
@@ -911,6 +998,7 @@ int ones_attention_backward(const ones_heads* dout, const ones_heads* q, const o
     if (!d_lse || !d_workspace) return ONES_ERR_NULL;
     if (!aligned(d_lse, 4) || !aligned(d_workspace, 256)) return ONES_ERR_ALIGN;
     const BackPlan p = back_plan(tokens, sequences, q->heads, k->heads, dim);
+    if (p.most[0] * k->heads >= 1ll << 31) return ONES_ERR_BAD_PARAM;
     if (workspace_bytes < p.bytes) return ONES_ERR_WORKSPACE;
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
     uint8_t* const ws = static_cast<uint8_t*>(d_workspace);
@@ -923,17 +1011,17 @@ int ones_attention_backward(const ones_heads* dout, const ones_heads* q, const o
     unsigned* const largest = reinterpret_cast<unsigned*>(ws + p.at_largest);
     plan.zero = largest, plan.zeros = 4 * k->heads;
     float* const delta = reinterpret_cast<float*>(ws + p.at_delta);
-    const HeadsOut o = heads_out(*out, tokens);
+    const HeadsOut o = heads_out(*out, dim, tokens);
     const ones_heads* const five[5] = {dout, v, q, k, out};
     SurveyArgs d = {};
     for (int i = 0; i < 5; ++i) d.p[i] = static_cast<const uint16_t*>(five[i]->d_data), d.token[i] = five[i]->token, d.head[i] = five[i]->head;
     d.plan = plan.head, d.delta = delta, d.largest = largest, d.tokens = tokens, d.heads = q->heads, d.kv = k->heads, d.dim = dim;
-    d.wide = o.wide && dim % 8 == 0;
+    d.wide = o.wide;
     NarrowArgs n = {};
     for (int i = 0; i < 2; ++i)
         n.p[i] = d.p[2 + i], n.token[i] = d.token[2 + i], n.head[i] = d.head[2 + i], n.out[i] = reinterpret_cast<uint16_t*>(ws + p.at_narrow[i]);
     n.plan = plan.head, n.largest = largest, n.heads = q->heads, n.kv = k->heads, n.dim = dim, n.row = p.row;
-    const BackArgs a = {nullptr, nullptr, d_lse, delta, largest, heads_out(*dq, tokens), heads_out(*dk, tokens), heads_out(*dv, tokens), tokens,
+    const BackArgs a = {nullptr, nullptr, d_lse, delta, largest, heads_out(*dq, dim, tokens), heads_out(*dk, dim, tokens), heads_out(*dv, dim, tokens), tokens,
                         q->heads, k->heads, p.group, p.kt, dim, scale};
     const bool f16 = type == ONES_F16;
     cudaError_t err;
