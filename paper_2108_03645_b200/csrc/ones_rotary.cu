@@ -1,12 +1,16 @@
 // Norms of queries and keys with the rotation of their positions, and their gradients.
 //
-// Bound by bytes: a vector is read once and written once (backward: x and dy read, dx written). A block takes a few tokens:
-// their sines and cosines are formed once, in 64 bits up to the reduced angle, and serve all heads from shared memory; then
-// groups of lanes take one vector each. A lane holds two pieces that turn into each other (value i and i + rotary / 2, or
-// neighbours), so that the rotation needs no exchange between lanes, and the norm is one butterfly over the group.
+// Bound by bytes: a vector is read once and written once (backward: x and dy read, dx written). A block takes a few tokens at a
+// time. Their sines and cosines are formed once, in 64 bits up to the reduced angle, and serve all heads from shared memory.
+// Groups of lanes take one vector each, neighbours neighbouring ones: where each group kept to a token of its own, the memory was
+// read in pieces of 256 bytes from ten thousand places at once (65536 x 40 x 128: 380 us for the forward pass). A lane holds two
+// pieces that turn into each other (value i and i + rotary / 2, or neighbours), so that the rotation needs no exchange between
+// lanes, and the norm is one butterfly over the group. Arithmetic is on pairs.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
+
+#include <type_traits>
 
 #include "ones_attention.h"
 #include "ones_mma.cuh"
@@ -17,7 +21,7 @@ namespace ones {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxBlocks = 148 * 4;  // partial sums of the weights' gradients: one row for each block
+constexpr int kMaxBlocks = 148 * 2;  // partial sums of the weights' gradients: one row for each block
 
 __device__ __forceinline__ float to_f(float v) { return v; }
 __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
@@ -31,11 +35,6 @@ __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return
 template <>
 __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
 
-template <class T, int V>
-struct alignas(sizeof(T) * V) Pack {
-    T v[V];
-};
-
 struct Side {  // queries or keys
     const void *x, *dy, *weight;
     void *out, *dweight;
@@ -47,204 +46,289 @@ struct Args {
     const int64_t* positions;
     const double* frequencies;
     float* part;  // [blocks][2][dim]
-    int tokens, dim, rotary, interleaved, wf32, tile;  // tile: tokens of a block at a time
-    int group_log;                                     // lanes of a vector
-    float eps;
+    int tokens, dim, rotary, interleaved, wf32;
+    int group_log;     // lanes of a vector
+    int tile, angles;  // tokens of a block at a time; room for a token's angles
+    float eps, per_dim;
 };
 
-// The two pieces of unit u: where they start, and how they turn. kind 0: not at all, 1: into each other, 2: neighbours within
-// each. Either may start past the vector's end, when it is not there.
+// The two pieces of unit u: where they start, and whether they turn (into each other, or with INTER and several values, as
+// neighbours within each). Either may start past the vector's end, when it is not there.
 struct Unit {
-    int a, b, kind, angle;  // angle: index of the first angle (kind 1), of piece a's first and, V / 2 further, of piece b's (kind 2)
+    int a, b, turns, angle;  // angle: the first of the V angles that turn the pieces
 };
-template <int V>
+template <int V, bool INTER>
 __device__ __forceinline__ Unit unit_at(const Args& g, int u) {
     const int half = g.rotary / 2;
-    if (V == 1 && g.interleaved) {
-        const bool in = 2 * u < g.rotary;
-        return {2 * u, 2 * u + 1, in ? 1 : 0, u};
-    }
-    if (g.interleaved) return {2 * V * u, 2 * V * u + V, 2 * V * u < g.rotary ? 2 : 0, u * V};
+    if (INTER) return {2 * V * u, 2 * V * u + V, 2 * V * u < g.rotary, u * V};
     if (u * V < half) return {u * V, u * V + half, 1, u * V};
     const int at = g.rotary + 2 * (u * V - half);
     return {at, at + V, 0, 0};
 }
 
-template <int V>
-__device__ __forceinline__ void turn(const Unit& w, float (&x)[2 * V], const float* cs, const float* sn, float sign) {
-    if (w.kind == 1) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float c = cs[w.angle + i], s = sign * sn[w.angle + i], a = x[i], b = x[V + i];
-            x[i] = a * c - b * s, x[V + i] = b * c + a * s;
+// 2 V values of a lane as V pairs: of its first piece, then of its second one (V = 1: both in one pair).
+template <class T, int V>
+struct Row {
+    static constexpr int kWords = V * sizeof(T) / 4 > 0 ? V * sizeof(T) / 4 : 1;
+    uint32_t a[kWords] = {}, b[kWords] = {};  // as they lie in memory; zeros where the vector has none
+    __device__ __forceinline__ void load(const T* p, const Unit& w, int dim) {
+        if constexpr (V == 1) {
+            if (w.a < dim) a[0] = word(p[w.a]);
+            if (w.b < dim) b[0] = word(p[w.b]);
+        } else {
+            if (w.a < dim) {
+                const uint4 q = *reinterpret_cast<const uint4*>(p + w.a);
+                a[0] = q.x, a[1] = q.y, a[2] = q.z, a[3] = q.w;
+            }
+            if (w.b < dim) {
+                const uint4 q = *reinterpret_cast<const uint4*>(p + w.b);
+                b[0] = q.x, b[1] = q.y, b[2] = q.z, b[3] = q.w;
+            }
         }
-    } else if (V > 1 && w.kind == 2) {
+    }
+    static __device__ __forceinline__ uint32_t word(float v) { return __float_as_uint(v); }
+    static __device__ __forceinline__ uint32_t word(__nv_bfloat16 v) { return __bfloat16_as_ushort(v); }
+    static __device__ __forceinline__ uint32_t word(__half v) { return __half_as_ushort(v); }
+    static __device__ __forceinline__ Pair pair_of(uint32_t w) {
+        if constexpr (sizeof(T) == 4) return pair(0.f, 0.f);
+        if constexpr (std::is_same<T, __half>::value) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+            return pair(f.x, f.y);
+        }
+        return pair(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+    }
+    __device__ __forceinline__ void get(Pair (&x)[V]) const {
+        if constexpr (V == 1) {
+            if constexpr (sizeof(T) == 4)
+                x[0] = pair(__uint_as_float(a[0]), __uint_as_float(b[0]));
+            else
+                x[0] = pair_of(a[0] | b[0] << 16);
+        } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float c = cs[w.angle + i], s = sign * sn[w.angle + i], a = x[2 * i], b = x[2 * i + 1];
-            x[2 * i] = a * c - b * s, x[2 * i + 1] = b * c + a * s;
+            for (int i = 0; i < 2; ++i)
+                x[i] = pair(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1])), x[2 + i] = pair(__uint_as_float(b[2 * i]), __uint_as_float(b[2 * i + 1]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = pair_of(a[i]), x[4 + i] = pair_of(b[i]);
+        }
+    }
+    static __device__ __forceinline__ uint32_t packed(Pair p) {
+        const float2 f = split(p);
+        if constexpr (std::is_same<T, __half>::value) {
+            const __half2 h = __floats2half2_rn(f.x, f.y);
+            return *reinterpret_cast<const uint32_t*>(&h);
+        }
+        const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+    static __device__ __forceinline__ void store(T* p, const Unit& w, int dim, const Pair (&x)[V]) {
+        if constexpr (V == 1) {
+            const float2 f = split(x[0]);
+            if (w.a < dim) p[w.a] = from_f<T>(f.x);
+            if (w.b < dim) p[w.b] = from_f<T>(f.y);
+        } else if constexpr (sizeof(T) == 4) {
+            const float2 f[4] = {split(x[0]), split(x[1]), split(x[2]), split(x[3])};
+            if (w.a < dim) *reinterpret_cast<float4*>(p + w.a) = make_float4(f[0].x, f[0].y, f[1].x, f[1].y);
+            if (w.b < dim) *reinterpret_cast<float4*>(p + w.b) = make_float4(f[2].x, f[2].y, f[3].x, f[3].y);
+        } else {
+            if (w.a < dim) *reinterpret_cast<uint4*>(p + w.a) = make_uint4(packed(x[0]), packed(x[1]), packed(x[2]), packed(x[3]));
+            if (w.b < dim) *reinterpret_cast<uint4*>(p + w.b) = make_uint4(packed(x[4]), packed(x[5]), packed(x[6]), packed(x[7]));
+        }
+    }
+};
+
+__device__ __forceinline__ Pair operator-(Pair a, Pair b) {
+    Pair r;
+    asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+// V / 2 pairs from shared memory
+template <int V>
+__device__ __forceinline__ void fetch_pairs(const float* p, Pair (&x)[V / 2]) {
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i) {
+        const float4 f = reinterpret_cast<const float4*>(p)[i];
+        x[2 * i] = pair(f.x, f.y), x[2 * i + 1] = pair(f.z, f.w);
+    }
+}
+// The lane's values turned by the angles whose cosines and sines start at cs, sn (BACK: by their negatives).
+template <int V, bool INTER, bool BACK>
+__device__ __forceinline__ void turn(Pair (&x)[V], const float* cs, const float* sn) {
+    if constexpr (V == 1) {
+        const float2 f = split(x[0]);
+        const float c = cs[0], s = BACK ? -sn[0] : sn[0];
+        x[0] = pair(f.x * c - f.y * s, f.y * c + f.x * s);
+    } else {
+        Pair c[V / 2], s[V / 2];
+        fetch_pairs<V>(cs, c), fetch_pairs<V>(sn, s);
+        if constexpr (INTER) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float2 f = split(x[i]), cc = split(c[i / 2]), ss = split(s[i / 2]);
+                const float u = i & 1 ? cc.y : cc.x, t = i & 1 ? (BACK ? -ss.y : ss.y) : (BACK ? -ss.x : ss.x);
+                x[i] = pair(f.x * u - f.y * t, f.y * u + f.x * t);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) {
+                const Pair a = x[i], b = x[V / 2 + i];
+                x[i] = BACK ? fma2(b, s[i], a * c[i]) : a * c[i] - b * s[i];
+                x[V / 2 + i] = BACK ? b * c[i] - a * s[i] : fma2(a, s[i], b * c[i]);
+            }
         }
     }
 }
-
-template <class T, int V>
-__device__ __forceinline__ void load(const T* p, const Unit& w, int dim, float (&x)[2 * V]) {
-    Pack<T, V> a = {}, b = {};
-    if (w.a < dim) a = *reinterpret_cast<const Pack<T, V>*>(p + w.a);
-    if (w.b < dim) b = *reinterpret_cast<const Pack<T, V>*>(p + w.b);
+// The weights of the lane's values, from a vector in shared memory that goes on with zeros behind dim.
+template <int V>
+__device__ __forceinline__ void weights(const float* w, const Unit& u, Pair (&x)[V]) {
+    if constexpr (V == 1) {
+        x[0] = pair(w[u.a], w[u.b]);
+    } else {
+        Pair a[V / 2], b[V / 2];
+        fetch_pairs<V>(w + u.a, a), fetch_pairs<V>(w + u.b, b);
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = w.a < dim ? to_f(a.v[i]) : 0.f, x[V + i] = w.b < dim ? to_f(b.v[i]) : 0.f;
-}
-template <class T, int V>
-__device__ __forceinline__ void store(T* p, const Unit& w, int dim, const float (&x)[2 * V]) {
-    Pack<T, V> a, b;
-#pragma unroll
-    for (int i = 0; i < V; ++i) a.v[i] = from_f<T>(x[i]), b.v[i] = from_f<T>(x[V + i]);
-    if (w.a < dim) *reinterpret_cast<Pack<T, V>*>(p + w.a) = a;
-    if (w.b < dim) *reinterpret_cast<Pack<T, V>*>(p + w.b) = b;
-}
-template <class T, int V>
-__device__ __forceinline__ void load_weight(const void* p, bool f32, const Unit& w, int dim, float (&x)[2 * V]) {
-#pragma unroll
-    for (int i = 0; i < 2 * V; ++i) {
-        const int c = i < V ? w.a + i : w.b + i - V;
-        x[i] = c >= dim ? 0.f : !p ? 1.f : f32 ? static_cast<const float*>(p)[c] : to_f(static_cast<const T*>(p)[c]);
+        for (int i = 0; i < V / 2; ++i) x[i] = a[i], x[V / 2 + i] = b[i];
     }
 }
 
 __device__ __forceinline__ float group_sum(float v, int lanes) {
-    for (int m = lanes / 2; m; m >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, m);
+#pragma unroll
+    for (int m = 16; m; m >>= 1)
+        if (m < lanes) v += __shfl_xor_sync(0xFFFFFFFFu, v, m);
     return v;
 }
-
-// Cosines and sines of `n` tokens from t0 on, [n][rotary / 2] each.
-__device__ __forceinline__ void form_angles(const Args& g, int t0, int n, float* cs, float* sn) {
-    const int half = g.rotary / 2;
-    for (int i = threadIdx.x; i < n * half; i += kThreads) {
-        const int t = i / half, f = i - t * half;
-        double turns = (double)g.positions[t0 + t] * g.frequencies[f] * 0.15915494309189533577;  // 1 / (2 pi)
-        turns -= rint(turns);
-        float s, c;
-        sincospif((float)(2.0 * turns), &s, &c);
-        cs[i] = c, sn[i] = s;
-    }
+__device__ __forceinline__ float inverse_root(float ss, const Args& g) {
+    const float v = fmaf(ss, g.per_dim, g.eps), r = rsqrtf(v);
+    return r * fmaf(-0.5f * v * r, r, 1.5f);  // a Newton step: to the last place or two
 }
 
-// U units per lane: 1 where 16-byte pieces are possible, more for single values.
-template <class T, int V, int U>
-__global__ void __launch_bounds__(kThreads) k_qk_norm(const __grid_constant__ Args g) {
+constexpr int kWeightRow = ONES_QK_NORM_MAX_DIM + 16;
+
+// U units per lane: 1 where pieces of 16 bytes are possible, more for single values. The next vector of a group is on its way
+// while the present one is worked on; four blocks (backward: two) on an SM hide the rest.
+template <class T, int V, int U, bool INTER, bool BACK>
+__global__ void __launch_bounds__(kThreads, BACK ? 2 : 4) k_qk_norm(const __grid_constant__ Args g) {
     extern __shared__ float smem[];
-    const int half = g.rotary / 2, lanes = 1 << g.group_log, groups = kThreads >> g.group_log;
+    __shared__ __align__(16) float s_weight[2][kWeightRow];
+    const int lanes = 1 << g.group_log, groups = kThreads >> g.group_log;
     const int lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> g.group_log;
-    float *cs = smem, *sn = smem + g.tile * half;
+    float *cs = smem, *sn = smem + g.tile * g.angles;
     Unit unit[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) unit[u] = unit_at<V>(g, lane + u * lanes);
+    for (int u = 0; u < U; ++u) unit[u] = unit_at<V, INTER>(g, lane + u * lanes);
     const int tiles = (g.tokens + g.tile - 1) / g.tile;
+    for (int i = threadIdx.x; i < 2 * kWeightRow; i += kThreads) {
+        const int which = i >= kWeightRow, c = i - which * kWeightRow;
+        const void* p = g.side[which].weight;
+        s_weight[which][c] = c >= g.dim ? 0.f : !p ? 1.f : g.wf32 ? static_cast<const float*>(p)[c] : to_f(static_cast<const T*>(p)[c]);
+    }
+    Pair dw[BACK ? 2 : 1][U][V];
+    if (BACK) {
+#pragma unroll
+        for (int which = 0; which < (BACK ? 2 : 1); ++which)
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < V; ++i) dw[which][u][i] = both(0.f);
+    }
     for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int t0 = tile * g.tile, n = min(g.tile, g.tokens - t0);
+        const int t0 = tile * g.tile, n = min(g.tile, g.tokens - t0), half = g.rotary / 2;
         __syncthreads();
-        form_angles(g, t0, n, cs, sn);
+        for (int i = threadIdx.x; i < n * g.angles; i += kThreads) {
+            const int t = i / g.angles, f = i - t * g.angles;
+            if (f >= half) continue;
+            double turns = (double)g.positions[t0 + t] * g.frequencies[f] * 0.15915494309189533577;  // 1 / (2 pi)
+            turns -= rint(turns);
+            sincospif((float)(2.0 * turns), &sn[i], &cs[i]);
+        }
         __syncthreads();
+#pragma unroll
         for (int which = 0; which < 2; ++which) {
             const Side& side = g.side[which];
-            if (!side.heads) continue;
-            float w[U][2 * V];
-#pragma unroll
-            for (int u = 0; u < U; ++u) load_weight<T, V>(side.weight, g.wf32, unit[u], g.dim, w[u]);
             const int rows = n * side.heads;
+            const T* const px = static_cast<const T*>(side.x) + (int64_t)t0 * side.x_token;
+            const T* const py = static_cast<const T*>(side.dy) + (int64_t)t0 * side.dy_token;
+            T* const po = static_cast<T*>(side.out) + (int64_t)t0 * side.out_token;
+            Row<T, V> rx[U], ry[U], nx[U], ny[U];
+            // a group's vectors are `groups` apart
+            const int step_t = groups / max(side.heads, 1), step_h = groups - step_t * side.heads;
+            int t = group / max(side.heads, 1), h = group - t * side.heads;
+            auto fetch = [&](Row<T, V>(&x)[U], Row<T, V>(&y)[U], int t, int h) {
+                if (t >= n) return;
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    x[u].load(px + t * side.x_token + h * side.x_head, unit[u], g.dim);
+                    if (BACK) y[u].load(py + t * side.dy_token + h * side.dy_head, unit[u], g.dim);
+                }
+            };
+            if (rows) fetch(rx, ry, t, h);
             for (int first = 0; first < rows; first += groups) {
-                const int row = first + group, t = min(row, rows - 1) / side.heads, h = min(row, rows - 1) - t * side.heads;
-                const T* p = static_cast<const T*>(side.x) + (int64_t)(t0 + t) * side.x_token + h * side.x_head;
-                float x[U][2 * V], ss = 0.f;
+                int next_t = t + step_t, next_h = h + step_h;
+                if (next_h >= side.heads) next_h -= side.heads, ++next_t;
+                fetch(nx, ny, next_t, next_h);
+                const bool live = t < n;
+                const int at = min(t, n - 1);
+                T* const q = po + at * side.out_token + h * side.out_head;
+                const float *c = cs + at * g.angles, *s = sn + at * g.angles;
+                Pair x[U][V], y[U][V], w[U][V], ss = both(0.f), gx = both(0.f);
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    load<T, V>(p, unit[u], g.dim, x[u]);
+                    rx[u].get(x[u]);
+                    if (BACK) {
+                        ry[u].get(y[u]);
+                        if (unit[u].turns) turn<V, INTER, true>(y[u], c + unit[u].angle, s + unit[u].angle);
+                        weights<V>(s_weight[which], unit[u], w[u]);
+                    }
 #pragma unroll
-                    for (int i = 0; i < 2 * V; ++i) ss = fmaf(x[u][i], x[u][i], ss);
+                    for (int i = 0; i < V; ++i) {
+                        ss = fma2(x[u][i], x[u][i], ss);
+                        if (BACK) w[u][i] = y[u][i] * w[u][i], gx = fma2(w[u][i], x[u][i], gx);
+                    }
                 }
-                const float r = 1.f / sqrtf(group_sum(ss, lanes) / g.dim + g.eps);
-                T* q = static_cast<T*>(side.out) + (int64_t)(t0 + t) * side.out_token + h * side.out_head;
+                const float f = inverse_root(group_sum(total(ss), lanes), g);
+                if (!BACK) {
+                    const Pair f2 = both(f);
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
+                    for (int u = 0; u < U; ++u) {
+                        weights<V>(s_weight[which], unit[u], w[u]);
 #pragma unroll
-                    for (int i = 0; i < 2 * V; ++i) x[u][i] *= r * w[u][i];
-                    turn<V>(unit[u], x[u], cs + t * half, sn + t * half, 1.f);
-                    if (row < rows) store<T, V>(q, unit[u], g.dim, x[u]);
+                        for (int i = 0; i < V; ++i) x[u][i] = x[u][i] * f2 * w[u][i];
+                        if (unit[u].turns) turn<V, INTER, false>(x[u], c + unit[u].angle, s + unit[u].angle);
+                        if (live) Row<T, V>::store(q, unit[u], g.dim, x[u]);
+                    }
+                } else {
+                    const float back = f * f * (group_sum(total(gx), lanes) * g.per_dim);
+                    const Pair f2 = both(live ? f : 0.f), fb = both(-f * back), fx = both(f);
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+#pragma unroll
+                        for (int i = 0; i < V; ++i) {
+                            dw[BACK ? which : 0][u][i] = fma2(y[u][i], x[u][i] * f2, dw[BACK ? which : 0][u][i]);
+                            x[u][i] = fma2(x[u][i], fb, fx * w[u][i]);
+                        }
+                        if (live) Row<T, V>::store(q, unit[u], g.dim, x[u]);
+                    }
                 }
+#pragma unroll
+                for (int u = 0; u < U; ++u) rx[u] = nx[u], ry[u] = ny[u];
+                t = next_t, h = next_h;
             }
         }
     }
-}
-
-template <class T, int V, int U>
-__global__ void __launch_bounds__(kThreads) k_qk_norm_back(const __grid_constant__ Args g) {
-    extern __shared__ float smem[];
-    const int half = g.rotary / 2, lanes = 1 << g.group_log, groups = kThreads >> g.group_log;
-    const int lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> g.group_log;
-    float *cs = smem, *sn = smem + g.tile * half;
-    Unit unit[U];
+    if (!BACK || !g.part) return;
+    // the block's sums: group after group, in order
 #pragma unroll
-    for (int u = 0; u < U; ++u) unit[u] = unit_at<V>(g, lane + u * lanes);
-    const int tiles = (g.tokens + g.tile - 1) / g.tile;
-    for (int which = 0; which < 2; ++which) {
-        const Side& side = g.side[which];
-        float w[U][2 * V], dw[U][2 * V];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            load_weight<T, V>(side.weight, g.wf32, unit[u], g.dim, w[u]);
-#pragma unroll
-            for (int i = 0; i < 2 * V; ++i) dw[u][i] = 0.f;
-        }
-        for (int tile = blockIdx.x; side.heads && tile < tiles; tile += gridDim.x) {
-            const int t0 = tile * g.tile, n = min(g.tile, g.tokens - t0);
-            __syncthreads();
-            form_angles(g, t0, n, cs, sn);
-            __syncthreads();
-            const int rows = n * side.heads;
-            for (int first = 0; first < rows; first += groups) {
-                const int row = first + group, t = min(row, rows - 1) / side.heads, h = min(row, rows - 1) - t * side.heads;
-                const T* p = static_cast<const T*>(side.x) + (int64_t)(t0 + t) * side.x_token + h * side.x_head;
-                const T* d = static_cast<const T*>(side.dy) + (int64_t)(t0 + t) * side.dy_token + h * side.dy_head;
-                float x[U][2 * V], y[U][2 * V], ss = 0.f, gx = 0.f;
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    load<T, V>(p, unit[u], g.dim, x[u]);
-                    load<T, V>(d, unit[u], g.dim, y[u]);
-                }
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    turn<V>(unit[u], y[u], cs + t * half, sn + t * half, -1.f);
-#pragma unroll
-                    for (int i = 0; i < 2 * V; ++i) {
-                        ss = fmaf(x[u][i], x[u][i], ss);
-                        gx = fmaf(y[u][i] * w[u][i], x[u][i], gx);
-                    }
-                }
-                const float r = 1.f / sqrtf(group_sum(ss, lanes) / g.dim + g.eps);
-                const float back = r * r * (group_sum(gx, lanes) / g.dim);
-                T* q = static_cast<T*>(side.out) + (int64_t)(t0 + t) * side.out_token + h * side.out_head;
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-#pragma unroll
-                    for (int i = 0; i < 2 * V; ++i) {
-                        if (row < rows) dw[u][i] = fmaf(y[u][i], x[u][i] * r, dw[u][i]);
-                        x[u][i] = r * (y[u][i] * w[u][i] - x[u][i] * back);
-                    }
-                    if (row < rows) store<T, V>(q, unit[u], g.dim, x[u]);
-                }
-            }
-        }
-        if (!g.part) continue;
-        // the block's sums: group after group, in order
+    for (int which = 0; which < (BACK ? 2 : 1); ++which) {
         __syncthreads();
-        float* sums = smem;  // [groups][dim]
+        float* const sums = smem;  // [groups][dim]
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int i = 0; i < 2 * V; ++i) {
-                const int c = i < V ? unit[u].a + i : unit[u].b + i - V;
-                if (c < g.dim) sums[group * g.dim + c] = dw[u][i];
+            for (int i = 0; i < V; ++i) {
+                const float2 d = split(dw[which][u][i]);
+                const int c = V == 1 ? unit[u].a : 2 * i < V ? unit[u].a + 2 * i : unit[u].b + 2 * i - V, e = V == 1 ? unit[u].b : c + 1;
+                if (c < g.dim) sums[group * g.dim + c] = d.x;
+                if (e < g.dim) sums[group * g.dim + e] = d.y;
             }
         __syncthreads();
         for (int c = threadIdx.x; c < g.dim; c += kThreads) {
@@ -255,21 +339,22 @@ __global__ void __launch_bounds__(kThreads) k_qk_norm_back(const __grid_constant
     }
 }
 
-// Sums of the blocks' rows, in order: 32 columns a block, 8 warps with every eighth row each.
+// Sums of the blocks' rows, in a fixed order: 32 columns a block, 32 warps with every 32nd row each.
 template <class W>
-__global__ void __launch_bounds__(256) k_join_weights(const float* part, int blocks, int dim, W* dq, W* dk) {
-    __shared__ float sums[8][32];
+__global__ void __launch_bounds__(1024) k_join_weights(const float* part, int blocks, int dim, W* dq, W* dk) {
+    __shared__ float sums[32][33];
     wait_for_predecessor();
-    const int c = blockIdx.x * 32 + threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int lane = threadIdx.x % 32, c = blockIdx.x * 32 + lane, warp = threadIdx.x / 32;
     float s = 0.f;
-    if (c < dim)
-        for (int b = warp; b < blocks; b += 8) s += part[((int64_t)b * 2 + blockIdx.y) * dim + c];
-    sums[warp][threadIdx.x % 32] = s;
+#pragma unroll 4
+    for (int b = warp; b < blocks; b += 32)
+        if (c < dim) s += part[((int64_t)b * 2 + blockIdx.y) * dim + c];
+    sums[warp][lane] = s;
     __syncthreads();
     W* out = blockIdx.y ? dk : dq;
-    if (warp || c >= dim || !out) return;
-    for (int i = 1; i < 8; ++i) s += sums[i][threadIdx.x];
-    out[c] = from_f<W>(s);
+    s = sums[lane][warp];  // a warp has a column now
+    for (int m = 16; m; m >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, m);
+    if (lane == 0 && blockIdx.x * 32 + warp < dim && out) out[blockIdx.x * 32 + warp] = from_f<W>(s);
 }
 
 int size_of(int type) { return type == ONES_F32 ? 4 : 2; }
@@ -278,28 +363,30 @@ bool bad_heads(const ones_heads& h, int dim, int tokens) {
     return h.heads < 0 || h.heads > ONES_MAX_HEADS || h.head < dim || (h.token < 0 && tokens > 1);
 }
 
-template <class T, int V, int U>
+template <class T, int V, int U, bool INTER>
 cudaError_t launch(Args& a, bool back, cudaStream_t stream, int* blocks) {
     const int units = V == 1 ? (a.dim + 1) / 2 : (a.dim / V + 1) / 2;
     a.group_log = 0;
     while ((1 << a.group_log) * U < units) ++a.group_log;
     const int groups = kThreads >> a.group_log, heads = max(1, a.side[0].heads + a.side[1].heads);
-    // Tokens of a block: enough vectors for two turns of all groups, at most 32, and fewer where that leaves SMs idle.
-    a.tile = max(1, min(32, 2 * groups / heads));
-    while (a.tile > 1 && (a.tokens + a.tile - 1) / a.tile < 2 * device_sms()) a.tile = (a.tile + 1) / 2;
+    // Tokens of a block at a time: enough vectors for four rounds of all groups (backward, where a block has many tiles: eight), at most
+    // 16, and fewer where that leaves SMs idle.
+    a.tile = max(1, min(16, (back ? 8 : 4) * groups / heads));
+    while (a.tile > 1 && (a.tokens + a.tile - 1) / a.tile < 4 * device_sms()) a.tile = (a.tile + 1) / 2;
+    a.angles = (a.rotary / 2 + 3) / 4 * 4;
     const int tiles = (a.tokens + a.tile - 1) / a.tile;
-    const int grid = back ? min(tiles, kMaxBlocks) : min(tiles, 148 * 8);
-    const int smem = max(a.tile * a.rotary, back ? groups * a.dim : 0) * 4;
-    *blocks = grid;
-    auto kernel = back ? k_qk_norm_back<T, V, U> : k_qk_norm<T, V, U>;
-    kernel<<<grid, kThreads, smem, stream>>>(a);
+    *blocks = back ? min(tiles, kMaxBlocks) : tiles;
+    const int smem = max(2 * a.tile * a.angles, back && a.part ? groups * a.dim : 0) * 4;
+    auto kernel = back ? k_qk_norm<T, V, U, INTER, true> : k_qk_norm<T, V, U, INTER, false>;
+    kernel<<<*blocks, kThreads, smem, stream>>>(a);
     return cudaGetLastError();
 }
 
 template <class T>
 cudaError_t launch_of(Args& a, bool back, bool wide, cudaStream_t stream, int* blocks) {
-    if (wide) return launch<T, 16 / sizeof(T), 1>(a, back, stream, blocks);
-    return launch<T, 1, 4>(a, back, stream, blocks);
+    constexpr int V = 16 / sizeof(T);
+    if (wide) return a.interleaved ? launch<T, V, 1, true>(a, back, stream, blocks) : launch<T, V, 1, false>(a, back, stream, blocks);
+    return a.interleaved ? launch<T, 1, 4, true>(a, back, stream, blocks) : launch<T, 1, 4, false>(a, back, stream, blocks);
 }
 
 int run(const ones_heads* dq, const ones_heads* dk, const ones_heads* q, const ones_heads* k, const int64_t* positions,
@@ -319,7 +406,7 @@ int run(const ones_heads* dq, const ones_heads* dk, const ones_heads* q, const o
     const bool sums = back && (q_dweight || k_dweight);
     Args a = {};
     const int v = 16 / size;
-    // 16-byte pieces: every vector starts on such a boundary, and no piece holds both rotated values and others
+    // Pieces of 16 bytes: every vector starts on the boundary of one, and none holds both rotated values and others.
     bool wide = dim % v == 0 && rotary % (2 * v) == 0;
     for (int i = 0; i < 2; ++i) {
         if (x[i]->heads != o[i]->heads || (back && x[i]->heads != y[i]->heads) || x[i]->heads < 0 || x[i]->heads > ONES_MAX_HEADS)
@@ -329,7 +416,7 @@ int run(const ones_heads* dq, const ones_heads* dk, const ones_heads* q, const o
             if (bad_heads(*h, dim, tokens)) return ONES_ERR_BAD_PARAM;
             if (tokens && !h->d_data) return ONES_ERR_NULL;
             if (!aligned(h->d_data, size)) return ONES_ERR_ALIGN;
-            wide = wide && aligned(h->d_data, 16) && (h->heads == 1 || h->head % v == 0) && (tokens <= 1 || h->token % v == 0);
+            wide = wide && aligned(h->d_data, v * size) && (h->heads == 1 || h->head % v == 0) && (tokens <= 1 || h->token % v == 0);
         }
         if (!aligned(w[i], wsize) || !aligned(dw[i], wsize)) return ONES_ERR_ALIGN;
         a.side[i] = {x[i]->d_data, back ? y[i]->d_data : nullptr, w[i], o[i]->d_data, dw[i], x[i]->token, x[i]->head,
@@ -350,17 +437,17 @@ int run(const ones_heads* dq, const ones_heads* dk, const ones_heads* q, const o
         return err == cudaSuccess ? ONES_OK : ONES_ERR_CUDA;
     }
     a.positions = positions, a.frequencies = frequencies, a.part = sums ? static_cast<float*>(workspace) : nullptr;
-    a.tokens = tokens, a.dim = dim, a.rotary = rotary, a.interleaved = interleaved != 0, a.wf32 = wtype == ONES_F32, a.eps = eps;
+    a.tokens = tokens, a.dim = dim, a.rotary = rotary, a.interleaved = interleaved != 0, a.wf32 = wtype == ONES_F32, a.eps = eps, a.per_dim = 1.f / dim;
     int blocks = 0;
     err = type == ONES_F32 ? launch_of<float>(a, back, wide, stream, &blocks)
           : type == ONES_BF16 ? launch_of<__nv_bfloat16>(a, back, wide, stream, &blocks)
                               : launch_of<__half>(a, back, wide, stream, &blocks);
     if (err == cudaSuccess && sums) {
         const dim3 grid((dim + 31) / 32, 2);
-        err = wtype == ONES_F32 ? launch_after(k_join_weights<float>, grid, dim3(256), stream, a.part, blocks, dim, (float*)q_dweight, (float*)k_dweight)
-              : wtype == ONES_BF16 ? launch_after(k_join_weights<__nv_bfloat16>, grid, dim3(256), stream, a.part, blocks, dim,
+        err = wtype == ONES_F32 ? launch_after(k_join_weights<float>, grid, dim3(1024), stream, a.part, blocks, dim, (float*)q_dweight, (float*)k_dweight)
+              : wtype == ONES_BF16 ? launch_after(k_join_weights<__nv_bfloat16>, grid, dim3(1024), stream, a.part, blocks, dim,
                                                   (__nv_bfloat16*)q_dweight, (__nv_bfloat16*)k_dweight)
-                                   : launch_after(k_join_weights<__half>, grid, dim3(256), stream, a.part, blocks, dim, (__half*)q_dweight,
+                                   : launch_after(k_join_weights<__half>, grid, dim3(1024), stream, a.part, blocks, dim, (__half*)q_dweight,
                                                   (__half*)k_dweight);
     }
     return err == cudaSuccess ? ONES_OK : ONES_ERR_CUDA;
