@@ -28,7 +28,8 @@ struct BackArgs {
     const PlanHead* head;
     const float* lse;           // [tokens][heads]
     float* delta;               // the same; exact from the first pass on
-    const unsigned* largest;    // [4][kv]: bits of the largest finite |dout|, |v|, |q| and |k| of a head or group
+    const unsigned* largest;    // [2][kv]: bits of the largest finite |dout| and |v| of a head or group
+    const int* power;           // [2][kv]: of q and k
     HeadsOut dq, dk, dv;
     int tokens, heads, kv, group, kt, dim;
     float scale;
@@ -42,35 +43,44 @@ struct Powers {
     int sigma, q, k;
 };
 __device__ __forceinline__ int above(unsigned bits) { return (int)(bits >> 23) - 126; }  // |x| < 2^above
+// The power of a head's queries or keys is guessed from those of the first token, whose largest goes to 2^(15 - kRoom); where the
+// others turn out to be larger than there is room for, they are laid out again.
+constexpr int kRoom = 6;
 __device__ __forceinline__ int operand_power(unsigned bits) { return min(15 - above(bits), 100); }
 template <bool F16>
 __device__ __forceinline__ Powers powers_of(const BackArgs& g, int h) {
     Powers p;
     const int bound = 8 + above(g.largest[h]) + above(g.largest[g.kv + h]);  // 2^7 >= dim
     p.sigma = min(max(15 - bound, -100), 100);
-    p.q = F16 ? 0 : operand_power(g.largest[2 * g.kv + h]);
-    p.k = F16 ? 0 : operand_power(g.largest[3 * g.kv + h]);
+    p.q = F16 ? 0 : g.power[h];
+    p.k = F16 ? 0 : g.power[g.kv + h];
     return p;
 }
 
-// ---- delta = dout . out, and the largest values ----
+// ---- delta = dout . out, the largest values, and bfloat16 queries and keys as float16 ----
 
+struct Vectors {
+    const uint16_t* p;
+    int64_t token, head;
+};
 struct SurveyArgs {
-    const uint16_t* p[5];  // dout, v, q, k, out
-    int64_t token[5], head[5];
+    Vectors dout, out, v, q, k;
+    uint16_t* narrow[2];  // of q and k, [tokens][heads][row]
     const PlanHead* plan;
     float* delta;
-    unsigned* largest;
-    int tokens, heads, kv, dim, wide;  // wide: out starts on 16-byte boundaries
+    unsigned* largest;    // [4][kv]: bits of the largest finite |dout|, |v|, |q| and |k|
+    int* power;           // [2][kv]
+    int tokens, heads, kv, dim, row, wide;  // wide: out starts on 16-byte boundaries
 };
 
 template <bool F16>
 __device__ __forceinline__ float value16(uint16_t b) {
     return F16 ? __half2float(__ushort_as_half(b)) : __uint_as_float((uint32_t)b << 16);
 }
-__device__ __forceinline__ uint16_t half_of(const uint4& v, int i) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    return (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+template <bool F16>
+__device__ __forceinline__ float2 values16(uint32_t w) {
+    if constexpr (F16) return __half22float2(*reinterpret_cast<const __half2*>(&w));
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
 }
 
 // Values c..c + 7 of a vector of dim values that starts on a 16-byte boundary; none behind its last is read.
@@ -82,75 +92,136 @@ __device__ __forceinline__ uint4 eight_of(const uint16_t* p, int c, int dim) {
         if (c + i < dim) w[i / 2] |= (uint32_t)p[c + i] << (16 * (i & 1));
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
+// The largest finite value's bits, as a 32-bit number.
+template <bool F16>
+__device__ __forceinline__ unsigned largest_of(const uint4& v) {
+    constexpr unsigned kLimit = F16 ? 0x7C00u : 0x7F80u;  // infinity
+    const uint32_t w[4] = {v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu, v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu};
+    const uint32_t m = __vmaxu2(__vmaxu2(w[0], w[1]), __vmaxu2(w[2], w[3]));
+    unsigned top = max(m & 0xFFFFu, m >> 16);
+    if (top >= kLimit) {
+        top = 0;
+        for (int i = 0; i < 8; ++i) {
+            const unsigned b = w[i / 2] >> (16 * (i & 1)) & 0xFFFFu;
+            if (b < kLimit) top = max(top, b);
+        }
+    }
+    return __float_as_uint(value16<F16>((uint16_t)top));
+}
+// bfloat16 as float16 times a power of two.
+__device__ __forceinline__ uint4 narrowed(const uint4& v, float f) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 x = split(pair(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u)) * both(f));
+        r[i] = pack16<true>(x.x, x.y);
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
+}
 
-// LANES x 8 values are a vector. A group of lanes takes a token and goes through its heads, four at a time.
+// LANES x 8 values are a vector, which a group of lanes takes. A block takes kTokens tokens at a time.
+constexpr int kTokens = 16;
 template <bool F16, int LANES>
-__global__ void __launch_bounds__(256) k_survey(const SurveyArgs g) {
-    extern __shared__ unsigned top[];  // [4][kv]
+__global__ void __launch_bounds__(256) k_survey(const __grid_constant__ SurveyArgs g) {
+    extern __shared__ unsigned top[];  // [4][kv], then the factors of q and k, [2][kv]
     constexpr int kGroups = 256 / LANES, kAtOnce = 4;
+    float* const factor = reinterpret_cast<float*>(top + 4 * g.kv);
     const int lane = threadIdx.x % LANES, c = 8 * lane;
-    for (int i = threadIdx.x; i < 4 * g.kv; i += 256) top[i] = 0;
-    __syncthreads();
     wait_for_predecessor();
     let_successor_start();
     const int t0 = g.plan->covered[0], t1 = g.plan->covered[1], group = g.heads / g.kv;
-    auto fetch = [&](int which, int t, int h) { return eight_of(g.p[which] + t * g.token[which] + h * g.head[which], c, g.dim); };
+    for (int i = threadIdx.x; i < 4 * g.kv; i += 256) top[i] = 0;
+    __syncthreads();
     auto note = [&](const uint4& v, int which, int h) {
-        unsigned m = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const unsigned b = __float_as_uint(value16<F16>(half_of(v, i))) & 0x7FFFFFFFu;
-            if (b < 0x7F800000u) m = max(m, b);
-        }
+        const unsigned m = largest_of<F16>(v);
         unsigned* const at = top + which * g.kv + h;
         if (m > *at) atomicMax(at, m);
     };
-    const int rounds = (t1 - t0 + kGroups * gridDim.x - 1) / (kGroups * gridDim.x);
-    for (int round = 0; round < rounds; ++round) {
-        const int t = t0 + (round * gridDim.x + blockIdx.x) * kGroups + threadIdx.x / LANES;
-        const bool live = t < t1;
-        for (int h0 = 0; h0 < g.heads; h0 += kAtOnce) {
+    if (!F16) {
+        // the guess, the same by every block
+        for (int i = threadIdx.x / LANES; t0 < t1 && i < g.heads + g.kv; i += kGroups) {
+            const bool keys = i >= g.heads;
+            const int h = keys ? i - g.heads : i;
+            const Vectors& x = keys ? g.k : g.q;
+            note(eight_of(x.p + t0 * x.token + h * x.head, c, g.dim), keys ? 3 : 2, keys ? h : h / group);
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * g.kv; i += 256) {
+            const int p = operand_power(top[2 * g.kv + i]) - kRoom;
+            factor[i] = exp2f((float)p);
+            if (blockIdx.x == 0) g.power[i] = p;
+        }
+        __syncthreads();
+    }
+    const int own = threadIdx.x / LANES;
+    const uint32_t per_head = 0xFFFFFFFFu / g.heads + 1, per_kv = 0xFFFFFFFFu / g.kv + 1, per_group = 0xFFFFFFFFu / group + 1;
+    auto over = [](uint32_t r, uint32_t n, uint32_t per) { return n == 1 ? r : __umulhi(r, per); };  // r / n below 2^16, with 2^32 / n rounded up
+    for (int first = t0 + blockIdx.x * kTokens; first < t1; first += gridDim.x * kTokens) {
+        const int n_t = min(kTokens, t1 - first);
+        // Neighbouring groups have neighbouring vectors: four of each group are on their way at a time.
+        const uint16_t *dout = g.dout.p + first * g.dout.token, *out = g.out.p + first * g.out.token;
+        for (int r0 = 0; r0 < n_t * g.heads; r0 += kAtOnce * kGroups) {
             uint4 a[kAtOnce], b[kAtOnce];
-            float dot[kAtOnce] = {};
+            int at_t[kAtOnce], at_h[kAtOnce];
 #pragma unroll
             for (int x = 0; x < kAtOnce; ++x) {
+                const int r = r0 + x * kGroups + own;
+                at_t[x] = over(r, g.heads, per_head), at_h[x] = r - at_t[x] * g.heads;
                 a[x] = b[x] = make_uint4(0, 0, 0, 0);
-                if (!live || h0 + x >= g.heads) continue;
-                a[x] = fetch(0, t, h0 + x);
-                if (g.wide) b[x] = fetch(4, t, h0 + x);
+                if (at_t[x] >= n_t) continue;
+                a[x] = eight_of(dout + at_t[x] * g.dout.token + at_h[x] * g.dout.head, c, g.dim);
+                if (g.wide) b[x] = eight_of(out + at_t[x] * g.out.token + at_h[x] * g.out.head, c, g.dim);
             }
-            if (!g.wide && live) {  // single values, in another order: dout is read again, from the first-level cache
 #pragma unroll
-                for (int x = 0; x < kAtOnce; ++x) {
-                    if (h0 + x >= g.heads) continue;
-                    const uint16_t* const u = g.p[0] + t * g.token[0] + (h0 + x) * g.head[0];
-                    const uint16_t* const w = g.p[4] + t * g.token[4] + (h0 + x) * g.head[4];
+            for (int x = 0; x < kAtOnce; ++x) {
+                const bool live = at_t[x] < n_t;
+                float dot = 0.f;
+                if (live) note(a[x], 0, over(at_h[x], group, per_group));
+                if (g.wide) {
+                    const uint32_t u[4] = {a[x].x, a[x].y, a[x].z, a[x].w}, w[4] = {b[x].x, b[x].y, b[x].z, b[x].w};
+                    Pair d = both(0.f);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 y = values16<F16>(u[i]), z = values16<F16>(w[i]);
+                        d = fma2(pair(y.x, y.y), pair(z.x, z.y), d);
+                    }
+                    dot = total_of(d);
+                } else if (live) {  // single values, in another order: dout is read again, from the first-level cache
+                    const uint16_t* const u = dout + at_t[x] * g.dout.token + at_h[x] * g.dout.head;
+                    const uint16_t* const w = out + at_t[x] * g.out.token + at_h[x] * g.out.head;
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        if (lane + i * LANES < g.dim) dot[x] = fmaf(value16<F16>(u[lane + i * LANES]), value16<F16>(w[lane + i * LANES]), dot[x]);
-                }
-            }
-#pragma unroll
-            for (int x = 0; x < kAtOnce; ++x) {
-                if (live && h0 + x < g.heads) note(a[x], 0, (h0 + x) / group);
-                if (g.wide) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) dot[x] = fmaf(value16<F16>(half_of(a[x], i)), value16<F16>(half_of(b[x], i)), dot[x]);
+                        if (lane + i * LANES < g.dim) dot = fmaf(value16<F16>(u[lane + i * LANES]), value16<F16>(w[lane + i * LANES]), dot);
                 }
 #pragma unroll
-                for (int m = LANES / 2; m; m >>= 1) dot[x] += __shfl_xor_sync(0xFFFFFFFFu, dot[x], m);
-                if (lane == 0 && live && h0 + x < g.heads) g.delta[(int64_t)t * g.heads + h0 + x] = dot[x];
+                for (int m = LANES / 2; m; m >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, m);
+                if (lane == 0 && live) g.delta[(int64_t)(first + at_t[x]) * g.heads + at_h[x]] = dot;
             }
         }
-        for (int which = 1; live && which < (F16 ? 2 : 4); ++which) {
-            const int n = which == 2 ? g.heads : g.kv;
-            for (int h0 = 0; h0 < n; h0 += kAtOnce) {
+        // v, then (bfloat16) q and k
+#pragma unroll
+        for (int kind = 0; kind < (F16 ? 1 : 3); ++kind) {
+            const Vectors& from = kind == 0 ? g.v : kind == 1 ? g.q : g.k;
+            const int n = kind == 1 ? g.heads : g.kv;
+            const uint32_t per = kind == 1 ? per_head : per_kv;
+            const uint16_t* const in = from.p + first * from.token;
+            for (int r0 = 0; r0 < n_t * n; r0 += kAtOnce * kGroups) {
                 uint4 a[kAtOnce];
 #pragma unroll
-                for (int x = 0; x < kAtOnce; ++x) a[x] = h0 + x < n ? fetch(which, t, h0 + x) : make_uint4(0, 0, 0, 0);
+                for (int x = 0; x < kAtOnce; ++x) {
+                    const int r = r0 + x * kGroups + own, t = over(r, n, per);
+                    a[x] = t < n_t ? eight_of(in + t * from.token + (r - t * n) * from.head, c, g.dim) : make_uint4(0, 0, 0, 0);
+                }
 #pragma unroll
-                for (int x = 0; x < kAtOnce; ++x)
-                    if (h0 + x < n) note(a[x], which, which == 2 ? (h0 + x) / group : h0 + x);
+                for (int x = 0; x < kAtOnce; ++x) {
+                    const int r = r0 + x * kGroups + own, t = over(r, n, per);
+                    if (t >= n_t) continue;
+                    const int h = kind == 1 ? over(r - t * n, group, per_group) : r - t * n;
+                    note(a[x], 1 + kind, h);
+                    if (kind && c < g.row)
+                        *reinterpret_cast<uint4*>(g.narrow[kind - 1] + ((int64_t)first * n + r) * g.row + c) = narrowed(a[x], factor[(kind - 1) * g.kv + h]);
+                }
             }
         }
     }
@@ -159,44 +230,30 @@ __global__ void __launch_bounds__(256) k_survey(const SurveyArgs g) {
         if (top[i]) atomicMax(g.largest + i, top[i]);
 }
 
-// ---- bfloat16 queries and keys as float16 ----
-
-struct NarrowArgs {
-    const uint16_t* p[2];  // q, k
-    int64_t token[2], head[2];
-    uint16_t* out[2];      // [tokens][heads][row]
-    const PlanHead* plan;
-    const unsigned* largest;
-    int heads, kv, dim, row;
-};
-
+// Lays out again the heads whose guess was too small (or had nothing to go by). Every block looks, none writes the powers before all
+// have: the passes take them from `settled`.
 template <int LANES>
-__global__ void __launch_bounds__(256) k_narrow(const NarrowArgs g) {
-    constexpr int kGroups = 256 / LANES, kAtOnce = 4;
+__global__ void __launch_bounds__(256) k_settle(const __grid_constant__ SurveyArgs g, int* settled) {
+    constexpr int kGroups = 256 / LANES;
     const int c = 8 * (threadIdx.x % LANES);
     wait_for_predecessor();
     let_successor_start();
     const int t0 = g.plan->covered[0], t1 = g.plan->covered[1], group = g.heads / g.kv;
-    if (c >= g.row) return;
-    for (int t = t0 + blockIdx.x * kGroups + threadIdx.x / LANES; t < t1; t += gridDim.x * kGroups)
-        for (int which = 0; which < 2; ++which) {
-            const int n = which ? g.kv : g.heads;
-            for (int h0 = 0; h0 < n; h0 += kAtOnce) {
-                uint4 a[kAtOnce];
-#pragma unroll
-                for (int x = 0; x < kAtOnce; ++x)
-                    if (h0 + x < n) a[x] = eight_of(g.p[which] + t * g.token[which] + (h0 + x) * g.head[which], c, g.dim);
-#pragma unroll
-                for (int x = 0; x < kAtOnce; ++x) {
-                    if (h0 + x >= n) continue;
-                    const float f = exp2f((float)operand_power(g.largest[(2 + which) * g.kv + (which ? h0 + x : (h0 + x) / group)]));
-                    uint32_t w[4];
-#pragma unroll
-                    for (int i = 0; i < 8; i += 2) w[i / 2] = pack16<true>(value16<false>(half_of(a[x], i)) * f, value16<false>(half_of(a[x], i + 1)) * f);
-                    *reinterpret_cast<uint4*>(g.out[which] + ((int64_t)t * n + h0 + x) * g.row + c) = make_uint4(w[0], w[1], w[2], w[3]);
-                }
-            }
+    for (int i = 0; i < 2 * g.kv; ++i) {
+        const int guess = g.power[i], best = operand_power(g.largest[2 * g.kv + i]);
+        const bool again = best < guess || guess >= 100 - kRoom;
+        if (blockIdx.x == 0 && threadIdx.x == 0) settled[i] = again ? best : guess;
+        if (!again) continue;
+        const int keys = i >= g.kv, h = i - keys * g.kv, n = keys ? g.kv : g.heads, times = keys ? 1 : group;
+        const Vectors& from = keys ? g.k : g.q;
+        const float f = exp2f((float)best);
+        for (int64_t r = (int64_t)blockIdx.x * kGroups + threadIdx.x / LANES; r < (int64_t)(t1 - t0) * times; r += (int64_t)gridDim.x * kGroups) {
+            const int64_t t = t0 + r / times;
+            const int head = h * times + (int)(r % times);
+            if (c < g.row)
+                *reinterpret_cast<uint4*>(g.narrow[keys] + (t * n + head) * g.row + c) = narrowed(eight_of(from.p + t * from.token + head * from.head, c, g.dim), f);
         }
+    }
 }
 
 // Heads of up to 64 values leave room for two sets of what belongs to an item (its tiles in shared memory, its sums in tensor
@@ -903,7 +960,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 struct BackPlan {
     int group, kt, row;
     int64_t most[2];
-    size_t at_start, at_prefix[2], at_items[2], at_largest, at_delta, at_narrow[2], bytes;
+    size_t at_start, at_prefix[2], at_items[2], at_largest, at_power, at_delta, at_narrow[2], bytes;
 };
 BackPlan back_plan(int tokens, int sequences, int heads, int kv, int dim) {
     BackPlan p;
@@ -914,7 +971,7 @@ BackPlan back_plan(int tokens, int sequences, int heads, int kv, int dim) {
     const size_t bounds = ((size_t)sequences + 1) * 4;
     p.at_start = take(2 * bounds);
     for (int i = 0; i < 2; ++i) p.at_prefix[i] = take(bounds), p.at_items[i] = take((size_t)p.most[i] * sizeof(Item));
-    p.at_largest = take((size_t)4 * kv * 4);
+    p.at_largest = take((size_t)4 * kv * 4), p.at_power = take((size_t)4 * kv * 4);
     p.at_delta = take((size_t)tokens * heads * 4);
     p.row = (dim + 7) / 8 * 8;
     p.at_narrow[0] = take((size_t)tokens * heads * p.row * 2), p.at_narrow[1] = take((size_t)tokens * kv * p.row * 2);  // for bfloat16
@@ -942,27 +999,27 @@ cudaError_t launch_pass(K kernel, int smem, std::atomic<uint64_t>& ready, int64_
 }
 
 template <int HALVES, bool F16>
-cudaError_t launch_back(const ones_heads& dout, const ones_heads& q, const ones_heads& k, const ones_heads& v, const SurveyArgs& d,
-                        const NarrowArgs& n, BackArgs a, const PlanArgs& plan, const BackPlan& p, cudaStream_t stream) {
-    constexpr int kLanes = 8 * HALVES, kGroups = 256 / kLanes;
+cudaError_t launch_back(const ones_heads& dout, const ones_heads& q, const ones_heads& k, const ones_heads& v, const SurveyArgs& d, BackArgs a,
+                        const PlanArgs& plan, const BackPlan& p, cudaStream_t stream) {
+    constexpr int kLanes = 8 * HALVES;
     CUtensorMap maps[4];
     ones_heads qs = q, ks = k;
-    if (!F16) qs = {n.out[0], (int64_t)a.heads * n.row, n.row, a.heads}, ks = {n.out[1], (int64_t)a.kv * n.row, n.row, a.kv};
+    if (!F16) qs = {d.narrow[0], (int64_t)a.heads * d.row, d.row, a.heads}, ks = {d.narrow[1], (int64_t)a.kv * d.row, d.row, a.kv};
     cudaError_t err = make_heads_map(&maps[0], qs, a.dim, a.tokens, a.group, a.kt, true);
     if (err == cudaSuccess) err = make_heads_map(&maps[1], dout, a.dim, a.tokens, a.group, a.kt, F16);
     if (err == cudaSuccess) err = make_heads_map(&maps[2], ks, a.dim, a.tokens, 1, kKeys, true);
     if (err == cudaSuccess) err = make_heads_map(&maps[3], v, a.dim, a.tokens, 1, kKeys, F16);
     if (err == cudaSuccess) err = launch_plan(plan, 2, stream);
     if (err != cudaSuccess) return err;
-    const int blocks = (a.tokens + kGroups - 1) / kGroups, most = 8 * device_sms(), grid = blocks < most ? blocks : most;
+    const int blocks = (a.tokens + kTokens - 1) / kTokens, most = 8 * device_sms(), grid = blocks < most ? blocks : most;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid), cfg.blockDim = dim3(256), cfg.dynamicSmemBytes = (size_t)4 * a.kv * 4, cfg.stream = stream;
+    cfg.gridDim = dim3(grid), cfg.blockDim = dim3(256), cfg.dynamicSmemBytes = (size_t)6 * a.kv * 4, cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr, cfg.numAttrs = 1;
     err = cudaLaunchKernelEx(&cfg, k_survey<F16, kLanes>, d);
-    if (err == cudaSuccess && !F16) err = launch_after(k_narrow<kLanes>, dim3(grid), dim3(256), stream, n);
+    if (err == cudaSuccess && !F16) err = launch_after(k_settle<kLanes>, dim3(grid < device_sms() ? grid : device_sms()), dim3(256), stream, d, const_cast<int*>(a.power));
     if (err != cudaSuccess) return err;
     static std::atomic<uint64_t> ready[2];
     a.items = plan.items[0], a.head = plan.head;
@@ -1012,23 +1069,20 @@ int ones_attention_backward(const ones_heads* dout, const ones_heads* q, const o
     plan.zero = largest, plan.zeros = 4 * k->heads;
     float* const delta = reinterpret_cast<float*>(ws + p.at_delta);
     const HeadsOut o = heads_out(*out, dim, tokens);
-    const ones_heads* const five[5] = {dout, v, q, k, out};
-    SurveyArgs d = {};
-    for (int i = 0; i < 5; ++i) d.p[i] = static_cast<const uint16_t*>(five[i]->d_data), d.token[i] = five[i]->token, d.head[i] = five[i]->head;
-    d.plan = plan.head, d.delta = delta, d.largest = largest, d.tokens = tokens, d.heads = q->heads, d.kv = k->heads, d.dim = dim;
-    d.wide = o.wide;
-    NarrowArgs n = {};
-    for (int i = 0; i < 2; ++i)
-        n.p[i] = d.p[2 + i], n.token[i] = d.token[2 + i], n.head[i] = d.head[2 + i], n.out[i] = reinterpret_cast<uint16_t*>(ws + p.at_narrow[i]);
-    n.plan = plan.head, n.largest = largest, n.heads = q->heads, n.kv = k->heads, n.dim = dim, n.row = p.row;
-    const BackArgs a = {nullptr, nullptr, d_lse, delta, largest, heads_out(*dq, dim, tokens), heads_out(*dk, dim, tokens), heads_out(*dv, dim, tokens), tokens,
+    auto vectors = [](const ones_heads& h) { return Vectors{static_cast<const uint16_t*>(h.d_data), h.token, h.head}; };
+    int* const power = reinterpret_cast<int*>(ws + p.at_power);  // guessed, then settled
+    SurveyArgs d = {vectors(*dout), vectors(*out), vectors(*v), vectors(*q), vectors(*k)};
+    for (int i = 0; i < 2; ++i) d.narrow[i] = reinterpret_cast<uint16_t*>(ws + p.at_narrow[i]);
+    d.plan = plan.head, d.delta = delta, d.largest = largest, d.power = power, d.tokens = tokens, d.heads = q->heads, d.kv = k->heads, d.dim = dim;
+    d.row = p.row, d.wide = o.wide;
+    const BackArgs a = {nullptr, nullptr, d_lse, delta, largest, power + 2 * k->heads, heads_out(*dq, dim, tokens), heads_out(*dk, dim, tokens), heads_out(*dv, dim, tokens), tokens,
                         q->heads, k->heads, p.group, p.kt, dim, scale};
     const bool f16 = type == ONES_F16;
     cudaError_t err;
     if (dim > 64)
-        err = f16 ? launch_back<2, true>(*dout, *q, *k, *v, d, n, a, plan, p, stream) : launch_back<2, false>(*dout, *q, *k, *v, d, n, a, plan, p, stream);
+        err = f16 ? launch_back<2, true>(*dout, *q, *k, *v, d, a, plan, p, stream) : launch_back<2, false>(*dout, *q, *k, *v, d, a, plan, p, stream);
     else
-        err = f16 ? launch_back<1, true>(*dout, *q, *k, *v, d, n, a, plan, p, stream) : launch_back<1, false>(*dout, *q, *k, *v, d, n, a, plan, p, stream);
+        err = f16 ? launch_back<1, true>(*dout, *q, *k, *v, d, a, plan, p, stream) : launch_back<1, false>(*dout, *q, *k, *v, d, a, plan, p, stream);
     return err == cudaSuccess ? ONES_OK : ONES_ERR_CUDA;
 }
 

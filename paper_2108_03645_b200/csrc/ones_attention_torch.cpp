@@ -171,7 +171,8 @@ py::object attention_backward(const Tensor& dout, const Tensor& q, const Tensor&
     TORCH_CHECK_VALUE(lse.scalar_type() == at::kFloat && lse.device() == q.device() && lse.sizes() == q.sizes().slice(0, q.dim() - 1) && lse.is_contiguous(),
                       "lse: what attention returned is needed");
     int rc = 0;
-    const Tensor ga = aligned_heads(dout, rc), qa = aligned_heads(q, rc), ka = aligned_heads(k, rc), va = aligned_heads(v, rc), oa = readable(out);
+    const Tensor ga = aligned_heads(dout, rc), qa = aligned_heads(q, rc), ka = aligned_heads(k, rc), va = aligned_heads(v, rc),
+                 oa = aligned_heads(out, rc);  // read faster so, though it need not be
     if (rc) return py::int_(rc);
     Tensor dq = fresh(q.sizes(), q, q.scalar_type()), dk = fresh(k.sizes(), q, q.scalar_type()), dv = fresh(v.sizes(), q, q.scalar_type());
     const size_t nbytes = ones_attention_backward_workspace_bytes(p.tokens, p.sequences, (int)q.size(-2), (int)k.size(-2), (int)q.size(-1));
