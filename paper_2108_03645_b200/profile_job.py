@@ -7,7 +7,9 @@ is the last block and the output head of a language model on synthetic token seq
     x = embedding[token];  h = layer_norm(x + gelu(x W1) W2);  loss = cross entropy of h against the head,
 
 whose step uses the operators of `train` (layer norm, the cross entropy that never keeps the logits, the orthogonalised
-update for the block's two matrices; the plain matrix products are the library's).  `profile` times the step at every
+update for the block's matrices; the plain matrix products are the library's). With `heads` in its shape the block has causal
+attention within each sample before that, x = x + attention(rotated norms of q and k, v) Wo, and with `clip` the gradients are
+scaled down to that norm before the update.  `profile` times the step at every
 batch b0 << k that fits, `fit` turns the times into a and c (one GPU cannot measure d, which is passed in), `job_row` makes
 the row of the job table, and the command
 
@@ -34,6 +36,16 @@ class JobShape:
     vocab: int = 32000
     seq: int = 256          # tokens per sample
     ignored: float = 0.1    # share of tokens without a target
+    heads: int = 0          # query heads of the attention (0: a block without one)
+    kv_heads: int = 0       # key and value heads, a divisor of heads (0: as many)
+    clip: float = 0.0       # largest norm of all gradients together (0: as they are)
+
+    def __post_init__(self):
+        kv = self.kv_heads or self.heads
+        if self.heads < 0 or kv < 0 or (self.heads and (self.width % self.heads or self.heads % kv or self.width // self.heads > 128)):
+            raise ValueError("JobShape: heads have to divide the width into parts of at most 128, and kv_heads the heads")
+        if not self.clip >= 0.0:
+            raise ValueError("JobShape: clip is a norm, or 0")
 
 
 def fit(batches, seconds) -> tuple[float, float]:
@@ -79,7 +91,17 @@ class LanguageModelJob:
         self.head = normal(v, d, std=0.02)
         self.gain = torch.ones(d, device=self.device)
         self.shift = torch.zeros(d, device=self.device)
-        self.momentum = [torch.zeros_like(w, dtype=torch.float32) for w in (self.w1, self.w2)]
+        self.matrices = [self.w1, self.w2]
+        if shape.heads:
+            from . import train
+            self.kv_heads = shape.kv_heads or shape.heads
+            self.head_dim = d // shape.heads
+            self.wqkv = normal(d, (shape.heads + 2 * self.kv_heads) * self.head_dim, std=1 / math.sqrt(d))
+            self.wo = normal(d, d, std=1 / math.sqrt(d))
+            self.q_gain, self.k_gain = (torch.ones(self.head_dim, device=self.device) for _ in range(2))
+            self.frequencies = train.rotary_frequencies(self.head_dim // 2 * 2, device=self.device)
+            self.matrices += [self.wqkv, self.wo]
+        self.momentum = [torch.zeros_like(w, dtype=torch.float32) for w in self.matrices]
 
     def batch(self, samples: int, seed: int):
         """Synthetic sequences: the next token follows from the present one, some have no target."""
@@ -91,11 +113,38 @@ class LanguageModelJob:
         target[torch.rand(n, generator=g, device=self.device) < self.shape.ignored] = -100
         return token, target
 
+    def attend(self, x):
+        """The attention of each sample: (its sum with x, what the gradients need)."""
+        import torch
+        from . import train
+        n, (h, kv, d) = x.shape[0], (self.shape.heads, self.kv_heads, self.head_dim)
+        q, k, v = (x @ self.wqkv).view(n, h + 2 * kv, d).split([h, kv, kv], 1)
+        position = torch.arange(n, device=x.device) % self.shape.seq
+        offsets = torch.arange(0, n + 1, self.shape.seq, device=x.device)
+        qn, kn = train.qk_norm(q, k, position, self.frequencies, self.q_gain, self.k_gain)
+        out, lse = train.attention(qn, kn, v, offsets)
+        return x + out.view(n, -1) @ self.wo, (x, q, k, v, position, offsets, qn, kn, out, lse)
+
+    def attend_backward(self, dy, kept):
+        """Gradients of wqkv, wo, q_gain and k_gain (embeddings are not trained)."""
+        import torch
+        from . import train
+        x, q, k, v, position, offsets, qn, kn, out, lse = kept
+        flat = out.view(x.shape[0], -1)
+        dout = (dy @ self.wo.t()).view_as(out)
+        dqn, dkn, dv = train.attention_backward(dout, qn, kn, v, out, lse, offsets)
+        dq, dk, dqg, dkg = train.qk_norm_backward(dqn, dkn, q, k, position, self.frequencies, self.q_gain, self.k_gain)
+        return x.t() @ torch.cat([dq, dk, dv], 1).view(x.shape[0], -1), flat.t() @ dy, dqg, dkg
+
     def gradients(self, token, target):
-        """(mean loss, gradients of w1, w2, head, gain, shift); the loss is a 0-d tensor, nothing synchronises."""
+        """(mean loss, gradients of w1, w2, head, gain, shift, and with attention of wqkv, wo, q_gain, k_gain); the loss is a 0-d
+        tensor, nothing synchronises."""
         import torch
         from . import train
         x = self.embedding[token]
+        kept = None
+        if self.shape.heads:
+            x, kept = self.attend(x)
         u = x @ self.w1
         act = torch.nn.functional.gelu(u)
         z = x + act @ self.w2
@@ -108,18 +157,27 @@ class LanguageModelJob:
         dw2 = act.t() @ dz
         du = torch.ops.aten.gelu_backward(dz @ self.w2.t(), u)
         dw1 = x.t() @ du
-        return loss.sum() / live, (dw1, dw2, dhead, dgain, dshift)
+        grads = (dw1, dw2, dhead, dgain, dshift)
+        if kept:
+            grads += self.attend_backward(dz + du @ self.w1.t(), kept)
+        return loss.sum() / live, grads
 
     def step(self, token, target, *, lr: float = 0.02, head_lr: float = 20.0, beta: float = 0.9):
         """One training step; returns the mean loss (0-d tensor)."""
         from . import train
-        loss, (dw1, dw2, dhead, dgain, dshift) = self.gradients(token, target)
-        for w, m, dw in zip((self.w1, self.w2), self.momentum, (dw1, dw2)):
+        loss, grads = self.gradients(token, target)
+        if self.shape.clip:
+            train.clip_gradients(grads, self.shape.clip)
+        dw1, dw2, dhead, dgain, dshift, *attention = grads
+        for w, m, dw in zip(self.matrices, self.momentum, (dw1, dw2, *attention[:2])):
             m.mul_(beta).add_(dw)
             w.sub_(train.orthogonalize(m), alpha=lr * math.sqrt(max(1.0, w.shape[0] / w.shape[1])))
         self.head.sub_(dhead, alpha=head_lr)
         self.gain.sub_(dgain, alpha=lr)
         self.shift.sub_(dshift, alpha=lr)
+        if attention:
+            self.q_gain.sub_(attention[2], alpha=lr)
+            self.k_gain.sub_(attention[3], alpha=lr)
         return loss
 
 
@@ -158,13 +216,17 @@ def main(argv=None) -> dict:
     ap.add_argument("--width", type=int, default=JobShape.width)
     ap.add_argument("--vocab", type=int, default=JobShape.vocab)
     ap.add_argument("--seq", type=int, default=JobShape.seq)
+    ap.add_argument("--heads", type=int, default=0, help="query heads of the block's attention (default: a block without one)")
+    ap.add_argument("--kv-heads", type=int, default=0, help="key and value heads (default: as many)")
+    ap.add_argument("--clip", type=float, default=0.0, help="largest norm of all gradients together (default: as they are)")
     ap.add_argument("--generations", type=int, default=50)
     a = ap.parse_args(argv)
     from . import binding, inputs
 
     most = a.max_per_gpu or a.b0 << a.kmax
     batches = [a.b0 << k for k in range(a.kmax + 1) if a.b0 << k <= most]
-    job = LanguageModelJob(JobShape(width=a.width, inner=4 * a.width, vocab=a.vocab, seq=a.seq))
+    job = LanguageModelJob(JobShape(width=a.width, inner=4 * a.width, vocab=a.vocab, seq=a.seq, heads=a.heads, kv_heads=a.kv_heads,
+                                    clip=a.clip))
     seconds = profile(job, batches)
     fa, fc = fit(batches, seconds)
     w = inputs.paper_scale()
