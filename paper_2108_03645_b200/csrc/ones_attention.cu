@@ -472,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (tile_top == -INFINITY) tile_top = j ? m_row : 0.f;
                 if (j == 0) {
                     m_row = tile_top;
-                } else if (__any_sync(0xFFFFFFFFu, (tile_top - m_row) * c > kGrow)) {
+                } else if (__any_sync(0xFFFFFFFFu, live && (tile_top - m_row) * c > kGrow)) {  // rows that are not there have no say
                     const float next = fmaxf(m_row, tile_top), f = exp2_of((m_row - next) * c);
                     m_row = next;
                     sum = sum * both(f);

@@ -321,6 +321,26 @@ def test_attention_sequences_do_not_reach_each_other():
                     assert torch.equal(a[keep], b[keep])
 
 
+@pytest.mark.parametrize("heads, kv, dim", [(3, 1, 64), (4, 2, 128), (5, 1, 128), (7, 1, 64), (15, 3, 77)])
+def test_attention_rows_that_are_not_there_have_no_say(heads, kv, dim):
+    """Sequences whose rows share a tile with rows of the next one, which is NaN or large, or with none: the output's bits are theirs alone."""
+    from paper_2108_03645_b200 import train
+    lengths = [70, 300, 5, 331, 129]
+    offsets = torch.tensor([0] + lengths).cumsum(0).cuda()
+    q, k, v = (3 * t for t in qkv(lengths, heads, kv, dim, BF16, pack=False))
+    want = train.attention(q, k, v, offsets)
+    for value in (float("nan"), 1e4, -1e4):
+        for sequence in range(5):
+            rows = slice(int(offsets[sequence]), int(offsets[sequence + 1]))
+            args = [t.clone() for t in (q, k, v)]
+            for t in args:
+                t[rows] = value
+            keep = torch.ones(sum(lengths), dtype=torch.bool, device="cuda")
+            keep[rows] = False
+            for a, b in zip(train.attention(*args, offsets), want):
+                assert torch.equal(a[keep], b[keep])
+
+
 def test_attention_dense_batches_and_offsets_agree():
     from paper_2108_03645_b200 import train
     q, k, v = (randn(3, 150, h, 64, seed=h).bfloat16() for h in (4, 2, 2))
