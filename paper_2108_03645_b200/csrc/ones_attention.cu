@@ -177,7 +177,7 @@ __device__ __forceinline__ QueryTile query_tile(const Work& it, int which, int k
     return q;
 }
 
-template <int HALVES, bool F16>
+template <int HALVES, bool F16, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 1)
     k_attention(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                 const ForwardArgs g) {
@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     };
 
     if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
         if (warp == 8) {
             // load: keys and values in turn, each lane's queries before the first of them
             uint32_t n = 0, items[2] = {0, 0};
@@ -387,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
         const int which = warp / 4, row = threadIdx.x % 128;
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;
         const uint32_t ts = tmem + 128 * which + lanes, to = tmem + 256 + 128 * which + lanes;
@@ -411,7 +411,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 uint32_t o[32];
                 tmem_fetch(to + 64 * set.at + 32 * x, o);
                 tmem_wait(o);
-                out.write<F16>(32 * x, g.dim, g.out.wide, o, inv, stage);
+                out.write<F16, WIDE>(32 * x, g.dim, o, inv, stage);
             }
             mma_fence_before();
             __syncwarp();
@@ -615,9 +615,9 @@ cudaError_t launch_forward(const ones_heads& q, const ones_heads& k, const ones_
     if (err == cudaSuccess) err = make_heads_map(&mk, k, a.dim, a.tokens, 1, kKeys, F16);
     if (err == cudaSuccess) err = make_heads_map(&mv, v, a.dim, a.tokens, 1, kKeys, F16);
     if (err != cudaSuccess) return err;
-    auto kernel = k_attention<HALVES, F16>;
-    static std::atomic<uint64_t> ready{0};
-    err = allow_smem(kernel, Forward<HALVES>::kSmem, ready);
+    auto kernel = a.out.wide ? k_attention<HALVES, F16, true> : k_attention<HALVES, F16, false>;
+    static std::atomic<uint64_t> ready[2];
+    err = allow_smem(kernel, Forward<HALVES>::kSmem, ready[a.out.wide != 0]);
     if (err != cudaSuccess) return err;
     cudaLaunchConfig_t cfg = {};
     const int64_t work = most * a.kv, slots = device_sms();

@@ -215,9 +215,9 @@ struct RowsOut {
 #pragma unroll
         for (int i = 0; i < 4; ++i) to[i] = __shfl_sync(0xFFFFFFFFu, own, (threadIdx.x & 28) + i);
     }
-    // wide: rows start on 16-byte boundaries and have a multiple of 8 columns
-    template <bool F16>
-    __device__ __forceinline__ void write(int c, int dim, bool wide, const uint32_t (&o)[32], float factor, uint8_t* stage) const {
+    // WIDE: rows start on 16-byte boundaries and have a multiple of 8 columns
+    template <bool F16, bool WIDE>
+    __device__ __forceinline__ void write(int c, int dim, const uint32_t (&o)[32], float factor, uint8_t* stage) const {
         uint32_t w[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -225,7 +225,7 @@ struct RowsOut {
             w[i] = pack16<F16>(f.x, f.y);
         }
         const int lane = threadIdx.x % 32;
-        if (wide) {
+        if constexpr (WIDE) {
             const int at = c + 8 * (lane % 4);
             if (stage) {
                 uint4* const s = reinterpret_cast<uint4*>(stage);

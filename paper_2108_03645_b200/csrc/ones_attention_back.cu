@@ -17,6 +17,8 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 namespace ones {
 
 namespace {
@@ -285,7 +287,7 @@ __device__ __forceinline__ int key_tiles(const Work& it, int kt) {
     return it.begin < 0 ? 0 : (min(it.first + kt, it.end) - 1 - it.begin) / kKeys + 1;
 }
 
-template <int HALVES, bool F16>
+template <int HALVES, bool F16, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 1)
     k_attention_queries(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_do,
                         const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const BackArgs g) {
@@ -471,7 +473,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 uint32_t o[32];
                 tmem_fetch(t_acc + 64 * set.at + col + lanes, o);
                 tmem_wait(o);
-                out.write<F16>(col, g.dim, g.dq.wide, o, factor, stage);
+                out.write<F16, WIDE>(col, g.dim, o, factor, stage);
             }
             mma_fence_before();
             __syncwarp();
@@ -631,7 +633,7 @@ __device__ __forceinline__ QuerySpan query_span(const Work& it, int kt) {
     return {it.begin + f * kt, (it.end - it.begin + kt - 1) / kt - f};
 }
 
-template <int HALVES, bool F16>
+template <int HALVES, bool F16, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 1)
     k_attention_keys(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_do,
                      const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const BackArgs g) {
@@ -837,7 +839,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         RowsOut out = {};
         float factor = 0.f;
         bool pending = false;
-        const bool wide = half ? g.dk.wide : g.dv.wide;
         auto write = [&](uint32_t item) {
             const Set set(item);
             if (!warp_wait(acc_full + 8 * set.at, set.parity)) return false;
@@ -848,7 +849,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 uint32_t a[32];
                 tmem_fetch((half ? t_dk : t_dv) + 64 * set.at + 32 * x + lanes, a);
                 tmem_wait(a);
-                out.write<F16>(32 * x, g.dim, wide, a, factor, stage);
+                out.write<F16, WIDE>(32 * x, g.dim, a, factor, stage);
             }
             mma_fence_before();
             __syncwarp();
@@ -998,7 +999,7 @@ cudaError_t launch_pass(K kernel, int smem, std::atomic<uint64_t>& ready, int64_
     return cudaLaunchKernelEx(&cfg, kernel, maps[0], maps[1], maps[2], maps[3], a);
 }
 
-template <int HALVES, bool F16>
+template <int HALVES, bool F16, bool WIDE>
 cudaError_t launch_back(const ones_heads& dout, const ones_heads& q, const ones_heads& k, const ones_heads& v, const SurveyArgs& d, BackArgs a,
                         const PlanArgs& plan, const BackPlan& p, cudaStream_t stream) {
     constexpr int kLanes = 8 * HALVES;
@@ -1023,10 +1024,10 @@ cudaError_t launch_back(const ones_heads& dout, const ones_heads& q, const ones_
     if (err != cudaSuccess) return err;
     static std::atomic<uint64_t> ready[2];
     a.items = plan.items[0], a.head = plan.head;
-    err = launch_pass(k_attention_queries<HALVES, F16>, Back<HALVES>::kSmemQueries, ready[0], p.most[0] * a.kv, stream, maps, a);
+    err = launch_pass(k_attention_queries<HALVES, F16, WIDE>, Back<HALVES>::kSmemQueries, ready[0], p.most[0] * a.kv, stream, maps, a);
     if (err != cudaSuccess) return err;
     a.items = plan.items[1], a.head = plan.head + 1;
-    return launch_pass(k_attention_keys<HALVES, F16>, Back<HALVES>::kSmemKeys, ready[1], p.most[1] * a.kv, stream, maps, a);
+    return launch_pass(k_attention_keys<HALVES, F16, WIDE>, Back<HALVES>::kSmemKeys, ready[1], p.most[1] * a.kv, stream, maps, a);
 }
 
 }  // namespace
@@ -1079,10 +1080,13 @@ int ones_attention_backward(const ones_heads* dout, const ones_heads* q, const o
                         q->heads, k->heads, p.group, p.kt, dim, scale};
     const bool f16 = type == ONES_F16;
     cudaError_t err;
-    if (dim > 64)
-        err = f16 ? launch_back<2, true>(*dout, *q, *k, *v, d, a, plan, p, stream) : launch_back<2, false>(*dout, *q, *k, *v, d, a, plan, p, stream);
-    else
-        err = f16 ? launch_back<1, true>(*dout, *q, *k, *v, d, a, plan, p, stream) : launch_back<1, false>(*dout, *q, *k, *v, d, a, plan, p, stream);
+    auto launch = [&](auto narrow) {
+        constexpr int H = decltype(narrow)::value;
+        if (a.dq.wide && a.dk.wide && a.dv.wide)
+            return f16 ? launch_back<H, true, true>(*dout, *q, *k, *v, d, a, plan, p, stream) : launch_back<H, false, true>(*dout, *q, *k, *v, d, a, plan, p, stream);
+        return f16 ? launch_back<H, true, false>(*dout, *q, *k, *v, d, a, plan, p, stream) : launch_back<H, false, false>(*dout, *q, *k, *v, d, a, plan, p, stream);
+    };
+    err = dim > 64 ? launch(std::integral_constant<int, 2>{}) : launch(std::integral_constant<int, 1>{});
     return err == cudaSuccess ? ONES_OK : ONES_ERR_CUDA;
 }
 
