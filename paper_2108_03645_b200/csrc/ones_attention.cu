@@ -18,6 +18,7 @@ namespace {
 
 constexpr int kPlanThreads = 1024;
 constexpr int kBins = 1024;
+constexpr int kNear = 2047;  // so many sequences' bounds stay in shared memory: looked up in global memory they took 4 of 7 us
 
 __device__ __forceinline__ int block_scan(int v, int* sums, bool is_max) {  // inclusive; sums[32]
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
@@ -47,9 +48,12 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const PlanArgs a) {
     __shared__ int sums[32];
     __shared__ int bins[kBins];
     __shared__ int s_total;
-    const int list = blockIdx.x, step = a.step[list];
-    int* prefix = a.prefix[list];
-    int* start = a.start + (int64_t)list * (a.sequences + 1);
+    __shared__ int s_start[kNear + 1], s_prefix[kNear + 1];
+    const int list = blockIdx.x, step = list ? a.step[1] : a.step[0], per = list ? a.tile[1] : a.tile[0];
+    const bool near = a.sequences <= kNear;
+    int* const prefix = near ? s_prefix : list ? a.prefix[1] : a.prefix[0];
+    int* const start = near ? s_start : a.start + (int64_t)list * (a.sequences + 1);
+    Item* const items = list ? a.items[1] : a.items[0];
     wait_for_predecessor();
     let_successor_start();
     if (list == 0)
@@ -88,26 +92,28 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const PlanArgs a) {
     // items of tokens before the first and behind the last sequence: at the end of the list
     const int n_front = (front + step - 1) / step, n_back = (a.tokens - back + step - 1) / step;
     int shift = 0;
-    while ((a.tokens / a.tile[list] + 1) >> shift >= kBins) ++shift;
+    while ((a.tokens / per + 1) >> shift >= kBins) ++shift;
+    Item it = {};
+    int bin = 0;
     for (int pass = 0; pass < 2; ++pass) {
         for (int i = threadIdx.x; i < total; i += kPlanThreads) {
-            int lo = 0, hi = a.sequences;  // the last sequence with prefix <= i
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) / 2;
-                if (prefix[mid] <= i)
-                    lo = mid;
-                else
-                    hi = mid;
+            if (!pass || total > kPlanThreads) {
+                int lo = 0, hi = a.sequences;  // the last sequence with prefix <= i
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) / 2;
+                    if (prefix[mid] <= i)
+                        lo = mid;
+                    else
+                        hi = mid;
+                }
+                it.begin = start[lo], it.end = start[lo + 1];
+                it.first = it.begin + (i - prefix[lo]) * step;
+                // queries: the keys up to their last one; keys: the queries from their first one on
+                it.cost = ((list == 0 ? min(it.first + step, it.end) - it.begin : it.end - it.first) + per - 1) / per;
+                bin = kBins - 1 - min(it.cost >> shift, kBins - 1);
             }
-            Item it;
-            it.begin = start[lo], it.end = start[lo + 1];
-            it.first = it.begin + (i - prefix[lo]) * step;
-            // queries: the keys up to their last one; keys: the queries from their first one on
-            it.cost = list == 0 ? (min(it.first + step, it.end) - it.begin + a.tile[0] - 1) / a.tile[0]
-                                : (it.end - it.first + a.tile[1] - 1) / a.tile[1];
-            const int bin = kBins - 1 - min(it.cost >> shift, kBins - 1);
             const int at = atomicAdd(&bins[bin], 1);
-            if (pass) a.items[list][at] = it;
+            if (pass) items[at] = it;
         }
         __syncthreads();
         if (!pass) {
@@ -117,11 +123,10 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const PlanArgs a) {
         }
     }
     for (int i = threadIdx.x; i < n_front + n_back; i += kPlanThreads) {
-        Item it;
         it.begin = -1, it.cost = 0;
         it.first = i < n_front ? i * step : back + (i - n_front) * step;
         it.end = min(it.first + step, i < n_front ? front : a.tokens);
-        a.items[list][total + i] = it;
+        items[total + i] = it;
     }
     if (threadIdx.x == 0) {
         PlanHead h = {};
