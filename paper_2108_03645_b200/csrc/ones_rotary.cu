@@ -205,9 +205,9 @@ __device__ __forceinline__ float inverse_root(float ss, const Args& g) {
 constexpr int kWeightRow = ONES_QK_NORM_MAX_DIM + 16;
 
 // U units per lane: 1 where pieces of 16 bytes are possible, more for single values. The next vector of a group is on its way
-// while the present one is worked on; four blocks (backward: two) on an SM hide the rest.
+// while the present one is worked on; five blocks (backward: two) on an SM hide the rest.
 template <class T, int V, int U, bool INTER, bool BACK>
-__global__ void __launch_bounds__(kThreads, BACK ? 2 : 4) k_qk_norm(const __grid_constant__ Args g) {
+__global__ void __launch_bounds__(kThreads, BACK ? 2 : 5) k_qk_norm(const __grid_constant__ Args g) {
     extern __shared__ float smem[];
     __shared__ __align__(16) float s_weight[2][kWeightRow];
     const int lanes = 1 << g.group_log, groups = kThreads >> g.group_log;
@@ -369,10 +369,10 @@ cudaError_t launch(Args& a, bool back, cudaStream_t stream, int* blocks) {
     a.group_log = 0;
     while ((1 << a.group_log) * U < units) ++a.group_log;
     const int groups = kThreads >> a.group_log, heads = max(1, a.side[0].heads + a.side[1].heads);
-    // Tokens of a block at a time: enough vectors for four rounds of all groups (backward, where a block has many tiles: eight), at most
-    // 16, and fewer where that leaves SMs idle.
-    a.tile = max(1, min(16, (back ? 8 : 4) * groups / heads));
-    while (a.tile > 1 && (a.tokens + a.tile - 1) / a.tile < 4 * device_sms()) a.tile = (a.tile + 1) / 2;
+    // Tokens of a block at a time: enough vectors for sixteen rounds of all groups, so that the angles and the barriers around them
+    // weigh little (65536 x 40 x 128 forward: four rounds 305 us, eight 274, sixteen 242), and fewer where that leaves SMs idle.
+    a.tile = max(1, min(64, 16 * groups / heads));
+    while (a.tile > 1 && (a.tokens + a.tile - 1) / a.tile < 5 * device_sms()) a.tile = (a.tile + 1) / 2;
     a.angles = (a.rotary / 2 + 3) / 4 * 4;
     const int tiles = (a.tokens + a.tile - 1) / a.tile;
     *blocks = back ? min(tiles, kMaxBlocks) : tiles;
