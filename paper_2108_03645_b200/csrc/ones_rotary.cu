@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(kThreads, BACK ? 2 : 5) k_qk_norm(const __grid
     Unit unit[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) unit[u] = unit_at<V, INTER>(g, lane + u * lanes);
-    const int tiles = (g.tokens + g.tile - 1) / g.tile;
+    const int tiles = (g.tokens - 1) / g.tile + 1;
     for (int i = threadIdx.x; i < 2 * kWeightRow; i += kThreads) {
         const int which = i >= kWeightRow, c = i - which * kWeightRow;
         const void* p = g.side[which].weight;
@@ -371,10 +371,11 @@ cudaError_t launch(Args& a, bool back, cudaStream_t stream, int* blocks) {
     const int groups = kThreads >> a.group_log, heads = max(1, a.side[0].heads + a.side[1].heads);
     // Tokens of a block at a time: enough vectors for sixteen rounds of all groups, so that the angles and the barriers around them
     // weigh little (65536 x 40 x 128 forward: four rounds 305 us, eight 274, sixteen 242), and fewer where that leaves SMs idle.
-    a.tile = max(1, min(64, 16 * groups / heads));
-    while (a.tile > 1 && (a.tokens + a.tile - 1) / a.tile < 5 * device_sms()) a.tile = (a.tile + 1) / 2;
+    // Their angles take 32 KB at most, so that five blocks are on an SM.
     a.angles = (a.rotary / 2 + 3) / 4 * 4;
-    const int tiles = (a.tokens + a.tile - 1) / a.tile;
+    a.tile = max(1, min(min(64, 16 * groups / heads), 4096 / max(a.angles, 1)));
+    while (a.tile > 1 && (a.tokens - 1) / a.tile + 1 < 5 * device_sms()) a.tile = (a.tile + 1) / 2;
+    const int tiles = (a.tokens - 1) / a.tile + 1;
     *blocks = back ? min(tiles, kMaxBlocks) : tiles;
     const int smem = max(2 * a.tile * a.angles, back && a.part ? groups * a.dim : 0) * 4;
     auto kernel = back ? k_qk_norm<T, V, U, INTER, true> : k_qk_norm<T, V, U, INTER, false>;

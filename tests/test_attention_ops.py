@@ -109,6 +109,16 @@ def test_qk_norm(dtype, tokens, heads, kv, dim, rotary, interleaved, wtype):
     check_qk_norm(q, k, pos, train.rotary_frequencies(rotary), qw, kw, dq, dk, interleaved=interleaved)
 
 
+@pytest.mark.parametrize("dtype, heads, kv, dim, rotary", [(BF16, 1, 1, 256, 256), (BF16, 2, 2, 192, 192), (F32, 1, 0, 256, 256), (F16, 2, 1, 255, 254)])
+def test_qk_norm_many_tokens_of_few_heads(dtype, heads, kv, dim, rotary):
+    """Blocks take as many tokens at a time as the room for their angles allows."""
+    from paper_2108_03645_b200 import train
+    n = 50000
+    q, k = randn(n, heads, dim).to(dtype), randn(n, kv, dim, seed=1).to(dtype)
+    freq, w = train.rotary_frequencies(rotary), 1 + 0.2 * randn(dim, seed=3)
+    check_qk_norm(q, k, torch.arange(n, device="cuda"), freq, w, w, randn(n, heads, dim, seed=5).to(dtype), randn(n, kv, dim, seed=6).to(dtype))
+
+
 def test_qk_norm_at_far_positions_and_back():
     """Angles of 2^40 radians keep what 64 bits hold of them; negative positions turn the other way."""
     from paper_2108_03645_b200 import train
