@@ -18,7 +18,7 @@ ones_heads heads_of(const Tensor& t) {
 bool plain(const Tensor& t) {
     return (t.stride(2) == 1 || t.size(2) == 1) && (t.size(1) == 1 || t.stride(1) >= t.size(2)) && (t.size(0) == 1 || t.stride(0) >= 1);
 }
-Tensor flat(const Tensor& t) { return t.dim() == 3 ? t : t.reshape({-1, t.size(-2), t.size(-1)}); }
+Tensor flat(const Tensor& t) { return t.dim() == 3 ? t : t.flatten(0, t.dim() - 3); }
 Tensor readable(const Tensor& t) {
     const Tensor f = flat(t);
     return f.numel() == 0 || plain(f) ? f : f.contiguous();

@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(1024) k_join_weights(const float* part, int bl
 int size_of(int type) { return type == ONES_F32 ? 4 : 2; }
 
 bool bad_heads(const ones_heads& h, int dim, int tokens) {
-    return h.heads < 0 || h.heads > ONES_MAX_HEADS || h.head < dim || (h.token < 0 && tokens > 1);
+    return h.heads < 0 || h.heads > ONES_MAX_HEADS || (h.heads > 1 && h.head < dim) || (h.token < 0 && tokens > 1);
 }
 
 template <class T, int V, int U, bool INTER>

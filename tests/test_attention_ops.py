@@ -154,6 +154,21 @@ def test_qk_norm_shapes_zeros_and_no_tokens():
     assert not bool(dw.any())
 
 
+def test_qk_norm_one_head_or_none():
+    """A single head's distance to the next does not matter, and one side may have no heads."""
+    from paper_2108_03645_b200 import train
+    freq, pos = train.rotary_frequencies(32), torch.arange(10, device="cuda").view(2, 5)
+    q, k = randn(2, 5, 1, 32), randn(2, 5, 3, 32, seed=1)
+    want = train.qk_norm(q, k, pos, freq)
+    odd = q.as_strided((2, 5, 1, 32), (160, 32, 1, 1))
+    assert torch.equal(train.qk_norm(odd, k, pos, freq)[0], want[0])
+    for x in train.qk_norm_backward(odd, k, odd, k, pos, freq), train.qk_norm_backward(q, k, q, k, pos, freq):
+        assert torch.equal(x[0], train.qk_norm_backward(q, k, q, k, pos, freq)[0])
+    none = train.qk_norm(q[:, :, :0], k, pos, freq)
+    assert none[0].shape == (2, 5, 0, 32) and torch.equal(none[1], want[1])
+    assert torch.equal(train.qk_norm(q, k[:, :, :0], pos, freq)[0], want[0])
+
+
 def test_qk_norm_keeps_what_is_not_finite_in_its_vector():
     from paper_2108_03645_b200 import train
     q, k = randn(9, 4, 64).half(), randn(9, 2, 64, seed=1).half()

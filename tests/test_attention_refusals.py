@@ -105,6 +105,17 @@ def test_attention_backward_refuses(change, want):
     assert _lib().ones_attention_backward(*_change(a, change)) == want
 
 
+def test_attention_refuses_more_work_than_is_counted():
+    """Tiles of tokens times heads of the keys are counted in 31 bits."""
+    L = _lib()
+    many, few = _heads(token=1024 * 64, heads=1024), _heads(token=1024 * 64, heads=512)
+    n = (1 << 30) - 1
+    for h in (many, few):
+        a = [C.byref(h)] * 3
+        assert L.ones_attention(*a, P, n, 1, 64, 0.125, 1, C.byref(h), P, P, 1 << 62, None) == PARAM
+        assert L.ones_attention_backward(*a, C.byref(h), C.byref(h), P, P, n, 1, 64, 0.125, 1, *a, P, 1 << 62, None) == PARAM
+
+
 def _list(values, kind):
     return (kind * max(len(values), 1))(*values)
 
