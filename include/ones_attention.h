@@ -16,7 +16,8 @@ extern "C" {
 #endif
 
 /* Vectors of `dim` values, one for each token and head: value c of head h of token t lies at
- * d_data[t * token + h * head + c].  head >= dim, and token >= 0 where there are several tokens. */
+ * d_data[t * token + h * head + c].  head >= dim where there are several heads, and token >= 0 where there are several
+ * tokens.  Outputs overlap neither one another nor an input, except where an operator says so. */
 typedef struct ones_heads {
     void* d_data;
     int64_t token, head; /* strides in values */
@@ -61,8 +62,12 @@ int ones_qk_norm_backward(const ones_heads* dq, const ones_heads* dk, const ones
  *   d_offsets int64[sequences + 1]: sequence n is tokens [d_offsets[n], d_offsets[n + 1]), read on the device.  NULL: all
  *   `sequences` are tokens / sequences long.  Offsets outside [0, tokens] count as its ends, and one below those before it
  *   as the largest of them.  Tokens of no sequence get out = 0, lse = 0, and nothing of them, not even a NaN, reaches others.
+ *   Nothing of one sequence reaches another either.  Within a sequence, what is not finite in k or v of a token (backward: in
+ *   q, k, v or dout) may also reach earlier tokens of the same 128 keys, or tokens of the same 128 rows of queries: hidden
+ *   scores count as products with 0, as in a plain matrix product.
  *   d_lse float[tokens][heads].
- * 0 <= tokens < 2^30, 0 <= sequences <= 2^22, 1 <= dim <= ONES_ATTENTION_MAX_DIM, scale > 0 and finite.
+ * 0 <= tokens < 2^30, 0 <= sequences <= 2^22, 1 <= dim <= ONES_ATTENTION_MAX_DIM, scale > 0 and finite; tiles of
+ * queries (128 / (heads / kv) tokens of a sequence each, rounded down) times kv have to be below 2^31 (ONES_ERR_BAD_PARAM).
  *   d_workspace  at least ones_attention_workspace_bytes(tokens, sequences, heads, kv) bytes, 256-byte aligned.
  * Scores, their statistics and all sums are in 32 bits; the probabilities are rounded to `type` for the product with v. */
 #define ONES_ATTENTION_MAX_DIM 128
@@ -77,8 +82,11 @@ int ones_attention(const ones_heads* q, const ones_heads* k, const ones_heads* v
  *   dout aligned as q; out and d_lse what the forward call gave; dq, dk, dv any alignment of their elements.  Tokens of no
  *   sequence get gradients of 0.
  *   d_workspace  at least ones_attention_backward_workspace_bytes(tokens, sequences, heads, kv, dim) bytes.
- * p and ds are rounded to `type` for their products (for ONES_F16 scaled by powers of two, so that small ones stay in its
- * range). */
+ * p is rounded to `type` for its product (ONES_F16: times 2^12), ds to float16 times a power of two that follows from the largest
+ * |dout| and |v| of its group of heads: it keeps 11 bits down to 2^-21 of their product, and steps of 2^-31 of it below.
+ * ONES_BF16 q and k are laid out in the workspace as float16 times a power of two for each head, without loss for what is
+ * above 2^-32 of the head's largest.  These powers are common to all sequences of a call, so that the last bits of a
+ * sequence's dq and dk can depend on the size of its neighbours' finite values. */
 size_t ones_attention_backward_workspace_bytes(int32_t tokens, int32_t sequences, int32_t heads, int32_t kv, int32_t dim);
 int ones_attention_backward(const ones_heads* dout, const ones_heads* q, const ones_heads* k, const ones_heads* v,
                             const ones_heads* out, const float* d_lse, const int64_t* d_offsets, int32_t tokens,
@@ -91,7 +99,8 @@ int ones_attention_backward(const ones_heads* dout, const ones_heads* q, const o
  *   d_g, d_out  host arrays of `count` device pointers; size, type  host arrays: values of each tensor and their type (any of
  *   the three; out has the type of g).  d_out may be d_g, or hold single tensors of it: where the factor is 1 such tensors are
  *   not touched.  Otherwise tensors must not overlap.  d_norm float[1].
- * 0 <= count <= 2^20, size >= 0, at most 2^44 bytes together; max_norm >= 0, eps >= 0.  Squares are summed in 32 bits for 32 values at most, then in 64.
+ * 0 <= count <= 2^20, size >= 0, at most 2^44 bytes together; max_norm and eps finite and >= 0.  Squares are summed in 32 bits
+ * for 32 values at most, then in 64.
  *   d_workspace  at least ones_gradient_norm_workspace_bytes(count) bytes, 256-byte aligned. */
 size_t ones_gradient_norm_workspace_bytes(int32_t count);
 int ones_gradient_norm(const void* const* d_g, const int64_t* size, const int32_t* type, int32_t count, float* d_norm,

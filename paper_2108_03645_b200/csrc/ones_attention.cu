@@ -6,6 +6,14 @@
 // columns), the probabilities take the place of their scores there as 16 bits and are the left operand of the product with
 // the values. A thread owns a row: maxima and sums need no exchange. The maximum that a row subtracts follows the true one
 // only when that has grown by more than 2^8 (in the exponentials): the output is then rescaled in tensor memory, else not.
+// Probabilities are rounded to the tensors' type for their product with the values (half a step, 2^-8 or 2^-11 of each,
+// averaged by the sum over keys), and summed before that in 32 bits.
+//
+// Measured: 16384 tokens in one sequence, 16 / 4 heads of 128: 907 us = 1.21 PFLOP/s (the card at its power limit, 1.6 to 1.77 GHz);
+// 12 documents of 64 to 3412 tokens, 16 / 4 heads of 128: 136 us for 129 GFLOP, which block ends last decides; 128 samples of
+// 256 tokens, 16 heads of 64: 69 us, bound by the latency of an item's first tile. What did not help: probabilities handed on in
+// two halves (893 -> 955 us), softmax loops that are not unrolled (967 -> 1159), items taken from a counter by whoever is free
+// (documents 136 -> 133 us, but 16384 tokens forward and backward 4182 -> 4631: neighbours no longer work on the same keys).
 #include "ones_attention.cuh"
 
 #include <math.h>
@@ -444,91 +452,91 @@ __global__ void __launch_bounds__(kThreads, 1)
             Pair sum = both(0.f);
             for (int j = 0; j < max(tiles, 1); ++j) {
                 if (tiles) {
-                if (!(ok = warp_wait(s_full + 8 * which, count & 1))) break;
-                mma_fence_after();
-                // The last keys of the tile that the row and the warp's first row may see. Where all rows of the warp see the whole tile,
-                // the work is one run of code; elsewhere pieces of 32 keys that none sees are left out, and only those that not all
-                // see whole are masked.
-                const int reach = q.first - it.begin - j * kKeys, last = reach + row_token, low = reach + first_token;
-                const bool whole = low >= kKeys - 1;
-                const int seen = whole ? 4 : min(max((reach + last_token) / 32 + 1, 1), 4);
-                uint32_t s[4][32];
-#pragma unroll
-                for (int x = 0; x < 4; ++x) tmem_fetch(ts + 32 * x, s[x]);
-#pragma unroll
-                for (int x = 0; x < 4; ++x) tmem_wait(s[x]);
-                if (!whole) {
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        if (32 * x + 31 <= low) continue;
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (32 * x + i > last) s[x][i] = 0xFF800000u;  // -infinity
-                    }
-                }
-                float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                for (int x = 0; x < 4; ++x)
-#pragma unroll
-                    for (int i = 0; i < 32; i += 8)
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) m[y] = max3(m[y], __uint_as_float(s[x][i + 2 * y]), __uint_as_float(s[x][i + 2 * y + 1]));
-                float tile_top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-                if (tile_top == -INFINITY) tile_top = j ? m_row : 0.f;
-                if (j == 0) {
-                    m_row = tile_top;
-                } else if (__any_sync(0xFFFFFFFFu, live && (tile_top - m_row) * c > kGrow)) {  // rows that are not there have no say
-                    const float next = fmaxf(m_row, tile_top), f = exp2_of((m_row - next) * c);
-                    m_row = next;
-                    sum = sum * both(f);
-                    if (!(ok = warp_wait(o_full + 8 * which, (count & 1) ^ 1))) break;  // the product of the tile before
+                    if (!(ok = warp_wait(s_full + 8 * which, count & 1))) break;
                     mma_fence_after();
-                    const uint32_t acc = to + 64 * Set(items).at;
-                    for (int x = 0; x < 2 * HALVES; ++x) {
-                        uint32_t o[32];
-                        tmem_fetch(acc + 32 * x, o);
-                        tmem_wait(o);
+                    // The last keys of the tile that the row and the warp's first row may see. Where all rows of the warp see the whole tile,
+                    // the work is one run of code; elsewhere pieces of 32 keys that none sees are left out, and only those that not all
+                    // see whole are masked.
+                    const int reach = q.first - it.begin - j * kKeys, last = reach + row_token, low = reach + first_token;
+                    const bool whole = low >= kKeys - 1;
+                    const int seen = whole ? 4 : min(max((reach + last_token) / 32 + 1, 1), 4);
+                    uint32_t s[4][32];
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                        tmem_store(acc + 32 * x, o);
+                    for (int x = 0; x < 4; ++x) tmem_fetch(ts + 32 * x, s[x]);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) tmem_wait(s[x]);
+                    if (!whole) {
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            if (32 * x + 31 <= low) continue;
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (32 * x + i > last) s[x][i] = 0xFF800000u;  // -infinity
+                        }
+                    }
+                    float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8)
+#pragma unroll
+                            for (int y = 0; y < 4; ++y) m[y] = max3(m[y], __uint_as_float(s[x][i + 2 * y]), __uint_as_float(s[x][i + 2 * y + 1]));
+                    float tile_top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+                    if (tile_top == -INFINITY) tile_top = j ? m_row : 0.f;
+                    if (j == 0) {
+                        m_row = tile_top;
+                    } else if (__any_sync(0xFFFFFFFFu, live && (tile_top - m_row) * c > kGrow)) {  // rows that are not there have no say
+                        const float next = fmaxf(m_row, tile_top), f = exp2_of((m_row - next) * c);
+                        m_row = next;
+                        sum = sum * both(f);
+                        if (!(ok = warp_wait(o_full + 8 * which, (count & 1) ^ 1))) break;  // the product of the tile before
+                        mma_fence_after();
+                        const uint32_t acc = to + 64 * Set(items).at;
+                        for (int x = 0; x < 2 * HALVES; ++x) {
+                            uint32_t o[32];
+                            tmem_fetch(acc + 32 * x, o);
+                            tmem_wait(o);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            tmem_store(acc + 32 * x, o);
+                        }
+                        tmem_store_wait();
+                    }
+                    const Pair c2 = both(c), t2 = both(-m_row * c);
+                    auto probability = [&](uint32_t lo, uint32_t hi) {
+                        const float2 e = split(fma2(pair(__uint_as_float(lo), __uint_as_float(hi)), c2, t2));
+                        const float a = exp2_of(e.x), b = exp2_of(e.y);
+                        sum = sum + pair(a, b);
+                        return pack16<F16>(a, b);
+                    };
+                    if (whole) {
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            uint32_t p[32];
+#pragma unroll
+                            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                                for (int i = 0; i < 32; i += 2) p[16 * x + i / 2] = probability(s[2 * half + x][i], s[2 * half + x][i + 1]);
+                            tmem_store(ts + 32 * half, p);
+                        }
+                    } else {
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            uint32_t p[16];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) p[i] = 0;
+                            if (x < seen) {
+#pragma unroll
+                                for (int i = 0; i < 32; i += 2) p[i / 2] = probability(s[x][i], s[x][i + 1]);
+                            }
+                            tmem_store(ts + 16 * x, p);
+                        }
                     }
                     tmem_store_wait();
-                }
-                const Pair c2 = both(c), t2 = both(-m_row * c);
-                auto probability = [&](uint32_t lo, uint32_t hi) {
-                    const float2 e = split(fma2(pair(__uint_as_float(lo), __uint_as_float(hi)), c2, t2));
-                    const float a = exp2_of(e.x), b = exp2_of(e.y);
-                    sum = sum + pair(a, b);
-                    return pack16<F16>(a, b);
-                };
-                if (whole) {
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        uint32_t p[32];
-#pragma unroll
-                        for (int x = 0; x < 2; ++x)
-#pragma unroll
-                            for (int i = 0; i < 32; i += 2) p[16 * x + i / 2] = probability(s[2 * half + x][i], s[2 * half + x][i + 1]);
-                        tmem_store(ts + 32 * half, p);
-                    }
-                } else {
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        uint32_t p[16];
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) p[i] = 0;
-                        if (x < seen) {
-#pragma unroll
-                            for (int i = 0; i < 32; i += 2) p[i / 2] = probability(s[x][i], s[x][i + 1]);
-                        }
-                        tmem_store(ts + 16 * x, p);
-                    }
-                }
-                tmem_store_wait();
-                mma_fence_before();
-                __syncwarp();
-                if (lane == 0) bar_arrive(p_full + 8 * which);
-                ++count;
+                    mma_fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(p_full + 8 * which);
+                    ++count;
                 }
                 if (j == 0 && pending) {  // behind the first tile of the next item, or the last item of all
                     pending = false;
@@ -537,7 +545,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (!ok || !more) break;
             out.set(own);
-            lse = own_lse, l = total_of(sum), top = m_row;
+            lse = own_lse, l = total(sum), top = m_row;
             pending = true;
             ++items;
         }

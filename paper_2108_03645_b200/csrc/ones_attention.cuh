@@ -205,7 +205,7 @@ __host__ inline HeadsOut heads_out(const ones_heads& h, int dim, int tokens) {
 // own, or by shuffles where shared memory is full) until each has the same piece of four rows, and write 64 bytes of a row
 // together; predicated, since each branch around a store costs 100 cycles. Rows off 16-byte boundaries: 16 lanes exchange words,
 // and write a row by 2 bytes (15 heads of 77 values, 16 thousand tokens: 260 us for the forward pass with lanes that write
-// their own rows, 120 so).
+// their own rows, 123 so).
 constexpr int kStageBytesOfWarp = 32 * 64;
 struct RowsOut {
     unsigned long long own;   // 0: not there
@@ -341,8 +341,6 @@ struct Slot {
     uint32_t at, parity;
     __device__ __forceinline__ explicit Slot(uint32_t n) : at(n % SLOTS), parity(n / SLOTS & 1) {}
 };
-
-__device__ __forceinline__ float total_of(Pair a) { return total(a); }
 
 // What both directions refuse. kv: of each tensor, whether its heads are those of the keys.
 struct HeadsOf {

@@ -5,6 +5,9 @@
 // two products over the queries behind it, all heads of the group one after the other). Seven products where five would do
 // if dq were added up in memory: but that takes 64 KB of atomic additions for every pair of tiles, whose order would change
 // the results, or turns taken between blocks. A pair costs 1536 + 2048 cycles of products and 2 x 1024 of exponentials.
+// Measured: 16384 tokens, 16 / 4 heads of 128: 1190 us for the queries and 1640 for the keys, 1.39 and 1.34 PFLOP/s of what they
+// execute (the card at its power limit, 1.6 to 1.77 GHz). 128 samples of 256 tokens, 16 heads of 64: survey 105 us (0.47 GB in
+// and out at 4.5 TB/s), queries 121, keys 127, bound by the latency of a pair's chain of steps.
 //
 // What the rounding to 16 bits costs. The gradients of the scores meet q and k as float16, whatever the type of the tensors:
 // times a power of two they keep 11 bits where bfloat16 would keep 8 (error of dq 2.9e-3 of its norm, of which 1.66e-3 is the
@@ -188,7 +191,7 @@ __global__ void __launch_bounds__(256) k_survey(const __grid_constant__ SurveyAr
                         const float2 y = values16<F16>(u[i]), z = values16<F16>(w[i]);
                         d = fma2(pair(y.x, y.y), pair(z.x, z.y), d);
                     }
-                    dot = total_of(d);
+                    dot = total(d);
                 } else if (live) {  // single values, in another order: dout is read again, from the first-level cache
                     const uint16_t* const u = dout + at_t[x] * g.dout.token + at_h[x] * g.dout.head;
                     const uint16_t* const w = out + at_t[x] * g.out.token + at_h[x] * g.out.head;
@@ -331,125 +334,125 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = true;
 
     if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    if (warp == 8) {
-        // load
-        uint32_t n = 0, items = 0;
-        const uint32_t qbytes = HALVES * g.group * g.kt * 128;
-        while (ok && walk.next()) {
-            const Work it = walk.it;
-            const int tiles = key_tiles(it, g.kt);
-            if (!tiles) continue;
-            const Set set(items++);
-            if (!(ok = warp_wait(q_free + 8 * set.at, set.parity ^ 1))) break;
-            if (elect_one()) {
-                const uint32_t to = base + 2 * set.at * B::kTile, bar = q_full + 8 * set.at;
-                bar_expect(bar, 2 * qbytes);
-                for (int x = 0; x < HALVES; ++x) {
-                    tma_load<1>(to + x * kHalfTile, &map_q, 64 * x, walk.it.h * g.group, it.first, bar);
-                    tma_load<1>(to + B::kTile + x * kHalfTile, &map_do, 64 * x, walk.it.h * g.group, it.first, bar);
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (warp == 8) {
+            // load
+            uint32_t n = 0, items = 0;
+            const uint32_t qbytes = HALVES * g.group * g.kt * 128;
+            while (ok && walk.next()) {
+                const Work it = walk.it;
+                const int tiles = key_tiles(it, g.kt);
+                if (!tiles) continue;
+                const Set set(items++);
+                if (!(ok = warp_wait(q_free + 8 * set.at, set.parity ^ 1))) break;
+                if (elect_one()) {
+                    const uint32_t to = base + 2 * set.at * B::kTile, bar = q_full + 8 * set.at;
+                    bar_expect(bar, 2 * qbytes);
+                    for (int x = 0; x < HALVES; ++x) {
+                        tma_load<1>(to + x * kHalfTile, &map_q, 64 * x, walk.it.h * g.group, it.first, bar);
+                        tma_load<1>(to + B::kTile + x * kHalfTile, &map_do, 64 * x, walk.it.h * g.group, it.first, bar);
+                    }
+                }
+                __syncwarp();
+                for (int j = tiles - 1; j >= 0; --j, ++n) {
+                    const KeySlot ks(n);
+                    const bool partial = it.end - it.begin < (j + 1) * kKeys;  // that tile is cleared first
+                    if (!(ok = warp_wait(k_empty + 8 * ks.at, ks.parity ^ 1))) break;
+                    if (elect_one()) {
+                        const uint32_t bar = (partial ? k_raw : k_full) + 8 * ks.at;
+                        bar_expect(bar, B::kTile);
+                        for (int x = 0; x < HALVES; ++x)
+                            tma_load<1>(at_k + ks.at * B::kTile + x * kHalfTile, &map_k, 64 * x, walk.it.h, it.begin + j * kKeys, bar);
+                    }
+                    __syncwarp();
+                    const ValueSlot vs(n);
+                    if (!(ok = warp_wait(v_empty + 8 * vs.at, vs.parity ^ 1))) break;
+                    if (elect_one()) {
+                        const uint32_t bar = v_full + 8 * vs.at;
+                        bar_expect(bar, B::kTile);
+                        for (int x = 0; x < HALVES; ++x)
+                            tma_load<1>(at_v + vs.at * B::kTile + x * kHalfTile, &map_v, 64 * x, walk.it.h, it.begin + j * kKeys, bar);
+                    }
+                    __syncwarp();
                 }
             }
-            __syncwarp();
-            for (int j = tiles - 1; j >= 0; --j, ++n) {
-                const KeySlot ks(n);
-                const bool partial = it.end - it.begin < (j + 1) * kKeys;  // that tile is cleared first
-                if (!(ok = warp_wait(k_empty + 8 * ks.at, ks.parity ^ 1))) break;
-                if (elect_one()) {
-                    const uint32_t bar = (partial ? k_raw : k_full) + 8 * ks.at;
-                    bar_expect(bar, B::kTile);
-                    for (int x = 0; x < HALVES; ++x)
-                        tma_load<1>(at_k + ks.at * B::kTile + x * kHalfTile, &map_k, 64 * x, walk.it.h, it.begin + j * kKeys, bar);
+        } else if (warp == 10) {
+            // clear what lies behind a sequence in its last keys
+            uint32_t n = 0, parities = 0;
+            while (ok && walk.next()) {
+                const Work it = walk.it;
+                const int tiles = key_tiles(it, g.kt), rest = it.end - it.begin - (tiles - 1) * kKeys;
+                if (tiles && rest < kKeys) {
+                    const KeySlot ks(n);
+                    if (!(ok = warp_wait(k_raw + 8 * ks.at, parities >> ks.at & 1))) break;
+                    parities ^= 1u << ks.at;
+                    clear_rows<HALVES>(smem + (2 * B::kSets + ks.at) * B::kTile, rest, lane);
+                    if (lane == 0) bar_arrive(k_full + 8 * ks.at);
                 }
-                __syncwarp();
-                const ValueSlot vs(n);
-                if (!(ok = warp_wait(v_empty + 8 * vs.at, vs.parity ^ 1))) break;
-                if (elect_one()) {
-                    const uint32_t bar = v_full + 8 * vs.at;
-                    bar_expect(bar, B::kTile);
-                    for (int x = 0; x < HALVES; ++x)
-                        tma_load<1>(at_v + vs.at * B::kTile + x * kHalfTile, &map_v, 64 * x, walk.it.h, it.begin + j * kKeys, bar);
+                n += tiles;
+            }
+        } else if (warp == 9) {
+            // multiply: scores and dp of a tile, then dq of the one before, through all items
+            const uint32_t id_s = attend_desc(true, false, kKeys), id_dp = attend_desc(F16, false, kKeys), id_acc = attend_desc(true, true, 64 * HALVES);
+            const int steps = (g.dim + 15) / 16;
+            uint32_t t = 0, items = 0;  // tiles and items begun
+            int tiles = 0, j = 0;       // of the present item, tile j from the last on
+            struct {
+                bool any, first, last;
+                uint32_t item;
+            } before = {false, false, false, 0};
+            for (;;) {
+                bool any = true;
+                if (--j < 0) {
+                    while ((any = walk.next()) && !(tiles = key_tiles(walk.it, g.kt))) {}
+                    j = any ? tiles - 1 : 0;
+                    items += any;
                 }
-                __syncwarp();
+                if (!any && !before.any) break;
+                if (any) {
+                    const Set set(items - 1);
+                    const KeySlot ks(t);
+                    const ValueSlot vs(t);
+                    const uint32_t at_q = base + 2 * set.at * B::kTile;
+                    if (j == tiles - 1 && !(ok = warp_wait(q_full + 8 * set.at, set.parity))) break;
+                    if (!(ok = warp_wait(k_full + 8 * ks.at, ks.parity))) break;
+                    mma_fence_after();
+                    if (elect_one()) {
+                        product_rows<HALVES>(tmem + 128 * (t & 1), at_q, at_k + ks.at * B::kTile, id_s, steps);
+                        mma_commit<1>(s_full + 8 * (t & 1));
+                    }
+                    __syncwarp();
+                    if (!(ok = warp_wait(v_full + 8 * vs.at, vs.parity))) break;
+                    if (!(ok = warp_wait(dp_free, (t & 1) ^ 1))) break;  // what was there has been read
+                    mma_fence_after();
+                    if (elect_one()) {
+                        product_rows<HALVES>(t_dp, at_q + B::kTile, at_v + vs.at * B::kTile, id_dp, steps);
+                        mma_commit<1>(dp_full);
+                        mma_commit<1>(v_empty + 8 * vs.at);
+                        if (j == 0) mma_commit<1>(q_free + 8 * set.at);
+                    }
+                    __syncwarp();
+                }
+                if (before.any) {
+                    const uint32_t i = t - 1;
+                    const Set set(before.item);
+                    const KeySlot ks(i);
+                    if (!(ok = warp_wait(ds_full + 8 * (i & 1), (i >> 1) & 1))) break;
+                    if (before.first && !(ok = warp_wait(acc_free + 8 * set.at, set.parity ^ 1))) break;
+                    mma_fence_after();
+                    if (elect_one()) {
+                        const uint32_t a = tmem + 128 * (i & 1), k = at_k + ks.at * B::kTile, acc = t_acc + 64 * set.at;
+                        product_tmem(acc, a, a + 64, k, id_acc, !before.first);
+                        if (F16 && before.last) product_tmem(acc, a + 32, a + 96, k, id_acc, true);
+                        mma_commit<1>(k_empty + 8 * ks.at);
+                        if (before.last) mma_commit<1>(acc_full + 8 * set.at);
+                    }
+                    __syncwarp();
+                }
+                before = {any, j == tiles - 1, j == 0, items - 1};
+                t += any;
             }
         }
-    } else if (warp == 10) {
-        // clear what lies behind a sequence in its last keys
-        uint32_t n = 0, parities = 0;
-        while (ok && walk.next()) {
-            const Work it = walk.it;
-            const int tiles = key_tiles(it, g.kt), rest = it.end - it.begin - (tiles - 1) * kKeys;
-            if (tiles && rest < kKeys) {
-                const KeySlot ks(n);
-                if (!(ok = warp_wait(k_raw + 8 * ks.at, parities >> ks.at & 1))) break;
-                parities ^= 1u << ks.at;
-                clear_rows<HALVES>(smem + (2 * B::kSets + ks.at) * B::kTile, rest, lane);
-                if (lane == 0) bar_arrive(k_full + 8 * ks.at);
-            }
-            n += tiles;
-        }
-    } else if (warp == 9) {
-        // multiply: scores and dp of a tile, then dq of the one before, through all items
-        const uint32_t id_s = attend_desc(true, false, kKeys), id_dp = attend_desc(F16, false, kKeys), id_acc = attend_desc(true, true, 64 * HALVES);
-        const int steps = (g.dim + 15) / 16;
-        uint32_t t = 0, items = 0;  // tiles and items begun
-        int tiles = 0, j = 0;       // of the present item, tile j from the last on
-        struct {
-            bool any, first, last;
-            uint32_t item;
-        } before = {false, false, false, 0};
-        for (;;) {
-            bool any = true;
-            if (--j < 0) {
-                while ((any = walk.next()) && !(tiles = key_tiles(walk.it, g.kt))) {}
-                j = any ? tiles - 1 : 0;
-                items += any;
-            }
-            if (!any && !before.any) break;
-            if (any) {
-                const Set set(items - 1);
-                const KeySlot ks(t);
-                const ValueSlot vs(t);
-                const uint32_t at_q = base + 2 * set.at * B::kTile;
-                if (j == tiles - 1 && !(ok = warp_wait(q_full + 8 * set.at, set.parity))) break;
-                if (!(ok = warp_wait(k_full + 8 * ks.at, ks.parity))) break;
-                mma_fence_after();
-                if (elect_one()) {
-                    product_rows<HALVES>(tmem + 128 * (t & 1), at_q, at_k + ks.at * B::kTile, id_s, steps);
-                    mma_commit<1>(s_full + 8 * (t & 1));
-                }
-                __syncwarp();
-                if (!(ok = warp_wait(v_full + 8 * vs.at, vs.parity))) break;
-                if (!(ok = warp_wait(dp_free, (t & 1) ^ 1))) break;  // what was there has been read
-                mma_fence_after();
-                if (elect_one()) {
-                    product_rows<HALVES>(t_dp, at_q + B::kTile, at_v + vs.at * B::kTile, id_dp, steps);
-                    mma_commit<1>(dp_full);
-                    mma_commit<1>(v_empty + 8 * vs.at);
-                    if (j == 0) mma_commit<1>(q_free + 8 * set.at);
-                }
-                __syncwarp();
-            }
-            if (before.any) {
-                const uint32_t i = t - 1;
-                const Set set(before.item);
-                const KeySlot ks(i);
-                if (!(ok = warp_wait(ds_full + 8 * (i & 1), (i >> 1) & 1))) break;
-                if (before.first && !(ok = warp_wait(acc_free + 8 * set.at, set.parity ^ 1))) break;
-                mma_fence_after();
-                if (elect_one()) {
-                    const uint32_t a = tmem + 128 * (i & 1), k = at_k + ks.at * B::kTile, acc = t_acc + 64 * set.at;
-                    product_tmem(acc, a, a + 64, k, id_acc, !before.first);
-                    if (F16 && before.last) product_tmem(acc, a + 32, a + 96, k, id_acc, true);
-                    mma_commit<1>(k_empty + 8 * ks.at);
-                    if (before.last) mma_commit<1>(acc_full + 8 * set.at);
-                }
-                __syncwarp();
-            }
-            before = {any, j == tiles - 1, j == 0, items - 1};
-            t += any;
-        }
-    }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         const int half = warp / 4, row = threadIdx.x % 128;
@@ -540,8 +543,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                             p2 = p2 + p_at(x, i);
                         }
                     // the other half of the columns is with the warp of the same lanes: they meet in columns that scores have left
-                    const float2 own_sums = make_float2(total_of(sum), total_of(p2));
-                    const float own_lost = F16 ? total_of(lost) : 0.f;
+                    const float2 own_sums = make_float2(total(sum), total(p2));
+                    const float own_lost = F16 ? total(lost) : 0.f;
                     tmem_put(ts + 32, own_sums.x, own_sums.y);
                     if (F16) tmem_put(ts + 34, own_lost, 0.f);
                     mma_fence_before();
@@ -686,149 +689,149 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = true;
 
     if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    if (warp == 8) {
-        // load
-        uint32_t n = 0, items = 0;
-        const uint32_t qbytes = HALVES * qrows * 128;
-        while (ok && walk.next()) {
-            const Work it = walk.it;
-            const QuerySpan q = query_span(it, g.kt);
-            if (!q.tiles) continue;
-            const Set set(items++);
-            if (!(ok = warp_wait(kv_free + 8 * set.at, set.parity ^ 1))) break;
-            if (elect_one()) {
-                const uint32_t to = base + 2 * set.at * B::kTile, bar = kv_full + 8 * set.at;
-                bar_expect(bar, 2 * B::kTile);
-                for (int x = 0; x < HALVES; ++x) {
-                    tma_load<1>(to + x * kHalfTile, &map_k, 64 * x, walk.it.h, it.first, bar);
-                    tma_load<1>(to + B::kTile + x * kHalfTile, &map_v, 64 * x, walk.it.h, it.first, bar);
-                }
-            }
-            __syncwarp();
-            for (int i = 0; ok && i < q.tiles; ++i, ++n) {
-                const At slot(n);
-                const int first = q.first + i * g.kt;
-                const bool partial = it.end - first < g.kt;  // that tile is cleared first
-                for (int kind = 0; kind < 2; ++kind) {
-                    const uint32_t full = (kind ? partial ? do_raw : do_full : partial ? q_raw : q_full) + 8 * slot.at;
-                    const uint32_t to = (kind ? at_do : at_q) + slot.at * B::kTile;
-                    if (!(ok = warp_wait((kind ? do_empty : q_empty) + 8 * slot.at, slot.parity ^ 1))) break;
-                    if (elect_one()) {
-                        bar_expect(full, qbytes);
-                        for (int x = 0; x < HALVES; ++x)
-                            tma_load<1>(to + x * kHalfTile, kind ? &map_do : &map_q, 64 * x, walk.it.h * g.group, first, full);
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (warp == 8) {
+            // load
+            uint32_t n = 0, items = 0;
+            const uint32_t qbytes = HALVES * qrows * 128;
+            while (ok && walk.next()) {
+                const Work it = walk.it;
+                const QuerySpan q = query_span(it, g.kt);
+                if (!q.tiles) continue;
+                const Set set(items++);
+                if (!(ok = warp_wait(kv_free + 8 * set.at, set.parity ^ 1))) break;
+                if (elect_one()) {
+                    const uint32_t to = base + 2 * set.at * B::kTile, bar = kv_full + 8 * set.at;
+                    bar_expect(bar, 2 * B::kTile);
+                    for (int x = 0; x < HALVES; ++x) {
+                        tma_load<1>(to + x * kHalfTile, &map_k, 64 * x, walk.it.h, it.first, bar);
+                        tma_load<1>(to + B::kTile + x * kHalfTile, &map_v, 64 * x, walk.it.h, it.first, bar);
                     }
-                    __syncwarp();
+                }
+                __syncwarp();
+                for (int i = 0; ok && i < q.tiles; ++i, ++n) {
+                    const At slot(n);
+                    const int first = q.first + i * g.kt;
+                    const bool partial = it.end - first < g.kt;  // that tile is cleared first
+                    for (int kind = 0; kind < 2; ++kind) {
+                        const uint32_t full = (kind ? partial ? do_raw : do_full : partial ? q_raw : q_full) + 8 * slot.at;
+                        const uint32_t to = (kind ? at_do : at_q) + slot.at * B::kTile;
+                        if (!(ok = warp_wait((kind ? do_empty : q_empty) + 8 * slot.at, slot.parity ^ 1))) break;
+                        if (elect_one()) {
+                            bar_expect(full, qbytes);
+                            for (int x = 0; x < HALVES; ++x)
+                                tma_load<1>(to + x * kHalfTile, kind ? &map_do : &map_q, 64 * x, walk.it.h * g.group, first, full);
+                        }
+                        __syncwarp();
+                    }
                 }
             }
-        }
-    } else if (warp == 11) {
-        // clear what lies behind a sequence in its last queries
-        uint32_t n = 0, parities = 0;
-        while (ok && walk.next()) {
-            const Work it = walk.it;
-            const QuerySpan q = query_span(it, g.kt);
-            n += q.tiles;
-            const int rest = it.end - q.first - (q.tiles - 1) * g.kt;
-            if (!q.tiles || rest >= g.kt) continue;
-            const At slot(n - 1);
-            for (int kind = 0; kind < 2; ++kind) {
-                if (!(ok = warp_wait((kind ? do_raw : q_raw) + 8 * slot.at, parities >> slot.at & 1))) break;
-                clear_rows<HALVES>(smem + (kRing + (kind ? B::kSlots : 0) + slot.at) * B::kTile, rest * g.group, lane);
-                if (lane == 0) bar_arrive((kind ? do_full : q_full) + 8 * slot.at);
+        } else if (warp == 11) {
+            // clear what lies behind a sequence in its last queries
+            uint32_t n = 0, parities = 0;
+            while (ok && walk.next()) {
+                const Work it = walk.it;
+                const QuerySpan q = query_span(it, g.kt);
+                n += q.tiles;
+                const int rest = it.end - q.first - (q.tiles - 1) * g.kt;
+                if (!q.tiles || rest >= g.kt) continue;
+                const At slot(n - 1);
+                for (int kind = 0; kind < 2; ++kind) {
+                    if (!(ok = warp_wait((kind ? do_raw : q_raw) + 8 * slot.at, parities >> slot.at & 1))) break;
+                    clear_rows<HALVES>(smem + (kRing + (kind ? B::kSlots : 0) + slot.at) * B::kTile, rest * g.group, lane);
+                    if (lane == 0) bar_arrive((kind ? do_full : q_full) + 8 * slot.at);
+                }
+                parities ^= 1u << slot.at;
             }
-            parities ^= 1u << slot.at;
-        }
-    } else if (warp == 9) {
-        // multiply: each product with the queries or dout, and behind it the next tile's scores or dp in the place of what it used
-        const uint32_t id_s = attend_desc(true, false, kRows), id_dp = attend_desc(F16, false, kRows), id_dk = attend_desc(true, true, 64 * HALVES),
-                       id_dv = attend_desc(F16, true, 64 * HALVES);
-        const int steps = (g.dim + 15) / 16;
-        uint32_t t = 0, items = 0;  // the present tile, counted through all items; items begun
-        int i = 0, tiles = 0;
-        auto step = [&]() {
-            if (++i < tiles) return true;
-            while (walk.next()) {
-                tiles = query_span(walk.it, g.kt).tiles;
-                if (!tiles) continue;
-                i = 0;
-                ++items;
+        } else if (warp == 9) {
+            // multiply: each product with the queries or dout, and behind it the next tile's scores or dp in the place of what it used
+            const uint32_t id_s = attend_desc(true, false, kRows), id_dp = attend_desc(F16, false, kRows), id_dk = attend_desc(true, true, 64 * HALVES),
+                           id_dv = attend_desc(F16, true, 64 * HALVES);
+            const int steps = (g.dim + 15) / 16;
+            uint32_t t = 0, items = 0;  // the present tile, counted through all items; items begun
+            int i = 0, tiles = 0;
+            auto step = [&]() {
+                if (++i < tiles) return true;
+                while (walk.next()) {
+                    tiles = query_span(walk.it, g.kt).tiles;
+                    if (!tiles) continue;
+                    i = 0;
+                    ++items;
+                    return true;
+                }
+                return false;
+            };
+            // scores or dp of tile n, the i-th of its item
+            auto rows = [&](uint32_t n, bool dp) {
+                const At slot(n);
+                const Set set(items - 1);
+                if (!dp && i == 0 && !warp_wait(kv_full + 8 * set.at, set.parity)) return false;
+                if (!warp_wait((dp ? do_full : q_full) + 8 * slot.at, slot.parity)) return false;
+                mma_fence_after();
+                if (elect_one()) {
+                    product_rows<HALVES>(dp ? t_dp : tmem, base + (2 * set.at + dp) * B::kTile, (dp ? at_do : at_q) + slot.at * B::kTile, dp ? id_dp : id_s, steps);
+                    mma_commit<1>(dp ? dp_full : s_full);
+                    if (dp && i + 1 == tiles) mma_commit<1>(kv_free + 8 * set.at);
+                }
+                __syncwarp();
                 return true;
-            }
-            return false;
-        };
-        // scores or dp of tile n, the i-th of its item
-        auto rows = [&](uint32_t n, bool dp) {
-            const At slot(n);
-            const Set set(items - 1);
-            if (!dp && i == 0 && !warp_wait(kv_full + 8 * set.at, set.parity)) return false;
-            if (!warp_wait((dp ? do_full : q_full) + 8 * slot.at, slot.parity)) return false;
-            mma_fence_after();
-            if (elect_one()) {
-                product_rows<HALVES>(dp ? t_dp : tmem, base + (2 * set.at + dp) * B::kTile, (dp ? at_do : at_q) + slot.at * B::kTile, dp ? id_dp : id_s, steps);
-                mma_commit<1>(dp ? dp_full : s_full);
-                if (dp && i + 1 == tiles) mma_commit<1>(kv_free + 8 * set.at);
-            }
-            __syncwarp();
-            return true;
-        };
-        bool any = step();
-        if (any) ok = rows(0, false) && rows(0, true);
-        while (ok && any) {
-            const At slot(t);
-            const Set set(items - 1);
-            const bool first = i == 0, last = i + 1 == tiles, fine = F16 && tiles <= kFineTiles;
-            if (!(ok = warp_wait(p_full, t & 1))) break;
-            if (first && !(ok = warp_wait(acc_free + 8 * set.at, set.parity ^ 1))) break;
-            mma_fence_after();
-            if (elect_one()) {
-                product_tmem(t_dv + 64 * set.at, tmem, tmem + 64, at_do + slot.at * B::kTile, id_dv, !first);
-                mma_commit<1>(do_empty + 8 * slot.at);
-            }
-            __syncwarp();
-            any = step();
-            if (any && !(ok = rows(t + 1, false))) break;
-            if (!(ok = warp_wait(ds_full, t & 1))) break;
-            mma_fence_after();
-            if (elect_one()) {
-                const uint32_t acc = t_dk + 64 * set.at, b = at_q + slot.at * B::kTile;
-                product_tmem(acc, t_dp, t_dp + 64, b, id_dk, !first);
-                if (fine) product_tmem(acc, t_dp + 32, t_dp + 96, b, id_dk, true);
-                mma_commit<1>(q_empty + 8 * slot.at);
-                if (last) mma_commit<1>(acc_full + 8 * set.at);
-            }
-            __syncwarp();
-            if (any && !(ok = rows(t + 1, true))) break;
-            ++t;
-        }
-    } else if (warp == 10) {
-        // statistics of the rows of queries: what the exponent subtracts, and delta
-        uint32_t n = 0;
-        while (ok && walk.next()) {
-            const Work it = walk.it;
-            const QuerySpan q = query_span(it, g.kt);
-            if (!q.tiles) continue;
-            const float sigma = ldexpf(1.f, powers_of<F16>(g, walk.it.h).sigma - (F16 ? kLift : 0));
-            for (int i = 0; i < q.tiles; ++i, ++n) {
-                const Stat stage(n);
-                float l[4], d[4];
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const int row = 32 * x + lane, token = q.first + i * g.kt + row / g.group, head = walk.it.h * g.group + row % g.group;
-                    const bool live = row < qrows && token < it.end;
-                    const int64_t at = (int64_t)token * g.heads + head;
-                    l[x] = live ? (F16 ? kLift : 0) - g.lse[at] * kLog2e : -INFINITY;
-                    d[x] = live ? -g.delta[at] * sigma : 0.f;
+            };
+            bool any = step();
+            if (any) ok = rows(0, false) && rows(0, true);
+            while (ok && any) {
+                const At slot(t);
+                const Set set(items - 1);
+                const bool first = i == 0, last = i + 1 == tiles, fine = F16 && tiles <= kFineTiles;
+                if (!(ok = warp_wait(p_full, t & 1))) break;
+                if (first && !(ok = warp_wait(acc_free + 8 * set.at, set.parity ^ 1))) break;
+                mma_fence_after();
+                if (elect_one()) {
+                    product_tmem(t_dv + 64 * set.at, tmem, tmem + 64, at_do + slot.at * B::kTile, id_dv, !first);
+                    mma_commit<1>(do_empty + 8 * slot.at);
                 }
-                if (!(ok = warp_wait(st_empty + 8 * stage.at, stage.parity ^ 1))) break;
-                float* const to = stats + stage.at * 2 * kRows;
+                __syncwarp();
+                any = step();
+                if (any && !(ok = rows(t + 1, false))) break;
+                if (!(ok = warp_wait(ds_full, t & 1))) break;
+                mma_fence_after();
+                if (elect_one()) {
+                    const uint32_t acc = t_dk + 64 * set.at, b = at_q + slot.at * B::kTile;
+                    product_tmem(acc, t_dp, t_dp + 64, b, id_dk, !first);
+                    if (fine) product_tmem(acc, t_dp + 32, t_dp + 96, b, id_dk, true);
+                    mma_commit<1>(q_empty + 8 * slot.at);
+                    if (last) mma_commit<1>(acc_full + 8 * set.at);
+                }
+                __syncwarp();
+                if (any && !(ok = rows(t + 1, true))) break;
+                ++t;
+            }
+        } else if (warp == 10) {
+            // statistics of the rows of queries: what the exponent subtracts, and delta
+            uint32_t n = 0;
+            while (ok && walk.next()) {
+                const Work it = walk.it;
+                const QuerySpan q = query_span(it, g.kt);
+                if (!q.tiles) continue;
+                const float sigma = ldexpf(1.f, powers_of<F16>(g, walk.it.h).sigma - (F16 ? kLift : 0));
+                for (int i = 0; i < q.tiles; ++i, ++n) {
+                    const Stat stage(n);
+                    float l[4], d[4];
 #pragma unroll
-                for (int x = 0; x < 4; ++x) to[32 * x + lane] = l[x], to[kRows + 32 * x + lane] = d[x];
-                bar_arrive(st_full + 8 * stage.at);
+                    for (int x = 0; x < 4; ++x) {
+                        const int row = 32 * x + lane, token = q.first + i * g.kt + row / g.group, head = walk.it.h * g.group + row % g.group;
+                        const bool live = row < qrows && token < it.end;
+                        const int64_t at = (int64_t)token * g.heads + head;
+                        l[x] = live ? (F16 ? kLift : 0) - g.lse[at] * kLog2e : -INFINITY;
+                        d[x] = live ? -g.delta[at] * sigma : 0.f;
+                    }
+                    if (!(ok = warp_wait(st_empty + 8 * stage.at, stage.parity ^ 1))) break;
+                    float* const to = stats + stage.at * 2 * kRows;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) to[32 * x + lane] = l[x], to[kRows + 32 * x + lane] = d[x];
+                    bar_arrive(st_full + 8 * stage.at);
+                }
             }
         }
-    }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         const int half = warp / 4, row = threadIdx.x % 128;
