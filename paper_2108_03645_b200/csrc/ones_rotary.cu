@@ -10,6 +10,7 @@
 #include <cuda_fp16.h>
 #include <math.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "ones_attention.h"
@@ -40,6 +41,7 @@ struct Side {  // queries or keys
     void *out, *dweight;
     int64_t x_token, x_head, dy_token, dy_head, out_token, out_head;
     int heads;
+    int step_t, step_h;  // from a group's vector to its next one, which lies as many vectors on as there are groups
 };
 struct Args {
     Side side[2];
@@ -85,6 +87,10 @@ struct Row {
                 b[0] = q.x, b[1] = q.y, b[2] = q.z, b[3] = q.w;
             }
         }
+    }
+    __device__ __forceinline__ void take(const uint4& p, const uint4& q) {
+        a[0] = p.x, a[1] = p.y, a[2] = p.z, a[3] = p.w;
+        b[0] = q.x, b[1] = q.y, b[2] = q.z, b[3] = q.w;
     }
     static __device__ __forceinline__ uint32_t word(float v) { return __float_as_uint(v); }
     static __device__ __forceinline__ uint32_t word(__nv_bfloat16 v) { return __bfloat16_as_ushort(v); }
@@ -204,15 +210,28 @@ __device__ __forceinline__ float inverse_root(float ss, const Args& g) {
 
 constexpr int kWeightRow = ONES_QK_NORM_MAX_DIM + 16;
 
-// U units per lane: 1 where pieces of 16 bytes are possible, more for single values. The next vector of a group is on its way
-// while the present one is worked on; five blocks (backward: two) on an SM hide the rest.
+// Pieces of vectors on their way into shared memory. Each thread has slots of its own, so that nothing but its own copies is
+// waited for.
+constexpr int kStages = 4;
+constexpr int kRingBytes = kStages * 4 * kThreads * 16;
+__device__ __forceinline__ void copy_async(const uint4* to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+}
+
+// U units per lane: 1 where pieces of 16 bytes are possible, more for single values. Forward, the next vector of a group is on its
+// way while the present one is worked on, and five blocks on an SM hide the rest (through shared memory, whose reads it is bound
+// by, 240 -> 269 us for 65536 x 40 x 128). Backward, the sums for the weights leave room for two blocks, and three vectors of each
+// group are on their way, through shared memory (one, in registers: 517 us, so 385).
 template <class T, int V, int U, bool INTER, bool BACK>
 __global__ void __launch_bounds__(kThreads, BACK ? 2 : 5) k_qk_norm(const __grid_constant__ Args g) {
-    extern __shared__ float smem[];
+    constexpr bool kRing = BACK && V > 1;
+    constexpr int kPieces = 4;  // of a vector and a lane: two of x, two of dy
+    extern __shared__ __align__(16) float smem[];
     __shared__ __align__(16) float s_weight[2][kWeightRow];
     const int lanes = 1 << g.group_log, groups = kThreads >> g.group_log;
     const int lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> g.group_log;
     float *cs = smem, *sn = smem + g.tile * g.angles;
+    uint4* const ring = reinterpret_cast<uint4*>(sn + g.tile * g.angles) + threadIdx.x;
     Unit unit[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) unit[u] = unit_at<V, INTER>(g, lane + u * lanes);
@@ -230,6 +249,46 @@ __global__ void __launch_bounds__(kThreads, BACK ? 2 : 5) k_qk_norm(const __grid
             for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int i = 0; i < V; ++i) dw[which][u][i] = both(0.f);
+    }
+    // What is copied next, three vectors ahead: through both sides of all tiles. left: rounds of this side of this tile; t, h: the
+    // token in the tile and the head; slot: where to.
+    struct {
+        int tile, which, left, t, h, slot;
+    } ahead = {(int)blockIdx.x - (int)gridDim.x, 1, 0, 0, 0, 0};
+    auto copy_next = [&]() {
+        while (ahead.left == 0 && ahead.tile < tiles) {
+            if (ahead.which) ahead.tile += gridDim.x;
+            ahead.which ^= 1;
+            if (ahead.tile >= tiles) break;
+            const int heads = g.side[ahead.which].heads;
+            ahead.left = (min(g.tile, g.tokens - ahead.tile * g.tile) * heads + groups - 1) / groups;
+            if (heads) ahead.t = group / heads, ahead.h = group - ahead.t * heads;
+        }
+        if (ahead.left) {
+            const Side& side = g.side[ahead.which];
+            const int64_t t = (int64_t)ahead.tile * g.tile + ahead.t;
+            if (ahead.t < g.tile && t < g.tokens) {
+                const T* const x = static_cast<const T*>(side.x) + t * side.x_token + ahead.h * side.x_head;
+                const T* const y = static_cast<const T*>(side.dy) + t * side.dy_token + ahead.h * side.dy_head;
+                uint4* const to = ring + ahead.slot * kPieces * kThreads;
+                if (unit[0].a < g.dim) copy_async(to, x + unit[0].a);
+                if (unit[0].b < g.dim) copy_async(to + kThreads, x + unit[0].b);
+                if (unit[0].a < g.dim) copy_async(to + 2 * kThreads, y + unit[0].a);
+                if (unit[0].b < g.dim) copy_async(to + 3 * kThreads, y + unit[0].b);
+            }
+            ahead.t += side.step_t, ahead.h += side.step_h;
+            if (ahead.h >= side.heads) ahead.h -= side.heads, ++ahead.t;
+            --ahead.left;
+        }
+        ahead.slot = (ahead.slot + 1) % kStages;
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    int now = 0;  // the slot of the present vector
+    if (kRing) {
+#pragma unroll
+        for (int i = 0; i < kPieces * kStages; ++i) ring[i * kThreads] = make_uint4(0, 0, 0, 0);  // pieces that are not there stay so
+#pragma unroll
+        for (int i = 0; i < kStages - 1; ++i) copy_next();
     }
     for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const int t0 = tile * g.tile, n = min(g.tile, g.tokens - t0), half = g.rotary / 2;
@@ -250,7 +309,6 @@ __global__ void __launch_bounds__(kThreads, BACK ? 2 : 5) k_qk_norm(const __grid
             const T* const py = static_cast<const T*>(side.dy) + (int64_t)t0 * side.dy_token;
             T* const po = static_cast<T*>(side.out) + (int64_t)t0 * side.out_token;
             Row<T, V> rx[U], ry[U], nx[U], ny[U];
-            // a group's vectors are `groups` apart
             const int step_t = groups / max(side.heads, 1), step_h = groups - step_t * side.heads;
             int t = group / max(side.heads, 1), h = group - t * side.heads;
             auto fetch = [&](Row<T, V>(&x)[U], Row<T, V>(&y)[U], int t, int h) {
@@ -261,11 +319,20 @@ __global__ void __launch_bounds__(kThreads, BACK ? 2 : 5) k_qk_norm(const __grid
                     if (BACK) y[u].load(py + t * side.dy_token + h * side.dy_head, unit[u], g.dim);
                 }
             };
-            if (rows) fetch(rx, ry, t, h);
+            if (!kRing && rows) fetch(rx, ry, t, h);
             for (int first = 0; first < rows; first += groups) {
                 int next_t = t + step_t, next_h = h + step_h;
                 if (next_h >= side.heads) next_h -= side.heads, ++next_t;
-                fetch(nx, ny, next_t, next_h);
+                if constexpr (kRing) {
+                    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+                    const uint4* const from = ring + now * kPieces * kThreads;
+                    rx[0].take(from[0], from[kThreads]);
+                    ry[0].take(from[2 * kThreads], from[3 * kThreads]);
+                    now = (now + 1) % kStages;
+                    copy_next();
+                } else {
+                    fetch(nx, ny, next_t, next_h);
+                }
                 const bool live = t < n;
                 const int at = min(t, n - 1);
                 T* const q = po + at * side.out_token + h * side.out_head;
@@ -298,19 +365,23 @@ __global__ void __launch_bounds__(kThreads, BACK ? 2 : 5) k_qk_norm(const __grid
                     }
                 } else {
                     const float back = f * f * (group_sum(total(gx), lanes) * g.per_dim);
-                    const Pair f2 = both(live ? f : 0.f), fb = both(-f * back), fx = both(f);
+                    const Pair fb = both(-f * back), fx = both(f);
+                    if (live) {
 #pragma unroll
-                    for (int u = 0; u < U; ++u) {
+                        for (int u = 0; u < U; ++u) {
 #pragma unroll
-                        for (int i = 0; i < V; ++i) {
-                            dw[BACK ? which : 0][u][i] = fma2(y[u][i], x[u][i] * f2, dw[BACK ? which : 0][u][i]);
-                            x[u][i] = fma2(x[u][i], fb, fx * w[u][i]);
+                            for (int i = 0; i < V; ++i) {
+                                dw[BACK ? which : 0][u][i] = fma2(y[u][i], x[u][i] * fx, dw[BACK ? which : 0][u][i]);
+                                x[u][i] = fma2(x[u][i], fb, fx * w[u][i]);
+                            }
+                            Row<T, V>::store(q, unit[u], g.dim, x[u]);
                         }
-                        if (live) Row<T, V>::store(q, unit[u], g.dim, x[u]);
                     }
                 }
+                if (!kRing) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) rx[u] = nx[u], ry[u] = ny[u];
+                    for (int u = 0; u < U; ++u) rx[u] = nx[u], ry[u] = ny[u];
+                }
                 t = next_t, h = next_h;
             }
         }
@@ -373,12 +444,18 @@ cudaError_t launch(Args& a, bool back, cudaStream_t stream, int* blocks) {
     // weigh little (65536 x 40 x 128 forward: four rounds 305 us, eight 274, sixteen 242), and fewer where that leaves SMs idle.
     // Their angles take 32 KB at most, so that five blocks are on an SM.
     a.angles = (a.rotary / 2 + 3) / 4 * 4;
+    for (Side& s : a.side) s.step_t = groups / max(s.heads, 1), s.step_h = groups - s.step_t * s.heads;
     a.tile = max(1, min(min(64, 16 * groups / heads), 4096 / max(a.angles, 1)));
     while (a.tile > 1 && (a.tokens - 1) / a.tile + 1 < 5 * device_sms()) a.tile = (a.tile + 1) / 2;
     const int tiles = (a.tokens - 1) / a.tile + 1;
     *blocks = back ? min(tiles, kMaxBlocks) : tiles;
-    const int smem = max(2 * a.tile * a.angles, back && a.part ? groups * a.dim : 0) * 4;
+    const int smem = max(2 * a.tile * a.angles * 4 + (back && V > 1 ? kRingBytes : 0), back && a.part ? groups * a.dim * 4 : 0);
     auto kernel = back ? k_qk_norm<T, V, U, INTER, true> : k_qk_norm<T, V, U, INTER, false>;
+    if (smem > 46 * 1024) {  // with the weights in shared memory, what a launch gets without asking
+        static std::atomic<uint64_t> ready[2];
+        const cudaError_t err = allow_smem(kernel, 32 * 1024 + kRingBytes, ready[back]);
+        if (err != cudaSuccess) return err;
+    }
     kernel<<<*blocks, kThreads, smem, stream>>>(a);
     return cudaGetLastError();
 }
