@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!warp_wait(p_full + 8 * which, count & 1)) return false;
         mma_fence_after();
         if (elect_one()) {
-            product_tmem(to, ts, ts + 32, ring + slot * F::kTile, attend_desc(F16, true, 64 * HALVES), j != 0);
+            product_tmem(to, ts, ts + 32, ring + slot * F::kTile, attend_desc(F16, true, 16 * ((g.dim + 15) / 16)), j != 0);
             mma_commit<1>(o_full + 8 * which);
             if (j + 1 == tiles) mma_commit<1>(acc_full + bar);
         }

@@ -6,8 +6,8 @@
 // if dq were added up in memory: but that takes 64 KB of atomic additions for every pair of tiles, whose order would change
 // the results, or turns taken between blocks. A pair costs 1536 + 2048 cycles of products and 2 x 1024 of exponentials.
 // Measured: 16384 tokens, 16 / 4 heads of 128: 1190 us for the queries and 1640 for the keys, 1.39 and 1.34 PFLOP/s of what they
-// execute (the card at its power limit, 1.6 to 1.77 GHz). 128 samples of 256 tokens, 16 heads of 64: survey 105 us (0.47 GB in
-// and out at 4.5 TB/s), queries 121, keys 127, bound by the latency of a pair's chain of steps.
+// execute (the card at its power limit, 1.6 to 1.77 GHz). 128 samples of 256 tokens, 16 heads of 64: survey 90 us (0.47 GB in
+// and out at 5.2 TB/s), queries 121, keys 127, bound by the latency of a pair's chain of steps.
 //
 // What the rounding to 16 bits costs. The gradients of the scores meet q and k as float16, whatever the type of the tensors:
 // times a power of two they keep 11 bits where bfloat16 would keep 8 (error of dq 2.9e-3 of its norm, of which 1.66e-3 is the
@@ -88,15 +88,31 @@ __device__ __forceinline__ float2 values16(uint32_t w) {
     return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
 }
 
-// Values c..c + 7 of a vector of dim values that starts on a 16-byte boundary; none behind its last is read.
-__device__ __forceinline__ uint4 eight_of(const uint16_t* p, int c, int dim) {
-    if (c + 8 <= dim) return *reinterpret_cast<const uint4*>(p + c);
+// Values c..c + 7 of a vector of dim values that starts on a 16-byte boundary. RAGGED: dim is no multiple of 8, and what lies behind
+// the vector's end is read along with it, to be masked out where the values are used (masked at once, it keeps the next loads
+// waiting: 54 us instead of 35 for 16102 tokens x 15 heads x 77), but not behind the last vector of all: vectors start on 16-byte
+// boundaries, so that any other one's last piece ends before the last one does.
+template <bool RAGGED>
+__device__ __forceinline__ uint4 eight_of(const uint16_t* p, int c, int dim, bool last) {
+    if (c >= dim) return make_uint4(0, 0, 0, 0);
+    if (!RAGGED || !last || c + 8 <= dim) return *reinterpret_cast<const uint4*>(p + c);
     uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         if (c + i < dim) w[i / 2] |= (uint32_t)p[c + i] << (16 * (i & 1));
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
+template <bool RAGGED>
+struct Own {  // which of the lane's eight values the vectors have
+    uint4 mask;
+    __device__ __forceinline__ Own(int c, int dim) {
+        auto word = [&](int i) { return c + i + 1 < dim ? 0xFFFFFFFFu : c + i < dim ? 0xFFFFu : 0u; };
+        mask = make_uint4(word(0), word(2), word(4), word(6));
+    }
+    __device__ __forceinline__ uint4 operator()(const uint4& v) const {
+        return RAGGED ? make_uint4(v.x & mask.x, v.y & mask.y, v.z & mask.z, v.w & mask.w) : v;
+    }
+};
 // The largest finite value's bits, as a 32-bit number.
 template <bool F16>
 __device__ __forceinline__ unsigned largest_of(const uint4& v) {
@@ -127,12 +143,13 @@ __device__ __forceinline__ uint4 narrowed(const uint4& v, float f) {
 
 // LANES x 8 values are a vector, which a group of lanes takes. A block takes kTokens tokens at a time.
 constexpr int kTokens = 16;
-template <bool F16, int LANES>
-__global__ void __launch_bounds__(256) k_survey(const __grid_constant__ SurveyArgs g) {
+template <bool F16, int LANES, bool RAGGED>
+__global__ void __launch_bounds__(256, 4) k_survey(const __grid_constant__ SurveyArgs g) {
     extern __shared__ unsigned top[];  // [4][kv], then the factors of q and k, [2][kv]
     constexpr int kGroups = 256 / LANES, kAtOnce = 4;
     float* const factor = reinterpret_cast<float*>(top + 4 * g.kv);
     const int lane = threadIdx.x % LANES, c = 8 * lane;
+    const Own<RAGGED> own_of(c, g.dim);
     wait_for_predecessor();
     let_successor_start();
     const int t0 = g.plan->covered[0], t1 = g.plan->covered[1], group = g.heads / g.kv;
@@ -149,7 +166,7 @@ __global__ void __launch_bounds__(256) k_survey(const __grid_constant__ SurveyAr
             const bool keys = i >= g.heads;
             const int h = keys ? i - g.heads : i;
             const Vectors& x = keys ? g.k : g.q;
-            note(eight_of(x.p + t0 * x.token + h * x.head, c, g.dim), keys ? 3 : 2, keys ? h : h / group);
+            note(own_of(eight_of<RAGGED>(x.p + t0 * x.token + h * x.head, c, g.dim, t0 == g.tokens - 1 && h == (keys ? g.kv : g.heads) - 1)), keys ? 3 : 2, keys ? h : h / group);
         }
         __syncthreads();
         for (int i = threadIdx.x; i < 2 * g.kv; i += 256) {
@@ -175,13 +192,15 @@ __global__ void __launch_bounds__(256) k_survey(const __grid_constant__ SurveyAr
                 at_t[x] = over(r, g.heads, per_head), at_h[x] = r - at_t[x] * g.heads;
                 a[x] = b[x] = make_uint4(0, 0, 0, 0);
                 if (at_t[x] >= n_t) continue;
-                a[x] = eight_of(dout + at_t[x] * g.dout.token + at_h[x] * g.dout.head, c, g.dim);
-                if (g.wide) b[x] = eight_of(out + at_t[x] * g.out.token + at_h[x] * g.out.head, c, g.dim);
+                const bool last = first + at_t[x] == g.tokens - 1 && at_h[x] == g.heads - 1;
+                a[x] = eight_of<RAGGED>(dout + at_t[x] * g.dout.token + at_h[x] * g.dout.head, c, g.dim, last);
+                if (g.wide) b[x] = eight_of<RAGGED>(out + at_t[x] * g.out.token + at_h[x] * g.out.head, c, g.dim, last);
             }
 #pragma unroll
             for (int x = 0; x < kAtOnce; ++x) {
                 const bool live = at_t[x] < n_t;
                 float dot = 0.f;
+                a[x] = own_of(a[x]), b[x] = own_of(b[x]);
                 if (live) note(a[x], 0, over(at_h[x], group, per_group));
                 if (g.wide) {
                     const uint32_t u[4] = {a[x].x, a[x].y, a[x].z, a[x].w}, w[4] = {b[x].x, b[x].y, b[x].z, b[x].w};
@@ -216,12 +235,13 @@ __global__ void __launch_bounds__(256) k_survey(const __grid_constant__ SurveyAr
 #pragma unroll
                 for (int x = 0; x < kAtOnce; ++x) {
                     const int r = r0 + x * kGroups + own, t = over(r, n, per);
-                    a[x] = t < n_t ? eight_of(in + t * from.token + (r - t * n) * from.head, c, g.dim) : make_uint4(0, 0, 0, 0);
+                    a[x] = t < n_t ? eight_of<RAGGED>(in + t * from.token + (r - t * n) * from.head, c, g.dim, first + t == g.tokens - 1 && r - t * n == n - 1) : make_uint4(0, 0, 0, 0);
                 }
 #pragma unroll
                 for (int x = 0; x < kAtOnce; ++x) {
                     const int r = r0 + x * kGroups + own, t = over(r, n, per);
                     if (t >= n_t) continue;
+                    a[x] = own_of(a[x]);
                     const int h = kind == 1 ? over(r - t * n, group, per_group) : r - t * n;
                     note(a[x], 1 + kind, h);
                     if (kind && c < g.row)
@@ -241,6 +261,7 @@ template <int LANES>
 __global__ void __launch_bounds__(256) k_settle(const __grid_constant__ SurveyArgs g, int* settled) {
     constexpr int kGroups = 256 / LANES;
     const int c = 8 * (threadIdx.x % LANES);
+    const Own<true> own_of(c, g.dim);
     wait_for_predecessor();
     let_successor_start();
     const int t0 = g.plan->covered[0], t1 = g.plan->covered[1], group = g.heads / g.kv;
@@ -256,7 +277,7 @@ __global__ void __launch_bounds__(256) k_settle(const __grid_constant__ SurveyAr
             const int64_t t = t0 + r / times;
             const int head = h * times + (int)(r % times);
             if (c < g.row)
-                *reinterpret_cast<uint4*>(g.narrow[keys] + (t * n + head) * g.row + c) = narrowed(eight_of(from.p + t * from.token + head * from.head, c, g.dim), f);
+                *reinterpret_cast<uint4*>(g.narrow[keys] + (t * n + head) * g.row + c) = narrowed(own_of(eight_of<true>(from.p + t * from.token + head * from.head, c, g.dim, t == g.tokens - 1 && head == n - 1)), f);
         }
     }
 }
@@ -393,7 +414,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         } else if (warp == 9) {
             // multiply: scores and dp of a tile, then dq of the one before, through all items
-            const uint32_t id_s = attend_desc(true, false, kKeys), id_dp = attend_desc(F16, false, kKeys), id_acc = attend_desc(true, true, 64 * HALVES);
+            const uint32_t id_s = attend_desc(true, false, kKeys), id_dp = attend_desc(F16, false, kKeys), id_acc = attend_desc(true, true, 16 * ((g.dim + 15) / 16));
             const int steps = (g.dim + 15) / 16;
             uint32_t t = 0, items = 0;  // tiles and items begun
             int tiles = 0, j = 0;       // of the present item, tile j from the last on
@@ -745,8 +766,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         } else if (warp == 9) {
             // multiply: each product with the queries or dout, and behind it the next tile's scores or dp in the place of what it used
-            const uint32_t id_s = attend_desc(true, false, kRows), id_dp = attend_desc(F16, false, kRows), id_dk = attend_desc(true, true, 64 * HALVES),
-                           id_dv = attend_desc(F16, true, 64 * HALVES);
+            const uint32_t id_s = attend_desc(true, false, kRows), id_dp = attend_desc(F16, false, kRows), id_dk = attend_desc(true, true, 16 * ((g.dim + 15) / 16)),
+                           id_dv = attend_desc(F16, true, 16 * ((g.dim + 15) / 16));
             const int steps = (g.dim + 15) / 16;
             uint32_t t = 0, items = 0;  // the present tile, counted through all items; items begun
             int i = 0, tiles = 0;
@@ -1022,7 +1043,7 @@ cudaError_t launch_back(const ones_heads& dout, const ones_heads& q, const ones_
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr, cfg.numAttrs = 1;
-    err = cudaLaunchKernelEx(&cfg, k_survey<F16, kLanes>, d);
+    err = cudaLaunchKernelEx(&cfg, a.dim % 8 ? k_survey<F16, kLanes, true> : k_survey<F16, kLanes, false>, d);
     if (err == cudaSuccess && !F16) err = launch_after(k_settle<kLanes>, dim3(grid < device_sms() ? grid : device_sms()), dim3(256), stream, d, const_cast<int*>(a.power));
     if (err != cudaSuccess) return err;
     static std::atomic<uint64_t> ready[2];
@@ -1072,13 +1093,12 @@ int ones_attention_backward(const ones_heads* dout, const ones_heads* q, const o
     unsigned* const largest = reinterpret_cast<unsigned*>(ws + p.at_largest);
     plan.zero = largest, plan.zeros = 4 * k->heads;
     float* const delta = reinterpret_cast<float*>(ws + p.at_delta);
-    const HeadsOut o = heads_out(*out, dim, tokens);
     auto vectors = [](const ones_heads& h) { return Vectors{static_cast<const uint16_t*>(h.d_data), h.token, h.head}; };
     int* const power = reinterpret_cast<int*>(ws + p.at_power);  // guessed, then settled
     SurveyArgs d = {vectors(*dout), vectors(*out), vectors(*v), vectors(*q), vectors(*k)};
     for (int i = 0; i < 2; ++i) d.narrow[i] = reinterpret_cast<uint16_t*>(ws + p.at_narrow[i]);
     d.plan = plan.head, d.delta = delta, d.largest = largest, d.power = power, d.tokens = tokens, d.heads = q->heads, d.kv = k->heads, d.dim = dim;
-    d.row = p.row, d.wide = o.wide;
+    d.row = p.row, d.wide = aligned(out->d_data, 16) && (out->heads <= 1 || out->head % 8 == 0) && (tokens <= 1 || out->token % 8 == 0);
     const BackArgs a = {nullptr, nullptr, d_lse, delta, largest, power + 2 * k->heads, heads_out(*dq, dim, tokens), heads_out(*dk, dim, tokens), heads_out(*dv, dim, tokens), tokens,
                         q->heads, k->heads, p.group, p.kt, dim, scale};
     const bool f16 = type == ONES_F16;

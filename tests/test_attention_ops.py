@@ -393,6 +393,32 @@ def test_attention_layouts():
     assert torch.equal(train.attention(q, one, one)[0], train.attention(q, one.contiguous(), one.contiguous())[0])
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("dim", [77, 50, 121])
+def test_attention_what_lies_between_heads_does_not_matter(dtype, dim):
+    """Heads on 16-byte boundaries that end off them: NaN or zeros behind each, and nothing behind the last."""
+    from paper_2108_03645_b200 import train
+    n, wide = 150, (dim + 7) // 8 * 8
+    plain = [randn(n, h, dim, seed=h).to(dtype) for h in (4, 2, 3, 5)]
+    plain = [plain[0], plain[1], plain[1] * 0.5, plain[0] * 0.1]
+    results = []
+    for value in (0.0, float("nan")):
+        args = []
+        for x in plain:
+            buf = torch.full((n * x.shape[1] * wide,), value, dtype=dtype, device="cuda")
+            y = buf.as_strided(x.shape, (x.shape[1] * wide, wide, 1))
+            y.copy_(x)
+            args.append(buf[:buf.numel() - wide + dim].as_strided(x.shape, (x.shape[1] * wide, wide, 1)))
+        q, k, v, dout = args
+        out, lse = train.attention(q, k, v)
+        gap = torch.full((n, 4, wide), value, dtype=dtype, device="cuda")[..., :dim]
+        gap.copy_(out)
+        results.append([out, lse, *train.attention_backward(dout, q, k, v, gap, lse)])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+    check_attention(*plain[:3], [n], plain[3])
+
+
 def test_attention_offsets_out_of_order_stay_inside():
     """Offsets count as their running maximum within [0, tokens]; what they cover no more is zeros."""
     from paper_2108_03645_b200 import train
