@@ -52,15 +52,20 @@ __device__ __forceinline__ int above(unsigned bits) { return (int)(bits >> 23) -
 // others turn out to be larger than there is room for, they are laid out again.
 constexpr int kRoom = 6;
 __device__ __forceinline__ int operand_power(unsigned bits) { return min(15 - above(bits), 100); }
+// What they are made of, as it lies in memory.
 template <bool F16>
-__device__ __forceinline__ Powers powers_of(const BackArgs& g, int h) {
-    Powers p;
-    const int bound = 8 + above(g.largest[h]) + above(g.largest[g.kv + h]);  // 2^7 >= dim
-    p.sigma = min(max(15 - bound, -100), 100);
-    p.q = F16 ? 0 : g.power[h];
-    p.k = F16 ? 0 : g.power[g.kv + h];
-    return p;
-}
+struct RawPowers {
+    unsigned dout, v;
+    int q, k;
+    __device__ __forceinline__ void fetch(const BackArgs& g, int h) {
+        dout = g.largest[h], v = g.largest[g.kv + h];
+        q = F16 ? 0 : g.power[h], k = F16 ? 0 : g.power[g.kv + h];
+    }
+    __device__ __forceinline__ Powers get() const {
+        const int bound = 8 + above(dout) + above(v);  // 2^7 >= dim
+        return {min(max(15 - bound, -100), 100), q, k};
+    }
+};
 
 // ---- delta = dout . out, the largest values, and bfloat16 queries and keys as float16 ----
 
@@ -504,22 +509,39 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (lane == 0) bar_arrive(acc_free + 8 * set.at);
             return true;
         };
-        while (ok && walk.next()) {
+        // what the next item needs of memory is fetched before the present one is worked on (128 samples of 256 tokens: 118 -> 113 us;
+        // the same in the pass over the keys, which needs the powers only: 120 -> 126)
+        struct {
+            float lse, delta;
+            RawPowers<F16> powers;
+        } ahead = {};
+        bool more;
+        auto look = [&]() {
+            more = walk.next();
+            if (!more || walk.it.begin < 0) return;
+            const int token = walk.it.first + row_token;
+            const int64_t at = (int64_t)token * g.heads + walk.it.h * g.group + row_head;
+            ahead.powers.fetch(g, walk.it.h);
+            if (row < g.group * g.kt && token < walk.it.end) ahead.lse = g.lse[at], ahead.delta = g.delta[at];
+        };
+        look();
+        while (ok && more) {
             const Work it = walk.it;
-            const int h = walk.it.h, tiles = key_tiles(it, g.kt);
+            const int h = it.h, tiles = key_tiles(it, g.kt);
             const int token = it.first + row_token, head = h * g.group + row_head;
             const bool live = row < g.group * g.kt && token < it.end;
             uint16_t* const own = live ? g.dq.p + (int64_t)token * g.dq.token + head * g.dq.head : nullptr;
+            const Powers pw = ahead.powers.get();
+            const float lse = ahead.lse, delta = live ? ahead.delta : 0.f;
+            look();
             if (it.begin < 0) {
                 if (half == 0) write_zeros(own, g.dim);
                 continue;
             }
-            const Powers pw = powers_of<F16>(g, h);
             const int lift = F16 ? kLift : 0;
             const float sigma = ldexpf(1.f, pw.sigma - lift);
             const int64_t at = (int64_t)token * g.heads + head;
-            const float delta = live ? g.delta[at] : 0.f;
-            const Pair c2 = both(ldexpf(g.scale * kLog2e, -pw.q - pw.k)), l2 = both(live ? lift - g.lse[at] * kLog2e : -INFINITY), s2 = both(sigma);
+            const Pair c2 = both(ldexpf(g.scale * kLog2e, -pw.q - pw.k)), l2 = both(live ? lift - lse * kLog2e : -INFINITY), s2 = both(sigma);
             Pair d2 = both(-delta * sigma), sum = both(0.f), lost = both(0.f);  // lost: what the rounding of ds adds to its sum
             const int clean = (it.first - it.begin + 1) / kKeys;
             for (int j = tiles - 1; j >= 0; --j, ++t) {
@@ -833,7 +855,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const Work it = walk.it;
                 const QuerySpan q = query_span(it, g.kt);
                 if (!q.tiles) continue;
-                const float sigma = ldexpf(1.f, powers_of<F16>(g, walk.it.h).sigma - (F16 ? kLift : 0));
+                RawPowers<F16> powers;
+            powers.fetch(g, it.h);
+            const float sigma = ldexpf(1.f, powers.get().sigma - (F16 ? kLift : 0));
                 for (int i = 0; i < q.tiles; ++i, ++n) {
                     const Stat stage(n);
                     float l[4], d[4];
@@ -891,7 +915,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 write_zeros(own, g.dim);
                 continue;
             }
-            const Powers pw = powers_of<F16>(g, h);
+            RawPowers<F16> powers;
+            powers.fetch(g, h);
+            const Powers pw = powers.get();
             const Pair c2 = both(ldexpf(g.scale * kLog2e, -pw.q - pw.k)), s2 = both(ldexpf(1.f, pw.sigma - (F16 ? kLift : 0)));
             const bool fine = F16 && q.tiles <= kFineTiles;
             for (int i = 0; i < q.tiles; ++i, ++t) {
