@@ -52,6 +52,9 @@ __device__ __forceinline__ int above(unsigned bits) { return (int)(bits >> 23) -
 // others turn out to be larger than there is room for, they are laid out again.
 constexpr int kRoom = 6;
 __device__ __forceinline__ int operand_power(unsigned bits) { return min(15 - above(bits), 100); }
+__device__ __forceinline__ float power2(int n) { return __int_as_float((n + 127) << 23); }  // -127 < n < 128
+// What a score is multiplied with for the exponent. (Powers that leave the range belong to scores that do.)
+__device__ __forceinline__ float exponent_factor(float scale, const Powers& p) { return scale * kLog2e * power2(min(max(-p.q - p.k, -126), 127)); }
 // What they are made of, as it lies in memory.
 template <bool F16>
 struct RawPowers {
@@ -539,11 +542,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                 continue;
             }
             const int lift = F16 ? kLift : 0;
-            const float sigma = ldexpf(1.f, pw.sigma - lift);
+            const float sigma = power2(pw.sigma - lift);
             const int64_t at = (int64_t)token * g.heads + head;
-            const Pair c2 = both(ldexpf(g.scale * kLog2e, -pw.q - pw.k)), l2 = both(live ? lift - lse * kLog2e : -INFINITY), s2 = both(sigma);
+            const Pair c2 = both(exponent_factor(g.scale, pw)), l2 = both(live ? lift - lse * kLog2e : -INFINITY), s2 = both(sigma);
             Pair d2 = both(-delta * sigma), sum = both(0.f), lost = both(0.f);  // lost: what the rounding of ds adds to its sum
-            const int clean = (it.first - it.begin + 1) / kKeys;
+            const int front = it.first + (row & ~31) / g.group - it.begin - 64 * half;  // the last key of this half that the warp's first row sees
             for (int j = tiles - 1; j >= 0; --j, ++t) {
                 if (!(ok = warp_wait(s_full + 8 * (t & 1), (t >> 1) & 1))) break;
                 mma_fence_after();
@@ -565,13 +568,20 @@ __global__ void __launch_bounds__(kThreads, 1)
                 mma_fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(dp_free);
-                if (j >= clean) {
+                if (front - j * kKeys < 63) {
                     const int last = token - it.begin - j * kKeys - 64 * half;  // the last key of this half that the row sees
 #pragma unroll
                     for (int x = 0; x < 2; ++x)
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (32 * x + i > last) s[x][i] = dp[x][i] = 0;
+                            if (32 * x + i > last) s[x][i] = 0;
+                    if (it.end - it.begin < (j + 1) * kKeys) {  // values behind the sequence's end
+#pragma unroll
+                        for (int x = 0; x < 2; ++x)
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (32 * x + i > last) dp[x][i] = 0;
+                    }
                 }
                 auto p_at = [&](int x, int i) { return pair(__uint_as_float(s[x][i]), __uint_as_float(s[x][i + 1])); };
                 auto ds_at = [&](int x, int i) { return p_at(x, i) * fma2(pair(__uint_as_float(dp[x][i]), __uint_as_float(dp[x][i + 1])), s2, d2); };
@@ -599,7 +609,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const uint32_t there = tmem + 128 * (t & 1) + 64 * (1 - half) + 32 + lanes;
                     const float2 other = tmem_get(there);
                     const float r = own_sums.x + other.x, p = own_sums.y + other.y;
-                    if (half == 0 && live) g.delta[at] = delta + ldexpf(r, -pw.sigma);
+                    if (half == 0 && live) g.delta[at] = delta + r * power2(-pw.sigma);
                     const float all = F16 ? r + own_lost + tmem_get(there + 2).x : r;
                     if (p > 0x1p-100f) d2 = d2 + both(-all / p);
                     if (F16) {  // both have read before either writes there again
@@ -643,7 +653,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (!ok) break;
             out.set(own);
-            factor = ldexpf(g.scale, -pw.sigma - pw.k);
+            factor = g.scale * power2(-pw.sigma) * power2(-pw.k);
             pending = true;
             ++items;
         }
@@ -857,7 +867,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (!q.tiles) continue;
                 RawPowers<F16> powers;
             powers.fetch(g, it.h);
-            const float sigma = ldexpf(1.f, powers.get().sigma - (F16 ? kLift : 0));
+            const float sigma = power2(powers.get().sigma - (F16 ? kLift : 0));
                 for (int i = 0; i < q.tiles; ++i, ++n) {
                     const Stat stage(n);
                     float l[4], d[4];
@@ -918,12 +928,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             RawPowers<F16> powers;
             powers.fetch(g, h);
             const Powers pw = powers.get();
-            const Pair c2 = both(ldexpf(g.scale * kLog2e, -pw.q - pw.k)), s2 = both(ldexpf(1.f, pw.sigma - (F16 ? kLift : 0)));
+            const Pair c2 = both(exponent_factor(g.scale, pw)), s2 = both(power2(pw.sigma - (F16 ? kLift : 0)));
             const bool fine = F16 && q.tiles <= kFineTiles;
             for (int i = 0; i < q.tiles; ++i, ++t) {
                 const Stat step(t);
                 const int first = q.first + i * g.kt;  // token of the tile's first row
-                const bool masked = first < it.first + kRows - 1;
+                const bool masked = (it.first + (row | 31) - first) * g.group > 64 * half;  // some row of the warp, in some column
                 const int from = (token - first) * g.group - 64 * half;  // the first column of this half that sees this key
                 const float* const st = stats + step.at * 2 * kRows + 64 * half;
                 if (!(ok = warp_wait(st_full + 8 * step.at, step.parity))) break;
@@ -966,11 +976,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                                                fma2(pair(__uint_as_float(dp[x][j]), __uint_as_float(dp[x][j + 1])), s2, pair(d.x, d.y)));
                         const float2 b = split(pair(__uint_as_float(s[x][j + 2]), __uint_as_float(s[x][j + 3])) *
                                                fma2(pair(__uint_as_float(dp[x][j + 2]), __uint_as_float(dp[x][j + 3])), s2, pair(d.z, d.w)));
-                        float v[4] = {a.x, a.y, b.x, b.y};
-                        if (masked) {
-#pragma unroll
-                            for (int y = 0; y < 4; ++y) v[y] = 32 * x + j + y < from ? 0.f : v[y];
-                        }
+                        const float v[4] = {a.x, a.y, b.x, b.y};  // 0 where the probability is
                         e[16 * x + j / 2] = pack16<true>(v[0], v[1]), e[16 * x + j / 2 + 1] = pack16<true>(v[2], v[3]);
                         if (fine) {
                             const float2 a16 = __half22float2(*reinterpret_cast<const __half2*>(&e[16 * x + j / 2]));
@@ -992,7 +998,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (!ok) break;
             out.set(own);
-            factor = half ? ldexpf(g.scale, -pw.sigma - pw.q) : ldexpf(1.f, F16 ? -kLift : 0);
+            factor = half ? g.scale * power2(-pw.sigma) * power2(-pw.q) : power2(F16 ? -kLift : 0);
             pending = true;
             ++items;
         }
