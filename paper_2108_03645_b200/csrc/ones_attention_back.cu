@@ -7,7 +7,8 @@
 // the results, or turns taken between blocks. A pair costs 1536 + 2048 cycles of products and 2 x 1024 of exponentials.
 // Measured: 16384 tokens, 16 / 4 heads of 128: 1190 us for the queries and 1640 for the keys, 1.39 and 1.34 PFLOP/s of what they
 // execute (the card at its power limit, 1.6 to 1.77 GHz). 128 samples of 256 tokens, 16 heads of 64: survey 90 us (0.47 GB in
-// and out at 5.2 TB/s), queries 121, keys 127, bound by the latency of a pair's chain of steps.
+// and out at 5.2 TB/s), queries 106, keys 102: the warps that work on scores never wait for the tensor core there, a third of their
+// time goes to the way out of the sums and to what begins and ends an item.
 //
 // What the rounding to 16 bits costs. The gradients of the scores meet q and k as float16, whatever the type of the tensors:
 // times a power of two they keep 11 bits where bfloat16 would keep 8 (error of dq 2.9e-3 of its norm, of which 1.66e-3 is the
@@ -488,8 +489,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;
         uint32_t t = 0, items = 0, mph = 0;
         uint8_t* const stage = B::kStage ? smem + (2 * B::kSets + B::kKeySlots + B::kValueSlots) * B::kTile + warp * kStageBytesOfWarp : nullptr;
-        // of the row: its token in the tile and its head in the group
-        const int row_token = row / g.group, row_head = row - row_token * g.group;
+        // of the row: its token in the tile and its head in the group; the tokens of the warp's first and last row
+        const int row_token = row / g.group, row_head = row - row_token * g.group, first_token = (row & ~31) / g.group, last_token = (row | 31) / g.group;
         // the item whose dq is still to be written
         RowsOut out = {};
         float factor = 0.f;
@@ -546,7 +547,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int64_t at = (int64_t)token * g.heads + head;
             const Pair c2 = both(exponent_factor(g.scale, pw)), l2 = both(live ? lift - lse * kLog2e : -INFINITY), s2 = both(sigma);
             Pair d2 = both(-delta * sigma), sum = both(0.f), lost = both(0.f);  // lost: what the rounding of ds adds to its sum
-            const int front = it.first + (row & ~31) / g.group - it.begin - 64 * half;  // the last key of this half that the warp's first row sees
             for (int j = tiles - 1; j >= 0; --j, ++t) {
                 if (!(ok = warp_wait(s_full + 8 * (t & 1), (t >> 1) & 1))) break;
                 mma_fence_after();
@@ -554,13 +554,33 @@ __global__ void __launch_bounds__(kThreads, 1)
                 uint32_t s[2][32], dp[2][32];
                 tmem_fetch(ts, s[0]), tmem_fetch(ts + 32, s[1]);
                 tmem_wait(s[0]), tmem_wait(s[1]);
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
+                auto probabilities = [&](uint32_t (&p)[32]) {
 #pragma unroll
                     for (int i = 0; i < 32; i += 2) {
-                        const float2 e = split(fma2(pair(__uint_as_float(s[x][i]), __uint_as_float(s[x][i + 1])), c2, l2));
-                        s[x][i] = __float_as_uint(exp2_of(e.x)), s[x][i + 1] = __float_as_uint(exp2_of(e.y));
+                        const float2 e = split(fma2(pair(__uint_as_float(p[i]), __uint_as_float(p[i + 1])), c2, l2));
+                        p[i] = __float_as_uint(exp2_of(e.x)), p[i + 1] = __float_as_uint(exp2_of(e.y));
                     }
+                };
+                // of this half: the last key that the row sees, that the warp's first and that its last row does
+                const int last = token - it.begin - j * kKeys - 64 * half, low = last - (row_token - first_token), high = low + (last_token - first_token);
+                if (low >= 63) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) probabilities(s[x]);
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        if (high < 32 * x) {  // none of the warp's rows sees any of these keys
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) s[x][i] = 0;
+                            continue;
+                        }
+                        probabilities(s[x]);
+                        if (low >= 32 * x + 31) continue;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (32 * x + i > last) s[x][i] = 0;
+                    }
+                }
                 if (!(ok = warp_wait(dp_full, t & 1))) break;
                 mma_fence_after();
                 tmem_fetch(t_dp + 64 * half + lanes, dp[0]), tmem_fetch(t_dp + 64 * half + 32 + lanes, dp[1]);
@@ -568,20 +588,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                 mma_fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(dp_free);
-                if (front - j * kKeys < 63) {
-                    const int last = token - it.begin - j * kKeys - 64 * half;  // the last key of this half that the row sees
+                if (it.end - it.begin < (j + 1) * kKeys) {  // values behind the sequence's end
 #pragma unroll
                     for (int x = 0; x < 2; ++x)
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (32 * x + i > last) s[x][i] = 0;
-                    if (it.end - it.begin < (j + 1) * kKeys) {  // values behind the sequence's end
-#pragma unroll
-                        for (int x = 0; x < 2; ++x)
-#pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (32 * x + i > last) dp[x][i] = 0;
-                    }
+                            if (32 * x + i > last) dp[x][i] = 0;
                 }
                 auto p_at = [&](int x, int i) { return pair(__uint_as_float(s[x][i]), __uint_as_float(s[x][i + 1])); };
                 auto ds_at = [&](int x, int i) { return p_at(x, i) * fma2(pair(__uint_as_float(dp[x][i]), __uint_as_float(dp[x][i + 1])), s2, d2); };
@@ -933,8 +945,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int i = 0; i < q.tiles; ++i, ++t) {
                 const Stat step(t);
                 const int first = q.first + i * g.kt;  // token of the tile's first row
-                const bool masked = (it.first + (row | 31) - first) * g.group > 64 * half;  // some row of the warp, in some column
-                const int from = (token - first) * g.group - 64 * half;  // the first column of this half that sees this key
+                // the first column of this half that sees this key, the warp's first and its last key
+                const int from = (token - first) * g.group - 64 * half, low = from - lane * g.group, high = low + 31 * g.group;
                 const float* const st = stats + step.at * 2 * kRows + 64 * half;
                 if (!(ok = warp_wait(st_full + 8 * step.at, step.parity))) break;
                 if (!(ok = warp_wait(s_full, t & 1))) break;
@@ -942,22 +954,38 @@ __global__ void __launch_bounds__(kThreads, 1)
                 uint32_t s[2][32], dp[2][32], e[32], rest[32];
                 tmem_fetch(tmem + 64 * half + lanes, s[0]), tmem_fetch(tmem + 64 * half + 32 + lanes, s[1]);
                 tmem_wait(s[0]), tmem_wait(s[1]);
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
+                auto probabilities = [&](int x) {
 #pragma unroll
                     for (int j = 0; j < 32; j += 4) {
                         const float4 l = *reinterpret_cast<const float4*>(st + 32 * x + j);
                         const float2 a = split(fma2(pair(__uint_as_float(s[x][j]), __uint_as_float(s[x][j + 1])), c2, pair(l.x, l.y)));
                         const float2 b = split(fma2(pair(__uint_as_float(s[x][j + 2]), __uint_as_float(s[x][j + 3])), c2, pair(l.z, l.w)));
-                        float p[4] = {exp2_of(a.x), exp2_of(a.y), exp2_of(b.x), exp2_of(b.y)};
-                        if (masked) {
-#pragma unroll
-                            for (int y = 0; y < 4; ++y) p[y] = 32 * x + j + y < from ? 0.f : p[y];
-                        }
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) s[x][j + y] = __float_as_uint(p[y]);
-                        e[16 * x + j / 2] = pack16<F16>(p[0], p[1]), e[16 * x + j / 2 + 1] = pack16<F16>(p[2], p[3]);
+                        s[x][j] = __float_as_uint(exp2_of(a.x)), s[x][j + 1] = __float_as_uint(exp2_of(a.y));
+                        s[x][j + 2] = __float_as_uint(exp2_of(b.x)), s[x][j + 3] = __float_as_uint(exp2_of(b.y));
                     }
+                };
+                if (high <= 0) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) probabilities(x);
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        if (low >= 32 * x + 32) {  // none of these queries sees any of the warp's keys
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) s[x][j] = 0;
+                            continue;
+                        }
+                        probabilities(x);
+                        if (high <= 32 * x) continue;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (32 * x + j < from) s[x][j] = 0;
+                    }
+                }
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int j = 0; j < 32; j += 2) e[16 * x + j / 2] = pack16<F16>(__uint_as_float(s[x][j]), __uint_as_float(s[x][j + 1]));
                 tmem_store(tmem + 64 * half + lanes, e);
                 tmem_store_wait();
                 mma_fence_before();
