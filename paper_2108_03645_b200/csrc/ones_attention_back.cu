@@ -311,7 +311,7 @@ struct Back {
 
 struct QueriesShared {
     uint64_t q_full[2], q_free[2], k_full[4], k_raw[4], k_empty[4], v_full[4], v_empty[4], s_full[2], dp_full, dp_free, ds_full[2], acc_full[2],
-        acc_free[2], met;
+        acc_free[2], met[4];
     uint32_t tmem;
 };
 
@@ -338,10 +338,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t q_full = smem_u32(sh.q_full), q_free = smem_u32(sh.q_free), k_full = smem_u32(sh.k_full), k_raw = smem_u32(sh.k_raw),
                    k_empty = smem_u32(sh.k_empty), v_full = smem_u32(sh.v_full), v_empty = smem_u32(sh.v_empty), s_full = smem_u32(sh.s_full),
                    dp_full = smem_u32(&sh.dp_full), dp_free = smem_u32(&sh.dp_free), ds_full = smem_u32(sh.ds_full),
-                   acc_full = smem_u32(sh.acc_full), acc_free = smem_u32(sh.acc_free), met = smem_u32(&sh.met);
+                   acc_full = smem_u32(sh.acc_full), acc_free = smem_u32(sh.acc_free), met = smem_u32(sh.met) + 8 * (warp % 4);  // of the two warps that have the same rows
     if (threadIdx.x == 0) {
         tma_prefetch(&map_q), tma_prefetch(&map_do), tma_prefetch(&map_k), tma_prefetch(&map_v);
-        bar_init(dp_full, 1), bar_init(dp_free, 8), bar_init(met, 8);
+        bar_init(dp_full, 1), bar_init(dp_free, 8);
+        for (int i = 0; i < 4; ++i) bar_init(smem_u32(&sh.met[i]), 2);
         for (int i = 0; i < 2; ++i) {
             bar_init(q_full + 8 * i, 1), bar_init(q_free + 8 * i, 1), bar_init(s_full + 8 * i, 1), bar_init(ds_full + 8 * i, 8);
             bar_init(acc_full + 8 * i, 1), bar_init(acc_free + 8 * i, 8);
