@@ -441,12 +441,13 @@ cudaError_t launch(Args& a, bool back, cudaStream_t stream, int* blocks) {
     while ((1 << a.group_log) * U < units) ++a.group_log;
     const int groups = kThreads >> a.group_log, heads = max(1, a.side[0].heads + a.side[1].heads);
     // Tokens of a block at a time: enough vectors for sixteen rounds of all groups, so that the angles and the barriers around them
-    // weigh little (65536 x 40 x 128 forward: four rounds 305 us, eight 274, sixteen 242), and fewer where that leaves SMs idle.
-    // Their angles take 32 KB at most, so that five blocks are on an SM.
+    // weigh little (65536 x 40 x 128 forward: four rounds 305 us, eight 274, sixteen 242), or fewer, so that all blocks together take
+    // a whole number of turns. Their angles take 32 KB at most, so that five blocks are on an SM.
     a.angles = (a.rotary / 2 + 3) / 4 * 4;
     for (Side& s : a.side) s.step_t = groups / max(s.heads, 1), s.step_h = groups - s.step_t * s.heads;
-    a.tile = max(1, min(min(64, 16 * groups / heads), 4096 / max(a.angles, 1)));
-    while (a.tile > 1 && (a.tokens - 1) / a.tile + 1 < 5 * device_sms()) a.tile = (a.tile + 1) / 2;
+    const int most = max(1, min(min(64, 16 * groups / heads), 4096 / max(a.angles, 1)));
+    const int64_t slots = (back ? 2 : 5) * device_sms(), turns = (a.tokens - 1) / (most * slots) + 1;
+    a.tile = (int)((a.tokens - 1) / (turns * slots)) + 1;
     const int tiles = (a.tokens - 1) / a.tile + 1;
     *blocks = back ? min(tiles, kMaxBlocks) : tiles;
     const int smem = max(2 * a.tile * a.angles * 4 + (back && V > 1 ? kRingBytes : 0), back && a.part ? groups * a.dim * 4 : 0);
