@@ -7,7 +7,7 @@
 // the results, or turns taken between blocks. A pair costs 1536 + 2048 cycles of products and 2 x 1024 of exponentials.
 // Measured: 16384 tokens, 16 / 4 heads of 128: 1190 us for the queries and 1640 for the keys, 1.39 and 1.34 PFLOP/s of what they
 // execute (the card at its power limit, 1.6 to 1.77 GHz). 128 samples of 256 tokens, 16 heads of 64: survey 90 us (0.47 GB in
-// and out at 5.2 TB/s), queries 106, keys 102: the warps that work on scores never wait for the tensor core there, a third of their
+// and out at 5.2 TB/s), queries 102, keys 102: the warps that work on scores never wait for the tensor core there, a third of their
 // time goes to the way out of the sums and to what begins and ends an item.
 //
 // What the rounding to 16 bits costs. The gradients of the scores meet q and k as float16, whatever the type of the tensors:
