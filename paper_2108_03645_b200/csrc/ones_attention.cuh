@@ -205,7 +205,7 @@ __host__ inline HeadsOut heads_out(const ones_heads& h, int dim, int tokens) {
 // own, or by shuffles where shared memory is full) until each has the same piece of four rows, and write 64 bytes of a row
 // together; predicated, since each branch around a store costs 100 cycles. Rows off 16-byte boundaries: 16 lanes exchange words,
 // and write a row by 2 bytes (15 heads of 77 values, 16 thousand tokens: 260 us for the forward pass with lanes that write
-// their own rows, 123 so).
+// their own rows, 114 so).
 constexpr int kStageBytesOfWarp = 32 * 64;
 struct RowsOut {
     unsigned long long own;   // 0: not there

@@ -286,7 +286,8 @@ __global__ void __launch_bounds__(kThreads, BACK ? 2 : 5) k_qk_norm(const __grid
     int now = 0;  // the slot of the present vector
     if (kRing) {
 #pragma unroll
-        for (int i = 0; i < kPieces * kStages; ++i) ring[i * kThreads] = make_uint4(0, 0, 0, 0);  // pieces that are not there stay so
+        for (int i = 0; i < kPieces * kStages; ++i)
+            if ((i & 1 ? unit[0].b : unit[0].a) >= g.dim) ring[i * kThreads] = make_uint4(0, 0, 0, 0);  // pieces that are not there
 #pragma unroll
         for (int i = 0; i < kStages - 1; ++i) copy_next();
     }
