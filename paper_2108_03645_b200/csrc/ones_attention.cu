@@ -148,6 +148,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const PlanArgs a) {
 
 constexpr int kThreads = 384;  // two groups of softmax warps, then load, two that multiply, and one that clears
 constexpr float kGrow = 8.f;   // a row's maximum may grow by so much (log2 of the exponentials) before it is followed
+constexpr float kFar = 16384.f;  // up to here the rounding of a maximum (log2 of the exponentials) is below 2^-10, and common to its row
 
 struct ForwardArgs {
     const Item* items;
@@ -487,12 +488,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                             piece_top(s[x]);
                         }
                     }
-                    float tile_top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-                    if (tile_top == -INFINITY) tile_top = j ? m_row : 0.f;
+                    const float tile_top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+                    // A row that has only met scores of -infinity keeps that as its maximum, so that whatever comes next is followed.
                     if (j == 0) {
                         m_row = tile_top;
                     } else if (__any_sync(0xFFFFFFFFu, live && (tile_top - m_row) * c > kGrow)) {  // rows that are not there have no say
-                        const float next = fmaxf(m_row, tile_top), f = exp2_of((m_row - next) * c);
+                        const float next = fmaxf(m_row, tile_top), f = next > m_row ? exp2_of((m_row - next) * c) : 1.f;
                         m_row = next;
                         sum = sum * both(f);
                         if (!(ok = warp_wait(o_full + 8 * which, (count & 1) ^ 1))) break;  // the product of the tile before
@@ -508,7 +509,21 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                         tmem_store_wait();
                     }
-                    const Pair c2 = both(c), t2 = both(-m_row * c);
+                    // (s - maximum) c as one multiplication and addition is off by 2^-24 |maximum c|, since only one of the products is rounded.
+                    // Where that is not small, the maximum is subtracted first; not where it is -infinity.
+                    const float shift = m_row * c;
+                    const bool far = live && !(fabsf(shift) < kFar);
+                    if (__any_sync(0xFFFFFFFFu, far)) {
+                        const Pair top2 = both(far && m_row > -INFINITY ? -m_row : 0.f);
+#pragma unroll
+                        for (int x = 0; x < 4; ++x)
+#pragma unroll
+                            for (int i = 0; i < 32; i += 2) {
+                                const float2 d = split(pair(__uint_as_float(s[x][i]), __uint_as_float(s[x][i + 1])) + top2);
+                                s[x][i] = __float_as_uint(d.x), s[x][i + 1] = __float_as_uint(d.y);
+                            }
+                    }
+                    const Pair c2 = both(c), t2 = both(far ? 0.f : -shift);
                     auto probability = [&](uint32_t lo, uint32_t hi) {
                         const float2 e = split(fma2(pair(__uint_as_float(lo), __uint_as_float(hi)), c2, t2));
                         const float a = exp2_of(e.x), b = exp2_of(e.y);
