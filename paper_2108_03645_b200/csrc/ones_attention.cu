@@ -177,6 +177,7 @@ struct Forward {
 struct ForwardShared {
     uint64_t q_full[2][2], q_free[2][2], full[8], raw[8], empty[8], s_full[2], p_full[2], o_full[2], acc_full[2][2], acc_free[2][2];
     uint32_t tmem;
+    volatile uint32_t loads;  // how many tiles have been sent for: what the other warps' waits go by
 };
 
 // A tile of queries of an item: its first token, how many tiles of keys it meets.
@@ -209,6 +210,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                    empty = smem_u32(sh.empty), s_full = smem_u32(sh.s_full), p_full = smem_u32(sh.p_full), o_full = smem_u32(sh.o_full),
                    acc_full = smem_u32(sh.acc_full), acc_free = smem_u32(sh.acc_free);
     if (threadIdx.x == 0) {
+        sh.loads = 0;
         tma_prefetch(&map_q), tma_prefetch(&map_k), tma_prefetch(&map_v);
         for (int i = 0; i < 2; ++i) bar_init(s_full + 8 * i, 1), bar_init(p_full + 8 * i, 4), bar_init(o_full + 8 * i, 1);
         for (int i = 0; i < 4; ++i) bar_init(q_full + 8 * i, 1), bar_init(q_free + 8 * i, 1), bar_init(acc_full + 8 * i, 1), bar_init(acc_free + 8 * i, 4);
@@ -230,8 +232,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto first_product = [&](int which, uint32_t item, int j, int tiles, uint32_t slot, uint32_t parity) {
         const Set set(item);
         const uint32_t bar = 8 * (2 * which + set.at);
-        if (j == 0 && !warp_wait(q_full + bar, set.parity)) return false;
-        if (!warp_wait(full + 8 * slot, parity)) return false;
+        if (j == 0 && !warp_wait(q_full + bar, set.parity, &sh.loads)) return false;
+        if (!warp_wait(full + 8 * slot, parity, &sh.loads)) return false;
         mma_fence_after();
         if (elect_one()) {
             product_rows<HALVES>(tmem + 128 * which, base + (which * F::kSets + set.at) * F::kTile, ring + slot * F::kTile, attend_desc(F16, false, kKeys),
@@ -245,9 +247,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto second_product = [&](int which, uint32_t item, int j, int tiles, uint32_t slot, uint32_t parity, uint32_t count) {
         const Set set(item);
         const uint32_t bar = 8 * (2 * which + set.at), to = tmem + 256 + 128 * which + 64 * set.at, ts = tmem + 128 * which;
-        if (!warp_wait(full + 8 * slot, parity)) return false;
-        if (j == 0 && !warp_wait(acc_free + bar, set.parity ^ 1)) return false;
-        if (!warp_wait(p_full + 8 * which, count & 1)) return false;
+        if (!warp_wait(full + 8 * slot, parity, &sh.loads)) return false;
+        if (j == 0 && !warp_wait(acc_free + bar, set.parity ^ 1, &sh.loads)) return false;
+        if (!warp_wait(p_full + 8 * which, count & 1, &sh.loads)) return false;
         mma_fence_after();
         if (elect_one()) {
             product_tmem(to, ts, ts + 32, ring + slot * F::kTile, attend_desc(F16, true, 16 * ((g.dim + 15) / 16)), j != 0);
@@ -293,6 +295,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         for (int y = 0; y < HALVES; ++y)
                             tma_load<1>(ring + slot.at * F::kTile + y * kHalfTile, values ? &map_v : &map_k, 64 * y, walk.it.h, it.begin + i / 2 * kKeys, bar);
                     }
+                    if (lane == 0) sh.loads = n + 1;
                     __syncwarp();
                 }
             }
@@ -307,7 +310,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int rest = it.end - it.begin - (tiles - 1) * kKeys;
                 if (rest >= kKeys) continue;
                 const At slot(n - 1);
-                if (!(ok = warp_wait(raw + 8 * slot.at, parities >> slot.at & 1))) break;
+                if (!(ok = warp_wait(raw + 8 * slot.at, parities >> slot.at & 1, &sh.loads))) break;
                 parities ^= 1u << slot.at;
                 clear_rows<HALVES>(smem + (2 * F::kSets + slot.at) * F::kTile, rest, lane);
                 if (lane == 0) bar_arrive(full + 8 * slot.at);
@@ -332,7 +335,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (;;) {
                     for (int i = 2 * j; i < 2 * most; ++i) {
                         const At slot(n + i);
-                        if (!(ok = warp_wait(full + 8 * slot.at, slot.parity))) return false;
+                        if (!(ok = warp_wait(full + 8 * slot.at, slot.parity, &sh.loads))) return false;
                         if (lane == 0) bar_arrive(empty + 8 * slot.at);
                         __syncwarp();
                     }
@@ -416,7 +419,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         auto write = [&](uint32_t item) {
             const Set set(item);
             const uint32_t bar = 8 * (2 * which + set.at);
-            if (!warp_wait(acc_full + bar, set.parity)) return false;
+            if (!warp_wait(acc_full + bar, set.parity, &sh.loads)) return false;
             mma_fence_after();
             const float inv = __frcp_rn(l);
 #pragma unroll 1
@@ -453,7 +456,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             Pair sum = both(0.f);
             for (int j = 0; j < max(tiles, 1); ++j) {
                 if (tiles) {
-                    if (!(ok = warp_wait(s_full + 8 * which, count & 1))) break;
+                    if (!(ok = warp_wait(s_full + 8 * which, count & 1, &sh.loads))) break;
                     mma_fence_after();
                     // The last keys of the tile that the row and the warp's first row may see. Where all rows of the warp see the whole tile,
                     // the work is one run of code; elsewhere pieces of 32 keys that none sees are left out, and only those that not all
@@ -496,7 +499,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         const float next = fmaxf(m_row, tile_top), f = next > m_row ? exp2_of((m_row - next) * c) : 1.f;
                         m_row = next;
                         sum = sum * both(f);
-                        if (!(ok = warp_wait(o_full + 8 * which, (count & 1) ^ 1))) break;  // the product of the tile before
+                        if (!(ok = warp_wait(o_full + 8 * which, (count & 1) ^ 1, &sh.loads))) break;  // the product of the tile before
                         mma_fence_after();
                         const uint32_t acc = to + 64 * Set(items).at;
                         for (int x = 0; x < 2 * HALVES; ++x) {

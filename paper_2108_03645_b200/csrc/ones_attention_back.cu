@@ -313,6 +313,7 @@ struct QueriesShared {
     uint64_t q_full[2], q_free[2], k_full[4], k_raw[4], k_empty[4], v_full[4], v_empty[4], s_full[2], dp_full, dp_free, ds_full[2], acc_full[2],
         acc_free[2], met[4];
     uint32_t tmem;
+    volatile uint32_t loads;  // how many tiles have been sent for: what the other warps' waits go by
 };
 
 // Tiles of keys that a tile of queries meets; they are taken from the last to the first.
@@ -340,6 +341,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                    dp_full = smem_u32(&sh.dp_full), dp_free = smem_u32(&sh.dp_free), ds_full = smem_u32(sh.ds_full),
                    acc_full = smem_u32(sh.acc_full), acc_free = smem_u32(sh.acc_free), met = smem_u32(sh.met) + 8 * (warp % 4);  // of the two warps that have the same rows
     if (threadIdx.x == 0) {
+        sh.loads = 0;
         tma_prefetch(&map_q), tma_prefetch(&map_do), tma_prefetch(&map_k), tma_prefetch(&map_v);
         bar_init(dp_full, 1), bar_init(dp_free, 8);
         for (int i = 0; i < 4; ++i) bar_init(smem_u32(&sh.met[i]), 2);
@@ -404,6 +406,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         for (int x = 0; x < HALVES; ++x)
                             tma_load<1>(at_v + vs.at * B::kTile + x * kHalfTile, &map_v, 64 * x, walk.it.h, it.begin + j * kKeys, bar);
                     }
+                    if (lane == 0) sh.loads = n + 1;
                     __syncwarp();
                 }
             }
@@ -415,7 +418,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int tiles = key_tiles(it, g.kt), rest = it.end - it.begin - (tiles - 1) * kKeys;
                 if (tiles && rest < kKeys) {
                     const KeySlot ks(n);
-                    if (!(ok = warp_wait(k_raw + 8 * ks.at, parities >> ks.at & 1))) break;
+                    if (!(ok = warp_wait(k_raw + 8 * ks.at, parities >> ks.at & 1, &sh.loads))) break;
                     parities ^= 1u << ks.at;
                     clear_rows<HALVES>(smem + (2 * B::kSets + ks.at) * B::kTile, rest, lane);
                     if (lane == 0) bar_arrive(k_full + 8 * ks.at);
@@ -445,16 +448,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const KeySlot ks(t);
                     const ValueSlot vs(t);
                     const uint32_t at_q = base + 2 * set.at * B::kTile;
-                    if (j == tiles - 1 && !(ok = warp_wait(q_full + 8 * set.at, set.parity))) break;
-                    if (!(ok = warp_wait(k_full + 8 * ks.at, ks.parity))) break;
+                    if (j == tiles - 1 && !(ok = warp_wait(q_full + 8 * set.at, set.parity, &sh.loads))) break;
+                    if (!(ok = warp_wait(k_full + 8 * ks.at, ks.parity, &sh.loads))) break;
                     mma_fence_after();
                     if (elect_one()) {
                         product_rows<HALVES>(tmem + 128 * (t & 1), at_q, at_k + ks.at * B::kTile, id_s, steps);
                         mma_commit<1>(s_full + 8 * (t & 1));
                     }
                     __syncwarp();
-                    if (!(ok = warp_wait(v_full + 8 * vs.at, vs.parity))) break;
-                    if (!(ok = warp_wait(dp_free, (t & 1) ^ 1))) break;  // what was there has been read
+                    if (!(ok = warp_wait(v_full + 8 * vs.at, vs.parity, &sh.loads))) break;
+                    if (!(ok = warp_wait(dp_free, (t & 1) ^ 1, &sh.loads))) break;  // what was there has been read
                     mma_fence_after();
                     if (elect_one()) {
                         product_rows<HALVES>(t_dp, at_q + B::kTile, at_v + vs.at * B::kTile, id_dp, steps);
@@ -468,8 +471,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const uint32_t i = t - 1;
                     const Set set(before.item);
                     const KeySlot ks(i);
-                    if (!(ok = warp_wait(ds_full + 8 * (i & 1), (i >> 1) & 1))) break;
-                    if (before.first && !(ok = warp_wait(acc_free + 8 * set.at, set.parity ^ 1))) break;
+                    if (!(ok = warp_wait(ds_full + 8 * (i & 1), (i >> 1) & 1, &sh.loads))) break;
+                    if (before.first && !(ok = warp_wait(acc_free + 8 * set.at, set.parity ^ 1, &sh.loads))) break;
                     mma_fence_after();
                     if (elect_one()) {
                         const uint32_t a = tmem + 128 * (i & 1), k = at_k + ks.at * B::kTile, acc = t_acc + 64 * set.at;
@@ -498,7 +501,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         bool pending = false;
         auto write = [&](uint32_t item) {
             const Set set(item);
-            if (!warp_wait(acc_full + 8 * set.at, set.parity)) return false;
+            if (!warp_wait(acc_full + 8 * set.at, set.parity, &sh.loads)) return false;
             mma_fence_after();
 #pragma unroll 1
             for (int x = 0; x < HALVES; ++x) {
@@ -549,7 +552,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const Pair c2 = both(exponent_factor(g.scale, pw)), l2 = both(live ? lift - lse * kLog2e : -INFINITY), s2 = both(sigma);
             Pair d2 = both(-delta * sigma), sum = both(0.f), lost = both(0.f);  // lost: what the rounding of ds adds to its sum
             for (int j = tiles - 1; j >= 0; --j, ++t) {
-                if (!(ok = warp_wait(s_full + 8 * (t & 1), (t >> 1) & 1))) break;
+                if (!(ok = warp_wait(s_full + 8 * (t & 1), (t >> 1) & 1, &sh.loads))) break;
                 mma_fence_after();
                 const uint32_t ts = tmem + 128 * (t & 1) + 64 * half + lanes;
                 uint32_t s[2][32], dp[2][32];
@@ -582,7 +585,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             if (32 * x + i > last) s[x][i] = 0;
                     }
                 }
-                if (!(ok = warp_wait(dp_full, t & 1))) break;
+                if (!(ok = warp_wait(dp_full, t & 1, &sh.loads))) break;
                 mma_fence_after();
                 tmem_fetch(t_dp + 64 * half + lanes, dp[0]), tmem_fetch(t_dp + 64 * half + 32 + lanes, dp[1]);
                 tmem_wait(dp[0]), tmem_wait(dp[1]);
@@ -616,7 +619,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     mma_fence_before();
                     __syncwarp();
                     if (lane == 0) bar_arrive(met);
-                    if (!(ok = warp_wait(met, mph))) break;
+                    if (!(ok = warp_wait(met, mph, &sh.loads))) break;
                     mph ^= 1;
                     mma_fence_after();
                     const uint32_t there = tmem + 128 * (t & 1) + 64 * (1 - half) + 32 + lanes;
@@ -629,7 +632,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         mma_fence_before();
                         __syncwarp();
                         if (lane == 0) bar_arrive(met);
-                        if (!(ok = warp_wait(met, mph))) break;
+                        if (!(ok = warp_wait(met, mph, &sh.loads))) break;
                         mph ^= 1;
                         mma_fence_after();
                     }
@@ -690,6 +693,7 @@ struct KeysShared {
     uint64_t kv_full[2], kv_free[2], q_full[4], q_raw[4], q_empty[4], do_full[4], do_raw[4], do_empty[4], st_full[2], st_empty[2], s_full, p_full, dp_full,
         ds_full, acc_full[2], acc_free[2];
     uint32_t tmem;
+    volatile uint32_t loads;  // how many tiles have been sent for: what the other warps' waits go by
 };
 
 // Tiles of queries that see a tile of keys: from the one that holds its first token to the sequence's last.
@@ -725,6 +729,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                    dp_full = smem_u32(&sh.dp_full), ds_full = smem_u32(&sh.ds_full), acc_full = smem_u32(sh.acc_full), acc_free = smem_u32(sh.acc_free);
     const int qrows = g.group * g.kt;
     if (threadIdx.x == 0) {
+        sh.loads = 0;
         tma_prefetch(&map_q), tma_prefetch(&map_do), tma_prefetch(&map_k), tma_prefetch(&map_v);
         bar_init(s_full, 1), bar_init(p_full, 8), bar_init(dp_full, 1), bar_init(ds_full, 8);
         for (int i = 0; i < 4; ++i) {
@@ -790,6 +795,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                         __syncwarp();
                     }
+                    if (lane == 0) sh.loads = n + 1;
                 }
             }
         } else if (warp == 11) {
@@ -803,7 +809,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (!q.tiles || rest >= g.kt) continue;
                 const At slot(n - 1);
                 for (int kind = 0; kind < 2; ++kind) {
-                    if (!(ok = warp_wait((kind ? do_raw : q_raw) + 8 * slot.at, parities >> slot.at & 1))) break;
+                    if (!(ok = warp_wait((kind ? do_raw : q_raw) + 8 * slot.at, parities >> slot.at & 1, &sh.loads))) break;
                     clear_rows<HALVES>(smem + (kRing + (kind ? B::kSlots : 0) + slot.at) * B::kTile, rest * g.group, lane);
                     if (lane == 0) bar_arrive((kind ? do_full : q_full) + 8 * slot.at);
                 }
@@ -831,8 +837,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             auto rows = [&](uint32_t n, bool dp) {
                 const At slot(n);
                 const Set set(items - 1);
-                if (!dp && i == 0 && !warp_wait(kv_full + 8 * set.at, set.parity)) return false;
-                if (!warp_wait((dp ? do_full : q_full) + 8 * slot.at, slot.parity)) return false;
+                if (!dp && i == 0 && !warp_wait(kv_full + 8 * set.at, set.parity, &sh.loads)) return false;
+                if (!warp_wait((dp ? do_full : q_full) + 8 * slot.at, slot.parity, &sh.loads)) return false;
                 mma_fence_after();
                 if (elect_one()) {
                     product_rows<HALVES>(dp ? t_dp : tmem, base + (2 * set.at + dp) * B::kTile, (dp ? at_do : at_q) + slot.at * B::kTile, dp ? id_dp : id_s, steps);
@@ -848,8 +854,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const At slot(t);
                 const Set set(items - 1);
                 const bool first = i == 0, last = i + 1 == tiles, fine = F16 && tiles <= kFineTiles;
-                if (!(ok = warp_wait(p_full, t & 1))) break;
-                if (first && !(ok = warp_wait(acc_free + 8 * set.at, set.parity ^ 1))) break;
+                if (!(ok = warp_wait(p_full, t & 1, &sh.loads))) break;
+                if (first && !(ok = warp_wait(acc_free + 8 * set.at, set.parity ^ 1, &sh.loads))) break;
                 mma_fence_after();
                 if (elect_one()) {
                     product_tmem(t_dv + 64 * set.at, tmem, tmem + 64, at_do + slot.at * B::kTile, id_dv, !first);
@@ -858,7 +864,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 __syncwarp();
                 any = step();
                 if (any && !(ok = rows(t + 1, false))) break;
-                if (!(ok = warp_wait(ds_full, t & 1))) break;
+                if (!(ok = warp_wait(ds_full, t & 1, &sh.loads))) break;
                 mma_fence_after();
                 if (elect_one()) {
                     const uint32_t acc = t_dk + 64 * set.at, b = at_q + slot.at * B::kTile;
@@ -892,7 +898,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         l[x] = live ? (F16 ? kLift : 0) - g.lse[at] * kLog2e : -INFINITY;
                         d[x] = live ? -g.delta[at] * sigma : 0.f;
                     }
-                    if (!(ok = warp_wait(st_empty + 8 * stage.at, stage.parity ^ 1))) break;
+                    if (!(ok = warp_wait(st_empty + 8 * stage.at, stage.parity ^ 1, &sh.loads))) break;
                     float* const to = stats + stage.at * 2 * kRows;
 #pragma unroll
                     for (int x = 0; x < 4; ++x) to[32 * x + lane] = l[x], to[kRows + 32 * x + lane] = d[x];
@@ -912,7 +918,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         bool pending = false;
         auto write = [&](uint32_t item) {
             const Set set(item);
-            if (!warp_wait(acc_full + 8 * set.at, set.parity)) return false;
+            if (!warp_wait(acc_full + 8 * set.at, set.parity, &sh.loads)) return false;
             mma_fence_after();
 #pragma unroll 1
             for (int x = 0; x < 2 * HALVES; ++x) {
@@ -949,8 +955,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 // the first column of this half that sees this key, the warp's first and its last key
                 const int from = (token - first) * g.group - 64 * half, low = from - lane * g.group, high = low + 31 * g.group;
                 const float* const st = stats + step.at * 2 * kRows + 64 * half;
-                if (!(ok = warp_wait(st_full + 8 * step.at, step.parity))) break;
-                if (!(ok = warp_wait(s_full, t & 1))) break;
+                if (!(ok = warp_wait(st_full + 8 * step.at, step.parity, &sh.loads))) break;
+                if (!(ok = warp_wait(s_full, t & 1, &sh.loads))) break;
                 mma_fence_after();
                 uint32_t s[2][32], dp[2][32], e[32], rest[32];
                 tmem_fetch(tmem + 64 * half + lanes, s[0]), tmem_fetch(tmem + 64 * half + 32 + lanes, s[1]);
@@ -992,7 +998,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 mma_fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(p_full);
-                if (!(ok = warp_wait(dp_full, t & 1))) break;
+                if (!(ok = warp_wait(dp_full, t & 1, &sh.loads))) break;
                 mma_fence_after();
                 tmem_fetch(t_dp + 64 * half + lanes, dp[0]), tmem_fetch(t_dp + 64 * half + 32 + lanes, dp[1]);
                 tmem_wait(dp[0]), tmem_wait(dp[1]);

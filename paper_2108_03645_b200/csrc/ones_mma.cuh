@@ -136,6 +136,28 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
 // The same by a whole warp, with one answer for all of it: lanes may see the limit pass at different looks, and those that
 // give up alone would be missing where the warp meets next.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, bar_wait(bar, parity)); }
+// Waits that may span many steps of another warp of the block, which counts them in `steps` (shared memory): the limit is one for the
+// time without a step, so that they end when that warp's own waits do.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, const volatile uint32_t* steps) {
+    if (bar_try(bar, parity)) return true;
+    uint64_t begin = now_ns();
+    uint32_t seen = *steps;
+    while (!bar_try(bar, parity)) {
+        const uint64_t waited = now_ns() - begin;
+        if (waited > kShortWaitNs && waited > g_wait_limit) {
+            const uint32_t n = *steps;
+            if (n == seen) {
+                atomicExch(&g_wait_expired, 1u);
+                return false;
+            }
+            seen = n, begin += waited;
+        }
+    }
+    return true;
+}
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const volatile uint32_t* steps) {
+    return __all_sync(0xFFFFFFFFu, bar_wait(bar, parity, steps));
+}
 // The waits of a thread that comes by again and again: after one that ran out, a look is all. That is asked only where the
 // first look has found nothing: asked before it, a pass over 8192 rows of 2048 takes 22.4 us instead of 22.1.
 struct Waits {

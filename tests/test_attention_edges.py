@@ -61,3 +61,27 @@ def test_attention_first_keys_hold_the_lowest_value(first, scale, mark):
         mean = v[:first].double().cumsum(0) / torch.arange(1, first + 1, device="cuda").view(-1, 1, 1)
         size = v[:first].double().abs().cumsum(0) / torch.arange(1, first + 1, device="cuda").view(-1, 1, 1)
         close(out[:first], mean, 2.0 ** -8 * mean.abs() + (2.0 ** -8 + first * 2.0 ** -24) * size)
+
+
+@pytest.mark.parametrize("heads, kv, dim", [(1, 1, 64), (1, 1, 128), (3, 1, 64)])
+def test_attention_calls_outlast_the_limit_of_a_wait(heads, kv, dim):
+    """A long sequence whose tiles are all whole, then a short one whose last tile is not: the warps that have to do with the short one only
+    wait as long as the others are at work, whatever that takes."""
+    import ctypes as C
+    from paper_2108_03645_b200 import train
+    n = 1 << 16
+    q, k, v, dout = (randn(n + 100, h, dim, seed=h + i).bfloat16() for i, h in enumerate((heads, kv, kv, heads)))
+    offsets = torch.tensor([0, n, n + 100], device="cuda")
+    out, lse = train.attention(q, k, v, offsets)
+    want = [out, lse, *train.attention_backward(dout, q, k, v, out, lse, offsets)]
+    train.check()
+    L = train.lib()
+    assert L.ones_train_wait_limit(C.c_ulonglong(200_000)) == 0  # a fraction of each pass
+    try:
+        out, lse = train.attention(q, k, v, offsets)
+        got = [out, lse, *train.attention_backward(dout, q, k, v, out, lse, offsets)]
+        train.check()
+    finally:
+        assert L.ones_train_wait_limit(C.c_ulonglong(0)) == 0
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
