@@ -4,8 +4,8 @@
 // queries (dq: scores, dp and one product over the keys before it), then one for each tile of keys (dk and dv: scores, dp and
 // two products over the queries behind it, all heads of the group one after the other). Seven products where five would do
 // if dq were added up in memory: but that takes 64 KB of atomic additions for every pair of tiles, whose order would change
-// the results, or turns taken between blocks. A pair costs 1536 + 2048 cycles of products and 2 x 1024 of exponentials.
-// Measured: 16384 tokens, 16 / 4 heads of 128: 1190 us for the queries and 1640 for the keys, 1.39 and 1.34 PFLOP/s of what they
+// the results, or turns taken between blocks. A pair costs 2 x 2048 cycles of products (see below for the eighth) and 2 x 1024 of
+// exponentials. Measured: 16384 tokens, 16 / 4 heads of 128: 1740 us for the queries and 1690 for the keys, 1.27 and 1.30 PFLOP/s of what they
 // execute (the card at its power limit, 1.6 to 1.77 GHz). 128 samples of 256 tokens, 16 heads of 64: survey 90 us (0.47 GB in
 // and out at 5.2 TB/s), queries 102, keys 102: the warps that work on scores never wait for the tensor core there, a third of their
 // time goes to the way out of the sums and to what begins and ends an item.
@@ -14,9 +14,10 @@
 // times a power of two they keep 11 bits where bfloat16 would keep 8 (error of dq 2.9e-3 of its norm, of which 1.66e-3 is the
 // rounding of the result, before; 1.7e-3 now). bfloat16 queries and keys are laid out as float16 times a power of two for
 // each head, which is exact for all that is not below 2^-32 of the largest. And delta = dout . out takes over the rounding of
-// out: an error that all pairs of a row share. The sum of a row's ds has to be 0: what the pass over the keys finds it to be is
-// spread over the keys of the row's last tile in proportion to their probabilities, and the delta that this amounts to is
-// left for the second pass.
+// out: an error e that all pairs of a row share, and that adds e sum_j p_j k_j to its dq (with values that have a common mean, 3e-2 of
+// its norm). The sum of a row's ds has to be 0, so the pass over the queries finds e: it adds up p k beside ds k, one product more,
+// takes e times that off, and leaves the exact delta for the second pass. The last tile of a row, where e is known, needs no
+// such product: its ds are formed with the exact delta at once.
 #include "ones_attention.cuh"
 
 #include <math.h>
@@ -310,8 +311,7 @@ struct Back {
 // ---- dq ----
 
 struct QueriesShared {
-    uint64_t q_full[2], q_free[2], k_full[4], k_raw[4], k_empty[4], v_full[4], v_empty[4], s_full[2], dp_full, dp_free, ds_full[2], acc_full[2],
-        acc_free[2], met[4];
+    uint64_t q_full[2], q_free[2], k_full[4], k_raw[4], k_empty[4], v_full[4], v_empty[4], s_full, p_full, dp_full, ds_full, acc_full[2], acc_free[2], met[4];
     uint32_t tmem;
     volatile uint32_t loads;  // how many tiles have been sent for: what the other warps' waits go by
 };
@@ -337,16 +337,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint8_t* const smem = smem_raw + (base - smem_u32(smem_raw));
     const uint32_t at_k = base + 2 * B::kSets * B::kTile, at_v = at_k + B::kKeySlots * B::kTile;  // before: queries and dout of each set
     const uint32_t q_full = smem_u32(sh.q_full), q_free = smem_u32(sh.q_free), k_full = smem_u32(sh.k_full), k_raw = smem_u32(sh.k_raw),
-                   k_empty = smem_u32(sh.k_empty), v_full = smem_u32(sh.v_full), v_empty = smem_u32(sh.v_empty), s_full = smem_u32(sh.s_full),
-                   dp_full = smem_u32(&sh.dp_full), dp_free = smem_u32(&sh.dp_free), ds_full = smem_u32(sh.ds_full),
+                   k_empty = smem_u32(sh.k_empty), v_full = smem_u32(sh.v_full), v_empty = smem_u32(sh.v_empty), s_full = smem_u32(&sh.s_full),
+                   p_full = smem_u32(&sh.p_full), dp_full = smem_u32(&sh.dp_full), ds_full = smem_u32(&sh.ds_full),
                    acc_full = smem_u32(sh.acc_full), acc_free = smem_u32(sh.acc_free), met = smem_u32(sh.met) + 8 * (warp % 4);  // of the two warps that have the same rows
     if (threadIdx.x == 0) {
         sh.loads = 0;
         tma_prefetch(&map_q), tma_prefetch(&map_do), tma_prefetch(&map_k), tma_prefetch(&map_v);
-        bar_init(dp_full, 1), bar_init(dp_free, 8);
+        bar_init(s_full, 1), bar_init(p_full, 8), bar_init(dp_full, 1), bar_init(ds_full, 8);
         for (int i = 0; i < 4; ++i) bar_init(smem_u32(&sh.met[i]), 2);
         for (int i = 0; i < 2; ++i) {
-            bar_init(q_full + 8 * i, 1), bar_init(q_free + 8 * i, 1), bar_init(s_full + 8 * i, 1), bar_init(ds_full + 8 * i, 8);
+            bar_init(q_full + 8 * i, 1), bar_init(q_free + 8 * i, 1);
             bar_init(acc_full + 8 * i, 1), bar_init(acc_free + 8 * i, 8);
         }
         for (int i = 0; i < 4; ++i) {
@@ -362,7 +362,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     mma_fence_before();
     __syncthreads();
     mma_fence_after();
-    const uint32_t tmem = sh.tmem, t_dp = tmem + 256, t_acc = tmem + 384;
+    const uint32_t tmem = sh.tmem, t_dp = tmem + 128, t_acc = tmem + 256, t_pk = tmem + 384;
     Walk walk(list, g.items, g.kv);
     bool ok = true;
 
@@ -426,65 +426,75 @@ __global__ void __launch_bounds__(kThreads, 1)
                 n += tiles;
             }
         } else if (warp == 9) {
-            // multiply: scores and dp of a tile, then dq of the one before, through all items
+            // multiply: p or ds with the keys, and behind each product the next tile's scores or dp in the place of what it used
             const uint32_t id_s = attend_desc(true, false, kKeys), id_dp = attend_desc(F16, false, kKeys), id_acc = attend_desc(true, true, 16 * ((g.dim + 15) / 16));
             const int steps = (g.dim + 15) / 16;
-            uint32_t t = 0, items = 0;  // tiles and items begun
+            uint32_t t = 0, items = 0;  // the present tile, counted through all items; items begun
             int tiles = 0, j = 0;       // of the present item, tile j from the last on
-            struct {
-                bool any, first, last;
-                uint32_t item;
-            } before = {false, false, false, 0};
-            for (;;) {
-                bool any = true;
-                if (--j < 0) {
-                    while ((any = walk.next()) && !(tiles = key_tiles(walk.it, g.kt))) {}
-                    j = any ? tiles - 1 : 0;
-                    items += any;
+            auto step = [&]() {
+                if (--j >= 0) return true;
+                do {
+                    if (!walk.next()) return false;
+                    tiles = key_tiles(walk.it, g.kt);
+                } while (!tiles);
+                j = tiles - 1;
+                ++items;
+                return true;
+            };
+            auto scores = [&](uint32_t n) {
+                const Set set(items - 1);
+                const KeySlot ks(n);
+                if (j == tiles - 1 && !warp_wait(q_full + 8 * set.at, set.parity, &sh.loads)) return false;
+                if (!warp_wait(k_full + 8 * ks.at, ks.parity, &sh.loads)) return false;
+                mma_fence_after();
+                if (elect_one()) {
+                    product_rows<HALVES>(tmem, base + 2 * set.at * B::kTile, at_k + ks.at * B::kTile, id_s, steps);
+                    mma_commit<1>(s_full);
                 }
-                if (!any && !before.any) break;
-                if (any) {
-                    const Set set(items - 1);
-                    const KeySlot ks(t);
-                    const ValueSlot vs(t);
-                    const uint32_t at_q = base + 2 * set.at * B::kTile;
-                    if (j == tiles - 1 && !(ok = warp_wait(q_full + 8 * set.at, set.parity, &sh.loads))) break;
-                    if (!(ok = warp_wait(k_full + 8 * ks.at, ks.parity, &sh.loads))) break;
-                    mma_fence_after();
-                    if (elect_one()) {
-                        product_rows<HALVES>(tmem + 128 * (t & 1), at_q, at_k + ks.at * B::kTile, id_s, steps);
-                        mma_commit<1>(s_full + 8 * (t & 1));
-                    }
-                    __syncwarp();
-                    if (!(ok = warp_wait(v_full + 8 * vs.at, vs.parity, &sh.loads))) break;
-                    if (!(ok = warp_wait(dp_free, (t & 1) ^ 1, &sh.loads))) break;  // what was there has been read
-                    mma_fence_after();
-                    if (elect_one()) {
-                        product_rows<HALVES>(t_dp, at_q + B::kTile, at_v + vs.at * B::kTile, id_dp, steps);
-                        mma_commit<1>(dp_full);
-                        mma_commit<1>(v_empty + 8 * vs.at);
-                        if (j == 0) mma_commit<1>(q_free + 8 * set.at);
-                    }
+                __syncwarp();
+                return true;
+            };
+            auto products_of_dout = [&](uint32_t n) {
+                const Set set(items - 1);
+                const ValueSlot vs(n);
+                if (!warp_wait(v_full + 8 * vs.at, vs.parity, &sh.loads)) return false;
+                mma_fence_after();
+                if (elect_one()) {
+                    product_rows<HALVES>(t_dp, base + (2 * set.at + 1) * B::kTile, at_v + vs.at * B::kTile, id_dp, steps);
+                    mma_commit<1>(dp_full);
+                    mma_commit<1>(v_empty + 8 * vs.at);
+                    if (j == 0) mma_commit<1>(q_free + 8 * set.at);
+                }
+                __syncwarp();
+                return true;
+            };
+            bool any = step();
+            if (any) ok = scores(0) && products_of_dout(0);
+            while (ok && any) {
+                const Set set(items - 1);
+                const KeySlot ks(t);
+                const bool first = j == tiles - 1, last = j == 0;
+                const uint32_t k = at_k + ks.at * B::kTile;
+                if (!(ok = warp_wait(p_full, t & 1, &sh.loads))) break;
+                if (first && !(ok = warp_wait(acc_free + 8 * set.at, set.parity ^ 1, &sh.loads))) break;
+                mma_fence_after();
+                if (!last) {
+                    if (elect_one()) product_tmem(t_pk + 64 * set.at, tmem, tmem + 64, k, id_acc, !first);
                     __syncwarp();
                 }
-                if (before.any) {
-                    const uint32_t i = t - 1;
-                    const Set set(before.item);
-                    const KeySlot ks(i);
-                    if (!(ok = warp_wait(ds_full + 8 * (i & 1), (i >> 1) & 1, &sh.loads))) break;
-                    if (before.first && !(ok = warp_wait(acc_free + 8 * set.at, set.parity ^ 1, &sh.loads))) break;
-                    mma_fence_after();
-                    if (elect_one()) {
-                        const uint32_t a = tmem + 128 * (i & 1), k = at_k + ks.at * B::kTile, acc = t_acc + 64 * set.at;
-                        product_tmem(acc, a, a + 64, k, id_acc, !before.first);
-                        if (F16 && before.last) product_tmem(acc, a + 32, a + 96, k, id_acc, true);
-                        mma_commit<1>(k_empty + 8 * ks.at);
-                        if (before.last) mma_commit<1>(acc_full + 8 * set.at);
-                    }
-                    __syncwarp();
+                any = step();
+                if (any && !(ok = scores(t + 1))) break;
+                if (!(ok = warp_wait(ds_full, t & 1, &sh.loads))) break;
+                mma_fence_after();
+                if (elect_one()) {
+                    product_tmem(t_acc + 64 * set.at, t_dp, t_dp + 64, k, id_acc, !first);
+                    if (F16 && last) product_tmem(t_acc + 64 * set.at, t_dp + 32, t_dp + 96, k, id_acc, true);
+                    mma_commit<1>(k_empty + 8 * ks.at);
+                    if (last) mma_commit<1>(acc_full + 8 * set.at);
                 }
-                before = {any, j == tiles - 1, j == 0, items - 1};
-                t += any;
+                __syncwarp();
+                if (any && !(ok = products_of_dout(t + 1))) break;
+                ++t;
             }
         }
     } else {
@@ -497,8 +507,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int row_token = row / g.group, row_head = row - row_token * g.group, first_token = (row & ~31) / g.group, last_token = (row | 31) / g.group;
         // the item whose dq is still to be written
         RowsOut out = {};
-        float factor = 0.f;
-        bool pending = false;
+        float factor = 0.f, excess = 0.f;  // excess: of its ds (but those of the last tile), for each p
+        bool pending = false, several = false;
         auto write = [&](uint32_t item) {
             const Set set(item);
             if (!warp_wait(acc_full + 8 * set.at, set.parity, &sh.loads)) return false;
@@ -510,6 +520,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                 uint32_t o[32];
                 tmem_fetch(t_acc + 64 * set.at + col + lanes, o);
                 tmem_wait(o);
+                if (several) {
+                    uint32_t pk[32];
+                    tmem_fetch(t_pk + 64 * set.at + col + lanes, pk);
+                    tmem_wait(pk);
+                    const Pair e2 = both(-excess);
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2) {
+                        const float2 d = split(fma2(pair(__uint_as_float(pk[i]), __uint_as_float(pk[i + 1])), e2, pair(__uint_as_float(o[i]), __uint_as_float(o[i + 1]))));
+                        o[i] = __float_as_uint(d.x), o[i + 1] = __float_as_uint(d.y);
+                    }
+                }
                 out.write<F16, WIDE>(col, g.dim, o, factor, stage);
             }
             mma_fence_before();
@@ -546,15 +567,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (half == 0) write_zeros(own, g.dim);
                 continue;
             }
-            const int lift = F16 ? kLift : 0;
+            constexpr int lift = kLift;
             const float sigma = power2(pw.sigma - lift);
+            float fix = 0.f;
             const int64_t at = (int64_t)token * g.heads + head;
             const Pair c2 = both(exponent_factor(g.scale, pw)), l2 = both(live ? lift - lse * kLog2e : -INFINITY), s2 = both(sigma);
             Pair d2 = both(-delta * sigma), sum = both(0.f), lost = both(0.f);  // lost: what the rounding of ds adds to its sum
             for (int j = tiles - 1; j >= 0; --j, ++t) {
-                if (!(ok = warp_wait(s_full + 8 * (t & 1), (t >> 1) & 1, &sh.loads))) break;
+                if (!(ok = warp_wait(s_full, t & 1, &sh.loads))) break;
                 mma_fence_after();
-                const uint32_t ts = tmem + 128 * (t & 1) + 64 * half + lanes;
+                const uint32_t ts = tmem + 64 * half + lanes, td = t_dp + 64 * half + lanes;
                 uint32_t s[2][32], dp[2][32];
                 tmem_fetch(ts, s[0]), tmem_fetch(ts + 32, s[1]);
                 tmem_wait(s[0]), tmem_wait(s[1]);
@@ -585,13 +607,20 @@ __global__ void __launch_bounds__(kThreads, 1)
                             if (32 * x + i > last) s[x][i] = 0;
                     }
                 }
-                if (!(ok = warp_wait(dp_full, t & 1, &sh.loads))) break;
-                mma_fence_after();
-                tmem_fetch(t_dp + 64 * half + lanes, dp[0]), tmem_fetch(t_dp + 64 * half + 32 + lanes, dp[1]);
-                tmem_wait(dp[0]), tmem_wait(dp[1]);
+                if (j) {
+                    uint32_t p[32];
+#pragma unroll
+                    for (int i = 0; i < 64; i += 2) p[i / 2] = pack16<true>(__uint_as_float(s[i / 32][i % 32]), __uint_as_float(s[i / 32][i % 32 + 1]));
+                    tmem_store(ts, p);
+                    tmem_store_wait();
+                }
                 mma_fence_before();
                 __syncwarp();
-                if (lane == 0) bar_arrive(dp_free);
+                if (lane == 0) bar_arrive(p_full);
+                if (!(ok = warp_wait(dp_full, t & 1, &sh.loads))) break;
+                mma_fence_after();
+                tmem_fetch(td, dp[0]), tmem_fetch(td + 32, dp[1]);
+                tmem_wait(dp[0]), tmem_wait(dp[1]);
                 if (it.end - it.begin < (j + 1) * kKeys) {  // values behind the sequence's end
 #pragma unroll
                     for (int x = 0; x < 2; ++x)
@@ -602,32 +631,25 @@ __global__ void __launch_bounds__(kThreads, 1)
                 auto p_at = [&](int x, int i) { return pair(__uint_as_float(s[x][i]), __uint_as_float(s[x][i + 1])); };
                 auto ds_at = [&](int x, int i) { return p_at(x, i) * fma2(pair(__uint_as_float(dp[x][i]), __uint_as_float(dp[x][i + 1])), s2, d2); };
                 if (j == 0) {
-                    // the last tile: what the row's ds add up to goes into its delta
-                    Pair p2 = both(0.f);
+                    // the last tile: what the row's ds add up to is what its delta is off by
 #pragma unroll
                     for (int x = 0; x < 2; ++x)
 #pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            sum = sum + ds_at(x, i);
-                            p2 = p2 + p_at(x, i);
-                        }
-                    // the other half of the columns is with the warp of the same lanes: they meet in columns that scores have left
-                    const float2 own_sums = make_float2(total(sum), total(p2));
-                    const float own_lost = F16 ? total(lost) : 0.f;
-                    tmem_put(ts + 32, own_sums.x, own_sums.y);
-                    if (F16) tmem_put(ts + 34, own_lost, 0.f);
+                        for (int i = 0; i < 32; i += 2) sum = sum + ds_at(x, i);
+                    // the other half of the columns is with the warp of the same lanes: they meet in columns that dp has left
+                    const float own_sum = total(sum), own_lost = total(lost);
+                    tmem_put(td + 32, own_sum, own_lost);
                     mma_fence_before();
                     __syncwarp();
                     if (lane == 0) bar_arrive(met);
                     if (!(ok = warp_wait(met, mph, &sh.loads))) break;
                     mph ^= 1;
                     mma_fence_after();
-                    const uint32_t there = tmem + 128 * (t & 1) + 64 * (1 - half) + 32 + lanes;
-                    const float2 other = tmem_get(there);
-                    const float r = own_sums.x + other.x, p = own_sums.y + other.y;
+                    const float2 other = tmem_get(t_dp + 64 * (1 - half) + 32 + lanes);
+                    const float r = own_sum + other.x;
                     if (half == 0 && live) g.delta[at] = delta + r * power2(-pw.sigma);
-                    const float all = F16 ? r + own_lost + tmem_get(there + 2).x : r;
-                    if (p > 0x1p-100f) d2 = d2 + both(-all / p);
+                    fix = (r + (own_lost + other.y)) * power2(-lift);
+                    d2 = d2 + both(-fix);
                     if (F16) {  // both have read before either writes there again
                         mma_fence_before();
                         __syncwarp();
@@ -646,22 +668,21 @@ __global__ void __launch_bounds__(kThreads, 1)
                         const float2 f = split(v);
                         const uint32_t d = pack16<true>(f.x, f.y);
                         ds[16 * x + i / 2] = d;
-                        sum = sum + v;
+                        const float2 e = __half22float2(*reinterpret_cast<const __half2*>(&d));
+                        const Pair off = fma2(both(-1.f), v, pair(e.x, e.y));
+                        sum = sum + v, lost = lost + off;
                         if (F16) {
-                            const float2 e = __half22float2(*reinterpret_cast<const __half2*>(&d));
-                            const Pair off = fma2(both(-1.f), v, pair(e.x, e.y));
-                            lost = lost + off;
                             const float2 o = split(off);
                             rest[16 * x + i / 2] = pack16<true>(-o.x, -o.y);
                         }
                     }
                 // float16 tensors: the last tile, which is the only one of short rows, has two terms
-                if (F16 && j == 0) tmem_store(ts + 32, rest);
-                tmem_store(ts, ds);
+                if (F16 && j == 0) tmem_store(td + 32, rest);
+                tmem_store(td, ds);
                 tmem_store_wait();
                 mma_fence_before();
                 __syncwarp();
-                if (lane == 0) bar_arrive(ds_full + 8 * (t & 1));
+                if (lane == 0) bar_arrive(ds_full);
                 if (j == tiles - 1 && pending) {
                     pending = false;
                     if (!(ok = write(items - 1))) break;
@@ -670,6 +691,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!ok) break;
             out.set(own);
             factor = g.scale * power2(-pw.sigma) * power2(-pw.k);
+            excess = fix, several = tiles > 1;
             pending = true;
             ++items;
         }

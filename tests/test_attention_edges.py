@@ -85,3 +85,78 @@ def test_attention_calls_outlast_the_limit_of_a_wait(heads, kv, dim):
         assert L.ones_train_wait_limit(C.c_ulonglong(0)) == 0
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+def gradients64(q, k, v, dout, scale):
+    """Gradients of one sequence and bounds of their errors: {name: (value, bound)}."""
+    u, f16 = U[q.dtype], q.dtype == F16
+    n, h, d = q.shape
+    kv = k.shape[1]
+    x = {"dq": q, "dk": k, "dv": v}
+    g, ge = ({name: torch.zeros_like(t, dtype=torch.float64) for name, t in x.items()} for _ in range(2))
+    mask = torch.ones(n, n, dtype=torch.bool, device="cuda").tril()
+    # float16: ds is held times a power of two that takes 2 dim |dout| |v| to 2^15 at most and 2^13 at least (two powers of two, rounded up),
+    # dim <= 128, in steps of 2^-24: off by 2^-25 2^8 / 2^13 = 2^-30 of the largest |dout| |v|, of the row for dq and of all for dk
+    step = 2.0 ** -30 if f16 else 0.0
+    for head in range(h):
+        kh = head // (h // kv)
+        a, b, c, do = (t.double() for t in (q[:, head], k[:, kh], v[:, kh], dout[:, head]))
+        s = (a @ b.T * scale).masked_fill(~mask, -math.inf)
+        # a score: sums of up to 128 products cut off at every 16 (2^-23 each), its factor and the argument of the exponential
+        se = ((a.abs() @ b.abs().T * scale) * 2.0 ** -19 + 2.0 ** -20).masked_fill(~mask, 0).amax(1, keepdim=True)
+        p = (s - torch.logsumexp(s, 1)[:, None]).exp()
+        o = p @ c
+        dp = do @ c.T
+        off = dp - (do * o).sum(1, keepdim=True)
+        ds = p * off
+        g["dv"][:, kh] += p.T @ do
+        g["dq"][:, head] = scale * ds @ b
+        g["dk"][:, kh] += scale * ds.T @ a
+        ge["dv"][:, kh] += (p * (u + 4 * se + n * 2.0 ** -22)).T @ do.abs()
+        # out is off by two roundings of u (its own and the probabilities'), and so is dout . out; dp by its 32-bit sums
+        de = (2 * u + 4 * se + n * 2.0 ** -24) * (do.abs() * (p @ c.abs())).sum(1, keepdim=True)
+        dpe = 2.0 ** -19 * ((do.abs() * o.abs()).sum(1, keepdim=True) + do.abs() @ c.abs().T)
+        # ds: its rounding, that of p, and dp's; its sum over the row, which is 0, is known to n 2^-22 of its terms (all of which shift with it by
+        # their p), but for the rounding of what they shift by
+        own = ds.abs() * (u + 4 * se + n * 2.0 ** -22) + p * dpe
+        common = p * (own.sum(1, keepdim=True) * (u + 4 * se) + ds.abs().sum(1, keepdim=True) * (n * 2.0 ** -22) + de * (u + 4 * se) +
+                      (p * dpe).sum(1, keepdim=True))
+        most = do.abs().amax(1, keepdim=True) * c.abs().max()
+        ge["dq"][:, head] += scale * (own + common + mask * most * step) @ b.abs()
+        ge["dk"][:, kh] += scale * (own + common + mask * most.max() * step).T @ a.abs()
+        if f16:
+            ge["dv"][:, kh] += 2.0 ** -37 * mask.double().T @ do.abs() + TINY[F16]
+            ge["dq"][:, head] += TINY[F16]
+            ge["dk"][:, kh] += TINY[F16]
+    return {name: (g[name], ge[name] + u * g[name].abs() + 2.0 ** -130) for name in x}
+
+
+def check_gradients(q, k, v, dout, lengths, scale=None):
+    """Every sequence by itself."""
+    from paper_2108_03645_b200 import train
+    offsets = torch.tensor([0] + lengths).cumsum(0).cuda()
+    out, lse = train.attention(q, k, v, offsets, scale=scale)
+    got = dict(zip(("dq", "dk", "dv"), train.attention_backward(dout, q, k, v, out, lse, offsets, scale=scale)))
+    for i in range(len(lengths)):
+        rows = slice(int(offsets[i]), int(offsets[i + 1]))
+        for name, (want, bound) in gradients64(q[rows], k[rows], v[rows], dout[rows], scale or q.shape[-1] ** -0.5).items():
+            close(got[name][rows], want, bound)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("heads, kv, dim", [(1, 1, 64), (2, 1, 128), (3, 1, 77)])
+@pytest.mark.parametrize("mean, recent, large", [(4, False, False), (4, True, False), (4, True, True), (0, True, True)])
+def test_attention_gradients_of_inputs_with_structure(mean, recent, large, heads, kv, dim, dtype):
+    """Values with a common mean, scores that favour the latest keys, and first keys that are large where no query looks: the rounding of
+    `out` does not show in the gradients, wherever a row's probabilities lie."""
+    n = 1000
+    q, k, v, dout = (randn(n, h, dim, seed=h + i) * f for i, (h, f) in enumerate(((heads, 1.0), (kv, 0.5), (kv, 1.0), (heads, 1.0))))
+    v += mean * (1 + 0.25 * randn(1, 1, dim, seed=9))
+    q[..., 0], k[..., 0] = 2.0, 0.0
+    if recent:
+        k[..., 0] = torch.arange(n, device="cuda").view(-1, 1) * 0.1
+    q[..., 3] = 0.0
+    if large:
+        k[:128, :, 3] = 60 * randn(128, kv, seed=7).sign()
+        k[:128, :, 0] -= 40.0
+    check_gradients(*(t.to(dtype) for t in (q, k, v, dout)), [n], scale=0.25)
