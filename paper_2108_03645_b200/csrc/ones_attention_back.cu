@@ -10,10 +10,11 @@
 // and out at 5.2 TB/s), queries 102, keys 102: the warps that work on scores never wait for the tensor core there, a third of their
 // time goes to the way out of the sums and to what begins and ends an item.
 //
-// What the rounding to 16 bits costs. The gradients of the scores meet q and k as float16, whatever the type of the tensors:
-// times a power of two they keep 11 bits where bfloat16 would keep 8 (error of dq 2.9e-3 of its norm, of which 1.66e-3 is the
-// rounding of the result, before; 1.7e-3 now). bfloat16 queries and keys are laid out as float16 times a power of two for
-// each head, which is exact for all that is not below 2^-32 of the largest. And delta = dout . out takes over the rounding of
+// What the rounding to 16 bits costs. Probabilities and the gradients of the scores (ds) are rounded to the tensors' type for their
+// products: half a step of each, averaged by the sums (bfloat16: 1.7e-3 of the norm of dq and dk, as much as the rounding of the
+// result). bfloat16 has the range for whatever ds and its operands hold; float16 takes ds times a power of two. (bfloat16 queries
+// and keys laid out as float16 times a power of two for each head left 11 bits of ds, but nothing of a sequence far below its
+// neighbours, or beside keys that hold the type's lowest value.) And delta = dout . out takes over the rounding of
 // out: an error e that all pairs of a row share, and that adds e sum_j p_j k_j to its dq (with values that have a common mean, 3e-2 of
 // its norm). The sum of a row's ds has to be 0, so the pass over the queries finds e: it adds up p k beside ds k, one product more,
 // takes e times that off, and leaves the exact delta for the second pass. The last tile of a row, where e is known, needs no
@@ -35,57 +36,47 @@ struct BackArgs {
     const PlanHead* head;
     const float* lse;           // [tokens][heads]
     float* delta;               // the same; exact from the first pass on
-    const unsigned* largest;    // [2][kv]: bits of the largest finite |dout| and |v| of a head or group
-    const int* power;           // [2][kv]: of q and k
+    const unsigned* largest;    // float16: [2][kv], bits of the largest finite |dout| and |v| of a head or group
     HeadsOut dq, dk, dv;
     int tokens, heads, kv, group, kt, dim;
     float scale;
 };
 
-// Powers of two. float16 tensors: probabilities times 2^12 for their product with dout, so that small ones keep their bits.
-// Gradients of the scores: times 2^sigma, which takes the bound 2 dim max |dout| max |v| of |dp - delta| to 2^15. bfloat16
-// queries and keys: times 2^q and 2^k, which takes their largest to 2^15.
-constexpr int kLift = 12;
-struct Powers {
-    int sigma, q, k;
-};
-__device__ __forceinline__ int above(unsigned bits) { return (int)(bits >> 23) - 126; }  // |x| < 2^above
-// The power of a head's queries or keys is guessed from those of the first token, whose largest goes to 2^(15 - kRoom); where the
-// others turn out to be larger than there is room for, they are laid out again.
-constexpr int kRoom = 6;
-__device__ __forceinline__ int operand_power(unsigned bits) { return min(15 - above(bits), 100); }
-__device__ __forceinline__ float power2(int n) { return __int_as_float((n + 127) << 23); }  // -127 < n < 128
-// What a score is multiplied with for the exponent. (Powers that leave the range belong to scores that do.)
-__device__ __forceinline__ float exponent_factor(float scale, const Powers& p) { return scale * kLog2e * power2(min(max(-p.q - p.k, -126), 127)); }
-// What they are made of, as it lies in memory.
+// float16 tensors: probabilities times 2^12 for their products, so that small ones keep their bits, and ds times 2^sigma, which takes the bound
+// 2 dim max |dout| max |v| of |dp - delta| to 2^15.
 template <bool F16>
-struct RawPowers {
-    unsigned dout, v;
-    int q, k;
+constexpr int kLift = F16 ? 12 : 0;
+__device__ __forceinline__ float power2(int n) { return __int_as_float((n + 127) << 23); }  // -127 < n < 128
+template <bool F16>
+struct Sigma {
+    unsigned dout, v;  // as they lie in memory
     __device__ __forceinline__ void fetch(const BackArgs& g, int h) {
-        dout = g.largest[h], v = g.largest[g.kv + h];
-        q = F16 ? 0 : g.power[h], k = F16 ? 0 : g.power[g.kv + h];
+        if (F16) dout = g.largest[h], v = g.largest[g.kv + h];
     }
-    __device__ __forceinline__ Powers get() const {
-        const int bound = 8 + above(dout) + above(v);  // 2^7 >= dim
-        return {min(max(15 - bound, -100), 100), q, k};
+    __device__ __forceinline__ int get() const {
+        auto above = [](unsigned bits) { return (int)(bits >> 23) - 126; };  // |x| < 2^above
+        return F16 ? min(max(15 - 8 - above(dout) - above(v), -100), 100) : 0;  // 2^7 >= dim
     }
 };
+// What the exponent of a row's probabilities subtracts. A row whose lse lies beyond 2^24, where 32 bits hold no more of its keys' shares
+// than that, has only seen keys that a mask's lowest value hides: its probabilities count as 0.
+__device__ __forceinline__ float row_shift(float lse, int lift) {
+    const float a = fabsf(lse);
+    return a >= 0x1p24f && a < INFINITY ? -INFINITY : lift - lse * kLog2e;
+}
 
-// ---- delta = dout . out, the largest values, and bfloat16 queries and keys as float16 ----
+// ---- delta = dout . out, and the largest values of float16 tensors ----
 
 struct Vectors {
     const uint16_t* p;
     int64_t token, head;
 };
 struct SurveyArgs {
-    Vectors dout, out, v, q, k;
-    uint16_t* narrow[2];  // of q and k, [tokens][heads][row]
+    Vectors dout, out, v;
     const PlanHead* plan;
     float* delta;
-    unsigned* largest;    // [4][kv]: bits of the largest finite |dout|, |v|, |q| and |k|
-    int* power;           // [2][kv]
-    int tokens, heads, kv, dim, row, wide;  // wide: out starts on 16-byte boundaries
+    unsigned* largest;  // float16: [2][kv], bits of the largest finite |dout| and |v|
+    int tokens, heads, kv, dim, wide;  // wide: out starts on 16-byte boundaries
 };
 
 template <bool F16>
@@ -123,10 +114,9 @@ struct Own {  // which of the lane's eight values the vectors have
         return RAGGED ? make_uint4(v.x & mask.x, v.y & mask.y, v.z & mask.z, v.w & mask.w) : v;
     }
 };
-// The largest finite value's bits, as a 32-bit number.
-template <bool F16>
+// The largest finite float16's bits, as a 32-bit number.
 __device__ __forceinline__ unsigned largest_of(const uint4& v) {
-    constexpr unsigned kLimit = F16 ? 0x7C00u : 0x7F80u;  // infinity
+    constexpr unsigned kLimit = 0x7C00u;  // infinity
     const uint32_t w[4] = {v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu, v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu};
     const uint32_t m = __vmaxu2(__vmaxu2(w[0], w[1]), __vmaxu2(w[2], w[3]));
     unsigned top = max(m & 0xFFFFu, m >> 16);
@@ -137,55 +127,27 @@ __device__ __forceinline__ unsigned largest_of(const uint4& v) {
             if (b < kLimit) top = max(top, b);
         }
     }
-    return __float_as_uint(value16<F16>((uint16_t)top));
-}
-// bfloat16 as float16 times a power of two.
-__device__ __forceinline__ uint4 narrowed(const uint4& v, float f) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    uint32_t r[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 x = split(pair(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u)) * both(f));
-        r[i] = pack16<true>(x.x, x.y);
-    }
-    return make_uint4(r[0], r[1], r[2], r[3]);
+    return __float_as_uint(value16<true>((uint16_t)top));
 }
 
 // LANES x 8 values are a vector, which a group of lanes takes. A block takes kTokens tokens at a time.
 constexpr int kTokens = 16;
 template <bool F16, int LANES, bool RAGGED>
 __global__ void __launch_bounds__(256, 4) k_survey(const __grid_constant__ SurveyArgs g) {
-    extern __shared__ unsigned top[];  // [4][kv], then the factors of q and k, [2][kv]
+    extern __shared__ unsigned top[];  // float16: [2][kv]
     constexpr int kGroups = 256 / LANES, kAtOnce = 4;
-    float* const factor = reinterpret_cast<float*>(top + 4 * g.kv);
     const int lane = threadIdx.x % LANES, c = 8 * lane;
     const Own<RAGGED> own_of(c, g.dim);
     wait_for_predecessor();
     let_successor_start();
     const int t0 = g.plan->covered[0], t1 = g.plan->covered[1], group = g.heads / g.kv;
-    for (int i = threadIdx.x; i < 4 * g.kv; i += 256) top[i] = 0;
+    for (int i = threadIdx.x; F16 && i < 2 * g.kv; i += 256) top[i] = 0;
     __syncthreads();
     auto note = [&](const uint4& v, int which, int h) {
-        const unsigned m = largest_of<F16>(v);
+        const unsigned m = largest_of(v);
         unsigned* const at = top + which * g.kv + h;
         if (m > *at) atomicMax(at, m);
     };
-    if (!F16) {
-        // the guess, the same by every block
-        for (int i = threadIdx.x / LANES; t0 < t1 && i < g.heads + g.kv; i += kGroups) {
-            const bool keys = i >= g.heads;
-            const int h = keys ? i - g.heads : i;
-            const Vectors& x = keys ? g.k : g.q;
-            note(own_of(eight_of<RAGGED>(x.p + t0 * x.token + h * x.head, c, g.dim, t0 == g.tokens - 1 && h == (keys ? g.kv : g.heads) - 1)), keys ? 3 : 2, keys ? h : h / group);
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < 2 * g.kv; i += 256) {
-            const int p = operand_power(top[2 * g.kv + i]) - kRoom;
-            factor[i] = exp2f((float)p);
-            if (blockIdx.x == 0) g.power[i] = p;
-        }
-        __syncthreads();
-    }
     const int own = threadIdx.x / LANES;
     const uint32_t per_head = 0xFFFFFFFFu / g.heads + 1, per_kv = 0xFFFFFFFFu / g.kv + 1, per_group = 0xFFFFFFFFu / group + 1;
     auto over = [](uint32_t r, uint32_t n, uint32_t per) { return n == 1 ? r : __umulhi(r, per); };  // r / n below 2^16, with 2^32 / n rounded up
@@ -211,7 +173,7 @@ __global__ void __launch_bounds__(256, 4) k_survey(const __grid_constant__ Surve
                 const bool live = at_t[x] < n_t;
                 float dot = 0.f;
                 a[x] = own_of(a[x]), b[x] = own_of(b[x]);
-                if (live) note(a[x], 0, over(at_h[x], group, per_group));
+                if (F16 && live) note(a[x], 0, over(at_h[x], group, per_group));
                 if (g.wide) {
                     const uint32_t u[4] = {a[x].x, a[x].y, a[x].z, a[x].w}, w[4] = {b[x].x, b[x].y, b[x].z, b[x].w};
                     Pair d = both(0.f);
@@ -233,63 +195,24 @@ __global__ void __launch_bounds__(256, 4) k_survey(const __grid_constant__ Surve
                 if (lane == 0 && live) g.delta[(int64_t)(first + at_t[x]) * g.heads + at_h[x]] = dot;
             }
         }
-        // v, then (bfloat16) q and k
+        for (int r0 = 0; F16 && r0 < n_t * g.kv; r0 += kAtOnce * kGroups) {
+            const uint16_t* const v = g.v.p + first * g.v.token;
+            uint4 a[kAtOnce];
 #pragma unroll
-        for (int kind = 0; kind < (F16 ? 1 : 3); ++kind) {
-            const Vectors& from = kind == 0 ? g.v : kind == 1 ? g.q : g.k;
-            const int n = kind == 1 ? g.heads : g.kv;
-            const uint32_t per = kind == 1 ? per_head : per_kv;
-            const uint16_t* const in = from.p + first * from.token;
-            for (int r0 = 0; r0 < n_t * n; r0 += kAtOnce * kGroups) {
-                uint4 a[kAtOnce];
+            for (int x = 0; x < kAtOnce; ++x) {
+                const int r = r0 + x * kGroups + own, t = over(r, g.kv, per_kv), h = r - t * g.kv;
+                a[x] = t < n_t ? eight_of<RAGGED>(v + t * g.v.token + h * g.v.head, c, g.dim, first + t == g.tokens - 1 && h == g.kv - 1) : make_uint4(0, 0, 0, 0);
+            }
 #pragma unroll
-                for (int x = 0; x < kAtOnce; ++x) {
-                    const int r = r0 + x * kGroups + own, t = over(r, n, per);
-                    a[x] = t < n_t ? eight_of<RAGGED>(in + t * from.token + (r - t * n) * from.head, c, g.dim, first + t == g.tokens - 1 && r - t * n == n - 1) : make_uint4(0, 0, 0, 0);
-                }
-#pragma unroll
-                for (int x = 0; x < kAtOnce; ++x) {
-                    const int r = r0 + x * kGroups + own, t = over(r, n, per);
-                    if (t >= n_t) continue;
-                    a[x] = own_of(a[x]);
-                    const int h = kind == 1 ? over(r - t * n, group, per_group) : r - t * n;
-                    note(a[x], 1 + kind, h);
-                    if (kind && c < g.row)
-                        *reinterpret_cast<uint4*>(g.narrow[kind - 1] + ((int64_t)first * n + r) * g.row + c) = narrowed(a[x], factor[(kind - 1) * g.kv + h]);
-                }
+            for (int x = 0; x < kAtOnce; ++x) {
+                const int r = r0 + x * kGroups + own, t = over(r, g.kv, per_kv);
+                if (t < n_t) note(own_of(a[x]), 1, r - t * g.kv);
             }
         }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < 4 * g.kv; i += 256)
+    for (int i = threadIdx.x; F16 && i < 2 * g.kv; i += 256)
         if (top[i]) atomicMax(g.largest + i, top[i]);
-}
-
-// Lays out again the heads whose guess was too small (or had nothing to go by). Every block looks, none writes the powers before all
-// have: the passes take them from `settled`.
-template <int LANES>
-__global__ void __launch_bounds__(256) k_settle(const __grid_constant__ SurveyArgs g, int* settled) {
-    constexpr int kGroups = 256 / LANES;
-    const int c = 8 * (threadIdx.x % LANES);
-    const Own<true> own_of(c, g.dim);
-    wait_for_predecessor();
-    let_successor_start();
-    const int t0 = g.plan->covered[0], t1 = g.plan->covered[1], group = g.heads / g.kv;
-    for (int i = 0; i < 2 * g.kv; ++i) {
-        const int guess = g.power[i], best = operand_power(g.largest[2 * g.kv + i]);
-        const bool again = best < guess || guess >= 100 - kRoom;
-        if (blockIdx.x == 0 && threadIdx.x == 0) settled[i] = again ? best : guess;
-        if (!again) continue;
-        const int keys = i >= g.kv, h = i - keys * g.kv, n = keys ? g.kv : g.heads, times = keys ? 1 : group;
-        const Vectors& from = keys ? g.k : g.q;
-        const float f = exp2f((float)best);
-        for (int64_t r = (int64_t)blockIdx.x * kGroups + threadIdx.x / LANES; r < (int64_t)(t1 - t0) * times; r += (int64_t)gridDim.x * kGroups) {
-            const int64_t t = t0 + r / times;
-            const int head = h * times + (int)(r % times);
-            if (c < g.row)
-                *reinterpret_cast<uint4*>(g.narrow[keys] + (t * n + head) * g.row + c) = narrowed(own_of(eight_of<true>(from.p + t * from.token + head * from.head, c, g.dim, t == g.tokens - 1 && head == n - 1)), f);
-        }
-    }
 }
 
 // Heads of up to 64 values leave room for two sets of what belongs to an item (its tiles in shared memory, its sums in tensor
@@ -427,7 +350,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         } else if (warp == 9) {
             // multiply: p or ds with the keys, and behind each product the next tile's scores or dp in the place of what it used
-            const uint32_t id_s = attend_desc(true, false, kKeys), id_dp = attend_desc(F16, false, kKeys), id_acc = attend_desc(true, true, 16 * ((g.dim + 15) / 16));
+            const uint32_t id_rows = attend_desc(F16, false, kKeys), id_acc = attend_desc(F16, true, 16 * ((g.dim + 15) / 16));
             const int steps = (g.dim + 15) / 16;
             uint32_t t = 0, items = 0;  // the present tile, counted through all items; items begun
             int tiles = 0, j = 0;       // of the present item, tile j from the last on
@@ -448,7 +371,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (!warp_wait(k_full + 8 * ks.at, ks.parity, &sh.loads)) return false;
                 mma_fence_after();
                 if (elect_one()) {
-                    product_rows<HALVES>(tmem, base + 2 * set.at * B::kTile, at_k + ks.at * B::kTile, id_s, steps);
+                    product_rows<HALVES>(tmem, base + 2 * set.at * B::kTile, at_k + ks.at * B::kTile, id_rows, steps);
                     mma_commit<1>(s_full);
                 }
                 __syncwarp();
@@ -460,7 +383,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (!warp_wait(v_full + 8 * vs.at, vs.parity, &sh.loads)) return false;
                 mma_fence_after();
                 if (elect_one()) {
-                    product_rows<HALVES>(t_dp, base + (2 * set.at + 1) * B::kTile, at_v + vs.at * B::kTile, id_dp, steps);
+                    product_rows<HALVES>(t_dp, base + (2 * set.at + 1) * B::kTile, at_v + vs.at * B::kTile, id_rows, steps);
                     mma_commit<1>(dp_full);
                     mma_commit<1>(v_empty + 8 * vs.at);
                     if (j == 0) mma_commit<1>(q_free + 8 * set.at);
@@ -542,7 +465,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // the same in the pass over the keys, which needs the powers only: 120 -> 126)
         struct {
             float lse, delta;
-            RawPowers<F16> powers;
+            Sigma<F16> sigma;
         } ahead = {};
         bool more;
         auto look = [&]() {
@@ -550,7 +473,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!more || walk.it.begin < 0) return;
             const int token = walk.it.first + row_token;
             const int64_t at = (int64_t)token * g.heads + walk.it.h * g.group + row_head;
-            ahead.powers.fetch(g, walk.it.h);
+            ahead.sigma.fetch(g, walk.it.h);
             if (row < g.group * g.kt && token < walk.it.end) ahead.lse = g.lse[at], ahead.delta = g.delta[at];
         };
         look();
@@ -560,19 +483,18 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int token = it.first + row_token, head = h * g.group + row_head;
             const bool live = row < g.group * g.kt && token < it.end;
             uint16_t* const own = live ? g.dq.p + (int64_t)token * g.dq.token + head * g.dq.head : nullptr;
-            const Powers pw = ahead.powers.get();
+            const int sigma = ahead.sigma.get();
             const float lse = ahead.lse, delta = live ? ahead.delta : 0.f;
             look();
             if (it.begin < 0) {
                 if (half == 0) write_zeros(own, g.dim);
                 continue;
             }
-            constexpr int lift = kLift;
-            const float sigma = power2(pw.sigma - lift);
+            const float unit = power2(sigma - kLift<F16>);  // of ds by that of p
             float fix = 0.f;
             const int64_t at = (int64_t)token * g.heads + head;
-            const Pair c2 = both(exponent_factor(g.scale, pw)), l2 = both(live ? lift - lse * kLog2e : -INFINITY), s2 = both(sigma);
-            Pair d2 = both(-delta * sigma), sum = both(0.f), lost = both(0.f);  // lost: what the rounding of ds adds to its sum
+            const Pair c2 = both(g.scale * kLog2e), l2 = both(live ? row_shift(lse, kLift<F16>) : -INFINITY), s2 = both(unit);
+            Pair d2 = both(-delta * unit), sum = both(0.f), lost = both(0.f);  // lost: what the rounding of ds adds to its sum
             for (int j = tiles - 1; j >= 0; --j, ++t) {
                 if (!(ok = warp_wait(s_full, t & 1, &sh.loads))) break;
                 mma_fence_after();
@@ -610,7 +532,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (j) {
                     uint32_t p[32];
 #pragma unroll
-                    for (int i = 0; i < 64; i += 2) p[i / 2] = pack16<true>(__uint_as_float(s[i / 32][i % 32]), __uint_as_float(s[i / 32][i % 32 + 1]));
+                    for (int i = 0; i < 64; i += 2) p[i / 2] = pack16<F16>(__uint_as_float(s[i / 32][i % 32]), __uint_as_float(s[i / 32][i % 32 + 1]));
                     tmem_store(ts, p);
                     tmem_store_wait();
                 }
@@ -629,7 +551,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                             if (32 * x + i > last) dp[x][i] = 0;
                 }
                 auto p_at = [&](int x, int i) { return pair(__uint_as_float(s[x][i]), __uint_as_float(s[x][i + 1])); };
-                auto ds_at = [&](int x, int i) { return p_at(x, i) * fma2(pair(__uint_as_float(dp[x][i]), __uint_as_float(dp[x][i + 1])), s2, d2); };
+                auto ds_at = [&](int x, int i) {
+                    const Pair y = pair(__uint_as_float(dp[x][i]), __uint_as_float(dp[x][i + 1]));
+                    return p_at(x, i) * (F16 ? fma2(y, s2, d2) : y + d2);
+                };
                 if (j == 0) {
                     // the last tile: what the row's ds add up to is what its delta is off by
 #pragma unroll
@@ -647,8 +572,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     mma_fence_after();
                     const float2 other = tmem_get(t_dp + 64 * (1 - half) + 32 + lanes);
                     const float r = own_sum + other.x;
-                    if (half == 0 && live) g.delta[at] = delta + r * power2(-pw.sigma);
-                    fix = (r + (own_lost + other.y)) * power2(-lift);
+                    if (half == 0 && live) g.delta[at] = delta + r * power2(-sigma);
+                    fix = (r + (own_lost + other.y)) * power2(-kLift<F16>);
                     d2 = d2 + both(-fix);
                     if (F16) {  // both have read before either writes there again
                         mma_fence_before();
@@ -666,9 +591,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                     for (int i = 0; i < 32; i += 2) {
                         const Pair v = ds_at(x, i);
                         const float2 f = split(v);
-                        const uint32_t d = pack16<true>(f.x, f.y);
+                        const uint32_t d = pack16<F16>(f.x, f.y);
                         ds[16 * x + i / 2] = d;
-                        const float2 e = __half22float2(*reinterpret_cast<const __half2*>(&d));
+                        const float2 e = values16<F16>(d);
                         const Pair off = fma2(both(-1.f), v, pair(e.x, e.y));
                         sum = sum + v, lost = lost + off;
                         if (F16) {
@@ -690,7 +615,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (!ok) break;
             out.set(own);
-            factor = g.scale * power2(-pw.sigma) * power2(-pw.k);
+            factor = g.scale * power2(-sigma);
             excess = fix, several = tiles > 1;
             pending = true;
             ++items;
@@ -839,8 +764,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         } else if (warp == 9) {
             // multiply: each product with the queries or dout, and behind it the next tile's scores or dp in the place of what it used
-            const uint32_t id_s = attend_desc(true, false, kRows), id_dp = attend_desc(F16, false, kRows), id_dk = attend_desc(true, true, 16 * ((g.dim + 15) / 16)),
-                           id_dv = attend_desc(F16, true, 16 * ((g.dim + 15) / 16));
+            const uint32_t id_rows = attend_desc(F16, false, kRows), id_acc = attend_desc(F16, true, 16 * ((g.dim + 15) / 16));
             const int steps = (g.dim + 15) / 16;
             uint32_t t = 0, items = 0;  // the present tile, counted through all items; items begun
             int i = 0, tiles = 0;
@@ -863,7 +787,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (!warp_wait((dp ? do_full : q_full) + 8 * slot.at, slot.parity, &sh.loads)) return false;
                 mma_fence_after();
                 if (elect_one()) {
-                    product_rows<HALVES>(dp ? t_dp : tmem, base + (2 * set.at + dp) * B::kTile, (dp ? at_do : at_q) + slot.at * B::kTile, dp ? id_dp : id_s, steps);
+                    product_rows<HALVES>(dp ? t_dp : tmem, base + (2 * set.at + dp) * B::kTile, (dp ? at_do : at_q) + slot.at * B::kTile, id_rows, steps);
                     mma_commit<1>(dp ? dp_full : s_full);
                     if (dp && i + 1 == tiles) mma_commit<1>(kv_free + 8 * set.at);
                 }
@@ -880,7 +804,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (first && !(ok = warp_wait(acc_free + 8 * set.at, set.parity ^ 1, &sh.loads))) break;
                 mma_fence_after();
                 if (elect_one()) {
-                    product_tmem(t_dv + 64 * set.at, tmem, tmem + 64, at_do + slot.at * B::kTile, id_dv, !first);
+                    product_tmem(t_dv + 64 * set.at, tmem, tmem + 64, at_do + slot.at * B::kTile, id_acc, !first);
                     mma_commit<1>(do_empty + 8 * slot.at);
                 }
                 __syncwarp();
@@ -890,8 +814,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 mma_fence_after();
                 if (elect_one()) {
                     const uint32_t acc = t_dk + 64 * set.at, b = at_q + slot.at * B::kTile;
-                    product_tmem(acc, t_dp, t_dp + 64, b, id_dk, !first);
-                    if (fine) product_tmem(acc, t_dp + 32, t_dp + 96, b, id_dk, true);
+                    product_tmem(acc, t_dp, t_dp + 64, b, id_acc, !first);
+                    if (fine) product_tmem(acc, t_dp + 32, t_dp + 96, b, id_acc, true);
                     mma_commit<1>(q_empty + 8 * slot.at);
                     if (last) mma_commit<1>(acc_full + 8 * set.at);
                 }
@@ -906,9 +830,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const Work it = walk.it;
                 const QuerySpan q = query_span(it, g.kt);
                 if (!q.tiles) continue;
-                RawPowers<F16> powers;
-            powers.fetch(g, it.h);
-            const float sigma = power2(powers.get().sigma - (F16 ? kLift : 0));
+                Sigma<F16> sigma;
+                sigma.fetch(g, it.h);
+                const float unit = power2(sigma.get() - kLift<F16>);
                 for (int i = 0; i < q.tiles; ++i, ++n) {
                     const Stat stage(n);
                     float l[4], d[4];
@@ -917,8 +841,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                         const int row = 32 * x + lane, token = q.first + i * g.kt + row / g.group, head = walk.it.h * g.group + row % g.group;
                         const bool live = row < qrows && token < it.end;
                         const int64_t at = (int64_t)token * g.heads + head;
-                        l[x] = live ? (F16 ? kLift : 0) - g.lse[at] * kLog2e : -INFINITY;
-                        d[x] = live ? -g.delta[at] * sigma : 0.f;
+                        l[x] = live ? row_shift(g.lse[at], kLift<F16>) : -INFINITY;
+                        d[x] = live ? -g.delta[at] * unit : 0.f;
                     }
                     if (!(ok = warp_wait(st_empty + 8 * stage.at, stage.parity ^ 1, &sh.loads))) break;
                     float* const to = stats + stage.at * 2 * kRows;
@@ -966,10 +890,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                 write_zeros(own, g.dim);
                 continue;
             }
-            RawPowers<F16> powers;
-            powers.fetch(g, h);
-            const Powers pw = powers.get();
-            const Pair c2 = both(exponent_factor(g.scale, pw)), s2 = both(power2(pw.sigma - (F16 ? kLift : 0)));
+            Sigma<F16> raw;
+            raw.fetch(g, h);
+            const int sigma = raw.get();
+            const Pair c2 = both(g.scale * kLog2e), s2 = both(power2(sigma - kLift<F16>));
             const bool fine = F16 && q.tiles <= kFineTiles;
             for (int i = 0; i < q.tiles; ++i, ++t) {
                 const Stat step(t);
@@ -1029,12 +953,13 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                     for (int j = 0; j < 32; j += 4) {
                         const float4 d = *reinterpret_cast<const float4*>(st + kRows + 32 * x + j);
-                        const float2 a = split(pair(__uint_as_float(s[x][j]), __uint_as_float(s[x][j + 1])) *
-                                               fma2(pair(__uint_as_float(dp[x][j]), __uint_as_float(dp[x][j + 1])), s2, pair(d.x, d.y)));
-                        const float2 b = split(pair(__uint_as_float(s[x][j + 2]), __uint_as_float(s[x][j + 3])) *
-                                               fma2(pair(__uint_as_float(dp[x][j + 2]), __uint_as_float(dp[x][j + 3])), s2, pair(d.z, d.w)));
+                        auto ds_at = [&](int i, float d0, float d1) {
+                            const Pair y = pair(__uint_as_float(dp[x][i]), __uint_as_float(dp[x][i + 1])), d2 = pair(d0, d1);
+                            return split(pair(__uint_as_float(s[x][i]), __uint_as_float(s[x][i + 1])) * (F16 ? fma2(y, s2, d2) : y + d2));
+                        };
+                        const float2 a = ds_at(j, d.x, d.y), b = ds_at(j + 2, d.z, d.w);
                         const float v[4] = {a.x, a.y, b.x, b.y};  // 0 where the probability is
-                        e[16 * x + j / 2] = pack16<true>(v[0], v[1]), e[16 * x + j / 2 + 1] = pack16<true>(v[2], v[3]);
+                        e[16 * x + j / 2] = pack16<F16>(v[0], v[1]), e[16 * x + j / 2 + 1] = pack16<F16>(v[2], v[3]);
                         if (fine) {
                             const float2 a16 = __half22float2(*reinterpret_cast<const __half2*>(&e[16 * x + j / 2]));
                             const float2 b16 = __half22float2(*reinterpret_cast<const __half2*>(&e[16 * x + j / 2 + 1]));
@@ -1055,7 +980,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (!ok) break;
             out.set(own);
-            factor = half ? g.scale * power2(-pw.sigma) * power2(-pw.q) : power2(F16 ? -kLift : 0);
+            factor = half ? g.scale * power2(-sigma) : power2(-kLift<F16>);
             pending = true;
             ++items;
         }
@@ -1072,11 +997,11 @@ __global__ void __launch_bounds__(kThreads, 1)
 // ---- host side ----
 
 struct BackPlan {
-    int group, kt, row;
+    int group, kt;
     int64_t most[2];
-    size_t at_start, at_prefix[2], at_items[2], at_largest, at_power, at_delta, at_narrow[2], bytes;
+    size_t at_start, at_prefix[2], at_items[2], at_largest, at_delta, bytes;
 };
-BackPlan back_plan(int tokens, int sequences, int heads, int kv, int dim) {
+BackPlan back_plan(int tokens, int sequences, int heads, int kv) {
     BackPlan p;
     p.group = heads / kv, p.kt = kRows / p.group;
     p.most[0] = items_at_most(tokens, sequences, p.kt), p.most[1] = items_at_most(tokens, sequences, kKeys);
@@ -1085,10 +1010,8 @@ BackPlan back_plan(int tokens, int sequences, int heads, int kv, int dim) {
     const size_t bounds = ((size_t)sequences + 1) * 4;
     p.at_start = take(2 * bounds);
     for (int i = 0; i < 2; ++i) p.at_prefix[i] = take(bounds), p.at_items[i] = take((size_t)p.most[i] * sizeof(Item));
-    p.at_largest = take((size_t)4 * kv * 4), p.at_power = take((size_t)4 * kv * 4);
+    p.at_largest = take((size_t)2 * kv * 4);
     p.at_delta = take((size_t)tokens * heads * 4);
-    p.row = (dim + 7) / 8 * 8;
-    p.at_narrow[0] = take((size_t)tokens * heads * p.row * 2), p.at_narrow[1] = take((size_t)tokens * kv * p.row * 2);  // for bfloat16
     p.bytes = at;
     return p;
 }
@@ -1117,23 +1040,20 @@ cudaError_t launch_back(const ones_heads& dout, const ones_heads& q, const ones_
                         const PlanArgs& plan, const BackPlan& p, cudaStream_t stream) {
     constexpr int kLanes = 8 * HALVES;
     CUtensorMap maps[4];
-    ones_heads qs = q, ks = k;
-    if (!F16) qs = {d.narrow[0], (int64_t)a.heads * d.row, d.row, a.heads}, ks = {d.narrow[1], (int64_t)a.kv * d.row, d.row, a.kv};
-    cudaError_t err = make_heads_map(&maps[0], qs, a.dim, a.tokens, a.group, a.kt, true);
+    cudaError_t err = make_heads_map(&maps[0], q, a.dim, a.tokens, a.group, a.kt, F16);
     if (err == cudaSuccess) err = make_heads_map(&maps[1], dout, a.dim, a.tokens, a.group, a.kt, F16);
-    if (err == cudaSuccess) err = make_heads_map(&maps[2], ks, a.dim, a.tokens, 1, kKeys, true);
+    if (err == cudaSuccess) err = make_heads_map(&maps[2], k, a.dim, a.tokens, 1, kKeys, F16);
     if (err == cudaSuccess) err = make_heads_map(&maps[3], v, a.dim, a.tokens, 1, kKeys, F16);
     if (err == cudaSuccess) err = launch_plan(plan, 2, stream);
     if (err != cudaSuccess) return err;
     const int blocks = (a.tokens + kTokens - 1) / kTokens, most = 8 * device_sms(), grid = blocks < most ? blocks : most;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid), cfg.blockDim = dim3(256), cfg.dynamicSmemBytes = (size_t)6 * a.kv * 4, cfg.stream = stream;
+    cfg.gridDim = dim3(grid), cfg.blockDim = dim3(256), cfg.dynamicSmemBytes = F16 ? (size_t)2 * a.kv * 4 : 0, cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr, cfg.numAttrs = 1;
     err = cudaLaunchKernelEx(&cfg, a.dim % 8 ? k_survey<F16, kLanes, true> : k_survey<F16, kLanes, false>, d);
-    if (err == cudaSuccess && !F16) err = launch_after(k_settle<kLanes>, dim3(grid < device_sms() ? grid : device_sms()), dim3(256), stream, d, const_cast<int*>(a.power));
     if (err != cudaSuccess) return err;
     static std::atomic<uint64_t> ready[2];
     a.items = plan.items[0], a.head = plan.head;
@@ -1153,7 +1073,7 @@ extern "C" {
 
 size_t ones_attention_backward_workspace_bytes(int32_t tokens, int32_t sequences, int32_t heads, int32_t kv, int32_t dim) {
     if (ones::bad_counts(tokens, sequences, heads, kv) || dim < 1 || dim > ONES_ATTENTION_MAX_DIM) return 0;
-    return ones::back_plan(tokens, sequences, heads, kv, dim).bytes;
+    return ones::back_plan(tokens, sequences, heads, kv).bytes;
 }
 
 int ones_attention_backward(const ones_heads* dout, const ones_heads* q, const ones_heads* k, const ones_heads* v,
@@ -1168,7 +1088,7 @@ int ones_attention_backward(const ones_heads* dout, const ones_heads* q, const o
     if (bad || !tokens) return bad;
     if (!d_lse || !d_workspace) return ONES_ERR_NULL;
     if (!aligned(d_lse, 4) || !aligned(d_workspace, 256)) return ONES_ERR_ALIGN;
-    const BackPlan p = back_plan(tokens, sequences, q->heads, k->heads, dim);
+    const BackPlan p = back_plan(tokens, sequences, q->heads, k->heads);
     if (p.most[0] * k->heads >= 1ll << 31) return ONES_ERR_BAD_PARAM;
     if (workspace_bytes < p.bytes) return ONES_ERR_WORKSPACE;
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
@@ -1180,15 +1100,13 @@ int ones_attention_backward(const ones_heads* dout, const ones_heads* q, const o
     for (int i = 0; i < 2; ++i)
         plan.prefix[i] = reinterpret_cast<int*>(ws + p.at_prefix[i]), plan.items[i] = reinterpret_cast<Item*>(ws + p.at_items[i]);
     unsigned* const largest = reinterpret_cast<unsigned*>(ws + p.at_largest);
-    plan.zero = largest, plan.zeros = 4 * k->heads;
+    plan.zero = largest, plan.zeros = type == ONES_F16 ? 2 * k->heads : 0;
     float* const delta = reinterpret_cast<float*>(ws + p.at_delta);
     auto vectors = [](const ones_heads& h) { return Vectors{static_cast<const uint16_t*>(h.d_data), h.token, h.head}; };
-    int* const power = reinterpret_cast<int*>(ws + p.at_power);  // guessed, then settled
-    SurveyArgs d = {vectors(*dout), vectors(*out), vectors(*v), vectors(*q), vectors(*k)};
-    for (int i = 0; i < 2; ++i) d.narrow[i] = reinterpret_cast<uint16_t*>(ws + p.at_narrow[i]);
-    d.plan = plan.head, d.delta = delta, d.largest = largest, d.power = power, d.tokens = tokens, d.heads = q->heads, d.kv = k->heads, d.dim = dim;
-    d.row = p.row, d.wide = aligned(out->d_data, 16) && (out->heads <= 1 || out->head % 8 == 0) && (tokens <= 1 || out->token % 8 == 0);
-    const BackArgs a = {nullptr, nullptr, d_lse, delta, largest, power + 2 * k->heads, heads_out(*dq, dim, tokens), heads_out(*dk, dim, tokens), heads_out(*dv, dim, tokens), tokens,
+    SurveyArgs d = {vectors(*dout), vectors(*out), vectors(*v)};
+    d.plan = plan.head, d.delta = delta, d.largest = largest, d.tokens = tokens, d.heads = q->heads, d.kv = k->heads, d.dim = dim;
+    d.wide = aligned(out->d_data, 16) && (out->heads <= 1 || out->head % 8 == 0) && (tokens <= 1 || out->token % 8 == 0);
+    const BackArgs a = {nullptr, nullptr, d_lse, delta, largest, heads_out(*dq, dim, tokens), heads_out(*dk, dim, tokens), heads_out(*dv, dim, tokens), tokens,
                         q->heads, k->heads, p.group, p.kt, dim, scale};
     const bool f16 = type == ONES_F16;
     cudaError_t err;

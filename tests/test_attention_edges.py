@@ -116,10 +116,11 @@ def gradients64(q, k, v, dout, scale):
         # out is off by two roundings of u (its own and the probabilities'), and so is dout . out; dp by its 32-bit sums
         de = (2 * u + 4 * se + n * 2.0 ** -24) * (do.abs() * (p @ c.abs())).sum(1, keepdim=True)
         dpe = 2.0 ** -19 * ((do.abs() * o.abs()).sum(1, keepdim=True) + do.abs() @ c.abs().T)
-        # ds: its rounding, that of p, and dp's; its sum over the row, which is 0, is known to n 2^-22 of its terms (all of which shift with it by
-        # their p), but for the rounding of what they shift by
+        # ds: its rounding, that of p, and dp's. Its sum over the row, which is 0, is known to n 2^-22 of its terms. What it is off by is taken off all of
+        # them by their p. Of de, ds + p de is rounded (u p de), what all of these roundings add up to is in the sum (u de), and so is de, to be
+        # met by the rounding of p (u p de): sum_j (1 + x_j) (ds_j + p_j e) k_j - (e + sum_j x_j (ds_j + p_j e)) sum_j (1 + y_j) p_j k_j, |x|, |y| <= u
         own = ds.abs() * (u + 4 * se + n * 2.0 ** -22) + p * dpe
-        common = p * (own.sum(1, keepdim=True) * (u + 4 * se) + ds.abs().sum(1, keepdim=True) * (n * 2.0 ** -22) + de * (u + 4 * se) +
+        common = p * (own.sum(1, keepdim=True) * (u + 4 * se) + ds.abs().sum(1, keepdim=True) * (n * 2.0 ** -22) + de * (3 * u + 4 * se) +
                       (p * dpe).sum(1, keepdim=True))
         most = do.abs().amax(1, keepdim=True) * c.abs().max()
         ge["dq"][:, head] += scale * (own + common + mask * most * step) @ b.abs()
@@ -145,7 +146,7 @@ def check_gradients(q, k, v, dout, lengths, scale=None):
 
 @pytest.mark.parametrize("dtype", [BF16, F16])
 @pytest.mark.parametrize("heads, kv, dim", [(1, 1, 64), (2, 1, 128), (3, 1, 77)])
-@pytest.mark.parametrize("mean, recent, large", [(4, False, False), (4, True, False), (4, True, True), (0, True, True)])
+@pytest.mark.parametrize("mean, recent, large", [(4, False, False), (4, True, False), (4, False, True), (4, True, True), (0, True, True)])
 def test_attention_gradients_of_inputs_with_structure(mean, recent, large, heads, kv, dim, dtype):
     """Values with a common mean, scores that favour the latest keys, and first keys that are large where no query looks: the rounding of
     `out` does not show in the gradients, wherever a row's probabilities lie."""
@@ -160,3 +161,38 @@ def test_attention_gradients_of_inputs_with_structure(mean, recent, large, heads
         k[:128, :, 3] = 60 * randn(128, kv, seed=7).sign()
         k[:128, :, 0] -= 40.0
     check_gradients(*(t.to(dtype) for t in (q, k, v, dout)), [n], scale=0.25)
+
+
+@pytest.mark.parametrize("first, mark", [(100, 1.0), (128, 1.0), (150, 1.0), (128, 4.0)])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_attention_gradients_beside_the_lowest_value(dim, first, mark):
+    """Keys that a column with the type's lowest value hides take nothing from the others' precision, and get nothing."""
+    from paper_2108_03645_b200 import train
+    n = 400
+    q, k, v = hidden(n, first, dim, BF16, torch.finfo(BF16).min, -3, mark)
+    dout = randn(n, 1, dim, seed=5).bfloat16()
+    dout[:first] = 0
+    out, lse = train.attention(q, k, v, scale=0.125)
+    got = dict(zip(("dq", "dk", "dv"), train.attention_backward(dout, q, k, v, out, lse, scale=0.125)))
+    for name, (want, bound) in gradients64(q[first:], k[first:], v[first:], dout[first:], 0.125).items():
+        close(got[name][first:], want, bound)
+        if mark == 1.0:  # (where the hidden rows' own scores are -infinity, they are NaN)
+            assert not bool(got[name][:first].any())
+
+
+@pytest.mark.parametrize("which", ["q", "k", "v", "dout"])
+@pytest.mark.parametrize("size", [2.0 ** -13, 2.0 ** -40])
+def test_attention_bfloat16_gradients_beside_larger_sequences(which, size):
+    """A sequence whose tensor is far smaller than its neighbour's has gradients as exact as by itself."""
+    lengths = [300, 200, 70]
+    x = {name: randn(570, h, 64, seed=h + i) for i, (name, h) in enumerate((("q", 4), ("k", 2), ("v", 2), ("dout", 4)))}
+    x[which][300:500] *= size
+    check_gradients(*(t.bfloat16() for t in x.values()), lengths)
+
+
+@pytest.mark.parametrize("which", ["v", "dout"])
+def test_attention_bfloat16_gradients_of_small_tokens(which):
+    """The same between tokens of one sequence."""
+    x = {name: randn(600, h, 128, seed=h + i) for i, (name, h) in enumerate((("q", 2), ("k", 1), ("v", 1), ("dout", 2)))}
+    x[which][:100] *= 2.0 ** 14
+    check_gradients(*(t.bfloat16() for t in x.values()), [600])
