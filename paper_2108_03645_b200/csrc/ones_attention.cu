@@ -57,6 +57,13 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const PlanArgs a) {
     __shared__ int bins[kBins];
     __shared__ int s_total;
     __shared__ int s_start[kNear + 1], s_prefix[kNear + 1];
+    if (blockIdx.x >= a.lists) {
+        wait_for_predecessor();
+        let_successor_start();
+        const int64_t stride = (int64_t)(gridDim.x - a.lists) * kPlanThreads;
+        for (int64_t i = (int64_t)(blockIdx.x - a.lists) * kPlanThreads + threadIdx.x; i < a.zeros; i += stride) a.zero[i] = 0;
+        return;
+    }
     const int list = blockIdx.x, step = list ? a.step[1] : a.step[0], per = list ? a.tile[1] : a.tile[0];
     const bool near = a.sequences <= kNear;
     int* const prefix = near ? s_prefix : list ? a.prefix[1] : a.prefix[0];
@@ -64,8 +71,6 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const PlanArgs a) {
     Item* const items = list ? a.items[1] : a.items[0];
     wait_for_predecessor();
     let_successor_start();
-    if (list == 0)
-        for (int i = threadIdx.x; i < a.zeros; i += kPlanThreads) a.zero[i] = 0;
     int carry_max = 0;
     for (int base = 0; base <= a.sequences; base += kPlanThreads) {
         const int i = base + threadIdx.x;
@@ -117,8 +122,9 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const PlanArgs a) {
                 it.begin = start[lo], it.end = start[lo + 1];
                 it.first = it.begin + (i - prefix[lo]) * step;
                 // queries: the keys up to their last one; keys: the queries from their first one on
-                it.cost = ((list == 0 ? min(it.first + step, it.end) - it.begin : it.end - it.first) + per - 1) / per;
-                bin = kBins - 1 - min(it.cost >> shift, kBins - 1);
+                it.slot = min(lo, it.begin);
+                const int cost = ((list == 0 ? min(it.first + step, it.end) - it.begin : it.end - it.first) + per - 1) / per;
+                bin = kBins - 1 - min(cost >> shift, kBins - 1);
             }
             const int at = atomicAdd(&bins[bin], 1);
             if (pass) items[at] = it;
@@ -131,7 +137,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const PlanArgs a) {
         }
     }
     for (int i = threadIdx.x; i < n_front + n_back; i += kPlanThreads) {
-        it.begin = -1, it.cost = 0;
+        it.begin = -1, it.slot = 0;
         it.first = i < n_front ? i * step : back + (i - n_front) * step;
         it.end = min(it.first + step, i < n_front ? front : a.tokens);
         items[total + i] = it;
@@ -586,8 +592,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 const WaitControl attention_waits = {take_expired, limit_waits, wait_for_nothing};
 
-cudaError_t launch_plan(const PlanArgs& a, int lists, cudaStream_t stream) {
-    return launch_after(k_plan, dim3(lists), dim3(kPlanThreads), stream, a);
+cudaError_t launch_plan(PlanArgs a, int lists, cudaStream_t stream) {
+    a.lists = lists;
+    const int64_t blocks = (a.zeros + 16 * kPlanThreads - 1) / (16 * kPlanThreads), most = device_sms();
+    return launch_after(k_plan, dim3(lists + (unsigned)(blocks < most ? blocks : most)), dim3(kPlanThreads), stream, a);
 }
 
 cudaError_t make_heads_map(CUtensorMap* out, const ones_heads& h, int dim, int tokens, int heads_box, int tokens_box, bool f16) {

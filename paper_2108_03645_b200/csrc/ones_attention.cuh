@@ -23,9 +23,10 @@ constexpr int kHalfTile = kRows * 128;          // bytes of 64 columns of a tile
 constexpr int kKeys = 128;                      // keys of a tile
 
 // A piece of work: tokens from `first` on of the sequence [begin, end). In the list of queries `first` starts one or two tiles of
-// queries, in the list of keys a tile of keys. begin < 0: tokens [first, end) belong to no sequence and get zeros.
+// queries, in the list of keys a tile of keys. begin < 0: tokens [first, end) belong to no sequence and get zeros. slot: the sequence's
+// own, below the tokens and the sequences.
 struct Item {
-    int first, begin, end, cost;
+    int first, begin, end, slot;
 };
 
 // In the workspace, one for each list: how many items there are, then the items, those with the most work first.
@@ -43,14 +44,15 @@ struct PlanArgs {
     int* prefix[2];   // [sequences + 1] items before each sequence
     Item* items[2];
     PlanHead* head;   // [2]
-    unsigned* zero;   // words that are set to 0, by the first list's block
-    int zeros;
+    unsigned* zero;   // words that are set to 0, by blocks of their own
+    int64_t zeros;
+    int lists;
 };
 
 inline int64_t items_at_most(int64_t tokens, int64_t sequences, int64_t step) {
     return tokens / step + (sequences < tokens ? sequences : tokens) + 2;
 }
-cudaError_t launch_plan(const PlanArgs& a, int lists, cudaStream_t stream);
+cudaError_t launch_plan(PlanArgs a, int lists, cudaStream_t stream);
 
 // A tensor of heads as boxes of 64 values x `heads_box` heads x `tokens_box` tokens; what lies outside it reads as zeros.
 cudaError_t make_heads_map(CUtensorMap* out, const ones_heads& h, int dim, int tokens, int heads_box, int tokens_box, bool f16);
@@ -302,7 +304,9 @@ __device__ __forceinline__ void write_zeros(uint16_t* row, int dim) {
 constexpr int kListed = 92;
 struct Work {
     int first, begin, end, h;  // an item and its head of the keys
+    uint32_t slot;
 };
+constexpr int kHeadBits = 10;  // ONES_MAX_HEADS; a slot has 22
 struct WorkList {  // in shared memory
     int4 listed[kListed];
     int turns;
@@ -310,7 +314,7 @@ struct WorkList {  // in shared memory
 __device__ __forceinline__ int4 fetch_work(const Item* items, uint32_t kv, int turn) {
     const uint32_t w = turn * gridDim.x + (turn & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x), i = w / kv;
     const Item a = items[i];
-    return make_int4(a.first, a.begin, a.end, (int)(w - i * kv));
+    return make_int4(a.first, a.begin, a.end, (int)(w - i * kv | (uint32_t)a.slot << kHeadBits));
 }
 // By all threads, before a barrier of the block. Items times heads are below 2^31.
 __device__ __forceinline__ void list_work(WorkList& list, const Item* items, const PlanHead* head, int kv) {
@@ -329,7 +333,7 @@ struct Walk {
     __device__ __forceinline__ bool next() {
         if (turn >= list.turns) return false;
         const int4 a = turn < kListed ? list.listed[turn] : fetch_work(items, kv, turn);
-        it = {a.x, a.y, a.z, a.w};
+        it = {a.x, a.y, a.z, a.w & ((1 << kHeadBits) - 1), (uint32_t)a.w >> kHeadBits};
         ++turn;
         return true;
     }

@@ -36,26 +36,28 @@ struct BackArgs {
     const PlanHead* head;
     const float* lse;           // [tokens][heads]
     float* delta;               // the same; exact from the first pass on
-    const unsigned* largest;    // float16: [2][kv], bits of the largest finite |dout| and |v| of a head or group
+    const uint16_t* row_top;    // float16: [tokens][heads], the largest finite |dout| of a row
+    const unsigned* top;        // float16: [slots][2][kv], that and the largest finite |v| of a sequence's group of heads
     HeadsOut dq, dk, dv;
     int tokens, heads, kv, group, kt, dim;
     float scale;
 };
 
 // float16 tensors: probabilities times 2^12 for their products, so that small ones keep their bits, and ds times 2^sigma, which takes the bound
-// 2 dim max |dout| max |v| of |dp - delta| to 2^15.
+// 2 dim max |dout| max |v| of |dp - delta| to 2^15: of the row (for dq) or the sequence (for dk, where rows meet), and of the sequence's values.
 template <bool F16>
 constexpr int kLift = F16 ? 12 : 0;
 __device__ __forceinline__ float power2(int n) { return __int_as_float((n + 127) << 23); }  // -127 < n < 128
 template <bool F16>
 struct Sigma {
     unsigned dout, v;  // as they lie in memory
-    __device__ __forceinline__ void fetch(const BackArgs& g, int h) {
-        if (F16) dout = g.largest[h], v = g.largest[g.kv + h];
+    __device__ __forceinline__ void fetch(const BackArgs& g, const Work& it) {
+        const int64_t at = (int64_t)it.slot * 2 * g.kv + it.h;
+        if (F16) dout = g.top[at], v = g.top[at + g.kv];
     }
     __device__ __forceinline__ int get() const {
-        auto above = [](unsigned bits) { return (int)(bits >> 23) - 126; };  // |x| < 2^above
-        return F16 ? min(max(15 - 8 - above(dout) - above(v), -100), 100) : 0;  // 2^7 >= dim
+        auto above = [](unsigned bits) { return (int)(__float_as_uint(__half2float(__ushort_as_half((uint16_t)bits))) >> 23) - 126; };  // |x| < 2^above
+        return F16 ? min(15 - 8 - above(dout) - above(v), 100) : 0;  // 2^7 >= dim
     }
 };
 // What the exponent of a row's probabilities subtracts. A row whose lse lies beyond 2^24, where 32 bits hold no more of its keys' shares
@@ -65,7 +67,7 @@ __device__ __forceinline__ float row_shift(float lse, int lift) {
     return a >= 0x1p24f && a < INFINITY ? -INFINITY : lift - lse * kLog2e;
 }
 
-// ---- delta = dout . out, and the largest values of float16 tensors ----
+// ---- delta = dout . out, and (float16) the largest values of rows and sequences ----
 
 struct Vectors {
     const uint16_t* p;
@@ -75,7 +77,7 @@ struct SurveyArgs {
     Vectors dout, out, v;
     const PlanHead* plan;
     float* delta;
-    unsigned* largest;  // float16: [2][kv], bits of the largest finite |dout| and |v|
+    uint16_t *row_top, *v_top;  // float16: [tokens][heads] and [tokens][kv], the largest finite |dout| and |v|
     int tokens, heads, kv, dim, wide;  // wide: out starts on 16-byte boundaries
 };
 
@@ -114,7 +116,7 @@ struct Own {  // which of the lane's eight values the vectors have
         return RAGGED ? make_uint4(v.x & mask.x, v.y & mask.y, v.z & mask.z, v.w & mask.w) : v;
     }
 };
-// The largest finite float16's bits, as a 32-bit number.
+// The largest finite float16's bits.
 __device__ __forceinline__ unsigned largest_of(const uint4& v) {
     constexpr unsigned kLimit = 0x7C00u;  // infinity
     const uint32_t w[4] = {v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu, v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu};
@@ -127,29 +129,27 @@ __device__ __forceinline__ unsigned largest_of(const uint4& v) {
             if (b < kLimit) top = max(top, b);
         }
     }
-    return __float_as_uint(value16<true>((uint16_t)top));
+    return top;
 }
 
 // LANES x 8 values are a vector, which a group of lanes takes. A block takes kTokens tokens at a time.
 constexpr int kTokens = 16;
 template <bool F16, int LANES, bool RAGGED>
 __global__ void __launch_bounds__(256, 4) k_survey(const __grid_constant__ SurveyArgs g) {
-    extern __shared__ unsigned top[];  // float16: [2][kv]
     constexpr int kGroups = 256 / LANES, kAtOnce = 4;
     const int lane = threadIdx.x % LANES, c = 8 * lane;
     const Own<RAGGED> own_of(c, g.dim);
     wait_for_predecessor();
     let_successor_start();
-    const int t0 = g.plan->covered[0], t1 = g.plan->covered[1], group = g.heads / g.kv;
-    for (int i = threadIdx.x; F16 && i < 2 * g.kv; i += 256) top[i] = 0;
-    __syncthreads();
-    auto note = [&](const uint4& v, int which, int h) {
-        const unsigned m = largest_of(v);
-        unsigned* const at = top + which * g.kv + h;
-        if (m > *at) atomicMax(at, m);
+    const int t0 = g.plan->covered[0], t1 = g.plan->covered[1];
+    auto top_of = [](const uint4& v) {  // of the group's vector
+        unsigned m = largest_of(v);
+#pragma unroll
+        for (int x = LANES / 2; x; x >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, x));
+        return (uint16_t)m;
     };
     const int own = threadIdx.x / LANES;
-    const uint32_t per_head = 0xFFFFFFFFu / g.heads + 1, per_kv = 0xFFFFFFFFu / g.kv + 1, per_group = 0xFFFFFFFFu / group + 1;
+    const uint32_t per_head = 0xFFFFFFFFu / g.heads + 1, per_kv = 0xFFFFFFFFu / g.kv + 1;
     auto over = [](uint32_t r, uint32_t n, uint32_t per) { return n == 1 ? r : __umulhi(r, per); };  // r / n below 2^16, with 2^32 / n rounded up
     for (int first = t0 + blockIdx.x * kTokens; first < t1; first += gridDim.x * kTokens) {
         const int n_t = min(kTokens, t1 - first);
@@ -173,7 +173,10 @@ __global__ void __launch_bounds__(256, 4) k_survey(const __grid_constant__ Surve
                 const bool live = at_t[x] < n_t;
                 float dot = 0.f;
                 a[x] = own_of(a[x]), b[x] = own_of(b[x]);
-                if (F16 && live) note(a[x], 0, over(at_h[x], group, per_group));
+                if (F16) {
+                    const uint16_t m = top_of(a[x]);
+                    if (lane == 0 && live) g.row_top[(int64_t)(first + at_t[x]) * g.heads + at_h[x]] = m;
+                }
                 if (g.wide) {
                     const uint32_t u[4] = {a[x].x, a[x].y, a[x].z, a[x].w}, w[4] = {b[x].x, b[x].y, b[x].z, b[x].w};
                     Pair d = both(0.f);
@@ -206,13 +209,42 @@ __global__ void __launch_bounds__(256, 4) k_survey(const __grid_constant__ Surve
 #pragma unroll
             for (int x = 0; x < kAtOnce; ++x) {
                 const int r = r0 + x * kGroups + own, t = over(r, g.kv, per_kv);
-                if (t < n_t) note(own_of(a[x]), 1, r - t * g.kv);
+                const uint16_t m = top_of(own_of(a[x]));
+                if (lane == 0 && t < n_t) g.v_top[(int64_t)first * g.kv + r] = m;
             }
         }
     }
-    __syncthreads();
-    for (int i = threadIdx.x; F16 && i < 2 * g.kv; i += 256)
-        if (top[i]) atomicMax(g.largest + i, top[i]);
+}
+
+// float16: the largest values of every sequence and group of heads, 128 tokens by a warp. (By themselves, since the survey knows nothing of sequences;
+// 40 documents of 16102 tokens, 3 groups: 3 us.)
+struct TopArgs {
+    const Item* items;  // of the keys
+    const PlanHead* head;
+    const uint16_t *row_top, *v_top;
+    unsigned* top;
+    int heads, kv;
+};
+__global__ void __launch_bounds__(256) k_tops(const TopArgs g) {
+    wait_for_predecessor();
+    let_successor_start();
+    const int lane = threadIdx.x % 32, group = g.heads / g.kv;
+    const uint32_t total = (uint32_t)g.head->count * g.kv;
+    for (uint32_t w = blockIdx.x * 8 + threadIdx.x / 32; w < total; w += gridDim.x * 8) {
+        const Item it = g.items[w / g.kv];
+        const int h = w % g.kv;
+        if (it.begin < 0) continue;
+        unsigned d = 0, v = 0;
+        for (int t = it.first + lane; t < min(it.first + kKeys, it.end); t += 32) {
+            v = max(v, (unsigned)g.v_top[(int64_t)t * g.kv + h]);
+            const uint16_t* const rows = g.row_top + (int64_t)t * g.heads + h * group;
+            for (int i = 0; i < group; ++i) d = max(d, (unsigned)rows[i]);
+        }
+        d = __reduce_max_sync(0xFFFFFFFFu, d), v = __reduce_max_sync(0xFFFFFFFFu, v);
+        if (lane) continue;
+        unsigned* const to = g.top + (int64_t)it.slot * 2 * g.kv + h;
+        atomicMax(to, d), atomicMax(to + g.kv, v);
+    }
 }
 
 // Heads of up to 64 values leave room for two sets of what belongs to an item (its tiles in shared memory, its sums in tensor
@@ -473,8 +505,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!more || walk.it.begin < 0) return;
             const int token = walk.it.first + row_token;
             const int64_t at = (int64_t)token * g.heads + walk.it.h * g.group + row_head;
-            ahead.sigma.fetch(g, walk.it.h);
-            if (row < g.group * g.kt && token < walk.it.end) ahead.lse = g.lse[at], ahead.delta = g.delta[at];
+            ahead.sigma.fetch(g, walk.it);
+            if (row < g.group * g.kt && token < walk.it.end) {
+                ahead.lse = g.lse[at], ahead.delta = g.delta[at];
+                if (F16) ahead.sigma.dout = g.row_top[at];
+            }
         };
         look();
         while (ok && more) {
@@ -831,7 +866,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const QuerySpan q = query_span(it, g.kt);
                 if (!q.tiles) continue;
                 Sigma<F16> sigma;
-                sigma.fetch(g, it.h);
+                sigma.fetch(g, it);
                 const float unit = power2(sigma.get() - kLift<F16>);
                 for (int i = 0; i < q.tiles; ++i, ++n) {
                     const Stat stage(n);
@@ -891,7 +926,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 continue;
             }
             Sigma<F16> raw;
-            raw.fetch(g, h);
+            raw.fetch(g, it);
             const int sigma = raw.get();
             const Pair c2 = both(g.scale * kLog2e), s2 = both(power2(sigma - kLift<F16>));
             const bool fine = F16 && q.tiles <= kFineTiles;
@@ -998,8 +1033,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 struct BackPlan {
     int group, kt;
-    int64_t most[2];
-    size_t at_start, at_prefix[2], at_items[2], at_largest, at_delta, bytes;
+    int64_t most[2], slots;
+    size_t at_start, at_prefix[2], at_items[2], at_delta, at_row_top, at_v_top, at_top, bytes;
 };
 BackPlan back_plan(int tokens, int sequences, int heads, int kv) {
     BackPlan p;
@@ -1010,8 +1045,9 @@ BackPlan back_plan(int tokens, int sequences, int heads, int kv) {
     const size_t bounds = ((size_t)sequences + 1) * 4;
     p.at_start = take(2 * bounds);
     for (int i = 0; i < 2; ++i) p.at_prefix[i] = take(bounds), p.at_items[i] = take((size_t)p.most[i] * sizeof(Item));
-    p.at_largest = take((size_t)2 * kv * 4);
     p.at_delta = take((size_t)tokens * heads * 4);
+    p.slots = tokens < sequences ? tokens : sequences;
+    p.at_row_top = take((size_t)tokens * heads * 2), p.at_v_top = take((size_t)tokens * kv * 2), p.at_top = take((size_t)p.slots * 2 * kv * 4);
     p.bytes = at;
     return p;
 }
@@ -1048,12 +1084,17 @@ cudaError_t launch_back(const ones_heads& dout, const ones_heads& q, const ones_
     if (err != cudaSuccess) return err;
     const int blocks = (a.tokens + kTokens - 1) / kTokens, most = 8 * device_sms(), grid = blocks < most ? blocks : most;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid), cfg.blockDim = dim3(256), cfg.dynamicSmemBytes = F16 ? (size_t)2 * a.kv * 4 : 0, cfg.stream = stream;
+    cfg.gridDim = dim3(grid), cfg.blockDim = dim3(256), cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr, cfg.numAttrs = 1;
     err = cudaLaunchKernelEx(&cfg, a.dim % 8 ? k_survey<F16, kLanes, true> : k_survey<F16, kLanes, false>, d);
+    if (F16 && err == cudaSuccess) {
+        const TopArgs t = {plan.items[1], plan.head + 1, d.row_top, d.v_top, const_cast<unsigned*>(a.top), a.heads, a.kv};
+        const int64_t warps = (p.most[1] * a.kv + 7) / 8, slots = 8 * device_sms();
+        err = launch_after(k_tops, dim3((unsigned)(warps < slots ? warps : slots)), dim3(256), stream, t);
+    }
     if (err != cudaSuccess) return err;
     static std::atomic<uint64_t> ready[2];
     a.items = plan.items[0], a.head = plan.head;
@@ -1099,14 +1140,15 @@ int ones_attention_backward(const ones_heads* dout, const ones_heads* q, const o
     plan.start = reinterpret_cast<int*>(ws + p.at_start), plan.head = reinterpret_cast<PlanHead*>(ws);
     for (int i = 0; i < 2; ++i)
         plan.prefix[i] = reinterpret_cast<int*>(ws + p.at_prefix[i]), plan.items[i] = reinterpret_cast<Item*>(ws + p.at_items[i]);
-    unsigned* const largest = reinterpret_cast<unsigned*>(ws + p.at_largest);
-    plan.zero = largest, plan.zeros = type == ONES_F16 ? 2 * k->heads : 0;
+    unsigned* const top = reinterpret_cast<unsigned*>(ws + p.at_top);
+    plan.zero = top, plan.zeros = type == ONES_F16 ? p.slots * 2 * k->heads : 0;
+    uint16_t *const row_top = reinterpret_cast<uint16_t*>(ws + p.at_row_top), *const v_top = reinterpret_cast<uint16_t*>(ws + p.at_v_top);
     float* const delta = reinterpret_cast<float*>(ws + p.at_delta);
     auto vectors = [](const ones_heads& h) { return Vectors{static_cast<const uint16_t*>(h.d_data), h.token, h.head}; };
     SurveyArgs d = {vectors(*dout), vectors(*out), vectors(*v)};
-    d.plan = plan.head, d.delta = delta, d.largest = largest, d.tokens = tokens, d.heads = q->heads, d.kv = k->heads, d.dim = dim;
+    d.plan = plan.head, d.delta = delta, d.row_top = row_top, d.v_top = v_top, d.tokens = tokens, d.heads = q->heads, d.kv = k->heads, d.dim = dim;
     d.wide = aligned(out->d_data, 16) && (out->heads <= 1 || out->head % 8 == 0) && (tokens <= 1 || out->token % 8 == 0);
-    const BackArgs a = {nullptr, nullptr, d_lse, delta, largest, heads_out(*dq, dim, tokens), heads_out(*dk, dim, tokens), heads_out(*dv, dim, tokens), tokens,
+    const BackArgs a = {nullptr, nullptr, d_lse, delta, row_top, top, heads_out(*dq, dim, tokens), heads_out(*dk, dim, tokens), heads_out(*dv, dim, tokens), tokens,
                         q->heads, k->heads, p.group, p.kt, dim, scale};
     const bool f16 = type == ONES_F16;
     cudaError_t err;

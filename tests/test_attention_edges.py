@@ -140,6 +140,8 @@ def check_gradients(q, k, v, dout, lengths, scale=None):
     got = dict(zip(("dq", "dk", "dv"), train.attention_backward(dout, q, k, v, out, lse, offsets, scale=scale)))
     for i in range(len(lengths)):
         rows = slice(int(offsets[i]), int(offsets[i + 1]))
+        if not lengths[i]:
+            continue
         for name, (want, bound) in gradients64(q[rows], k[rows], v[rows], dout[rows], scale or q.shape[-1] ** -0.5).items():
             close(got[name][rows], want, bound)
 
@@ -196,3 +198,30 @@ def test_attention_bfloat16_gradients_of_small_tokens(which):
     x = {name: randn(600, h, 128, seed=h + i) for i, (name, h) in enumerate((("q", 2), ("k", 1), ("v", 1), ("dout", 2)))}
     x[which][:100] *= 2.0 ** 14
     check_gradients(*(t.bfloat16() for t in x.values()), [600])
+
+
+@pytest.mark.parametrize("heads, kv, dim", [(4, 2, 64), (3, 3, 128), (5, 1, 77)])
+@pytest.mark.parametrize("which", ["v", "dout", "both"])
+def test_attention_float16_gradients_beside_larger_sequences(which, heads, kv, dim):
+    """A sequence whose dout or v is far smaller than its neighbours' has gradients as exact as by itself."""
+    lengths = [300, 1, 200, 0, 129, 70]
+    n = sum(lengths)
+    q, k, v, dout = (randn(n, h, dim, seed=h + i) for i, h in enumerate((heads, kv, kv, heads)))
+    small = slice(301, 501)
+    if which != "dout":
+        v *= 2.0 ** 7
+        v[small] *= 2.0 ** -14
+    if which != "v":
+        dout *= 2.0 ** 6
+        dout[small] *= 2.0 ** -12
+    check_gradients(*(t.half() for t in (q, k, v, dout)), lengths)
+
+
+@pytest.mark.parametrize("heads, kv", [(2, 1), (3, 3)])
+def test_attention_float16_dq_of_small_rows(heads, kv):
+    """dq of each row is as exact as its own dout allows."""
+    q, k, v, dout = (randn(600, h, 64, seed=h + i) for i, h in enumerate((heads, kv, kv, heads)))
+    dout *= 2.0 ** 8
+    dout[50:] *= 2.0 ** -13
+    dout[300:, -1] *= 2.0 ** -2
+    check_gradients(*(t.half() for t in (q, k, v, dout)), [600])
