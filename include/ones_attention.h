@@ -71,7 +71,8 @@ int ones_qk_norm_backward(const ones_heads* dq, const ones_heads* dk, const ones
  * 0 <= tokens < 2^30, 0 <= sequences <= 2^22, 1 <= dim <= ONES_ATTENTION_MAX_DIM, scale > 0 and finite; tiles of
  * queries (128 / (heads / kv) tokens of a sequence each, rounded down) times kv have to be below 2^31 (ONES_ERR_BAD_PARAM).
  *   d_workspace  at least ones_attention_workspace_bytes(tokens, sequences, heads, kv) bytes, 256-byte aligned.
- * Scores, their statistics and all sums are in 32 bits; the probabilities are rounded to `type` for the product with v. */
+ * Scores, their statistics and all sums are in 32 bits; the probabilities are rounded to `type` for the product with v (ONES_F16: in steps of
+ * 2^-31 of the row's largest at most). */
 #define ONES_ATTENTION_MAX_DIM 128
 size_t ones_attention_workspace_bytes(int32_t tokens, int32_t sequences, int32_t heads, int32_t kv);
 int ones_attention(const ones_heads* q, const ones_heads* k, const ones_heads* v, const int64_t* d_offsets,

@@ -7,7 +7,7 @@
 // the values. A thread owns a row: maxima and sums need no exchange. The maximum that a row subtracts follows the true one
 // only when that has grown by more than 2^8 (in the exponentials): the output is then rescaled in tensor memory, else not.
 // Probabilities are rounded to the tensors' type for their product with the values (half a step, 2^-8 or 2^-11 of each,
-// averaged by the sum over keys), and summed before that in 32 bits.
+// averaged by the sum over keys), and summed before that in 32 bits, each tile by itself.
 //
 // Measured: 16384 tokens in one sequence, 16 / 4 heads of 128: 907 us = 1.21 PFLOP/s (the card at its power limit, 1.6 to 1.77 GHz);
 // 12 documents of 64 to 3412 tokens, 16 / 4 heads of 128: 136 us for 129 GFLOP, which block ends last decides; 128 samples of
@@ -154,6 +154,10 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const PlanArgs a) {
 
 constexpr int kThreads = 384;  // two groups of softmax warps, then load, two that multiply, and one that clears
 constexpr float kGrow = 8.f;   // a row's maximum may grow by so much (log2 of the exponentials) before it is followed
+// float16: log2 of what all probabilities are multiplied with, so that the largest there can be, 2^8, becomes 2^15, which the type holds, and its
+// steps are 2^-31 of the row's largest. (Steps of 2^-24 lose what many keys can have a share of the row by: 131071 keys at 2^-25 each.)
+template <bool F16>
+constexpr float kRaise = F16 ? 7.f : 0.f;
 constexpr float kFar = 16384.f;  // up to here the rounding of a maximum (log2 of the exponentials) is below 2^-10, and common to its row
 
 struct ForwardArgs {
@@ -439,7 +443,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             mma_fence_before();
             __syncwarp();
             if (lane == 0) bar_arrive(acc_free + bar);
-            if (out.own) *lse = top * g.scale + log2_of(l) * kLn2;
+            if (out.own) *lse = top * g.scale + (log2_of(l) - kRaise<F16>) * kLn2;
             return true;
         };
         // of the row: its token in the tile and its head in the group; the tokens of the warp's first and last row
@@ -532,11 +536,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                                 s[x][i] = __float_as_uint(d.x), s[x][i + 1] = __float_as_uint(d.y);
                             }
                     }
-                    const Pair c2 = both(c), t2 = both(far ? 0.f : -shift);
+                    const Pair c2 = both(c), t2 = both(kRaise<F16> - (far ? 0.f : shift));
+                    Pair tile_sum = both(0.f);  // small probabilities add up before they meet the sum of the row
                     auto probability = [&](uint32_t lo, uint32_t hi) {
                         const float2 e = split(fma2(pair(__uint_as_float(lo), __uint_as_float(hi)), c2, t2));
                         const float a = exp2_of(e.x), b = exp2_of(e.y);
-                        sum = sum + pair(a, b);
+                        tile_sum = tile_sum + pair(a, b);
                         return pack16<F16>(a, b);
                     };
                     if (whole) {
@@ -562,6 +567,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             tmem_store(ts + 16 * x, p);
                         }
                     }
+                    sum = sum + tile_sum;
                     tmem_store_wait();
                     mma_fence_before();
                     __syncwarp();

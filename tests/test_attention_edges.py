@@ -225,3 +225,21 @@ def test_attention_float16_dq_of_small_rows(heads, kv):
     dout[50:] *= 2.0 ** -13
     dout[300:, -1] *= 2.0 ** -2
     check_gradients(*(t.half() for t in (q, k, v, dout)), [600])
+
+
+@pytest.mark.parametrize("gap", [17.0, 17.5, 18.5])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_attention_many_small_probabilities(gap, dtype):
+    """One key far above 131071 others that together have a share of the row: float16 keeps them in steps of 2^-31 of the largest."""
+    from paper_2108_03645_b200 import train
+    n = 1 << 17
+    q, k, v = torch.zeros(n, 1, 64, device="cuda"), torch.zeros(n, 1, 64, device="cuda"), torch.ones(n, 1, 64, device="cuda")
+    q[..., 0], k[0, 0, 0], v[0] = 1.0, gap, 0.0
+    out, lse = train.attention(*(t.to(dtype) for t in (q, k, v)), scale=1.0)
+    rest = torch.arange(n, device="cuda", dtype=torch.float64) * math.exp(-gap)
+    want, u = rest / (1 + rest), U[dtype]
+    # 32-bit sums: 64 probabilities of a tile one after the other, then n / 128 tiles; products with v in n / 16 steps, cut off
+    sums = (64 + n / 128) * 2.0 ** -24
+    close(lse[:, 0], gap + torch.log1p(rest), torch.full_like(rest, 2.0 ** -20 + 2.0 ** -22 * gap + sums))
+    bound = want * (2 * u + sums + n / 16 * 2.0 ** -23) + (2.0 ** -32 * n if dtype == F16 else 0.0) + TINY[dtype]
+    close(out[:, 0], want[:, None].expand(n, 64), bound[:, None].expand(n, 64))
