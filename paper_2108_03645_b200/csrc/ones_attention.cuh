@@ -49,6 +49,10 @@ struct PlanArgs {
     int lists;
 };
 
+// The first row of a tile of queries (token * group + head) that sees a key which lies `behind` tokens behind the tile's first token; far keys
+// count as 256 tokens away, where a tile is seen whole or not at all: 2^30 tokens times a group of 128 do not fit 32 bits.
+__host__ __device__ inline int first_row(int behind, int group) { return (behind < -256 ? -256 : behind > 256 ? 256 : behind) * group; }
+
 inline int64_t items_at_most(int64_t tokens, int64_t sequences, int64_t step) {
     return tokens / step + (sequences < tokens ? sequences : tokens) + 2;
 }

@@ -934,7 +934,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const Stat step(t);
                 const int first = q.first + i * g.kt;  // token of the tile's first row
                 // the first column of this half that sees this key, the warp's first and its last key
-                const int from = (token - first) * g.group - 64 * half, low = from - lane * g.group, high = low + 31 * g.group;
+                const int low = first_row(token - lane - first, g.group) - 64 * half, from = low + lane * g.group, high = low + 31 * g.group;
                 const float* const st = stats + step.at * 2 * kRows + 64 * half;
                 if (!(ok = warp_wait(st_full + 8 * step.at, step.parity, &sh.loads))) break;
                 if (!(ok = warp_wait(s_full, t & 1, &sh.loads))) break;
@@ -1111,6 +1111,8 @@ const WaitControl attention_back_waits = {take_expired, limit_waits, wait_for_no
 }  // namespace ones
 
 extern "C" {
+
+int ones_attention_first_row(int behind, int group) { return ones::first_row(behind, group); }
 
 size_t ones_attention_backward_workspace_bytes(int32_t tokens, int32_t sequences, int32_t heads, int32_t kv, int32_t dim) {
     if (ones::bad_counts(tokens, sequences, heads, kv) || dim < 1 || dim > ONES_ATTENTION_MAX_DIM) return 0;

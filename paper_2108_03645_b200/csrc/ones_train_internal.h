@@ -45,3 +45,5 @@ cudaError_t launch_after(void (*kernel)(P...), dim3 grid, dim3 block, cudaStream
 // of the five files (0 to 4) that waits `times` times for what never comes.
 extern "C" int ones_train_wait_limit(unsigned long long ns);
 extern "C" int ones_train_wait_for_nothing(int which, int times, void* cuda_stream);
+// The row of a tile of queries from which on a key is seen, as the attention's kernels have it.
+extern "C" int ones_attention_first_row(int behind, int group);
