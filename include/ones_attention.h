@@ -33,7 +33,7 @@ typedef struct ones_heads {
  *   formed and reduced to one turn in 64 bits.
  *   d_q_weight, d_k_weight  [dim] of `wtype`, each NULL for 1.
  * 0 <= tokens < 2^31, 1 <= dim <= ONES_QK_NORM_MAX_DIM, rotary even, 0 <= rotary <= dim, heads <= ONES_MAX_HEADS, eps >= 0.
- * wtype is ONES_F32 or `type`.  Sums are in 32 bits. */
+ * wtype is ONES_F32 or `type`.  Sums are in 32 bits, of values times a power of two where their squares leave that range. */
 #define ONES_QK_NORM_MAX_DIM 256
 #define ONES_MAX_HEADS 1024
 int ones_qk_norm(const ones_heads* q, const ones_heads* k, const int64_t* d_positions, const double* d_frequencies,

@@ -203,11 +203,10 @@ __device__ __forceinline__ float group_sum(float v, int lanes) {
         if (m < lanes) v += __shfl_xor_sync(0xFFFFFFFFu, v, m);
     return v;
 }
-__device__ __forceinline__ float inverse_root(float ss, const Args& g) {
-    const float v = fmaf(ss, g.per_dim, g.eps), r = rsqrtf(v);
+__device__ __forceinline__ float inverse_root(float v) {
+    const float r = rsqrtf(v);
     return r * fmaf(-0.5f * v * r, r, 1.5f);  // a Newton step: to the last place or two
 }
-
 constexpr int kWeightRow = ONES_QK_NORM_MAX_DIM + 16;
 
 // Pieces of vectors on their way into shared memory. Each thread has slots of its own, so that nothing but its own copies is
@@ -353,7 +352,24 @@ __global__ void __launch_bounds__(kThreads, BACK ? 2 : 5) k_qk_norm(const __grid
                         if (BACK) w[u][i] = y[u][i] * w[u][i], gx = fma2(w[u][i], x[u][i], gx);
                     }
                 }
-                const float f = inverse_root(group_sum(total(ss), lanes), g);
+                const float v = fmaf(group_sum(total(ss), lanes), g.per_dim, g.eps);
+                float f = inverse_root(v), mean = BACK ? f * group_sum(total(gx), lanes) * g.per_dim : 0.f;  // of n = x r times the gradient
+                // sums that leave the range of 32 bits, or come near: again, of x times a power of two
+                const bool far = !(v > 0x1p-60f && v < 0x1p100f);
+                if (__any_sync(0xFFFFFFFFu, far)) {
+                    const float unit = v < 1.f ? 0x1p80f : 0x1p-100f;
+                    ss = gx = both(0.f);
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+#pragma unroll
+                        for (int i = 0; i < V; ++i) {
+                            const Pair z = x[u][i] * both(unit);
+                            ss = fma2(z, z, ss);
+                            if (BACK) gx = fma2(w[u][i], z, gx);
+                        }
+                    const float r = rsqrtf(fmaf(group_sum(total(ss), lanes), g.per_dim, g.eps * unit * unit)), c = BACK ? group_sum(total(gx), lanes) : 0.f;
+                    if (far) f = r * unit, mean = r * c * g.per_dim;
+                }
                 if (!BACK) {
                     const Pair f2 = both(f);
 #pragma unroll
@@ -365,15 +381,15 @@ __global__ void __launch_bounds__(kThreads, BACK ? 2 : 5) k_qk_norm(const __grid
                         if (live) Row<T, V>::store(q, unit[u], g.dim, x[u]);
                     }
                 } else {
-                    const float back = f * f * (group_sum(total(gx), lanes) * g.per_dim);
-                    const Pair fb = both(-f * back), fx = both(f);
+                    const Pair m2 = both(-mean), f2 = both(f);
                     if (live) {
 #pragma unroll
                         for (int u = 0; u < U; ++u) {
 #pragma unroll
                             for (int i = 0; i < V; ++i) {
-                                dw[BACK ? which : 0][u][i] = fma2(y[u][i], x[u][i] * fx, dw[BACK ? which : 0][u][i]);
-                                x[u][i] = fma2(x[u][i], fb, fx * w[u][i]);
+                                const Pair n = x[u][i] * f2;
+                                dw[BACK ? which : 0][u][i] = fma2(y[u][i], n, dw[BACK ? which : 0][u][i]);
+                                x[u][i] = fma2(n, m2, w[u][i]) * f2;
                             }
                             Row<T, V>::store(q, unit[u], g.dim, x[u]);
                         }

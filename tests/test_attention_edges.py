@@ -243,3 +243,20 @@ def test_attention_many_small_probabilities(gap, dtype):
     close(lse[:, 0], gap + torch.log1p(rest), torch.full_like(rest, 2.0 ** -20 + 2.0 ** -22 * gap + sums))
     bound = want * (2 * u + sums + n / 16 * 2.0 ** -23) + (2.0 ** -32 * n if dtype == F16 else 0.0) + TINY[dtype]
     close(out[:, 0], want[:, None].expand(n, 64), bound[:, None].expand(n, 64))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("dim, rotary, interleaved", [(64, 64, False), (128, 64, True), (81, 40, False)])
+@pytest.mark.parametrize("size, eps", [(1e20, 1e-6), (1e30, 0.0), (3e37, 1e-6), (1e-25, 0.0), (1e-30, 1e-36)])
+def test_qk_norm_squares_that_32_bits_do_not_hold(size, eps, dim, rotary, interleaved, dtype):
+    """Vectors whose squares overflow or vanish, beside ordinary ones."""
+    from test_attention_ops import check_qk_norm
+    from paper_2108_03645_b200 import train
+    q, k = randn(21, 3, dim), randn(21, 2, dim, seed=1)
+    q[::2] *= size
+    k[1::2, 1] *= size
+    w = 1 + 0.2 * randn(dim, seed=3)
+    f = 1e-3 / max(1.0, 1 / size)  # what is divided by the vectors' size stays in range
+    dq, dk = f * randn(21, 3, dim, seed=5), f * randn(21, 2, dim, seed=6)
+    check_qk_norm(*(t.to(dtype) for t in (q, k)), torch.arange(21, device="cuda") * 3, train.rotary_frequencies(rotary), w, w, dq.to(dtype), dk.to(dtype),
+                  eps=eps, interleaved=interleaved)
