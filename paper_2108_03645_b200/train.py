@@ -286,7 +286,10 @@ def linear_cross_entropy_autograd(hidden, weight, target) -> torch.Tensor:
 
 
 def qk_norm_autograd(q, k, positions, frequencies, q_weight=None, k_weight=None, *, eps: float = 1e-6, interleaved: bool = False):
-    """`qk_norm` as a (once) differentiable function of q, k and the weights: (q, k)."""
+    """`qk_norm` as a (once) differentiable function of q, k and the weights: (q, k). Frequencies that require a gradient are refused: they
+    get none."""
+    if frequencies.requires_grad and torch.is_grad_enabled():
+        raise ValueError("frequencies require a gradient, but qk_norm_autograd has none for them: detach them, or call it under torch.no_grad()")
     return _QkNorm.apply(q, k, positions, frequencies, q_weight, k_weight, eps, interleaved)
 
 

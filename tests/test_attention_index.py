@@ -1,4 +1,4 @@
-"""Index arithmetic of the attention at the ends of its range, without a device."""
+"""What the attention layer's operators do at the ends of their range, without a device: index arithmetic, gradients that there are none of."""
 import pytest
 
 
@@ -13,3 +13,16 @@ def test_rows_that_see_a_key_far_away(group):
             got, exact = first_row(behind, group) + lane * group, (behind + lane) * group
             for row in (0, 1, 31, 32, 63, 64, 96, 127):
                 assert (row >= got) == (row >= exact), (behind, lane, row)
+
+
+def test_gradients_of_frequencies_are_refused():
+    """There are none, and whoever asks is told so, before any launch."""
+    torch = pytest.importorskip("torch")
+    from paper_2108_03645_b200 import train
+    q, k = torch.zeros(4, 2, 64), torch.zeros(4, 1, 64)
+    freq = train.rotary_frequencies(64, device="cpu").requires_grad_()
+    for x in (q, q.clone().requires_grad_()):
+        with pytest.raises(ValueError, match="frequencies"):
+            train.qk_norm_autograd(x, k, torch.arange(4), freq)
+    with torch.no_grad(), pytest.raises(ValueError, match="CUDA"):
+        train.qk_norm_autograd(q, k, torch.arange(4), freq)
