@@ -38,14 +38,15 @@ class JobShape:
     ignored: float = 0.1    # share of tokens without a target
     heads: int = 0          # query heads of the attention (0: a block without one)
     kv_heads: int = 0       # key and value heads, a divisor of heads (0: as many)
-    clip: float = 0.0       # largest norm of all gradients together (0: as they are)
+    clip: float = 0.0       # largest norm of all gradients together, finite (0: as they are)
 
     def __post_init__(self):
         kv = self.kv_heads or self.heads
-        if self.heads < 0 or kv < 0 or (self.heads and (self.width % self.heads or self.heads % kv or self.width // self.heads > 128)):
-            raise ValueError("JobShape: heads have to divide the width into parts of at most 128, and kv_heads the heads")
-        if not self.clip >= 0.0:
-            raise ValueError("JobShape: clip is a norm, or 0")
+        if self.heads < 0 or kv < 0 or (self.heads and (self.width % self.heads or self.heads % kv or
+                                                     self.width // self.heads > 128 or self.heads // kv > 128 or self.heads > 1024)):
+            raise ValueError("JobShape: at most 1024 heads have to divide the width into parts of at most 128, and kv_heads the heads into groups of at most 128")
+        if not 0.0 <= self.clip < math.inf:
+            raise ValueError("JobShape: clip is a finite norm, or 0")
 
 
 def fit(batches, seconds) -> tuple[float, float]:

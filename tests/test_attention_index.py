@@ -26,3 +26,12 @@ def test_gradients_of_frequencies_are_refused():
             train.qk_norm_autograd(x, k, torch.arange(4), freq)
     with torch.no_grad(), pytest.raises(ValueError, match="CUDA"):
         train.qk_norm_autograd(q, k, torch.arange(4), freq)
+
+
+def test_job_shapes_that_no_step_takes_are_refused():
+    """What the operators refuse is no shape of a job: it fails when it is made, not at its first step."""
+    from paper_2108_03645_b200 import profile_job as pj
+    for bad in (dict(clip=float("inf")), dict(width=4096, heads=256, kv_heads=1), dict(width=4096, heads=2048)):
+        with pytest.raises(ValueError):
+            pj.JobShape(**bad)
+    assert pj.JobShape(width=4096, heads=128, kv_heads=1, clip=1e30).heads == 128
