@@ -67,7 +67,7 @@ int ones_qk_norm_backward(const ones_heads* dq, const ones_heads* dk, const ones
  *   scores count as products with 0, as in a plain matrix product.
  *   d_lse float[tokens][heads].
  * Scores are in 32 bits before the factor: what does not fit is an infinity. Keys that score -infinity have no part in their row; a
- * row whose keys all do has lse = -infinity and out = NaN.
+ * row whose keys all do has lse = -infinity and out = NaN (and its gradients, and those of its keys, are NaN).
  * 0 <= tokens < 2^30, 0 <= sequences <= 2^22, 1 <= dim <= ONES_ATTENTION_MAX_DIM, scale > 0 and finite; tiles of
  * queries (128 / (heads / kv) tokens of a sequence each, rounded down) times kv have to be below 2^31 (ONES_ERR_BAD_PARAM).
  *   d_workspace  at least ones_attention_workspace_bytes(tokens, sequences, heads, kv) bytes, 256-byte aligned.

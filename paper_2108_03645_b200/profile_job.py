@@ -42,8 +42,8 @@ class JobShape:
 
     def __post_init__(self):
         kv = self.kv_heads or self.heads
-        if self.heads < 0 or kv < 0 or (self.heads and (self.width % self.heads or self.heads % kv or
-                                                     self.width // self.heads > 128 or self.heads // kv > 128 or self.heads > 1024)):
+        if self.heads < 0 or kv < 0 or (self.heads and (self.width % self.heads or self.heads % kv or self.width // self.heads > 128 or
+                                                        self.heads // kv > 128 or self.heads > 1024)):
             raise ValueError("JobShape: at most 1024 heads have to divide the width into parts of at most 128, and kv_heads the heads into groups of at most 128")
         if not 0.0 <= self.clip < math.inf:
             raise ValueError("JobShape: clip is a finite norm, or 0")

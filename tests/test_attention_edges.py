@@ -260,3 +260,41 @@ def test_qk_norm_squares_that_32_bits_do_not_hold(size, eps, dim, rotary, interl
     dq, dk = f * randn(21, 3, dim, seed=5), f * randn(21, 2, dim, seed=6)
     check_qk_norm(*(t.to(dtype) for t in (q, k)), torch.arange(21, device="cuda") * 3, train.rotary_frequencies(rotary), w, w, dq.to(dtype), dk.to(dtype),
                   eps=eps, interleaved=interleaved)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_attention_gradients_do_not_depend_on_other_sequences(dtype):
+    """The bits of a sequence's results, whatever its neighbours hold: large values, small ones, infinities, NaN."""
+    from paper_2108_03645_b200 import train
+    lengths = [70, 5, 200, 131]
+    offsets = torch.tensor([0] + lengths).cumsum(0).cuda()
+    for heads, kv, dim in ((4, 2, 128), (3, 1, 64), (5, 1, 77)):
+        plain = [randn(sum(lengths), h, dim, seed=i).to(dtype) for i, h in enumerate((heads, kv, kv, heads))]
+
+        def step(q, k, v, dout):
+            out, lse = train.attention(q, k, v, offsets)
+            return [out, lse, *train.attention_backward(dout, q, k, v, out, lse, offsets)]
+        want = step(*plain)
+        for factor in (100.0, 1e-3, math.inf, math.nan):
+            args = [t.clone() for t in plain]
+            for t in args:
+                t[75:275] *= factor
+            keep = torch.ones(sum(lengths), dtype=torch.bool, device="cuda")
+            keep[75:275] = False
+            for a, b in zip(step(*args), want):
+                assert torch.equal(a[keep], b[keep]), factor
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_attention_many_empty_sequences(dtype):
+    """Far more sequences than tokens: the same bits as without those that are empty."""
+    from paper_2108_03645_b200 import train
+    q, k, v, dout = (randn(450, h, 64, seed=i).to(dtype) for i, h in enumerate((4, 2, 2, 4)))
+    few = torch.tensor([0, 1, 300, 430], device="cuda")
+    many = few.repeat_interleave(2000)
+    results = []
+    for offsets in (few, many):
+        out, lse = train.attention(q, k, v, offsets)
+        results.append([out, lse, *train.attention_backward(dout, q, k, v, out, lse, offsets)])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)

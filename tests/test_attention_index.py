@@ -35,3 +35,11 @@ def test_job_shapes_that_no_step_takes_are_refused():
         with pytest.raises(ValueError):
             pj.JobShape(**bad)
     assert pj.JobShape(width=4096, heads=128, kv_heads=1, clip=1e30).heads == 128
+
+
+def test_backward_workspace_holds_no_copy_of_the_inputs():
+    """A few bytes for each row of each head, whatever the type, however long the vectors are."""
+    from paper_2108_03645_b200 import train
+    need = train.lib().ones_attention_backward_workspace_bytes
+    tokens, heads = 65536, 32
+    assert 4 * tokens * heads < need(tokens, 8, heads, heads, 128) < 9 * tokens * heads
