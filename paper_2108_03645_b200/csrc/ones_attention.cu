@@ -9,9 +9,9 @@
 // Probabilities are rounded to the tensors' type for their product with the values (half a step, 2^-8 or 2^-11 of each,
 // averaged by the sum over keys), and summed before that in 32 bits, each tile by itself.
 //
-// Measured: 16384 tokens in one sequence, 16 / 4 heads of 128: 907 us = 1.21 PFLOP/s (the card at its power limit, 1.6 to 1.77 GHz);
-// 12 documents of 64 to 3412 tokens, 16 / 4 heads of 128: 136 us for 129 GFLOP, which block ends last decides; 128 samples of
-// 256 tokens, 16 heads of 64: 69 us, bound by the latency of an item's first tile. What did not help: probabilities handed on in
+// Measured: 16384 tokens in one sequence, 16 / 4 heads of 128: 932 us by itself and 982 in a row = 1.12 PFLOP/s (the card at its power limit,
+// 1.6 to 1.77 GHz); 12 documents of 64 to 3412 tokens, 16 / 4 heads of 128: 137 us for 129 GFLOP, which block ends last decides; 128 samples of
+// 256 tokens, 16 heads of 64: 73 us, bound by the latency of an item's first tile. What did not help: probabilities handed on in
 // two halves (893 -> 955 us), softmax loops that are not unrolled (967 -> 1159), items taken from a counter by whoever is free
 // (documents 136 -> 133 us, but 16384 tokens forward and backward 4182 -> 4631: neighbours no longer work on the same keys).
 #include "ones_attention.cuh"

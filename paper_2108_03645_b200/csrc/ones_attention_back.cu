@@ -6,8 +6,8 @@
 // if dq were added up in memory: but that takes 64 KB of atomic additions for every pair of tiles, whose order would change
 // the results, or turns taken between blocks. A pair costs 2 x 2048 cycles of products (see below for the eighth) and 2 x 1024 of
 // exponentials. Measured: 16384 tokens, 16 / 4 heads of 128: 1740 us for the queries and 1690 for the keys, 1.27 and 1.30 PFLOP/s of what they
-// execute (the card at its power limit, 1.6 to 1.77 GHz). 128 samples of 256 tokens, 16 heads of 64: survey 90 us (0.47 GB in
-// and out at 5.2 TB/s), queries 102, keys 102: the warps that work on scores never wait for the tensor core there, a third of their
+// execute (the card at its power limit, 1.6 to 1.77 GHz). 128 samples of 256 tokens, 16 heads of 64: survey 25 us (0.14 GB in
+// and out at 5.4 TB/s), queries 110, keys 101: the warps that work on scores never wait for the tensor core there, a third of their
 // time goes to the way out of the sums and to what begins and ends an item.
 //
 // What the rounding to 16 bits costs. Probabilities and the gradients of the scores (ds) are rounded to the tensors' type for their
@@ -15,7 +15,7 @@
 // result: dq 1.66e-3 (one tile of keys) to 2.03e-3 (4096 tokens), dk 2.35e-3, dv 2.3e-3. bfloat16 has the range for whatever ds and its operands hold; float16 takes ds times a power of two. (bfloat16 queries
 // and keys laid out as float16 times a power of two for each head left 11 bits of ds, but nothing of a sequence far below its
 // neighbours, or beside keys that hold the type's lowest value.) And delta = dout . out takes over the rounding of
-// out: an error e that all pairs of a row share, and that adds e sum_j p_j k_j to its dq (with values that have a common mean, 3e-2 of
+// out: an error e that all pairs of a row share, and that adds e sum_j p_j k_j to its dq (with values that have a common mean, percents of
 // its norm). The sum of a row's ds has to be 0, so the pass over the queries finds e: it adds up p k beside ds k, one product more,
 // takes e times that off, and leaves the exact delta for the second pass. The last tile of a row, where e is known, needs no
 // such product: its ds are formed with the exact delta at once.

@@ -220,7 +220,7 @@ __device__ __forceinline__ void copy_async(const uint4* to, const void* from) {
 // U units per lane: 1 where pieces of 16 bytes are possible, more for single values. Forward, the next vector of a group is on its
 // way while the present one is worked on, and five blocks on an SM hide the rest (through shared memory, whose reads it is bound
 // by, 240 -> 269 us for 65536 x 40 x 128). Backward, the sums for the weights leave room for two blocks, and three vectors of each
-// group are on their way, through shared memory (one, in registers: 517 us, so 385).
+// group are on their way, through shared memory (one, in registers: 517 us, so 387 to 420).
 template <class T, int V, int U, bool INTER, bool BACK>
 __global__ void __launch_bounds__(kThreads, BACK ? 2 : 5) k_qk_norm(const __grid_constant__ Args g) {
     constexpr bool kRing = BACK && V > 1;
