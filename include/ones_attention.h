@@ -87,8 +87,8 @@ int ones_attention(const ones_heads* q, const ones_heads* k, const ones_heads* v
  *   d_workspace  at least ones_attention_backward_workspace_bytes(tokens, sequences, heads, kv, dim) bytes.
  * p and ds are rounded to `type` for their products, ONES_F16 times a power of two (p 2^12, ds what follows from the largest |dout| of its
  * row for dq, of the sequence and group of heads for dk, and the largest |v| of these): ds keeps 11 bits down to 2^-21 of their product, and
- * steps of 2^-31 of it below.  A row whose |lse| is
- * 2^24 or more and finite, which has only seen keys that a mask's lowest value hides, has p = 0. */
+ * steps of 2^-31 of it below.  A row whose |lse| is 2^24 or more and finite, which has only seen keys that a mask's lowest value
+ * hides, has p = 0. */
 size_t ones_attention_backward_workspace_bytes(int32_t tokens, int32_t sequences, int32_t heads, int32_t kv, int32_t dim);
 int ones_attention_backward(const ones_heads* dout, const ones_heads* q, const ones_heads* k, const ones_heads* v,
                             const ones_heads* out, const float* d_lse, const int64_t* d_offsets, int32_t tokens,

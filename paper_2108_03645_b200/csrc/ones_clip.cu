@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(kThreads) k_norm(const double* part, int parts
 }
 
 template <class T>
-__device__ __forceinline__ void scale(const Piece& p, void* out, float f) {
+__device__ __forceinline__ void scale(const Piece& p, void* out, float f, float before) {
     constexpr int V = 16 / sizeof(T);
     uint8_t* o = static_cast<uint8_t*>(out) - p.head;
     const bool wide = reinterpret_cast<uintptr_t>(o) % 16 == 0;
@@ -192,7 +192,7 @@ __device__ __forceinline__ void scale(const Piece& p, void* out, float f) {
         float x[V];
         values<T>(raw[i], x);
 #pragma unroll
-        for (int j = 0; j < V; ++j) x[j] *= f;
+        for (int j = 0; j < V; ++j) x[j] = x[j] * before * f;
         const uint4 r = packed<T>(x);
         if (wide && at >= p.head && at + 16 <= p.end) {
             *reinterpret_cast<uint4*>(o + at) = r;
@@ -215,14 +215,15 @@ __global__ void __launch_bounds__(kThreads) k_scale(const __grid_constant__ Tabl
     const double n = norm_of(part, parts);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
     const double f = max_norm / (n + eps);
-    const float factor = f >= 1.0 || n == 0.0 ? 1.f : (float)f;
+    // a factor that 32 bits hold no more, of gradients near the end of their range: in two steps
+    const float before = f < 0x1p-100 ? 0x1p-64f : 1.f, factor = f >= 1.0 || n == 0.0 ? 1.f : (float)(f < 0x1p-100 ? f * 0x1p64 : f);
     for (int c = t.chunks - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
         const Piece p = piece_at(t, c);
         if (factor == 1.f && t.in[p.tensor] == t.out[p.tensor]) continue;
         const int type = t.type[p.tensor];
         void* out = t.out[p.tensor];
-        type == ONES_F32 ? scale<float>(p, out, factor)
-                         : type == ONES_BF16 ? scale<__nv_bfloat16>(p, out, factor) : scale<__half>(p, out, factor);
+        type == ONES_F32 ? scale<float>(p, out, factor, before)
+                         : type == ONES_BF16 ? scale<__nv_bfloat16>(p, out, factor, before) : scale<__half>(p, out, factor, before);
     }
 }
 

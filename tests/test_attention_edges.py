@@ -298,3 +298,14 @@ def test_attention_many_empty_sequences(dtype):
         results.append([out, lse, *train.attention_backward(dout, q, k, v, out, lse, offsets)])
     for a, b in zip(*results):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("limit", [1e-4, 1.0, 1e20])
+def test_clip_factors_that_32_bits_do_not_hold(limit, dtype):
+    """Gradients near the end of their range, scaled to a small norm."""
+    from paper_2108_03645_b200 import train
+    g = (randn(5000) * 5e37).to(dtype)
+    want = g.double() * (limit / (float(g.double().norm()) + 1e-6))
+    train.clip_gradients([g], limit)
+    close(g, want, (U[dtype] + 2.0 ** -21) * want.abs() + TINY[dtype])
