@@ -5,7 +5,8 @@
 // tensor core multiplies for one, its softmax warps work on the other. Scores and outputs stay in tensor memory (4 x 128
 // columns), the probabilities take the place of their scores there as 16 bits and are the left operand of the product with
 // the values. A thread owns a row: maxima and sums need no exchange. The maximum that a row subtracts follows the true one
-// only when that has grown by more than 2^8 (in the exponentials): the output is then rescaled in tensor memory, else not.
+// only when that has grown by more than 2^8 (in the exponentials; a known way of rescaling seldom): the output is then rescaled in
+// tensor memory, else not.
 // Probabilities are rounded to the tensors' type for their product with the values (half a step, 2^-8 or 2^-11 of each,
 // averaged by the sum over keys), and summed before that in 32 bits, each tile by itself.
 //
